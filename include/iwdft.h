@@ -324,6 +324,70 @@ int iwdft_select_bins(const float* delta, int32_t n_layers, int32_t n_chunks, in
 int iwdft_ablate_chunk(const void* d_x, void* d_out, int64_t n_slices, int64_t M, int32_t head_dim,
                        int32_t kv_dtype, int32_t n_chunks, int32_t chunk, void* hip_stream);
 
+/* ---- The 8-bit paged cache: exact tokens of requests that are not (yet) in the frequency domain ----
+ *
+ * A pool of pages of P = page_tokens tokens each serves sequences of any lengths.  Everything is the caller's device memory, and the calls need no
+ * context; they enqueue kernels on hip_stream and never synchronise, allocate or clear memory.  The device that is current has to own all of it.
+ *   values     uint8 [n_layers][n_pages][n_kv_heads][2][P * 128]: OCP e4m3, K (first) as [token][channel], V as [token / 8][channel][token % 8].
+ *   exponents  int32 [n_layers][n_pages][n_kv_heads][2]: a stored v stands for v * 2^e.  e is the smallest exponent >= -100 for which the largest finite
+ *              value that entered the page (head, tensor) since its first token is at most 448 * 2^e.  Where it grows, the page's older
+ *              values are rounded once more, to nearest even as everywhere; infinities are stored as +-448, NaN as NaN.
+ *   table      int32 [batch][max_pages]: pages of a sequence, in order.  Entries outside [0, n_pages) hold no tokens.
+ *   lens       int32 [batch]: tokens of a sequence.
+ *   free       int32 [1 + n_pages]: a count, then the free pages as a stack, its top at the count; at first n_pages, 0, 1, 2, ...
+ *   starts     int32 [batch + 1]: new tokens of sequence b are rows starts[b] .. starts[b + 1] of k, v, q; they are its last tokens.
+ *   slots      int32 [n_tokens]: where each new token goes, page * P + place in the page; -1: nowhere.
+ * A page belongs to one sequence.  Lengths, table entries, starts and slots that do not fit are cut or left out; no call reads or writes outside of its arrays. */
+typedef struct {
+  int32_t n_layers;
+  int32_t n_pages;            /* n_pages * page_tokens < 2^31                                       */
+  int32_t n_kv_heads;
+  int32_t n_q_heads;          /* multiple of n_kv_heads; query head hq reads KV head hq / (n_q_heads / n_kv_heads) */
+  int32_t head_dim;           /* this build: 128                                    */
+  int32_t page_tokens;        /* this build: 16, 32, 64 or 128                      */
+  int32_t max_pages;          /* pages a sequence may have (a row of the table); max_pages * page_tokens <= 2^30 */
+  int32_t kv_dtype;           /* of k, v, q, out, K, V: IWDFT_F32 or IWDFT_BF16     */
+} iwdft_pages_desc;
+
+/* Bytes of values (16-byte aligned) and exponents (8-byte aligned). */
+int iwdft_pages_query_bytes(const iwdft_pages_desc* desc, size_t* values_bytes, size_t* exponents_bytes);
+
+/* Block tables and slot maps of a step.  Sequence b is to have d_want[b] tokens (negative: as many as it has).  Shorter ones give their last pages back;
+ * longer ones take pages, those that this call gives back among them, in the order of b while pages and slots last.  A sequence whose pages or tokens,
+ * added to what those before it asked for, are more than there are (one that needs no page is held to the slots alone), or that would pass
+ * max_pages, stays as it is: d_lens tells.  Out: d_lens, d_table (the new entries; others stay), d_free, d_starts, d_slots (-1 behind the last new token).  Pages are given
+ * back in the reverse order of taking, so that a call which undoes another one leaves the stack as it was (draft tokens that are
+ * rejected).  batch >= 0, n_slots >= 0. */
+int iwdft_pages_resize(int32_t page_tokens, int32_t n_pages, int32_t max_pages, const int32_t* d_want, int32_t batch, int32_t* d_table, int32_t* d_lens,
+                       int32_t* d_free, int32_t* d_starts, int32_t* d_slots, int32_t n_slots, void* d_workspace, size_t workspace_bytes,
+                       void* hip_stream);
+/* Its workspace: 0 for up to 1024 sequences and 2048 slots. */
+int iwdft_pages_resize_bytes(int32_t batch, int32_t n_slots, size_t* workspace_bytes);
+
+/* New tokens into the pages of layers layer .. layer + n_layers - 1.  d_k, d_v: [n_layers][n_tokens][n_kv_heads][head_dim], kv_dtype.  A page's new tokens
+ * stand behind each other in d_slots, in order (rows without a slot may lie between), and continue what the page holds: the page's tokens before the first
+ * new one are taken to be there, a page whose first slot is written starts afresh.  No slot may come twice. */
+int iwdft_pages_write(const iwdft_pages_desc* desc, int32_t layer, int32_t n_layers, const void* d_k, const void* d_v, const int32_t* d_slots, int32_t n_tokens,
+                      void* d_values, int32_t* d_exponents, void* hip_stream);
+
+/* Attention of the new tokens over their sequences (Eq. kv-attn over exact tokens), which hold them already: row t = starts[b] + i of q stands at position
+ * p = lens[b] - (starts[b + 1] - starts[b]) + i and sees the tokens j <= p, with n_recent > 0 those with j < n_sink or j > p - n_recent only (the windows of
+ * Sec. 4.2.1).  d_q, d_out: [n_layers][n_tokens][n_q_heads][head_dim], kv_dtype, not overlapping.  scale <= 0 selects 1/sqrt(head_dim).  A row without
+ * a token to see, or whose scores are all -infinity, is 0; rows from starts[batch] on stay as they are.  What a token holds that a row does not see, NaN too, does not reach the row.
+ * Prompts, drafts of a few tokens and single ones may be mixed.  Products run in fp16 on exact e4m3 values: bf16 queries are exact up to
+ * 2^-38 of their row's largest value, fp32 ones and their weights have 22 bits, the weights of bf16 calls 11; weights times the scale of V's page err by 2^-31
+ * (bf16; fp32 2^-40) of the largest such product whatever their size; sums are fp32. */
+int iwdft_pages_attn(const iwdft_pages_desc* desc, int32_t layer, int32_t n_layers, const void* d_q, const int32_t* d_starts, int32_t n_tokens,
+                     const int32_t* d_table, const int32_t* d_lens, int32_t batch, const void* d_values, const int32_t* d_exponents, void* d_out, int32_t n_sink,
+                     int32_t n_recent, float scale, void* d_workspace, size_t workspace_bytes, void* hip_stream);
+/* Its workspace (0: none), for calls on so many layers, sequences and rows.  Nothing in it outlives the call; calls that may overlap in time need one each. */
+int iwdft_pages_attn_bytes(const iwdft_pages_desc* desc, int32_t n_layers, int32_t batch, int32_t n_tokens, size_t* workspace_bytes);
+
+/* The first n_tokens tokens of every sequence as iwdft_prefill takes them: d_K, d_V [n_layers][batch][n_kv_heads][n_tokens][head_dim], kv_dtype, 0 where a
+ * sequence has fewer; either may be NULL. */
+int iwdft_pages_read(const iwdft_pages_desc* desc, int32_t layer, int32_t n_layers, const int32_t* d_table, const int32_t* d_lens, int32_t batch, int32_t n_tokens,
+                     const void* d_values, const int32_t* d_exponents, void* d_K, void* d_V, void* hip_stream);
+
 const char* iwdft_last_error(void); /* thread-local, static storage, never NULL */
 
 #ifdef __cplusplus

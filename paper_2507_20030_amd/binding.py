@@ -6,7 +6,9 @@ or a call fails, an exception is raised.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
+import functools
 import os
 from typing import Optional, Sequence
 
@@ -29,6 +31,7 @@ EXPORTED = [
     "iwdft_reconstruct", "iwdft_reconstruct_grid", "compressed_decode_attn", "iwdft_append_attn", "iwdft_export_coeffs", "iwdft_export_bins",
     "iwdft_num_tokens", "iwdft_set_num_tokens", "iwdft_last_error", "iwdft_phase_timing", "iwdft_phase_times", "iwdft_prefill_kind", "iwdft_attn_kind", "iwdft_attn_pipelined",
     "iwdft_select_bins", "iwdft_ablate_chunk", "iwdft_flush", "compressed_decode_attn_static", "iwdft_query_attn",
+    "iwdft_pages_query_bytes", "iwdft_pages_resize", "iwdft_pages_resize_bytes", "iwdft_pages_write", "iwdft_pages_attn", "iwdft_pages_attn_bytes", "iwdft_pages_read",
 ]
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libiwdft.so")
@@ -51,6 +54,10 @@ class iwdft_desc(ctypes.Structure):
         ("flags", ctypes.c_uint32), ("n_sink", ctypes.c_int32), ("n_recent", ctypes.c_int32),
         ("write_every", ctypes.c_uint32),
     ]
+
+
+class iwdft_pages_desc(ctypes.Structure):
+    _fields_ = [(name, ctypes.c_int32) for name in ("n_layers", "n_pages", "n_kv_heads", "n_q_heads", "head_dim", "page_tokens", "max_pages", "kv_dtype")]
 
 
 _lib = None
@@ -90,6 +97,14 @@ def load_library() -> ctypes.CDLL:
     lib.iwdft_phase_times.argtypes = [vp, ctypes.POINTER(ctypes.c_double), ctypes.POINTER(ctypes.c_int64)]
     lib.iwdft_export_coeffs.argtypes = [vp, i32, vp, vp, vp]
     lib.iwdft_export_bins.argtypes = [vp, i32, vp, vp]
+    pp = ctypes.POINTER(iwdft_pages_desc)
+    lib.iwdft_pages_query_bytes.argtypes = [pp, szp, szp]
+    lib.iwdft_pages_resize.argtypes = [i32, i32, i32, vp, i32, vp, vp, vp, vp, vp, i32, vp, ctypes.c_size_t, vp]
+    lib.iwdft_pages_resize_bytes.argtypes = [i32, i32, szp]
+    lib.iwdft_pages_write.argtypes = [pp, i32, i32, vp, vp, vp, i32, vp, vp, vp]
+    lib.iwdft_pages_attn.argtypes = [pp, i32, i32, vp, vp, i32, vp, vp, i32, vp, vp, vp, i32, i32, f32, vp, ctypes.c_size_t, vp]
+    lib.iwdft_pages_attn_bytes.argtypes = [pp, i32, i32, i32, szp]
+    lib.iwdft_pages_read.argtypes = [pp, i32, i32, vp, vp, i32, i32, vp, vp, vp, vp, vp]
     lib.iwdft_num_tokens.argtypes = [vp]
     lib.iwdft_num_tokens.restype = i64
     lib.iwdft_set_num_tokens.argtypes = [vp, i64]
@@ -349,3 +364,225 @@ class Cache:
         out = torch.empty(len(self.desc.bins[layer]), dtype=torch.int32, device=self.device)
         iwdft_export_bins(self.ctx, layer, out, stream)
         return out
+
+
+# ------------------------------------------------------------------------------------------------------------------ 8-bit pages
+# What include/iwdft.h says of the arrays; sizes come from the tensors' shapes:
+#   values uint8 [layers, pages, KV heads, 2, P * 128], exponents int32 [layers, pages, KV heads, 2], table int32 [batch, max_pages],
+#   lens int32 [batch], free int32 [1 + pages], starts int32 [batch + 1], slots int32 [tokens].
+@functools.lru_cache(maxsize=1024)
+def _pages_desc(n_layers, n_pages, n_kv_heads, n_q_heads, head_dim, page_tokens, max_pages, dtype):
+    return iwdft_pages_desc(n_layers, n_pages, n_kv_heads, n_q_heads, head_dim, page_tokens, max_pages, IWDFT_F32 if dtype == torch.float32 else IWDFT_BF16)
+
+
+def pages_desc(n_layers, n_pages, n_kv_heads, n_q_heads=None, head_dim=128, page_tokens=32, max_pages=1, dtype=torch.bfloat16) -> iwdft_pages_desc:
+    return _pages_desc(n_layers, n_pages, n_kv_heads, n_kv_heads if n_q_heads is None else n_q_heads, head_dim, page_tokens, max_pages, dtype)
+
+
+def _bytes_of(call, *args) -> int:
+    n = ctypes.c_size_t(0)
+    _check(call(*args, ctypes.byref(n)))
+    return n.value
+
+
+@functools.lru_cache(maxsize=1024)
+def _resize_bytes(batch, n_slots):
+    return _bytes_of(load_library().iwdft_pages_resize_bytes, batch, n_slots)
+
+
+@functools.lru_cache(maxsize=1024)
+def _attn_bytes(n_layers, batch, n_tokens, *desc):
+    return _bytes_of(load_library().iwdft_pages_attn_bytes, ctypes.byref(_pages_desc(*desc)), n_layers, batch, n_tokens)
+
+
+def iwdft_pages_query_bytes(desc: iwdft_pages_desc):
+    v, e = ctypes.c_size_t(0), ctypes.c_size_t(0)
+    _check(load_library().iwdft_pages_query_bytes(ctypes.byref(desc), ctypes.byref(v), ctypes.byref(e)))
+    return v.value, e.value
+
+
+def iwdft_pages_resize_bytes(batch: int, n_slots: int) -> int:
+    return _resize_bytes(batch, n_slots)
+
+
+def iwdft_pages_attn_bytes(desc: iwdft_pages_desc, n_layers: int, batch: int, n_tokens: int) -> int:
+    return _bytes_of(load_library().iwdft_pages_attn_bytes, ctypes.byref(desc), n_layers, batch, n_tokens)
+
+
+def _expect(name: str, t: torch.Tensor, dtype, shape, device) -> None:
+    """shape: None where any size will do."""
+    if t.dtype != dtype:
+        raise ValueError(f"{name} is {t.dtype}, not {dtype}")
+    if len(t.shape) != len(shape) or any(n is not None and n != m for n, m in zip(shape, t.shape)):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, not {tuple('any' if n is None else n for n in shape)}")
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, not on {device}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+
+
+def _pool_sizes(values: torch.Tensor, exponents: torch.Tensor):
+    """(layers, pages, KV heads, page tokens); the device is a GPU."""
+    if values.dim() != 5 or values.shape[3] != 2 or values.shape[4] % 128:
+        raise ValueError(f"values has shape {tuple(values.shape)}, not (layers, pages, heads, 2, 128 * page tokens)")
+    if not values.is_cuda:
+        raise ValueError("values must be device memory")
+    n_layers, n_pages, heads, _, row = values.shape
+    _expect("values", values, torch.uint8, values.shape, values.device)
+    _expect("exponents", exponents, torch.int32, (n_layers, n_pages, heads, 2), values.device)
+    return n_layers, n_pages, heads, row // 128
+
+
+def _kv_dtype(name: str, t: torch.Tensor):
+    if t.dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError(f"{name} is {t.dtype}, not float32 or bfloat16")
+    return t.dtype
+
+
+def _run_on(device: torch.device, stream, call, *args) -> None:
+    """The call with the tensors' device as the current one, on its current stream unless one is given."""
+    here = device.index == torch.cuda.current_device()
+    with contextlib.nullcontext() if here else torch.cuda.device(device):
+        _check(call(*args, _stream(stream)))
+
+
+def _on_stream(stream, device):
+    """Allocations and fills in the order of the call's stream."""
+    if stream is None:
+        return contextlib.nullcontext()
+    return torch.cuda.stream(stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream), device))
+
+
+def _scratch(n_bytes: int, device: torch.device, stream, workspace):
+    """The caller's workspace or memory of this call alone, kept until the call's stream is past it (it is allocated in that stream's order)."""
+    if workspace is None and n_bytes:
+        with _on_stream(stream, device):
+            workspace = torch.empty(n_bytes, dtype=torch.uint8, device=device)
+    elif workspace is not None and workspace.device != device:
+        raise ValueError(f"workspace is on {workspace.device}, not on {device}")
+    return _ptr(workspace), (workspace.numel() * workspace.element_size() if workspace is not None else 0)
+
+
+def iwdft_pages_resize(want, table, lens, free, starts, slots, page_tokens: int, stream=None, workspace=None) -> None:
+    """Brings the sequences to want[b] tokens (negative: as they are): table, lens, free, starts and slots are brought up to date."""
+    if table.dim() != 2 or not table.is_cuda:
+        raise ValueError(f"table must be a device tensor [batch, max_pages], not {tuple(table.shape)} on {table.device}")
+    batch, max_pages = table.shape
+    device = table.device
+    for name, t, shape in (("table", table, (batch, max_pages)), ("want", want, (batch,)), ("lens", lens, (batch,)), ("free", free, (None,)),
+                           ("starts", starts, (batch + 1,)), ("slots", slots, (None,))):
+        _expect(name, t, torch.int32, shape, device)
+    n_slots = slots.shape[0]
+    ws, ws_bytes = _scratch(_resize_bytes(batch, n_slots), device, stream, workspace)
+    _run_on(device, stream, load_library().iwdft_pages_resize, page_tokens, free.shape[0] - 1, max_pages, want.data_ptr(), batch, table.data_ptr(),
+            lens.data_ptr(), free.data_ptr(), starts.data_ptr(), slots.data_ptr(), n_slots, ws, ws_bytes)
+
+
+def iwdft_pages_write(values, exponents, k, v, slots, layer: int = 0, stream=None) -> None:
+    """k, v [layers written, tokens, KV heads, 128] into layers layer, layer + 1, ... at slots."""
+    n_layers, n_pages, heads, P = _pool_sizes(values, exponents)
+    dtype, device = _kv_dtype("k", k), values.device
+    _expect("slots", slots, torch.int32, (None,), device)
+    n = slots.shape[0]
+    _expect("k", k, dtype, (None, n, heads, 128), device)
+    _expect("v", v, dtype, k.shape, device)
+    if k.shape[0] == 0:
+        return
+    desc = _pages_desc(n_layers, n_pages, heads, heads, 128, P, 1, dtype)
+    _run_on(device, stream, load_library().iwdft_pages_write, ctypes.byref(desc), layer, k.shape[0], k.data_ptr(), v.data_ptr(), slots.data_ptr(), n,
+            values.data_ptr(), exponents.data_ptr())
+
+
+def iwdft_pages_attn(values, exponents, q, starts, table, lens, out, layer: int = 0, n_sink: int = 0, n_recent: int = 0, scale: float = 0.0, stream=None,
+                     workspace=None) -> None:
+    """q, out [layers, tokens, query heads, 128]: the new tokens' attention over their sequences in layers layer, layer + 1, ..."""
+    n_layers, n_pages, heads, P = _pool_sizes(values, exponents)
+    dtype, device = _kv_dtype("q", q), values.device
+    _expect("q", q, dtype, (None, None, None, 128), device)
+    _expect("out", out, dtype, q.shape, device)
+    _expect("table", table, torch.int32, (None, None), device)
+    batch, max_pages = table.shape
+    _expect("lens", lens, torch.int32, (batch,), device)
+    _expect("starts", starts, torch.int32, (batch + 1,), device)
+    if q.shape[0] == 0:
+        return
+    sizes = (n_layers, n_pages, heads, q.shape[2], 128, P, max_pages, dtype)
+    ws, ws_bytes = _scratch(_attn_bytes(q.shape[0], batch, q.shape[1], *sizes), device, stream, workspace)
+    _run_on(device, stream, load_library().iwdft_pages_attn, ctypes.byref(_pages_desc(*sizes)), layer, q.shape[0], q.data_ptr(), starts.data_ptr(), q.shape[1],
+            table.data_ptr(), lens.data_ptr(), batch, values.data_ptr(), exponents.data_ptr(), out.data_ptr(), n_sink, n_recent, scale, ws, ws_bytes)
+
+
+def iwdft_pages_read(values, exponents, table, lens, K, V, layer: int = 0, stream=None) -> None:
+    """K, V [layers, batch, KV heads, tokens, 128] (either may be None) from the first tokens of every sequence; 0 where it has fewer."""
+    n_layers, n_pages, heads, P = _pool_sizes(values, exponents)
+    device, some = values.device, K if K is not None else V
+    if some is None:
+        return
+    dtype = _kv_dtype("K or V", some)
+    _expect("table", table, torch.int32, (None, None), device)
+    batch, max_pages = table.shape
+    _expect("lens", lens, torch.int32, (batch,), device)
+    for name, t in (("K", K), ("V", V)):
+        if t is not None:
+            _expect(name, t, dtype, (some.shape[0], batch, heads, some.shape[3] if some.dim() == 5 else None, 128), device)
+    if some.shape[0] == 0:
+        return
+    desc = _pages_desc(n_layers, n_pages, heads, heads, 128, P, max_pages, dtype)
+    _run_on(device, stream, load_library().iwdft_pages_read, ctypes.byref(desc), layer, some.shape[0], table.data_ptr(), lens.data_ptr(), batch,
+            some.shape[3], values.data_ptr(), exponents.data_ptr(), _ptr(K), _ptr(V))
+
+
+class PagedCache:
+    """Owns the arrays of an 8-bit paged cache of up to max_batch sequences of max_tokens tokens; methods forward to the C calls.
+
+    A step: ``starts, slots = resize(want, n)``, and for each layer ``write(k, v, slots, layer)`` and ``attend(q, starts, layer)``; a sequence
+    that is to have 0 tokens gives its pages back.  ``compress`` hands what it holds to a frequency-domain cache."""
+
+    def __init__(self, n_layers, n_pages, n_kv_heads, n_q_heads, head_dim, dtype: torch.dtype, max_batch, max_tokens, page_tokens=32, device="cuda:0"):
+        if dtype not in (torch.float32, torch.bfloat16):
+            raise ValueError("dtype must be float32 or bfloat16")
+        self.dtype, self.device, self.page_tokens = dtype, torch.device(device), page_tokens
+        max_pages = -(-max_tokens // max(page_tokens, 1))
+        iwdft_pages_query_bytes(pages_desc(n_layers, n_pages, n_kv_heads, n_q_heads, head_dim, page_tokens, max_pages, dtype))  # checks the sizes
+        self.shape = (n_layers, n_kv_heads, n_q_heads, head_dim)
+        ints = dict(dtype=torch.int32, device=self.device)
+        self.values = torch.zeros((n_layers, n_pages, n_kv_heads, 2, page_tokens * head_dim), dtype=torch.uint8, device=self.device)
+        self.exponents = torch.zeros((n_layers, n_pages, n_kv_heads, 2), **ints)
+        self.table = torch.full((max_batch, max_pages), -1, **ints)
+        self.lens = torch.zeros(max_batch, **ints)
+        self.free = torch.cat([torch.tensor([n_pages], **ints), torch.arange(n_pages, **ints)])
+
+    def resize(self, want: torch.Tensor, n_slots: int, stream=None):
+        """want: int32 [max_batch] on the device.  Returns starts, slots; lens tells which sequences could not grow."""
+        with _on_stream(stream, self.device):
+            starts, slots = (torch.empty(n, dtype=torch.int32, device=self.device) for n in (self.lens.shape[0] + 1, n_slots))
+        iwdft_pages_resize(want, self.table, self.lens, self.free, starts, slots, self.page_tokens, stream)
+        return starts, slots
+
+    def write(self, k, v, slots, layer=0, stream=None):
+        iwdft_pages_write(self.values, self.exponents, k, v, slots, layer, stream)
+
+    def attend(self, q, starts, layer=0, out=None, n_sink=0, n_recent=0, scale=0.0, stream=None):
+        if out is None:
+            with _on_stream(stream, self.device):
+                out = torch.zeros_like(q)  # rows behind the last sequence
+        iwdft_pages_attn(self.values, self.exponents, q, starts, self.table, self.lens, out, layer, n_sink, n_recent, scale, stream)
+        return out
+
+    def read(self, n_tokens, stream=None):
+        """K, V of all layers, [layers, max_batch, KV heads, n_tokens, 128]."""
+        L, H, _, D = self.shape
+        with _on_stream(stream, self.device):
+            K, V = (torch.empty((L, self.lens.shape[0], H, n_tokens, D), dtype=self.dtype, device=self.device) for _ in range(2))
+        iwdft_pages_read(self.values, self.exponents, self.table, self.lens, K, V, 0, stream)
+        return K, V
+
+    def compress(self, cache: Cache, stream=None):
+        """The first S + M + R tokens of every sequence through iwdft_prefill into `cache`, which has to have this cache's layers, heads and dtype and a
+        batch of max_batch."""
+        L, H, G, D = self.shape
+        if cache.shape != (L, self.lens.shape[0], H, G, D) or cache.dtype != self.dtype or cache.device != self.device:
+            raise ValueError(f"cache holds {cache.shape} {cache.dtype} on {cache.device}, these pages {(L, self.lens.shape[0], H, G, D)} {self.dtype} on {self.device}")
+        d = cache.desc.c
+        K, V = self.read(d.n_sink + d.M + d.n_recent, stream)
+        cache.prefill(K, V, stream)

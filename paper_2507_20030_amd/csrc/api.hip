@@ -16,6 +16,7 @@
 #include "common.h"
 #include "fft_core.h"
 #include "fft_tab.h"
+#include "pages.h"
 #include "tables.h"
 
 using namespace iwdft;
@@ -627,6 +628,39 @@ int flush_pending(iwdft_ctx* c, hipStream_t st) {
   return IWDFT_OK;
 }
 
+// 8-bit pages.
+constexpr int64_t kMostRows = (int64_t)1 << 31;  // (token, head, layer) rows of a call: grids and 32-bit counts
+const char kPageAlignMsg[] = "values and token tensors must be 16-byte aligned, exponents 8-byte, int32 arrays 4-byte";
+template <class... T>
+bool unaligned(uintptr_t n, T... p) {
+  return ((((uintptr_t)p & (n - 1)) != 0) || ...);
+}
+int log2_of(int32_t x) {
+  int n = 0;
+  while ((1 << n) < x) ++n;
+  return n;
+}
+int check_page_size(int32_t page_tokens, int32_t n_pages, int32_t max_pages) {
+  if (page_tokens != 16 && page_tokens != 32 && page_tokens != 64 && page_tokens != 128)
+    return fail(IWDFT_ERR_UNSUPPORTED, "page_tokens = %d: this build handles 16, 32, 64 and 128", page_tokens);
+  if (n_pages <= 0 || (int64_t)n_pages * page_tokens > 0x7fffffff) return fail(IWDFT_ERR_ARG, "n_pages = %d out of range", n_pages);
+  if (max_pages <= 0 || (int64_t)max_pages * page_tokens > ((int64_t)1 << 30)) return fail(IWDFT_ERR_ARG, "max_pages = %d out of range", max_pages);
+  return IWDFT_OK;
+}
+int check_pages(const iwdft_pages_desc* d, int32_t layer, int32_t n_layers) {
+  if (!d) return fail(IWDFT_ERR_ARG, "desc is NULL");
+  if (d->n_layers <= 0 || d->n_kv_heads <= 0 || d->n_q_heads <= 0) return fail(IWDFT_ERR_ARG, "a dimension is not positive");
+  if (d->n_q_heads % d->n_kv_heads) return fail(IWDFT_ERR_ARG, "n_q_heads = %d is no multiple of n_kv_heads = %d", d->n_q_heads, d->n_kv_heads);
+  if (d->kv_dtype != IWDFT_F32 && d->kv_dtype != IWDFT_BF16) return fail(IWDFT_ERR_ARG, "bad kv_dtype %d", d->kv_dtype);
+  if (d->head_dim != kHeadDim) return fail(IWDFT_ERR_UNSUPPORTED, "head_dim %d: this build handles 128", d->head_dim);
+  if (layer < 0 || n_layers <= 0 || layer > d->n_layers - n_layers)
+    return fail(IWDFT_ERR_ARG, "layers %d .. %lld of %d", layer, (long long)layer + n_layers - 1, d->n_layers);
+  return check_page_size(d->page_tokens, d->n_pages, d->max_pages);
+}
+Pages pages_of(const iwdft_pages_desc& d, void* values, int32_t* exponents) {
+  return Pages{d.n_pages, d.n_kv_heads, d.n_q_heads / d.n_kv_heads, log2_of(d.page_tokens), d.max_pages, (uint8_t*)values, exponents};
+}
+
 }  // namespace
 
 extern "C" {
@@ -1119,6 +1153,101 @@ int iwdft_ablate_chunk(const void* d_x, void* d_out, int64_t n_slices, int64_t M
                                 (int)chunk_edge(chunk, M, n_chunks), (int)chunk_edge(chunk + 1, M, n_chunks),
                                 (hipStream_t)hip_stream),
                   "ablation launch");
+}
+
+// ---------------------------------------------------------------------------------------------- 8-bit pages
+
+int iwdft_pages_query_bytes(const iwdft_pages_desc* desc, size_t* values_bytes, size_t* exponents_bytes) {
+  if (!values_bytes || !exponents_bytes) return fail(IWDFT_ERR_ARG, "output pointer is NULL");
+  const int rc = check_pages(desc, 0, 1);
+  if (rc != IWDFT_OK) return rc;
+  const size_t heads = (size_t)desc->n_layers * (size_t)desc->n_pages * (size_t)desc->n_kv_heads;
+  *values_bytes = heads * 2 * (size_t)desc->page_tokens * kHeadDim;
+  *exponents_bytes = heads * 2 * sizeof(int32_t);
+  return IWDFT_OK;
+}
+
+int iwdft_pages_resize_bytes(int32_t batch, int32_t n_slots, size_t* workspace_bytes) {
+  if (!workspace_bytes) return fail(IWDFT_ERR_ARG, "output pointer is NULL");
+  if (batch < 0 || n_slots < 0) return fail(IWDFT_ERR_ARG, "batch = %d, n_slots = %d: negative", batch, n_slots);
+  *workspace_bytes = batch <= kResizeOneBatch && n_slots <= kResizeOneSlots ? 0 : sizeof(int32_t) * (4 + 3 * (size_t)batch);
+  return IWDFT_OK;
+}
+
+int iwdft_pages_resize(int32_t page_tokens, int32_t n_pages, int32_t max_pages, const int32_t* d_want, int32_t batch, int32_t* d_table, int32_t* d_lens,
+                       int32_t* d_free, int32_t* d_starts, int32_t* d_slots, int32_t n_slots, void* d_workspace, size_t workspace_bytes,
+                       void* hip_stream) {
+  size_t need = 0;
+  int rc = check_page_size(page_tokens, n_pages, max_pages);
+  if (rc == IWDFT_OK) rc = iwdft_pages_resize_bytes(batch, n_slots, &need);
+  if (rc != IWDFT_OK) return rc;
+  if (!d_free || !d_starts || (batch && (!d_want || !d_table || !d_lens)) || (n_slots && !d_slots)) return fail(IWDFT_ERR_ARG, "a device pointer is NULL");
+  if (unaligned(4, d_want, d_table, d_lens, d_free, d_starts, d_slots, d_workspace)) return fail(IWDFT_ERR_ARG, "an int32 array is not 4-byte aligned");
+  if (need && (!d_workspace || workspace_bytes < need)) return fail(IWDFT_ERR_SIZE, "workspace has %zu bytes, %zu needed", d_workspace ? workspace_bytes : 0, need);
+  ResizeArgs a{d_want, batch, log2_of(page_tokens), max_pages, n_pages, n_slots, d_table, d_lens, d_free, d_starts, d_slots, need ? (int32_t*)d_workspace : nullptr};
+  return launched(launch_pages_resize(a, (hipStream_t)hip_stream), "page table launch");
+}
+
+int iwdft_pages_write(const iwdft_pages_desc* desc, int32_t layer, int32_t n_layers, const void* d_k, const void* d_v, const int32_t* d_slots, int32_t n_tokens,
+                      void* d_values, int32_t* d_exponents, void* hip_stream) {
+  const int rc = check_pages(desc, layer, n_layers);
+  if (rc != IWDFT_OK) return rc;
+  if (n_tokens < 0 || (int64_t)n_tokens * desc->n_kv_heads * n_layers > kMostRows) return fail(IWDFT_ERR_ARG, "n_tokens = %d out of range", n_tokens);
+  if (n_tokens == 0) return IWDFT_OK;
+  if (!d_k || !d_v || !d_slots || !d_values || !d_exponents) return fail(IWDFT_ERR_ARG, "a device pointer is NULL");
+  if (unaligned(16, d_k, d_v, d_values) || unaligned(4, d_slots) || unaligned(8, d_exponents)) return fail(IWDFT_ERR_ARG, "%s", kPageAlignMsg);
+  return launched(launch_pages_write(pages_of(*desc, d_values, d_exponents), layer, n_layers, desc->kv_dtype == IWDFT_BF16, d_k, d_v, d_slots, n_tokens,
+                                     (hipStream_t)hip_stream),
+                  "page write launch");
+}
+
+int iwdft_pages_attn_bytes(const iwdft_pages_desc* desc, int32_t n_layers, int32_t batch, int32_t n_tokens, size_t* workspace_bytes) {
+  if (!workspace_bytes) return fail(IWDFT_ERR_ARG, "output pointer is NULL");
+  const int rc = check_pages(desc, 0, n_layers);
+  if (rc != IWDFT_OK) return rc;
+  if (batch < 0 || n_tokens < 0) return fail(IWDFT_ERR_ARG, "batch = %d, n_tokens = %d: negative", batch, n_tokens);
+  *workspace_bytes = pages_attn_bytes(pages_of(*desc, nullptr, nullptr), n_layers, batch, n_tokens, desc->kv_dtype == IWDFT_BF16);
+  return IWDFT_OK;
+}
+
+int iwdft_pages_attn(const iwdft_pages_desc* desc, int32_t layer, int32_t n_layers, const void* d_q, const int32_t* d_starts, int32_t n_tokens,
+                     const int32_t* d_table, const int32_t* d_lens, int32_t batch, const void* d_values, const int32_t* d_exponents, void* d_out, int32_t n_sink,
+                     int32_t n_recent, float scale, void* d_workspace, size_t workspace_bytes, void* hip_stream) {
+  int rc = check_pages(desc, layer, n_layers);
+  size_t need = 0;
+  if (rc == IWDFT_OK) rc = iwdft_pages_attn_bytes(desc, n_layers, batch, n_tokens, &need);
+  if (rc != IWDFT_OK) return rc;
+  if ((int64_t)n_tokens * desc->n_q_heads * n_layers > kMostRows) return fail(IWDFT_ERR_ARG, "n_tokens = %d out of range", n_tokens);
+  if (n_sink < 0 || n_recent < 0) return fail(IWDFT_ERR_ARG, "n_sink = %d, n_recent = %d: negative", n_sink, n_recent);
+  if (n_sink > 0 && n_recent == 0) return fail(IWDFT_ERR_ARG, "n_sink = %d without a window: n_recent = 0 lets every row see all tokens before it", n_sink);
+  if (scale != scale) return fail(IWDFT_ERR_ARG, "scale is NaN");
+  if (n_tokens == 0 || batch == 0) return IWDFT_OK;
+  if (!d_q || !d_starts || !d_table || !d_lens || !d_values || !d_exponents || !d_out) return fail(IWDFT_ERR_ARG, "a device pointer is NULL");
+  if (unaligned(16, d_q, d_out, d_values) || unaligned(4, d_starts, d_table, d_lens) || unaligned(8, d_exponents)) return fail(IWDFT_ERR_ARG, "%s", kPageAlignMsg);
+  const size_t bytes = (size_t)n_layers * (size_t)n_tokens * (size_t)desc->n_q_heads * kHeadDim * (desc->kv_dtype == IWDFT_BF16 ? 2 : 4);
+  if ((const char*)d_q < (const char*)d_out + bytes && (const char*)d_out < (const char*)d_q + bytes) return fail(IWDFT_ERR_ARG, "d_q and d_out overlap");
+  if (need && (!d_workspace || workspace_bytes < need)) return fail(IWDFT_ERR_SIZE, "workspace has %zu bytes, %zu needed", d_workspace ? workspace_bytes : 0, need);
+  if (need && unaligned(256, d_workspace)) return fail(IWDFT_ERR_ARG, "d_workspace must be 256-byte aligned");
+  PagesAttn a{};
+  a.S = pages_of(*desc, (void*)d_values, (int32_t*)d_exponents);
+  a.layer = layer, a.n_layers = n_layers, a.batch = batch, a.n_tokens = n_tokens, a.n_sink = n_sink, a.n_recent = n_recent;
+  a.scale = (scale > 0.f ? scale : (float)(1.0 / std::sqrt((double)kHeadDim))) * 1.4426950408889634f;
+  a.q = d_q, a.out = d_out, a.starts = d_starts, a.table = d_table, a.lens = d_lens;
+  return launched(launch_pages_attn(a, desc->kv_dtype == IWDFT_BF16, need ? d_workspace : nullptr, (hipStream_t)hip_stream), "page attention launch");
+}
+
+int iwdft_pages_read(const iwdft_pages_desc* desc, int32_t layer, int32_t n_layers, const int32_t* d_table, const int32_t* d_lens, int32_t batch, int32_t n_tokens,
+                     const void* d_values, const int32_t* d_exponents, void* d_K, void* d_V, void* hip_stream) {
+  const int rc = check_pages(desc, layer, n_layers);
+  if (rc != IWDFT_OK) return rc;
+  if (batch < 0 || n_tokens < 0 || (double)n_tokens * batch * desc->n_kv_heads * n_layers > (double)kMostRows)
+    return fail(IWDFT_ERR_ARG, "batch = %d, n_tokens = %d out of range", batch, n_tokens);
+  if (n_tokens == 0 || batch == 0 || (!d_K && !d_V)) return IWDFT_OK;
+  if (!d_table || !d_lens || !d_values || !d_exponents) return fail(IWDFT_ERR_ARG, "a device pointer is NULL");
+  if (unaligned(16, d_K, d_V, d_values) || unaligned(4, d_table, d_lens) || unaligned(8, d_exponents)) return fail(IWDFT_ERR_ARG, "%s", kPageAlignMsg);
+  return launched(launch_pages_read(pages_of(*desc, (void*)d_values, (int32_t*)d_exponents), layer, n_layers, desc->kv_dtype == IWDFT_BF16, d_table, d_lens,
+                                    batch, n_tokens, d_K, d_V, (hipStream_t)hip_stream),
+                  "page read launch");
 }
 
 }  // extern "C"

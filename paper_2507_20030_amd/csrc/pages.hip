@@ -1,0 +1,454 @@
+// The 8-bit paged cache: block tables and slot maps from lengths, new tokens into the pages, the pages' tokens back.
+#include <algorithm>
+
+#include "pages.h"
+
+namespace iwdft {
+
+namespace {
+
+constexpr int kWave = 64;
+
+// ------------------------------------------------------------------------------------------------ block tables
+// free[0] pages lie on a stack, free[1 ..]; a call gives back R pages and takes A.  With V = (stack, R given back) and its top at the end, page i that is
+// taken is V[count + R - 1 - i], and where fewer are taken than given back the first R - A of the latter are pushed.  The stack is
+// either read or written, never both, so nothing has to be ordered.  Pages are given back from the last one of the last sequence on:
+// a call that undoes another one leaves the stack as it was.
+struct ResizeState {
+  int count, released, taken, total;  // total: new tokens
+};
+
+// Sums over the threads before this one, and over all of them; every thread of the workgroup calls it.
+template <class T>
+__device__ __forceinline__ T scan_before(T x, T* lds, T* sum) {
+  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  T in = x;
+#pragma unroll
+  for (int d = 1; d < kWave; d <<= 1) {
+    const T up = __shfl_up(in, d);
+    if (lane >= d) in += up;
+  }
+  __syncthreads();  // the last call's sums have been read
+  if (lane == kWave - 1) lds[wave] = in;
+  __syncthreads();
+  T before = 0, all = 0;
+  for (int w = 0; w < kResizeThreads / kWave; ++w) {
+    const T s = lds[w];
+    if (w < wave) before += s;
+    all += s;
+  }
+  *sum = all;
+  return before + in - x;
+}
+
+struct Change {
+  int have, want;  // want: have where the sequence stays or cannot be so long
+};
+__device__ __forceinline__ Change change_of(const ResizeArgs& a, int b) {
+  const int most = a.max_pages << a.logP;
+  Change c;
+  c.have = min(max(a.lens[b], 0), most);
+  const int w = a.want[b];
+  c.want = w < 0 || w > most ? c.have : w;
+  return c;
+}
+
+// What a thread of the filling kernel looks up.
+struct Fill {
+  const int32_t *have, *need, *gone, *starts;  // per sequence: old length, new pages of those before, pages given back before
+  ResizeState s;
+};
+
+__device__ __forceinline__ int last_not_above(const int32_t* v, int n, int x) {  // largest i < n with v[i] <= x (v ascending, v[0] <= x)
+  int lo = 0, hi = n;
+  while (hi - lo > 1) {
+    const int m = (lo + hi) >> 1;
+    if (v[m] <= x) lo = m;
+    else hi = m;
+  }
+  return lo;
+}
+
+// k-th page that is given back.
+__device__ __forceinline__ int released_page(const ResizeArgs& a, const Fill& f, int k) {
+  const int ord = f.s.released - 1 - k, b = last_not_above(f.gone, a.batch, ord);
+  const int j = page_count(a.lens[b], a.logP) + ord - f.gone[b];
+  return a.table[(int64_t)b * a.max_pages + j];
+}
+
+__device__ void resize_fill(const ResizeArgs& a, const Fill& f, int at, int step) {
+  const int P = 1 << a.logP;
+  for (int64_t t0 = at; t0 < a.n_slots; t0 += step) {
+    const int t = (int)t0;
+    int slot = -1;
+    if (t < f.s.total) {
+      const int b = last_not_above(f.starts, a.batch, t);
+      const int have = f.have[b], had = page_count(have, a.logP), pos = have + t - f.starts[b], j = pos >> a.logP;
+      int32_t* row = a.table + (int64_t)b * a.max_pages;
+      int page;
+      if (j < had) {
+        page = row[j];
+      } else {
+        const int v = f.s.count + f.s.released - 1 - (f.need[b] + j - had);
+        page = v < f.s.count ? a.free[1 + v] : released_page(a, f, v - f.s.count);
+        if ((pos & (P - 1)) == 0) row[j] = page;
+      }
+      if (page >= 0 && page < a.n_pages) slot = (page << a.logP) + (pos & (P - 1));
+    }
+    a.slots[t] = slot;
+  }
+  const int push = min(f.s.released - f.s.taken, a.n_pages - f.s.count);
+  for (int64_t k = at; k < push; k += step) a.free[1 + f.s.count + (int)k] = released_page(a, f, (int)k);
+}
+
+// ONE: up to kResizeOneBatch sequences and kResizeOneSlots slots, everything in this launch.  A decode step's call is the chain of loads, sums and
+// stores of one workgroup.  Otherwise resize_fill_kernel follows.
+template <bool ONE>
+__global__ __launch_bounds__(kResizeThreads) void resize_kernel(ResizeArgs a) {
+  __shared__ long long lds64[kResizeThreads / kWave];
+  __shared__ int lds32[kResizeThreads / kWave];
+  __shared__ int32_t keep[ONE ? 4 * kResizeOneBatch + 1 : 1];
+  int32_t *have = ONE ? keep : a.scratch + 4, *need = have + (ONE ? kResizeOneBatch : a.batch), *gone = need + (ONE ? kResizeOneBatch : a.batch);
+  int32_t* starts = ONE ? gone + kResizeOneBatch : a.starts;
+  const int tid = threadIdx.x;
+  const int count = min(max(a.free[0], 0), a.n_pages);
+
+  int released = 0;
+  for (int b0 = 0; b0 < a.batch; b0 += kResizeThreads) {  // pages given back by all: they serve this call too
+    const int b = b0 + tid;
+    int g = 0, all;
+    if (b < a.batch) {
+      const Change c = change_of(a, b);
+      g = max(0, page_count(c.have, a.logP) - page_count(c.want, a.logP));
+    }
+    const int before = scan_before(g, lds32, &all);
+    if (b < a.batch) gone[b] = released + before;
+    released += all;
+  }
+  released = min(released, a.n_pages);  // more only if two sequences held the same page
+
+  long long asked = 0, fresh = 0;
+  int taken = 0, total = 0;
+  for (int b0 = 0; b0 < a.batch; b0 += kResizeThreads) {
+    const int b = b0 + tid;
+    Change c{0, 0};
+    if (b < a.batch) c = change_of(a, b);
+    const bool up = c.want > c.have;
+    const int pages = up ? page_count(c.want, a.logP) - page_count(c.have, a.logP) : 0, tokens = up ? c.want - c.have : 0;
+    long long all_pages, all_tokens;
+    const long long pages_to = asked + scan_before((long long)pages, lds64, &all_pages) + pages;
+    const long long tokens_to = fresh + scan_before((long long)tokens, lds64, &all_tokens) + tokens;
+    const bool ok = up && tokens_to <= a.n_slots && (pages == 0 || pages_to <= (long long)count + released);
+    int all_in, all_new;
+    scan_before(ok ? pages : 0, lds32, &all_in);
+    const int first = total + scan_before(ok ? tokens : 0, lds32, &all_new);
+    if (b < a.batch) {
+      have[b] = c.have;
+      need[b] = (int)min(pages_to - pages, (long long)0x7fffffff);  // of admitted sequences: whoever asked before them got it
+      starts[b] = first;
+      if (ONE) a.starts[b] = first;
+      a.lens[b] = ok || c.want < c.have ? c.want : c.have;
+    }
+    asked += all_pages, fresh += all_tokens, taken += all_in, total += all_new;
+  }
+  if (tid == 0) {
+    a.starts[a.batch] = total;
+    a.free[0] = min(count + released - taken, a.n_pages);
+    if (!ONE) a.scratch[0] = count, a.scratch[1] = released, a.scratch[2] = taken, a.scratch[3] = total;
+  }
+  if constexpr (ONE) {
+    __threadfence_block();
+    __syncthreads();
+    resize_fill(a, Fill{have, need, gone, starts, {count, released, taken, total}}, tid, kResizeThreads);
+  }
+}
+
+__global__ __launch_bounds__(256) void resize_fill_kernel(ResizeArgs a) {
+  const int32_t* s = a.scratch;
+  resize_fill(a, Fill{s + 4, s + 4 + a.batch, s + 4 + 2 * a.batch, a.starts, {s[0], s[1], s[2], s[3]}}, blockIdx.x * 256 + threadIdx.x, gridDim.x * 256);
+}
+
+// ------------------------------------------------------------------------------------------------ writing
+template <bool BF16>
+__device__ __forceinline__ void load2(const void* p, int64_t i, float* f) {  // two neighbouring channels
+  if constexpr (BF16) {
+    const uint32_t w = *(const uint32_t*)((const uint16_t*)p + i);
+    f[0] = __uint_as_float(w << 16), f[1] = __uint_as_float(w & 0xffff0000u);
+  } else {
+    const float2 x = *(const float2*)((const float*)p + i);
+    f[0] = x.x, f[1] = x.y;
+  }
+}
+template <bool BF16>
+__device__ __forceinline__ void load16(const void* p, int64_t i, float* f) {
+  if constexpr (BF16) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const uint4 w = ((const uint4*)((const uint16_t*)p + i))[h];
+      const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+      for (int c = 0; c < 4; ++c) f[8 * h + 2 * c] = __uint_as_float(u[c] << 16), f[8 * h + 2 * c + 1] = __uint_as_float(u[c] & 0xffff0000u);
+    }
+  } else {
+#pragma unroll
+    for (int h = 0; h < 4; ++h) {
+      const float4 x = ((const float4*)((const float*)p + i))[h];
+      f[4 * h] = x.x, f[4 * h + 1] = x.y, f[4 * h + 2] = x.z, f[4 * h + 3] = x.w;
+    }
+  }
+}
+
+__device__ __forceinline__ float finite_abs(float x) {
+  const float y = fabsf(x);
+  return y < __builtin_inff() ? y : 0.f;  // NaN and infinities do not set the scale
+}
+
+// A run -- new tokens that follow each other in one page -- is one wave's work for each head and tensor: its largest value, the page's exponent, the
+// values.  The run is read twice, the second time from the caches, so that nothing has to stay in registers and no two waves meet.
+// old: the page's exponent, used from its second token on; returns the new one.  Old values are only touched where it grows; of an octet of V that holds other tokens too the bytes of those stay.
+template <bool BF16, bool V>
+__device__ int write_run(const Pages& S, int64_t ph, const void* x, int64_t row0, int64_t row_step, int offset, int n, int old) {
+  const int lane = threadIdx.x % kWave;
+  float top = 0.f;
+#pragma unroll 8
+  for (int i = 0; i < n; ++i) {
+    float f[2];
+    load2<BF16>(x, row0 + i * row_step + 2 * lane, f);
+    top = fmaxf(top, fmaxf(finite_abs(f[0]), finite_abs(f[1])));
+  }
+#pragma unroll
+  for (int d = 1; d < kWave; d <<= 1) top = fmaxf(top, __shfl_xor(top, d));
+  int e = e4m3_exponent(top), grown = 0;
+  if (offset > 0) {
+    grown = max(0, e - old);
+    e = max(e, old);
+  }
+  if (lane == 0) S.exponents[2 * ph + (V ? 1 : 0)] = e;
+  uint8_t* base = page_values(S, ph) + (V ? (size_t)kHeadDim << S.logP : 0);
+
+  for (int o = grown ? 0 : offset / kOct; o * kOct < offset + n; ++o) {
+    uint4* at = (uint4*)(base + o * kOct * kHeadDim) + lane;  // K: token lane / 8 of the octet, channels 16 (lane % 8) ..; V: channels 2 lane, 2 lane + 1
+    if constexpr (!V) {
+      const int row = o * kOct + lane / 8;
+      const bool fresh = row >= offset && row < offset + n;
+      if (!fresh && !(grown && row < offset)) continue;
+      float f[16];
+      if (fresh) {
+        load16<BF16>(x, row0 + (row - offset) * row_step + 16 * (lane % 8), f);
+#pragma unroll
+        for (int c = 0; c < 16; ++c) f[c] = ldexpf(f[c], -e);
+      } else {
+        const uint4 w = *at;
+        e4m3_floats(w.x, f), e4m3_floats(w.y, f + 4), e4m3_floats(w.z, f + 8), e4m3_floats(w.w, f + 12);
+#pragma unroll
+        for (int c = 0; c < 16; ++c) f[c] = ldexpf(f[c], -grown);
+      }
+      *at = make_uint4(floats_e4m3(f), floats_e4m3(f + 4), floats_e4m3(f + 8), floats_e4m3(f + 12));
+    } else {
+      float f[16];  // [channel][token]
+      const bool whole = o * kOct >= offset && (o + 1) * kOct <= offset + n;
+      uint32_t was[4] = {0, 0, 0, 0};
+      if (!whole) {
+        const uint4 w = *at;
+        was[0] = w.x, was[1] = w.y, was[2] = w.z, was[3] = w.w;
+      }
+#pragma unroll
+      for (int j = 0; j < kOct; ++j) {
+        const int row = o * kOct + j;
+        float g[2] = {0.f, 0.f};
+        if (row >= offset && row < offset + n) load2<BF16>(x, row0 + (row - offset) * row_step + 2 * lane, g);
+        f[j] = ldexpf(g[0], -e), f[8 + j] = ldexpf(g[1], -e);
+      }
+      uint32_t now[4];
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        now[w] = floats_e4m3(f + 4 * w);
+        if (!whole) {
+          float g[4];
+          e4m3_floats(was[w], g);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) g[j] = ldexpf(g[j], -grown);
+          const uint32_t moved = grown ? floats_e4m3(g) : was[w];
+          uint32_t keep = 0, old = 0;  // bytes outside the run; of tokens before it
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const int row = o * kOct + 4 * (w & 1) + j;
+            if (row < offset) old |= 0xffu << (8 * j);
+            else if (row >= offset + n) keep |= 0xffu << (8 * j);
+          }
+          now[w] = (now[w] & ~(keep | old)) | (moved & old) | (was[w] & keep);
+        }
+      }
+      *at = make_uint4(now[0], now[1], now[2], now[3]);
+    }
+  }
+  return e;
+}
+
+// The nearest row with a slot, from `row` on in steps of DIR (1 or -1); outside [0, n): none.  512 rows a turn, for rows that pad a batch.
+template <int DIR>
+__device__ __forceinline__ int row_with_slot(const int32_t* slots, int row, int n, int top) {
+  const int lane = threadIdx.x % kWave;
+  for (; row >= 0 && row < n; row += DIR * 8 * kWave) {
+    unsigned long long m[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int64_t r = row + (int64_t)DIR * (j * kWave + lane);
+      const int s = r >= 0 && r < n ? slots[r] : -1;
+      m[j] = __ballot(s >= 0 && s < top);
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (m[j]) return row + DIR * (j * kWave + __builtin_ctzll(m[j]));
+    if (DIR > 0 && row > n - 8 * kWave) break;
+  }
+  return -1;
+}
+
+// One wave per (segment of the slots, layer, head, tensor): the runs that begin in its segment.  Rows without a slot inside a page's new tokens do not
+// end the wave's work: what follows is a second run of the same page, after the first.
+template <bool BF16>
+__global__ __launch_bounds__(256) void pages_write_kernel(Pages S, int layer0, int n_layers, const void* k, const void* v, const int32_t* slots, int n_tokens,
+                                                          int segment, int64_t units) {
+  const int64_t unit = (int64_t)blockIdx.x * 4 + threadIdx.x / kWave;
+  if (unit >= units) return;
+  const int lane = threadIdx.x % kWave, P = 1 << S.logP;
+  const int which = (int)(unit & 1), h = (int)((unit >> 1) % S.H);
+  const int64_t rest = (unit >> 1) / S.H;
+  const int layer = (int)(rest % n_layers);
+  const int t0 = (int)(rest / n_layers) * segment, top = S.n_pages << S.logP;
+  const int t = t0 + lane;
+  int slot = -1, prev = -2;
+  if (lane < segment && t < n_tokens) {
+    slot = slots[t];
+    if (t > 0) prev = slots[t - 1];
+  }
+  const bool in = slot >= 0 && slot < top;
+  const bool follows = in && (slot & (P - 1)) != 0 && prev + 1 == slot;
+  unsigned long long leads = __ballot(in && !follows);
+  unsigned long long unsure = __ballot(in && (slot & (P - 1)) != 0 && t > 0 && (prev < 0 || prev >= top));
+  while (unsure) {  // behind rows without a slot
+    const int at = __builtin_ctzll(unsure), r = row_with_slot<-1>(slots, t0 + at - 1, n_tokens, top);
+    if (r >= 0 && slots[r] + 1 == __builtin_amdgcn_readlane(slot, at)) leads &= ~(1ull << at);
+    unsure &= unsure - 1;
+  }
+  while (leads) {
+    const int first = __builtin_ctzll(leads);
+    leads &= leads - 1;
+    int start = __builtin_amdgcn_readlane(slot, first), t1 = t0 + first, e = 0;
+    const int64_t ph = page_head(S, layer0 + layer, start >> S.logP, h);
+    const int64_t row_step = (int64_t)S.H * kHeadDim;
+    if (start & (P - 1)) e = S.exponents[2 * ph + which];
+    for (;;) {
+      const int offset = start & (P - 1), most = min(P - offset, n_tokens - t1);
+      int n = 0;  // length of the run: up to 128
+      for (int c = 0; c < most; c += kWave) {
+        const int i = c + lane;
+        const bool same = i < most && slots[t1 + i] == start + i;
+        const unsigned long long m = ~__ballot(same);
+        const int got = m ? __builtin_ctzll(m) : kWave;
+        n += got;
+        if (got < kWave) break;
+      }
+      const int64_t row0 = ((int64_t)layer * n_tokens + t1) * row_step + h * kHeadDim;
+      if (which) e = write_run<BF16, true>(S, ph, v, row0, row_step, offset, n, e);
+      else e = write_run<BF16, false>(S, ph, k, row0, row_step, offset, n, e);
+      if (offset + n == P || t1 + n >= n_tokens) break;
+      const int after = slots[t1 + n];
+      if (after >= 0 && after < top) break;
+      t1 = row_with_slot<1>(slots, t1 + n, n_tokens, top);
+      if (t1 < 0 || slots[t1] != start + n) break;
+      start += n;
+    }
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ reading
+template <bool BF16>
+__device__ __forceinline__ void store2(void* p, int64_t i, float x, float y) {
+  if constexpr (BF16) *(uint32_t*)((uint16_t*)p + i) = (uint32_t)f32_to_bf16(x) | (uint32_t)f32_to_bf16(y) << 16;
+  else *(float2*)((float*)p + i) = make_float2(x, y);
+}
+
+// One wave per octet of tokens of a sequence and head, K and V.  Bound by what it writes.
+template <bool BF16>
+__global__ __launch_bounds__(256) void pages_read_kernel(Pages S, int layer0, int batch, int n, const int32_t* table, const int32_t* lens, void* K, void* V,
+                                                         int64_t units) {
+  const int64_t unit = (int64_t)blockIdx.x * 4 + threadIdx.x / kWave;
+  if (unit >= units) return;
+  const int lane = threadIdx.x % kWave, octets = (n + kOct - 1) / kOct;
+  const int o = (int)(unit % octets);
+  int64_t rest = unit / octets;
+  const int h = (int)(rest % S.H);
+  rest /= S.H;
+  const int b = (int)(rest % batch), layer = (int)(rest / batch);
+  const int len = min(max(lens[b], 0), S.max_pages << S.logP);
+  const int t0 = o * kOct;
+  uint4 k = make_uint4(0, 0, 0, 0), v = k;
+  int ek = 0, ev = 0, there = min(len - t0, kOct);  // tokens of the octet
+  if (there > 0) {
+    const int page = table[(int64_t)b * S.max_pages + (t0 >> S.logP)];
+    if (page < 0 || page >= S.n_pages) {
+      there = 0;
+    } else {
+      const int64_t ph = page_head(S, layer0 + layer, page, h);
+      const uint8_t* at = page_values(S, ph) + (t0 & ((1 << S.logP) - 1)) * kHeadDim;
+      k = ((const uint4*)at)[lane], v = ((const uint4*)(at + ((size_t)kHeadDim << S.logP)))[lane];
+      ek = S.exponents[2 * ph], ev = S.exponents[2 * ph + 1];
+    }
+  }
+  const int64_t row = ((((int64_t)layer * batch + b) * S.H + h) * n + t0) * kHeadDim;
+  float f[16];
+  e4m3_floats(k.x, f), e4m3_floats(k.y, f + 4), e4m3_floats(k.z, f + 8), e4m3_floats(k.w, f + 12);
+  const int mine = lane / 8;
+  if (K && t0 + mine < n) {
+#pragma unroll
+    for (int c = 0; c < 16; ++c) f[c] = mine < there ? ldexpf(f[c], ek) : 0.f;
+#pragma unroll
+    for (int c = 0; c < 16; c += 2) store2<BF16>(K, row + mine * kHeadDim + 16 * (lane % 8) + c, f[c], f[c + 1]);
+  }
+  if (V) {
+    e4m3_floats(v.x, f), e4m3_floats(v.y, f + 4), e4m3_floats(v.z, f + 8), e4m3_floats(v.w, f + 12);
+#pragma unroll
+    for (int j = 0; j < kOct; ++j)
+      if (t0 + j < n) store2<BF16>(V, row + j * kHeadDim + 2 * lane, j < there ? ldexpf(f[j], ev) : 0.f, j < there ? ldexpf(f[8 + j], ev) : 0.f);
+  }
+}
+
+}  // namespace
+
+hipError_t launch_pages_resize(const ResizeArgs& a, hipStream_t st) {
+  if (!a.scratch) {
+    resize_kernel<true><<<1, kResizeThreads, 0, st>>>(a);
+    return hipGetLastError();
+  }
+  resize_kernel<false><<<1, kResizeThreads, 0, st>>>(a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  const int64_t items = std::max<int64_t>(a.n_slots, (int64_t)a.batch * 16);
+  resize_fill_kernel<<<(unsigned)std::min<int64_t>(1024, (items + 255) / 256), 256, 0, st>>>(a);
+  return hipGetLastError();
+}
+
+hipError_t launch_pages_write(const Pages& S, int layer, int n_layers, bool bf16, const void* k, const void* v, const int32_t* slots, int n_tokens,
+                              hipStream_t st) {
+  // as many waves as fill the chip, each with up to a page of tokens, which is one run of a prompt
+  const int64_t per_token = (int64_t)n_layers * S.H * 2;
+  const int segment = (int)std::max<int64_t>(1, std::min<int64_t>({kWave, (int64_t)1 << S.logP, n_tokens * per_token / 8192}));
+  const int64_t units = ((n_tokens + segment - 1) / segment) * per_token;
+  const unsigned grid = (unsigned)((units + 3) / 4);
+  if (bf16) pages_write_kernel<true><<<grid, 256, 0, st>>>(S, layer, n_layers, k, v, slots, n_tokens, segment, units);
+  else pages_write_kernel<false><<<grid, 256, 0, st>>>(S, layer, n_layers, k, v, slots, n_tokens, segment, units);
+  return hipGetLastError();
+}
+
+hipError_t launch_pages_read(const Pages& S, int layer, int n_layers, bool bf16, const int32_t* table, const int32_t* lens, int batch, int64_t n, void* K,
+                             void* V, hipStream_t st) {
+  const int64_t units = (n + kOct - 1) / kOct * S.H * batch * n_layers;
+  const unsigned grid = (unsigned)((units + 3) / 4);
+  if (bf16) pages_read_kernel<true><<<grid, 256, 0, st>>>(S, layer, batch, (int)n, table, lens, K, V, units);
+  else pages_read_kernel<false><<<grid, 256, 0, st>>>(S, layer, batch, (int)n, table, lens, K, V, units);
+  return hipGetLastError();
+}
+
+}  // namespace iwdft

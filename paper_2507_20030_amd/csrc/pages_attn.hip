@@ -1,0 +1,577 @@
+// Attention of new tokens over the 8-bit pages of their sequences.
+//
+//   o_t = sum_j p_j v_j,  p = softmax_j (scale q_t k_j),  over the tokens j that t sees.
+//
+// All products run on the matrix cores in fp16, which holds e4m3 exactly.  What keeps the rest exact:
+//  * q: a row is multiplied by the power of two that brings its largest value to [2^14, 2^15); bf16 then fits (relative to the row's largest
+//    value down to 2^-38), fp32 as the sum of two fp16 parts (22 bits).
+//  * the pages' exponents: that of K enters the score's factor; that of V joins the exponent of the weight.  With s_j the score times log2 e and
+//    eV_j the exponent of j's page, the weights in the sum are P_j = 2^(s_j + eV_j - m), m a running bound of s_j + eV_j, and the
+//    denominator is sum 2^(s_j - m) = sum P_j 2^-eV_j.  So no weight overflows fp16 or loses bits because its page is small.
+//  * P_j is rounded to fp16 (11 bits; bf16 results have 8), for fp32 to two parts; the denominator and all sums are fp32.
+// The sums hold 2^lift P_j.  m grows where an exponent passes it by more than `slack`; 2^lift P_j <= 2^(slack + lift) < 65504 then.  bf16: lift 6,
+// slack 8, few rescalings.  fp32: lift 15, slack 0: fp16 ends at 2^-25, so weights err by 2^-40 of the largest one at least, and a page's
+// values, whose sizes are up to 2^18 apart, by 2^-22 of what they add up to.
+#include <algorithm>
+#include <cfloat>
+
+#include "pages.h"
+
+namespace iwdft {
+
+namespace {
+
+constexpr int kWave = 64;
+constexpr int kTile = 32;    // tokens of a step
+constexpr int kWaves = 4;
+template <bool BF16>
+struct Weights {
+  static constexpr float lift = BF16 ? 6.f : 15.f, slack = BF16 ? 8.f : 0.f;
+};
+constexpr int kQTop = 14;    // q rows: largest value in [2^14, 2^15)
+
+// ------------------------------------------------------------------------------------------------ sharing out the work
+// A block is `rows` consecutive (new token, query head of the KV head) pairs of a sequence; its tokens are cut into parts, one workgroup each, such that
+// all parts of a call hold about the same number of tiles and there are about kParts of them.  Lengths live on the device, so every wave
+// works out the shares by itself (64 sequences at a time): the launch only has to be large enough.
+constexpr int kParts = 512;
+constexpr int kLeastTiles = 4;
+
+struct Seq {
+  int len, first, nq, rows, tiles;  // tokens, first new token (row of q), new tokens, rows of all blocks, most tiles of a block
+};
+
+template <int BR>
+__device__ __forceinline__ Seq seq_of(const PagesAttn& a, int b) {
+  Seq s;
+  s.len = min(max(a.lens[b], 0), a.S.max_pages << a.S.logP);
+  s.first = min(max(a.starts[b], 0), a.n_tokens);
+  s.nq = min(max(a.starts[b + 1], s.first), a.n_tokens) - s.first;
+  s.rows = s.nq * a.S.G;
+  s.tiles = (s.len + kTile - 1) / kTile;
+  if (a.n_recent) {
+    const int sink = (min(a.n_sink, s.len) + kTile - 1) / kTile;
+    const int64_t span = (int64_t)a.n_recent + min(s.nq, BR / a.S.G + 2) + 2 * kTile;
+    s.tiles = (int)min((int64_t)s.tiles, sink + span / kTile);
+  }
+  return s;
+}
+
+__device__ __forceinline__ int blocks_of(int rows, int BR) { return (rows + BR - 1) / BR; }
+
+struct Shares {
+  int tiles;  // of a part
+  int parts;  // of all sequences, for one (layer, KV head)
+  int split;  // ... of blocks that are cut
+  int split_rows;  // rows of sequences whose blocks are cut
+};
+__device__ __forceinline__ int parts_of(const Seq& s, int tiles) { return s.nq ? max(1, (s.tiles + tiles - 1) / tiles) : 0; }
+
+__device__ __forceinline__ int wave_sum(int x) {
+#pragma unroll
+  for (int d = 1; d < kWave; d <<= 1) x += __shfl_xor(x, d);
+  return x;
+}
+__device__ __forceinline__ float wave_sum(float x) {
+#pragma unroll
+  for (int d = 1; d < kWave; d <<= 1) x += __shfl_xor(x, d);
+  return x;
+}
+
+template <int BR>
+__device__ Shares shares_of(const PagesAttn& a, int lane) {
+  float sum = 0.f;  // every wave adds in the same order: all agree
+  for (int b0 = 0; b0 < a.batch; b0 += kWave)
+    if (b0 + lane < a.batch) {
+      const Seq s = seq_of<BR>(a, b0 + lane);
+      sum += (float)s.tiles * (float)blocks_of(s.rows, BR);
+    }
+  sum = wave_sum(sum) * (float)(a.n_layers * a.S.H);
+  Shares w;
+  w.tiles = max(kLeastTiles, (int)fminf(ceilf(sum / (float)kParts), 1e9f));
+  w.parts = w.split = w.split_rows = 0;
+  for (int b0 = 0; b0 < a.batch; b0 += kWave)
+    if (b0 + lane < a.batch) {
+      const Seq s = seq_of<BR>(a, b0 + lane);
+      const int np = parts_of(s, w.tiles), n = np * blocks_of(s.rows, BR);
+      w.parts += n;
+      if (np > 1) w.split += n, w.split_rows += s.rows;
+    }
+  w.parts = wave_sum(w.parts), w.split = wave_sum(w.split), w.split_rows = wave_sum(w.split_rows);
+  return w;
+}
+
+// The sequence that holds entry y of a numbering that gives every sequence count(its Seq, its parts) entries: its index, y's place in it, and how many
+// parts of cut blocks the sequences before it have.
+struct Place {
+  int b, at, before, np;
+  Seq s;
+};
+template <int BR, class Count>
+__device__ Place place_of(const PagesAttn& a, const Shares& w, int y, int lane, Count count) {
+  int done = 0, cut = 0;
+  for (int b0 = 0;; b0 += kWave) {
+    Seq s{0, 0, 0, 0, 0};
+    int np = 0, n = 0, c = 0;
+    if (b0 + lane < a.batch) {
+      s = seq_of<BR>(a, b0 + lane);
+      np = parts_of(s, w.tiles);
+      n = count(s, np);
+      c = np > 1 ? np * blocks_of(s.rows, BR) : 0;
+    }
+    int in = n, cin = c;
+#pragma unroll
+    for (int d = 1; d < kWave; d <<= 1) {
+      const int u = __shfl_up(in, d), v = __shfl_up(cin, d);
+      if (lane >= d) in += u, cin += v;
+    }
+    const unsigned long long m = __ballot(y < done + in);
+    if (m || b0 + kWave >= a.batch) {  // always found: y is below the sum of all counts
+      const int src = m ? __builtin_ctzll(m) : 0;
+      const auto uni = [&](int x) { return __builtin_amdgcn_readlane(x, src); };
+      Place p;
+      p.b = b0 + src, p.at = y - done - uni(in - n), p.before = cut + uni(cin - c), p.np = uni(np);
+      p.s.len = uni(s.len), p.s.first = uni(s.first), p.s.nq = uni(s.nq), p.s.rows = uni(s.rows), p.s.tiles = uni(s.tiles);
+      return p;
+    }
+    done += __builtin_amdgcn_readlane(in, kWave - 1), cut += __builtin_amdgcn_readlane(cin, kWave - 1);
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ operands
+__device__ __forceinline__ half2v e4m3_halves(uint32_t w, bool high) {
+  return high ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, true) : __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, false);
+}
+// Eight bytes as an operand.
+__device__ __forceinline__ half8 operand(uint32_t lo, uint32_t hi) {
+  const half2v a = e4m3_halves(lo, false), b = e4m3_halves(lo, true), c = e4m3_halves(hi, false), d = e4m3_halves(hi, true);
+  return half8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+__device__ __forceinline__ uint32_t nan_bytes(uint32_t w) {  // 1 in every byte that is NaN (0x7f, 0xff)
+  return (((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) >> 7;
+}
+template <int N, int PARTS>
+__device__ __forceinline__ void to_halves(const float* x, half8* parts) {  // x[8] as PARTS fp16 numbers that add up to it
+#pragma unroll
+  for (int c = 0; c < 8; ++c) {
+    float rest = x[c];
+#pragma unroll
+    for (int p = 0; p < PARTS; ++p) {
+      const _Float16 h = (_Float16)rest;
+      parts[p][c] = h;
+      rest -= (float)h;
+    }
+  }
+}
+__device__ __forceinline__ float max_over_16s(float x) {  // over lanes that differ in their upper two bits
+  x = fmaxf(x, __shfl_xor(x, 16));
+  return fmaxf(x, __shfl_xor(x, 32));
+}
+
+template <bool BF16>
+__device__ __forceinline__ void load_channels(const void* p, int64_t i, float* f) {  // 16 channels
+  if constexpr (BF16) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const uint4 w = ((const uint4*)((const uint16_t*)p + i))[h];
+      const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+      for (int c = 0; c < 4; ++c) f[8 * h + 2 * c] = __uint_as_float(u[c] << 16), f[8 * h + 2 * c + 1] = __uint_as_float(u[c] & 0xffff0000u);
+    }
+  } else {
+#pragma unroll
+    for (int h = 0; h < 4; ++h) {
+      const float4 x = ((const float4*)((const float*)p + i))[h];
+      f[4 * h] = x.x, f[4 * h + 1] = x.y, f[4 * h + 2] = x.z, f[4 * h + 3] = x.w;
+    }
+  }
+}
+
+// Tiles that a block's rows see: those of the sinks, then the others.
+struct Span {
+  int sinks, skip, n;
+  __device__ __forceinline__ int tile(int i) const { return i < sinks ? i : i + skip; }
+};
+__device__ __forceinline__ Span span_of(const PagesAttn& a, int p_lo, int p_hi) {  // positions of the block's first and last token
+  Span s{0, 0, 0};
+  if (p_hi < 0) return s;
+  const int end = p_hi / kTile + 1;
+  int from = 0;
+  if (a.n_recent) {
+    from = (int)(max((int64_t)0, (int64_t)p_lo - a.n_recent + 1) / kTile);
+    s.sinks = a.n_sink > 0 ? min((min(a.n_sink, p_hi + 1) + kTile - 1) / kTile, end) : 0;
+  }
+  s.skip = max(from - s.sinks, 0);
+  s.n = max(end - s.skip, s.sinks);
+  return s;
+}
+
+// One row tile of 16 query rows: lane l holds row l % 16.
+template <int PARTS>
+struct Rows {
+  half8 q[4][PARTS];
+  floatx4 o[8];   // [16-byte load of V][channel of the pair]: row l % 16, channels 32 (i / 2) + 8 (l / 16) + 2 c + i % 2
+  float m, l, factor;
+  int pos, eq;
+};
+
+// ------------------------------------------------------------------------------------------------ few rows
+// A workgroup has a part of the tokens of one block of 16 R rows; its four waves take the tiles in turn and join their sums in the end.  A tile of 32
+// tokens is 8 KB, eight 16-byte loads a lane, the next one's in flight while this one is multiplied: S^T = K Q^T leaves lane l
+// with row l % 16 and the 8 tokens of octet l / 16, which is how O^T = V^T P^T wants them, so nothing moves between lanes but the maximum.
+template <bool BF16, int R>
+__global__ __launch_bounds__(kWaves* kWave) void pages_few_kernel(PagesAttn a) {
+  constexpr int PARTS = BF16 ? 1 : 2, BR = 16 * R;
+  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  const int row = lane & 15, oct = lane >> 4;
+  __shared__ __attribute__((aligned(16))) float join[2][BR][kHeadDim + 4];
+  __shared__ float2 join_stat[2][BR];
+
+  const Shares w = shares_of<BR>(a, lane);
+  const int64_t all = (int64_t)w.parts * a.n_layers * a.S.H;
+  for (int64_t x = blockIdx.x; x < all; x += gridDim.x) {
+    const int lh = (int)(x / w.parts);
+    const Place at = place_of<BR>(a, w, (int)(x % w.parts), lane, [](const Seq& s, int np) { return np * blocks_of(s.rows, BR); });
+    const Seq s = at.s;
+    const int block = at.at / at.np, part = at.at % at.np, layer = lh / a.S.H, h = lh % a.S.H, G = a.S.G;
+    const int row0 = block * BR, rows = min(s.rows - row0, BR);
+    const int before = s.len - s.nq;  // position of the sequence's first new token
+    const int p_lo = before + row0 / G, p_hi = before + (row0 + rows - 1) / G;
+    const Span span = span_of(a, p_lo, p_hi);
+    const int t_from = (int)((int64_t)span.n * part / at.np), t_to = (int)((int64_t)span.n * (part + 1) / at.np);
+    const int n_rt = (rows + 15) / 16;
+
+    Rows<PARTS> rt[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      Rows<PARTS>& z = rt[r];
+      const int mine = row0 + 16 * r + row;
+      const bool have = 16 * r + row < rows;
+      z.pos = have ? before + mine / G : -1;
+      z.m = -FLT_MAX, z.l = 0.f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) z.o[i] = floatx4{0.f, 0.f, 0.f, 0.f};
+      float f[2][16];
+      float top = 0.f;
+      if (have) {
+        const int64_t base = (((int64_t)layer * a.n_tokens + s.first + mine / G) * (a.S.H * G) + h * G + mine % G) * kHeadDim;
+#pragma unroll
+        for (int p = 0; p < 2; ++p) load_channels<BF16>(a.q, base + 64 * p + 16 * oct, f[p]);
+      } else {
+#pragma unroll
+        for (int p = 0; p < 2; ++p)
+#pragma unroll
+          for (int c = 0; c < 16; ++c) f[p][c] = 0.f;
+      }
+#pragma unroll
+      for (int p = 0; p < 2; ++p)
+#pragma unroll
+        for (int c = 0; c < 16; ++c) top = fmaxf(top, fabsf(f[p][c]));
+      top = max_over_16s(top);
+      z.eq = max((int)(__float_as_uint(top) >> 23) - 127, kLeastExponent);
+#pragma unroll
+      for (int p = 0; p < 2; ++p)
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+          float y[8];
+#pragma unroll
+          for (int c = 0; c < 8; ++c) y[c] = ldexpf(f[p][8 * g + c], kQTop - z.eq);
+          to_halves<8, PARTS>(y, z.q[2 * p + g]);
+        }
+    }
+
+    // pages of a lane's octets: that of its K row and that of its tokens in V and in the scores
+    const int32_t* table = a.table + (int64_t)at.b * a.S.max_pages;
+    const int last_page = max(page_count(s.len, a.S.logP) - 1, 0), in_page = (1 << a.S.logP) - 1;
+    const int k_oct = row >> 2, k_tok = 8 * k_oct + (row & 3);
+    struct Ids {
+      int k, v;
+    };
+    const auto pages_at = [&](int i) {
+      const int t = span.tile(i) * kTile;
+      return Ids{table[min((t + 8 * k_oct) >> a.S.logP, last_page)], table[min((t + 8 * oct) >> a.S.logP, last_page)]};
+    };
+    struct Data {
+      uint4 k[2][2], v[4];
+      int2 e;
+      bool bad;
+    };
+    const auto load_tile = [&](int i, Ids id) {
+      Data d;
+      const int t = span.tile(i) * kTile;
+      d.bad = id.v < 0 || id.v >= a.S.n_pages;
+      const int kp = id.k < 0 || id.k >= a.S.n_pages ? 0 : id.k, vp = d.bad ? 0 : id.v;
+      const int64_t vh = page_head(a.S, a.layer + layer, vp, h);
+      const uint8_t* kb = page_values(a.S, page_head(a.S, a.layer + layer, kp, h)) + ((t + k_tok) & in_page) * kHeadDim + 16 * oct;
+      const uint8_t* vb = page_values(a.S, vh) + ((size_t)kHeadDim << a.S.logP) + ((t + 8 * oct) & in_page) * kHeadDim + 16 * row;
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int p = 0; p < 2; ++p) d.k[u][p] = *(const uint4*)(kb + u * 4 * kHeadDim + 64 * p);
+#pragma unroll
+      for (int p = 0; p < 4; ++p) d.v[p] = *(const uint4*)(vb + 256 * p);
+      d.e = *(const int2*)(a.S.exponents + 2 * vh);
+      return d;
+    };
+
+    const int first = t_from + wave;
+    Ids id{0, 0};
+    Data next{};
+    if (first < t_to) {
+      next = load_tile(first, pages_at(first));
+      if (first + kWaves < t_to) id = pages_at(first + kWaves);
+    }
+    for (int i = first; i < t_to; i += kWaves) {
+      Data d = next;
+      if (i + kWaves < t_to) {
+        next = load_tile(i + kWaves, id);
+        if (i + 2 * kWaves < t_to) id = pages_at(i + 2 * kWaves);
+      }
+      const int t0 = span.tile(i) * kTile, t1 = t0 + kTile - 1, j0 = t0 + 8 * oct;
+      // whether every row sees the whole tile
+      const bool edge = t1 > p_lo || (a.n_recent && t1 >= a.n_sink && (int64_t)t0 <= (int64_t)p_hi - a.n_recent) || __any(d.bad);
+      bool poison = false;
+      if (edge) {  // tokens that no row sees may hold anything
+        uint32_t keep[2] = {0, 0};
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const int t = j0 + j;
+          const bool seen = !d.bad && t <= p_hi && (!a.n_recent || t < a.n_sink || (int64_t)t > (int64_t)p_lo - a.n_recent);
+          keep[j / 4] |= seen ? 0xffu << (8 * (j % 4)) : 0u;
+        }
+        uint32_t nans = 0;
+#pragma unroll
+        for (int p = 0; p < 4; ++p) {
+          d.v[p].x &= keep[0], d.v[p].y &= keep[1], d.v[p].z &= keep[0], d.v[p].w &= keep[1];
+          nans |= nan_bytes(d.v[p].x) | nan_bytes(d.v[p].y) | nan_bytes(d.v[p].z) | nan_bytes(d.v[p].w);
+        }
+        poison = __any(nans != 0);
+      }
+
+      half8 kf[2][4];
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int p = 0; p < 2; ++p) kf[u][2 * p] = operand(d.k[u][p].x, d.k[u][p].y), kf[u][2 * p + 1] = operand(d.k[u][p].z, d.k[u][p].w);
+      const float ev = (float)d.e.y;
+      half8 pw[R][PARTS], sees[R];
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        if (r >= n_rt) continue;
+        Rows<PARTS>& z = rt[r];
+        float sc[8];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          floatx4 acc{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int c = 0; c < 4; ++c)
+#pragma unroll
+            for (int p = PARTS - 1; p >= 0; --p) acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[u][c], z.q[c][p], acc, 0, 0, 0);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) sc[4 * u + j] = acc[j];
+        }
+        const float factor = ldexpf(a.scale, z.eq - kQTop + d.e.x);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sc[j] = sc[j] * factor + ev;
+        if (edge) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const int t = j0 + j;
+            const bool seen = !d.bad && t <= z.pos && (!a.n_recent || t < a.n_sink || (int64_t)t > (int64_t)z.pos - a.n_recent);
+            sees[r][j] = seen ? (_Float16)1.f : (_Float16)0.f;
+            sc[j] = seen ? sc[j] : -__builtin_inff();
+          }
+        }
+        float top = sc[0];
+#pragma unroll
+        for (int j = 1; j < 8; ++j) top = fmaxf(top, sc[j]);
+        if (__any(top > z.m + Weights<BF16>::slack)) {
+          top = fmaxf(z.m, max_over_16s(top));
+          const float fade = __builtin_amdgcn_exp2f(z.m - top);
+          z.m = top, z.l *= fade;
+#pragma unroll
+          for (int c = 0; c < 8; ++c) z.o[c] *= fade;
+        }
+        float y[8], sum = 0.f;
+        const float ref = z.m - Weights<BF16>::lift;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) y[j] = __builtin_amdgcn_exp2f(sc[j] - ref), sum += y[j];
+        z.l += ldexpf(sum, -d.e.y);
+        to_halves<8, PARTS>(y, pw[r]);
+      }
+      half8 vf[8];
+#pragma unroll
+      for (int p = 0; p < 4; ++p) {
+        uint4 v = d.v[p];
+        if (poison) {  // NaN where only some rows may see it: taken out here, brought back to those rows
+          const uint32_t n[4] = {nan_bytes(v.x), nan_bytes(v.y), nan_bytes(v.z), nan_bytes(v.w)};
+          v.x &= ~(n[0] * 0xffu), v.y &= ~(n[1] * 0xffu), v.z &= ~(n[2] * 0xffu), v.w &= ~(n[3] * 0xffu);
+          const half8 bad[2] = {operand(n[0] * 0x38u, n[1] * 0x38u), operand(n[2] * 0x38u, n[3] * 0x38u)};  // 0x38: 1
+#pragma unroll
+          for (int r = 0; r < R; ++r) {
+            if (r >= n_rt) continue;
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+              const floatx4 hit = __builtin_amdgcn_mfma_f32_16x16x32_f16(bad[c], sees[r], floatx4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+#pragma unroll
+              for (int j = 0; j < 4; ++j)
+                if (hit[j] > 0.f) rt[r].o[2 * p + c][j] = __builtin_nanf("");
+            }
+          }
+        }
+        vf[2 * p] = operand(v.x, v.y), vf[2 * p + 1] = operand(v.z, v.w);
+      }
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        if (r >= n_rt) continue;
+#pragma unroll
+        for (int c = 0; c < 8; ++c)
+#pragma unroll
+          for (int p = PARTS - 1; p >= 0; --p) rt[r].o[c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf[c], pw[r][p], rt[r].o[c], 0, 0, 0);
+      }
+    }
+
+    // the four waves' sums: 2 and 3 to 0 and 1, then 1 to 0
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      rt[r].l += __shfl_xor(rt[r].l, 16);
+      rt[r].l += __shfl_xor(rt[r].l, 32);
+    }
+#pragma unroll
+    for (int from = 2; from >= 1; --from) {
+      __syncthreads();
+      if (wave >= from && wave < 2 * from)
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+          float* at_row = join[wave - from][16 * r + row] + 8 * oct;
+#pragma unroll
+          for (int c = 0; c < 8; ++c)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) at_row[32 * (c / 2) + 2 * j + c % 2] = rt[r].o[c][j];
+          if (oct == 0) join_stat[wave - from][16 * r + row] = make_float2(rt[r].m, rt[r].l);
+        }
+      __syncthreads();
+      if (wave < from)
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+          Rows<PARTS>& z = rt[r];
+          const float* at_row = join[wave][16 * r + row] + 8 * oct;
+          const float2 st = join_stat[wave][16 * r + row];
+          const float m = fmaxf(z.m, st.x), f0 = __builtin_amdgcn_exp2f(z.m - m), f1 = __builtin_amdgcn_exp2f(st.x - m);
+          z.m = m, z.l = z.l * f0 + st.y * f1;
+#pragma unroll
+          for (int c = 0; c < 8; ++c)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) z.o[c][j] = z.o[c][j] * f0 + at_row[32 * (c / 2) + 2 * j + c % 2] * f1;
+        }
+    }
+    if (wave == 0) {
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        const Rows<PARTS>& z = rt[r];
+        if (16 * r + row >= rows) continue;
+        if (at.np == 1) {
+          const int mine = row0 + 16 * r + row;
+          const int64_t base = (((int64_t)layer * a.n_tokens + s.first + mine / G) * (a.S.H * G) + h * G + mine % G) * kHeadDim + 8 * oct;
+          const float inv = z.l == 0.f ? 0.f : 1.f / z.l;
+#pragma unroll
+          for (int c = 0; c < 8; ++c)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) store_kv<BF16>(a.out, base + 32 * (c / 2) + 2 * j + c % 2, z.o[c][j] * inv);
+        } else {
+          const int64_t slot = (int64_t)lh * w.split + at.before + at.at;
+          float* to = a.part + (slot * BR + 16 * r + row) * kHeadDim + 8 * oct;
+#pragma unroll
+          for (int c = 0; c < 8; ++c)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) to[32 * (c / 2) + 2 * j + c % 2] = z.o[c][j];
+          if (oct == 0) a.stat[slot * BR + 16 * r + row] = make_float2(z.m, z.l);
+        }
+      }
+    }
+    __syncthreads();
+  }
+}
+
+// Rows whose tokens were shared out: one workgroup per row, its waves take the parts in turn.
+template <bool BF16, int BR>
+__global__ __launch_bounds__(kWaves* kWave) void pages_join_kernel(PagesAttn a) {
+  __shared__ float2 sums[kWaves][kWave];
+  __shared__ float dens[kWaves];
+  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  const Shares w = shares_of<BR>(a, lane);
+  const int64_t all = (int64_t)w.split_rows * a.n_layers * a.S.H;
+  for (int64_t x = blockIdx.x; x < all; x += gridDim.x) {
+    const int lh = (int)(x / w.split_rows);
+    const Place at = place_of<BR>(a, w, (int)(x % w.split_rows), lane, [](const Seq& s, int np) { return np > 1 ? s.rows : 0; });
+    const int r = at.at, G = a.S.G;
+    const int64_t slot = (int64_t)lh * w.split + at.before + (int64_t)(r / BR) * at.np;
+    const float2* stat = a.stat + slot * BR + r % BR;
+    const float* part = a.part + (slot * BR + r % BR) * kHeadDim + 2 * lane;
+    float m = -FLT_MAX;
+    for (int k = lane; k < at.np; k += kWave) m = fmaxf(m, stat[(int64_t)k * BR].x);
+#pragma unroll
+    for (int d = 1; d < kWave; d <<= 1) m = fmaxf(m, __shfl_xor(m, d));
+    float2 o = make_float2(0.f, 0.f);
+    float l = 0.f;
+    for (int k = wave; k < at.np; k += kWaves) {
+      const float2 st = stat[(int64_t)k * BR], v = *(const float2*)(part + (int64_t)k * BR * kHeadDim);
+      const float f = __builtin_amdgcn_exp2f(st.x - m);
+      o.x += v.x * f, o.y += v.y * f, l += st.y * f;
+    }
+    sums[wave][lane] = o;
+    if (lane == 0) dens[wave] = l;
+    __syncthreads();
+    if (wave == 0) {
+#pragma unroll
+      for (int i = 1; i < kWaves; ++i) o.x += sums[i][lane].x, o.y += sums[i][lane].y, l += dens[i];
+      const float inv = l == 0.f ? 0.f : 1.f / l;
+      const int layer = lh / a.S.H, h = lh % a.S.H;
+      const int64_t base = (((int64_t)layer * a.n_tokens + at.s.first + r / G) * (a.S.H * G) + h * G + r % G) * kHeadDim + 2 * lane;
+      store_kv<BF16>(a.out, base, o.x * inv), store_kv<BF16>(a.out, base + 1, o.y * inv);
+    }
+    __syncthreads();
+  }
+}
+
+// Rows of a block (times 16): what an average sequence brings.
+int row_tiles(const Pages& S, int batch, int n_tokens, bool bf16) {
+  const int64_t rows = (int64_t)S.G * ((n_tokens + batch - 1) / batch);
+  return rows <= 16 ? 1 : rows <= 32 || !bf16 ? 2 : 4;
+}
+
+// Parts of cut blocks: a block of more than w.tiles tiles has fewer than 2 tiles / w.tiles of them, all blocks together kParts w.tiles tiles (rounding: + 64).
+constexpr int64_t kMostCut = 2 * kParts + 64;
+
+template <bool BF16, int R>
+hipError_t launch_few(const PagesAttn& a, hipStream_t st) {
+  constexpr int BR = 16 * R;
+  const int64_t lh = (int64_t)a.n_layers * a.S.H, blocks = (int64_t)a.n_tokens * a.S.G / BR + a.batch;
+  const unsigned grid = (unsigned)std::min<int64_t>(kParts + lh * blocks, 1 << 20);
+  pages_few_kernel<BF16, R><<<grid, kWaves * kWave, 0, st>>>(a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || !a.part) return e;
+  const unsigned join = (unsigned)std::min<int64_t>(lh * a.n_tokens * a.S.G, 2048);
+  pages_join_kernel<BF16, BR><<<join, kWaves * kWave, 0, st>>>(a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+size_t pages_attn_bytes(const Pages& S, int n_layers, int batch, int n_tokens, bool bf16) {
+  const int64_t most = ((int64_t)S.max_pages << S.logP) / kTile + 1;
+  if (most <= kLeastTiles || batch == 0 || n_tokens == 0) return 0;  // no block is ever cut
+  const int BR = 16 * row_tiles(S, batch, n_tokens, bf16);
+  (void)n_layers;
+  return (size_t)kMostCut * BR * (kHeadDim * sizeof(float) + sizeof(float2));
+}
+
+hipError_t launch_pages_attn(PagesAttn a, bool bf16, void* ws, hipStream_t st) {
+  const int R = row_tiles(a.S, a.batch, a.n_tokens, bf16);
+  a.part = pages_attn_bytes(a.S, a.n_layers, a.batch, a.n_tokens, bf16) ? (float*)ws : nullptr;
+  a.stat = a.part ? (float2*)(a.part + kMostCut * 16 * R * kHeadDim) : nullptr;
+  if (bf16) return R == 1 ? launch_few<true, 1>(a, st) : R == 2 ? launch_few<true, 2>(a, st) : launch_few<true, 4>(a, st);
+  return R == 1 ? launch_few<false, 1>(a, st) : launch_few<false, 2>(a, st);
+}
+
+}  // namespace iwdft

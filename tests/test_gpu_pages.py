@@ -1,0 +1,501 @@
+"""The 8-bit paged cache on the GPU against the integer / float64 oracle: whole numbers and stored bytes exactly, attention within what its roundings add up to."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import iwdft_oracle as orc
+from oracle import pages_oracle as po
+from paper_2507_20030_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+DT = {"f32": torch.float32, "bf16": torch.bfloat16}
+
+
+def dev(x):
+    return torch.from_numpy(np.ascontiguousarray(x)).to(DEV)
+
+
+def f64(t):
+    return t.detach().cpu().double().numpy()
+
+
+class Pool:
+    """Sequences of the given lengths with pages in random order, filled through the oracle; the same on the GPU."""
+
+    def __init__(self, rng, lens, P, heads=2, layers=1, n_pages=None, scale=None, stale=True):
+        used = sum(-(-n // P) for n in lens)
+        n_pages = used + 3 if n_pages is None else n_pages
+        self.store, self.P = po.Store(layers, n_pages, heads, P), P
+        self.lens = np.array(lens, np.int32)
+        self.table = np.full((len(lens), max(1, max(-(-n // P) for n in lens)) + 1), -1, np.int32)
+        order = list(rng.permutation(n_pages))
+        for b, n in enumerate(lens):
+            for j in range(-(-n // P)):
+                self.table[b, j] = order.pop()
+        full = rng.normal(size=(layers, n_pages * P, heads, 128)) * (10.0 ** rng.uniform(-1, 1, size=128) if scale is None else scale)
+        if stale:
+            self.store.write(full, rng.normal(size=full.shape) * 10.0 ** rng.uniform(-2, 2, size=(1, full.shape[1], 1, 1)), np.arange(n_pages * P))
+        self.upload()
+
+    def upload(self):
+        self.values, self.exponents = dev(self.store.packed()), dev(self.store.exponents)
+        self.d_table, self.d_lens = dev(self.table), dev(self.lens)
+
+
+# ------------------------------------------------------------------------------------------------------------------ tables
+def check_resize(rng, B_, W, P, n_pages, n_slots, rounds, most):
+    table, lens = np.full((B_, W), -1, np.int32), np.zeros(B_, np.int32)
+    free = np.concatenate([[n_pages], rng.permutation(n_pages)]).astype(np.int32)
+    d_table, d_lens, d_free = dev(table), dev(lens), dev(free)
+    refused = 0
+    for r in range(rounds):
+        want = rng.integers(0, most + 1, size=B_)
+        want = np.where(rng.random(B_) < 0.3, lens + rng.integers(0, 3, size=B_), want)
+        want = np.where(rng.random(B_) < 0.1, -1, np.where(rng.random(B_) < 0.15, 0, want))
+        if r % 3 == 2:
+            want[rng.integers(B_)] = W * P + 1
+        want = want.astype(np.int32)
+        d_starts, d_slots = (torch.full((n,), 77, dtype=torch.int32, device=DEV) for n in (B_ + 1, n_slots))
+        B.iwdft_pages_resize(dev(want), d_table, d_lens, d_free, d_starts, d_slots, P)
+        starts, slots = po.resize(want, table, lens, free, n_slots, P)
+        for name, got, ref in (("table", d_table, table), ("lens", d_lens, lens), ("free", d_free, free), ("starts", d_starts, starts), ("slots", d_slots, slots)):
+            assert np.array_equal(got.cpu().numpy(), ref), (name, r)
+        refused += int(((want > lens) & (want >= 0)).sum())
+    return refused
+
+
+@pytest.mark.parametrize("batch,W,P,n_pages,n_slots,most", [
+    (1, 4, 16, 5, 64, 60), (3, 6, 32, 12, 200, 150), (16, 20, 16, 200, 300, 300), (64, 9, 128, 300, 2048, 1000), (1024, 3, 16, 900, 1500, 40),
+    (1, 300, 16, 310, 5000, 4700), (40, 40, 32, 900, 30000, 1200), (1025, 4, 16, 2000, 700, 50), (2500, 5, 64, 6000, 100000, 300), (5, 3, 16, 9, 0, 40),
+])
+def test_tables_and_slots(batch, W, P, n_pages, n_slots, most):
+    """Pools and slot maps that run out, lengths beyond the table, idle and finished sequences; one launch and two."""
+    refused = check_resize(np.random.default_rng(batch * W + P), batch, W, P, n_pages, n_slots, 7, most)
+    assert refused > 0
+
+
+def test_a_call_that_undoes_another_leaves_the_stack():
+    for batch, new in ((9, 40), (9, 900)):
+        rng = np.random.default_rng(new)
+        base = rng.integers(0, 500, size=batch).astype(np.int32)
+        c = B.PagedCache(1, 700, 1, 1, 128, torch.float32, batch, 2000, 16, DEV)
+        c.resize(dev(base), 5000)
+        free, table = c.free.clone(), c.table.clone()
+        s1 = c.resize(dev(base + new), batch * new)
+        c.resize(dev(base), batch * new)
+        assert torch.equal(c.free[:1 + int(free[0])], free[:1 + int(free[0])]) and torch.equal(c.free[0], free[0])
+        s2 = c.resize(dev(base + new), batch * new)
+        assert torch.equal(s1[0], s2[0]) and torch.equal(s1[1], s2[1]) and int(c.lens.sum()) == int(base.sum()) + batch * new
+        held = table >= 0
+        assert torch.equal(c.table[held], table[held])
+
+
+def test_no_sequences_and_damaged_arrays():
+    """batch 0; lengths, counts, tables and page ids that nothing valid has: no slot outside of the pool comes out."""
+    starts, slots = torch.full((1,), 5, dtype=torch.int32, device=DEV), torch.full((7,), 5, dtype=torch.int32, device=DEV)
+    e = torch.empty(0, dtype=torch.int32, device=DEV)
+    B.iwdft_pages_resize(e, torch.empty((0, 4), dtype=torch.int32, device=DEV), e, dev(np.arange(5, dtype=np.int32)), starts, slots, 16)
+    assert starts.tolist() == [0] and slots.tolist() == [-1] * 7
+    for n_slots in (400, 3000):
+        table = dev(np.array([[9999, -5, 2, 3], [1, 1, 1, 1], [0, 0, 0, 0]], np.int32))
+        lens = dev(np.array([10 ** 9, -7, 33], np.int32))
+        free = dev(np.array([2 ** 30, 77777, -3, 5, 6], np.int32))
+        starts, slots = torch.empty(4, dtype=torch.int32, device=DEV), torch.empty(n_slots, dtype=torch.int32, device=DEV)
+        B.iwdft_pages_resize(dev(np.array([3, 64, 64], np.int32)), table, lens, free, starts, slots, 16)
+        B.iwdft_pages_resize(dev(np.array([64, 0, 1], np.int32)), table, lens, free, starts, slots, 16)
+        s = slots.cpu().numpy()
+        assert ((s >= -1) & (s < 4 * 16)).all() and 0 <= int(free[0]) <= 4
+
+
+# ------------------------------------------------------------------------------------------------------------------ writing
+def run_write(pool, k, v, slots, layer, dtype):
+    dk, dv = dev(k).to(dtype), dev(v).to(dtype)
+    B.iwdft_pages_write(pool.values, pool.exponents, dk, dv, dev(np.asarray(slots, np.int32)), layer)
+    pool.store.write(f64(dk), f64(dv), list(slots), layer)
+
+
+def same_pool(pool):
+    got, ref = pool.values.cpu().numpy(), pool.store.packed()
+    nan = (ref & 127) == 127
+    assert np.array_equal(pool.exponents.cpu().numpy(), pool.store.exponents)
+    assert np.array_equal(nan, (got & 127) == 127) and np.array_equal(got[~nan], ref[~nan])
+
+
+def slots_of(pool, runs):
+    """runs: (sequence, first position, tokens)."""
+    return [int(pool.table[b, p // pool.P]) * pool.P + p % pool.P for b, first, n in runs for p in range(first, first + n)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("P", [16, 32, 64, 128])
+def test_write_prompts_and_single_tokens(P, dtype):
+    rng = np.random.default_rng(P)
+    pool = Pool(rng, [3 * P + 5, 1, 2 * P, 7, 130], P, heads=3, layers=3)
+    runs = [(0, 0, 3 * P + 5), (1, 0, 1), (2, P - 3, P + 3), (3, 6, 1), (4, 100, 30)]
+    slots = slots_of(pool, runs)
+    cut = len(slots) // 2
+    slots[cut:cut] = [-1, -1]                                   # rows of nothing in between
+    slots += [-1, 10 ** 6, -5]
+    k, v = (rng.normal(size=(2, len(slots), 3, 128)) * 2.0 ** rng.integers(-3, 6, size=(1, len(slots), 1, 1)) for _ in range(2))
+    run_write(pool, k, v, slots, 1, DT[dtype])
+    same_pool(pool)
+    for step in range(4):                                       # decode: one token each, louder and quieter
+        lens = [3 * P + step - 8, step, P + step + 3]
+        slots = slots_of(pool, [(0, lens[0], 1), (2, lens[2], 1), (4, 97 + step, 1)])
+        k, v = (rng.normal(size=(3, 3, 3, 128)) * 8.0 ** rng.integers(-3, 4, size=(1, 3, 3, 1)) for _ in range(2))
+        run_write(pool, k, v, slots, 0, DT[dtype])
+        same_pool(pool)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_write_extreme_values(dtype):
+    """Zeros, values next to the border of a scale, ties, the type's largest and smallest, infinities and NaN."""
+    rng = np.random.default_rng(5)
+    pool = Pool(rng, [40, 64], 32, heads=1)
+    n = 40
+    x = rng.normal(size=(1, n, 1, 128)).astype(np.float32)
+    x[0, 0] = 0
+    x[0, 1, 0, :8] = [448, -448, 449, 447.9, 1.75, 1.7500001, 2.0 ** -9, 2.0 ** -10]
+    x[0, 2, 0, :6] = [np.inf, -np.inf, np.nan, -0.0, 3 * 2.0 ** -10, 5 * 2.0 ** -10]
+    x[0, 3] = po.TABLE[rng.integers(0, 126, size=128)] + po.TABLE[rng.integers(0, 126, size=128)]
+    x[0, 33, 0, 5] = np.nan
+    x[0, 34:] *= 2.0 ** -20
+    y = x.copy()
+    y[0, 36, 0, 7] = 3.3e38 if dtype == "f32" else 3.3e38
+    run_write(pool, x, y, slots_of(pool, [(0, 0, n)]), 0, DT[dtype])
+    same_pool(pool)
+    tiny = np.full((1, 20, 1, 128), 2.0 ** -120)
+    run_write(pool, tiny, np.zeros_like(tiny), slots_of(pool, [(1, 0, 20)]), 0, DT[dtype])
+    same_pool(pool)
+    for scale in (2.0 ** -130, 2.0 ** -90, 1.0, 2.0 ** 100):    # a page whose exponent passes through the whole range
+        x = rng.normal(size=(1, 1, 1, 128)) * scale
+        at = 20 + [2.0 ** -130, 2.0 ** -90, 1.0, 2.0 ** 100].index(scale)
+        run_write(pool, x, x, slots_of(pool, [(1, at, 1)]), 0, DT[dtype])
+        same_pool(pool)
+
+
+def test_write_far_into_a_long_pool():
+    """Offsets beyond 32 bits: 5 GB of values, the pages at both ends; neighbours stay."""
+    n_pages, P = 160_000, 128
+    values, exponents = torch.zeros((1, n_pages, 1, 2, P * 128), dtype=torch.uint8, device=DEV), torch.zeros((1, n_pages, 1, 2), dtype=torch.int32, device=DEV)
+    assert values.numel() > 1 << 32
+    rng = np.random.default_rng(3)
+    k, v = (dev(rng.normal(size=(1, 200, 1, 128))).float() for _ in range(2))
+    pages = [n_pages - 1, 140_001]
+    slots = np.array([pages[j // P] * P + j % P for j in range(200)], np.int32)
+    B.iwdft_pages_write(values, exponents, k, v, dev(slots))
+    small = po.Store(1, 2, 1, P)
+    small.write(f64(k), f64(v), list(range(200)))
+    got = values[:, pages].cpu().numpy()
+    ref = small.packed()
+    assert np.array_equal(got, ref) and np.array_equal(exponents[:, pages].cpu().numpy(), small.exponents)
+    assert int((values.view(-1)[:: 1 << 20] != 0).sum()) <= 1 and not values[0, 140_002].any() and not values[0, 0].any()
+    table, lens = dev(np.array([pages], np.int32)), dev(np.array([200], np.int32))
+    K, V = (torch.empty((1, 1, 1, 200, 128), device=DEV) for _ in range(2))
+    B.iwdft_pages_read(values, exponents, table, lens, K, V)
+    rk, rv = small.read(np.array([[0, 1]]), [200], 200, 0, 1)
+    assert np.array_equal(f64(K), rk) and np.array_equal(f64(V), rv)
+    q, out = torch.randn((1, 1, 2, 128), device=DEV), torch.empty((1, 1, 2, 128), device=DEV)
+    B.iwdft_pages_attn(values, exponents, q, dev(np.array([0, 1], np.int32)), table, lens, out)
+    ref, *rest = small.attend(f64(q), [0, 1], np.array([[0, 1]]), [200])
+    near(out, ref, *rest, "f32")
+
+
+# ------------------------------------------------------------------------------------------------------------------ reading
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("P,n", [(16, 1), (16, 43), (32, 70), (64, 64), (128, 137)])
+def test_read(P, n, dtype):
+    rng = np.random.default_rng(P + n)
+    pool = Pool(rng, [n, 0, n // 2, n + 40, 3], P, heads=2, layers=3)
+    pool.table[3, 1] = -1                                       # a page that is not there: its tokens are 0
+    pool.upload()
+    K, V = (torch.full((2, 5, 2, n, 128), float("nan"), device=DEV, dtype=DT[dtype]) for _ in range(2))
+    B.iwdft_pages_read(pool.values, pool.exponents, pool.d_table, pool.d_lens, K, V, 1)
+    ref = pool.store.read(pool.table, pool.lens, n, 1, 2)
+    assert np.array_equal(f64(K), ref[0]) and np.array_equal(f64(V), ref[1])
+    K2 = torch.full_like(K, float("nan"))
+    B.iwdft_pages_read(pool.values, pool.exponents, pool.d_table, pool.d_lens, K2, None, 1)
+    assert torch.equal(K, K2)
+
+
+# ------------------------------------------------------------------------------------------------------------------ attention
+def near(out, ref, weight, reach, seen, floor, dtype):
+    """|out - ref| <= half a step of the result + A * (weights + scores + sums), A = sum p |v|:
+    weights to 11 bits (bf16) or 22, the exponential one step of 2^-23 and its argument; a score errs by 2^-22 (fp32 query in two parts) and by the sums of 128
+    products, 2^-24 each, of sum |q k|, twice (the denominator has it too); the sums over the tokens by 2^-24 for each of the tiles, parts and rescalings.
+    And fp16 ends at 2^-25: a weight 2^lift P_j (lift 6, fp32 15) is off by that much, whatever its size.  With V_j = v_j 2^-e_j as stored, the result is
+    sum P_j V_j / sum P_j 2^-e_j, and the largest P_j, j = *, is at least 1: the denominator at least 2^-e*, the error at most
+    2^(-25 - lift) sum |V_j| / 2^-e*.  (Where the heaviest tokens store zeros in a channel, as small channels of a page do, nothing else is left.)"""
+    got = f64(out)
+    rows = ~np.isnan(ref).all(axis=(0, 2, 3)) if not np.isnan(weight).any() else np.ones(ref.shape[1], bool)
+    got, ref, weight, reach, seen, floor = (x[:, rows] for x in (got, ref, weight, reach, seen, floor))
+    assert np.array_equal(np.isnan(got), np.isnan(ref))
+    step, bits = (2.0 ** -8, 2.0 ** -11) if dtype == "bf16" else (2.0 ** -24, 2.0 ** -22)
+    # 1.45: log2 e, in which scores are taken
+    score = (2.0 ** -22 + 140 * 2.0 ** -24) * reach * 1.45 + 2.0 ** -22
+    rel = bits + 2 * score + (seen / 32 + 100) * 2.0 ** -24
+    bound = step * np.abs(ref) + (rel[..., None] * weight + 2.0 ** (-25 - (6 if dtype == "bf16" else 15)) * floor) * (1 + step) + 1e-30
+    err = np.abs(got - ref)
+    ok = ~(err > bound) | np.isnan(ref)
+    assert ok.all(), (float(np.nanmax(err / bound)), np.argwhere(~ok)[:5].tolist())
+
+
+def attend(pool, rng, news, G, dtype, layer=0, layers=1, pad=0, q_scale=1.0, q=None, **kw):
+    heads = pool.store.raw.shape[2]
+    starts = np.concatenate([[0], np.cumsum(news)]).astype(np.int32)
+    n = int(starts[-1]) + pad
+    q = dev(rng.normal(size=(layers, n, heads * G, 128)) * q_scale).to(DT[dtype]) if q is None else q
+    out = torch.full_like(q, 7.0)
+    B.iwdft_pages_attn(pool.values, pool.exponents, q, dev(starts), pool.d_table, pool.d_lens, out, layer, **kw)
+    args = {k: v for k, v in kw.items() if k in ("n_sink", "n_recent")}
+    ref, *rest = pool.store.attend(f64(q), starts, pool.table, pool.lens, layer, scale=kw.get("scale") or None, **args)
+    if pad:
+        assert (out[:, starts[-1]:] == 7.0).all()
+        ref, out = ref[:, :starts[-1]], out[:, :starts[-1]]
+        rest = [r[:, :starts[-1]] for r in rest]
+    near(out, ref, *rest, dtype)
+    return out
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("P", [16, 32, 64, 128])
+@pytest.mark.parametrize("lens", [[1], [31, 32, 33], [0, 200, 5, 127, 128, 129], [700]])
+def test_attention_single_tokens(lens, P, dtype):
+    rng = np.random.default_rng(sum(lens) + P)
+    attend(Pool(rng, lens, P), rng, [1 if n else 0 for n in lens], 4, dtype, pad=2)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("G,heads", [(1, 1), (2, 3), (3, 2), (8, 1), (16, 1), (20, 1), (64, 1)])
+def test_attention_heads(G, heads, dtype):
+    rng = np.random.default_rng(G)
+    attend(Pool(rng, [150, 40], 32, heads=heads, layers=2), rng, [2, 1], G, dtype, layer=1)
+    attend(Pool(rng, [70], 16, heads=heads, layers=3), rng, [1], G, dtype, layer=1, layers=2)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("lens,news,G", [
+    ([5, 64, 33], [5, 64, 33], 4), ([300, 80, 0, 9], [37, 1, 0, 9], 3), ([200], [200], 1), ([190], [190], 8), ([513, 260], [129, 1], 4), ([90, 90], [17, 70], 2), ([40] * 70, [1] * 69 + [40], 2),
+])
+def test_attention_drafts_and_prompts(lens, news, G, dtype):
+    rng = np.random.default_rng(len(lens) + G)
+    attend(Pool(rng, lens, 16 if G % 2 else 64, heads=2), rng, news, G, dtype, pad=1)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("sink,recent", [(0, 1), (0, 40), (10, 50), (33, 64), (1, 1), (64, 1000), (500, 3), (0, 2 ** 31 - 1), (2 ** 31 - 1, 5)])
+def test_attention_windows(sink, recent, dtype):
+    rng = np.random.default_rng(sink % 1000 + recent % 1000)
+    attend(Pool(rng, [400, 61, 12, 300], 32), rng, [1, 7, 12, 90], 2, dtype, n_sink=sink, n_recent=recent)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_attention_rows_before_the_first_token(dtype):
+    """More new tokens than the sequence is long: the first ones see nothing and are 0; scale and padding rows."""
+    rng = np.random.default_rng(8)
+    pool = Pool(rng, [3, 0, 40], 16)
+    out = attend(pool, rng, [8, 4, 1], 2, dtype, pad=3, scale=0.3)
+    assert not out[:, :5].any() and not out[:, 8:12].any() and out[:, 5:8].all(dim=-1).any()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_attention_does_not_see_what_is_masked(dtype):
+    """NaN and the largest values behind a sequence's end, outside the window, in pages of nobody and in tokens that only later rows see; NaN that
+    a row sees is its own."""
+    rng = np.random.default_rng(9)
+    for news, kw in (([1, 1], {}), ([6, 40], {}), ([6, 40], dict(n_sink=5, n_recent=20)), ([1, 1], dict(n_sink=3, n_recent=20)), ([60, 110], dict(n_sink=0, n_recent=40))):
+        pool = Pool(rng, [75, 110], 32, heads=2)
+        hidden = rng.integers(0, 2, size=pool.store.raw.shape[1:3])
+        raw = pool.store.raw
+        for b in (0, 1):
+            n = int(pool.lens[b])
+            raw[0, pool.table[b, (n - 1) // 32], :, :, n % 32 or 32:] = 0x7f                       # behind the end
+            if kw.get("n_recent") == 20:
+                raw[0, pool.table[b, 0], :, :, kw["n_sink"]:30] = 0xff                                   # between sinks and window of every row
+        raw[0, pool.table[1, 109 // 32], 1, 1, 109 % 32, 40] = 0x7f                                     # V, the last token: the last row sees it
+        raw[0, pool.table[0, 72 // 32], 0, 0, 72 % 32, 3] = 0x7f                                        # K, token 72
+        del hidden
+        pool.upload()
+        out = attend(pool, rng, news, 2, dtype, **kw)
+        nan = torch.isnan(out.float())
+        last = sum(news) - 1
+        assert nan[0, last, 2:4, 40].all() and int(nan[0, last].sum()) == 2  # heads 2, 3 read KV head 1
+        assert nan[0, news[0] - 1, :2].all() and not nan[0, news[0] - 1, 2:].any()
+        if news[0] == 6:
+            assert not nan[0, :3].any() and nan[0, 3:6, :2].all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_attention_queries_that_are_not_finite_stay_in_their_row(dtype):
+    rng = np.random.default_rng(10)
+    pool = Pool(rng, [100], 32, heads=1)
+    q = torch.randn((1, 5, 2, 128), device=DEV).to(DT[dtype])
+    q[0, 1, 0, 7], q[0, 3, 1, 0] = float("nan"), float("inf")
+    out, ref = torch.empty_like(q), torch.empty_like(q)
+    starts = dev(np.array([0, 5], np.int32))
+    B.iwdft_pages_attn(pool.values, pool.exponents, q, starts, pool.d_table, pool.d_lens, out)
+    q2 = torch.nan_to_num(q, nan=0.0, posinf=0.0)
+    B.iwdft_pages_attn(pool.values, pool.exponents, q2, starts, pool.d_table, pool.d_lens, ref)
+    bad = torch.isnan(out.float()).any(-1)
+    assert bad.nonzero().tolist() == [[0, 1, 0], [0, 3, 1]] and torch.equal(out[~bad], ref[~bad])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_attention_of_far_apart_scales(dtype):
+    """Pages whose K or V are 2^40 times as large as others', queries from 2^-60 to 2^30: no weight overflows, none of the small pages' bits are lost."""
+    rng = np.random.default_rng(11)
+    P, n = 16, 160
+    pool = Pool(rng, [n], P, heads=1, stale=False)
+    for j in range(n // P):
+        k = rng.normal(size=(1, P, 1, 128)) * (2.0 ** -30 if j % 3 == 1 else 1.0)
+        v = rng.normal(size=(1, P, 1, 128)) * 2.0 ** ((-90, 0, 40, -40)[j % 4])
+        pool.store.write(k, v, [int(pool.table[0, j]) * P + i for i in range(P)])
+    pool.upload()
+    for scale in (1.0, 2.0 ** -60, 30.0, 2.0 ** 30):
+        attend(pool, rng, [3], 3, dtype, q_scale=scale)
+    # one page only, of tiny values: the result is tiny and as exact as any
+    pool.lens[0] = P
+    pool.upload()
+    out = attend(pool, rng, [3], 3, dtype)
+    assert 0 < float(out.abs().max()) < 2.0 ** -80
+
+
+def test_attention_of_pages_that_are_not_there():
+    """Table entries outside the pool hold no tokens; a sequence of none but these is 0."""
+    rng = np.random.default_rng(12)
+    pool = Pool(rng, [100, 40, 200], 16)
+    pool.table[0, 1], pool.table[0, 4], pool.table[2, 12] = -1, 10 ** 6, pool.store.raw.shape[1]
+    pool.table[1] = -3
+    pool.upload()
+    out = attend(pool, rng, [2, 1, 9], 2, "bf16")
+    assert not out[:, 2].any()
+
+
+def test_attention_of_damaged_lengths_and_starts():
+    """Nothing that they say reaches memory outside the arrays; rows of no sequence stay."""
+    rng = np.random.default_rng(13)
+    pool = Pool(rng, [100, 40, 64], 16)
+    q, out = (torch.full((1, 6, 4, 128), 3.0, dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    B.iwdft_pages_attn(pool.values, pool.exponents, q, dev(np.array([5, 2, 2, 900], np.int32)), pool.d_table, dev(np.array([50, -9, 10 ** 9], np.int32)), out)
+    assert (out[:, :2] == 3.0).all() and torch.isfinite(out.float()).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("lens,news,G,P", [([5000], [1], 4, 16), ([20000, 3], [3, 1], 1, 128), ([9000], [90], 2, 32), ([6000, 800], [1, 300], 2, 64)])
+def test_attention_of_long_sequences_in_parts(lens, news, G, P, dtype):
+    rng = np.random.default_rng(sum(lens))
+    attend(Pool(rng, lens, P, heads=1), rng, news, G, dtype)
+    if lens[0] < 9000:
+        attend(Pool(rng, lens, P, heads=1), rng, news, G, dtype, n_sink=40, n_recent=2500)
+
+
+# ------------------------------------------------------------------------------------------------------------------ together
+def test_a_served_batch_from_prompt_to_frequency_domain():
+    """Prompts, drafts that are partly taken back, single tokens, a request that ends and one that takes its pages, and the hand-over to iwdft_prefill."""
+    rng = np.random.default_rng(14)
+    L, H, G, P, n, NB = 2, 2, 2, 32, 3, 26
+    c = B.PagedCache(L, NB, H, H * G, 128, torch.bfloat16, n, 400, P, DEV)
+    store, table, lens = po.Store(L, NB, H, P), np.full((n, c.table.shape[1]), -1, np.int32), np.zeros(n, np.int32)
+    free = np.concatenate([[NB], np.arange(NB)]).astype(np.int32)
+    steps = [[70, 130, 0], [73, 134, 5], [71, 134, 6], [72, 135, 7], [0, 136, 8], [300, 137, 9], [301, 138, 10], [302, 300, 300], [256 + 9, 256 + 9, 256 + 9]]
+    for i, want in enumerate(steps):
+        want = np.array(want, np.int32)
+        starts, slots = c.resize(dev(want), 700)
+        r_starts, r_slots = po.resize(want, table, lens, free, 700, P)
+        assert np.array_equal(starts.cpu().numpy(), r_starts) and np.array_equal(slots.cpu().numpy(), r_slots) and np.array_equal(c.lens.cpu().numpy(), lens)
+        m = int(r_starts[-1]) + 2
+        k, v = (torch.randn((L, m, H, 128), device=DEV, dtype=torch.bfloat16) for _ in range(2))
+        q = torch.randn((L, m, H * G, 128), device=DEV, dtype=torch.bfloat16)
+        for layer in range(L):  # as a model goes through them
+            c.write(k[layer:layer + 1], v[layer:layer + 1], slots[:m].contiguous(), layer)
+            out = c.attend(q[layer:layer + 1], starts, layer)
+            store.write(f64(k[layer:layer + 1]), f64(v[layer:layer + 1]), list(r_slots[:m]), layer)
+            ref, *rest = store.attend(f64(q[layer:layer + 1]), r_starts, table, lens, layer)
+            near(out[:, :-2], ref[:, :-2], *[x[:, :-2] for x in rest], "bf16")
+            assert not out[:, -2:].any()
+    bins = [np.arange(40, dtype=np.int32)] * L
+    cache = B.Cache(L, n, H, H * G, 128, torch.bfloat16, 256, bins, device=DEV, n_sink=4, n_recent=5)
+    c.compress(cache)
+    K, V = store.read(table, lens, 265, 0, L)
+    for layer in range(L):
+        SK, SV = cache.export_coeffs(layer)
+        for b in range(n):
+            for h in range(H):
+                for got, x in ((SK, K), (SV, V)):
+                    want = orc.prefill(x[layer, b, h, 4:260], bins[layer])
+                    assert np.linalg.norm(got[b, h].cpu().numpy() - want) <= 1e-4 * np.linalg.norm(want)
+    q = torch.randn((L, n, H * G, 128), device=DEV, dtype=torch.bfloat16)
+    assert torch.isfinite(cache.attend(q).float()).all()
+    with pytest.raises(ValueError):
+        c.compress(B.Cache(L, 1, H, H * G, 128, torch.bfloat16, 256, bins, device=DEV))
+    cache.close()
+
+
+def test_a_step_in_a_captured_graph():
+    """Tables, writing and attention of a decode step captured once and replayed, every replay against eager calls on a copy, with eager work between."""
+    H, G, P, n, L = 2, 4, 16, 5, 2
+    mk = lambda: B.PagedCache(L, 700, H, H * G, 128, torch.bfloat16, n, 2100, P, DEV)  # noqa: E731
+    a, b = mk(), mk()
+    gen = torch.Generator(DEV).manual_seed(4)
+    rnd = lambda *s: torch.randn(s, generator=gen, device=DEV).to(torch.bfloat16)  # noqa: E731
+    first = dev(np.array([2000, 1, 17, 0, 900], np.int32))
+    k, v = rnd(L, 2918, H, 128), rnd(L, 2918, H, 128)
+    for c in (a, b):
+        _, slots = c.resize(first, 2918)
+        c.write(k, v, slots)
+    want, k1, v1, q1 = first.clone(), rnd(L, n, H, 128), rnd(L, n, H, 128), rnd(L, n, H * G, 128)
+    out = torch.zeros_like(q1)
+
+    def step(c, out):
+        starts, slots = c.resize(want, n)
+        c.write(k1, v1, slots)
+        c.attend(q1, starts, out=out)
+    step(a, out), step(b, out)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        step(a, out)
+    for i in range(6):
+        want.copy_(torch.where(torch.arange(n, device=DEV) == i % n, want, want + 1))
+        if i == 4:
+            want[1] = 0
+        for x in (k1, v1, q1):
+            x.copy_(rnd(*x.shape))
+        ref = torch.zeros_like(q1)
+        step(b, ref)
+        torch.cuda.synchronize()
+        out.fill_(0)
+        g.replay()
+        torch.cuda.synchronize()
+        for x, y in ((out, ref), (a.values, b.values), (a.exponents, b.exponents), (a.table, b.table), (a.lens, b.lens), (a.free, b.free)):
+            assert torch.equal(x, y), i
+
+
+def test_two_calls_at_once_and_a_workspace_of_the_caller():
+    rng = np.random.default_rng(15)
+    pools = [Pool(rng, [3000], 32, heads=1) for _ in range(2)]
+    qs = [torch.randn((1, 2, 8, 128), device=DEV, dtype=torch.bfloat16) for _ in range(2)]
+    starts = dev(np.array([0, 2], np.int32))
+    call = lambda i, out, **kw: B.iwdft_pages_attn(pools[i].values, pools[i].exponents, qs[i], starts, pools[i].d_table, pools[i].d_lens, out, **kw)  # noqa: E731
+    refs = [torch.empty_like(q) for q in qs]
+    call(0, refs[0]), call(1, refs[1])
+    need = B.iwdft_pages_attn_bytes(B.pages_desc(1, pools[0].values.shape[1], 1, 8, 128, 32, pools[0].table.shape[1]), 1, 1, 2)
+    ws = torch.empty(need, dtype=torch.uint8, device=DEV)
+    out = torch.empty_like(qs[0])
+    call(0, out, workspace=ws)
+    assert torch.equal(out, refs[0])
+    with pytest.raises(B.IwdftError) as e:
+        call(0, out, workspace=ws[:need - 256])
+    assert e.value.code == B.IWDFT_ERR_SIZE
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    outs = [[torch.zeros_like(qs[i]) for _ in range(20)] for i in range(2)]
+    torch.cuda.synchronize()
+    for r in range(20):
+        for i in range(2):
+            call(i, outs[i][r], stream=streams[i] if r % 2 else streams[i].cuda_stream)
+    torch.cuda.synchronize()
+    for i in range(2):
+        for o in outs[i]:
+            assert torch.equal(o, refs[i])
