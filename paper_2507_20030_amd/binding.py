@@ -421,16 +421,23 @@ def _expect(name: str, t: torch.Tensor, dtype, shape, device) -> None:
         raise ValueError(f"{name} must be contiguous")
 
 
+def _fits(t: torch.Tensor, dtype, shape, device) -> bool:
+    return t.dtype is dtype and t.shape == shape and t.device == device and t.is_contiguous()
+
+
 def _pool_sizes(values: torch.Tensor, exponents: torch.Tensor):
-    """(layers, pages, KV heads, page tokens); the device is a GPU."""
-    if values.dim() != 5 or values.shape[3] != 2 or values.shape[4] % 128:
-        raise ValueError(f"values has shape {tuple(values.shape)}, not (layers, pages, heads, 2, 128 * page tokens)")
-    if not values.is_cuda:
+    """(device, layers, pages, KV heads, page tokens); the device is a GPU."""
+    shape = values.shape
+    if len(shape) != 5 or shape[3] != 2 or shape[4] % 128:
+        raise ValueError(f"values has shape {tuple(shape)}, not (layers, pages, heads, 2, 128 * page tokens)")
+    device = values.device
+    if device.type != "cuda":
         raise ValueError("values must be device memory")
-    n_layers, n_pages, heads, _, row = values.shape
-    _expect("values", values, torch.uint8, values.shape, values.device)
-    _expect("exponents", exponents, torch.int32, (n_layers, n_pages, heads, 2), values.device)
-    return n_layers, n_pages, heads, row // 128
+    n_layers, n_pages, heads, _, row = shape
+    if not (values.dtype is torch.uint8 and values.is_contiguous() and _fits(exponents, torch.int32, (n_layers, n_pages, heads, 2), device)):
+        _expect("values", values, torch.uint8, shape, device)
+        _expect("exponents", exponents, torch.int32, (n_layers, n_pages, heads, 2), device)
+    return device, n_layers, n_pages, heads, row // 128
 
 
 def _kv_dtype(name: str, t: torch.Tensor):
@@ -441,9 +448,14 @@ def _kv_dtype(name: str, t: torch.Tensor):
 
 def _run_on(device: torch.device, stream, call, *args) -> None:
     """The call with the tensors' device as the current one, on its current stream unless one is given."""
-    here = device.index == torch.cuda.current_device()
-    with contextlib.nullcontext() if here else torch.cuda.device(device):
-        _check(call(*args, _stream(stream)))
+    raw = torch._C._cuda_getCurrentRawStream(device.index) if stream is None else _stream(stream)
+    if device.index == torch.cuda.current_device():
+        rc = call(*args, raw)
+    else:
+        with torch.cuda.device(device):
+            rc = call(*args, raw)
+    if rc != IWDFT_OK:
+        _check(rc)
 
 
 def _on_stream(stream, device):
@@ -454,82 +466,93 @@ def _on_stream(stream, device):
 
 
 def _scratch(n_bytes: int, device: torch.device, stream, workspace):
-    """The caller's workspace or memory of this call alone, kept until the call's stream is past it (it is allocated in that stream's order)."""
-    if workspace is None and n_bytes:
+    """The caller's workspace, or memory of this call alone that is allocated and freed in the order of the call's stream."""
+    if workspace is None:
+        if not n_bytes:
+            return None
+        if stream is None:
+            return torch.empty(n_bytes, dtype=torch.uint8, device=device)
         with _on_stream(stream, device):
-            workspace = torch.empty(n_bytes, dtype=torch.uint8, device=device)
-    elif workspace is not None and workspace.device != device:
-        raise ValueError(f"workspace is on {workspace.device}, not on {device}")
-    return _ptr(workspace), (workspace.numel() * workspace.element_size() if workspace is not None else 0)
+            return torch.empty(n_bytes, dtype=torch.uint8, device=device)
+    if workspace.device != device or not workspace.is_contiguous():
+        raise ValueError(f"workspace must be contiguous and on {device}, not on {workspace.device}")
+    return workspace
 
 
 def iwdft_pages_resize(want, table, lens, free, starts, slots, page_tokens: int, stream=None, workspace=None) -> None:
     """Brings the sequences to want[b] tokens (negative: as they are): table, lens, free, starts and slots are brought up to date."""
-    if table.dim() != 2 or not table.is_cuda:
-        raise ValueError(f"table must be a device tensor [batch, max_pages], not {tuple(table.shape)} on {table.device}")
-    batch, max_pages = table.shape
-    device = table.device
-    for name, t, shape in (("table", table, (batch, max_pages)), ("want", want, (batch,)), ("lens", lens, (batch,)), ("free", free, (None,)),
-                           ("starts", starts, (batch + 1,)), ("slots", slots, (None,))):
-        _expect(name, t, torch.int32, shape, device)
-    n_slots = slots.shape[0]
-    ws, ws_bytes = _scratch(_resize_bytes(batch, n_slots), device, stream, workspace)
-    _run_on(device, stream, load_library().iwdft_pages_resize, page_tokens, free.shape[0] - 1, max_pages, want.data_ptr(), batch, table.data_ptr(),
-            lens.data_ptr(), free.data_ptr(), starts.data_ptr(), slots.data_ptr(), n_slots, ws, ws_bytes)
+    device, shape = table.device, table.shape
+    if len(shape) != 2 or device.type != "cuda":
+        raise ValueError(f"table must be a device tensor [batch, max_pages], not {tuple(shape)} on {device}")
+    batch, max_pages = shape
+    n_free, n_slots = free.numel(), slots.numel()
+    for name, t, size in (("table", table, shape), ("want", want, (batch,)), ("lens", lens, (batch,)), ("free", free, (n_free,)), ("starts", starts, (batch + 1,)),
+                          ("slots", slots, (n_slots,))):
+        if not _fits(t, torch.int32, size, device):
+            _expect(name, t, torch.int32, size, device)
+    ws = _scratch(_resize_bytes(batch, n_slots), device, stream, workspace)
+    _run_on(device, stream, load_library().iwdft_pages_resize, page_tokens, n_free - 1, max_pages, want.data_ptr(), batch, table.data_ptr(), lens.data_ptr(),
+            free.data_ptr(), starts.data_ptr(), slots.data_ptr(), n_slots, ws.data_ptr() if ws is not None else None, ws.nbytes if ws is not None else 0)
 
 
 def iwdft_pages_write(values, exponents, k, v, slots, layer: int = 0, stream=None) -> None:
     """k, v [layers written, tokens, KV heads, 128] into layers layer, layer + 1, ... at slots."""
-    n_layers, n_pages, heads, P = _pool_sizes(values, exponents)
-    dtype, device = _kv_dtype("k", k), values.device
-    _expect("slots", slots, torch.int32, (None,), device)
-    n = slots.shape[0]
-    _expect("k", k, dtype, (None, n, heads, 128), device)
-    _expect("v", v, dtype, k.shape, device)
-    if k.shape[0] == 0:
+    device, n_layers, n_pages, heads, P = _pool_sizes(values, exponents)
+    dtype, n, shape = _kv_dtype("k", k), slots.numel(), k.shape
+    if not (_fits(slots, torch.int32, (n,), device) and _fits(k, dtype, (*shape[:1], n, heads, 128), device) and _fits(v, dtype, shape, device)):
+        _expect("slots", slots, torch.int32, (n,), device)
+        _expect("k", k, dtype, (None, n, heads, 128), device)
+        _expect("v", v, dtype, shape, device)
+    if shape[0] == 0:
         return
     desc = _pages_desc(n_layers, n_pages, heads, heads, 128, P, 1, dtype)
-    _run_on(device, stream, load_library().iwdft_pages_write, ctypes.byref(desc), layer, k.shape[0], k.data_ptr(), v.data_ptr(), slots.data_ptr(), n,
+    _run_on(device, stream, load_library().iwdft_pages_write, ctypes.byref(desc), layer, shape[0], k.data_ptr(), v.data_ptr(), slots.data_ptr(), n,
             values.data_ptr(), exponents.data_ptr())
 
 
 def iwdft_pages_attn(values, exponents, q, starts, table, lens, out, layer: int = 0, n_sink: int = 0, n_recent: int = 0, scale: float = 0.0, stream=None,
                      workspace=None) -> None:
     """q, out [layers, tokens, query heads, 128]: the new tokens' attention over their sequences in layers layer, layer + 1, ..."""
-    n_layers, n_pages, heads, P = _pool_sizes(values, exponents)
-    dtype, device = _kv_dtype("q", q), values.device
-    _expect("q", q, dtype, (None, None, None, 128), device)
-    _expect("out", out, dtype, q.shape, device)
-    _expect("table", table, torch.int32, (None, None), device)
-    batch, max_pages = table.shape
-    _expect("lens", lens, torch.int32, (batch,), device)
-    _expect("starts", starts, torch.int32, (batch + 1,), device)
-    if q.shape[0] == 0:
+    device, n_layers, n_pages, heads, P = _pool_sizes(values, exponents)
+    dtype, shape, size = _kv_dtype("q", q), q.shape, table.shape
+    if len(shape) != 4 or len(size) != 2 or not (_fits(q, dtype, (*shape[:3], 128), device) and _fits(out, dtype, shape, device) and _fits(table, torch.int32, size, device)
+                                                 and _fits(lens, torch.int32, size[:1], device) and _fits(starts, torch.int32, (size[0] + 1,), device)):
+        _expect("q", q, dtype, (None, None, None, 128), device)
+        _expect("out", out, dtype, shape, device)
+        _expect("table", table, torch.int32, (None, None), device)
+        _expect("lens", lens, torch.int32, size[:1], device)
+        _expect("starts", starts, torch.int32, (size[0] + 1,), device)
+    n, n_tokens, n_q_heads, _ = shape
+    batch, max_pages = size
+    if n == 0:
         return
-    sizes = (n_layers, n_pages, heads, q.shape[2], 128, P, max_pages, dtype)
-    ws, ws_bytes = _scratch(_attn_bytes(q.shape[0], batch, q.shape[1], *sizes), device, stream, workspace)
-    _run_on(device, stream, load_library().iwdft_pages_attn, ctypes.byref(_pages_desc(*sizes)), layer, q.shape[0], q.data_ptr(), starts.data_ptr(), q.shape[1],
-            table.data_ptr(), lens.data_ptr(), batch, values.data_ptr(), exponents.data_ptr(), out.data_ptr(), n_sink, n_recent, scale, ws, ws_bytes)
+    sizes = (n_layers, n_pages, heads, n_q_heads, 128, P, max_pages, dtype)
+    ws = _scratch(_attn_bytes(n, batch, n_tokens, *sizes), device, stream, workspace)
+    _run_on(device, stream, load_library().iwdft_pages_attn, ctypes.byref(_pages_desc(*sizes)), layer, n, q.data_ptr(), starts.data_ptr(), n_tokens,
+            table.data_ptr(), lens.data_ptr(), batch, values.data_ptr(), exponents.data_ptr(), out.data_ptr(), n_sink, n_recent, scale,
+            ws.data_ptr() if ws is not None else None, ws.nbytes if ws is not None else 0)
 
 
 def iwdft_pages_read(values, exponents, table, lens, K, V, layer: int = 0, stream=None) -> None:
     """K, V [layers, batch, KV heads, tokens, 128] (either may be None) from the first tokens of every sequence; 0 where it has fewer."""
-    n_layers, n_pages, heads, P = _pool_sizes(values, exponents)
-    device, some = values.device, K if K is not None else V
+    device, n_layers, n_pages, heads, P = _pool_sizes(values, exponents)
+    some = K if K is not None else V
     if some is None:
         return
-    dtype = _kv_dtype("K or V", some)
-    _expect("table", table, torch.int32, (None, None), device)
-    batch, max_pages = table.shape
-    _expect("lens", lens, torch.int32, (batch,), device)
-    for name, t in (("K", K), ("V", V)):
-        if t is not None:
-            _expect(name, t, dtype, (some.shape[0], batch, heads, some.shape[3] if some.dim() == 5 else None, 128), device)
-    if some.shape[0] == 0:
+    dtype, shape, size = _kv_dtype("K or V", some), some.shape, table.shape
+    full = (*shape[:1], *size[:1], heads, *shape[3:4], 128)
+    if not (len(size) == 2 and _fits(table, torch.int32, size, device) and _fits(lens, torch.int32, size[:1], device)
+            and (K is None or _fits(K, dtype, full, device)) and (V is None or _fits(V, dtype, full, device))):
+        _expect("table", table, torch.int32, (None, None), device)
+        _expect("lens", lens, torch.int32, size[:1], device)
+        for name, t in (("K", K), ("V", V)):
+            if t is not None:
+                _expect(name, t, dtype, (shape[0], size[0], heads, shape[3] if len(shape) == 5 else None, 128), device)
+    if shape[0] == 0:
         return
-    desc = _pages_desc(n_layers, n_pages, heads, heads, 128, P, max_pages, dtype)
-    _run_on(device, stream, load_library().iwdft_pages_read, ctypes.byref(desc), layer, some.shape[0], table.data_ptr(), lens.data_ptr(), batch,
-            some.shape[3], values.data_ptr(), exponents.data_ptr(), _ptr(K), _ptr(V))
+    desc = _pages_desc(n_layers, n_pages, heads, heads, 128, P, size[1], dtype)
+    _run_on(device, stream, load_library().iwdft_pages_read, ctypes.byref(desc), layer, shape[0], table.data_ptr(), lens.data_ptr(), size[0], shape[3],
+            values.data_ptr(), exponents.data_ptr(), K.data_ptr() if K is not None else None, V.data_ptr() if V is not None else None)
 
 
 class PagedCache:

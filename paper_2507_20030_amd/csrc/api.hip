@@ -1206,7 +1206,7 @@ int iwdft_pages_attn_bytes(const iwdft_pages_desc* desc, int32_t n_layers, int32
   const int rc = check_pages(desc, 0, n_layers);
   if (rc != IWDFT_OK) return rc;
   if (batch < 0 || n_tokens < 0) return fail(IWDFT_ERR_ARG, "batch = %d, n_tokens = %d: negative", batch, n_tokens);
-  *workspace_bytes = pages_attn_bytes(pages_of(*desc, nullptr, nullptr), n_layers, batch, n_tokens, desc->kv_dtype == IWDFT_BF16);
+  *workspace_bytes = pages_attn_bytes(pages_of(*desc, nullptr, nullptr), batch, n_tokens, desc->kv_dtype == IWDFT_BF16);
   return IWDFT_OK;
 }
 

@@ -22,7 +22,6 @@ namespace iwdft {
 namespace {
 
 constexpr int kWave = 64;
-constexpr int kTile = 32;    // tokens of a step
 constexpr int kWaves = 4;
 template <bool BF16>
 struct Weights {
@@ -36,18 +35,29 @@ constexpr int kQTop = 14;    // q rows: largest value in [2^14, 2^15)
 // works out the shares by itself (64 sequences at a time): the launch only has to be large enough.
 constexpr int kParts = 512;
 constexpr int kLeastTiles = 4;
+constexpr int kFewRows = 64;  // sequences of up to so many rows go to pages_few_kernel, where a call has both
+
+template <int ROWS, int TOKENS>
+struct Geometry {
+  static constexpr int rows = ROWS, tile = TOKENS;  // of a block; of a tile
+};
+template <int R>
+using Few = Geometry<16 * R, 32>;
+using Many = Geometry<128, 64>;
 
 struct Seq {
   int len, first, nq, rows, tiles;  // tokens, first new token (row of q), new tokens, rows of all blocks, most tiles of a block
 };
 
-template <int BR>
+template <class Geo>
 __device__ __forceinline__ Seq seq_of(const PagesAttn& a, int b) {
+  constexpr int BR = Geo::rows, kTile = Geo::tile;
   Seq s;
   s.len = min(max(a.lens[b], 0), a.S.max_pages << a.S.logP);
   s.first = min(max(a.starts[b], 0), a.n_tokens);
   s.nq = min(max(a.starts[b + 1], s.first), a.n_tokens) - s.first;
   s.rows = s.nq * a.S.G;
+  if (s.rows <= a.rows_over || s.rows > a.rows_to) s.nq = s.rows = 0;
   s.tiles = (s.len + kTile - 1) / kTile;
   if (a.n_recent) {
     const int sink = (min(a.n_sink, s.len) + kTile - 1) / kTile;
@@ -78,13 +88,13 @@ __device__ __forceinline__ float wave_sum(float x) {
   return x;
 }
 
-template <int BR>
+template <class Geo>
 __device__ Shares shares_of(const PagesAttn& a, int lane) {
   float sum = 0.f;  // every wave adds in the same order: all agree
   for (int b0 = 0; b0 < a.batch; b0 += kWave)
     if (b0 + lane < a.batch) {
-      const Seq s = seq_of<BR>(a, b0 + lane);
-      sum += (float)s.tiles * (float)blocks_of(s.rows, BR);
+      const Seq s = seq_of<Geo>(a, b0 + lane);
+      sum += (float)s.tiles * (float)blocks_of(s.rows, Geo::rows);
     }
   sum = wave_sum(sum) * (float)(a.n_layers * a.S.H);
   Shares w;
@@ -92,8 +102,8 @@ __device__ Shares shares_of(const PagesAttn& a, int lane) {
   w.parts = w.split = w.split_rows = 0;
   for (int b0 = 0; b0 < a.batch; b0 += kWave)
     if (b0 + lane < a.batch) {
-      const Seq s = seq_of<BR>(a, b0 + lane);
-      const int np = parts_of(s, w.tiles), n = np * blocks_of(s.rows, BR);
+      const Seq s = seq_of<Geo>(a, b0 + lane);
+      const int np = parts_of(s, w.tiles), n = np * blocks_of(s.rows, Geo::rows);
       w.parts += n;
       if (np > 1) w.split += n, w.split_rows += s.rows;
     }
@@ -107,17 +117,17 @@ struct Place {
   int b, at, before, np;
   Seq s;
 };
-template <int BR, class Count>
+template <class Geo, class Count>
 __device__ Place place_of(const PagesAttn& a, const Shares& w, int y, int lane, Count count) {
   int done = 0, cut = 0;
   for (int b0 = 0;; b0 += kWave) {
     Seq s{0, 0, 0, 0, 0};
     int np = 0, n = 0, c = 0;
     if (b0 + lane < a.batch) {
-      s = seq_of<BR>(a, b0 + lane);
+      s = seq_of<Geo>(a, b0 + lane);
       np = parts_of(s, w.tiles);
       n = count(s, np);
-      c = np > 1 ? np * blocks_of(s.rows, BR) : 0;
+      c = np > 1 ? np * blocks_of(s.rows, Geo::rows) : 0;
     }
     int in = n, cin = c;
 #pragma unroll
@@ -192,6 +202,7 @@ struct Span {
   int sinks, skip, n;
   __device__ __forceinline__ int tile(int i) const { return i < sinks ? i : i + skip; }
 };
+template <int kTile>
 __device__ __forceinline__ Span span_of(const PagesAttn& a, int p_lo, int p_hi) {  // positions of the block's first and last token
   Span s{0, 0, 0};
   if (p_hi < 0) return s;
@@ -221,23 +232,24 @@ struct Rows {
 // with row l % 16 and the 8 tokens of octet l / 16, which is how O^T = V^T P^T wants them, so nothing moves between lanes but the maximum.
 template <bool BF16, int R>
 __global__ __launch_bounds__(kWaves* kWave) void pages_few_kernel(PagesAttn a) {
-  constexpr int PARTS = BF16 ? 1 : 2, BR = 16 * R;
+  using Geo = Few<R>;
+  constexpr int PARTS = BF16 ? 1 : 2, BR = Geo::rows, kTile = Geo::tile;
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
   const int row = lane & 15, oct = lane >> 4;
   __shared__ __attribute__((aligned(16))) float join[2][BR][kHeadDim + 4];
   __shared__ float2 join_stat[2][BR];
 
-  const Shares w = shares_of<BR>(a, lane);
+  const Shares w = shares_of<Geo>(a, lane);
   const int64_t all = (int64_t)w.parts * a.n_layers * a.S.H;
   for (int64_t x = blockIdx.x; x < all; x += gridDim.x) {
-    const int lh = (int)(x / w.parts);
-    const Place at = place_of<BR>(a, w, (int)(x % w.parts), lane, [](const Seq& s, int np) { return np * blocks_of(s.rows, BR); });
+    const int lh = (int)(x % (a.n_layers * a.S.H));  // workgroups are dealt to the XCDs in turn: with 8 heads each reads one head's pages
+    const Place at = place_of<Geo>(a, w, (int)(x / (a.n_layers * a.S.H)), lane, [](const Seq& s, int np) { return np * blocks_of(s.rows, Geo::rows); });
     const Seq s = at.s;
-    const int block = at.at / at.np, part = at.at % at.np, layer = lh / a.S.H, h = lh % a.S.H, G = a.S.G;
+    const int block = blocks_of(s.rows, BR) - 1 - at.at / at.np, part = at.at % at.np, layer = lh / a.S.H, h = lh % a.S.H, G = a.S.G;
     const int row0 = block * BR, rows = min(s.rows - row0, BR);
     const int before = s.len - s.nq;  // position of the sequence's first new token
     const int p_lo = before + row0 / G, p_hi = before + (row0 + rows - 1) / G;
-    const Span span = span_of(a, p_lo, p_hi);
+    const Span span = span_of<kTile>(a, p_lo, p_hi);
     const int t_from = (int)((int64_t)span.n * part / at.np), t_to = (int)((int64_t)span.n * (part + 1) / at.np);
     const int n_rt = (rows + 15) / 16;
 
@@ -493,19 +505,280 @@ __global__ __launch_bounds__(kWaves* kWave) void pages_few_kernel(PagesAttn a) {
   }
 }
 
+// ------------------------------------------------------------------------------------------------ many rows
+// Prompts: four waves of 32 rows share tiles of 64 tokens that go through LDS as bytes, the next tile's loads in flight while this one is multiplied; a wave
+// turns the bytes into operands itself (32 conversions per 8 products of 32 cycles; fp16 in LDS would need the LDS's whole bandwidth).
+// S^T = K Q^T leaves lane l with row l % 32 and tokens 16 t + 8 (l / 32) + j, the operand of O^T = V^T P^T.  K's 16-byte chunks are
+// swizzled by their token so that the eight lanes of a bank group read eight different ones.
+template <bool BF16>
+__global__ __launch_bounds__(kWaves* kWave, 2) void pages_many_kernel(PagesAttn a) {
+  using Geo = Many;
+  constexpr int PARTS = BF16 ? 1 : 2, BR = Geo::rows, kTile = Geo::tile, kHalf = 32;
+  constexpr float kLift = Weights<BF16>::lift;
+  static_assert(BR == 32 * kWaves && kTile == 2 * kHalf, "");
+  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  const int row = lane & 31, grp = lane >> 5;
+  __shared__ __attribute__((aligned(16))) uint8_t kbuf[2][kTile * kHeadDim], vbuf[2][kTile * kHeadDim];
+  __shared__ int2 meta[2][kTile / kOct];  // exponents of the octets' pages; x = kNoPage where the page is not there
+  constexpr int kNoPage = 1 << 20;
+
+  const Shares w = shares_of<Geo>(a, lane);
+  const int64_t all = (int64_t)w.parts * a.n_layers * a.S.H;
+  for (int64_t x = blockIdx.x; x < all; x += gridDim.x) {
+    const int lh = (int)(x % (a.n_layers * a.S.H));
+    const Place at = place_of<Geo>(a, w, (int)(x / (a.n_layers * a.S.H)), lane, [](const Seq& s, int np) { return np * blocks_of(s.rows, BR); });
+    const Seq s = at.s;
+    const int block = blocks_of(s.rows, BR) - 1 - at.at / at.np, part = at.at % at.np, layer = lh / a.S.H, h = lh % a.S.H, G = a.S.G;
+    const int row0 = block * BR, rows = min(s.rows - row0, BR), before = s.len - s.nq;
+    const int p_hi = before + (row0 + rows - 1) / G;
+    const Span span = span_of<kTile>(a, before + row0 / G, p_hi);
+    const int t_from = (int)((int64_t)span.n * part / at.np), t_to = (int)((int64_t)span.n * (part + 1) / at.np);
+
+    const int mine = row0 + 32 * wave + row;  // of the sequence's rows
+    const bool have = 32 * wave + row < rows;
+    const int pos = have ? before + mine / G : -1;
+    const bool any_row = 32 * wave < rows;
+    const int w_lo = before + (row0 + 32 * wave) / G, w_hi = any_row ? before + (row0 + min(32 * wave + 32, rows) - 1) / G : -1;  // positions of the wave's rows
+    const int64_t out_at = (((int64_t)layer * a.n_tokens + s.first + mine / G) * (a.S.H * G) + h * G + mine % G) * kHeadDim;
+
+    half8 q[8][PARTS];  // [16 channels 32 c + 16 grp, c = i / 2][8 of them: i % 2]
+    int eq;
+    {
+      float f[4][16], top = 0.f;
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        if (have) load_channels<BF16>(a.q, out_at + 32 * c + 16 * grp, f[c]);
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+          if (!have) f[c][j] = 0.f;
+          top = fmaxf(top, fabsf(f[c][j]));
+        }
+      }
+      top = fmaxf(top, __shfl_xor(top, 32));
+      eq = max((int)(__float_as_uint(top) >> 23) - 127, kLeastExponent);
+#pragma unroll
+      for (int c = 0; c < 8; ++c) {
+        float y[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) y[j] = ldexpf(f[c / 2][8 * (c % 2) + j], kQTop - eq);
+        to_halves<8, PARTS>(y, q[c]);
+      }
+    }
+    floatx16 o[4];  // rows 8 (i / 4) + 4 grp + i % 4 =: u of channel tile c: channel 64 (c / 2) + 2 u + c % 2
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[c][i] = 0.f;
+    float m = -FLT_MAX, l = 0.f;
+
+    // a wave brings octets wave and wave + 4 of a tile
+    const int32_t* table = a.table + (int64_t)at.b * a.S.max_pages;
+    const int last_page = max(page_count(s.len, a.S.logP) - 1, 0), in_page = (1 << a.S.logP) - 1;
+    uint4 nk[2], nv[2];
+    int2 ne[2];
+    const auto load_tile = [&](int i) {
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const int t = span.tile(i) * kTile + kOct * (wave + kWaves * u);
+        int page = __builtin_amdgcn_readfirstlane(table[min(t >> a.S.logP, last_page)]);
+        const bool bad = page < 0 || page >= a.S.n_pages;
+        page = bad ? 0 : page;
+        const int64_t ph = page_head(a.S, a.layer + layer, page, h);
+        const uint8_t* at_k = page_values(a.S, ph) + (t & in_page) * kHeadDim;
+        nk[u] = ((const uint4*)at_k)[lane];
+        nv[u] = ((const uint4*)(at_k + ((size_t)kHeadDim << a.S.logP)))[lane];
+        ne[u] = *(const int2*)(a.S.exponents + 2 * ph);
+        if (bad) ne[u].x = kNoPage;
+      }
+    };
+    const auto store_tile = [&](int b) {
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const int oc = wave + kWaves * u, tok = lane >> 3, ch = lane & 7;
+        ((uint4*)kbuf[b])[(kOct * oc + tok) * 8 + (ch ^ ((tok & 3) | ((oc & 1) << 2)))] = nk[u];
+        ((uint4*)vbuf[b])[64 * oc + lane] = nv[u];
+        if (lane == 0) meta[b][oc] = ne[u];
+      }
+    };
+    if (t_from < t_to) {
+      load_tile(t_from);
+      store_tile(0);
+    }
+    __syncthreads();
+    for (int i = t_from; i < t_to; ++i) {
+      const int b = (i - t_from) & 1;
+      if (i + 1 < t_to) load_tile(i + 1);
+#pragma unroll
+      for (int sub = 0; sub < 2; ++sub) {
+        const int t0 = span.tile(i) * kTile + kHalf * sub, t1 = t0 + kHalf - 1;
+        if (t0 > w_hi) continue;  // behind all of the wave's rows
+        int2 e[2];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) e[t] = meta[b][4 * sub + 2 * t + grp];
+        const bool bad[2] = {e[0].x == kNoPage, e[1].x == kNoPage};
+        const bool edge = t1 > w_lo || (a.n_recent && t1 >= a.n_sink && (int64_t)t0 <= (int64_t)w_hi - a.n_recent) || __any(bad[0] || bad[1]);
+
+        floatx16 acc;
+#pragma unroll
+        for (int j = 0; j < 16; ++j) acc[j] = 0.f;
+        // K row of this lane: token 16 (row / 16) + 8 ((row / 4) % 2) + 4 ((row / 8) % 2) + row % 4
+        const int tok = 16 * (row >> 4) + 8 * ((row >> 2) & 1) + 4 * ((row >> 3) & 1) + (row & 3);
+        const int swz = (row & 3) | ((row >> 2) & 1) << 2;
+        const uint4* krow = (const uint4*)kbuf[b] + (kHalf * sub + tok) * 8;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          const uint4 kw = krow[(2 * c + grp) ^ swz];
+          const half8 k0 = operand(kw.x, kw.y), k1 = operand(kw.z, kw.w);
+#pragma unroll
+          for (int p = PARTS - 1; p >= 0; --p) {
+            acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(k0, q[2 * c][p], acc, 0, 0, 0);
+            acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(k1, q[2 * c + 1][p], acc, 0, 0, 0);
+          }
+        }
+        float sc[16];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          const float factor = ldexpf(a.scale, eq - kQTop + e[t].x), ev = (float)e[t].y;
+#pragma unroll
+          for (int j = 0; j < 8; ++j) sc[8 * t + j] = acc[8 * t + j] * factor + ev;
+        }
+        half8 sees[2];
+        if (edge) {
+#pragma unroll
+          for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+              const int tt = t0 + 16 * t + 8 * grp + j;
+              const bool seen = !bad[t] && tt <= pos && (!a.n_recent || tt < a.n_sink || (int64_t)tt > (int64_t)pos - a.n_recent);
+              sees[t][j] = seen ? (_Float16)1.f : (_Float16)0.f;
+              sc[8 * t + j] = seen ? sc[8 * t + j] : -__builtin_inff();
+            }
+        }
+        float top = sc[0];
+#pragma unroll
+        for (int j = 1; j < 16; ++j) top = fmaxf(top, sc[j]);
+        if (__any(top > m + Weights<BF16>::slack)) {
+          top = fmaxf(m, fmaxf(top, __shfl_xor(top, 32)));
+          const float fade = __builtin_amdgcn_exp2f(m - top);
+          m = top, l *= fade;
+#pragma unroll
+          for (int c = 0; c < 4; ++c)
+#pragma unroll
+            for (int j = 0; j < 16; ++j) o[c][j] *= fade;
+        }
+        half8 pw[2][PARTS];
+        const float ref = m - kLift;
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          float y[8], sum = 0.f;
+#pragma unroll
+          for (int j = 0; j < 8; ++j) y[j] = __builtin_amdgcn_exp2f(sc[8 * t + j] - ref), sum += y[j];
+          l += ldexpf(sum, -e[t].y);
+          to_halves<8, PARTS>(y, pw[t]);
+        }
+        const uint4* vrow = (const uint4*)vbuf[b] + (4 * sub + grp) * 64 + row;
+        uint4 vw[2][2];
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int p = 0; p < 2; ++p) vw[t][p] = vrow[128 * t + 32 * p];
+        if (edge) {  // tokens that no row sees may hold anything; NaN that only some rows see is brought back to those
+          uint32_t nans = 0;
+#pragma unroll
+          for (int t = 0; t < 2; ++t) {
+            uint32_t keep[2] = {0, 0};
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+              const int tt = t0 + 16 * t + 8 * grp + j;
+              const bool seen = !bad[t] && tt <= w_hi && (!a.n_recent || tt < a.n_sink || (int64_t)tt > (int64_t)w_lo - a.n_recent);
+              keep[j / 4] |= seen ? 0xffu << (8 * (j % 4)) : 0u;
+            }
+#pragma unroll
+            for (int p = 0; p < 2; ++p) {
+              vw[t][p].x &= keep[0], vw[t][p].y &= keep[1], vw[t][p].z &= keep[0], vw[t][p].w &= keep[1];
+              nans |= nan_bytes(vw[t][p].x) | nan_bytes(vw[t][p].y) | nan_bytes(vw[t][p].z) | nan_bytes(vw[t][p].w);
+            }
+          }
+          if (__any(nans != 0)) {
+#pragma unroll
+            for (int p = 0; p < 2; ++p) {
+              floatx16 hit[2];
+#pragma unroll
+              for (int c = 0; c < 2; ++c)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) hit[c][j] = 0.f;
+#pragma unroll
+              for (int t = 0; t < 2; ++t) {
+                uint4& v = vw[t][p];
+                const uint32_t n[4] = {nan_bytes(v.x), nan_bytes(v.y), nan_bytes(v.z), nan_bytes(v.w)};
+                v.x &= ~(n[0] * 0xffu), v.y &= ~(n[1] * 0xffu), v.z &= ~(n[2] * 0xffu), v.w &= ~(n[3] * 0xffu);
+                hit[0] = __builtin_amdgcn_mfma_f32_32x32x16_f16(operand(n[0] * 0x38u, n[1] * 0x38u), sees[t], hit[0], 0, 0, 0);  // 0x38: 1
+                hit[1] = __builtin_amdgcn_mfma_f32_32x32x16_f16(operand(n[2] * 0x38u, n[3] * 0x38u), sees[t], hit[1], 0, 0, 0);
+              }
+#pragma unroll
+              for (int c = 0; c < 2; ++c)
+#pragma unroll
+                for (int j = 0; j < 16; ++j)
+                  if (hit[c][j] > 0.f) o[2 * p + c][j] = __builtin_nanf("");
+            }
+          }
+        }
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int p = 0; p < 2; ++p) {
+            const half8 v0 = operand(vw[t][p].x, vw[t][p].y), v1 = operand(vw[t][p].z, vw[t][p].w);
+#pragma unroll
+            for (int u = PARTS - 1; u >= 0; --u) {
+              o[2 * p] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v0, pw[t][u], o[2 * p], 0, 0, 0);
+              o[2 * p + 1] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v1, pw[t][u], o[2 * p + 1], 0, 0, 0);
+            }
+          }
+      }
+      if (i + 1 < t_to) store_tile(b ^ 1);
+      __syncthreads();
+    }
+
+    l += __shfl_xor(l, 32);
+    if (have) {
+      const bool whole = at.np == 1;
+      const int64_t slot = (int64_t)lh * w.split + at.before + at.at;
+      const float inv = !whole ? 1.f : l == 0.f ? 0.f : 1.f / l;
+      float* to = a.part + (slot * BR + 32 * wave + row) * kHeadDim;
+#pragma unroll
+      for (int p = 0; p < 2; ++p)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {  // 8 channels side by side
+          const int c0 = 64 * p + 16 * r + 8 * grp;
+          float y[8];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) y[2 * j] = o[2 * p][4 * r + j] * inv, y[2 * j + 1] = o[2 * p + 1][4 * r + j] * inv;
+          if (whole) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) store_kv<BF16>(a.out, out_at + c0 + j, y[j]);
+          } else {
+            *(float4*)(to + c0) = make_float4(y[0], y[1], y[2], y[3]), *(float4*)(to + c0 + 4) = make_float4(y[4], y[5], y[6], y[7]);
+          }
+        }
+      if (!whole && grp == 0) a.stat[slot * BR + 32 * wave + row] = make_float2(m, l);
+    }
+  }
+}
+
 // Rows whose tokens were shared out: one workgroup per row, its waves take the parts in turn.
-template <bool BF16, int BR>
+template <bool BF16, class Geo>
 __global__ __launch_bounds__(kWaves* kWave) void pages_join_kernel(PagesAttn a) {
+  constexpr int BR = Geo::rows;
   __shared__ float2 sums[kWaves][kWave];
   __shared__ float dens[kWaves];
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-  const Shares w = shares_of<BR>(a, lane);
+  const Shares w = shares_of<Geo>(a, lane);
   const int64_t all = (int64_t)w.split_rows * a.n_layers * a.S.H;
   for (int64_t x = blockIdx.x; x < all; x += gridDim.x) {
     const int lh = (int)(x / w.split_rows);
-    const Place at = place_of<BR>(a, w, (int)(x % w.split_rows), lane, [](const Seq& s, int np) { return np > 1 ? s.rows : 0; });
+    const Place at = place_of<Geo>(a, w, (int)(x % w.split_rows), lane, [](const Seq& s, int np) { return np > 1 ? s.rows : 0; });
     const int r = at.at, G = a.S.G;
-    const int64_t slot = (int64_t)lh * w.split + at.before + (int64_t)(r / BR) * at.np;
+    const int64_t slot = (int64_t)lh * w.split + at.before + (int64_t)(blocks_of(at.s.rows, BR) - 1 - r / BR) * at.np;
     const float2* stat = a.stat + slot * BR + r % BR;
     const float* part = a.part + (slot * BR + r % BR) * kHeadDim + 2 * lane;
     float m = -FLT_MAX;
@@ -534,44 +807,73 @@ __global__ __launch_bounds__(kWaves* kWave) void pages_join_kernel(PagesAttn a) 
   }
 }
 
-// Rows of a block (times 16): what an average sequence brings.
-int row_tiles(const Pages& S, int batch, int n_tokens, bool bf16) {
-  const int64_t rows = (int64_t)S.G * ((n_tokens + batch - 1) / batch);
-  return rows <= 16 ? 1 : rows <= 32 || !bf16 ? 2 : 4;
-}
-
 // Parts of cut blocks: a block of more than w.tiles tiles has fewer than 2 tiles / w.tiles of them, all blocks together kParts w.tiles tiles (rounding: + 64).
 constexpr int64_t kMostCut = 2 * kParts + 64;
 
-template <bool BF16, int R>
-hipError_t launch_few(const PagesAttn& a, hipStream_t st) {
-  constexpr int BR = 16 * R;
-  const int64_t lh = (int64_t)a.n_layers * a.S.H, blocks = (int64_t)a.n_tokens * a.S.G / BR + a.batch;
-  const unsigned grid = (unsigned)std::min<int64_t>(kParts + lh * blocks, 1 << 20);
-  pages_few_kernel<BF16, R><<<grid, kWaves * kWave, 0, st>>>(a);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess || !a.part) return e;
-  const unsigned join = (unsigned)std::min<int64_t>(lh * a.n_tokens * a.S.G, 2048);
-  pages_join_kernel<BF16, BR><<<join, kWaves * kWave, 0, st>>>(a);
+// What a call launches.  A sequence's rows are known on the device only; what the sizes exclude is not launched.
+struct Launches {
+  int few = 0;        // row tiles of pages_few_kernel's blocks, 0: not launched
+  bool many = false;  // pages_many_kernel
+  size_t few_bytes = 0, bytes = 0;  // of the workspace
+};
+Launches launches_of(const Pages& S, int batch, int n_tokens, bool bf16) {
+  Launches n;
+  const int64_t rows = (int64_t)n_tokens * S.G, average = S.G * (((int64_t)n_tokens + batch - 1) / batch);
+  n.many = rows > kFewRows;
+  if (!n.many || batch > 1) {
+    const int64_t usual = std::min<int64_t>(average > kFewRows ? S.G : average, kFewRows);  // beside prompts: single tokens
+    n.few = usual <= 16 ? 1 : usual <= 32 || !bf16 ? 2 : 4;
+  }
+  const auto part = [](int64_t block) { return (size_t)kMostCut * (size_t)block * (kHeadDim * sizeof(float) + sizeof(float2)); };
+  const int64_t most = ((int64_t)S.max_pages << S.logP) / 32 + 1;  // tiles of a sequence
+  if (most > kLeastTiles) {                                       // else no block is ever cut
+    n.few_bytes = n.few ? part(16 * n.few) : 0;
+    n.bytes = n.few_bytes + (n.many ? part(Many::rows) : 0);
+  }
+  return n;
+}
+
+template <class Geo, class Kernel, class Join>
+hipError_t launch_blocks(PagesAttn a, Kernel kernel, Join join, char* ws, hipStream_t st) {
+  a.part = (float*)ws;
+  a.stat = ws ? (float2*)(a.part + kMostCut * Geo::rows * kHeadDim) : nullptr;
+  const int64_t lh = (int64_t)a.n_layers * a.S.H, blocks = (int64_t)a.n_tokens * a.S.G / Geo::rows + a.batch;
+  kernel<<<(unsigned)std::min<int64_t>(kParts + lh * blocks, 1 << 20), kWaves * kWave, 0, st>>>(a);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || !ws) return e;
+  join<<<(unsigned)std::min<int64_t>(lh * a.n_tokens * a.S.G, 2048), kWaves * kWave, 0, st>>>(a);
   return hipGetLastError();
+}
+
+template <bool BF16, int R>
+hipError_t launch_few(const PagesAttn& a, char* ws, hipStream_t st) {
+  return launch_blocks<Few<R>>(a, pages_few_kernel<BF16, R>, pages_join_kernel<BF16, Few<R>>, ws, st);
+}
+template <bool BF16>
+hipError_t launch_many(const PagesAttn& a, char* ws, hipStream_t st) {
+  return launch_blocks<Many>(a, pages_many_kernel<BF16>, pages_join_kernel<BF16, Many>, ws, st);
 }
 
 }  // namespace
 
-size_t pages_attn_bytes(const Pages& S, int n_layers, int batch, int n_tokens, bool bf16) {
-  const int64_t most = ((int64_t)S.max_pages << S.logP) / kTile + 1;
-  if (most <= kLeastTiles || batch == 0 || n_tokens == 0) return 0;  // no block is ever cut
-  const int BR = 16 * row_tiles(S, batch, n_tokens, bf16);
-  (void)n_layers;
-  return (size_t)kMostCut * BR * (kHeadDim * sizeof(float) + sizeof(float2));
+size_t pages_attn_bytes(const Pages& S, int batch, int n_tokens, bool bf16) {
+  return batch == 0 || n_tokens == 0 ? 0 : launches_of(S, batch, n_tokens, bf16).bytes;
 }
 
 hipError_t launch_pages_attn(PagesAttn a, bool bf16, void* ws, hipStream_t st) {
-  const int R = row_tiles(a.S, a.batch, a.n_tokens, bf16);
-  a.part = pages_attn_bytes(a.S, a.n_layers, a.batch, a.n_tokens, bf16) ? (float*)ws : nullptr;
-  a.stat = a.part ? (float2*)(a.part + kMostCut * 16 * R * kHeadDim) : nullptr;
-  if (bf16) return R == 1 ? launch_few<true, 1>(a, st) : R == 2 ? launch_few<true, 2>(a, st) : launch_few<true, 4>(a, st);
-  return R == 1 ? launch_few<false, 1>(a, st) : launch_few<false, 2>(a, st);
+  const Launches n = launches_of(a.S, a.batch, a.n_tokens, bf16);
+  char* few = n.bytes ? (char*)ws : nullptr;
+  a.rows_to = 0x7fffffff;
+  if (n.many) {  // the longer work first
+    a.rows_over = n.few ? kFewRows : 0;
+    char* many = n.bytes ? (char*)ws + n.few_bytes : nullptr;
+    const hipError_t e = bf16 ? launch_many<true>(a, many, st) : launch_many<false>(a, many, st);
+    if (e != hipSuccess || !n.few) return e;
+    a.rows_to = kFewRows;
+  }
+  a.rows_over = 0;
+  if (bf16) return n.few == 1 ? launch_few<true, 1>(a, few, st) : n.few == 2 ? launch_few<true, 2>(a, few, st) : launch_few<true, 4>(a, few, st);
+  return n.few == 1 ? launch_few<false, 1>(a, few, st) : launch_few<false, 2>(a, few, st);
 }
 
 }  // namespace iwdft
