@@ -2,9 +2,13 @@
 //
 //   o_t = sum_j p_j v_j,  p = softmax_j (scale q_t k_j),  over the tokens j that t sees.
 //
-// All products run on the matrix cores in fp16, which holds e4m3 exactly.  What keeps the rest exact:
-//  * q: a row is multiplied by the power of two that brings its largest value to [2^14, 2^15); bf16 then fits (relative to the row's largest
-//    value down to 2^-38), fp32 as the sum of two fp16 parts (22 bits).
+// All products run on the matrix cores.  What keeps them exact:
+//  * q k in bf16 calls: K goes in as the bytes it is stored as.  A bf16 number has 8 significant bits and is the sum of two e4m3 numbers of 4: the
+//    nearest one and the rest, 32 times as large, which the instruction scales back.  A row of q is multiplied by the power of two that
+//    brings its largest value to [2^7, 2^8); down to 2^-14 of that value the sum is exact, smaller ones err by 2^-22 of it.  Two products of
+//    bytes take as long as one of fp16, and nothing has to be converted.
+//  * q k in fp32 calls: fp16, which holds e4m3 exactly; q, its largest value in [2^14, 2^15), as the sum of two fp16 parts (22 bits).
+//  * p v: fp16.
 //  * the pages' exponents: that of K enters the score's factor; that of V joins the exponent of the weight.  With s_j the score times log2 e and
 //    eV_j the exponent of j's page, the weights in the sum are P_j = 2^(s_j + eV_j - m), m a running bound of s_j + eV_j, and the
 //    denominator is sum 2^(s_j - m) = sum P_j 2^-eV_j.  So no weight overflows fp16 or loses bits because its page is small.
@@ -14,6 +18,7 @@
 // values, whose sizes are up to 2^18 apart, by 2^-22 of what they add up to.
 #include <algorithm>
 #include <cfloat>
+#include <type_traits>
 
 #include "pages.h"
 
@@ -26,8 +31,8 @@ constexpr int kWaves = 4;
 template <bool BF16>
 struct Weights {
   static constexpr float lift = BF16 ? 6.f : 15.f, slack = BF16 ? 8.f : 0.f;
+  static constexpr int q_top = BF16 ? 7 : 14;  // rows of q: largest value in [2^q_top, 2^(q_top + 1))
 };
-constexpr int kQTop = 14;    // q rows: largest value in [2^14, 2^15)
 
 // ------------------------------------------------------------------------------------------------ sharing out the work
 // A block is `rows` consecutive (new token, query head of the KV head) pairs of a sequence; its tokens are cut into parts, one workgroup each, such that
@@ -173,6 +178,23 @@ __device__ __forceinline__ void to_halves(const float* x, half8* parts) {  // x[
     }
   }
 }
+// 16 values as bytes hi + 2^-5 lo; what is not finite becomes NaN.
+typedef int intx8 __attribute__((ext_vector_type(8)));
+constexpr int kOne = 0x7f7f7f7f, kThirtySecond = 0x7a7a7a7a;  // scales of the matrix instructions: 2^0, 2^-5
+__device__ __forceinline__ void to_bytes(const float* x, int* hi, int* lo) {
+#pragma unroll
+  for (int c = 0; c < 16; c += 4) {
+    float y[4], back[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) y[j] = fabsf(x[c + j]) <= (float)kE4m3Max ? x[c + j] : __builtin_nanf("");
+    hi[c / 4] = (int)floats_e4m3(y);
+    e4m3_floats((uint32_t)hi[c / 4], back);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) y[j] = 32.f * (y[j] - back[j]);
+    lo[c / 4] = (int)floats_e4m3(y);
+  }
+}
+__device__ __forceinline__ intx8 operand8(uint4 a, uint4 b) { return intx8{(int)a.x, (int)a.y, (int)a.z, (int)a.w, (int)b.x, (int)b.y, (int)b.z, (int)b.w}; }
 __device__ __forceinline__ float max_over_16s(float x) {  // over lanes that differ in their upper two bits
   x = fmaxf(x, __shfl_xor(x, 16));
   return fmaxf(x, __shfl_xor(x, 32));
@@ -197,6 +219,10 @@ __device__ __forceinline__ void load_channels(const void* p, int64_t i, float* f
   }
 }
 
+// A row at position p sees the tokens (from, p] and those below sink.
+__device__ __forceinline__ int window_from(const PagesAttn& a, int p) { return a.n_recent ? max(p - a.n_recent, -1) : -1; }  // p >= -1, n_recent >= 0: no overflow
+__device__ __forceinline__ bool sees(int t, int from, int to, int sink) { return (t <= to) & ((t > from) | (t < sink)); }
+
 // Tiles that a block's rows see: those of the sinks, then the others.
 struct Span {
   int sinks, skip, n;
@@ -220,10 +246,11 @@ __device__ __forceinline__ Span span_of(const PagesAttn& a, int p_lo, int p_hi) 
 // One row tile of 16 query rows: lane l holds row l % 16.
 template <int PARTS>
 struct Rows {
-  half8 q[4][PARTS];
+  half8 q[PARTS == 1 ? 1 : 4][PARTS];  // fp32: [chunk of 16 channels oct + 4 (c / 2)][8 of them: c % 2]
+  intx8 q8[2];                         // bf16: both chunks, hi and lo
   floatx4 o[8];   // [16-byte load of V][channel of the pair]: row l % 16, channels 32 (i / 2) + 8 (l / 16) + 2 c + i % 2
   float m, l, factor;
-  int pos, eq;
+  int pos, from, eq;
 };
 
 // ------------------------------------------------------------------------------------------------ few rows
@@ -233,7 +260,7 @@ struct Rows {
 template <bool BF16, int R>
 __global__ __launch_bounds__(kWaves* kWave) void pages_few_kernel(PagesAttn a) {
   using Geo = Few<R>;
-  constexpr int PARTS = BF16 ? 1 : 2, BR = Geo::rows, kTile = Geo::tile;
+  constexpr int PARTS = BF16 ? 1 : 2, BR = Geo::rows, kTile = Geo::tile, kQTop = Weights<BF16>::q_top;
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
   const int row = lane & 15, oct = lane >> 4;
   __shared__ __attribute__((aligned(16))) float join[2][BR][kHeadDim + 4];
@@ -252,6 +279,7 @@ __global__ __launch_bounds__(kWaves* kWave) void pages_few_kernel(PagesAttn a) {
     const Span span = span_of<kTile>(a, p_lo, p_hi);
     const int t_from = (int)((int64_t)span.n * part / at.np), t_to = (int)((int64_t)span.n * (part + 1) / at.np);
     const int n_rt = (rows + 15) / 16;
+    const int sink = a.n_recent ? a.n_sink : 0, all_from = window_from(a, max(p_lo, -1));
 
     Rows<PARTS> rt[R];
 #pragma unroll
@@ -259,7 +287,7 @@ __global__ __launch_bounds__(kWaves* kWave) void pages_few_kernel(PagesAttn a) {
       Rows<PARTS>& z = rt[r];
       const int mine = row0 + 16 * r + row;
       const bool have = 16 * r + row < rows;
-      z.pos = have ? before + mine / G : -1;
+      z.pos = have ? max(before + mine / G, -1) : -1, z.from = window_from(a, z.pos);
       z.m = -FLT_MAX, z.l = 0.f;
 #pragma unroll
       for (int i = 0; i < 8; ++i) z.o[i] = floatx4{0.f, 0.f, 0.f, 0.f};
@@ -284,12 +312,16 @@ __global__ __launch_bounds__(kWaves* kWave) void pages_few_kernel(PagesAttn a) {
 #pragma unroll
       for (int p = 0; p < 2; ++p)
 #pragma unroll
-        for (int g = 0; g < 2; ++g) {
-          float y[8];
+        for (int c = 0; c < 16; ++c) f[p][c] = ldexpf(f[p][c], kQTop - z.eq);
+      if constexpr (BF16) {
+        int hi[8], lo[8];
+        to_bytes(f[0], hi, lo), to_bytes(f[1], hi + 4, lo + 4);
 #pragma unroll
-          for (int c = 0; c < 8; ++c) y[c] = ldexpf(f[p][8 * g + c], kQTop - z.eq);
-          to_halves<8, PARTS>(y, z.q[2 * p + g]);
-        }
+        for (int c = 0; c < 8; ++c) z.q8[0][c] = hi[c], z.q8[1][c] = lo[c];
+      } else {
+#pragma unroll
+        for (int c = 0; c < 4; ++c) to_halves<8, PARTS>(f[c / 2] + 8 * (c % 2), z.q[c]);
+      }
     }
 
     // pages of a lane's octets: that of its K row and that of its tokens in V and in the scores
@@ -341,14 +373,14 @@ __global__ __launch_bounds__(kWaves* kWave) void pages_few_kernel(PagesAttn a) {
       }
       const int t0 = span.tile(i) * kTile, t1 = t0 + kTile - 1, j0 = t0 + 8 * oct;
       // whether every row sees the whole tile
-      const bool edge = t1 > p_lo || (a.n_recent && t1 >= a.n_sink && (int64_t)t0 <= (int64_t)p_hi - a.n_recent) || __any(d.bad);
+      const bool edge = t1 > p_lo || (t1 >= sink && t0 <= window_from(a, p_hi)) || __any(d.bad);
       bool poison = false;
       if (edge) {  // tokens that no row sees may hold anything
         uint32_t keep[2] = {0, 0};
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           const int t = j0 + j;
-          const bool seen = !d.bad && t <= p_hi && (!a.n_recent || t < a.n_sink || (int64_t)t > (int64_t)p_lo - a.n_recent);
+          const bool seen = !d.bad & sees(t, all_from, p_hi, sink);
           keep[j / 4] |= seen ? 0xffu << (8 * (j % 4)) : 0u;
         }
         uint32_t nans = 0;
@@ -360,13 +392,14 @@ __global__ __launch_bounds__(kWaves* kWave) void pages_few_kernel(PagesAttn a) {
         poison = __any(nans != 0);
       }
 
-      half8 kf[2][4];
+      half8 kf[2][BF16 ? 1 : 4];
+      if constexpr (!BF16)
 #pragma unroll
-      for (int u = 0; u < 2; ++u)
+        for (int u = 0; u < 2; ++u)
 #pragma unroll
-        for (int p = 0; p < 2; ++p) kf[u][2 * p] = operand(d.k[u][p].x, d.k[u][p].y), kf[u][2 * p + 1] = operand(d.k[u][p].z, d.k[u][p].w);
+          for (int p = 0; p < 2; ++p) kf[u][2 * p] = operand(d.k[u][p].x, d.k[u][p].y), kf[u][2 * p + 1] = operand(d.k[u][p].z, d.k[u][p].w);
       const float ev = (float)d.e.y;
-      half8 pw[R][PARTS], sees[R];
+      half8 pw[R][PARTS], ones[R];
 #pragma unroll
       for (int r = 0; r < R; ++r) {
         if (r >= n_rt) continue;
@@ -375,10 +408,16 @@ __global__ __launch_bounds__(kWaves* kWave) void pages_few_kernel(PagesAttn a) {
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
           floatx4 acc{0.f, 0.f, 0.f, 0.f};
+          if constexpr (BF16) {
+            const intx8 k8 = operand8(d.k[u][0], d.k[u][1]);
+            acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k8, z.q8[1], acc, 0, 0, 0, kOne, 0, kThirtySecond);
+            acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k8, z.q8[0], acc, 0, 0, 0, kOne, 0, kOne);
+          } else {
 #pragma unroll
-          for (int c = 0; c < 4; ++c)
+            for (int c = 0; c < 4; ++c)
 #pragma unroll
-            for (int p = PARTS - 1; p >= 0; --p) acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[u][c], z.q[c][p], acc, 0, 0, 0);
+              for (int p = PARTS - 1; p >= 0; --p) acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[u][c], z.q[c][p], acc, 0, 0, 0);
+          }
 #pragma unroll
           for (int j = 0; j < 4; ++j) sc[4 * u + j] = acc[j];
         }
@@ -389,8 +428,8 @@ __global__ __launch_bounds__(kWaves* kWave) void pages_few_kernel(PagesAttn a) {
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
             const int t = j0 + j;
-            const bool seen = !d.bad && t <= z.pos && (!a.n_recent || t < a.n_sink || (int64_t)t > (int64_t)z.pos - a.n_recent);
-            sees[r][j] = seen ? (_Float16)1.f : (_Float16)0.f;
+            const bool seen = !d.bad & sees(t, z.from, z.pos, sink);
+            ones[r][j] = seen ? (_Float16)1.f : (_Float16)0.f;
             sc[j] = seen ? sc[j] : -__builtin_inff();
           }
         }
@@ -424,7 +463,7 @@ __global__ __launch_bounds__(kWaves* kWave) void pages_few_kernel(PagesAttn a) {
             if (r >= n_rt) continue;
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
-              const floatx4 hit = __builtin_amdgcn_mfma_f32_16x16x32_f16(bad[c], sees[r], floatx4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+              const floatx4 hit = __builtin_amdgcn_mfma_f32_16x16x32_f16(bad[c], ones[r], floatx4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
 #pragma unroll
               for (int j = 0; j < 4; ++j)
                 if (hit[j] > 0.f) rt[r].o[2 * p + c][j] = __builtin_nanf("");
@@ -511,16 +550,15 @@ __global__ __launch_bounds__(kWaves* kWave) void pages_few_kernel(PagesAttn a) {
 // S^T = K Q^T leaves lane l with row l % 32 and tokens 16 t + 8 (l / 32) + j, the operand of O^T = V^T P^T.  K's 16-byte chunks are
 // swizzled by their token so that the eight lanes of a bank group read eight different ones.
 template <bool BF16>
-__global__ __launch_bounds__(kWaves* kWave, 2) void pages_many_kernel(PagesAttn a) {
+__global__ __launch_bounds__(kWaves* kWave, BF16 ? 2 : 1) void pages_many_kernel(PagesAttn a) {
   using Geo = Many;
-  constexpr int PARTS = BF16 ? 1 : 2, BR = Geo::rows, kTile = Geo::tile, kHalf = 32;
+  constexpr int PARTS = BF16 ? 1 : 2, BR = Geo::rows, kTile = Geo::tile, kHalf = 32, kQTop = Weights<BF16>::q_top;
   constexpr float kLift = Weights<BF16>::lift;
   static_assert(BR == 32 * kWaves && kTile == 2 * kHalf, "");
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
   const int row = lane & 31, grp = lane >> 5;
   __shared__ __attribute__((aligned(16))) uint8_t kbuf[2][kTile * kHeadDim], vbuf[2][kTile * kHeadDim];
-  __shared__ int2 meta[2][kTile / kOct];  // exponents of the octets' pages; x = kNoPage where the page is not there
-  constexpr int kNoPage = 1 << 20;
+  __shared__ float4 meta[2][kTile / kOct];  // of the octets' pages: scale 2^(eK - kQTop), eV, 2^-eV
 
   const Shares w = shares_of<Geo>(a, lane);
   const int64_t all = (int64_t)w.parts * a.n_layers * a.S.H;
@@ -530,18 +568,20 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void pages_many_kernel(PagesAttn 
     const Seq s = at.s;
     const int block = blocks_of(s.rows, BR) - 1 - at.at / at.np, part = at.at % at.np, layer = lh / a.S.H, h = lh % a.S.H, G = a.S.G;
     const int row0 = block * BR, rows = min(s.rows - row0, BR), before = s.len - s.nq;
-    const int p_hi = before + (row0 + rows - 1) / G;
-    const Span span = span_of<kTile>(a, before + row0 / G, p_hi);
+    const int p_lo = before + row0 / G, p_hi = before + (row0 + rows - 1) / G;
+    const Span span = span_of<kTile>(a, p_lo, p_hi);
     const int t_from = (int)((int64_t)span.n * part / at.np), t_to = (int)((int64_t)span.n * (part + 1) / at.np);
 
     const int mine = row0 + 32 * wave + row;  // of the sequence's rows
     const bool have = 32 * wave + row < rows;
-    const int pos = have ? before + mine / G : -1;
+    const int pos = have ? max(before + mine / G, -1) : -1;
     const bool any_row = 32 * wave < rows;
     const int w_lo = before + (row0 + 32 * wave) / G, w_hi = any_row ? before + (row0 + min(32 * wave + 32, rows) - 1) / G : -1;  // positions of the wave's rows
+    const int sink = a.n_recent ? a.n_sink : 0, from = window_from(a, pos), w_from = window_from(a, max(w_lo, -1));
     const int64_t out_at = (((int64_t)layer * a.n_tokens + s.first + mine / G) * (a.S.H * G) + h * G + mine % G) * kHeadDim;
 
-    half8 q[8][PARTS];  // [16 channels 32 c + 16 grp, c = i / 2][8 of them: i % 2]
+    half8 q[BF16 ? 1 : 8][PARTS];  // fp32: [chunk of 16 channels 2 (c / 2) + grp][8 of them: c % 2]
+    intx8 q8[2][2];                // bf16: [two chunks][hi, lo]
     int eq;
     {
       float f[4][16], top = 0.f;
@@ -557,13 +597,23 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void pages_many_kernel(PagesAttn 
       top = fmaxf(top, __shfl_xor(top, 32));
       eq = max((int)(__float_as_uint(top) >> 23) - 127, kLeastExponent);
 #pragma unroll
-      for (int c = 0; c < 8; ++c) {
-        float y[8];
+      for (int c = 0; c < 4; ++c)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) y[j] = ldexpf(f[c / 2][8 * (c % 2) + j], kQTop - eq);
-        to_halves<8, PARTS>(y, q[c]);
+        for (int j = 0; j < 16; ++j) f[c][j] = ldexpf(f[c][j], kQTop - eq);
+      if constexpr (BF16) {
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          int hi[8], lo[8];
+          to_bytes(f[2 * c], hi, lo), to_bytes(f[2 * c + 1], hi + 4, lo + 4);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) q8[c][0][j] = hi[j], q8[c][1][j] = lo[j];
+        }
+      } else {
+#pragma unroll
+        for (int c = 0; c < 8; ++c) to_halves<8, PARTS>(f[c / 2] + 8 * (c % 2), q[c]);
       }
     }
+    const float q_scale = ldexpf(1.f, eq);
     floatx16 o[4];  // rows 8 (i / 4) + 4 grp + i % 4 =: u of channel tile c: channel 64 (c / 2) + 2 u + c % 2
 #pragma unroll
     for (int c = 0; c < 4; ++c)
@@ -571,173 +621,196 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void pages_many_kernel(PagesAttn 
       for (int i = 0; i < 16; ++i) o[c][i] = 0.f;
     float m = -FLT_MAX, l = 0.f;
 
-    // a wave brings octets wave and wave + 4 of a tile
+    // a wave brings octets wave and wave + 4 of a tile; their pages are looked up a tile earlier
     const int32_t* table = a.table + (int64_t)at.b * a.S.max_pages;
     const int last_page = max(page_count(s.len, a.S.logP) - 1, 0), in_page = (1 << a.S.logP) - 1;
+    int next_page[2] = {0, 0};
     uint4 nk[2], nv[2];
     int2 ne[2];
+    bool none[2];
+    const auto find_tile = [&](int i) {
+#pragma unroll
+      for (int u = 0; u < 2; ++u) next_page[u] = table[min((span.tile(i) * kTile + kOct * (wave + kWaves * u)) >> a.S.logP, last_page)];
+    };
     const auto load_tile = [&](int i) {
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
         const int t = span.tile(i) * kTile + kOct * (wave + kWaves * u);
-        int page = __builtin_amdgcn_readfirstlane(table[min(t >> a.S.logP, last_page)]);
-        const bool bad = page < 0 || page >= a.S.n_pages;
-        page = bad ? 0 : page;
+        int page = __builtin_amdgcn_readfirstlane(next_page[u]);
+        none[u] = page < 0 || page >= a.S.n_pages;
+        page = none[u] ? 0 : page;
         const int64_t ph = page_head(a.S, a.layer + layer, page, h);
         const uint8_t* at_k = page_values(a.S, ph) + (t & in_page) * kHeadDim;
         nk[u] = ((const uint4*)at_k)[lane];
         nv[u] = ((const uint4*)(at_k + ((size_t)kHeadDim << a.S.logP)))[lane];
         ne[u] = *(const int2*)(a.S.exponents + 2 * ph);
-        if (bad) ne[u].x = kNoPage;
       }
     };
     const auto store_tile = [&](int b) {
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
+        float4 e = make_float4(ldexpf(a.scale, ne[u].x - kQTop), (float)ne[u].y, ldexpf(1.f, -ne[u].y), 0.f);
+        if (none[u]) {  // a page that is not there: scores of -infinity, weights and values of 0
+          nk[u] = nv[u] = make_uint4(0, 0, 0, 0);
+          e = make_float4(0.f, -__builtin_inff(), 0.f, 0.f);
+        }
         const int oc = wave + kWaves * u, tok = lane >> 3, ch = lane & 7;
         ((uint4*)kbuf[b])[(kOct * oc + tok) * 8 + (ch ^ ((tok & 3) | ((oc & 1) << 2)))] = nk[u];
         ((uint4*)vbuf[b])[64 * oc + lane] = nv[u];
-        if (lane == 0) meta[b][oc] = ne[u];
+        if (lane == 0) meta[b][oc] = e;
       }
     };
     if (t_from < t_to) {
+      find_tile(t_from);
       load_tile(t_from);
       store_tile(0);
+      if (t_from + 1 < t_to) find_tile(t_from + 1);
     }
     __syncthreads();
-    for (int i = t_from; i < t_to; ++i) {
+    // K row of this lane in a half: token 16 (row / 16) + 8 ((row / 4) % 2) + 4 ((row / 8) % 2) + row % 4
+    const int k_tok = 16 * (row >> 4) + 8 * ((row >> 2) & 1) + 4 * ((row >> 3) & 1) + (row & 3), k_swz = (row & 3) | ((row >> 2) & 1) << 2;
+    // EDGE: some row of the block may not see all of the tile
+    const auto step = [&](int i, auto kEdge) {
+      constexpr bool EDGE = decltype(kEdge)::value;
       const int b = (i - t_from) & 1;
       if (i + 1 < t_to) load_tile(i + 1);
+      if (i + 2 < t_to) find_tile(i + 2);
+      const int t0 = span.tile(i) * kTile;
+      if (!EDGE || t0 <= w_hi) {  // else behind all of the wave's rows
+        floatx16 acc[2];
 #pragma unroll
-      for (int sub = 0; sub < 2; ++sub) {
-        const int t0 = span.tile(i) * kTile + kHalf * sub, t1 = t0 + kHalf - 1;
-        if (t0 > w_hi) continue;  // behind all of the wave's rows
-        int2 e[2];
+        for (int u = 0; u < 2; ++u)
 #pragma unroll
-        for (int t = 0; t < 2; ++t) e[t] = meta[b][4 * sub + 2 * t + grp];
-        const bool bad[2] = {e[0].x == kNoPage, e[1].x == kNoPage};
-        const bool edge = t1 > w_lo || (a.n_recent && t1 >= a.n_sink && (int64_t)t0 <= (int64_t)w_hi - a.n_recent) || __any(bad[0] || bad[1]);
-
-        floatx16 acc;
+          for (int j = 0; j < 16; ++j) acc[u][j] = 0.f;
+        const auto chunk = [&](int u, int c) { return ((const uint4*)kbuf[b])[(kHalf * u + k_tok) * 8 + ((2 * c + grp) ^ k_swz)]; };
+        if constexpr (BF16) {
 #pragma unroll
-        for (int j = 0; j < 16; ++j) acc[j] = 0.f;
-        // K row of this lane: token 16 (row / 16) + 8 ((row / 4) % 2) + 4 ((row / 8) % 2) + row % 4
-        const int tok = 16 * (row >> 4) + 8 * ((row >> 2) & 1) + 4 * ((row >> 3) & 1) + (row & 3);
-        const int swz = (row & 3) | ((row >> 2) & 1) << 2;
-        const uint4* krow = (const uint4*)kbuf[b] + (kHalf * sub + tok) * 8;
+          for (int c = 0; c < 2; ++c)
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          const uint4 kw = krow[(2 * c + grp) ^ swz];
-          const half8 k0 = operand(kw.x, kw.y), k1 = operand(kw.z, kw.w);
-#pragma unroll
-          for (int p = PARTS - 1; p >= 0; --p) {
-            acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(k0, q[2 * c][p], acc, 0, 0, 0);
-            acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(k1, q[2 * c + 1][p], acc, 0, 0, 0);
-          }
-        }
-        float sc[16];
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-          const float factor = ldexpf(a.scale, eq - kQTop + e[t].x), ev = (float)e[t].y;
-#pragma unroll
-          for (int j = 0; j < 8; ++j) sc[8 * t + j] = acc[8 * t + j] * factor + ev;
-        }
-        half8 sees[2];
-        if (edge) {
-#pragma unroll
-          for (int t = 0; t < 2; ++t)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-              const int tt = t0 + 16 * t + 8 * grp + j;
-              const bool seen = !bad[t] && tt <= pos && (!a.n_recent || tt < a.n_sink || (int64_t)tt > (int64_t)pos - a.n_recent);
-              sees[t][j] = seen ? (_Float16)1.f : (_Float16)0.f;
-              sc[8 * t + j] = seen ? sc[8 * t + j] : -__builtin_inff();
+            for (int u = 0; u < 2; ++u) {
+              const intx8 k8 = operand8(chunk(u, 2 * c), chunk(u, 2 * c + 1));
+              acc[u] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(k8, q8[c][1], acc[u], 0, 0, 0, kOne, 0, kThirtySecond);
+              acc[u] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(k8, q8[c][0], acc[u], 0, 0, 0, kOne, 0, kOne);
             }
+        } else {
+#pragma unroll
+          for (int c = 0; c < 4; ++c)
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+              const uint4 kw = chunk(u, c);
+              const half8 k0 = operand(kw.x, kw.y), k1 = operand(kw.z, kw.w);
+#pragma unroll
+              for (int p = PARTS - 1; p >= 0; --p) {
+                acc[u] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k0, q[2 * c][p], acc[u], 0, 0, 0);
+                acc[u] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k1, q[2 * c + 1][p], acc[u], 0, 0, 0);
+              }
+            }
+        }
+        const int base = t0 + 8 * grp;  // tokens of the lane: base + 16 t + j
+        float inv[4];
+        float sc[32];  // exponents of the weights as they enter the sums: relative to m - lift
+        const bool unset = m == -FLT_MAX;  // the row has seen nothing: relative to 0
+        const float ref = (unset ? 0.f : m) - kLift;
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          const float4 e = meta[b][2 * t + grp];
+          const float factor = e.x * q_scale, shift = e.y - ref;
+          inv[t] = e.z;
+#pragma unroll
+          for (int j = 0; j < 8; ++j) sc[8 * t + j] = acc[t / 2][8 * (t % 2) + j] * factor + shift;
+        }
+        if constexpr (EDGE) {
+#pragma unroll
+          for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) sc[8 * t + j] = sees(base + 16 * t + j, from, pos, sink) ? sc[8 * t + j] : -__builtin_inff();
         }
         float top = sc[0];
 #pragma unroll
-        for (int j = 1; j < 16; ++j) top = fmaxf(top, sc[j]);
-        if (__any(top > m + Weights<BF16>::slack)) {
-          top = fmaxf(m, fmaxf(top, __shfl_xor(top, 32)));
-          const float fade = __builtin_amdgcn_exp2f(m - top);
-          m = top, l *= fade;
+        for (int j = 1; j < 32; ++j) top = fmaxf(top, sc[j]);
+        if (__any(top > (unset ? -FLT_MAX : kLift + Weights<BF16>::slack))) {
+          top = fmaxf(top, __shfl_xor(top, 32));
+          const bool first = unset && top >= -FLT_MAX;
+          const float up = unset ? (first ? top - kLift : 0.f) : fmaxf(top - kLift, 0.f), fade = unset ? 1.f : __builtin_amdgcn_exp2f(-up);
+          m = first ? up : m + up, l *= fade;
+#pragma unroll
+          for (int j = 0; j < 32; ++j) sc[j] -= up;
 #pragma unroll
           for (int c = 0; c < 4; ++c)
 #pragma unroll
             for (int j = 0; j < 16; ++j) o[c][j] *= fade;
         }
-        half8 pw[2][PARTS];
-        const float ref = m - kLift;
+        half8 pw[4][PARTS];
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
+        for (int t = 0; t < 4; ++t) {
           float y[8], sum = 0.f;
 #pragma unroll
-          for (int j = 0; j < 8; ++j) y[j] = __builtin_amdgcn_exp2f(sc[8 * t + j] - ref), sum += y[j];
-          l += ldexpf(sum, -e[t].y);
+          for (int j = 0; j < 8; ++j) y[j] = __builtin_amdgcn_exp2f(sc[8 * t + j]);
           to_halves<8, PARTS>(y, pw[t]);
-        }
-        const uint4* vrow = (const uint4*)vbuf[b] + (4 * sub + grp) * 64 + row;
-        uint4 vw[2][2];
+          if constexpr (PARTS == 1) {  // of the rounded weights: half the instructions, and they add up to 1
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
+            for (int j = 0; j < 8; j += 2) sum = __builtin_amdgcn_fdot2(half2v{pw[t][0][j], pw[t][0][j + 1]}, half2v{(_Float16)1.f, (_Float16)1.f}, sum, false);
+          } else {
 #pragma unroll
-          for (int p = 0; p < 2; ++p) vw[t][p] = vrow[128 * t + 32 * p];
-        if (edge) {  // tokens that no row sees may hold anything; NaN that only some rows see is brought back to those
-          uint32_t nans = 0;
-#pragma unroll
-          for (int t = 0; t < 2; ++t) {
-            uint32_t keep[2] = {0, 0};
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-              const int tt = t0 + 16 * t + 8 * grp + j;
-              const bool seen = !bad[t] && tt <= w_hi && (!a.n_recent || tt < a.n_sink || (int64_t)tt > (int64_t)w_lo - a.n_recent);
-              keep[j / 4] |= seen ? 0xffu << (8 * (j % 4)) : 0u;
-            }
-#pragma unroll
-            for (int p = 0; p < 2; ++p) {
-              vw[t][p].x &= keep[0], vw[t][p].y &= keep[1], vw[t][p].z &= keep[0], vw[t][p].w &= keep[1];
-              nans |= nan_bytes(vw[t][p].x) | nan_bytes(vw[t][p].y) | nan_bytes(vw[t][p].z) | nan_bytes(vw[t][p].w);
-            }
+            for (int j = 0; j < 8; ++j) sum += y[j];
           }
-          if (__any(nans != 0)) {
+          l += sum * inv[t];
+        }
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          uint4 v[2];
+#pragma unroll
+          for (int p = 0; p < 2; ++p) v[p] = ((const uint4*)vbuf[b])[(2 * t + grp) * 64 + 32 * p + row];
+          if constexpr (EDGE) {  // tokens that no row sees may hold anything; NaN that only some rows see is brought back to those
+            uint32_t keep[2] = {0, 0}, nans = 0;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) keep[j / 4] |= sees(base + 16 * t + j, w_from, w_hi, sink) ? 0xffu << (8 * (j % 4)) : 0u;
 #pragma unroll
             for (int p = 0; p < 2; ++p) {
-              floatx16 hit[2];
+              v[p].x &= keep[0], v[p].y &= keep[1], v[p].z &= keep[0], v[p].w &= keep[1];
+              nans |= nan_bytes(v[p].x) | nan_bytes(v[p].y) | nan_bytes(v[p].z) | nan_bytes(v[p].w);
+            }
+            if (__builtin_expect(__any(nans != 0), 0)) {
+              half8 one;
 #pragma unroll
-              for (int c = 0; c < 2; ++c)
+              for (int j = 0; j < 8; ++j) one[j] = sees(base + 16 * t + j, from, pos, sink) ? (_Float16)1.f : (_Float16)0.f;
 #pragma unroll
-                for (int j = 0; j < 16; ++j) hit[c][j] = 0.f;
+              for (int p = 0; p < 2; ++p) {
+                const uint32_t n[4] = {nan_bytes(v[p].x), nan_bytes(v[p].y), nan_bytes(v[p].z), nan_bytes(v[p].w)};
+                v[p].x &= ~(n[0] * 0xffu), v[p].y &= ~(n[1] * 0xffu), v[p].z &= ~(n[2] * 0xffu), v[p].w &= ~(n[3] * 0xffu);
 #pragma unroll
-              for (int t = 0; t < 2; ++t) {
-                uint4& v = vw[t][p];
-                const uint32_t n[4] = {nan_bytes(v.x), nan_bytes(v.y), nan_bytes(v.z), nan_bytes(v.w)};
-                v.x &= ~(n[0] * 0xffu), v.y &= ~(n[1] * 0xffu), v.z &= ~(n[2] * 0xffu), v.w &= ~(n[3] * 0xffu);
-                hit[0] = __builtin_amdgcn_mfma_f32_32x32x16_f16(operand(n[0] * 0x38u, n[1] * 0x38u), sees[t], hit[0], 0, 0, 0);  // 0x38: 1
-                hit[1] = __builtin_amdgcn_mfma_f32_32x32x16_f16(operand(n[2] * 0x38u, n[3] * 0x38u), sees[t], hit[1], 0, 0, 0);
+                for (int c = 0; c < 2; ++c) {
+                  floatx16 hit;
+#pragma unroll
+                  for (int j = 0; j < 16; ++j) hit[j] = 0.f;
+                  hit = __builtin_amdgcn_mfma_f32_32x32x16_f16(operand(n[2 * c] * 0x38u, n[2 * c + 1] * 0x38u), one, hit, 0, 0, 0);  // 0x38: 1
+#pragma unroll
+                  for (int j = 0; j < 16; ++j) o[2 * p + c][j] += hit[j] > 0.f ? __builtin_nanf("") : 0.f;
+                }
               }
-#pragma unroll
-              for (int c = 0; c < 2; ++c)
-#pragma unroll
-                for (int j = 0; j < 16; ++j)
-                  if (hit[c][j] > 0.f) o[2 * p + c][j] = __builtin_nanf("");
             }
           }
-        }
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
 #pragma unroll
           for (int p = 0; p < 2; ++p) {
-            const half8 v0 = operand(vw[t][p].x, vw[t][p].y), v1 = operand(vw[t][p].z, vw[t][p].w);
+            const half8 v0 = operand(v[p].x, v[p].y), v1 = operand(v[p].z, v[p].w);
 #pragma unroll
             for (int u = PARTS - 1; u >= 0; --u) {
               o[2 * p] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v0, pw[t][u], o[2 * p], 0, 0, 0);
               o[2 * p + 1] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v1, pw[t][u], o[2 * p + 1], 0, 0, 0);
             }
           }
+        }
       }
       if (i + 1 < t_to) store_tile(b ^ 1);
       __syncthreads();
-    }
+    };
+    // The tiles that every row sees whole lie side by side, between the sinks and the window's left border and the diagonal.
+    const int full_from = max(t_from, a.n_recent ? max((window_from(a, p_hi) + kTile) / kTile - span.skip, span.sinks) : 0);
+    const int full_to = min(t_to, (p_lo + 1) / kTile - span.skip);
+    int i = t_from;
+    for (const int to = min(full_from, t_to); i < to; ++i) step(i, std::true_type{});
+    for (; i < full_to; ++i) step(i, std::false_type{});
+    for (; i < t_to; ++i) step(i, std::true_type{});
 
     l += __shfl_xor(l, 32);
     if (have) {
