@@ -68,16 +68,21 @@ hipError_t launch_pages_write(const Pages& S, int layer, int n_layers, bool bf16
 hipError_t launch_pages_read(const Pages& S, int layer, int n_layers, bool bf16, const int32_t* table, const int32_t* lens, int batch, int64_t n, void* K,
                              void* V, hipStream_t st);
 
+// The sequences of one kind of blocks.
+struct PagesRows {
+  int32_t over, to;          // rows (new tokens times query heads of a KV head): more than `over`, up to `to`
+  uint32_t grid, join_grid;  // workgroups
+  float* part;   // [slot][rows of a block][128]: sums of a part of the tokens
+  float2* stat;  // [slot][rows of a block]: (reference of the exponents, sum of weights)
+};
 struct PagesAttn {
   Pages S;
   int32_t layer, n_layers, batch, n_tokens, n_sink, n_recent;
-  int32_t rows_over, rows_to;  // the launch serves sequences of more rows (new tokens times query heads of a KV head) than rows_over, up to rows_to
   float scale;  // of the scores, times log2 e
   const void* q;
   void* out;
   const int32_t *starts, *table, *lens;
-  float* part;  // [slot][rows of a block][128]: sums of a part of the tokens
-  float2* stat; // [slot][rows of a block]: (reference of the exponents, sum of weights)
+  PagesRows few, many;
 };
 size_t pages_attn_bytes(const Pages& S, int batch, int n_tokens, bool bf16);
 hipError_t launch_pages_attn(PagesAttn a, bool bf16, void* ws, hipStream_t st);

@@ -36,121 +36,135 @@ struct Weights {
 
 // ------------------------------------------------------------------------------------------------ sharing out the work
 // A block is `rows` consecutive (new token, query head of the KV head) pairs of a sequence; its tokens are cut into parts, one workgroup each, such that
-// all parts of a call hold about the same number of tiles and there are about kParts of them.  Lengths live on the device, so every wave
-// works out the shares by itself (64 sequences at a time): the launch only has to be large enough.
-constexpr int kParts = 512;
+// all parts of a call hold about the same number of tiles and there are no more than `parts` of them, as many as the chip holds at a time (one more would run
+// alone in the end: 16 contexts of 4096 to 16384 tokens 90 us, with the blocks' last, shorter parts counted in 78).  Lengths live on the
+// device, so every wave works out the shares by itself, 64 sequences at a time: the launch only has to be large enough.
 constexpr int kLeastTiles = 4;
-constexpr int kFewRows = 64;  // sequences of up to so many rows go to pages_few_kernel, where a call has both
+constexpr int kFewRows = 64;  // sequences of up to so many rows go to few_rows, where a call may have both
 
-template <int ROWS, int TOKENS>
+template <int ROWS, int TOKENS, int PARTS>
 struct Geometry {
-  static constexpr int rows = ROWS, tile = TOKENS;  // of a block; of a tile
+  static constexpr int rows = ROWS, tile = TOKENS, parts = PARTS;  // of a block; of a tile; of a call
 };
 template <int R>
-using Few = Geometry<16 * R, 32>;
-using Many = Geometry<128, 64>;
+using Few = Geometry<16 * R, 32, 512>;
+using Many = Geometry<128, 64, 512>;
 
 struct Seq {
   int len, first, nq, rows, tiles;  // tokens, first new token (row of q), new tokens, rows of all blocks, most tiles of a block
 };
-
-template <class Geo>
-__device__ __forceinline__ Seq seq_of(const PagesAttn& a, int b) {
-  constexpr int BR = Geo::rows, kTile = Geo::tile;
-  Seq s;
-  s.len = min(max(a.lens[b], 0), a.S.max_pages << a.S.logP);
-  s.first = min(max(a.starts[b], 0), a.n_tokens);
-  s.nq = min(max(a.starts[b + 1], s.first), a.n_tokens) - s.first;
-  s.rows = s.nq * a.S.G;
-  if (s.rows <= a.rows_over || s.rows > a.rows_to) s.nq = s.rows = 0;
-  s.tiles = (s.len + kTile - 1) / kTile;
-  if (a.n_recent) {
-    const int sink = (min(a.n_sink, s.len) + kTile - 1) / kTile;
-    const int64_t span = (int64_t)a.n_recent + min(s.nq, BR / a.S.G + 2) + 2 * kTile;
-    s.tiles = (int)min((int64_t)s.tiles, sink + span / kTile);
-  }
-  return s;
-}
-
-__device__ __forceinline__ int blocks_of(int rows, int BR) { return (rows + BR - 1) / BR; }
-
 struct Shares {
-  int tiles;  // of a part
-  int parts;  // of all sequences, for one (layer, KV head)
-  int split;  // ... of blocks that are cut
+  int tiles;       // of a part
+  int parts;       // of all sequences, for one (layer, KV head)
+  int split;       // ... of blocks that are cut
   int split_rows;  // rows of sequences whose blocks are cut
 };
-__device__ __forceinline__ int parts_of(const Seq& s, int tiles) { return s.nq ? max(1, (s.tiles + tiles - 1) / tiles) : 0; }
-
-__device__ __forceinline__ int wave_sum(int x) {
-#pragma unroll
-  for (int d = 1; d < kWave; d <<= 1) x += __shfl_xor(x, d);
-  return x;
-}
-__device__ __forceinline__ float wave_sum(float x) {
-#pragma unroll
-  for (int d = 1; d < kWave; d <<= 1) x += __shfl_xor(x, d);
-  return x;
-}
-
-template <class Geo>
-__device__ Shares shares_of(const PagesAttn& a, int lane) {
-  float sum = 0.f;  // every wave adds in the same order: all agree
-  for (int b0 = 0; b0 < a.batch; b0 += kWave)
-    if (b0 + lane < a.batch) {
-      const Seq s = seq_of<Geo>(a, b0 + lane);
-      sum += (float)s.tiles * (float)blocks_of(s.rows, Geo::rows);
-    }
-  sum = wave_sum(sum) * (float)(a.n_layers * a.S.H);
-  Shares w;
-  w.tiles = max(kLeastTiles, (int)fminf(ceilf(sum / (float)kParts), 1e9f));
-  w.parts = w.split = w.split_rows = 0;
-  for (int b0 = 0; b0 < a.batch; b0 += kWave)
-    if (b0 + lane < a.batch) {
-      const Seq s = seq_of<Geo>(a, b0 + lane);
-      const int np = parts_of(s, w.tiles), n = np * blocks_of(s.rows, Geo::rows);
-      w.parts += n;
-      if (np > 1) w.split += n, w.split_rows += s.rows;
-    }
-  w.parts = wave_sum(w.parts), w.split = wave_sum(w.split), w.split_rows = wave_sum(w.split_rows);
-  return w;
-}
-
-// The sequence that holds entry y of a numbering that gives every sequence count(its Seq, its parts) entries: its index, y's place in it, and how many
-// parts of cut blocks the sequences before it have.
+// The sequence that holds entry y of a numbering that gives every sequence some entries: its index, y's place in it, its blocks' parts, and how
+// many parts of cut blocks the sequences before it have.
 struct Place {
   int b, at, before, np;
   Seq s;
 };
-template <class Geo, class Count>
-__device__ Place place_of(const PagesAttn& a, const Shares& w, int y, int lane, Count count) {
-  int done = 0, cut = 0;
-  for (int b0 = 0;; b0 += kWave) {
-    Seq s{0, 0, 0, 0, 0};
-    int np = 0, n = 0, c = 0;
-    if (b0 + lane < a.batch) {
-      s = seq_of<Geo>(a, b0 + lane);
-      np = parts_of(s, w.tiles);
-      n = count(s, np);
-      c = np > 1 ? np * blocks_of(s.rows, Geo::rows) : 0;
-    }
-    int in = n, cin = c;
-#pragma unroll
-    for (int d = 1; d < kWave; d <<= 1) {
-      const int u = __shfl_up(in, d), v = __shfl_up(cin, d);
-      if (lane >= d) in += u, cin += v;
-    }
-    const unsigned long long m = __ballot(y < done + in);
-    if (m || b0 + kWave >= a.batch) {  // always found: y is below the sum of all counts
-      const int src = m ? __builtin_ctzll(m) : 0;
-      const auto uni = [&](int x) { return __builtin_amdgcn_readlane(x, src); };
-      Place p;
-      p.b = b0 + src, p.at = y - done - uni(in - n), p.before = cut + uni(cin - c), p.np = uni(np);
-      p.s.len = uni(s.len), p.s.first = uni(s.first), p.s.nq = uni(s.nq), p.s.rows = uni(s.rows), p.s.tiles = uni(s.tiles);
-      return p;
-    }
-    done += __builtin_amdgcn_readlane(in, kWave - 1), cut += __builtin_amdgcn_readlane(cin, kWave - 1);
+
+// Inclusive sums over the lanes, within rows of 16 and then across them.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int from_lane(int x) {
+  return __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xf, false);
+}
+__device__ __forceinline__ int scan(int x) {
+  x += from_lane<0x111, 0xf>(x), x += from_lane<0x112, 0xf>(x), x += from_lane<0x114, 0xf>(x), x += from_lane<0x118, 0xf>(x);
+  x += from_lane<0x142, 0xa>(x);
+  return x + from_lane<0x143, 0xc>(x);
+}
+__device__ __forceinline__ float scan(float x) {
+  const auto add = [](float y, int z) { return y + __int_as_float(z); };
+  x = add(x, from_lane<0x111, 0xf>(__float_as_int(x))), x = add(x, from_lane<0x112, 0xf>(__float_as_int(x)));
+  x = add(x, from_lane<0x114, 0xf>(__float_as_int(x))), x = add(x, from_lane<0x118, 0xf>(__float_as_int(x)));
+  x = add(x, from_lane<0x142, 0xa>(__float_as_int(x)));
+  return add(x, from_lane<0x143, 0xc>(__float_as_int(x)));
+}
+__device__ __forceinline__ int last_lane(int x) { return __builtin_amdgcn_readlane(x, kWave - 1); }
+
+template <class Geo>
+class Schedule {
+ public:
+  Shares w;
+
+  __device__ __forceinline__ Schedule(const PagesAttn& args, const PagesRows& which, int lane) : a(args), which(which), lane(lane), head(load(lane)) {
+    float sum = 0.f, all_blocks = 0.f;  // every wave adds in the same order: all agree
+    each([&](int, const Seq& s) {
+      const float n = (float)blocks(s.rows);
+      sum += (float)s.tiles * n, all_blocks += n;
+    });
+    const float slices = (float)(a.n_layers * a.S.H);
+    sum = __int_as_float(last_lane(__float_as_int(scan(sum)))) * slices;
+    all_blocks = __int_as_float(last_lane(__float_as_int(scan(all_blocks)))) * slices;
+    w.tiles = max(kLeastTiles, (int)fminf(ceilf(sum / fmaxf((float)Geo::parts - all_blocks, 0.5f * (float)Geo::parts)), 1e9f));
+    int n = 0, cut = 0, cut_rows = 0;
+    each([&](int, const Seq& s) {
+      const int np = parts(s), all = np * blocks(s.rows);
+      n += all;
+      if (np > 1) cut += all, cut_rows += s.rows;
+    });
+    w.parts = last_lane(scan(n)), w.split = last_lane(scan(cut)), w.split_rows = last_lane(scan(cut_rows));
   }
+
+  static __device__ __forceinline__ int blocks(int rows) { return (rows + Geo::rows - 1) / Geo::rows; }
+  __device__ __forceinline__ int parts(const Seq& s) const { return s.nq ? max(1, (s.tiles + w.tiles - 1) / w.tiles) : 0; }
+
+  template <class Count>
+  __device__ __forceinline__ Place find(int y, Count count) const {
+    int done = 0, cut = 0;
+    for (int b0 = 0;; b0 += kWave) {
+      const Seq s = b0 == 0 ? head : load(b0 + lane);
+      const int np = parts(s), n = count(s, np), c = np > 1 ? np * blocks(s.rows) : 0, in = scan(n), cin = scan(c);
+      const unsigned long long m = __ballot(y < done + in);
+      if (m || b0 + kWave >= a.batch) {  // always found: y is below the sum of all counts
+        const int src = m ? __builtin_ctzll(m) : 0;
+        const auto uni = [&](int x) { return __builtin_amdgcn_readlane(x, src); };
+        return Place{b0 + src, y - done - uni(in - n), cut + uni(cin - c), uni(np), {uni(s.len), uni(s.first), uni(s.nq), uni(s.rows), uni(s.tiles)}};
+      }
+      done += last_lane(in), cut += last_lane(cin);
+    }
+  }
+
+ private:
+  const PagesAttn& a;
+  const PagesRows& which;
+  int lane;
+  Seq head;  // the lane's sequence of the first 64
+
+  template <class Do>
+  __device__ __forceinline__ void each(Do use) const {
+    use(0, head);
+    for (int b0 = kWave; b0 < a.batch; b0 += kWave) use(b0, load(b0 + lane));
+  }
+
+  __device__ __forceinline__ Seq load(int b) const {
+    Seq s{0, 0, 0, 0, 0};
+    if (b >= a.batch) return s;
+    s.len = min(max(a.lens[b], 0), a.S.max_pages << a.S.logP);
+    s.first = min(max(a.starts[b], 0), a.n_tokens);
+    s.nq = min(max(a.starts[b + 1], s.first), a.n_tokens) - s.first;
+    s.rows = s.nq * a.S.G;
+    if (s.rows <= which.over || s.rows > which.to) s.nq = s.rows = 0;
+    s.tiles = (s.len + Geo::tile - 1) / Geo::tile;
+    if (a.n_recent) {
+      const int sink = (min(a.n_sink, s.len) + Geo::tile - 1) / Geo::tile;
+      const uint32_t span = (uint32_t)a.n_recent + (uint32_t)(min(s.nq, Geo::rows / a.S.G + 2) + 2 * Geo::tile);
+      s.tiles = min(s.tiles, sink + (int)(span / (uint32_t)Geo::tile));
+    }
+    return s;
+  }
+};
+
+// Tiles of part k of n: as even as they can be.
+struct Share {
+  int from, to;
+};
+__device__ __forceinline__ Share share_of(int tiles, int k, int n) {
+  const int each = (int)((uint32_t)tiles / (uint32_t)n), more = tiles - each * n;
+  return Share{k * each + min(k, more), (k + 1) * each + min(k + 1, more)};
 }
 
 // ------------------------------------------------------------------------------------------------ operands
@@ -219,6 +233,19 @@ __device__ __forceinline__ void load_channels(const void* p, int64_t i, float* f
   }
 }
 
+template <bool BF16>
+__device__ __forceinline__ void store8(void* p, int64_t i, const float* y, float factor) {  // 8 channels
+  if constexpr (BF16) {
+    uint32_t w[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) w[j] = (uint32_t)f32_to_bf16(y[2 * j] * factor) | (uint32_t)f32_to_bf16(y[2 * j + 1] * factor) << 16;
+    *(uint4*)((uint16_t*)p + i) = make_uint4(w[0], w[1], w[2], w[3]);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; j += 4) *(float4*)((float*)p + i + j) = make_float4(y[j] * factor, y[j + 1] * factor, y[j + 2] * factor, y[j + 3] * factor);
+  }
+}
+
 // A row at position p sees the tokens (from, p] and those below sink.
 __device__ __forceinline__ int window_from(const PagesAttn& a, int p) { return a.n_recent ? max(p - a.n_recent, -1) : -1; }  // p >= -1, n_recent >= 0: no overflow
 __device__ __forceinline__ bool sees(int t, int from, int to, int sink) { return (t <= to) & ((t > from) | (t < sink)); }
@@ -235,7 +262,7 @@ __device__ __forceinline__ Span span_of(const PagesAttn& a, int p_lo, int p_hi) 
   const int end = p_hi / kTile + 1;
   int from = 0;
   if (a.n_recent) {
-    from = (int)(max((int64_t)0, (int64_t)p_lo - a.n_recent + 1) / kTile);
+    from = (window_from(a, max(p_lo, -1)) + 1) / kTile;
     s.sinks = a.n_sink > 0 ? min((min(a.n_sink, p_hi + 1) + kTile - 1) / kTile, end) : 0;
   }
   s.skip = max(from - s.sinks, 0);
@@ -249,80 +276,40 @@ struct Rows {
   half8 q[PARTS == 1 ? 1 : 4][PARTS];  // fp32: [chunk of 16 channels oct + 4 (c / 2)][8 of them: c % 2]
   intx8 q8[2];                         // bf16: both chunks, hi and lo
   floatx4 o[8];   // [16-byte load of V][channel of the pair]: row l % 16, channels 32 (i / 2) + 8 (l / 16) + 2 c + i % 2
-  float m, l, factor;
+  float m, l;
   int pos, from, eq;
 };
 
 // ------------------------------------------------------------------------------------------------ few rows
 // A workgroup has a part of the tokens of one block of 16 R rows; its four waves take the tiles in turn and join their sums in the end.  A tile of 32
-// tokens is 8 KB, eight 16-byte loads a lane, the next one's in flight while this one is multiplied: S^T = K Q^T leaves lane l
+// tokens is 8 KB, eight 16-byte loads a lane, the next one's on their way while this one is multiplied (two or three ahead are no faster): S^T = K Q^T leaves lane l
 // with row l % 16 and the 8 tokens of octet l / 16, which is how O^T = V^T P^T wants them, so nothing moves between lanes but the maximum.
+// Bound by memory where there is much of it, by the chain lengths -> table -> tokens -> sums where there is little: the first tile is on its
+// way before q is looked at.
 template <bool BF16, int R>
-__global__ __launch_bounds__(kWaves* kWave) void pages_few_kernel(PagesAttn a) {
+__device__ __forceinline__ void few_rows(const PagesAttn& a, uint32_t x0, uint32_t step) {
   using Geo = Few<R>;
   constexpr int PARTS = BF16 ? 1 : 2, BR = Geo::rows, kTile = Geo::tile, kQTop = Weights<BF16>::q_top;
-  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int row = lane & 15, oct = lane >> 4;
-  __shared__ __attribute__((aligned(16))) float join[2][BR][kHeadDim + 4];
-  __shared__ float2 join_stat[2][BR];
+  __shared__ __attribute__((aligned(16))) float join[kWaves][16][kHeadDim + 4];
+  __shared__ float2 join_stat[kWaves][16];
 
-  const Shares w = shares_of<Geo>(a, lane);
-  const int64_t all = (int64_t)w.parts * a.n_layers * a.S.H;
-  for (int64_t x = blockIdx.x; x < all; x += gridDim.x) {
-    const int lh = (int)(x % (a.n_layers * a.S.H));  // workgroups are dealt to the XCDs in turn: with 8 heads each reads one head's pages
-    const Place at = place_of<Geo>(a, w, (int)(x / (a.n_layers * a.S.H)), lane, [](const Seq& s, int np) { return np * blocks_of(s.rows, Geo::rows); });
+  const Schedule<Geo> plan(a, a.few, lane);
+  const uint32_t slices = (uint32_t)(a.n_layers * a.S.H), all = (uint32_t)plan.w.parts * slices;
+  for (uint32_t x = x0; x < all; x += step) {
+    const int lh = (int)(x % slices);  // workgroups are dealt to the XCDs in turn: with 8 heads each reads one head's pages
+    const Place at = plan.find((int)(x / slices), [](const Seq& s, int np) { return np * Schedule<Geo>::blocks(s.rows); });
     const Seq s = at.s;
-    const int block = blocks_of(s.rows, BR) - 1 - at.at / at.np, part = at.at % at.np, layer = lh / a.S.H, h = lh % a.S.H, G = a.S.G;
+    const int turn = (int)((uint32_t)at.at / (uint32_t)at.np), part = at.at - turn * at.np, block = plan.blocks(s.rows) - 1 - turn;
+    const int layer = (int)((uint32_t)lh / (uint32_t)a.S.H), h = lh - layer * a.S.H, G = a.S.G;
     const int row0 = block * BR, rows = min(s.rows - row0, BR);
     const int before = s.len - s.nq;  // position of the sequence's first new token
-    const int p_lo = before + row0 / G, p_hi = before + (row0 + rows - 1) / G;
+    const int p_lo = before + (int)((uint32_t)row0 / (uint32_t)G), p_hi = before + (int)((uint32_t)(row0 + rows - 1) / (uint32_t)G);
     const Span span = span_of<kTile>(a, p_lo, p_hi);
-    const int t_from = (int)((int64_t)span.n * part / at.np), t_to = (int)((int64_t)span.n * (part + 1) / at.np);
+    const Share mine = share_of(span.n, part, at.np);
     const int n_rt = (rows + 15) / 16;
     const int sink = a.n_recent ? a.n_sink : 0, all_from = window_from(a, max(p_lo, -1));
-
-    Rows<PARTS> rt[R];
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-      Rows<PARTS>& z = rt[r];
-      const int mine = row0 + 16 * r + row;
-      const bool have = 16 * r + row < rows;
-      z.pos = have ? max(before + mine / G, -1) : -1, z.from = window_from(a, z.pos);
-      z.m = -FLT_MAX, z.l = 0.f;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) z.o[i] = floatx4{0.f, 0.f, 0.f, 0.f};
-      float f[2][16];
-      float top = 0.f;
-      if (have) {
-        const int64_t base = (((int64_t)layer * a.n_tokens + s.first + mine / G) * (a.S.H * G) + h * G + mine % G) * kHeadDim;
-#pragma unroll
-        for (int p = 0; p < 2; ++p) load_channels<BF16>(a.q, base + 64 * p + 16 * oct, f[p]);
-      } else {
-#pragma unroll
-        for (int p = 0; p < 2; ++p)
-#pragma unroll
-          for (int c = 0; c < 16; ++c) f[p][c] = 0.f;
-      }
-#pragma unroll
-      for (int p = 0; p < 2; ++p)
-#pragma unroll
-        for (int c = 0; c < 16; ++c) top = fmaxf(top, fabsf(f[p][c]));
-      top = max_over_16s(top);
-      z.eq = max((int)(__float_as_uint(top) >> 23) - 127, kLeastExponent);
-#pragma unroll
-      for (int p = 0; p < 2; ++p)
-#pragma unroll
-        for (int c = 0; c < 16; ++c) f[p][c] = ldexpf(f[p][c], kQTop - z.eq);
-      if constexpr (BF16) {
-        int hi[8], lo[8];
-        to_bytes(f[0], hi, lo), to_bytes(f[1], hi + 4, lo + 4);
-#pragma unroll
-        for (int c = 0; c < 8; ++c) z.q8[0][c] = hi[c], z.q8[1][c] = lo[c];
-      } else {
-#pragma unroll
-        for (int c = 0; c < 4; ++c) to_halves<8, PARTS>(f[c / 2] + 8 * (c % 2), z.q[c]);
-      }
-    }
 
     // pages of a lane's octets: that of its K row and that of its tokens in V and in the scores
     const int32_t* table = a.table + (int64_t)at.b * a.S.max_pages;
@@ -357,19 +344,63 @@ __global__ __launch_bounds__(kWaves* kWave) void pages_few_kernel(PagesAttn a) {
       d.e = *(const int2*)(a.S.exponents + 2 * vh);
       return d;
     };
-
-    const int first = t_from + wave;
+    const int first = mine.from + wave;
     Ids id{0, 0};
     Data next{};
-    if (first < t_to) {
+    if (first < mine.to) {
       next = load_tile(first, pages_at(first));
-      if (first + kWaves < t_to) id = pages_at(first + kWaves);
+      if (first + kWaves < mine.to) id = pages_at(first + kWaves);
     }
-    for (int i = first; i < t_to; i += kWaves) {
+
+    Rows<PARTS> rt[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      Rows<PARTS>& z = rt[r];
+      const uint32_t n = (uint32_t)(row0 + 16 * r + row);  // of the sequence's rows
+      const int token = (int)(n / (uint32_t)G);
+      const bool have = 16 * r + row < rows;
+      z.pos = have ? max(before + token, -1) : -1, z.from = window_from(a, z.pos);
+      z.m = -FLT_MAX, z.l = 0.f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) z.o[i] = floatx4{0.f, 0.f, 0.f, 0.f};
+      float f[2][16];
+      float top = 0.f;
+      if (have) {
+        const int64_t base = (((int64_t)layer * a.n_tokens + s.first + token) * (a.S.H * G) + h * G + (int)(n - (uint32_t)token * (uint32_t)G)) * kHeadDim;
+#pragma unroll
+        for (int p = 0; p < 2; ++p) load_channels<BF16>(a.q, base + 64 * p + 16 * oct, f[p]);
+      } else {
+#pragma unroll
+        for (int p = 0; p < 2; ++p)
+#pragma unroll
+          for (int c = 0; c < 16; ++c) f[p][c] = 0.f;
+      }
+#pragma unroll
+      for (int p = 0; p < 2; ++p)
+#pragma unroll
+        for (int c = 0; c < 16; ++c) top = fmaxf(top, fabsf(f[p][c]));
+      top = max_over_16s(top);
+      z.eq = max((int)(__float_as_uint(top) >> 23) - 127, kLeastExponent);
+#pragma unroll
+      for (int p = 0; p < 2; ++p)
+#pragma unroll
+        for (int c = 0; c < 16; ++c) f[p][c] = ldexpf(f[p][c], kQTop - z.eq);
+      if constexpr (BF16) {
+        int hi[8], lo[8];
+        to_bytes(f[0], hi, lo), to_bytes(f[1], hi + 4, lo + 4);
+#pragma unroll
+        for (int c = 0; c < 8; ++c) z.q8[0][c] = hi[c], z.q8[1][c] = lo[c];
+      } else {
+#pragma unroll
+        for (int c = 0; c < 4; ++c) to_halves<8, PARTS>(f[c / 2] + 8 * (c % 2), z.q[c]);
+      }
+    }
+
+    for (int i = first; i < mine.to; i += kWaves) {
       Data d = next;
-      if (i + kWaves < t_to) {
+      if (i + kWaves < mine.to) {
         next = load_tile(i + kWaves, id);
-        if (i + 2 * kWaves < t_to) id = pages_at(i + 2 * kWaves);
+        if (i + 2 * kWaves < mine.to) id = pages_at(i + 2 * kWaves);
       }
       const int t0 = span.tile(i) * kTile, t1 = t0 + kTile - 1, j0 = t0 + 8 * oct;
       // whether every row sees the whole tile
@@ -378,11 +409,7 @@ __global__ __launch_bounds__(kWaves* kWave) void pages_few_kernel(PagesAttn a) {
       if (edge) {  // tokens that no row sees may hold anything
         uint32_t keep[2] = {0, 0};
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const int t = j0 + j;
-          const bool seen = !d.bad & sees(t, all_from, p_hi, sink);
-          keep[j / 4] |= seen ? 0xffu << (8 * (j % 4)) : 0u;
-        }
+        for (int j = 0; j < 8; ++j) keep[j / 4] |= (!d.bad & sees(j0 + j, all_from, p_hi, sink)) ? 0xffu << (8 * (j % 4)) : 0u;
         uint32_t nans = 0;
 #pragma unroll
         for (int p = 0; p < 4; ++p) {
@@ -399,7 +426,7 @@ __global__ __launch_bounds__(kWaves* kWave) void pages_few_kernel(PagesAttn a) {
 #pragma unroll
           for (int p = 0; p < 2; ++p) kf[u][2 * p] = operand(d.k[u][p].x, d.k[u][p].y), kf[u][2 * p + 1] = operand(d.k[u][p].z, d.k[u][p].w);
       const float ev = (float)d.e.y;
-      half8 pw[R][PARTS], ones[R];
+      half8 pw[R][PARTS];
 #pragma unroll
       for (int r = 0; r < R; ++r) {
         if (r >= n_rt) continue;
@@ -426,12 +453,7 @@ __global__ __launch_bounds__(kWaves* kWave) void pages_few_kernel(PagesAttn a) {
         for (int j = 0; j < 8; ++j) sc[j] = sc[j] * factor + ev;
         if (edge) {
 #pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            const int t = j0 + j;
-            const bool seen = !d.bad & sees(t, z.from, z.pos, sink);
-            ones[r][j] = seen ? (_Float16)1.f : (_Float16)0.f;
-            sc[j] = seen ? sc[j] : -__builtin_inff();
-          }
+          for (int j = 0; j < 8; ++j) sc[j] = (!d.bad & sees(j0 + j, z.from, z.pos, sink)) ? sc[j] : -__builtin_inff();
         }
         float top = sc[0];
 #pragma unroll
@@ -450,94 +472,80 @@ __global__ __launch_bounds__(kWaves* kWave) void pages_few_kernel(PagesAttn a) {
         z.l += ldexpf(sum, -d.e.y);
         to_halves<8, PARTS>(y, pw[r]);
       }
-      half8 vf[8];
 #pragma unroll
       for (int p = 0; p < 4; ++p) {
         uint4 v = d.v[p];
-        if (poison) {  // NaN where only some rows may see it: taken out here, brought back to those rows
+        if (__builtin_expect(poison, 0)) {  // NaN where only some rows may see it: taken out here, brought back to those rows
           const uint32_t n[4] = {nan_bytes(v.x), nan_bytes(v.y), nan_bytes(v.z), nan_bytes(v.w)};
           v.x &= ~(n[0] * 0xffu), v.y &= ~(n[1] * 0xffu), v.z &= ~(n[2] * 0xffu), v.w &= ~(n[3] * 0xffu);
           const half8 bad[2] = {operand(n[0] * 0x38u, n[1] * 0x38u), operand(n[2] * 0x38u, n[3] * 0x38u)};  // 0x38: 1
 #pragma unroll
           for (int r = 0; r < R; ++r) {
-            if (r >= n_rt) continue;
+            half8 one;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) one[j] = (!d.bad & sees(j0 + j, rt[r].from, rt[r].pos, sink)) ? (_Float16)1.f : (_Float16)0.f;
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
-              const floatx4 hit = __builtin_amdgcn_mfma_f32_16x16x32_f16(bad[c], ones[r], floatx4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+              const floatx4 hit = __builtin_amdgcn_mfma_f32_16x16x32_f16(bad[c], one, floatx4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
 #pragma unroll
-              for (int j = 0; j < 4; ++j)
-                if (hit[j] > 0.f) rt[r].o[2 * p + c][j] = __builtin_nanf("");
+              for (int j = 0; j < 4; ++j) rt[r].o[2 * p + c][j] += hit[j] > 0.f ? __builtin_nanf("") : 0.f;
             }
           }
         }
-        vf[2 * p] = operand(v.x, v.y), vf[2 * p + 1] = operand(v.z, v.w);
-      }
+        const half8 v0 = operand(v.x, v.y), v1 = operand(v.z, v.w);
 #pragma unroll
-      for (int r = 0; r < R; ++r) {
-        if (r >= n_rt) continue;
+        for (int r = 0; r < R; ++r) {
+          if (r >= n_rt) continue;
 #pragma unroll
-        for (int c = 0; c < 8; ++c)
-#pragma unroll
-          for (int p = PARTS - 1; p >= 0; --p) rt[r].o[c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf[c], pw[r][p], rt[r].o[c], 0, 0, 0);
+          for (int u = PARTS - 1; u >= 0; --u) {
+            rt[r].o[2 * p] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, pw[r][u], rt[r].o[2 * p], 0, 0, 0);
+            rt[r].o[2 * p + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, pw[r][u], rt[r].o[2 * p + 1], 0, 0, 0);
+          }
+        }
       }
     }
 
-    // the four waves' sums: 2 and 3 to 0 and 1, then 1 to 0
+    // the four waves' sums of 16 rows at a time, then 8 channels of a row to each thread
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-      rt[r].l += __shfl_xor(rt[r].l, 16);
-      rt[r].l += __shfl_xor(rt[r].l, 32);
-    }
+      if (r >= n_rt) continue;
+      Rows<PARTS>& z = rt[r];
+      z.l += __shfl_xor(z.l, 16);
+      z.l += __shfl_xor(z.l, 32);
+      if (r) __syncthreads();
 #pragma unroll
-    for (int from = 2; from >= 1; --from) {
+      for (int p = 0; p < 4; ++p) {
+        float* to = join[wave][row] + 32 * p + 8 * oct;
+        *(float4*)to = make_float4(z.o[2 * p][0], z.o[2 * p + 1][0], z.o[2 * p][1], z.o[2 * p + 1][1]);
+        *(float4*)(to + 4) = make_float4(z.o[2 * p][2], z.o[2 * p + 1][2], z.o[2 * p][3], z.o[2 * p + 1][3]);
+      }
+      if (oct == 0) join_stat[wave][row] = make_float2(z.m, z.l);
       __syncthreads();
-      if (wave >= from && wave < 2 * from)
+      const int jr = threadIdx.x >> 4, jc = 8 * (threadIdx.x & 15);
+      float2 st[kWaves];
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
-          float* at_row = join[wave - from][16 * r + row] + 8 * oct;
+      for (int v = 0; v < kWaves; ++v) st[v] = join_stat[v][jr];
+      const float m = fmaxf(fmaxf(st[0].x, st[1].x), fmaxf(st[2].x, st[3].x));
+      float y[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, l = 0.f;
 #pragma unroll
-          for (int c = 0; c < 8; ++c)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) at_row[32 * (c / 2) + 2 * j + c % 2] = rt[r].o[c][j];
-          if (oct == 0) join_stat[wave - from][16 * r + row] = make_float2(rt[r].m, rt[r].l);
-        }
-      __syncthreads();
-      if (wave < from)
-#pragma unroll
-        for (int r = 0; r < R; ++r) {
-          Rows<PARTS>& z = rt[r];
-          const float* at_row = join[wave][16 * r + row] + 8 * oct;
-          const float2 st = join_stat[wave][16 * r + row];
-          const float m = fmaxf(z.m, st.x), f0 = __builtin_amdgcn_exp2f(z.m - m), f1 = __builtin_amdgcn_exp2f(st.x - m);
-          z.m = m, z.l = z.l * f0 + st.y * f1;
-#pragma unroll
-          for (int c = 0; c < 8; ++c)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) z.o[c][j] = z.o[c][j] * f0 + at_row[32 * (c / 2) + 2 * j + c % 2] * f1;
-        }
-    }
-    if (wave == 0) {
-#pragma unroll
-      for (int r = 0; r < R; ++r) {
-        const Rows<PARTS>& z = rt[r];
-        if (16 * r + row >= rows) continue;
-        if (at.np == 1) {
-          const int mine = row0 + 16 * r + row;
-          const int64_t base = (((int64_t)layer * a.n_tokens + s.first + mine / G) * (a.S.H * G) + h * G + mine % G) * kHeadDim + 8 * oct;
-          const float inv = z.l == 0.f ? 0.f : 1.f / z.l;
-#pragma unroll
-          for (int c = 0; c < 8; ++c)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) store_kv<BF16>(a.out, base + 32 * (c / 2) + 2 * j + c % 2, z.o[c][j] * inv);
-        } else {
-          const int64_t slot = (int64_t)lh * w.split + at.before + at.at;
-          float* to = a.part + (slot * BR + 16 * r + row) * kHeadDim + 8 * oct;
-#pragma unroll
-          for (int c = 0; c < 8; ++c)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) to[32 * (c / 2) + 2 * j + c % 2] = z.o[c][j];
-          if (oct == 0) a.stat[slot * BR + 16 * r + row] = make_float2(z.m, z.l);
-        }
+      for (int v = 0; v < kWaves; ++v) {
+        const float fade = __builtin_amdgcn_exp2f(st[v].x - m);
+        const float4 lo = *(const float4*)(join[v][jr] + jc), hi = *(const float4*)(join[v][jr] + jc + 4);
+        l += st[v].y * fade;
+        y[0] += lo.x * fade, y[1] += lo.y * fade, y[2] += lo.z * fade, y[3] += lo.w * fade;
+        y[4] += hi.x * fade, y[5] += hi.y * fade, y[6] += hi.z * fade, y[7] += hi.w * fade;
+      }
+      if (16 * r + jr >= rows) continue;
+      if (at.np == 1) {
+        const uint32_t n = (uint32_t)(row0 + 16 * r + jr);
+        const int token = (int)(n / (uint32_t)G);
+        store8<BF16>(a.out, (((int64_t)layer * a.n_tokens + s.first + token) * (a.S.H * G) + h * G + (int)(n - (uint32_t)token * (uint32_t)G)) * kHeadDim + jc, y,
+                     l == 0.f ? 0.f : 1.f / l);
+      } else {
+        const int64_t slot = (int64_t)lh * plan.w.split + at.before + at.at;
+        float* to = a.few.part + (slot * BR + 16 * r + jr) * kHeadDim + jc;
+        *(float4*)to = make_float4(y[0], y[1], y[2], y[3]), *(float4*)(to + 4) = make_float4(y[4], y[5], y[6], y[7]);
+        if (jc == 0) a.few.stat[slot * BR + 16 * r + jr] = make_float2(m, l);
       }
     }
     __syncthreads();
@@ -550,35 +558,38 @@ __global__ __launch_bounds__(kWaves* kWave) void pages_few_kernel(PagesAttn a) {
 // S^T = K Q^T leaves lane l with row l % 32 and tokens 16 t + 8 (l / 32) + j, the operand of O^T = V^T P^T.  K's 16-byte chunks are
 // swizzled by their token so that the eight lanes of a bank group read eight different ones.
 template <bool BF16>
-__global__ __launch_bounds__(kWaves* kWave, BF16 ? 2 : 1) void pages_many_kernel(PagesAttn a) {
+__device__ __forceinline__ uint32_t many_rows(const PagesAttn& a, uint32_t x0, uint32_t step) {  // returns the workgroups' number
   using Geo = Many;
   constexpr int PARTS = BF16 ? 1 : 2, BR = Geo::rows, kTile = Geo::tile, kHalf = 32, kQTop = Weights<BF16>::q_top;
   constexpr float kLift = Weights<BF16>::lift;
   static_assert(BR == 32 * kWaves && kTile == 2 * kHalf, "");
-  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int row = lane & 31, grp = lane >> 5;
   __shared__ __attribute__((aligned(16))) uint8_t kbuf[2][kTile * kHeadDim], vbuf[2][kTile * kHeadDim];
   __shared__ float4 meta[2][kTile / kOct];  // of the octets' pages: scale 2^(eK - kQTop), eV, 2^-eV
 
-  const Shares w = shares_of<Geo>(a, lane);
-  const int64_t all = (int64_t)w.parts * a.n_layers * a.S.H;
-  for (int64_t x = blockIdx.x; x < all; x += gridDim.x) {
-    const int lh = (int)(x % (a.n_layers * a.S.H));
-    const Place at = place_of<Geo>(a, w, (int)(x / (a.n_layers * a.S.H)), lane, [](const Seq& s, int np) { return np * blocks_of(s.rows, BR); });
+  const Schedule<Geo> plan(a, a.many, lane);
+  const uint32_t slices = (uint32_t)(a.n_layers * a.S.H), all = (uint32_t)plan.w.parts * slices;
+  for (uint32_t x = x0; x < all; x += step) {
+    const int lh = (int)(x % slices);
+    const Place at = plan.find((int)(x / slices), [](const Seq& s, int np) { return np * Schedule<Geo>::blocks(s.rows); });
     const Seq s = at.s;
-    const int block = blocks_of(s.rows, BR) - 1 - at.at / at.np, part = at.at % at.np, layer = lh / a.S.H, h = lh % a.S.H, G = a.S.G;
+    const int turn = (int)((uint32_t)at.at / (uint32_t)at.np), part = at.at - turn * at.np, block = plan.blocks(s.rows) - 1 - turn;  // the longest first
+    const int layer = (int)((uint32_t)lh / (uint32_t)a.S.H), h = lh - layer * a.S.H, G = a.S.G;
     const int row0 = block * BR, rows = min(s.rows - row0, BR), before = s.len - s.nq;
-    const int p_lo = before + row0 / G, p_hi = before + (row0 + rows - 1) / G;
+    const int p_lo = before + (int)((uint32_t)row0 / (uint32_t)G), p_hi = before + (int)((uint32_t)(row0 + rows - 1) / (uint32_t)G);
     const Span span = span_of<kTile>(a, p_lo, p_hi);
-    const int t_from = (int)((int64_t)span.n * part / at.np), t_to = (int)((int64_t)span.n * (part + 1) / at.np);
+    const Share share = share_of(span.n, part, at.np);
+    const int t_from = share.from, t_to = share.to;
 
-    const int mine = row0 + 32 * wave + row;  // of the sequence's rows
+    const uint32_t mine = (uint32_t)(row0 + 32 * wave + row);  // of the sequence's rows
+    const int token = (int)(mine / (uint32_t)G);
     const bool have = 32 * wave + row < rows;
-    const int pos = have ? max(before + mine / G, -1) : -1;
+    const int pos = have ? max(before + token, -1) : -1;
     const bool any_row = 32 * wave < rows;
     const int w_lo = before + (row0 + 32 * wave) / G, w_hi = any_row ? before + (row0 + min(32 * wave + 32, rows) - 1) / G : -1;  // positions of the wave's rows
     const int sink = a.n_recent ? a.n_sink : 0, from = window_from(a, pos), w_from = window_from(a, max(w_lo, -1));
-    const int64_t out_at = (((int64_t)layer * a.n_tokens + s.first + mine / G) * (a.S.H * G) + h * G + mine % G) * kHeadDim;
+    const int64_t out_at = (((int64_t)layer * a.n_tokens + s.first + token) * (a.S.H * G) + h * G + (int)(mine - (uint32_t)token * (uint32_t)G)) * kHeadDim;
 
     half8 q[BF16 ? 1 : 8][PARTS];  // fp32: [chunk of 16 channels 2 (c / 2) + grp][8 of them: c % 2]
     intx8 q8[2][2];                // bf16: [two chunks][hi, lo]
@@ -815,9 +826,9 @@ __global__ __launch_bounds__(kWaves* kWave, BF16 ? 2 : 1) void pages_many_kernel
     l += __shfl_xor(l, 32);
     if (have) {
       const bool whole = at.np == 1;
-      const int64_t slot = (int64_t)lh * w.split + at.before + at.at;
-      const float inv = !whole ? 1.f : l == 0.f ? 0.f : 1.f / l;
-      float* to = a.part + (slot * BR + 32 * wave + row) * kHeadDim;
+      const int64_t slot = (int64_t)lh * plan.w.split + at.before + at.at;
+      const float inv = l == 0.f ? 0.f : 1.f / l;
+      float* to = a.many.part + (slot * BR + 32 * wave + row) * kHeadDim;
 #pragma unroll
       for (int p = 0; p < 2; ++p)
 #pragma unroll
@@ -825,106 +836,135 @@ __global__ __launch_bounds__(kWaves* kWave, BF16 ? 2 : 1) void pages_many_kernel
           const int c0 = 64 * p + 16 * r + 8 * grp;
           float y[8];
 #pragma unroll
-          for (int j = 0; j < 4; ++j) y[2 * j] = o[2 * p][4 * r + j] * inv, y[2 * j + 1] = o[2 * p + 1][4 * r + j] * inv;
+          for (int j = 0; j < 4; ++j) y[2 * j] = o[2 * p][4 * r + j], y[2 * j + 1] = o[2 * p + 1][4 * r + j];
           if (whole) {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) store_kv<BF16>(a.out, out_at + c0 + j, y[j]);
+            store8<BF16>(a.out, out_at + c0, y, inv);
           } else {
             *(float4*)(to + c0) = make_float4(y[0], y[1], y[2], y[3]), *(float4*)(to + c0 + 4) = make_float4(y[4], y[5], y[6], y[7]);
           }
         }
-      if (!whole && grp == 0) a.stat[slot * BR + 32 * wave + row] = make_float2(m, l);
+      if (!whole && grp == 0) a.many.stat[slot * BR + 32 * wave + row] = make_float2(m, l);
     }
   }
+  return all;
 }
 
-// Rows whose tokens were shared out: one workgroup per row, its waves take the parts in turn.
+// ------------------------------------------------------------------------------------------------ joining the parts
+// Rows whose tokens were shared out.  Few of them: a workgroup for each, its waves take the parts in turn.  Many: a wave for each.
+constexpr uint32_t kManyJoined = 4096;
 template <bool BF16, class Geo>
-__global__ __launch_bounds__(kWaves* kWave) void pages_join_kernel(PagesAttn a) {
+__device__ __forceinline__ void join_rows(const PagesAttn& a, const PagesRows& which, uint32_t block_id) {
   constexpr int BR = Geo::rows;
-  __shared__ float2 sums[kWaves][kWave];
-  __shared__ float dens[kWaves];
-  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-  const Shares w = shares_of<Geo>(a, lane);
-  const int64_t all = (int64_t)w.split_rows * a.n_layers * a.S.H;
-  for (int64_t x = blockIdx.x; x < all; x += gridDim.x) {
-    const int lh = (int)(x / w.split_rows);
-    const Place at = place_of<Geo>(a, w, (int)(x % w.split_rows), lane, [](const Seq& s, int np) { return np > 1 ? s.rows : 0; });
-    const int r = at.at, G = a.S.G;
-    const int64_t slot = (int64_t)lh * w.split + at.before + (int64_t)(blocks_of(at.s.rows, BR) - 1 - r / BR) * at.np;
-    const float2* stat = a.stat + slot * BR + r % BR;
-    const float* part = a.part + (slot * BR + r % BR) * kHeadDim + 2 * lane;
-    float m = -FLT_MAX;
-    for (int k = lane; k < at.np; k += kWave) m = fmaxf(m, stat[(int64_t)k * BR].x);
-#pragma unroll
-    for (int d = 1; d < kWave; d <<= 1) m = fmaxf(m, __shfl_xor(m, d));
+  __shared__ float2 sums[kWaves][kWave], stats[kWaves];
+  const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const Schedule<Geo> plan(a, which, lane);
+  const uint32_t slices = (uint32_t)(a.n_layers * a.S.H), all = (uint32_t)plan.w.split_rows * slices;
+  const bool many = all > kManyJoined;
+  const uint32_t step = many ? which.join_grid * kWaves : which.join_grid;
+  for (uint32_t x = many ? block_id * kWaves + wave : block_id; x < all; x += step) {
+    const int lh = (int)(x / (uint32_t)plan.w.split_rows);
+    const Place at = plan.find((int)(x - (uint32_t)lh * (uint32_t)plan.w.split_rows), [](const Seq& s, int np) { return np > 1 ? s.rows : 0; });
+    const int r = at.at, block = r / BR;
+    const int64_t slot = (int64_t)lh * plan.w.split + at.before + (plan.blocks(at.s.rows) - 1 - block) * at.np;
+    const float2* stat = which.stat + slot * BR + (r - block * BR);
+    const float* part = which.part + (slot * BR + (r - block * BR)) * kHeadDim + 2 * lane;
+    const int k0 = many ? 0 : wave, dk = many ? 1 : kWaves;
+    float m = -FLT_MAX, l = 0.f;
     float2 o = make_float2(0.f, 0.f);
-    float l = 0.f;
-    for (int k = wave; k < at.np; k += kWaves) {
-      const float2 st = stat[(int64_t)k * BR], v = *(const float2*)(part + (int64_t)k * BR * kHeadDim);
-      const float f = __builtin_amdgcn_exp2f(st.x - m);
-      o.x += v.x * f, o.y += v.y * f, l += st.y * f;
-    }
-    sums[wave][lane] = o;
-    if (lane == 0) dens[wave] = l;
-    __syncthreads();
-    if (wave == 0) {
+    const auto add = [&](float2 st, float2 v) {  // (reference, sum of weights), sum
+      const float up = fmaxf(m, st.x), f = __builtin_amdgcn_exp2f(m - up), g = __builtin_amdgcn_exp2f(st.x - up);
+      o.x = o.x * f + v.x * g, o.y = o.y * f + v.y * g, l = l * f + st.y * g, m = up;
+    };
+#pragma unroll 8
+    for (int k = k0; k < at.np; k += dk) add(stat[(int64_t)k * BR], *(const float2*)(part + (int64_t)k * BR * kHeadDim));
+    if (!many) {
+      sums[wave][lane] = o;
+      if (lane == 0) stats[wave] = make_float2(m, l);
+      __syncthreads();
+      m = -FLT_MAX, l = 0.f, o = make_float2(0.f, 0.f);
 #pragma unroll
-      for (int i = 1; i < kWaves; ++i) o.x += sums[i][lane].x, o.y += sums[i][lane].y, l += dens[i];
-      const float inv = l == 0.f ? 0.f : 1.f / l;
-      const int layer = lh / a.S.H, h = lh % a.S.H;
-      const int64_t base = (((int64_t)layer * a.n_tokens + at.s.first + r / G) * (a.S.H * G) + h * G + r % G) * kHeadDim + 2 * lane;
-      store_kv<BF16>(a.out, base, o.x * inv), store_kv<BF16>(a.out, base + 1, o.y * inv);
+      for (int i = 0; i < kWaves; ++i) add(stats[i], sums[i][lane]);
+      __syncthreads();
+      if (wave) continue;
     }
-    __syncthreads();
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    const int layer = (int)((uint32_t)lh / (uint32_t)a.S.H), h = lh - layer * a.S.H, G = a.S.G, token = (int)((uint32_t)r / (uint32_t)G);
+    const int64_t base = (((int64_t)layer * a.n_tokens + at.s.first + token) * (a.S.H * G) + h * G + r - token * G) * kHeadDim + 2 * lane;
+    if constexpr (BF16) *(uint32_t*)((uint16_t*)a.out + base) = (uint32_t)f32_to_bf16(o.x * inv) | (uint32_t)f32_to_bf16(o.y * inv) << 16;
+    else *(float2*)((float*)a.out + base) = make_float2(o.x * inv, o.y * inv);
   }
 }
 
-// Parts of cut blocks: a block of more than w.tiles tiles has fewer than 2 tiles / w.tiles of them, all blocks together kParts w.tiles tiles (rounding: + 64).
-constexpr int64_t kMostCut = 2 * kParts + 64;
+// ------------------------------------------------------------------------------------------------ launches
+// R: row tiles of few_rows (0: none), MANY: many_rows too.  A call that may have both kinds of sequences is one launch, the blocks of many rows first: the
+// others fill what these leave free in the end.  (Two 1000-token prompts beside six single tokens, windows: four launches 206 us, one and a join 181.)
+template <bool BF16, int R, bool MANY>
+__global__ __launch_bounds__(kWaves* kWave, BF16 ? (R <= 2 ? 2 : 1) : (R == 1 && !MANY ? 2 : 1)) void pages_attn_kernel(PagesAttn a) {
+  uint32_t x = blockIdx.x;
+  if constexpr (MANY) {
+    const uint32_t n = many_rows<BF16>(a, x, gridDim.x);
+    if (x < n) x += (n - x + gridDim.x - 1) / gridDim.x * gridDim.x;  // its next turn
+    x -= n;
+  }
+  if constexpr (R > 0) few_rows<BF16, R>(a, x, gridDim.x);
+}
+template <bool BF16, int R, bool MANY>
+__global__ __launch_bounds__(kWaves* kWave) void pages_join_kernel(PagesAttn a) {
+  if constexpr (R > 0)
+    if (!MANY || blockIdx.x < a.few.join_grid) return join_rows<BF16, Few<R>>(a, a.few, blockIdx.x);
+  if constexpr (MANY) join_rows<BF16, Many>(a, a.many, blockIdx.x - a.few.join_grid);
+}
+
+// Parts of cut blocks: a block of more than w.tiles tiles has fewer than 2 tiles / w.tiles of them, all blocks together `parts` times w.tiles tiles (rounding: + 64).
+template <class Geo>
+constexpr int64_t kMostCut = 2 * Geo::parts + 64;
+template <class Geo>
+constexpr size_t kPartsBytes = (size_t)kMostCut<Geo> * Geo::rows * (kHeadDim * sizeof(float) + sizeof(float2));
 
 // What a call launches.  A sequence's rows are known on the device only; what the sizes exclude is not launched.
 struct Launches {
-  int few = 0;        // row tiles of pages_few_kernel's blocks, 0: not launched
-  bool many = false;  // pages_many_kernel
+  int few = 0;        // row tiles of few_rows' blocks, 0: none
+  bool many = false;  // many_rows
   size_t few_bytes = 0, bytes = 0;  // of the workspace
 };
 Launches launches_of(const Pages& S, int batch, int n_tokens, bool bf16) {
   Launches n;
   const int64_t rows = (int64_t)n_tokens * S.G, average = S.G * (((int64_t)n_tokens + batch - 1) / batch);
-  n.many = rows > kFewRows;
+  n.many = rows > kFewRows && n_tokens >= 2 * (int64_t)batch;  // about one token for each sequence: few_rows alone, whoever brings more
   if (!n.many || batch > 1) {
-    const int64_t usual = std::min<int64_t>(average > kFewRows ? S.G : average, kFewRows);  // beside prompts: single tokens
-    n.few = usual <= 16 ? 1 : usual <= 32 || !bf16 ? 2 : 4;
+    const int64_t usual = average > kFewRows ? S.G : average;  // beside prompts: single tokens
+    n.few = usual <= 16 ? 1 : usual <= 32 || !bf16 || n.many ? 2 : 4;
   }
-  const auto part = [](int64_t block) { return (size_t)kMostCut * (size_t)block * (kHeadDim * sizeof(float) + sizeof(float2)); };
   const int64_t most = ((int64_t)S.max_pages << S.logP) / 32 + 1;  // tiles of a sequence
   if (most > kLeastTiles) {                                       // else no block is ever cut
-    n.few_bytes = n.few ? part(16 * n.few) : 0;
-    n.bytes = n.few_bytes + (n.many ? part(Many::rows) : 0);
+    n.few_bytes = n.few == 1 ? kPartsBytes<Few<1>> : n.few == 2 ? kPartsBytes<Few<2>> : n.few == 4 ? kPartsBytes<Few<4>> : 0;
+    n.bytes = n.few_bytes + (n.many ? kPartsBytes<Many> : 0);
   }
   return n;
 }
 
-template <class Geo, class Kernel, class Join>
-hipError_t launch_blocks(PagesAttn a, Kernel kernel, Join join, char* ws, hipStream_t st) {
-  a.part = (float*)ws;
-  a.stat = ws ? (float2*)(a.part + kMostCut * Geo::rows * kHeadDim) : nullptr;
+template <class Geo>
+PagesRows rows_of(const PagesAttn& a, int over, int to, char* ws) {
   const int64_t lh = (int64_t)a.n_layers * a.S.H, blocks = (int64_t)a.n_tokens * a.S.G / Geo::rows + a.batch;
-  kernel<<<(unsigned)std::min<int64_t>(kParts + lh * blocks, 1 << 20), kWaves * kWave, 0, st>>>(a);
-  const hipError_t e = hipGetLastError();
-  if (e != hipSuccess || !ws) return e;
-  join<<<(unsigned)std::min<int64_t>(lh * a.n_tokens * a.S.G, 2048), kWaves * kWave, 0, st>>>(a);
-  return hipGetLastError();
+  PagesRows r{};
+  r.over = over, r.to = to;
+  r.grid = (uint32_t)std::min<int64_t>(Geo::parts + lh * blocks, 1 << 20);
+  if (ws) {
+    r.join_grid = (uint32_t)std::min<int64_t>(lh * a.n_tokens * a.S.G, 2048);
+    r.part = (float*)ws;
+    r.stat = (float2*)(r.part + kMostCut<Geo> * Geo::rows * kHeadDim);
+  }
+  return r;
 }
 
-template <bool BF16, int R>
-hipError_t launch_few(const PagesAttn& a, char* ws, hipStream_t st) {
-  return launch_blocks<Few<R>>(a, pages_few_kernel<BF16, R>, pages_join_kernel<BF16, Few<R>>, ws, st);
-}
-template <bool BF16>
-hipError_t launch_many(const PagesAttn& a, char* ws, hipStream_t st) {
-  return launch_blocks<Many>(a, pages_many_kernel<BF16>, pages_join_kernel<BF16, Many>, ws, st);
+template <bool BF16, int R, bool MANY>
+hipError_t launch(const PagesAttn& a, hipStream_t st) {
+  pages_attn_kernel<BF16, R, MANY><<<a.few.grid + a.many.grid, kWaves * kWave, 0, st>>>(a);
+  const hipError_t e = hipGetLastError();
+  const uint32_t join = a.few.join_grid + a.many.join_grid;
+  if (e != hipSuccess || !join) return e;
+  pages_join_kernel<BF16, R, MANY><<<join, kWaves * kWave, 0, st>>>(a);
+  return hipGetLastError();
 }
 
 }  // namespace
@@ -935,18 +975,24 @@ size_t pages_attn_bytes(const Pages& S, int batch, int n_tokens, bool bf16) {
 
 hipError_t launch_pages_attn(PagesAttn a, bool bf16, void* ws, hipStream_t st) {
   const Launches n = launches_of(a.S, a.batch, a.n_tokens, bf16);
-  char* few = n.bytes ? (char*)ws : nullptr;
-  a.rows_to = 0x7fffffff;
-  if (n.many) {  // the longer work first
-    a.rows_over = n.few ? kFewRows : 0;
-    char* many = n.bytes ? (char*)ws + n.few_bytes : nullptr;
-    const hipError_t e = bf16 ? launch_many<true>(a, many, st) : launch_many<false>(a, many, st);
-    if (e != hipSuccess || !n.few) return e;
-    a.rows_to = kFewRows;
+  char* at = n.bytes ? (char*)ws : nullptr;
+  constexpr int kAny = 0x7fffffff;
+  const int few_to = n.many ? kFewRows : kAny;
+  if (n.few) a.few = n.few == 1 ? rows_of<Few<1>>(a, 0, few_to, at) : n.few == 2 ? rows_of<Few<2>>(a, 0, few_to, at) : rows_of<Few<4>>(a, 0, few_to, at);
+  if (n.many) a.many = rows_of<Many>(a, n.few ? kFewRows : 0, kAny, at ? at + n.few_bytes : nullptr);
+  if (bf16) {
+    if (n.many) return n.few == 0 ? launch<true, 0, true>(a, st) : n.few == 1 ? launch<true, 1, true>(a, st) : launch<true, 2, true>(a, st);
+    return n.few == 1 ? launch<true, 1, false>(a, st) : n.few == 2 ? launch<true, 2, false>(a, st) : launch<true, 4, false>(a, st);
   }
-  a.rows_over = 0;
-  if (bf16) return n.few == 1 ? launch_few<true, 1>(a, few, st) : n.few == 2 ? launch_few<true, 2>(a, few, st) : launch_few<true, 4>(a, few, st);
-  return n.few == 1 ? launch_few<false, 1>(a, few, st) : launch_few<false, 2>(a, few, st);
+  // fp32: many_rows takes twice the registers; together few_rows would have half of the waves
+  if (n.many) {
+    PagesAttn b = a;
+    b.few = PagesRows{};
+    const hipError_t e = launch<false, 0, true>(b, st);
+    if (e != hipSuccess || !n.few) return e;
+    a.many = PagesRows{};
+  }
+  return n.few == 1 ? launch<false, 1, false>(a, st) : launch<false, 2, false>(a, st);
 }
 
 }  // namespace iwdft
