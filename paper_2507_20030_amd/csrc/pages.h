@@ -52,6 +52,18 @@ __device__ __forceinline__ int e4m3_exponent(float a) {
   return e < kLeastExponent ? kLeastExponent : e;  // below 2^-126 as well
 }
 
+// Inclusive sums over the lanes of a wave, within rows of 16 and then across them.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int from_lane(int x) {
+  return __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xf, false);
+}
+__device__ __forceinline__ int scan(int x) {
+  x += from_lane<0x111, 0xf>(x), x += from_lane<0x112, 0xf>(x), x += from_lane<0x114, 0xf>(x), x += from_lane<0x118, 0xf>(x);
+  x += from_lane<0x142, 0xa>(x);
+  return x + from_lane<0x143, 0xc>(x);
+}
+__device__ __forceinline__ int last_lane(int x) { return __builtin_amdgcn_readlane(x, 63); }
+
 struct ResizeArgs {
   const int32_t* want;
   int32_t batch, logP, max_pages, n_pages, n_slots;
@@ -59,8 +71,8 @@ struct ResizeArgs {
   int32_t* scratch;  // 4 + 3 * batch ints, or null where one workgroup does it all
 };
 constexpr int kResizeThreads = 1024;
-// One launch, without scratch, up to so many sequences and slots.
-constexpr int kResizeOneBatch = 1024, kResizeOneSlots = 2048;
+// One launch, without scratch, up to so many sequences and slots; one wave's scans up to kResizeWaveBatch sequences.
+constexpr int kResizeOneBatch = 1024, kResizeOneSlots = 2048, kResizeWaveBatch = 64;
 hipError_t launch_pages_resize(const ResizeArgs& a, hipStream_t st);
 
 hipError_t launch_pages_write(const Pages& S, int layer, int n_layers, bool bf16, const void* k, const void* v, const int32_t* slots, int n_tokens,

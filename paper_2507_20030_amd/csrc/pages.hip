@@ -55,7 +55,7 @@ __device__ __forceinline__ Change change_of(const ResizeArgs& a, int b) {
 
 // What a thread of the filling kernel looks up.
 struct Fill {
-  const int32_t *have, *need, *gone, *starts;  // per sequence: old length, new pages of those before, pages given back before
+  const int32_t *have, *now, *need, *gone, *starts;  // per sequence: old length, new one, new pages of those before, pages given back before
   ResizeState s;
 };
 
@@ -72,8 +72,8 @@ __device__ __forceinline__ int last_not_above(const int32_t* v, int n, int x) { 
 // k-th page that is given back.
 __device__ __forceinline__ int released_page(const ResizeArgs& a, const Fill& f, int k) {
   const int ord = f.s.released - 1 - k, b = last_not_above(f.gone, a.batch, ord);
-  const int j = page_count(a.lens[b], a.logP) + ord - f.gone[b];
-  return a.table[(int64_t)b * a.max_pages + j];
+  const int j = page_count(f.now[b], a.logP) + ord - f.gone[b];
+  return (uint32_t)j < (uint32_t)a.max_pages ? a.table[(int64_t)b * a.max_pages + j] : -1;  // always, unless lengths are damaged
 }
 
 __device__ void resize_fill(const ResizeArgs& a, const Fill& f, int at, int step) {
@@ -159,62 +159,127 @@ __global__ __launch_bounds__(kResizeThreads) void resize_kernel(ResizeArgs a) {
   if constexpr (ONE) {
     __threadfence_block();
     __syncthreads();
-    resize_fill(a, Fill{have, need, gone, starts, {count, released, taken, total}}, tid, kResizeThreads);
+    resize_fill(a, Fill{have, a.lens, need, gone, starts, {count, released, taken, total}}, tid, kResizeThreads);
   }
+}
+
+// Up to 64 sequences: the sums are one wave's scans, then everybody fills.  Tokens and pages of a sequence are cut to what passes the slots anyway (a new page
+// has a new token), so that 32 bits hold the sums.  A decode step of 16 sequences: XX us with the scans of 16 waves above, XX with these.
+__global__ __launch_bounds__(256) void resize_wave_kernel(ResizeArgs a) {
+  __shared__ int32_t keep[5][kResizeWaveBatch];
+  __shared__ ResizeState state;
+  if (threadIdx.x < kWave) {
+    const int b = threadIdx.x;
+    const int count = min(max(a.free[0], 0), a.n_pages);
+    Change c{0, 0};
+    if (b < a.batch) c = change_of(a, b);
+    const int had = page_count(c.have, a.logP), get = page_count(c.want, a.logP);
+    const int gone = max(0, had - get), gone_to = scan(gone), released = min(max(last_lane(gone_to), 0), a.n_pages);
+    const bool up = c.want > c.have;
+    const int tokens = up ? min(c.want - c.have, kResizeOneSlots + 1) : 0, pages = up ? min(get - had, kResizeOneSlots + 1) : 0;
+    const int tokens_to = scan(tokens), pages_to = scan(pages);
+    const bool ok = up && tokens_to <= a.n_slots && (pages == 0 || pages_to <= count + released);
+    const int in = ok ? pages : 0, fresh = ok ? tokens : 0, taken = last_lane(scan(in)), fresh_to = scan(fresh), total = last_lane(fresh_to);
+    const int now = ok || c.want < c.have ? c.want : c.have;
+    keep[0][b] = c.have, keep[1][b] = now, keep[2][b] = pages_to - pages, keep[3][b] = gone_to - gone, keep[4][b] = fresh_to - fresh;
+    if (b < a.batch) a.starts[b] = fresh_to - fresh, a.lens[b] = now;
+    if (b == 0) {
+      a.starts[a.batch] = total;
+      a.free[0] = min(count + released - taken, a.n_pages);
+      state = ResizeState{count, released, taken, total};
+    }
+  }
+  __syncthreads();
+  resize_fill(a, Fill{keep[0], keep[1], keep[2], keep[3], keep[4], state}, threadIdx.x, 256);
 }
 
 __global__ __launch_bounds__(256) void resize_fill_kernel(ResizeArgs a) {
   const int32_t* s = a.scratch;
-  resize_fill(a, Fill{s + 4, s + 4 + a.batch, s + 4 + 2 * a.batch, a.starts, {s[0], s[1], s[2], s[3]}}, blockIdx.x * 256 + threadIdx.x, gridDim.x * 256);
+  resize_fill(a, Fill{s + 4, a.lens, s + 4 + a.batch, s + 4 + 2 * a.batch, a.starts, {s[0], s[1], s[2], s[3]}}, blockIdx.x * 256 + threadIdx.x, gridDim.x * 256);
 }
 
 // ------------------------------------------------------------------------------------------------ writing
-template <bool BF16>
-__device__ __forceinline__ void load2(const void* p, int64_t i, float* f) {  // two neighbouring channels
-  if constexpr (BF16) {
-    const uint32_t w = *(const uint32_t*)((const uint16_t*)p + i);
-    f[0] = __uint_as_float(w << 16), f[1] = __uint_as_float(w & 0xffff0000u);
-  } else {
-    const float2 x = *(const float2*)((const float*)p + i);
-    f[0] = x.x, f[1] = x.y;
-  }
-}
-template <bool BF16>
-__device__ __forceinline__ void load16(const void* p, int64_t i, float* f) {
-  if constexpr (BF16) {
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const uint4 w = ((const uint4*)((const uint16_t*)p + i))[h];
-      const uint32_t u[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-      for (int c = 0; c < 4; ++c) f[8 * h + 2 * c] = __uint_as_float(u[c] << 16), f[8 * h + 2 * c + 1] = __uint_as_float(u[c] & 0xffff0000u);
-    }
-  } else {
-#pragma unroll
-    for (int h = 0; h < 4; ++h) {
-      const float4 x = ((const float4*)((const float*)p + i))[h];
-      f[4 * h] = x.x, f[4 * h + 1] = x.y, f[4 * h + 2] = x.z, f[4 * h + 3] = x.w;
-    }
-  }
-}
-
 __device__ __forceinline__ float finite_abs(float x) {
   const float y = fabsf(x);
   return y < __builtin_inff() ? y : 0.f;  // NaN and infinities do not set the scale
 }
 
+// 8 tokens of one head as a lane stores them.  K: token lane / 8, channels 16 (lane % 8) ..; V: channels 2 lane, 2 lane + 1 of every token.
+template <bool BF16, bool V>
+struct Octet {
+  uint32_t w[BF16 ? 8 : 16];
+
+  __device__ __forceinline__ void load(const void* x, int64_t row0, int64_t row_step, int first, int n) {  // tokens [first, n) of the run; the rest is 0
+    const int lane = threadIdx.x % kWave;
+    constexpr int kElem = BF16 ? 2 : 4;
+#pragma unroll
+    for (int i = 0; i < (BF16 ? 8 : 16); ++i) w[i] = 0;
+    if constexpr (!V) {
+      const int t = first + lane / 8;
+      if (t >= 0 && t < n) {
+        const uint4* p = (const uint4*)((const char*)x + (row0 + t * row_step + 16 * (lane % 8)) * kElem);
+#pragma unroll
+        for (int i = 0; i < (BF16 ? 2 : 4); ++i) {
+          const uint4 v = p[i];
+          w[4 * i] = v.x, w[4 * i + 1] = v.y, w[4 * i + 2] = v.z, w[4 * i + 3] = v.w;
+        }
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < kOct; ++j) {
+        const int t = first + j;
+        if (t < 0 || t >= n) continue;
+        const char* p = (const char*)x + (row0 + t * row_step + 2 * lane) * kElem;
+        if constexpr (BF16) {
+          w[j] = *(const uint32_t*)p;
+        } else {
+          const uint2 v = *(const uint2*)p;
+          w[2 * j] = v.x, w[2 * j + 1] = v.y;
+        }
+      }
+    }
+  }
+  __device__ __forceinline__ float value(int i) const {  // K: channel i; V: channel i % 2 of token i / 2
+    if constexpr (BF16) return __uint_as_float(i % 2 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
+    else return __uint_as_float(w[i]);
+  }
+  __device__ __forceinline__ float top() const {
+    float t = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) t = fmaxf(t, finite_abs(value(i)));
+    return t;
+  }
+  __device__ __forceinline__ void bytes(int e, uint32_t* out) const {  // in the page's order, times 2^-e
+    float f[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) f[V ? 8 * (i % 2) + i / 2 : i] = ldexpf(value(i), -e);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) out[i] = floats_e4m3(f + 4 * i);
+  }
+};
+
 // A run -- new tokens that follow each other in one page -- is one wave's work for each head and tensor: its largest value, the page's exponent, the
-// values.  The run is read twice, the second time from the caches, so that nothing has to stay in registers and no two waves meet.
-// old: the page's exponent, used from its second token on; returns the new one.  Old values are only touched where it grows; of an octet of V that holds other tokens too the bytes of those stay.
+// values, and no two waves meet.  Up to kHeld octets stay in registers, all on their way at a time; a longer run (pages of 128) is read twice, the
+// second time from the caches.  Bound by memory: 46000 tokens of 8 heads, bf16, XX us with every run read twice, 256 bytes at a time, XX now.
+// old: the page's exponent, used from its second token on; returns the new one.  Old values are only touched where it grows; of an octet of V that
+// holds other tokens too the bytes of those stay.
+constexpr int kHeld = 8;
 template <bool BF16, bool V>
 __device__ int write_run(const Pages& S, int64_t ph, const void* x, int64_t row0, int64_t row_step, int offset, int n, int old) {
   const int lane = threadIdx.x % kWave;
+  const int o0 = offset / kOct, octets = (offset + n + kOct - 1) / kOct - o0;
+  Octet<BF16, V> held[kHeld];
   float top = 0.f;
-#pragma unroll 8
-  for (int i = 0; i < n; ++i) {
-    float f[2];
-    load2<BF16>(x, row0 + i * row_step + 2 * lane, f);
-    top = fmaxf(top, fmaxf(finite_abs(f[0]), finite_abs(f[1])));
+#pragma unroll
+  for (int k = 0; k < kHeld; ++k)
+    if (k < octets) held[k].load(x, row0, row_step, (o0 + k) * kOct - offset, n);
+#pragma unroll
+  for (int k = 0; k < kHeld; ++k)
+    if (k < octets) top = fmaxf(top, held[k].top());
+  for (int k = kHeld; k < octets; ++k) {
+    Octet<BF16, V> more;
+    more.load(x, row0, row_step, (o0 + k) * kOct - offset, n);
+    top = fmaxf(top, more.top());
   }
 #pragma unroll
   for (int d = 1; d < kWave; d <<= 1) top = fmaxf(top, __shfl_xor(top, d));
@@ -226,62 +291,55 @@ __device__ int write_run(const Pages& S, int64_t ph, const void* x, int64_t row0
   if (lane == 0) S.exponents[2 * ph + (V ? 1 : 0)] = e;
   uint8_t* base = page_values(S, ph) + (V ? (size_t)kHeadDim << S.logP : 0);
 
-  for (int o = grown ? 0 : offset / kOct; o * kOct < offset + n; ++o) {
-    uint4* at = (uint4*)(base + o * kOct * kHeadDim) + lane;  // K: token lane / 8 of the octet, channels 16 (lane % 8) ..; V: channels 2 lane, 2 lane + 1
+  const auto rescaled = [&](uint32_t w) {
+    float f[4];
+    e4m3_floats(w, f);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) f[j] = ldexpf(f[j], -grown);
+    return floats_e4m3(f);
+  };
+  const auto store = [&](const Octet<BF16, V>& oct, int o) {
+    uint4* at = (uint4*)(base + o * kOct * kHeadDim) + lane;
+    uint32_t now[4];
+    oct.bytes(e, now);
     if constexpr (!V) {
       const int row = o * kOct + lane / 8;
-      const bool fresh = row >= offset && row < offset + n;
-      if (!fresh && !(grown && row < offset)) continue;
-      float f[16];
-      if (fresh) {
-        load16<BF16>(x, row0 + (row - offset) * row_step + 16 * (lane % 8), f);
-#pragma unroll
-        for (int c = 0; c < 16; ++c) f[c] = ldexpf(f[c], -e);
-      } else {
+      if (row < offset && grown) {
         const uint4 w = *at;
-        e4m3_floats(w.x, f), e4m3_floats(w.y, f + 4), e4m3_floats(w.z, f + 8), e4m3_floats(w.w, f + 12);
-#pragma unroll
-        for (int c = 0; c < 16; ++c) f[c] = ldexpf(f[c], -grown);
+        now[0] = rescaled(w.x), now[1] = rescaled(w.y), now[2] = rescaled(w.z), now[3] = rescaled(w.w);
       }
-      *at = make_uint4(floats_e4m3(f), floats_e4m3(f + 4), floats_e4m3(f + 8), floats_e4m3(f + 12));
-    } else {
-      float f[16];  // [channel][token]
-      const bool whole = o * kOct >= offset && (o + 1) * kOct <= offset + n;
-      uint32_t was[4] = {0, 0, 0, 0};
-      if (!whole) {
-        const uint4 w = *at;
-        was[0] = w.x, was[1] = w.y, was[2] = w.z, was[3] = w.w;
-      }
-#pragma unroll
-      for (int j = 0; j < kOct; ++j) {
-        const int row = o * kOct + j;
-        float g[2] = {0.f, 0.f};
-        if (row >= offset && row < offset + n) load2<BF16>(x, row0 + (row - offset) * row_step + 2 * lane, g);
-        f[j] = ldexpf(g[0], -e), f[8 + j] = ldexpf(g[1], -e);
-      }
-      uint32_t now[4];
+      if (row >= offset + n || (row < offset && !grown)) return;
+    } else if (o * kOct < offset || (o + 1) * kOct > offset + n) {
+      const uint4 was4 = *at;
+      const uint32_t was[4] = {was4.x, was4.y, was4.z, was4.w};
 #pragma unroll
       for (int w = 0; w < 4; ++w) {
-        now[w] = floats_e4m3(f + 4 * w);
-        if (!whole) {
-          float g[4];
-          e4m3_floats(was[w], g);
+        uint32_t after = 0, before = 0;  // bytes of tokens behind the run and in front of it
 #pragma unroll
-          for (int j = 0; j < 4; ++j) g[j] = ldexpf(g[j], -grown);
-          const uint32_t moved = grown ? floats_e4m3(g) : was[w];
-          uint32_t keep = 0, old = 0;  // bytes outside the run; of tokens before it
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const int row = o * kOct + 4 * (w & 1) + j;
-            if (row < offset) old |= 0xffu << (8 * j);
-            else if (row >= offset + n) keep |= 0xffu << (8 * j);
-          }
-          now[w] = (now[w] & ~(keep | old)) | (moved & old) | (was[w] & keep);
+        for (int j = 0; j < 4; ++j) {
+          const int row = o * kOct + 4 * (w & 1) + j;
+          if (row < offset) before |= 0xffu << (8 * j);
+          else if (row >= offset + n) after |= 0xffu << (8 * j);
         }
+        now[w] = (now[w] & ~(after | before)) | ((grown ? rescaled(was[w]) : was[w]) & before) | (was[w] & after);
       }
-      *at = make_uint4(now[0], now[1], now[2], now[3]);
     }
+    *at = make_uint4(now[0], now[1], now[2], now[3]);
+  };
+#pragma unroll
+  for (int k = 0; k < kHeld; ++k)
+    if (k < octets) store(held[k], o0 + k);
+  for (int k = kHeld; k < octets; ++k) {
+    Octet<BF16, V> more;
+    more.load(x, row0, row_step, (o0 + k) * kOct - offset, n);
+    store(more, o0 + k);
   }
+  if (grown)  // octets of old tokens only
+    for (int o = 0; o < o0; ++o) {
+      uint4* at = (uint4*)(base + o * kOct * kHeadDim) + lane;
+      const uint4 w = *at;
+      *at = make_uint4(rescaled(w.x), rescaled(w.y), rescaled(w.z), rescaled(w.w));
+    }
   return e;
 }
 
@@ -404,8 +462,17 @@ __global__ __launch_bounds__(256) void pages_read_kernel(Pages S, int layer0, in
   if (K && t0 + mine < n) {
 #pragma unroll
     for (int c = 0; c < 16; ++c) f[c] = mine < there ? ldexpf(f[c], ek) : 0.f;
+    const int64_t to = row + mine * kHeadDim + 16 * (lane % 8);
+    if constexpr (BF16) {
+      uint32_t w[8];
 #pragma unroll
-    for (int c = 0; c < 16; c += 2) store2<BF16>(K, row + mine * kHeadDim + 16 * (lane % 8) + c, f[c], f[c + 1]);
+      for (int c = 0; c < 8; ++c) w[c] = (uint32_t)f32_to_bf16(f[2 * c]) | (uint32_t)f32_to_bf16(f[2 * c + 1]) << 16;
+      uint4* p = (uint4*)((uint16_t*)K + to);
+      p[0] = make_uint4(w[0], w[1], w[2], w[3]), p[1] = make_uint4(w[4], w[5], w[6], w[7]);
+    } else {
+#pragma unroll
+      for (int c = 0; c < 16; c += 4) *(float4*)((float*)K + to + c) = make_float4(f[c], f[c + 1], f[c + 2], f[c + 3]);
+    }
   }
   if (V) {
     e4m3_floats(v.x, f), e4m3_floats(v.y, f + 4), e4m3_floats(v.z, f + 8), e4m3_floats(v.w, f + 12);
@@ -418,6 +485,10 @@ __global__ __launch_bounds__(256) void pages_read_kernel(Pages S, int layer0, in
 }  // namespace
 
 hipError_t launch_pages_resize(const ResizeArgs& a, hipStream_t st) {
+  if (!a.scratch && a.batch <= kResizeWaveBatch) {
+    resize_wave_kernel<<<1, 256, 0, st>>>(a);
+    return hipGetLastError();
+  }
   if (!a.scratch) {
     resize_kernel<true><<<1, kResizeThreads, 0, st>>>(a);
     return hipGetLastError();

@@ -66,16 +66,6 @@ struct Place {
   Seq s;
 };
 
-// Inclusive sums over the lanes, within rows of 16 and then across them.
-template <int CTRL, int ROWS>
-__device__ __forceinline__ int from_lane(int x) {
-  return __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xf, false);
-}
-__device__ __forceinline__ int scan(int x) {
-  x += from_lane<0x111, 0xf>(x), x += from_lane<0x112, 0xf>(x), x += from_lane<0x114, 0xf>(x), x += from_lane<0x118, 0xf>(x);
-  x += from_lane<0x142, 0xa>(x);
-  return x + from_lane<0x143, 0xc>(x);
-}
 __device__ __forceinline__ float scan(float x) {
   const auto add = [](float y, int z) { return y + __int_as_float(z); };
   x = add(x, from_lane<0x111, 0xf>(__float_as_int(x))), x = add(x, from_lane<0x112, 0xf>(__float_as_int(x)));
@@ -83,7 +73,6 @@ __device__ __forceinline__ float scan(float x) {
   x = add(x, from_lane<0x142, 0xa>(__float_as_int(x)));
   return add(x, from_lane<0x143, 0xc>(__float_as_int(x)));
 }
-__device__ __forceinline__ int last_lane(int x) { return __builtin_amdgcn_readlane(x, kWave - 1); }
 
 template <class Geo>
 class Schedule {
