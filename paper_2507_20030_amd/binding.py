@@ -391,8 +391,10 @@ def _resize_bytes(batch, n_slots):
 
 
 @functools.lru_cache(maxsize=1024)
-def _attn_bytes(n_layers, batch, n_tokens, *desc):
-    return _bytes_of(load_library().iwdft_pages_attn_bytes, ctypes.byref(_pages_desc(*desc)), n_layers, batch, n_tokens)
+def _attn_sizes(n_layers, batch, n_tokens, *desc):
+    """The descriptor, as the call takes it, and the workspace's bytes."""
+    ref = ctypes.byref(_pages_desc(*desc))
+    return ref, _bytes_of(load_library().iwdft_pages_attn_bytes, ref, n_layers, batch, n_tokens)
 
 
 def iwdft_pages_query_bytes(desc: iwdft_pages_desc):
@@ -446,15 +448,14 @@ def _kv_dtype(name: str, t: torch.Tensor):
     return t.dtype
 
 
-def _run_on(device: torch.device, stream, call, *args) -> None:
+def _run_on(index: int, stream, call, *args) -> None:
     """The call with the tensors' device as the current one, on its current stream unless one is given."""
-    raw = torch._C._cuda_getCurrentRawStream(device.index) if stream is None else _stream(stream)
-    if device.index == torch.cuda.current_device():
-        rc = call(*args, raw)
+    if index == torch.cuda.current_device():
+        rc = call(*args, torch._C._cuda_getCurrentRawStream(index) if stream is None else _stream(stream))
     else:
-        with torch.cuda.device(device):
-            rc = call(*args, raw)
-    if rc != IWDFT_OK:
+        with torch.cuda.device(index):
+            rc = call(*args, _stream(stream))
+    if rc:
         _check(rc)
 
 
@@ -491,7 +492,7 @@ def iwdft_pages_resize(want, table, lens, free, starts, slots, page_tokens: int,
         if not _fits(t, torch.int32, size, device):
             _expect(name, t, torch.int32, size, device)
     ws = _scratch(_resize_bytes(batch, n_slots), device, stream, workspace)
-    _run_on(device, stream, load_library().iwdft_pages_resize, page_tokens, n_free - 1, max_pages, want.data_ptr(), batch, table.data_ptr(), lens.data_ptr(),
+    _run_on(device.index, stream, load_library().iwdft_pages_resize, page_tokens, n_free - 1, max_pages, want.data_ptr(), batch, table.data_ptr(), lens.data_ptr(),
             free.data_ptr(), starts.data_ptr(), slots.data_ptr(), n_slots, ws.data_ptr() if ws is not None else None, ws.nbytes if ws is not None else 0)
 
 
@@ -506,7 +507,7 @@ def iwdft_pages_write(values, exponents, k, v, slots, layer: int = 0, stream=Non
     if shape[0] == 0:
         return
     desc = _pages_desc(n_layers, n_pages, heads, heads, 128, P, 1, dtype)
-    _run_on(device, stream, load_library().iwdft_pages_write, ctypes.byref(desc), layer, shape[0], k.data_ptr(), v.data_ptr(), slots.data_ptr(), n,
+    _run_on(device.index, stream, load_library().iwdft_pages_write, ctypes.byref(desc), layer, shape[0], k.data_ptr(), v.data_ptr(), slots.data_ptr(), n,
             values.data_ptr(), exponents.data_ptr())
 
 
@@ -526,9 +527,9 @@ def iwdft_pages_attn(values, exponents, q, starts, table, lens, out, layer: int 
     batch, max_pages = size
     if n == 0:
         return
-    sizes = (n_layers, n_pages, heads, n_q_heads, 128, P, max_pages, dtype)
-    ws = _scratch(_attn_bytes(n, batch, n_tokens, *sizes), device, stream, workspace)
-    _run_on(device, stream, load_library().iwdft_pages_attn, ctypes.byref(_pages_desc(*sizes)), layer, n, q.data_ptr(), starts.data_ptr(), n_tokens,
+    desc, need = _attn_sizes(n, batch, n_tokens, n_layers, n_pages, heads, n_q_heads, 128, P, max_pages, dtype)
+    ws = _scratch(need, device, stream, workspace)
+    _run_on(device.index, stream, load_library().iwdft_pages_attn, desc, layer, n, q.data_ptr(), starts.data_ptr(), n_tokens,
             table.data_ptr(), lens.data_ptr(), batch, values.data_ptr(), exponents.data_ptr(), out.data_ptr(), n_sink, n_recent, scale,
             ws.data_ptr() if ws is not None else None, ws.nbytes if ws is not None else 0)
 
@@ -551,7 +552,7 @@ def iwdft_pages_read(values, exponents, table, lens, K, V, layer: int = 0, strea
     if shape[0] == 0:
         return
     desc = _pages_desc(n_layers, n_pages, heads, heads, 128, P, size[1], dtype)
-    _run_on(device, stream, load_library().iwdft_pages_read, ctypes.byref(desc), layer, shape[0], table.data_ptr(), lens.data_ptr(), size[0], shape[3],
+    _run_on(device.index, stream, load_library().iwdft_pages_read, ctypes.byref(desc), layer, shape[0], table.data_ptr(), lens.data_ptr(), size[0], shape[3],
             values.data_ptr(), exponents.data_ptr(), K.data_ptr() if K is not None else None, V.data_ptr() if V is not None else None)
 
 

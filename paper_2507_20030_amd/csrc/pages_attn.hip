@@ -88,7 +88,7 @@ class Schedule {
     const float slices = (float)(a.n_layers * a.S.H);
     sum = __int_as_float(last_lane(__float_as_int(scan(sum)))) * slices;
     all_blocks = __int_as_float(last_lane(__float_as_int(scan(all_blocks)))) * slices;
-    w.tiles = max(kLeastTiles, (int)fminf(ceilf(sum / fmaxf((float)Geo::parts - all_blocks, 0.5f * (float)Geo::parts)), 1e9f));
+    w.tiles = which.part ? max(kLeastTiles, (int)fminf(ceilf(sum / fmaxf((float)Geo::parts - all_blocks, 0.5f * (float)Geo::parts)), 1e9f)) : 0x7fffffff;
     int n = 0, cut = 0, cut_rows = 0;
     each([&](int, const Seq& s) {
       const int np = parts(s), all = np * blocks(s.rows);
@@ -99,7 +99,7 @@ class Schedule {
   }
 
   static __device__ __forceinline__ int blocks(int rows) { return (rows + Geo::rows - 1) / Geo::rows; }
-  __device__ __forceinline__ int parts(const Seq& s) const { return s.nq ? max(1, (s.tiles + w.tiles - 1) / w.tiles) : 0; }
+  __device__ __forceinline__ int parts(const Seq& s) const { return s.nq ? max(1, (int)(((uint32_t)s.tiles + (uint32_t)w.tiles - 1u) / (uint32_t)w.tiles)) : 0; }
 
   template <class Count>
   __device__ __forceinline__ Place find(int y, Count count) const {
@@ -270,19 +270,19 @@ struct Rows {
 };
 
 // ------------------------------------------------------------------------------------------------ few rows
-// A workgroup has a part of the tokens of one block of 16 R rows; its four waves take the tiles in turn and join their sums in the end.  A tile of 32
+// A workgroup has a part of the tokens of one block of 16 R rows; its W waves take the tiles in turn and join their sums in the end.  A tile of 32
 // tokens is 8 KB, eight 16-byte loads a lane, the next one's on their way while this one is multiplied (two or three ahead are no faster): S^T = K Q^T leaves lane l
 // with row l % 16 and the 8 tokens of octet l / 16, which is how O^T = V^T P^T wants them, so nothing moves between lanes but the maximum.
 // Bound by memory where there is much of it, by the chain lengths -> table -> tokens -> sums where there is little: the first tile is on its
 // way before q is looked at.
-template <bool BF16, int R>
+template <bool BF16, int R, int W>
 __device__ __forceinline__ void few_rows(const PagesAttn& a, uint32_t x0, uint32_t step) {
   using Geo = Few<R>;
   constexpr int PARTS = BF16 ? 1 : 2, BR = Geo::rows, kTile = Geo::tile, kQTop = Weights<BF16>::q_top;
   const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int row = lane & 15, oct = lane >> 4;
-  __shared__ __attribute__((aligned(16))) float join[kWaves][16][kHeadDim + 4];
-  __shared__ float2 join_stat[kWaves][16];
+  __shared__ __attribute__((aligned(16))) float join[W][16][kHeadDim + 4];
+  __shared__ float2 join_stat[W][16];
 
   const Schedule<Geo> plan(a, a.few, lane);
   const uint32_t slices = (uint32_t)(a.n_layers * a.S.H), all = (uint32_t)plan.w.parts * slices;
@@ -338,7 +338,7 @@ __device__ __forceinline__ void few_rows(const PagesAttn& a, uint32_t x0, uint32
     Data next{};
     if (first < mine.to) {
       next = load_tile(first, pages_at(first));
-      if (first + kWaves < mine.to) id = pages_at(first + kWaves);
+      if (first + W < mine.to) id = pages_at(first + W);
     }
 
     Rows<PARTS> rt[R];
@@ -385,11 +385,11 @@ __device__ __forceinline__ void few_rows(const PagesAttn& a, uint32_t x0, uint32
       }
     }
 
-    for (int i = first; i < mine.to; i += kWaves) {
+    for (int i = first; i < mine.to; i += W) {
       Data d = next;
-      if (i + kWaves < mine.to) {
-        next = load_tile(i + kWaves, id);
-        if (i + 2 * kWaves < mine.to) id = pages_at(i + 2 * kWaves);
+      if (i + W < mine.to) {
+        next = load_tile(i + W, id);
+        if (i + 2 * W < mine.to) id = pages_at(i + 2 * W);
       }
       const int t0 = span.tile(i) * kTile, t1 = t0 + kTile - 1, j0 = t0 + 8 * oct;
       // whether every row sees the whole tile
@@ -510,14 +510,17 @@ __device__ __forceinline__ void few_rows(const PagesAttn& a, uint32_t x0, uint32
       }
       if (oct == 0) join_stat[wave][row] = make_float2(z.m, z.l);
       __syncthreads();
+      if (threadIdx.x >= 256) continue;
       const int jr = threadIdx.x >> 4, jc = 8 * (threadIdx.x & 15);
-      float2 st[kWaves];
+      float2 st[W];
 #pragma unroll
-      for (int v = 0; v < kWaves; ++v) st[v] = join_stat[v][jr];
-      const float m = fmaxf(fmaxf(st[0].x, st[1].x), fmaxf(st[2].x, st[3].x));
+      for (int v = 0; v < W; ++v) st[v] = join_stat[v][jr];
+      float m = st[0].x;
+#pragma unroll
+      for (int v = 1; v < W; ++v) m = fmaxf(m, st[v].x);
       float y[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, l = 0.f;
 #pragma unroll
-      for (int v = 0; v < kWaves; ++v) {
+      for (int v = 0; v < W; ++v) {
         const float fade = __builtin_amdgcn_exp2f(st[v].x - m);
         const float4 lo = *(const float4*)(join[v][jr] + jc), hi = *(const float4*)(join[v][jr] + jc + 4);
         l += st[v].y * fade;
@@ -895,7 +898,15 @@ __global__ __launch_bounds__(kWaves* kWave, BF16 ? (R <= 2 ? 2 : 1) : (R == 1 &&
     if (x < n) x += (n - x + gridDim.x - 1) / gridDim.x * gridDim.x;  // its next turn
     x -= n;
   }
-  if constexpr (R > 0) few_rows<BF16, R>(a, x, gridDim.x);
+  if constexpr (R > 0) few_rows<BF16, R, kWaves>(a, x, gridDim.x);
+}
+// Tables of up to kShortTiles tiles: blocks are not cut, so nothing is to be joined; twice the waves share their tiles.  One sequence, 8 heads, us with parts
+// and a join / so: fp32, 100 tokens 7.9 / 6.2, 500 9.1 / 9.0, 1000 9.2 / 11.9; bf16, 4 query heads, 500 10.1 / 9.6, 1000 10.4 / 11.9 (a workgroup cannot
+// draw more than 50 KB a microsecond); 8 sequences of 1000 13.7 / 12.9, 64 29.2 / 30.3.
+constexpr int kShortTiles = 17, kShortWaves = 8;
+template <bool BF16, int R>
+__global__ __launch_bounds__(kShortWaves* kWave, 2) void pages_short_kernel(PagesAttn a) {
+  few_rows<BF16, R, kShortWaves>(a, blockIdx.x, gridDim.x);
 }
 template <bool BF16, int R, bool MANY>
 __global__ __launch_bounds__(kWaves* kWave) void pages_join_kernel(PagesAttn a) {
@@ -914,6 +925,7 @@ constexpr size_t kPartsBytes = (size_t)kMostCut<Geo> * Geo::rows * (kHeadDim * s
 struct Launches {
   int few = 0;        // row tiles of few_rows' blocks, 0: none
   bool many = false;  // many_rows
+  bool cut = false;   // blocks may be cut into parts
   size_t few_bytes = 0, bytes = 0;  // of the workspace
 };
 Launches launches_of(const Pages& S, int batch, int n_tokens, bool bf16) {
@@ -924,8 +936,8 @@ Launches launches_of(const Pages& S, int batch, int n_tokens, bool bf16) {
     const int64_t usual = average > kFewRows ? S.G : average;  // beside prompts: single tokens
     n.few = usual <= 16 ? 1 : usual <= 32 || !bf16 || n.many ? 2 : 4;
   }
-  const int64_t most = ((int64_t)S.max_pages << S.logP) / 32 + 1;  // tiles of a sequence
-  if (most > kLeastTiles) {                                       // else no block is ever cut
+  n.cut = ((int64_t)S.max_pages << S.logP) > (int64_t)kShortTiles * 32;
+  if (n.cut) {
     n.few_bytes = n.few == 1 ? kPartsBytes<Few<1>> : n.few == 2 ? kPartsBytes<Few<2>> : n.few == 4 ? kPartsBytes<Few<4>> : 0;
     n.bytes = n.few_bytes + (n.many ? kPartsBytes<Many> : 0);
   }
@@ -946,6 +958,11 @@ PagesRows rows_of(const PagesAttn& a, int over, int to, char* ws) {
   return r;
 }
 
+template <bool BF16, int R>
+hipError_t launch_short(const PagesAttn& a, hipStream_t st) {
+  pages_short_kernel<BF16, R><<<a.few.grid, kShortWaves * kWave, 0, st>>>(a);
+  return hipGetLastError();
+}
 template <bool BF16, int R, bool MANY>
 hipError_t launch(const PagesAttn& a, hipStream_t st) {
   pages_attn_kernel<BF16, R, MANY><<<a.few.grid + a.many.grid, kWaves * kWave, 0, st>>>(a);
@@ -971,6 +988,7 @@ hipError_t launch_pages_attn(PagesAttn a, bool bf16, void* ws, hipStream_t st) {
   if (n.many) a.many = rows_of<Many>(a, n.few ? kFewRows : 0, kAny, at ? at + n.few_bytes : nullptr);
   if (bf16) {
     if (n.many) return n.few == 0 ? launch<true, 0, true>(a, st) : n.few == 1 ? launch<true, 1, true>(a, st) : launch<true, 2, true>(a, st);
+    if (!n.cut && n.few <= 2) return n.few == 1 ? launch_short<true, 1>(a, st) : launch_short<true, 2>(a, st);
     return n.few == 1 ? launch<true, 1, false>(a, st) : n.few == 2 ? launch<true, 2, false>(a, st) : launch<true, 4, false>(a, st);
   }
   // fp32: many_rows takes twice the registers; together few_rows would have half of the waves
@@ -981,6 +999,7 @@ hipError_t launch_pages_attn(PagesAttn a, bool bf16, void* ws, hipStream_t st) {
     if (e != hipSuccess || !n.few) return e;
     a.many = PagesRows{};
   }
+  if (!n.cut && n.few == 1) return launch_short<false, 1>(a, st);
   return n.few == 1 ? launch<false, 1, false>(a, st) : launch<false, 2, false>(a, st);
 }
 
