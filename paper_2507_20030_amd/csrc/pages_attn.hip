@@ -237,7 +237,16 @@ __device__ __forceinline__ void store8(void* p, int64_t i, const float* y, float
 
 // A row at position p sees the tokens (from, p] and those below sink.
 __device__ __forceinline__ int window_from(const PagesAttn& a, int p) { return a.n_recent ? max(p - a.n_recent, -1) : -1; }  // p >= -1, n_recent >= 0: no overflow
-__device__ __forceinline__ bool sees(int t, int from, int to, int sink) { return (t <= to) & ((t > from) | (t < sink)); }
+// ... as one bit for each of the eight tokens from j0 on.  (Bits in a register, not a comparison's mask for each token: those would push the loops' own scalars out.)
+__device__ __forceinline__ uint32_t seen_bits(int j0, int from, int to, int sink) {
+  const auto below = [&](int n) { return (1u << min(max(n, 0), 8)) - 1u; };
+  return below(to + 1 - j0) & (~below(from + 1 - j0) | below(sink - j0));
+}
+__device__ __forceinline__ uint32_t bytes_of_bits(uint32_t four) { return (four & 15u) * 0x00204081u & 0x01010101u; }  // 1 in the byte of every bit
+__device__ __forceinline__ float seen_or_none(float x, uint32_t bits, int j) {  // -infinity unless bit j is set
+  const uint32_t keep = (uint32_t)((int32_t)(bits << (31 - j)) >> 31);
+  return __uint_as_float((__float_as_uint(x) & keep) | (0xff800000u & ~keep));
+}
 
 // Tiles that a block's rows see: those of the sinks, then the others.
 struct Span {
@@ -396,9 +405,7 @@ __device__ __forceinline__ void few_rows(const PagesAttn& a, uint32_t x0, uint32
       const bool edge = t1 > p_lo || (t1 >= sink && t0 <= window_from(a, p_hi)) || __any(d.bad);
       bool poison = false;
       if (edge) {  // tokens that no row sees may hold anything
-        uint32_t keep[2] = {0, 0};
-#pragma unroll
-        for (int j = 0; j < 8; ++j) keep[j / 4] |= (!d.bad & sees(j0 + j, all_from, p_hi, sink)) ? 0xffu << (8 * (j % 4)) : 0u;
+        const uint32_t any = d.bad ? 0u : seen_bits(j0, all_from, p_hi, sink), keep[2] = {bytes_of_bits(any) * 0xffu, bytes_of_bits(any >> 4) * 0xffu};
         uint32_t nans = 0;
 #pragma unroll
         for (int p = 0; p < 4; ++p) {
@@ -441,8 +448,9 @@ __device__ __forceinline__ void few_rows(const PagesAttn& a, uint32_t x0, uint32
 #pragma unroll
         for (int j = 0; j < 8; ++j) sc[j] = sc[j] * factor + ev;
         if (edge) {
+          const uint32_t bits = d.bad ? 0u : seen_bits(j0, z.from, z.pos, sink);
 #pragma unroll
-          for (int j = 0; j < 8; ++j) sc[j] = (!d.bad & sees(j0 + j, z.from, z.pos, sink)) ? sc[j] : -__builtin_inff();
+          for (int j = 0; j < 8; ++j) sc[j] = seen_or_none(sc[j], bits, j);
         }
         float top = sc[0];
 #pragma unroll
@@ -470,9 +478,8 @@ __device__ __forceinline__ void few_rows(const PagesAttn& a, uint32_t x0, uint32
           const half8 bad[2] = {operand(n[0] * 0x38u, n[1] * 0x38u), operand(n[2] * 0x38u, n[3] * 0x38u)};  // 0x38: 1
 #pragma unroll
           for (int r = 0; r < R; ++r) {
-            half8 one;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) one[j] = (!d.bad & sees(j0 + j, rt[r].from, rt[r].pos, sink)) ? (_Float16)1.f : (_Float16)0.f;
+            const uint32_t bits = d.bad ? 0u : seen_bits(j0, rt[r].from, rt[r].pos, sink);
+            const half8 one = operand(bytes_of_bits(bits) * 0x38u, bytes_of_bits(bits >> 4) * 0x38u);
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
               const floatx4 hit = __builtin_amdgcn_mfma_f32_16x16x32_f16(bad[c], one, floatx4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
@@ -558,7 +565,7 @@ __device__ __forceinline__ uint32_t many_rows(const PagesAttn& a, uint32_t x0, u
   const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int row = lane & 31, grp = lane >> 5;
   __shared__ __attribute__((aligned(16))) uint8_t kbuf[2][kTile * kHeadDim], vbuf[2][kTile * kHeadDim];
-  __shared__ float4 meta[2][kTile / kOct];  // of the octets' pages: scale 2^(eK - kQTop), eV, 2^-eV
+  __shared__ float4 meta[2][kTile / 16];  // of the pages of 16 tokens each: scale 2^(eK - kQTop), eV, 2^-eV
 
   const Schedule<Geo> plan(a, a.many, lane);
   const uint32_t slices = (uint32_t)(a.n_layers * a.S.H), all = (uint32_t)plan.w.parts * slices;
@@ -624,44 +631,42 @@ __device__ __forceinline__ uint32_t many_rows(const PagesAttn& a, uint32_t x0, u
       for (int i = 0; i < 16; ++i) o[c][i] = 0.f;
     float m = -FLT_MAX, l = 0.f;
 
-    // a wave brings octets wave and wave + 4 of a tile; their pages are looked up a tile earlier
+    // a wave brings 16 tokens of a tile, which are in one page; that page is looked up a tile earlier
     const int32_t* table = a.table + (int64_t)at.b * a.S.max_pages;
     const int last_page = max(page_count(s.len, a.S.logP) - 1, 0), in_page = (1 << a.S.logP) - 1;
-    int next_page[2] = {0, 0};
+    const int64_t slice = (int64_t)(a.layer + layer) * a.S.n_pages * a.S.H + h;
+    const uint8_t* const slice_values = a.S.values + (slice << (a.S.logP + 8));
+    const int2* const slice_exponents = (const int2*)a.S.exponents + slice;
+    int next_page = 0;
     uint4 nk[2], nv[2];
-    int2 ne[2];
-    bool none[2];
-    const auto find_tile = [&](int i) {
-#pragma unroll
-      for (int u = 0; u < 2; ++u) next_page[u] = table[min((span.tile(i) * kTile + kOct * (wave + kWaves * u)) >> a.S.logP, last_page)];
-    };
+    int2 ne;
+    bool none;
+    const auto find_tile = [&](int i) { next_page = table[min((span.tile(i) * kTile + 16 * wave) >> a.S.logP, last_page)]; };
     const auto load_tile = [&](int i) {
-#pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        const int t = span.tile(i) * kTile + kOct * (wave + kWaves * u);
-        int page = __builtin_amdgcn_readfirstlane(next_page[u]);
-        none[u] = page < 0 || page >= a.S.n_pages;
-        page = none[u] ? 0 : page;
-        const int64_t ph = page_head(a.S, a.layer + layer, page, h);
-        const uint8_t* at_k = page_values(a.S, ph) + (t & in_page) * kHeadDim;
-        nk[u] = ((const uint4*)at_k)[lane];
-        nv[u] = ((const uint4*)(at_k + ((size_t)kHeadDim << a.S.logP)))[lane];
-        ne[u] = *(const int2*)(a.S.exponents + 2 * ph);
-      }
+      const int t = span.tile(i) * kTile + 16 * wave;
+      int page = __builtin_amdgcn_readfirstlane(next_page);
+      none = (uint32_t)page >= (uint32_t)a.S.n_pages;
+      page = none ? 0 : page;
+      const int64_t head = (int64_t)page * a.S.H;
+      const uint8_t* from = slice_values + (head << (a.S.logP + 8)) + (t & in_page) * kHeadDim;
+      nk[0] = ((const uint4*)from)[lane], nk[1] = ((const uint4*)from)[kWave + lane];
+      from += (size_t)kHeadDim << a.S.logP;
+      nv[0] = ((const uint4*)from)[lane], nv[1] = ((const uint4*)from)[kWave + lane];
+      ne = slice_exponents[head];
     };
     const auto store_tile = [&](int b) {
+      float4 e = make_float4(ldexpf(a.scale, ne.x - kQTop), (float)ne.y, ldexpf(1.f, -ne.y), 0.f);
+      if (none) {  // a page that is not there: scores of -infinity, weights and values of 0
+        nk[0] = nk[1] = nv[0] = nv[1] = make_uint4(0, 0, 0, 0);
+        e = make_float4(0.f, -__builtin_inff(), 0.f, 0.f);
+      }
+      const int tok = lane >> 3, ch = lane & 7;
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
-        float4 e = make_float4(ldexpf(a.scale, ne[u].x - kQTop), (float)ne[u].y, ldexpf(1.f, -ne[u].y), 0.f);
-        if (none[u]) {  // a page that is not there: scores of -infinity, weights and values of 0
-          nk[u] = nv[u] = make_uint4(0, 0, 0, 0);
-          e = make_float4(0.f, -__builtin_inff(), 0.f, 0.f);
-        }
-        const int oc = wave + kWaves * u, tok = lane >> 3, ch = lane & 7;
-        ((uint4*)kbuf[b])[(kOct * oc + tok) * 8 + (ch ^ ((tok & 3) | ((oc & 1) << 2)))] = nk[u];
-        ((uint4*)vbuf[b])[64 * oc + lane] = nv[u];
-        if (lane == 0) meta[b][oc] = e;
+        ((uint4*)kbuf[b])[(16 * wave + kOct * u + tok) * 8 + (ch ^ ((tok & 3) | u << 2))] = nk[u];
+        ((uint4*)vbuf[b])[64 * (2 * wave + u) + lane] = nv[u];
       }
+      if (lane == 0) meta[b][wave] = e;
     };
     if (t_from < t_to) {
       find_tile(t_from);
@@ -716,7 +721,7 @@ __device__ __forceinline__ uint32_t many_rows(const PagesAttn& a, uint32_t x0, u
         const float ref = (unset ? 0.f : m) - kLift;
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
-          const float4 e = meta[b][2 * t + grp];
+          const float4 e = meta[b][t];
           const float factor = e.x * q_scale, shift = e.y - ref;
           inv[t] = e.z;
 #pragma unroll
@@ -724,9 +729,11 @@ __device__ __forceinline__ uint32_t many_rows(const PagesAttn& a, uint32_t x0, u
         }
         if constexpr (EDGE) {
 #pragma unroll
-          for (int t = 0; t < 4; ++t)
+          for (int t = 0; t < 4; ++t) {
+            const uint32_t bits = seen_bits(base + 16 * t, from, pos, sink);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) sc[8 * t + j] = sees(base + 16 * t + j, from, pos, sink) ? sc[8 * t + j] : -__builtin_inff();
+            for (int j = 0; j < 8; ++j) sc[8 * t + j] = seen_or_none(sc[8 * t + j], bits, j);
+          }
         }
         float top = sc[0];
 #pragma unroll
@@ -765,18 +772,16 @@ __device__ __forceinline__ uint32_t many_rows(const PagesAttn& a, uint32_t x0, u
 #pragma unroll
           for (int p = 0; p < 2; ++p) v[p] = ((const uint4*)vbuf[b])[(2 * t + grp) * 64 + 32 * p + row];
           if constexpr (EDGE) {  // tokens that no row sees may hold anything; NaN that only some rows see is brought back to those
-            uint32_t keep[2] = {0, 0}, nans = 0;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) keep[j / 4] |= sees(base + 16 * t + j, w_from, w_hi, sink) ? 0xffu << (8 * (j % 4)) : 0u;
+            const uint32_t any = seen_bits(base + 16 * t, w_from, w_hi, sink), keep[2] = {bytes_of_bits(any) * 0xffu, bytes_of_bits(any >> 4) * 0xffu};
+            uint32_t nans = 0;
 #pragma unroll
             for (int p = 0; p < 2; ++p) {
               v[p].x &= keep[0], v[p].y &= keep[1], v[p].z &= keep[0], v[p].w &= keep[1];
               nans |= nan_bytes(v[p].x) | nan_bytes(v[p].y) | nan_bytes(v[p].z) | nan_bytes(v[p].w);
             }
             if (__builtin_expect(__any(nans != 0), 0)) {
-              half8 one;
-#pragma unroll
-              for (int j = 0; j < 8; ++j) one[j] = sees(base + 16 * t + j, from, pos, sink) ? (_Float16)1.f : (_Float16)0.f;
+              const uint32_t bits = seen_bits(base + 16 * t, from, pos, sink);
+              const half8 one = operand(bytes_of_bits(bits) * 0x38u, bytes_of_bits(bits >> 4) * 0x38u);
 #pragma unroll
               for (int p = 0; p < 2; ++p) {
                 const uint32_t n[4] = {nan_bytes(v[p].x), nan_bytes(v[p].y), nan_bytes(v[p].z), nan_bytes(v[p].w)};
