@@ -375,6 +375,11 @@ def _pages_desc(n_layers, n_pages, n_kv_heads, n_q_heads, head_dim, page_tokens,
     return iwdft_pages_desc(n_layers, n_pages, n_kv_heads, n_q_heads, head_dim, page_tokens, max_pages, IWDFT_F32 if dtype == torch.float32 else IWDFT_BF16)
 
 
+@functools.lru_cache(maxsize=1024)
+def _pages_ref(*sizes):
+    return ctypes.byref(_pages_desc(*sizes))  # as the calls take it; keeps the descriptor
+
+
 def pages_desc(n_layers, n_pages, n_kv_heads, n_q_heads=None, head_dim=128, page_tokens=32, max_pages=1, dtype=torch.bfloat16) -> iwdft_pages_desc:
     return _pages_desc(n_layers, n_pages, n_kv_heads, n_kv_heads if n_q_heads is None else n_q_heads, head_dim, page_tokens, max_pages, dtype)
 
@@ -393,7 +398,7 @@ def _resize_bytes(batch, n_slots):
 @functools.lru_cache(maxsize=1024)
 def _attn_sizes(n_layers, batch, n_tokens, *desc):
     """The descriptor, as the call takes it, and the workspace's bytes."""
-    ref = ctypes.byref(_pages_desc(*desc))
+    ref = _pages_ref(*desc)
     return ref, _bytes_of(load_library().iwdft_pages_attn_bytes, ref, n_layers, batch, n_tokens)
 
 
@@ -423,10 +428,6 @@ def _expect(name: str, t: torch.Tensor, dtype, shape, device) -> None:
         raise ValueError(f"{name} must be contiguous")
 
 
-def _fits(t: torch.Tensor, dtype, shape, device) -> bool:
-    return t.dtype is dtype and t.shape == shape and t.device == device and t.is_contiguous()
-
-
 def _pool_sizes(values: torch.Tensor, exponents: torch.Tensor):
     """(device, layers, pages, KV heads, page tokens); the device is a GPU."""
     shape = values.shape
@@ -436,7 +437,8 @@ def _pool_sizes(values: torch.Tensor, exponents: torch.Tensor):
     if device.type != "cuda":
         raise ValueError("values must be device memory")
     n_layers, n_pages, heads, _, row = shape
-    if not (values.dtype is torch.uint8 and values.is_contiguous() and _fits(exponents, torch.int32, (n_layers, n_pages, heads, 2), device)):
+    if not (values.dtype is torch.uint8 and values.is_contiguous() and exponents.dtype is torch.int32 and exponents.shape == (n_layers, n_pages, heads, 2)
+            and exponents.device == device and exponents.is_contiguous()):
         _expect("values", values, torch.uint8, shape, device)
         _expect("exponents", exponents, torch.int32, (n_layers, n_pages, heads, 2), device)
     return device, n_layers, n_pages, heads, row // 128
@@ -448,15 +450,9 @@ def _kv_dtype(name: str, t: torch.Tensor):
     return t.dtype
 
 
-def _run_on(index: int, stream, call, *args) -> None:
-    """The call with the tensors' device as the current one, on its current stream unless one is given."""
-    if index == torch.cuda.current_device():
-        rc = call(*args, torch._C._cuda_getCurrentRawStream(index) if stream is None else _stream(stream))
-    else:
-        with torch.cuda.device(index):
-            rc = call(*args, _stream(stream))
-    if rc:
-        _check(rc)
+def _stream_of(stream, index: int):
+    """The given stream or the device's current one."""
+    return torch._C._cuda_getCurrentRawStream(index) if stream is None else _stream(stream)
 
 
 def _on_stream(stream, device):
@@ -480,35 +476,53 @@ def _scratch(n_bytes: int, device: torch.device, stream, workspace):
     return workspace
 
 
+# The calls check their tensors in one expression -- a decode step makes one of these calls per layer -- and say what is wrong where it fails.
 def iwdft_pages_resize(want, table, lens, free, starts, slots, page_tokens: int, stream=None, workspace=None) -> None:
     """Brings the sequences to want[b] tokens (negative: as they are): table, lens, free, starts and slots are brought up to date."""
-    device, shape = table.device, table.shape
+    device, shape, i32 = table.device, table.shape, torch.int32
     if len(shape) != 2 or device.type != "cuda":
         raise ValueError(f"table must be a device tensor [batch, max_pages], not {tuple(shape)} on {device}")
     batch, max_pages = shape
     n_free, n_slots = free.numel(), slots.numel()
-    for name, t, size in (("table", table, shape), ("want", want, (batch,)), ("lens", lens, (batch,)), ("free", free, (n_free,)), ("starts", starts, (batch + 1,)),
-                          ("slots", slots, (n_slots,))):
-        if not _fits(t, torch.int32, size, device):
-            _expect(name, t, torch.int32, size, device)
+    if not (table.dtype is want.dtype is lens.dtype is free.dtype is starts.dtype is slots.dtype is i32
+            and device == want.device == lens.device == free.device == starts.device == slots.device
+            and want.shape == lens.shape == (batch,) and starts.shape == (batch + 1,) and free.dim() == slots.dim() == 1
+            and table.is_contiguous() and want.is_contiguous() and lens.is_contiguous() and free.is_contiguous() and starts.is_contiguous()
+            and slots.is_contiguous()):
+        for name, t, size in (("table", table, shape), ("want", want, (batch,)), ("lens", lens, (batch,)), ("free", free, (n_free,)),
+                              ("starts", starts, (batch + 1,)), ("slots", slots, (n_slots,))):
+            _expect(name, t, i32, size, device)
+    index = device.index
+    if index != torch.cuda.current_device():
+        with torch.cuda.device(index):
+            return iwdft_pages_resize(want, table, lens, free, starts, slots, page_tokens, stream, workspace)
     ws = _scratch(_resize_bytes(batch, n_slots), device, stream, workspace)
-    _run_on(device.index, stream, load_library().iwdft_pages_resize, page_tokens, n_free - 1, max_pages, want.data_ptr(), batch, table.data_ptr(), lens.data_ptr(),
-            free.data_ptr(), starts.data_ptr(), slots.data_ptr(), n_slots, ws.data_ptr() if ws is not None else None, ws.nbytes if ws is not None else 0)
+    rc = load_library().iwdft_pages_resize(page_tokens, n_free - 1, max_pages, want.data_ptr(), batch, table.data_ptr(), lens.data_ptr(), free.data_ptr(),
+                                           starts.data_ptr(), slots.data_ptr(), n_slots, ws.data_ptr() if ws is not None else None,
+                                           ws.nbytes if ws is not None else 0, _stream_of(stream, index))
+    if rc:
+        _check(rc)
 
 
 def iwdft_pages_write(values, exponents, k, v, slots, layer: int = 0, stream=None) -> None:
     """k, v [layers written, tokens, KV heads, 128] into layers layer, layer + 1, ... at slots."""
     device, n_layers, n_pages, heads, P = _pool_sizes(values, exponents)
     dtype, n, shape = _kv_dtype("k", k), slots.numel(), k.shape
-    if not (_fits(slots, torch.int32, (n,), device) and _fits(k, dtype, (*shape[:1], n, heads, 128), device) and _fits(v, dtype, shape, device)):
+    if not (slots.dtype is torch.int32 and slots.dim() == 1 and v.dtype is dtype and device == slots.device == k.device == v.device
+            and shape == v.shape and shape[1:] == (n, heads, 128) and slots.is_contiguous() and k.is_contiguous() and v.is_contiguous()):
         _expect("slots", slots, torch.int32, (n,), device)
         _expect("k", k, dtype, (None, n, heads, 128), device)
         _expect("v", v, dtype, shape, device)
     if shape[0] == 0:
         return
-    desc = _pages_desc(n_layers, n_pages, heads, heads, 128, P, 1, dtype)
-    _run_on(device.index, stream, load_library().iwdft_pages_write, ctypes.byref(desc), layer, shape[0], k.data_ptr(), v.data_ptr(), slots.data_ptr(), n,
-            values.data_ptr(), exponents.data_ptr())
+    index = device.index
+    if index != torch.cuda.current_device():
+        with torch.cuda.device(index):
+            return iwdft_pages_write(values, exponents, k, v, slots, layer, stream)
+    rc = load_library().iwdft_pages_write(_pages_ref(n_layers, n_pages, heads, heads, 128, P, 1, dtype), layer, shape[0], k.data_ptr(), v.data_ptr(),
+                                          slots.data_ptr(), n, values.data_ptr(), exponents.data_ptr(), _stream_of(stream, index))
+    if rc:
+        _check(rc)
 
 
 def iwdft_pages_attn(values, exponents, q, starts, table, lens, out, layer: int = 0, n_sink: int = 0, n_recent: int = 0, scale: float = 0.0, stream=None,
@@ -516,8 +530,10 @@ def iwdft_pages_attn(values, exponents, q, starts, table, lens, out, layer: int 
     """q, out [layers, tokens, query heads, 128]: the new tokens' attention over their sequences in layers layer, layer + 1, ..."""
     device, n_layers, n_pages, heads, P = _pool_sizes(values, exponents)
     dtype, shape, size = _kv_dtype("q", q), q.shape, table.shape
-    if len(shape) != 4 or len(size) != 2 or not (_fits(q, dtype, (*shape[:3], 128), device) and _fits(out, dtype, shape, device) and _fits(table, torch.int32, size, device)
-                                                 and _fits(lens, torch.int32, size[:1], device) and _fits(starts, torch.int32, (size[0] + 1,), device)):
+    if not (len(shape) == 4 and len(size) == 2 and shape[3] == 128 and out.dtype is dtype and shape == out.shape
+            and starts.dtype is table.dtype is lens.dtype is torch.int32 and lens.shape == size[:1] and starts.shape == (size[0] + 1,)
+            and device == q.device == out.device == starts.device == table.device == lens.device and q.is_contiguous() and out.is_contiguous()
+            and starts.is_contiguous() and table.is_contiguous() and lens.is_contiguous()):
         _expect("q", q, dtype, (None, None, None, 128), device)
         _expect("out", out, dtype, shape, device)
         _expect("table", table, torch.int32, (None, None), device)
@@ -527,11 +543,17 @@ def iwdft_pages_attn(values, exponents, q, starts, table, lens, out, layer: int 
     batch, max_pages = size
     if n == 0:
         return
+    index = device.index
+    if index != torch.cuda.current_device():
+        with torch.cuda.device(index):
+            return iwdft_pages_attn(values, exponents, q, starts, table, lens, out, layer, n_sink, n_recent, scale, stream, workspace)
     desc, need = _attn_sizes(n, batch, n_tokens, n_layers, n_pages, heads, n_q_heads, 128, P, max_pages, dtype)
-    ws = _scratch(need, device, stream, workspace)
-    _run_on(device.index, stream, load_library().iwdft_pages_attn, desc, layer, n, q.data_ptr(), starts.data_ptr(), n_tokens,
-            table.data_ptr(), lens.data_ptr(), batch, values.data_ptr(), exponents.data_ptr(), out.data_ptr(), n_sink, n_recent, scale,
-            ws.data_ptr() if ws is not None else None, ws.nbytes if ws is not None else 0)
+    ws = _scratch(need, device, stream, workspace) if need or workspace is not None else None
+    rc = load_library().iwdft_pages_attn(desc, layer, n, q.data_ptr(), starts.data_ptr(), n_tokens, table.data_ptr(), lens.data_ptr(), batch,
+                                         values.data_ptr(), exponents.data_ptr(), out.data_ptr(), n_sink, n_recent, scale,
+                                         ws.data_ptr() if ws is not None else None, ws.nbytes if ws is not None else 0, _stream_of(stream, index))
+    if rc:
+        _check(rc)
 
 
 def iwdft_pages_read(values, exponents, table, lens, K, V, layer: int = 0, stream=None) -> None:
@@ -541,9 +563,9 @@ def iwdft_pages_read(values, exponents, table, lens, K, V, layer: int = 0, strea
     if some is None:
         return
     dtype, shape, size = _kv_dtype("K or V", some), some.shape, table.shape
-    full = (*shape[:1], *size[:1], heads, *shape[3:4], 128)
-    if not (len(size) == 2 and _fits(table, torch.int32, size, device) and _fits(lens, torch.int32, size[:1], device)
-            and (K is None or _fits(K, dtype, full, device)) and (V is None or _fits(V, dtype, full, device))):
+    if not (len(size) == 2 and len(shape) == 5 and shape[1:3] == (size[0], heads) and shape[4] == 128 and table.dtype is lens.dtype is torch.int32
+            and lens.shape == size[:1] and device == table.device == lens.device == some.device and table.is_contiguous() and lens.is_contiguous()
+            and some.is_contiguous() and (V is None or (V.dtype is dtype and V.shape == shape and V.device == device and V.is_contiguous()))):
         _expect("table", table, torch.int32, (None, None), device)
         _expect("lens", lens, torch.int32, size[:1], device)
         for name, t in (("K", K), ("V", V)):
@@ -551,9 +573,15 @@ def iwdft_pages_read(values, exponents, table, lens, K, V, layer: int = 0, strea
                 _expect(name, t, dtype, (shape[0], size[0], heads, shape[3] if len(shape) == 5 else None, 128), device)
     if shape[0] == 0:
         return
-    desc = _pages_desc(n_layers, n_pages, heads, heads, 128, P, size[1], dtype)
-    _run_on(device.index, stream, load_library().iwdft_pages_read, ctypes.byref(desc), layer, shape[0], table.data_ptr(), lens.data_ptr(), size[0], shape[3],
-            values.data_ptr(), exponents.data_ptr(), K.data_ptr() if K is not None else None, V.data_ptr() if V is not None else None)
+    index = device.index
+    if index != torch.cuda.current_device():
+        with torch.cuda.device(index):
+            return iwdft_pages_read(values, exponents, table, lens, K, V, layer, stream)
+    rc = load_library().iwdft_pages_read(_pages_ref(n_layers, n_pages, heads, heads, 128, P, size[1], dtype), layer, shape[0], table.data_ptr(), lens.data_ptr(),
+                                         size[0], shape[3], values.data_ptr(), exponents.data_ptr(), K.data_ptr() if K is not None else None,
+                                         V.data_ptr() if V is not None else None, _stream_of(stream, index))
+    if rc:
+        _check(rc)
 
 
 class PagedCache:
