@@ -39,16 +39,19 @@ struct Weights {
 // all parts of a call hold about the same number of tiles and there are no more than `parts` of them, as many as the chip holds at a time (one more would run
 // alone in the end: 16 contexts of 4096 to 16384 tokens 90 us, with the blocks' last, shorter parts counted in 78).  Lengths live on the
 // device, so every wave works out the shares by itself, 64 sequences at a time: the launch only has to be large enough.
-constexpr int kLeastTiles = 4;
+// Short parts cost more in the join than the second workgroup on a CU gains: one token over 8192 tokens of 8 heads 15.0 us with parts of 4 tiles, 12.0 with 8,
+// over 16000 17.3 with 8 and 15.6 with 16.
+constexpr int kLeastTiles = 4, kCus = 256;
 constexpr int kFewRows = 64;  // sequences of up to so many rows go to few_rows, where a call may have both
 
-template <int ROWS, int TOKENS, int PARTS>
+template <int ROWS, int TOKENS, int PARTS, int PAIR>
 struct Geometry {
   static constexpr int rows = ROWS, tile = TOKENS, parts = PARTS;  // of a block; of a tile; of a call
+  static constexpr int pair = PAIR;  // a second workgroup on a CU from parts of so many tiles on: more parts are more to join
 };
 template <int R>
-using Few = Geometry<16 * R, 32, 512>;
-using Many = Geometry<128, 64, 512>;
+using Few = Geometry<16 * R, 32, 512, 16>;
+using Many = Geometry<128, 64, 512, 8>;
 
 struct Seq {
   int len, first, nq, rows, tiles;  // tokens, first new token (row of q), new tokens, rows of all blocks, most tiles of a block
@@ -88,7 +91,8 @@ class Schedule {
     const float slices = (float)(a.n_layers * a.S.H);
     sum = __int_as_float(last_lane(__float_as_int(scan(sum)))) * slices;
     all_blocks = __int_as_float(last_lane(__float_as_int(scan(all_blocks)))) * slices;
-    w.tiles = which.part ? max(kLeastTiles, (int)fminf(ceilf(sum / fmaxf((float)Geo::parts - all_blocks, 0.5f * (float)Geo::parts)), 1e9f)) : 0x7fffffff;
+    const float alone = fminf(ceilf(sum / (float)kCus), (float)Geo::pair);
+    w.tiles = which.part ? (int)fminf(fmaxf(fmaxf((float)kLeastTiles, alone), ceilf(sum / fmaxf((float)Geo::parts - all_blocks, 0.5f * (float)Geo::parts))), 1e9f) : 0x7fffffff;
     int n = 0, cut = 0, cut_rows = 0;
     each([&](int, const Seq& s) {
       const int np = parts(s), all = np * blocks(s.rows);
