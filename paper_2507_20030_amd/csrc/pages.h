@@ -40,6 +40,10 @@ __device__ __forceinline__ void e4m3_floats(uint32_t w, float* f) {
 }
 // Nearest e4m3 of four floats, ties to even; beyond 448 (infinities) 448, NaN stays NaN.
 __device__ __forceinline__ float e4m3_range(float x) { return x != x ? x : fminf(fmaxf(x, -(float)kE4m3Max), (float)kE4m3Max); }
+__device__ __forceinline__ uint32_t floats_e4m3_in_range(const float* f) {  // |f| <= 448
+  const int w = __builtin_amdgcn_cvt_pk_fp8_f32(f[0], f[1], 0, false);
+  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(f[2], f[3], w, true);
+}
 __device__ __forceinline__ uint32_t floats_e4m3(const float* f) {
   int w = __builtin_amdgcn_cvt_pk_fp8_f32(e4m3_range(f[0]), e4m3_range(f[1]), 0, false);
   return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(e4m3_range(f[2]), e4m3_range(f[3]), w, true);

@@ -199,10 +199,7 @@ __global__ __launch_bounds__(256) void resize_fill_kernel(ResizeArgs a) {
 }
 
 // ------------------------------------------------------------------------------------------------ writing
-__device__ __forceinline__ float finite_abs(float x) {
-  const float y = fabsf(x);
-  return y < __builtin_inff() ? y : 0.f;  // NaN and infinities do not set the scale
-}
+typedef unsigned short ushort2v __attribute__((ext_vector_type(2)));
 
 // 8 tokens of one head as a lane stores them.  K: token lane / 8, channels 16 (lane % 8) ..; V: channels 2 lane, 2 lane + 1 of every token.
 template <bool BF16, bool V>
@@ -243,18 +240,37 @@ struct Octet {
     if constexpr (BF16) return __uint_as_float(i % 2 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
     else return __uint_as_float(w[i]);
   }
-  __device__ __forceinline__ float top() const {
-    float t = 0.f;
+  // Magnitudes compare like their bits: largest |x| as a float's bits, NaN and infinities (kInf and more) among them, or without them.
+  static constexpr uint32_t kInf = 0x7f800000u;
+  __device__ __forceinline__ uint32_t top() const {
+    if constexpr (BF16) {
+      ushort2v t{0, 0};
 #pragma unroll
-    for (int i = 0; i < 16; ++i) t = fmaxf(t, finite_abs(value(i)));
+      for (int i = 0; i < 8; ++i) t = __builtin_elementwise_max(t, __builtin_bit_cast(ushort2v, w[i] & 0x7fff7fffu));
+      return (uint32_t)max(t[0], t[1]) << 16;
+    } else {
+      uint32_t t = 0;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) t = max(t, w[i] & 0x7fffffffu);
+      return t;
+    }
+  }
+  __device__ __forceinline__ uint32_t finite_top() const {
+    uint32_t t = 0;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const uint32_t u = __float_as_uint(value(i)) & 0x7fffffffu;
+      t = u < kInf && u > t ? u : t;
+    }
     return t;
   }
-  __device__ __forceinline__ void bytes(int e, uint32_t* out) const {  // in the page's order, times 2^-e
+  // in the page's order, times scale = 2^-e, which brings every finite value to 448 at most
+  __device__ __forceinline__ void bytes(float scale, bool finite, uint32_t* out) const {
     float f[16];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) f[V ? 8 * (i % 2) + i / 2 : i] = ldexpf(value(i), -e);
+    for (int i = 0; i < 16; ++i) f[V ? 8 * (i % 2) + i / 2 : i] = value(i) * scale;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) out[i] = floats_e4m3(f + 4 * i);
+    for (int i = 0; i < 4; ++i) out[i] = finite ? floats_e4m3_in_range(f + 4 * i) : floats_e4m3(f + 4 * i);
   }
 };
 
@@ -269,25 +285,32 @@ __device__ int write_run(const Pages& S, int64_t ph, const void* x, int64_t row0
   const int lane = threadIdx.x % kWave;
   const int o0 = offset / kOct, octets = (offset + n + kOct - 1) / kOct - o0;
   Octet<BF16, V> held[kHeld];
-  float top = 0.f;
 #pragma unroll
   for (int k = 0; k < kHeld; ++k)
     if (k < octets) held[k].load(x, row0, row_step, (o0 + k) * kOct - offset, n);
+  const auto over = [&](auto top_of) {  // the octets, then the lanes
+    uint32_t top = 0;
 #pragma unroll
-  for (int k = 0; k < kHeld; ++k)
-    if (k < octets) top = fmaxf(top, held[k].top());
-  for (int k = kHeld; k < octets; ++k) {
-    Octet<BF16, V> more;
-    more.load(x, row0, row_step, (o0 + k) * kOct - offset, n);
-    top = fmaxf(top, more.top());
-  }
+    for (int k = 0; k < kHeld; ++k)
+      if (k < octets) top = max(top, top_of(held[k]));
+    for (int k = kHeld; k < octets; ++k) {
+      Octet<BF16, V> more;
+      more.load(x, row0, row_step, (o0 + k) * kOct - offset, n);
+      top = max(top, top_of(more));
+    }
 #pragma unroll
-  for (int d = 1; d < kWave; d <<= 1) top = fmaxf(top, __shfl_xor(top, d));
-  int e = e4m3_exponent(top), grown = 0;
+    for (int d = 1; d < kWave; d <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, d));
+    return top;
+  };
+  uint32_t top = over([](const Octet<BF16, V>& y) { return y.top(); });
+  const bool finite = __builtin_amdgcn_readfirstlane((int)top) < (int)Octet<BF16, V>::kInf;
+  if (!finite) top = over([](const Octet<BF16, V>& y) { return y.finite_top(); });  // NaN and infinities do not set the scale
+  int e = e4m3_exponent(__uint_as_float(top)), grown = 0;
   if (offset > 0) {
     grown = max(0, e - old);
     e = max(e, old);
   }
+  const float scale = ldexpf(1.f, -e);
   if (lane == 0) S.exponents[2 * ph + (V ? 1 : 0)] = e;
   uint8_t* base = page_values(S, ph) + (V ? (size_t)kHeadDim << S.logP : 0);
 
@@ -301,7 +324,7 @@ __device__ int write_run(const Pages& S, int64_t ph, const void* x, int64_t row0
   const auto store = [&](const Octet<BF16, V>& oct, int o) {
     uint4* at = (uint4*)(base + o * kOct * kHeadDim) + lane;
     uint32_t now[4];
-    oct.bytes(e, now);
+    oct.bytes(scale, finite, now);
     if constexpr (!V) {
       const int row = o * kOct + lane / 8;
       if (row < offset && grown) {
