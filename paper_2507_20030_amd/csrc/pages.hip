@@ -18,27 +18,31 @@ struct ResizeState {
   int count, released, taken, total;  // total: new tokens
 };
 
-// Sums over the threads before this one, and over all of them; every thread of the workgroup calls it.
-template <class T>
-__device__ __forceinline__ T scan_before(T x, T* lds, T* sum) {
+// Sums of N numbers >= 0 over the threads before this one and over all threads of the workgroup; every thread calls it.  In two halves of 16 bits, whose sums over
+// a wave fit 32.
+template <int N>
+__device__ __forceinline__ void sums_before(const int (&x)[N], long long (&before)[N], long long (&all)[N], long long (*lds)[N]) {
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-  T in = x;
 #pragma unroll
-  for (int d = 1; d < kWave; d <<= 1) {
-    const T up = __shfl_up(in, d);
-    if (lane >= d) in += up;
+  for (int i = 0; i < N; ++i) {
+    const int lo = scan(x[i] & 0xffff), hi = scan((int)((uint32_t)x[i] >> 16));
+    before[i] = ((long long)hi << 16) + lo;
   }
   __syncthreads();  // the last call's sums have been read
-  if (lane == kWave - 1) lds[wave] = in;
+  if (lane == kWave - 1)
+#pragma unroll
+    for (int i = 0; i < N; ++i) lds[wave][i] = before[i];
   __syncthreads();
-  T before = 0, all = 0;
-  for (int w = 0; w < kResizeThreads / kWave; ++w) {
-    const T s = lds[w];
-    if (w < wave) before += s;
-    all += s;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    long long sum = 0, mine = 0;
+#pragma unroll 4
+    for (int w = 0; w < kResizeThreads / kWave; ++w) {
+      mine = w == wave ? sum : mine;
+      sum += lds[w][i];
+    }
+    before[i] += mine - x[i], all[i] = sum;
   }
-  *sum = all;
-  return before + in - x;
 }
 
 struct Change {
@@ -105,51 +109,48 @@ __device__ void resize_fill(const ResizeArgs& a, const Fill& f, int at, int step
 // stores of one workgroup.  Otherwise resize_fill_kernel follows.
 template <bool ONE>
 __global__ __launch_bounds__(kResizeThreads) void resize_kernel(ResizeArgs a) {
-  __shared__ long long lds64[kResizeThreads / kWave];
-  __shared__ int lds32[kResizeThreads / kWave];
-  __shared__ int32_t keep[ONE ? 4 * kResizeOneBatch + 1 : 1];
+  __shared__ long long lds3[kResizeThreads / kWave][3], lds2[kResizeThreads / kWave][2], lds1[kResizeThreads / kWave][1];
+  __shared__ int32_t keep[ONE ? 4 * kResizeOneBatch : 1];
   int32_t *have = ONE ? keep : a.scratch + 4, *need = have + (ONE ? kResizeOneBatch : a.batch), *gone = need + (ONE ? kResizeOneBatch : a.batch);
   int32_t* starts = ONE ? gone + kResizeOneBatch : a.starts;
   const int tid = threadIdx.x;
   const int count = min(max(a.free[0], 0), a.n_pages);
+  const auto pages_gone = [&](const Change& c) { return max(0, page_count(c.have, a.logP) - page_count(c.want, a.logP)); };
 
-  int released = 0;
-  for (int b0 = 0; b0 < a.batch; b0 += kResizeThreads) {  // pages given back by all: they serve this call too
-    const int b = b0 + tid;
-    int g = 0, all;
-    if (b < a.batch) {
-      const Change c = change_of(a, b);
-      g = max(0, page_count(c.have, a.logP) - page_count(c.want, a.logP));
+  long long given = 0;  // pages given back by all: they serve this call too
+  if (!ONE && a.batch > kResizeThreads)
+    for (int b0 = 0; b0 < a.batch; b0 += kResizeThreads) {
+      const int b = b0 + tid, x[1] = {b < a.batch ? pages_gone(change_of(a, b)) : 0};
+      long long before[1], all[1];
+      sums_before(x, before, all, lds1);
+      given += all[0];
     }
-    const int before = scan_before(g, lds32, &all);
-    if (b < a.batch) gone[b] = released + before;
-    released += all;
-  }
-  released = min(released, a.n_pages);  // more only if two sequences held the same page
 
-  long long asked = 0, fresh = 0;
-  int taken = 0, total = 0;
+  long long asked = 0, fresh = 0, back = 0;
+  int taken = 0, total = 0, released = 0;
   for (int b0 = 0; b0 < a.batch; b0 += kResizeThreads) {
     const int b = b0 + tid;
     Change c{0, 0};
     if (b < a.batch) c = change_of(a, b);
     const bool up = c.want > c.have;
-    const int pages = up ? page_count(c.want, a.logP) - page_count(c.have, a.logP) : 0, tokens = up ? c.want - c.have : 0;
-    long long all_pages, all_tokens;
-    const long long pages_to = asked + scan_before((long long)pages, lds64, &all_pages) + pages;
-    const long long tokens_to = fresh + scan_before((long long)tokens, lds64, &all_tokens) + tokens;
-    const bool ok = up && tokens_to <= a.n_slots && (pages == 0 || pages_to <= (long long)count + released);
-    int all_in, all_new;
-    scan_before(ok ? pages : 0, lds32, &all_in);
-    const int first = total + scan_before(ok ? tokens : 0, lds32, &all_new);
+    const int x[3] = {pages_gone(c), up ? page_count(c.want, a.logP) - page_count(c.have, a.logP) : 0, up ? c.want - c.have : 0};
+    long long before[3], all[3];
+    sums_before(x, before, all, lds3);
+    released = (int)min(a.batch > kResizeThreads ? given : all[0], (long long)a.n_pages);  // more only if two sequences held the same page
+    const long long pages_to = asked + before[1] + x[1], tokens_to = fresh + before[2] + x[2];
+    const bool ok = up && tokens_to <= a.n_slots && (x[1] == 0 || pages_to <= (long long)count + released);
+    const int in[2] = {ok ? x[1] : 0, ok ? x[2] : 0};
+    long long in_before[2], in_all[2];
+    sums_before(in, in_before, in_all, lds2);
     if (b < a.batch) {
       have[b] = c.have;
-      need[b] = (int)min(pages_to - pages, (long long)0x7fffffff);  // of admitted sequences: whoever asked before them got it
-      starts[b] = first;
-      if (ONE) a.starts[b] = first;
+      need[b] = (int)min(pages_to - x[1], (long long)0x7fffffff);  // of admitted sequences: whoever asked before them got it
+      gone[b] = (int)min(back + before[0], (long long)0x7fffffff);
+      starts[b] = total + (int)in_before[1];
+      if (ONE) a.starts[b] = starts[b];
       a.lens[b] = ok || c.want < c.have ? c.want : c.have;
     }
-    asked += all_pages, fresh += all_tokens, taken += all_in, total += all_new;
+    asked += all[1], fresh += all[2], back += all[0], taken += (int)in_all[0], total += (int)in_all[1];
   }
   if (tid == 0) {
     a.starts[a.batch] = total;
@@ -164,7 +165,7 @@ __global__ __launch_bounds__(kResizeThreads) void resize_kernel(ResizeArgs a) {
 }
 
 // Up to 64 sequences: the sums are one wave's scans, then everybody fills.  Tokens and pages of a sequence are cut to what passes the slots anyway (a new page
-// has a new token), so that 32 bits hold the sums.  A decode step of 16 sequences: XX us with the scans of 16 waves above, XX with these.
+// has a new token), so that 32 bits hold the sums.  A decode step of 16 sequences: 6.8 us with the scans of 16 waves above, 1.9 with these.
 __global__ __launch_bounds__(256) void resize_wave_kernel(ResizeArgs a) {
   __shared__ int32_t keep[5][kResizeWaveBatch];
   __shared__ ResizeState state;
@@ -193,9 +194,17 @@ __global__ __launch_bounds__(256) void resize_wave_kernel(ResizeArgs a) {
   resize_fill(a, Fill{keep[0], keep[1], keep[2], keep[3], keep[4], state}, threadIdx.x, 256);
 }
 
+// Every slot looks its sequence up: in LDS where the starts fit (256 sequences, 280000 slots: 5.9 us with eight dependent loads from memory, 5.5 so).
 __global__ __launch_bounds__(256) void resize_fill_kernel(ResizeArgs a) {
+  __shared__ int32_t starts[kResizeOneBatch];
   const int32_t* s = a.scratch;
-  resize_fill(a, Fill{s + 4, a.lens, s + 4 + a.batch, s + 4 + 2 * a.batch, a.starts, {s[0], s[1], s[2], s[3]}}, blockIdx.x * 256 + threadIdx.x, gridDim.x * 256);
+  const bool fits = a.batch <= kResizeOneBatch;
+  if (fits) {
+    for (int b = threadIdx.x; b < a.batch; b += 256) starts[b] = a.starts[b];
+    __syncthreads();
+  }
+  resize_fill(a, Fill{s + 4, a.lens, s + 4 + a.batch, s + 4 + 2 * a.batch, fits ? starts : a.starts, {s[0], s[1], s[2], s[3]}}, blockIdx.x * 256 + threadIdx.x,
+              gridDim.x * 256);
 }
 
 // ------------------------------------------------------------------------------------------------ writing
@@ -276,7 +285,8 @@ struct Octet {
 
 // A run -- new tokens that follow each other in one page -- is one wave's work for each head and tensor: its largest value, the page's exponent, the
 // values, and no two waves meet.  Up to kHeld octets stay in registers, all on their way at a time; a longer run (pages of 128) is read twice, the
-// second time from the caches.  Bound by memory: 46000 tokens of 8 heads, bf16, XX us with every run read twice, 256 bytes at a time, XX now.
+// second time from the caches.  Bound by memory: 46000 tokens of 8 heads, bf16 (189 MB):
+// 78 us with every run read twice, 256 bytes at a time, 50 held in registers, 43 with integer maxima.
 // old: the page's exponent, used from its second token on; returns the new one.  Old values are only touched where it grows; of an octet of V that
 // holds other tokens too the bytes of those stay.
 constexpr int kHeld = 8;
