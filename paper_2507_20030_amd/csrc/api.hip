@@ -629,7 +629,9 @@ int flush_pending(iwdft_ctx* c, hipStream_t st) {
 }
 
 // 8-bit pages.
-constexpr int64_t kMostRows = (int64_t)1 << 31;  // (token, head, layer) rows of a call: grids and 32-bit counts
+constexpr double kMostRows = 1 << 30;   // (token, head, layer) rows of a call: 32-bit counts
+constexpr int kMostCount = 1 << 30;     // sequences, slots
+constexpr double kMostBytes = 1e15;     // of the values
 const char kPageAlignMsg[] = "values and token tensors must be 16-byte aligned, exponents 8-byte, int32 arrays 4-byte";
 template <class... T>
 bool unaligned(uintptr_t n, T... p) {
@@ -655,7 +657,10 @@ int check_pages(const iwdft_pages_desc* d, int32_t layer, int32_t n_layers) {
   if (d->head_dim != kHeadDim) return fail(IWDFT_ERR_UNSUPPORTED, "head_dim %d: this build handles 128", d->head_dim);
   if (layer < 0 || n_layers <= 0 || layer > d->n_layers - n_layers)
     return fail(IWDFT_ERR_ARG, "layers %d .. %lld of %d", layer, (long long)layer + n_layers - 1, d->n_layers);
-  return check_page_size(d->page_tokens, d->n_pages, d->max_pages);
+  const int rc = check_page_size(d->page_tokens, d->n_pages, d->max_pages);
+  if (rc == IWDFT_OK && 2.0 * kHeadDim * d->n_layers * d->n_pages * d->n_kv_heads * d->page_tokens > kMostBytes)
+    return fail(IWDFT_ERR_ARG, "%d layers of %d pages of %d heads: too many bytes", d->n_layers, d->n_pages, d->n_kv_heads);
+  return rc;
 }
 Pages pages_of(const iwdft_pages_desc& d, void* values, int32_t* exponents) {
   return Pages{d.n_pages, d.n_kv_heads, d.n_q_heads / d.n_kv_heads, log2_of(d.page_tokens), d.max_pages, (uint8_t*)values, exponents};
@@ -1169,7 +1174,7 @@ int iwdft_pages_query_bytes(const iwdft_pages_desc* desc, size_t* values_bytes, 
 
 int iwdft_pages_resize_bytes(int32_t batch, int32_t n_slots, size_t* workspace_bytes) {
   if (!workspace_bytes) return fail(IWDFT_ERR_ARG, "output pointer is NULL");
-  if (batch < 0 || n_slots < 0) return fail(IWDFT_ERR_ARG, "batch = %d, n_slots = %d: negative", batch, n_slots);
+  if (batch < 0 || n_slots < 0 || batch > kMostCount || n_slots > kMostCount) return fail(IWDFT_ERR_ARG, "batch = %d, n_slots = %d out of range", batch, n_slots);
   *workspace_bytes = batch <= kResizeOneBatch && n_slots <= kResizeOneSlots ? 0 : sizeof(int32_t) * (4 + 3 * (size_t)batch);
   return IWDFT_OK;
 }
@@ -1192,12 +1197,13 @@ int iwdft_pages_write(const iwdft_pages_desc* desc, int32_t layer, int32_t n_lay
                       void* d_values, int32_t* d_exponents, void* hip_stream) {
   const int rc = check_pages(desc, layer, n_layers);
   if (rc != IWDFT_OK) return rc;
-  if (n_tokens < 0 || (int64_t)n_tokens * desc->n_kv_heads * n_layers > kMostRows) return fail(IWDFT_ERR_ARG, "n_tokens = %d out of range", n_tokens);
+  const Pages pages = pages_of(*desc, d_values, d_exponents);
+  if (n_tokens < 0 || (double)n_tokens * desc->n_kv_heads * n_layers > kMostRows || pages_write_units(pages, n_layers, n_tokens) > kMostUnits)
+    return fail(IWDFT_ERR_ARG, "n_tokens = %d out of range", n_tokens);
   if (n_tokens == 0) return IWDFT_OK;
   if (!d_k || !d_v || !d_slots || !d_values || !d_exponents) return fail(IWDFT_ERR_ARG, "a device pointer is NULL");
   if (unaligned(16, d_k, d_v, d_values) || unaligned(4, d_slots) || unaligned(8, d_exponents)) return fail(IWDFT_ERR_ARG, "%s", kPageAlignMsg);
-  return launched(launch_pages_write(pages_of(*desc, d_values, d_exponents), layer, n_layers, desc->kv_dtype == IWDFT_BF16, d_k, d_v, d_slots, n_tokens,
-                                     (hipStream_t)hip_stream),
+  return launched(launch_pages_write(pages, layer, n_layers, desc->kv_dtype == IWDFT_BF16, d_k, d_v, d_slots, n_tokens, (hipStream_t)hip_stream),
                   "page write launch");
 }
 
@@ -1205,7 +1211,8 @@ int iwdft_pages_attn_bytes(const iwdft_pages_desc* desc, int32_t n_layers, int32
   if (!workspace_bytes) return fail(IWDFT_ERR_ARG, "output pointer is NULL");
   const int rc = check_pages(desc, 0, n_layers);
   if (rc != IWDFT_OK) return rc;
-  if (batch < 0 || n_tokens < 0) return fail(IWDFT_ERR_ARG, "batch = %d, n_tokens = %d: negative", batch, n_tokens);
+  if (batch < 0 || batch > kMostCount || n_tokens < 0 || (double)n_tokens * desc->n_q_heads * n_layers > kMostRows)
+    return fail(IWDFT_ERR_ARG, "batch = %d, n_tokens = %d out of range", batch, n_tokens);
   *workspace_bytes = pages_attn_bytes(pages_of(*desc, nullptr, nullptr), batch, n_tokens, desc->kv_dtype == IWDFT_BF16);
   return IWDFT_OK;
 }
@@ -1217,7 +1224,6 @@ int iwdft_pages_attn(const iwdft_pages_desc* desc, int32_t layer, int32_t n_laye
   size_t need = 0;
   if (rc == IWDFT_OK) rc = iwdft_pages_attn_bytes(desc, n_layers, batch, n_tokens, &need);
   if (rc != IWDFT_OK) return rc;
-  if ((int64_t)n_tokens * desc->n_q_heads * n_layers > kMostRows) return fail(IWDFT_ERR_ARG, "n_tokens = %d out of range", n_tokens);
   if (n_sink < 0 || n_recent < 0) return fail(IWDFT_ERR_ARG, "n_sink = %d, n_recent = %d: negative", n_sink, n_recent);
   if (n_sink > 0 && n_recent == 0) return fail(IWDFT_ERR_ARG, "n_sink = %d without a window: n_recent = 0 lets every row see all tokens before it", n_sink);
   if (scale != scale) return fail(IWDFT_ERR_ARG, "scale is NaN");
@@ -1240,13 +1246,13 @@ int iwdft_pages_read(const iwdft_pages_desc* desc, int32_t layer, int32_t n_laye
                      const void* d_values, const int32_t* d_exponents, void* d_K, void* d_V, void* hip_stream) {
   const int rc = check_pages(desc, layer, n_layers);
   if (rc != IWDFT_OK) return rc;
-  if (batch < 0 || n_tokens < 0 || (double)n_tokens * batch * desc->n_kv_heads * n_layers > (double)kMostRows)
+  const Pages pages = pages_of(*desc, (void*)d_values, (int32_t*)d_exponents);
+  if (batch < 0 || n_tokens < 0 || (double)n_tokens * batch * desc->n_kv_heads * n_layers > kMostRows || pages_read_units(pages, n_layers, batch, n_tokens) > kMostUnits)
     return fail(IWDFT_ERR_ARG, "batch = %d, n_tokens = %d out of range", batch, n_tokens);
   if (n_tokens == 0 || batch == 0 || (!d_K && !d_V)) return IWDFT_OK;
   if (!d_table || !d_lens || !d_values || !d_exponents) return fail(IWDFT_ERR_ARG, "a device pointer is NULL");
   if (unaligned(16, d_K, d_V, d_values) || unaligned(4, d_table, d_lens) || unaligned(8, d_exponents)) return fail(IWDFT_ERR_ARG, "%s", kPageAlignMsg);
-  return launched(launch_pages_read(pages_of(*desc, (void*)d_values, (int32_t*)d_exponents), layer, n_layers, desc->kv_dtype == IWDFT_BF16, d_table, d_lens,
-                                    batch, n_tokens, d_K, d_V, (hipStream_t)hip_stream),
+  return launched(launch_pages_read(pages, layer, n_layers, desc->kv_dtype == IWDFT_BF16, d_table, d_lens, batch, n_tokens, d_K, d_V, (hipStream_t)hip_stream),
                   "page read launch");
 }
 

@@ -79,9 +79,12 @@ constexpr int kResizeThreads = 1024;
 constexpr int kResizeOneBatch = 1024, kResizeOneSlots = 2048, kResizeWaveBatch = 64;
 hipError_t launch_pages_resize(const ResizeArgs& a, hipStream_t st);
 
+constexpr int64_t kMostUnits = ((int64_t)1 << 26) - 4;  // waves of a launch: 2^32 threads are too many
+int64_t pages_write_units(const Pages& S, int n_layers, int n_tokens);
+int64_t pages_read_units(const Pages& S, int n_layers, int batch, int n);
 hipError_t launch_pages_write(const Pages& S, int layer, int n_layers, bool bf16, const void* k, const void* v, const int32_t* slots, int n_tokens,
                               hipStream_t st);
-hipError_t launch_pages_read(const Pages& S, int layer, int n_layers, bool bf16, const int32_t* table, const int32_t* lens, int batch, int64_t n, void* K,
+hipError_t launch_pages_read(const Pages& S, int layer, int n_layers, bool bf16, const int32_t* table, const int32_t* lens, int batch, int n, void* K,
                              void* V, hipStream_t st);
 
 // The sequences of one kind of blocks.

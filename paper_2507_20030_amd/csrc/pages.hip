@@ -534,24 +534,34 @@ hipError_t launch_pages_resize(const ResizeArgs& a, hipStream_t st) {
   return hipGetLastError();
 }
 
+namespace {
+// as many waves as fill the chip, each with up to a page of tokens, which is one run of a prompt
+int write_segment(const Pages& S, int n_layers, int n_tokens) {
+  return (int)std::max<int64_t>(1, std::min<int64_t>({kWave, (int64_t)1 << S.logP, n_tokens * ((int64_t)n_layers * S.H * 2) / 8192}));
+}
+}  // namespace
+int64_t pages_write_units(const Pages& S, int n_layers, int n_tokens) {
+  const int segment = write_segment(S, n_layers, n_tokens);
+  return ((int64_t)n_tokens + segment - 1) / segment * n_layers * S.H * 2;
+}
+int64_t pages_read_units(const Pages& S, int n_layers, int batch, int n) { return ((int64_t)n + kOct - 1) / kOct * S.H * batch * n_layers; }
+
 hipError_t launch_pages_write(const Pages& S, int layer, int n_layers, bool bf16, const void* k, const void* v, const int32_t* slots, int n_tokens,
                               hipStream_t st) {
-  // as many waves as fill the chip, each with up to a page of tokens, which is one run of a prompt
-  const int64_t per_token = (int64_t)n_layers * S.H * 2;
-  const int segment = (int)std::max<int64_t>(1, std::min<int64_t>({kWave, (int64_t)1 << S.logP, n_tokens * per_token / 8192}));
-  const int64_t units = ((n_tokens + segment - 1) / segment) * per_token;
+  const int segment = write_segment(S, n_layers, n_tokens);
+  const int64_t units = pages_write_units(S, n_layers, n_tokens);
   const unsigned grid = (unsigned)((units + 3) / 4);
   if (bf16) pages_write_kernel<true><<<grid, 256, 0, st>>>(S, layer, n_layers, k, v, slots, n_tokens, segment, units);
   else pages_write_kernel<false><<<grid, 256, 0, st>>>(S, layer, n_layers, k, v, slots, n_tokens, segment, units);
   return hipGetLastError();
 }
 
-hipError_t launch_pages_read(const Pages& S, int layer, int n_layers, bool bf16, const int32_t* table, const int32_t* lens, int batch, int64_t n, void* K,
-                             void* V, hipStream_t st) {
-  const int64_t units = (n + kOct - 1) / kOct * S.H * batch * n_layers;
+hipError_t launch_pages_read(const Pages& S, int layer, int n_layers, bool bf16, const int32_t* table, const int32_t* lens, int batch, int n, void* K, void* V,
+                             hipStream_t st) {
+  const int64_t units = pages_read_units(S, n_layers, batch, n);
   const unsigned grid = (unsigned)((units + 3) / 4);
-  if (bf16) pages_read_kernel<true><<<grid, 256, 0, st>>>(S, layer, batch, (int)n, table, lens, K, V, units);
-  else pages_read_kernel<false><<<grid, 256, 0, st>>>(S, layer, batch, (int)n, table, lens, K, V, units);
+  if (bf16) pages_read_kernel<true><<<grid, 256, 0, st>>>(S, layer, batch, n, table, lens, K, V, units);
+  else pages_read_kernel<false><<<grid, 256, 0, st>>>(S, layer, batch, n, table, lens, K, V, units);
   return hipGetLastError();
 }
 

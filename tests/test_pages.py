@@ -163,3 +163,21 @@ def test_binding_refuses_tensors_that_do_not_fit():
         B.PagedCache(1, 4, 2, 2, 128, torch.float16, 1, 64)
     with pytest.raises(B.IwdftError):
         B.PagedCache(1, 4, 2, 3, 128, torch.float32, 1, 64)
+
+
+def test_sizes_whose_counts_would_not_fit():
+    """Products of sizes that pass 64 bits, launches of 2^32 threads and more, counts that pass 32 bits."""
+    lib, n = B.load_library(), ctypes.c_size_t()
+    huge = dict(n_layers=2 ** 31 - 1, n_pages=2 ** 24, n_kv_heads=2 ** 30, n_q_heads=2 ** 30, page_tokens=64)
+    with pytest.raises(B.IwdftError) as e:
+        B.iwdft_pages_query_bytes(c_desc(**huge))
+    assert e.value.code == B.IWDFT_ERR_ARG
+    wide = ctypes.byref(c_desc(n_layers=2 ** 20, n_kv_heads=2 ** 14, n_q_heads=2 ** 30, page_tokens=16, n_pages=1))
+    for call, args in ((lib.iwdft_pages_attn_bytes, (wide, 2 ** 20, 1, 2 ** 30, ctypes.byref(n))), (lib.iwdft_pages_attn_bytes, (wide, 1, 2 ** 30 + 1, 1, ctypes.byref(n))),
+                       (lib.iwdft_pages_resize_bytes, (2 ** 30 + 1, 1, ctypes.byref(n))), (lib.iwdft_pages_resize_bytes, (1, 2 ** 30 + 1, ctypes.byref(n))),
+                       (lib.iwdft_pages_write, (wide, 0, 2 ** 20, FAKE, FAKE, FAKE, 2 ** 30, FAKE, FAKE, None)),
+                       (lib.iwdft_pages_write, (wide, 0, 2 ** 12, FAKE, FAKE, FAKE, 1, FAKE, FAKE, None)),                       # 2^27 waves
+                       (lib.iwdft_pages_write, (ctypes.byref(c_desc(page_tokens=16)), 0, 1, FAKE, FAKE, FAKE, 2 ** 29, FAKE, FAKE, None)),
+                       (lib.iwdft_pages_read, (wide, 0, 2 ** 20, FAKE, FAKE, 2 ** 30, 2 ** 30, FAKE, FAKE, FAKE, FAKE, None)),
+                       (lib.iwdft_pages_read, (ctypes.byref(c_desc()), 0, 2, FAKE, FAKE, 2 ** 25, 1, FAKE, FAKE, FAKE, FAKE, None))):  # 2^27 waves of one token
+        assert call(*args) == B.IWDFT_ERR_ARG, args
