@@ -42,6 +42,7 @@ struct Weights {
 // Short parts cost more in the join than the second workgroup on a CU gains: one token over 8192 tokens of 8 heads 15.0 us with parts of 4 tiles, 12.0 with 8,
 // over 16000 17.3 with 8 and 15.6 with 16.
 constexpr int kLeastTiles = 4, kCus = 256;
+constexpr float kMostBlocks = 1100000000.f;  // 2^30 rows have fewer: starts that overlap, whose counts would not fit; such a call does nothing
 constexpr int kFewRows = 64;  // sequences of up to so many rows go to few_rows, where a call may have both
 
 template <int ROWS, int TOKENS, int PARTS, int PAIR>
@@ -100,6 +101,7 @@ class Schedule {
       if (np > 1) cut += all, cut_rows += s.rows;
     });
     w.parts = last_lane(scan(n)), w.split = last_lane(scan(cut)), w.split_rows = last_lane(scan(cut_rows));
+    if (all_blocks > kMostBlocks) w.parts = w.split = w.split_rows = 0;
   }
 
   static __device__ __forceinline__ int blocks(int rows) { return (rows + Geo::rows - 1) / Geo::rows; }
