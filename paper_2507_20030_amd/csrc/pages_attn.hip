@@ -763,13 +763,8 @@ __device__ __forceinline__ uint32_t many_rows(const PagesAttn& a, uint32_t x0, u
 #pragma unroll
           for (int j = 0; j < 8; ++j) y[j] = __builtin_amdgcn_exp2f(sc[8 * t + j]);
           to_halves<8, PARTS>(y, pw[t]);
-          if constexpr (PARTS == 1) {  // of the rounded weights: half the instructions, and they add up to 1
 #pragma unroll
-            for (int j = 0; j < 8; j += 2) sum = __builtin_amdgcn_fdot2(half2v{pw[t][0][j], pw[t][0][j + 1]}, half2v{(_Float16)1.f, (_Float16)1.f}, sum, false);
-          } else {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) sum += y[j];
-          }
+          for (int j = 0; j < 8; ++j) sum += y[j];  // not of the rounded weights: where V's pages are far apart, those of a small page may all be 0 in fp16
           l += sum * inv[t];
         }
 #pragma unroll

@@ -499,3 +499,21 @@ def test_two_calls_at_once_and_a_workspace_of_the_caller():
     for i in range(2):
         for o in outs[i]:
             assert torch.equal(o, refs[i])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("news", [[3, 1], [120, 1], [40, 100]])
+@pytest.mark.parametrize("apart", [(-100, -6), (-30, 0), (-14, 2), (-6, 0), (-90, 30)])
+def test_attention_over_pages_of_small_or_no_values(apart, news, dtype):
+    """Pages of V that hold zeros or much smaller values than others have their full share of the weights: in front of the others, behind them, in turn."""
+    rng = np.random.default_rng(news[0] - apart[0])
+    P = 32 if apart[0] == -30 else 16
+    for small in (lambda j: j < 4, lambda j: j >= 4, lambda j: j % 2 == 0):
+        pool = Pool(rng, [150, 100], P, heads=1, stale=False)
+        for b in (0, 1):
+            for j in range(-(-int(pool.lens[b]) // P)):
+                k, v = (rng.normal(size=(1, P, 1, 128)) for _ in range(2))
+                v = v * 0.0 if small(j) and apart[0] == -100 else v * 2.0 ** apart[0 if small(j) else 1]
+                pool.store.write(k, v, [int(pool.table[b, j]) * P + i for i in range(P)])
+        pool.upload()
+        attend(pool, rng, news, 3, dtype)
