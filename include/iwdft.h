@@ -365,7 +365,7 @@ int iwdft_pages_resize(int32_t page_tokens, int32_t n_pages, int32_t max_pages, 
 int iwdft_pages_resize_bytes(int32_t batch, int32_t n_slots, size_t* workspace_bytes);
 
 /* New tokens into the pages of layers layer .. layer + n_layers - 1.  d_k, d_v: [n_layers][n_tokens][n_kv_heads][head_dim], kv_dtype.  A page's new tokens
- * stand behind each other in d_slots, in order (rows without a slot may lie between), and continue what the page holds: the page's tokens before the first
+ * stand behind each other in d_slots, in order (rows without a slot may lie between, none of another page), and continue what the page holds: the page's tokens before the first
  * new one are taken to be there, a page whose first slot is written starts afresh.  No slot may come twice. */
 int iwdft_pages_write(const iwdft_pages_desc* desc, int32_t layer, int32_t n_layers, const void* d_k, const void* d_v, const int32_t* d_slots, int32_t n_tokens,
                       void* d_values, int32_t* d_exponents, void* hip_stream);

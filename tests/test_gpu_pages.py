@@ -517,3 +517,176 @@ def test_attention_over_pages_of_small_or_no_values(apart, news, dtype):
                 pool.store.write(k, v, [int(pool.table[b, j]) * P + i for i in range(P)])
         pool.upload()
         attend(pool, rng, news, 3, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("news", [[2], [70]])
+def test_attention_of_queries_of_all_sizes(news, dtype):
+    """Channels of q from 2^-30 of the largest one on, rows of zeros, and the largest channel over a column of K that is zero.  Beside what `near` allows, a
+    score errs by 2^-22 of the row's largest |q| (fp32, two fp16 parts: 2^-39) times sum |k|: added to `reach` in units of its factor."""
+    rng = np.random.default_rng(21)
+    heads, G = 2, 2
+    pool = Pool(rng, [130], 32, heads=heads, scale=1.0)
+    pool.store.raw[:, :, :, 0, :, 5] = 0
+    pool.upload()
+    q = rng.normal(size=(1, news[0], heads * G, 128)) * 2.0 ** -rng.uniform(0, 30, size=(1, news[0], heads * G, 128))
+    q[0, 1] = 0.0
+    q[0, 0, :, 5] = 2.0 ** 6
+    q = dev(q).to(DT[dtype])
+    starts, out = np.array([0, news[0]], np.int32), torch.empty_like(q)
+    B.iwdft_pages_attn(pool.values, pool.exponents, q, dev(starts), pool.d_table, pool.d_lens, out)
+    ref, weight, reach, seen, floor = pool.store.attend(f64(q), starts, pool.table, pool.lens)
+    sums = np.array([np.abs(pool.store.sequence(0, h // G, 0, pool.table[0], 130)).sum(1).max() for h in range(heads * G)])
+    err = 2.0 ** (-22 if dtype == "bf16" else -39) * np.abs(f64(q)).max(-1) * sums / np.sqrt(128.0)
+    near(out, ref, weight, reach + err / (2.0 ** -22 + 140 * 2.0 ** -24), seen, floor, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("lens,news,G,kw", [
+    ([3000] + [20] * 70 + [1500], [1] * 72, 2, {}),                                   # more sequences than lanes, two of them cut
+    ([20] * 66 + [1500, 900], [1] * 66 + [70, 90], 2, {}),                             # ... beside prompts
+    ([2500, 700], [2, 1], 20, {}), ([3000], [1], 64, {}),                              # 33 to 64 rows
+    ([1500], [75], 7, dict(n_sink=3, n_recent=1300)),                                  # 525 rows of 8 layers and heads: the other way of joining
+    ([700, 40, 1300], [130, 1, 60], 3, {}),
+])
+def test_attention_schedules(lens, news, G, kw, dtype):
+    rng = np.random.default_rng(sum(lens) + G)
+    heads, layers = (2, 4) if lens == [1500] else (1, 2)
+    pool = Pool(rng, lens, 16 if G % 2 else 64, heads=heads, layers=layers + 1)
+    attend(pool, rng, news, G, dtype, layer=1, layers=layers, pad=2, **kw)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("P", [16, 64])
+def test_attention_with_pages_missing_everywhere(P, dtype):
+    rng = np.random.default_rng(P + 1)
+    pool = Pool(rng, [900, 300, 130, 64], P)
+    for b, n in enumerate(pool.lens):
+        gone = rng.random(-(-int(n) // P)) < 0.4
+        gone[0] = b == 0
+        pool.table[b, :len(gone)][gone] = rng.choice([-1, -2 ** 31, 2 ** 31 - 1, pool.store.raw.shape[1]], size=int(gone.sum()))
+    pool.table[3] = -1
+    pool.upload()
+    for kw in ({}, dict(n_sink=20, n_recent=100)):
+        attend(pool, rng, [90, 1, 70, 33], 2, dtype, pad=1, **kw)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_write_past_rows_of_nothing(dtype):
+    """Pages' new tokens with any number of rows without a slot between them, in front and behind; runs that end with a segment of the slots."""
+    rng = np.random.default_rng(23)
+    for P, gaps in ((16, (1, 2, 600)), (128, (1, 63, 64, 65, 511, 512, 513, 1100))):
+        pool = Pool(rng, [5 * P, 3 * P], P, heads=2)
+        parts = [slots_of(pool, [(0, 3, 2 * P)]), slots_of(pool, [(0, 2 * P + 3, 1)]), slots_of(pool, [(0, 2 * P + 4, P)]), slots_of(pool, [(1, P - 1, 1)]),
+                 slots_of(pool, [(1, P, P)]), slots_of(pool, [(0, 3 * P + 4, 7)])]
+        for gap, those in [(gap, those) for gap in gaps for those in (parts[:-1], parts[-1:])]:  # the last part continues a page that others follow: a call of its own
+            slots = []
+            for part in those:
+                cut = int(rng.integers(0, len(part) + 1))
+                slots += part[:cut] + [-1] * gap + part[cut:]
+            n = len(slots)
+            k, v = (rng.normal(size=(1, n, 2, 128)) * 2.0 ** rng.integers(-3, 6, size=(1, n, 1, 1)) for _ in range(2))
+            dk, dv = dev(k).to(DT[dtype]), dev(v).to(DT[dtype])
+            B.iwdft_pages_write(pool.values, pool.exponents, dk, dv, dev(np.asarray(slots, np.int32)))
+            # the oracle takes a page's runs one after the other; each call here continues what the last one left
+            keep = [i for i, s in enumerate(slots) if s >= 0]
+            runs, at = [], 0
+            while at < len(keep):
+                end = at + 1
+                while end < len(keep) and keep[end] == keep[end - 1] + 1:
+                    end += 1
+                runs.append(keep[at:end])
+                at = end
+            for run in runs:
+                pool.store.write(f64(dk)[:, run], f64(dv)[:, run], [slots[i] for i in run])
+            same_pool(pool)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_prompts_beside_single_tokens_in_a_captured_graph(dtype):
+    """Lengths and starts change between replays; the workspace is the graph's own; eager work between."""
+    rng = np.random.default_rng(24)
+    pool = Pool(rng, [1400, 900, 30], 32, heads=2)
+    q = torch.randn((1, 160, 4, 128), device=DEV).to(DT[dtype])
+    starts, lens = dev(np.array([0, 120, 121, 122], np.int32)), pool.d_lens.clone()
+    out, ref = torch.zeros_like(q), torch.zeros_like(q)
+    call = lambda o: B.iwdft_pages_attn(pool.values, pool.exponents, q, starts, pool.d_table, lens, o, n_sink=4, n_recent=1000)  # noqa: E731
+    call(ref)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        call(out)
+    for new_lens, new_starts in (([1400, 900, 30], [0, 120, 121, 122]), ([130, 900, 5], [0, 1, 120, 125]), ([0, 0, 0], [0, 0, 0, 0]), ([1400, 900, 30], [0, 7, 107, 137])):
+        lens.copy_(dev(np.array(new_lens, np.int32))), starts.copy_(dev(np.array(new_starts, np.int32)))
+        q.normal_()
+        ref.fill_(3.0)
+        call(ref)
+        out.fill_(3.0)
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, ref) and (out[:, new_starts[-1]:] == 3.0).all()
+        assert torch.isfinite(out.float()).all() and (out[:, :new_starts[-1]] != 3.0).any() == (new_starts[-1] > 0)
+
+
+def test_calls_on_another_stream():
+    """Everything on a stream of the caller's, given as such or as a number; arrays that are allocated for the call follow it."""
+    rng = np.random.default_rng(25)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    c, d = (B.PagedCache(1, 300, 2, 4, 128, torch.bfloat16, 2, 4000, 32, DEV) for _ in range(2))
+    want = dev(np.array([3000, 50], np.int32))
+    k, v, q = (torch.randn((1, 3050, h, 128), device=DEV).to(torch.bfloat16) for h in (2, 2, 4))
+    K, V = (torch.empty((1, 2, 2, 100, 128), dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    torch.cuda.synchronize()
+    starts, slots = c.resize(want, 3050, stream=side)
+    c.write(k, v, slots, stream=side.cuda_stream)
+    out = c.attend(q, starts, stream=side)
+    got = c.read(100, stream=side.cuda_stream)
+    s2, sl2 = d.resize(want, 3050)
+    d.write(k, v, sl2)
+    ref = d.attend(q, s2)
+    K, V = d.read(100)
+    torch.cuda.synchronize()
+    assert torch.equal(out, ref) and torch.equal(got[0], K) and torch.equal(got[1], V) and torch.equal(c.values, d.values) and torch.equal(slots, sl2)
+    del rng
+
+
+def test_the_binding_refuses_what_does_not_fit_on_the_gpu():
+    z = lambda *s, dtype=torch.int32, device=DEV: torch.zeros(s, dtype=dtype, device=device)  # noqa: E731
+    f = torch.float32
+    values, exponents = z(2, 4, 2, 2, 32 * 128, dtype=torch.uint8), z(2, 4, 2, 2)
+    k, q, table, lens, starts, slots = z(1, 3, 2, 128, dtype=f), z(1, 3, 4, 128, dtype=f), z(2, 4), z(2), z(3), z(3)
+    kv = z(1, 2, 2, 5, 128, dtype=f)
+    calls = {
+        "write": (B.iwdft_pages_write, dict(values=values, exponents=exponents, k=k, v=k.clone(), slots=slots - 1)),
+        "attn": (B.iwdft_pages_attn, dict(values=values, exponents=exponents, q=q, starts=starts, table=table, lens=lens, out=q.clone())),
+        "read": (B.iwdft_pages_read, dict(values=values, exponents=exponents, table=table, lens=lens, K=kv, V=kv.clone())),
+        "resize": (B.iwdft_pages_resize, dict(want=lens.clone(), table=table, lens=lens, free=z(5), starts=starts, slots=slots, page_tokens=32)),
+    }
+    for name, (call, good) in calls.items():
+        call(**good)
+        for arg, t in good.items():
+            if not isinstance(t, torch.Tensor):
+                continue
+            bad = [t.cpu(), t.to(torch.float64) if t.dtype != torch.uint8 else t.to(torch.int8), t[..., :-1], t.unsqueeze(0)]
+            if t.numel() > 1 and t.dim() == 1:
+                bad.append(torch.stack([t, t], 1)[:, 0])
+            if t.dim() > 1:
+                bad.append(t.transpose(0, 1).contiguous().transpose(0, 1) if t.shape[0] > 1 and t.shape[1] > 1 else torch.stack([t, t], -1)[..., 0])
+            for x in bad:
+                if name == "resize" and arg in ("free", "slots") and x.dim() == 1 and x.is_contiguous() and x.dtype == torch.int32 and x.is_cuda:
+                    continue  # any length will do
+                with pytest.raises((ValueError, B.IwdftError)):
+                    call(**{**good, arg: x})
+    for name in ("write", "attn", "read"):
+        call, good = calls[name]
+        for layer in (-1, 2, 2 ** 31 - 1):
+            with pytest.raises(B.IwdftError):
+                call(**good, layer=layer)
+    with pytest.raises(ValueError):
+        B.iwdft_pages_attn(**calls["attn"][1], workspace=torch.empty(10, dtype=torch.uint8))
+    with pytest.raises(B.IwdftError):
+        B.iwdft_pages_attn(**{**calls["attn"][1], "out": q})  # in place
+    with pytest.raises(B.IwdftError):
+        B.iwdft_pages_attn(**calls["attn"][1], n_sink=2)
+    torch.cuda.synchronize()
