@@ -74,7 +74,7 @@ struct ResizeArgs {
   int32_t *table, *lens, *free, *starts, *slots;
   int32_t* scratch;  // 4 + 3 * batch ints, or null where one workgroup does it all
 };
-constexpr int kResizeThreads = 1024;
+constexpr int kResizeThreads = 1024, kResizeSmallThreads = 256;  // up to so many sequences: fewer waves, whose sums are joined sooner
 // One launch, without scratch, up to so many sequences and slots; one wave's scans up to kResizeWaveBatch sequences.
 constexpr int kResizeOneBatch = 1024, kResizeOneSlots = 2048, kResizeWaveBatch = 64;
 hipError_t launch_pages_resize(const ResizeArgs& a, hipStream_t st);

@@ -20,7 +20,7 @@ struct ResizeState {
 
 // Sums of N numbers >= 0 over the threads before this one and over all threads of the workgroup; every thread calls it.  In two halves of 16 bits, whose sums over
 // a wave fit 32.
-template <int N>
+template <int THREADS, int N>
 __device__ __forceinline__ void sums_before(const int (&x)[N], long long (&before)[N], long long (&all)[N], long long (*lds)[N]) {
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
 #pragma unroll
@@ -37,7 +37,7 @@ __device__ __forceinline__ void sums_before(const int (&x)[N], long long (&befor
   for (int i = 0; i < N; ++i) {
     long long sum = 0, mine = 0;
 #pragma unroll 4
-    for (int w = 0; w < kResizeThreads / kWave; ++w) {
+    for (int w = 0; w < THREADS / kWave; ++w) {
       mine = w == wave ? sum : mine;
       sum += lds[w][i];
     }
@@ -106,10 +106,10 @@ __device__ void resize_fill(const ResizeArgs& a, const Fill& f, int at, int step
 }
 
 // ONE: up to kResizeOneBatch sequences and kResizeOneSlots slots, everything in this launch.  A decode step's call is the chain of loads, sums and
-// stores of one workgroup.  Otherwise resize_fill_kernel follows.
-template <bool ONE>
-__global__ __launch_bounds__(kResizeThreads) void resize_kernel(ResizeArgs a) {
-  __shared__ long long lds3[kResizeThreads / kWave][3], lds2[kResizeThreads / kWave][2], lds1[kResizeThreads / kWave][1];
+// stores of one workgroup.  Otherwise resize_fill_kernel follows.  THREADS: 256 sequences, 5.6 us with 1024 threads, whose 16 waves join their sums, 2.2 with 256.
+template <bool ONE, int THREADS>
+__global__ __launch_bounds__(THREADS) void resize_kernel(ResizeArgs a) {
+  __shared__ long long lds3[THREADS / kWave][3], lds2[THREADS / kWave][2], lds1[THREADS / kWave][1];
   __shared__ int32_t keep[ONE ? 4 * kResizeOneBatch : 1];
   int32_t *have = ONE ? keep : a.scratch + 4, *need = have + (ONE ? kResizeOneBatch : a.batch), *gone = need + (ONE ? kResizeOneBatch : a.batch);
   int32_t* starts = ONE ? gone + kResizeOneBatch : a.starts;
@@ -118,30 +118,30 @@ __global__ __launch_bounds__(kResizeThreads) void resize_kernel(ResizeArgs a) {
   const auto pages_gone = [&](const Change& c) { return max(0, page_count(c.have, a.logP) - page_count(c.want, a.logP)); };
 
   long long given = 0;  // pages given back by all: they serve this call too
-  if (!ONE && a.batch > kResizeThreads)
-    for (int b0 = 0; b0 < a.batch; b0 += kResizeThreads) {
+  if (!ONE && a.batch > THREADS)
+    for (int b0 = 0; b0 < a.batch; b0 += THREADS) {
       const int b = b0 + tid, x[1] = {b < a.batch ? pages_gone(change_of(a, b)) : 0};
       long long before[1], all[1];
-      sums_before(x, before, all, lds1);
+      sums_before<THREADS>(x, before, all, lds1);
       given += all[0];
     }
 
   long long asked = 0, fresh = 0, back = 0;
   int taken = 0, total = 0, released = 0;
-  for (int b0 = 0; b0 < a.batch; b0 += kResizeThreads) {
+  for (int b0 = 0; b0 < a.batch; b0 += THREADS) {
     const int b = b0 + tid;
     Change c{0, 0};
     if (b < a.batch) c = change_of(a, b);
     const bool up = c.want > c.have;
     const int x[3] = {pages_gone(c), up ? page_count(c.want, a.logP) - page_count(c.have, a.logP) : 0, up ? c.want - c.have : 0};
     long long before[3], all[3];
-    sums_before(x, before, all, lds3);
-    released = (int)min(a.batch > kResizeThreads ? given : all[0], (long long)a.n_pages);  // more only if two sequences held the same page
+    sums_before<THREADS>(x, before, all, lds3);
+    released = (int)min(a.batch > THREADS ? given : all[0], (long long)a.n_pages);  // more only if two sequences held the same page
     const long long pages_to = asked + before[1] + x[1], tokens_to = fresh + before[2] + x[2];
     const bool ok = up && tokens_to <= a.n_slots && (x[1] == 0 || pages_to <= (long long)count + released);
     const int in[2] = {ok ? x[1] : 0, ok ? x[2] : 0};
     long long in_before[2], in_all[2];
-    sums_before(in, in_before, in_all, lds2);
+    sums_before<THREADS>(in, in_before, in_all, lds2);
     if (b < a.batch) {
       have[b] = c.have;
       need[b] = (int)min(pages_to - x[1], (long long)0x7fffffff);  // of admitted sequences: whoever asked before them got it
@@ -160,7 +160,7 @@ __global__ __launch_bounds__(kResizeThreads) void resize_kernel(ResizeArgs a) {
   if constexpr (ONE) {
     __threadfence_block();
     __syncthreads();
-    resize_fill(a, Fill{have, a.lens, need, gone, starts, {count, released, taken, total}}, tid, kResizeThreads);
+    resize_fill(a, Fill{have, a.lens, need, gone, starts, {count, released, taken, total}}, tid, THREADS);
   }
 }
 
@@ -194,17 +194,18 @@ __global__ __launch_bounds__(256) void resize_wave_kernel(ResizeArgs a) {
   resize_fill(a, Fill{keep[0], keep[1], keep[2], keep[3], keep[4], state}, threadIdx.x, 256);
 }
 
-// Every slot looks its sequence up: in LDS where the starts fit (256 sequences, 280000 slots: 5.9 us with eight dependent loads from memory, 5.5 so).
+// Every slot looks its sequence up, in LDS where the sequences fit (256 sequences, 280000 slots: 5.9 us with eight dependent loads from memory, 5.2 with the starts in LDS,
+// 4.8 with what is looked up there beside them).
 __global__ __launch_bounds__(256) void resize_fill_kernel(ResizeArgs a) {
-  __shared__ int32_t starts[kResizeOneBatch];
+  __shared__ int32_t keep[3][kResizeOneBatch];
   const int32_t* s = a.scratch;
-  const bool fits = a.batch <= kResizeOneBatch;
-  if (fits) {
-    for (int b = threadIdx.x; b < a.batch; b += 256) starts[b] = a.starts[b];
+  Fill f{s + 4, a.lens, s + 4 + a.batch, s + 4 + 2 * a.batch, a.starts, {s[0], s[1], s[2], s[3]}};
+  if (a.batch <= kResizeOneBatch) {
+    for (int b = threadIdx.x; b < a.batch; b += 256) keep[0][b] = f.have[b], keep[1][b] = f.need[b], keep[2][b] = f.starts[b];
+    f.have = keep[0], f.need = keep[1], f.starts = keep[2];
     __syncthreads();
   }
-  resize_fill(a, Fill{s + 4, a.lens, s + 4 + a.batch, s + 4 + 2 * a.batch, fits ? starts : a.starts, {s[0], s[1], s[2], s[3]}}, blockIdx.x * 256 + threadIdx.x,
-              gridDim.x * 256);
+  resize_fill(a, f, blockIdx.x * 256 + threadIdx.x, gridDim.x * 256);
 }
 
 // ------------------------------------------------------------------------------------------------ writing
@@ -522,11 +523,14 @@ hipError_t launch_pages_resize(const ResizeArgs& a, hipStream_t st) {
     resize_wave_kernel<<<1, 256, 0, st>>>(a);
     return hipGetLastError();
   }
+  const bool small = a.batch <= kResizeSmallThreads;
   if (!a.scratch) {
-    resize_kernel<true><<<1, kResizeThreads, 0, st>>>(a);
+    if (small) resize_kernel<true, kResizeSmallThreads><<<1, kResizeSmallThreads, 0, st>>>(a);
+    else resize_kernel<true, kResizeThreads><<<1, kResizeThreads, 0, st>>>(a);
     return hipGetLastError();
   }
-  resize_kernel<false><<<1, kResizeThreads, 0, st>>>(a);
+  if (small) resize_kernel<false, kResizeSmallThreads><<<1, kResizeSmallThreads, 0, st>>>(a);
+  else resize_kernel<false, kResizeThreads><<<1, kResizeThreads, 0, st>>>(a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const int64_t items = std::max<int64_t>(a.n_slots, (int64_t)a.batch * 16);
