@@ -690,3 +690,21 @@ def test_the_binding_refuses_what_does_not_fit_on_the_gpu():
     with pytest.raises(B.IwdftError):
         B.iwdft_pages_attn(**calls["attn"][1], n_sink=2)
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("batch", [65, 256, 257, 1024])
+@pytest.mark.parametrize("n_slots", [900, 2049])
+def test_tables_of_every_kind_of_launch(batch, n_slots):
+    """Sequences by one wave, 256 and 1024 threads, in one launch and two; a call that takes what it gives back."""
+    check_resize(np.random.default_rng(batch + n_slots), batch, 6, 16, 2 * batch, n_slots, 5, 60)
+    rng = np.random.default_rng(batch)
+    table, lens = np.full((batch, 6), -1, np.int32), np.zeros(batch, np.int32)
+    free = np.concatenate([[batch], rng.permutation(batch)]).astype(np.int32)
+    arrays = [dev(x) for x in (table, lens, free)]
+    for want in (np.where(np.arange(batch) % 2, 32, 0), np.where(np.arange(batch) % 2, 0, 32), np.full(batch, 16)):
+        want = np.where(np.cumsum(want) <= n_slots, want, 0).astype(np.int32)
+        d_starts, d_slots = (torch.full((n,), 77, dtype=torch.int32, device=DEV) for n in (batch + 1, n_slots))
+        B.iwdft_pages_resize(dev(want), *arrays, d_starts, d_slots, 16)
+        starts, slots = po.resize(want, table, lens, free, n_slots, 16)
+        for got, ref in zip(arrays + [d_starts, d_slots], (table, lens, free, starts, slots)):
+            assert np.array_equal(got.cpu().numpy(), ref)
