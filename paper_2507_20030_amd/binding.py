@@ -429,19 +429,18 @@ def _expect(name: str, t: torch.Tensor, dtype, shape, device) -> None:
 
 
 def _pool_sizes(values: torch.Tensor, exponents: torch.Tensor):
-    """(device, layers, pages, KV heads, page tokens); the device is a GPU."""
-    shape = values.shape
+    """(index of the GPU, layers, pages, KV heads, page tokens)."""
+    shape, index = values.shape, values.get_device()
     if len(shape) != 5 or shape[3] != 2 or shape[4] % 128:
         raise ValueError(f"values has shape {tuple(shape)}, not (layers, pages, heads, 2, 128 * page tokens)")
-    device = values.device
-    if device.type != "cuda":
+    if index < 0:
         raise ValueError("values must be device memory")
     n_layers, n_pages, heads, _, row = shape
     if not (values.dtype is torch.uint8 and values.is_contiguous() and exponents.dtype is torch.int32 and exponents.shape == (n_layers, n_pages, heads, 2)
-            and exponents.device == device and exponents.is_contiguous()):
-        _expect("values", values, torch.uint8, shape, device)
-        _expect("exponents", exponents, torch.int32, (n_layers, n_pages, heads, 2), device)
-    return device, n_layers, n_pages, heads, row // 128
+            and exponents.get_device() == index and exponents.is_contiguous()):
+        _expect("values", values, torch.uint8, shape, values.device)
+        _expect("exponents", exponents, torch.int32, (n_layers, n_pages, heads, 2), values.device)
+    return index, n_layers, n_pages, heads, row // 128
 
 
 def _kv_dtype(name: str, t: torch.Tensor):
@@ -479,24 +478,24 @@ def _scratch(n_bytes: int, device: torch.device, stream, workspace):
 # The calls check their tensors in one expression -- a decode step makes one of these calls per layer -- and say what is wrong where it fails.
 def iwdft_pages_resize(want, table, lens, free, starts, slots, page_tokens: int, stream=None, workspace=None) -> None:
     """Brings the sequences to want[b] tokens (negative: as they are): table, lens, free, starts and slots are brought up to date."""
-    device, shape, i32 = table.device, table.shape, torch.int32
-    if len(shape) != 2 or device.type != "cuda":
-        raise ValueError(f"table must be a device tensor [batch, max_pages], not {tuple(shape)} on {device}")
+    index, shape, i32 = table.get_device(), table.shape, torch.int32
+    if len(shape) != 2 or index < 0:
+        raise ValueError(f"table must be a device tensor [batch, max_pages], not {tuple(shape)} on {table.device}")
     batch, max_pages = shape
     n_free, n_slots = free.numel(), slots.numel()
     if not (table.dtype is want.dtype is lens.dtype is free.dtype is starts.dtype is slots.dtype is i32
-            and device == want.device == lens.device == free.device == starts.device == slots.device
+            and index == want.get_device() == lens.get_device() == free.get_device() == starts.get_device() == slots.get_device()
             and want.shape == lens.shape == (batch,) and starts.shape == (batch + 1,) and free.dim() == slots.dim() == 1
             and table.is_contiguous() and want.is_contiguous() and lens.is_contiguous() and free.is_contiguous() and starts.is_contiguous()
             and slots.is_contiguous()):
         for name, t, size in (("table", table, shape), ("want", want, (batch,)), ("lens", lens, (batch,)), ("free", free, (n_free,)),
                               ("starts", starts, (batch + 1,)), ("slots", slots, (n_slots,))):
-            _expect(name, t, i32, size, device)
-    index = device.index
-    if index != torch.cuda.current_device():
+            _expect(name, t, i32, size, table.device)
+    if index != torch._C._cuda_getDevice():
         with torch.cuda.device(index):
             return iwdft_pages_resize(want, table, lens, free, starts, slots, page_tokens, stream, workspace)
-    ws = _scratch(_resize_bytes(batch, n_slots), device, stream, workspace)
+    need = _resize_bytes(batch, n_slots)
+    ws = _scratch(need, table.device, stream, workspace) if need or workspace is not None else None
     rc = load_library().iwdft_pages_resize(page_tokens, n_free - 1, max_pages, want.data_ptr(), batch, table.data_ptr(), lens.data_ptr(), free.data_ptr(),
                                            starts.data_ptr(), slots.data_ptr(), n_slots, ws.data_ptr() if ws is not None else None,
                                            ws.nbytes if ws is not None else 0, _stream_of(stream, index))
@@ -506,17 +505,17 @@ def iwdft_pages_resize(want, table, lens, free, starts, slots, page_tokens: int,
 
 def iwdft_pages_write(values, exponents, k, v, slots, layer: int = 0, stream=None) -> None:
     """k, v [layers written, tokens, KV heads, 128] into layers layer, layer + 1, ... at slots."""
-    device, n_layers, n_pages, heads, P = _pool_sizes(values, exponents)
+    index, n_layers, n_pages, heads, P = _pool_sizes(values, exponents)
     dtype, n, shape = _kv_dtype("k", k), slots.numel(), k.shape
-    if not (slots.dtype is torch.int32 and slots.dim() == 1 and v.dtype is dtype and device == slots.device == k.device == v.device
+    if not (slots.dtype is torch.int32 and slots.dim() == 1 and v.dtype is dtype and index == slots.get_device() == k.get_device() == v.get_device()
             and shape == v.shape and shape[1:] == (n, heads, 128) and slots.is_contiguous() and k.is_contiguous() and v.is_contiguous()):
+        device = values.device
         _expect("slots", slots, torch.int32, (n,), device)
         _expect("k", k, dtype, (None, n, heads, 128), device)
         _expect("v", v, dtype, shape, device)
     if shape[0] == 0:
         return
-    index = device.index
-    if index != torch.cuda.current_device():
+    if index != torch._C._cuda_getDevice():
         with torch.cuda.device(index):
             return iwdft_pages_write(values, exponents, k, v, slots, layer, stream)
     rc = load_library().iwdft_pages_write(_pages_ref(n_layers, n_pages, heads, heads, 128, P, 1, dtype), layer, shape[0], k.data_ptr(), v.data_ptr(),
@@ -528,12 +527,14 @@ def iwdft_pages_write(values, exponents, k, v, slots, layer: int = 0, stream=Non
 def iwdft_pages_attn(values, exponents, q, starts, table, lens, out, layer: int = 0, n_sink: int = 0, n_recent: int = 0, scale: float = 0.0, stream=None,
                      workspace=None) -> None:
     """q, out [layers, tokens, query heads, 128]: the new tokens' attention over their sequences in layers layer, layer + 1, ..."""
-    device, n_layers, n_pages, heads, P = _pool_sizes(values, exponents)
+    index, n_layers, n_pages, heads, P = _pool_sizes(values, exponents)
     dtype, shape, size = _kv_dtype("q", q), q.shape, table.shape
     if not (len(shape) == 4 and len(size) == 2 and shape[3] == 128 and out.dtype is dtype and shape == out.shape
             and starts.dtype is table.dtype is lens.dtype is torch.int32 and lens.shape == size[:1] and starts.shape == (size[0] + 1,)
-            and device == q.device == out.device == starts.device == table.device == lens.device and q.is_contiguous() and out.is_contiguous()
+            and index == q.get_device() == out.get_device() == starts.get_device() == table.get_device() == lens.get_device()
+            and q.is_contiguous() and out.is_contiguous()
             and starts.is_contiguous() and table.is_contiguous() and lens.is_contiguous()):
+        device = values.device
         _expect("q", q, dtype, (None, None, None, 128), device)
         _expect("out", out, dtype, shape, device)
         _expect("table", table, torch.int32, (None, None), device)
@@ -543,12 +544,11 @@ def iwdft_pages_attn(values, exponents, q, starts, table, lens, out, layer: int 
     batch, max_pages = size
     if n == 0:
         return
-    index = device.index
-    if index != torch.cuda.current_device():
+    if index != torch._C._cuda_getDevice():
         with torch.cuda.device(index):
             return iwdft_pages_attn(values, exponents, q, starts, table, lens, out, layer, n_sink, n_recent, scale, stream, workspace)
     desc, need = _attn_sizes(n, batch, n_tokens, n_layers, n_pages, heads, n_q_heads, 128, P, max_pages, dtype)
-    ws = _scratch(need, device, stream, workspace) if need or workspace is not None else None
+    ws = _scratch(need, values.device, stream, workspace) if need or workspace is not None else None
     rc = load_library().iwdft_pages_attn(desc, layer, n, q.data_ptr(), starts.data_ptr(), n_tokens, table.data_ptr(), lens.data_ptr(), batch,
                                          values.data_ptr(), exponents.data_ptr(), out.data_ptr(), n_sink, n_recent, scale,
                                          ws.data_ptr() if ws is not None else None, ws.nbytes if ws is not None else 0, _stream_of(stream, index))
@@ -558,14 +558,16 @@ def iwdft_pages_attn(values, exponents, q, starts, table, lens, out, layer: int 
 
 def iwdft_pages_read(values, exponents, table, lens, K, V, layer: int = 0, stream=None) -> None:
     """K, V [layers, batch, KV heads, tokens, 128] (either may be None) from the first tokens of every sequence; 0 where it has fewer."""
-    device, n_layers, n_pages, heads, P = _pool_sizes(values, exponents)
+    index, n_layers, n_pages, heads, P = _pool_sizes(values, exponents)
     some = K if K is not None else V
     if some is None:
         return
     dtype, shape, size = _kv_dtype("K or V", some), some.shape, table.shape
     if not (len(size) == 2 and len(shape) == 5 and shape[1:3] == (size[0], heads) and shape[4] == 128 and table.dtype is lens.dtype is torch.int32
-            and lens.shape == size[:1] and device == table.device == lens.device == some.device and table.is_contiguous() and lens.is_contiguous()
-            and some.is_contiguous() and (V is None or (V.dtype is dtype and V.shape == shape and V.device == device and V.is_contiguous()))):
+            and lens.shape == size[:1] and index == table.get_device() == lens.get_device() == some.get_device() and table.is_contiguous()
+            and lens.is_contiguous() and some.is_contiguous()
+            and (V is None or (V.dtype is dtype and V.shape == shape and V.get_device() == index and V.is_contiguous()))):
+        device = values.device
         _expect("table", table, torch.int32, (None, None), device)
         _expect("lens", lens, torch.int32, size[:1], device)
         for name, t in (("K", K), ("V", V)):
@@ -573,8 +575,7 @@ def iwdft_pages_read(values, exponents, table, lens, K, V, layer: int = 0, strea
                 _expect(name, t, dtype, (shape[0], size[0], heads, shape[3] if len(shape) == 5 else None, 128), device)
     if shape[0] == 0:
         return
-    index = device.index
-    if index != torch.cuda.current_device():
+    if index != torch._C._cuda_getDevice():
         with torch.cuda.device(index):
             return iwdft_pages_read(values, exponents, table, lens, K, V, layer, stream)
     rc = load_library().iwdft_pages_read(_pages_ref(n_layers, n_pages, heads, heads, 128, P, size[1], dtype), layer, shape[0], table.data_ptr(), lens.data_ptr(),
