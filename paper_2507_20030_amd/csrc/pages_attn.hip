@@ -37,7 +37,7 @@ struct Weights {
 // ------------------------------------------------------------------------------------------------ sharing out the work
 // A block is `rows` consecutive (new token, query head of the KV head) pairs of a sequence; its tokens are cut into parts, one workgroup each, such that
 // all parts of a call hold about the same number of tiles and there are no more than `parts` of them, as many as the chip holds at a time (one more would run
-// alone in the end: 16 contexts of 4096 to 16384 tokens 90 us, with the blocks' last, shorter parts counted in 78).  Lengths live on the
+// alone in the end: 16 contexts of 4096 to 16384 tokens 90 us, with the blocks' last, shorter parts counted in 78, 71 with what is below).  Lengths live on the
 // device, so every wave works out the shares by itself, 64 sequences at a time: the launch only has to be large enough.
 // Short parts cost more in the join than the second workgroup on a CU gains: one token over 8192 tokens of 8 heads 15.0 us with parts of 4 tiles, 12.0 with 8,
 // over 16000 17.3 with 8 and 15.6 with 16.
@@ -895,7 +895,7 @@ __device__ __forceinline__ void join_rows(const PagesAttn& a, const PagesRows& w
 
 // ------------------------------------------------------------------------------------------------ launches
 // R: row tiles of few_rows (0: none), MANY: many_rows too.  A call that may have both kinds of sequences is one launch, the blocks of many rows first: the
-// others fill what these leave free in the end.  (Two 1000-token prompts beside six single tokens, windows: four launches 206 us, one and a join 181.)
+// others fill what these leave free in the end.  (Two 1000-token prompts beside six single tokens, windows: four launches 206 us, one and a join 181; 150 with what is below.)
 template <bool BF16, int R, bool MANY>
 __global__ __launch_bounds__(kWaves* kWave, BF16 ? (R <= 2 ? 2 : 1) : (R == 1 && !MANY ? 2 : 1)) void pages_attn_kernel(PagesAttn a) {
   uint32_t x = blockIdx.x;
