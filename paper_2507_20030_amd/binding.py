@@ -370,18 +370,14 @@ class Cache:
 # What include/iwdft.h says of the arrays; sizes come from the tensors' shapes:
 #   values uint8 [layers, pages, KV heads, 2, P * 128], exponents int32 [layers, pages, KV heads, 2], table int32 [batch, max_pages],
 #   lens int32 [batch], free int32 [1 + pages], starts int32 [batch + 1], slots int32 [tokens].
-@functools.lru_cache(maxsize=1024)
-def _pages_desc(n_layers, n_pages, n_kv_heads, n_q_heads, head_dim, page_tokens, max_pages, dtype):
-    return iwdft_pages_desc(n_layers, n_pages, n_kv_heads, n_q_heads, head_dim, page_tokens, max_pages, IWDFT_F32 if dtype == torch.float32 else IWDFT_BF16)
+def pages_desc(n_layers, n_pages, n_kv_heads, n_q_heads=None, head_dim=128, page_tokens=32, max_pages=1, dtype=torch.bfloat16) -> iwdft_pages_desc:
+    return iwdft_pages_desc(n_layers, n_pages, n_kv_heads, n_kv_heads if n_q_heads is None else n_q_heads, head_dim, page_tokens, max_pages,
+                            IWDFT_F32 if dtype == torch.float32 else IWDFT_BF16)
 
 
 @functools.lru_cache(maxsize=1024)
 def _pages_ref(*sizes):
-    return ctypes.byref(_pages_desc(*sizes))  # as the calls take it; keeps the descriptor
-
-
-def pages_desc(n_layers, n_pages, n_kv_heads, n_q_heads=None, head_dim=128, page_tokens=32, max_pages=1, dtype=torch.bfloat16) -> iwdft_pages_desc:
-    return _pages_desc(n_layers, n_pages, n_kv_heads, n_kv_heads if n_q_heads is None else n_q_heads, head_dim, page_tokens, max_pages, dtype)
+    return ctypes.byref(pages_desc(*sizes))  # as the calls take it; keeps a descriptor of its own, which no caller can change
 
 
 def _bytes_of(call, *args) -> int:

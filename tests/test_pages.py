@@ -181,3 +181,15 @@ def test_sizes_whose_counts_would_not_fit():
                        (lib.iwdft_pages_read, (wide, 0, 2 ** 20, FAKE, FAKE, 2 ** 30, 2 ** 30, FAKE, FAKE, FAKE, FAKE, None)),
                        (lib.iwdft_pages_read, (ctypes.byref(c_desc()), 0, 2, FAKE, FAKE, 2 ** 25, 1, FAKE, FAKE, FAKE, FAKE, None))):  # 2^27 waves of one token
         assert call(*args) == B.IWDFT_ERR_ARG, args
+
+
+def test_descriptors_are_the_callers_own():
+    """Changing the one that was handed out changes neither the next one nor what the calls take for the same sizes."""
+    sizes = dict(n_layers=1, n_pages=700, n_kv_heads=2, n_q_heads=4, head_dim=128, page_tokens=16, max_pages=512, dtype=torch.float32)
+    d = B.pages_desc(**sizes)
+    d.max_pages = 3
+    assert B.pages_desc(**sizes).max_pages == 512
+    ref = B._pages_ref(*sizes.values())
+    assert ref._obj.max_pages == 512 and B._attn_sizes(1, 1, 1, *sizes.values())[0]._obj.max_pages == 512
+    B.pages_desc(**sizes).kv_dtype = B.IWDFT_BF16
+    assert B._pages_ref(*sizes.values())._obj.kv_dtype == B.IWDFT_F32
