@@ -371,6 +371,8 @@ class Cache:
 #   values uint8 [layers, pages, KV heads, 2, P * 128], exponents int32 [layers, pages, KV heads, 2], table int32 [batch, max_pages],
 #   lens int32 [batch], free int32 [1 + pages], starts int32 [batch + 1], slots int32 [tokens].
 def pages_desc(n_layers, n_pages, n_kv_heads, n_q_heads=None, head_dim=128, page_tokens=32, max_pages=1, dtype=torch.bfloat16) -> iwdft_pages_desc:
+    if dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError("dtype must be float32 or bfloat16")
     return iwdft_pages_desc(n_layers, n_pages, n_kv_heads, n_kv_heads if n_q_heads is None else n_q_heads, head_dim, page_tokens, max_pages,
                             IWDFT_F32 if dtype == torch.float32 else IWDFT_BF16)
 

@@ -193,3 +193,9 @@ def test_descriptors_are_the_callers_own():
     assert ref._obj.max_pages == 512 and B._attn_sizes(1, 1, 1, *sizes.values())[0]._obj.max_pages == 512
     B.pages_desc(**sizes).kv_dtype = B.IWDFT_BF16
     assert B._pages_ref(*sizes.values())._obj.kv_dtype == B.IWDFT_F32
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.float64, torch.uint8])
+def test_descriptors_of_other_types_are_refused(dtype):
+    with pytest.raises(ValueError):
+        B.pages_desc(1, 4, 2, dtype=dtype)
