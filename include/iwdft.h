@@ -380,7 +380,7 @@ int iwdft_pages_write(const iwdft_pages_desc* desc, int32_t layer, int32_t n_lay
 int iwdft_pages_attn(const iwdft_pages_desc* desc, int32_t layer, int32_t n_layers, const void* d_q, const int32_t* d_starts, int32_t n_tokens,
                      const int32_t* d_table, const int32_t* d_lens, int32_t batch, const void* d_values, const int32_t* d_exponents, void* d_out, int32_t n_sink,
                      int32_t n_recent, float scale, void* d_workspace, size_t workspace_bytes, void* hip_stream);
-/* Its workspace (0: none), for calls on so many layers, sequences and rows.  Nothing in it outlives the call; calls that may overlap in time need one each. */
+/* Its workspace (0: none), for every call on up to so many layers, sequences and rows.  Nothing in it outlives the call; calls that may overlap in time need one each. */
 int iwdft_pages_attn_bytes(const iwdft_pages_desc* desc, int32_t n_layers, int32_t batch, int32_t n_tokens, size_t* workspace_bytes);
 
 /* The first n_tokens tokens of every sequence as iwdft_prefill takes them: d_K, d_V [n_layers][batch][n_kv_heads][n_tokens][head_dim], kv_dtype, 0 where a

@@ -662,6 +662,12 @@ int check_pages(const iwdft_pages_desc* d, int32_t layer, int32_t n_layers) {
     return fail(IWDFT_ERR_ARG, "%d layers of %d pages of %d heads: too many bytes", d->n_layers, d->n_pages, d->n_kv_heads);
   return rc;
 }
+int check_attn(const iwdft_pages_desc* d, int32_t layer, int32_t n_layers, int32_t batch, int32_t n_tokens) {
+  const int rc = check_pages(d, layer, n_layers);
+  if (rc == IWDFT_OK && (batch < 0 || batch > kMostCount || n_tokens < 0 || (double)n_tokens * d->n_q_heads * n_layers > kMostRows))
+    return fail(IWDFT_ERR_ARG, "batch = %d, n_tokens = %d out of range", batch, n_tokens);
+  return rc;
+}
 Pages pages_of(const iwdft_pages_desc& d, void* values, int32_t* exponents) {
   return Pages{d.n_pages, d.n_kv_heads, d.n_q_heads / d.n_kv_heads, log2_of(d.page_tokens), d.max_pages, (uint8_t*)values, exponents};
 }
@@ -1209,21 +1215,18 @@ int iwdft_pages_write(const iwdft_pages_desc* desc, int32_t layer, int32_t n_lay
 
 int iwdft_pages_attn_bytes(const iwdft_pages_desc* desc, int32_t n_layers, int32_t batch, int32_t n_tokens, size_t* workspace_bytes) {
   if (!workspace_bytes) return fail(IWDFT_ERR_ARG, "output pointer is NULL");
-  const int rc = check_pages(desc, 0, n_layers);
+  const int rc = check_attn(desc, 0, n_layers, batch, n_tokens);
   if (rc != IWDFT_OK) return rc;
-  if (batch < 0 || batch > kMostCount || n_tokens < 0 || (double)n_tokens * desc->n_q_heads * n_layers > kMostRows)
-    return fail(IWDFT_ERR_ARG, "batch = %d, n_tokens = %d out of range", batch, n_tokens);
-  *workspace_bytes = pages_attn_bytes(pages_of(*desc, nullptr, nullptr), batch, n_tokens, desc->kv_dtype == IWDFT_BF16);
+  *workspace_bytes = pages_attn_most_bytes(pages_of(*desc, nullptr, nullptr), batch, n_tokens, desc->kv_dtype == IWDFT_BF16);
   return IWDFT_OK;
 }
 
 int iwdft_pages_attn(const iwdft_pages_desc* desc, int32_t layer, int32_t n_layers, const void* d_q, const int32_t* d_starts, int32_t n_tokens,
                      const int32_t* d_table, const int32_t* d_lens, int32_t batch, const void* d_values, const int32_t* d_exponents, void* d_out, int32_t n_sink,
                      int32_t n_recent, float scale, void* d_workspace, size_t workspace_bytes, void* hip_stream) {
-  int rc = check_pages(desc, layer, n_layers);
-  size_t need = 0;
-  if (rc == IWDFT_OK) rc = iwdft_pages_attn_bytes(desc, n_layers, batch, n_tokens, &need);
+  const int rc = check_attn(desc, layer, n_layers, batch, n_tokens);
   if (rc != IWDFT_OK) return rc;
+  const size_t need = pages_attn_bytes(pages_of(*desc, nullptr, nullptr), batch, n_tokens, desc->kv_dtype == IWDFT_BF16);
   if (n_sink < 0 || n_recent < 0) return fail(IWDFT_ERR_ARG, "n_sink = %d, n_recent = %d: negative", n_sink, n_recent);
   if (n_sink > 0 && n_recent == 0) return fail(IWDFT_ERR_ARG, "n_sink = %d without a window: n_recent = 0 lets every row see all tokens before it", n_sink);
   if (scale != scale) return fail(IWDFT_ERR_ARG, "scale is NaN");

@@ -103,7 +103,8 @@ struct PagesAttn {
   const int32_t *starts, *table, *lens;
   PagesRows few, many;
 };
-size_t pages_attn_bytes(const Pages& S, int batch, int n_tokens, bool bf16);
+size_t pages_attn_bytes(const Pages& S, int batch, int n_tokens, bool bf16);       // of a call of these sizes
+size_t pages_attn_most_bytes(const Pages& S, int batch, int n_tokens, bool bf16);  // of any call of up to these sizes
 hipError_t launch_pages_attn(PagesAttn a, bool bf16, void* ws, hipStream_t st);
 
 }  // namespace iwdft

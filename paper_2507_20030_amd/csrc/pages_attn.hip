@@ -934,17 +934,17 @@ struct Launches {
   bool cut = false;   // blocks may be cut into parts
   size_t few_bytes = 0, bytes = 0;  // of the workspace
 };
+int few_tiles(int64_t usual, bool bf16, bool many) { return usual <= 16 ? 1 : usual <= 32 || !bf16 || many ? 2 : 4; }
+size_t few_bytes(int tiles) { return tiles == 1 ? kPartsBytes<Few<1>> : tiles == 2 ? kPartsBytes<Few<2>> : tiles == 4 ? kPartsBytes<Few<4>> : 0; }
+bool may_cut(const Pages& S) { return ((int64_t)S.max_pages << S.logP) > (int64_t)kShortTiles * 32; }
 Launches launches_of(const Pages& S, int batch, int n_tokens, bool bf16) {
   Launches n;
   const int64_t rows = (int64_t)n_tokens * S.G, average = S.G * (((int64_t)n_tokens + batch - 1) / batch);
   n.many = rows > kFewRows && n_tokens >= 2 * (int64_t)batch;  // about one token for each sequence: few_rows alone, whoever brings more
-  if (!n.many || batch > 1) {
-    const int64_t usual = average > kFewRows ? S.G : average;  // beside prompts: single tokens
-    n.few = usual <= 16 ? 1 : usual <= 32 || !bf16 || n.many ? 2 : 4;
-  }
-  n.cut = ((int64_t)S.max_pages << S.logP) > (int64_t)kShortTiles * 32;
+  if (!n.many || batch > 1) n.few = few_tiles(average > kFewRows ? S.G : average, bf16, n.many);  // beside prompts: single tokens
+  n.cut = may_cut(S);
   if (n.cut) {
-    n.few_bytes = n.few == 1 ? kPartsBytes<Few<1>> : n.few == 2 ? kPartsBytes<Few<2>> : n.few == 4 ? kPartsBytes<Few<4>> : 0;
+    n.few_bytes = few_bytes(n.few);
     n.bytes = n.few_bytes + (n.many ? kPartsBytes<Many> : 0);
   }
   return n;
@@ -983,6 +983,12 @@ hipError_t launch(const PagesAttn& a, hipStream_t st) {
 
 size_t pages_attn_bytes(const Pages& S, int batch, int n_tokens, bool bf16) {
   return batch == 0 || n_tokens == 0 ? 0 : launches_of(S, batch, n_tokens, bf16).bytes;
+}
+// The largest row tiles that few_rows takes in any of these calls, and many_rows, which one sequence with all rows takes.
+size_t pages_attn_most_bytes(const Pages& S, int batch, int n_tokens, bool bf16) {
+  if (batch == 0 || n_tokens == 0 || !may_cut(S)) return 0;
+  const int64_t rows = (int64_t)n_tokens * S.G;
+  return few_bytes(few_tiles(std::max<int64_t>(S.G, std::min<int64_t>(rows, kFewRows)), bf16, false)) + (rows > kFewRows ? kPartsBytes<Many> : 0);
 }
 
 hipError_t launch_pages_attn(PagesAttn a, bool bf16, void* ws, hipStream_t st) {

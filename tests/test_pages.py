@@ -199,3 +199,20 @@ def test_descriptors_are_the_callers_own():
 def test_descriptors_of_other_types_are_refused(dtype):
     with pytest.raises(ValueError):
         B.pages_desc(1, 4, 2, dtype=dtype)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("G", [1, 3, 4, 8, 16, 17, 33, 40, 64, 71])
+def test_attention_workspace_serves_smaller_calls(G, dtype):
+    """What is asked for the largest call never falls with its sizes and is enough for every smaller one: these get past the check of the workspace to the one
+    of its alignment."""
+    d = c_desc(n_kv_heads=8, n_q_heads=8 * G, max_pages=512, dtype=dtype)
+    lib, ref = B.load_library(), ctypes.byref(d)
+    tokens, batches = (1, 2, 3, 9, 15, 16, 17, 31, 32, 33, 63, 64, 65, 128, 129, 1000, 4096), (1, 2, 3, 4, 8, 16, 32, 33, 64, 256)
+    need = {(n, b): B.iwdft_pages_attn_bytes(d, 1, b, n) for n in tokens for b in batches}
+    for i, n in enumerate(tokens):
+        for j, b in enumerate(batches):
+            assert need[n, b] >= max(need[tokens[max(i - 1, 0)], b], need[n, batches[max(j - 1, 0)]])
+            for limit in (need[n, b], need[tokens[-1], batches[-1]]):
+                assert lib.iwdft_pages_attn(ref, 0, 1, FAKE, FAKE, n, FAKE, FAKE, b, FAKE, FAKE, 1 << 36, 0, 0, 0.0, FAKE + 16, limit, None) == B.IWDFT_ERR_ARG
+                assert "256-byte" in B.iwdft_last_error()
