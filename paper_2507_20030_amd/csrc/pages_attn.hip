@@ -12,6 +12,9 @@
 //  * the pages' exponents: that of K enters the score's factor; that of V joins the exponent of the weight.  With s_j the score times log2 e and
 //    eV_j the exponent of j's page, the weights in the sum are P_j = 2^(s_j + eV_j - m), m a running bound of s_j + eV_j, and the
 //    denominator is sum 2^(s_j - m) = sum P_j 2^-eV_j.  So no weight overflows fp16 or loses bits because its page is small.
+//  * the denominator where pages are far apart: of a page 2^130 smaller than another P_j is nothing in fp32, and 2^(s_j - m) may still be all of the
+//    denominator.  From the first tile with a page of |eV| > kNear on, a wave sums 2^(s_j - s), s the largest of them, and scales it by 2^(s - m).  m is then no
+//    less than any s_j + eV_j: the denominator lies between 2^-120 and 2^100 times the number of tokens, and is held 2^-4 times as large.
 //  * P_j is rounded to fp16 (11 bits; bf16 results have 8), for fp32 to two parts; the denominator and all sums are fp32.
 // The sums hold 2^lift P_j.  m grows where an exponent passes it by more than `slack`; 2^lift P_j <= 2^(slack + lift) < 65504 then.  bf16: lift 6,
 // slack 8, few rescalings.  fp32: lift 15, slack 0: fp16 ends at 2^-25, so weights err by 2^-40 of the largest one at least, and a page's
@@ -32,7 +35,23 @@ template <bool BF16>
 struct Weights {
   static constexpr float lift = BF16 ? 6.f : 15.f, slack = BF16 ? 8.f : 0.f;
   static constexpr int q_top = BF16 ? 7 : 14;  // rows of q: largest value in [2^q_top, 2^(q_top + 1))
+  static constexpr int down = (int)lift + 4;   // what the sums are larger than 2^4 times the denominator by
+  static constexpr float unit = 1.f / (float)(1 << down);
 };
+constexpr int kNear = 32;
+// x * 2^d.  In two factors: 2^d may be out of range where the product is not.
+__device__ __forceinline__ float times_power(float x, float d) {
+  const float k = ceilf(fmaxf(d, -1000.f));
+  return ldexpf(x * __builtin_amdgcn_exp2f(d - k), (int)k);
+}
+// Sum of 2^((x[j] - m) - d), j < 8; top: the largest x.  (x and m may be so large that m + d would be m.)
+__device__ __forceinline__ float sum_of_powers(const float* x, float top, float m, float d) {
+  const float t = fmaxf(top, -FLT_MAX);
+  float sum = 0.f;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) sum += __builtin_amdgcn_exp2f(x[j] - t);
+  return times_power(sum, (t - m) - d);
+}
 
 // ------------------------------------------------------------------------------------------------ sharing out the work
 // A block is `rows` consecutive (new token, query head of the KV head) pairs of a sequence; its tokens are cut into parts, one workgroup each, such that
@@ -229,15 +248,18 @@ __device__ __forceinline__ void load_channels(const void* p, int64_t i, float* f
 }
 
 template <bool BF16>
-__device__ __forceinline__ void store8(void* p, int64_t i, const float* y, float factor) {  // 8 channels
+__device__ __forceinline__ float result(float sum, float inv) { return sum * Weights<BF16>::unit * inv; }  // inv: of the denominator as it is held
+template <bool BF16>
+__device__ __forceinline__ void store8(void* p, int64_t i, const float* y, float inv) {  // 8 channels
   if constexpr (BF16) {
     uint32_t w[4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) w[j] = (uint32_t)f32_to_bf16(y[2 * j] * factor) | (uint32_t)f32_to_bf16(y[2 * j + 1] * factor) << 16;
+    for (int j = 0; j < 4; ++j) w[j] = (uint32_t)f32_to_bf16(result<true>(y[2 * j], inv)) | (uint32_t)f32_to_bf16(result<true>(y[2 * j + 1], inv)) << 16;
     *(uint4*)((uint16_t*)p + i) = make_uint4(w[0], w[1], w[2], w[3]);
   } else {
 #pragma unroll
-    for (int j = 0; j < 8; j += 4) *(float4*)((float*)p + i + j) = make_float4(y[j] * factor, y[j + 1] * factor, y[j + 2] * factor, y[j + 3] * factor);
+    for (int j = 0; j < 8; j += 4)
+      *(float4*)((float*)p + i + j) = make_float4(result<false>(y[j], inv), result<false>(y[j + 1], inv), result<false>(y[j + 2], inv), result<false>(y[j + 3], inv));
   }
 }
 
@@ -400,6 +422,7 @@ __device__ __forceinline__ void few_rows(const PagesAttn& a, uint32_t x0, uint32
       }
     }
 
+    int near = kNear;  // -1 from the first far page on
     for (int i = first; i < mine.to; i += W) {
       Data d = next;
       if (i + W < mine.to) {
@@ -428,6 +451,10 @@ __device__ __forceinline__ void few_rows(const PagesAttn& a, uint32_t x0, uint32
 #pragma unroll
           for (int p = 0; p < 2; ++p) kf[u][2 * p] = operand(d.k[u][p].x, d.k[u][p].y), kf[u][2 * p + 1] = operand(d.k[u][p].z, d.k[u][p].w);
       const float ev = (float)d.e.y;
+      const bool far = __builtin_expect(__any(abs(d.e.y) > near), 0);
+      near = far ? -1 : near;
+      const float slack = far ? -__builtin_inff() : Weights<BF16>::slack;
+      const int shift = far ? -1000 : -d.e.y - Weights<BF16>::down;  // of the weights' sum; far: it comes another way
       half8 pw[R][PARTS];
 #pragma unroll
       for (int r = 0; r < R; ++r) {
@@ -461,10 +488,11 @@ __device__ __forceinline__ void few_rows(const PagesAttn& a, uint32_t x0, uint32
         float top = sc[0];
 #pragma unroll
         for (int j = 1; j < 8; ++j) top = fmaxf(top, sc[j]);
-        if (__any(top > z.m + Weights<BF16>::slack)) {
-          top = fmaxf(z.m, max_over_16s(top));
-          const float fade = __builtin_amdgcn_exp2f(z.m - top);
-          z.m = top, z.l *= fade;
+        if (__any(top > z.m + slack)) {
+          const float up = fmaxf(z.m, max_over_16s(top)), fade = __builtin_amdgcn_exp2f(z.m - up);
+          if (__builtin_expect(far, 0)) z.l = times_power(z.l, z.m - up) + sum_of_powers(sc, top, up, ev + 4.f);
+          else z.l *= fade;
+          z.m = up;
 #pragma unroll
           for (int c = 0; c < 8; ++c) z.o[c] *= fade;
         }
@@ -472,7 +500,7 @@ __device__ __forceinline__ void few_rows(const PagesAttn& a, uint32_t x0, uint32
         const float ref = z.m - Weights<BF16>::lift;
 #pragma unroll
         for (int j = 0; j < 8; ++j) y[j] = __builtin_amdgcn_exp2f(sc[j] - ref), sum += y[j];
-        z.l += ldexpf(sum, -d.e.y);
+        z.l += ldexpf(sum, shift);
         to_halves<8, PARTS>(y, pw[r]);
       }
 #pragma unroll
@@ -534,9 +562,9 @@ __device__ __forceinline__ void few_rows(const PagesAttn& a, uint32_t x0, uint32
       float y[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, l = 0.f;
 #pragma unroll
       for (int v = 0; v < W; ++v) {
-        const float fade = __builtin_amdgcn_exp2f(st[v].x - m);
+        const float half = __builtin_amdgcn_exp2f(0.5f * (st[v].x - m)), fade = half * half;  // the denominator's share may need both factors
         const float4 lo = *(const float4*)(join[v][jr] + jc), hi = *(const float4*)(join[v][jr] + jc + 4);
-        l += st[v].y * fade;
+        l += st[v].y * half * half;
         y[0] += lo.x * fade, y[1] += lo.y * fade, y[2] += lo.z * fade, y[3] += lo.w * fade;
         y[4] += hi.x * fade, y[5] += hi.y * fade, y[6] += hi.z * fade, y[7] += hi.w * fade;
       }
@@ -571,7 +599,7 @@ __device__ __forceinline__ uint32_t many_rows(const PagesAttn& a, uint32_t x0, u
   const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int row = lane & 31, grp = lane >> 5;
   __shared__ __attribute__((aligned(16))) uint8_t kbuf[2][kTile * kHeadDim], vbuf[2][kTile * kHeadDim];
-  __shared__ float4 meta[2][kTile / 16];  // of the pages of 16 tokens each: scale 2^(eK - kQTop), eV, 2^-eV
+  __shared__ float4 meta[2][kTile / 16];  // of the pages of 16 tokens each: scale 2^(eK - kQTop), eV, 2^-eV in the denominator's unit, infinity where |eV| > kNear
 
   const Schedule<Geo> plan(a, a.many, lane);
   const uint32_t slices = (uint32_t)(a.n_layers * a.S.H), all = (uint32_t)plan.w.parts * slices;
@@ -636,6 +664,7 @@ __device__ __forceinline__ uint32_t many_rows(const PagesAttn& a, uint32_t x0, u
 #pragma unroll
       for (int i = 0; i < 16; ++i) o[c][i] = 0.f;
     float m = -FLT_MAX, l = 0.f;
+    float most = kLift + Weights<BF16>::slack;  // -infinity from the first far page on
 
     // a wave brings 16 tokens of a tile, which are in one page; that page is looked up a tile earlier
     const int32_t* table = a.table + (int64_t)at.b * a.S.max_pages;
@@ -661,10 +690,10 @@ __device__ __forceinline__ uint32_t many_rows(const PagesAttn& a, uint32_t x0, u
       ne = slice_exponents[head];
     };
     const auto store_tile = [&](int b) {
-      float4 e = make_float4(ldexpf(a.scale, ne.x - kQTop), (float)ne.y, ldexpf(1.f, -ne.y), 0.f);
+      float4 e = make_float4(ldexpf(a.scale, ne.x - kQTop), (float)ne.y, ldexpf(1.f, -ne.y - Weights<BF16>::down), abs(ne.y) > kNear ? __builtin_inff() : -__builtin_inff());
       if (none) {  // a page that is not there: scores of -infinity, weights and values of 0
         nk[0] = nk[1] = nv[0] = nv[1] = make_uint4(0, 0, 0, 0);
-        e = make_float4(0.f, -__builtin_inff(), 0.f, 0.f);
+        e = make_float4(0.f, -__builtin_inff(), 0.f, -__builtin_inff());
       }
       const int tok = lane >> 3, ch = lane & 7;
 #pragma unroll
@@ -721,7 +750,7 @@ __device__ __forceinline__ uint32_t many_rows(const PagesAttn& a, uint32_t x0, u
             }
         }
         const int base = t0 + 8 * grp;  // tokens of the lane: base + 16 t + j
-        float inv[4];
+        float inv[4], far = -__builtin_inff();
         float sc[32];  // exponents of the weights as they enter the sums: relative to m - lift
         const bool unset = m == -FLT_MAX;  // the row has seen nothing: relative to 0
         const float ref = (unset ? 0.f : m) - kLift;
@@ -729,7 +758,7 @@ __device__ __forceinline__ uint32_t many_rows(const PagesAttn& a, uint32_t x0, u
         for (int t = 0; t < 4; ++t) {
           const float4 e = meta[b][t];
           const float factor = e.x * q_scale, shift = e.y - ref;
-          inv[t] = e.z;
+          inv[t] = e.z, far = fmaxf(far, e.w);
 #pragma unroll
           for (int j = 0; j < 8; ++j) sc[8 * t + j] = acc[t / 2][8 * (t % 2) + j] * factor + shift;
         }
@@ -744,17 +773,29 @@ __device__ __forceinline__ uint32_t many_rows(const PagesAttn& a, uint32_t x0, u
         float top = sc[0];
 #pragma unroll
         for (int j = 1; j < 32; ++j) top = fmaxf(top, sc[j]);
-        if (__any(top > (unset ? -FLT_MAX : kLift + Weights<BF16>::slack))) {
+        if (__any(fmaxf(top, far) > (unset ? -FLT_MAX : most))) {
           top = fmaxf(top, __shfl_xor(top, 32));
           const bool first = unset && top >= -FLT_MAX;
           const float up = unset ? (first ? top - kLift : 0.f) : fmaxf(top - kLift, 0.f), fade = unset ? 1.f : __builtin_amdgcn_exp2f(-up);
-          m = first ? up : m + up, l *= fade;
+          m = first ? up : m + up, l = times_power(l, unset ? 0.f : -up);
 #pragma unroll
           for (int j = 0; j < 32; ++j) sc[j] -= up;
 #pragma unroll
           for (int c = 0; c < 4; ++c)
 #pragma unroll
             for (int j = 0; j < 16; ++j) o[c][j] *= fade;
+          if (__builtin_expect(__any(far > 0.f || most < 0.f), 0)) {
+            most = -__builtin_inff();
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+              const float ev = meta[b][t].y;
+              float s = sc[8 * t];
+#pragma unroll
+              for (int j = 1; j < 8; ++j) s = fmaxf(s, sc[8 * t + j]);
+              l += sum_of_powers(sc + 8 * t, s, 0.f, fmaxf(ev, -FLT_MAX) + (float)Weights<BF16>::down);
+              inv[t] = 0.f;  // not again below
+            }
+          }
         }
         half8 pw[4][PARTS];
 #pragma unroll
@@ -870,8 +911,8 @@ __device__ __forceinline__ void join_rows(const PagesAttn& a, const PagesRows& w
     float m = -FLT_MAX, l = 0.f;
     float2 o = make_float2(0.f, 0.f);
     const auto add = [&](float2 st, float2 v) {  // (reference, sum of weights), sum
-      const float up = fmaxf(m, st.x), f = __builtin_amdgcn_exp2f(m - up), g = __builtin_amdgcn_exp2f(st.x - up);
-      o.x = o.x * f + v.x * g, o.y = o.y * f + v.y * g, l = l * f + st.y * g, m = up;
+      const float up = fmaxf(m, st.x), f = __builtin_amdgcn_exp2f(0.5f * (m - up)), g = __builtin_amdgcn_exp2f(0.5f * (st.x - up));
+      o.x = o.x * (f * f) + v.x * (g * g), o.y = o.y * (f * f) + v.y * (g * g), l = l * f * f + st.y * g * g, m = up;
     };
 #pragma unroll 8
     for (int k = k0; k < at.np; k += dk) add(stat[(int64_t)k * BR], *(const float2*)(part + (int64_t)k * BR * kHeadDim));
@@ -888,8 +929,8 @@ __device__ __forceinline__ void join_rows(const PagesAttn& a, const PagesRows& w
     const float inv = l == 0.f ? 0.f : 1.f / l;
     const int layer = (int)((uint32_t)lh / (uint32_t)a.S.H), h = lh - layer * a.S.H, G = a.S.G, token = (int)((uint32_t)r / (uint32_t)G);
     const int64_t base = (((int64_t)layer * a.n_tokens + at.s.first + token) * (a.S.H * G) + h * G + r - token * G) * kHeadDim + 2 * lane;
-    if constexpr (BF16) *(uint32_t*)((uint16_t*)a.out + base) = (uint32_t)f32_to_bf16(o.x * inv) | (uint32_t)f32_to_bf16(o.y * inv) << 16;
-    else *(float2*)((float*)a.out + base) = make_float2(o.x * inv, o.y * inv);
+    if constexpr (BF16) *(uint32_t*)((uint16_t*)a.out + base) = (uint32_t)f32_to_bf16(result<true>(o.x, inv)) | (uint32_t)f32_to_bf16(result<true>(o.y, inv)) << 16;
+    else *(float2*)((float*)a.out + base) = make_float2(result<false>(o.x, inv), result<false>(o.y, inv));
   }
 }
 

@@ -708,3 +708,40 @@ def test_tables_of_every_kind_of_launch(batch, n_slots):
         starts, slots = po.resize(want, table, lens, free, n_slots, 16)
         for got, ref in zip(arrays + [d_starts, d_slots], (table, lens, free, starts, slots)):
             assert np.array_equal(got.cpu().numpy(), ref)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("news", [[3, 1], [120, 1], [40, 100]])
+@pytest.mark.parametrize("apart", [(-100, 60), (-95, 60), (-90, 112), (-100, 100), (-60, 112), (-30, 112)])
+def test_attention_over_pages_very_far_apart(apart, news, dtype):
+    """Pages of V whose sizes are 2^140 to 2^212 apart, more than fp32 holds: the small ones (-100: zeros) have their share of the weights all the same."""
+    rng = np.random.default_rng(news[0] + apart[1] - apart[0])
+    for small in (lambda j: j < 4, lambda j: j >= 4, lambda j: j % 2 == 0):
+        pool = Pool(rng, [150, 100], 16, heads=1, stale=False)
+        for b in (0, 1):
+            for j in range(-(-int(pool.lens[b]) // 16)):
+                k, v = (rng.normal(size=(1, 16, 1, 128)) for _ in range(2))
+                v = v * 0.0 if small(j) and apart[0] == -100 else v * 2.0 ** apart[0 if small(j) else 1]
+                pool.store.write(k, v, [int(pool.table[b, j]) * 16 + i for i in range(16)])
+        pool.upload()
+        for q_scale in (1.0, 8.0):
+            attend(pool, rng, news, 3, dtype, q_scale=q_scale)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("size,last", [(0.0, 1.0), (2.0 ** -92, 2.0 ** -92), (2.0 ** 110, 2.0 ** -80)])
+@pytest.mark.parametrize("G", [3, 80])
+def test_attention_over_many_pages_of_one_size(G, size, last, dtype):
+    """65536 tokens whose values are zeros, tiny or huge, 40 others behind them: the denominator neither overflows nor vanishes, in a part's sums and in their join."""
+    rng = np.random.default_rng(G)
+    P, n = 128, 65536 + 40
+    pool = Pool(rng, [n], P, heads=1, stale=False)
+    store, pages = pool.store, pool.table[0, :n // P]
+    k, v = (rng.normal(size=(1, 4 * P, 1, 128)) for _ in range(2))
+    store.write(k, v * size, [int(p) * P + i for p in pages[:4] for i in range(P)])
+    for j, page in enumerate(pages[4:]):
+        store.raw[:, page], store.exponents[:, page] = store.raw[:, pages[j % 4]], store.exponents[:, pages[j % 4]]
+    k, v = (rng.normal(size=(1, 40, 1, 128)) for _ in range(2))
+    store.write(k, v * last, [int(pool.table[0, n // P]) * P + i for i in range(40)])
+    pool.upload()
+    attend(pool, rng, [1], G, dtype)
