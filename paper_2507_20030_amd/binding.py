@@ -10,6 +10,7 @@ import contextlib
 import ctypes
 import functools
 import os
+import warnings
 from typing import Optional, Sequence
 
 import numpy as np
@@ -628,12 +629,36 @@ class PagedCache:
         iwdft_pages_read(self.values, self.exponents, self.table, self.lens, K, V, 0, stream)
         return K, V
 
-    def compress(self, cache: Cache, stream=None):
-        """The first S + M + R tokens of every sequence through iwdft_prefill into `cache`, which has to have this cache's layers, heads and dtype and a
-        batch of max_batch."""
+    def compress(self, cache: Cache, stream=None, sequences: Optional[Sequence[int]] = None):
+        """The first S + M + R tokens of the given sequences through iwdft_prefill into `cache`, which has to have this cache's layers, heads and dtype and a
+        batch of as many.  Tokens behind those stay here only: hand them to ``cache.append``, or give their pages back.  Returns by how many tokens each sequence is
+        longer than S + M + R.
+
+        The prefill knows no shorter sequences, it would take zeros for the tokens that are missing: a given sequence that has fewer is refused.  None stands for the
+        whole batch as it is, idle places included: there they are zeros, a warning names the places, and what attends to them is worth nothing.  The lengths are read for all
+        this, which waits for the stream.  While a graph is captured they cannot be: None is returned, and a given sequence that is too short at a replay becomes NaN."""
         L, H, G, D = self.shape
-        if cache.shape != (L, self.lens.shape[0], H, G, D) or cache.dtype != self.dtype or cache.device != self.device:
-            raise ValueError(f"cache holds {cache.shape} {cache.dtype} on {cache.device}, these pages {(L, self.lens.shape[0], H, G, D)} {self.dtype} on {self.device}")
+        rows = list(range(self.lens.shape[0])) if sequences is None else [int(b) for b in sequences]
+        if any(not 0 <= b < self.lens.shape[0] for b in rows):
+            raise ValueError(f"sequences {rows} of {self.lens.shape[0]}")
+        if cache.shape != (L, len(rows), H, G, D) or cache.dtype != self.dtype or cache.device != self.device:
+            raise ValueError(f"cache holds {cache.shape} {cache.dtype} on {cache.device}, these pages {(L, len(rows), H, G, D)} {self.dtype} on {self.device}")
         d = cache.desc.c
-        K, V = self.read(d.n_sink + d.M + d.n_recent, stream)
+        n = d.n_sink + d.M + d.n_recent
+        with _on_stream(stream, self.device):
+            table, lens = (self.table, self.lens) if sequences is None else (torch.cat([x[b:b + 1] for b in rows]) for x in (self.table, self.lens))
+            captured = torch.cuda.is_current_stream_capturing()
+            over = None if captured else [m - n for m in lens.tolist()]
+            short = [b for b, m in zip(rows, over or []) if m < 0]
+            if short and sequences is not None:
+                raise ValueError(f"sequences {short} have fewer than {n} tokens")
+            if short:
+                warnings.warn(f"sequences {short} have fewer than {n} tokens: zeros are compressed in their place", stacklevel=2)
+            K, V = (torch.empty((L, len(rows), H, n, D), dtype=self.dtype, device=self.device) for _ in range(2))
+        iwdft_pages_read(self.values, self.exponents, table, lens, K, V, 0, stream)
+        if captured and sequences is not None:
+            with _on_stream(stream, self.device):
+                for x in (K, V):
+                    x[:, :, :, 0].masked_fill_((lens < n).view(-1, 1, 1), float("nan"))
         cache.prefill(K, V, stream)
+        return over

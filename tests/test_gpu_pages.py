@@ -745,3 +745,86 @@ def test_attention_over_many_pages_of_one_size(G, size, last, dtype):
     store.write(k, v * last, [int(pool.table[0, n // P]) * P + i for i in range(40)])
     pool.upload()
     attend(pool, rng, [1], G, dtype)
+
+
+def filled(lens, max_tokens=400, L=2, H=2, G=2, P=32, dtype=torch.bfloat16):
+    """A paged cache with sequences of these lengths and what the oracle reads from it."""
+    c = B.PagedCache(L, 60, H, H * G, 128, dtype, len(lens), max_tokens, P, DEV)
+    _, slots = c.resize(dev(np.array(lens, np.int32)), sum(lens))
+    k, v = (torch.randn((L, sum(lens), H, 128), device=DEV).to(dtype) for _ in range(2))
+    c.write(k, v, slots)
+    store = po.Store(L, 60, H, P)
+    store.unpack(c.values.cpu().numpy(), c.exponents.cpu().numpy())
+    return c, store.read(c.table.cpu().numpy(), c.lens.cpu().numpy(), max(lens), 0, L)
+
+
+def frequency_cache(batch, M=256, L=2, H=2, G=2, device=DEV, dtype=torch.bfloat16):
+    return B.Cache(L, batch, H, H * G, 128, dtype, M, [np.arange(40, dtype=np.int32)] * L, device=device, n_sink=4, n_recent=5)
+
+
+def same_coefficients(cache, tokens, rows):
+    for layer in range(2):
+        for got, x in zip(cache.export_coeffs(layer), tokens):
+            for i, b in enumerate(rows):
+                for h in range(2):
+                    want = orc.prefill(x[layer, b, h, 4:260], np.arange(40))
+                    assert np.linalg.norm(got[i, h].cpu().numpy() - want) <= 1e-4 * np.linalg.norm(want)
+
+
+def test_compressing_sequences_that_are_too_short():
+    """Zeros for tokens that never were would have weight: given ones are refused and nothing is written; of the whole batch a warning and the counts tell which they are."""
+    for lens, short in (([265, 264], [1]), ([0, 300], [0]), ([20, 100], [0, 1])):
+        c, tokens = filled(lens)
+        cache = frequency_cache(2)
+        before = cache.T
+        with pytest.raises(ValueError, match=str(short[0])):
+            c.compress(cache, sequences=[0, 1])
+        assert cache.T == before
+        with pytest.warns(UserWarning, match=str(short[-1])):
+            assert c.compress(cache) == [n - 265 for n in lens]
+        cache.close()
+
+
+def test_compressing_some_sequences():
+    """Those that are long enough, in the order given; what they have behind the prompt is told and stays in the pages."""
+    c, tokens = filled([268, 20, 0, 265, 300])
+    for rows, left in (([0], [3]), ([3, 0], [0, 3]), ([4, 3], [35, 0])):
+        cache = frequency_cache(len(rows))
+        assert c.compress(cache, sequences=rows) == left
+        same_coefficients(cache, tokens, rows)
+        for row in (rows[0], rows[0]) if len(rows) == 1 else ():
+            with pytest.raises(ValueError):
+                c.compress(cache, sequences=[row, row])  # a batch of one
+        cache.close()
+    for bad in ([5], [-1], [1]):
+        cache = frequency_cache(1)
+        with pytest.raises(ValueError):
+            c.compress(cache, sequences=bad)
+        cache.close()
+    whole, tokens = filled([265, 270])
+    cache, side = frequency_cache(2), torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    assert whole.compress(cache, side) == [0, 5]
+    side.synchronize()
+    same_coefficients(cache, tokens, [0, 1])
+
+
+def test_compressing_in_a_captured_graph():
+    """Lengths may change before a replay: one that is too short then gives NaN, not a result with zeros for tokens."""
+    c, tokens = filled([268, 270, 20])
+    cache = frequency_cache(2)
+    c.compress(cache, sequences=[0, 1])
+    q = torch.randn((2, 2, 4, 128), device=DEV).to(torch.bfloat16)
+    ref = cache.attend(q).clone()
+    torch.cuda.synchronize()
+    g, out = torch.cuda.CUDAGraph(), torch.zeros_like(q)
+    with torch.cuda.graph(g):
+        assert c.compress(cache, sequences=[0, 1]) is None
+        cache.attend(q, out)
+    for lens, ok in (([268, 270], [True, True]), ([268, 264], [True, False]), ([265, 270], [True, True]), ([0, 265], [False, True])):
+        c.lens[:2].copy_(dev(np.array(lens, np.int32)))
+        out.fill_(0)
+        g.replay()
+        torch.cuda.synchronize()
+        for b in (0, 1):
+            assert torch.equal(out[:, b], ref[:, b]) if ok[b] else torch.isnan(out[:, b].float()).all(), lens
