@@ -637,12 +637,16 @@ class PagedCache:
         The prefill knows no shorter sequences, it would take zeros for the tokens that are missing: a given sequence that has fewer is refused.  None stands for the
         whole batch as it is, idle places included: there they are zeros, a warning names the places, and what attends to them is worth nothing.  The lengths are read for all
         this, which waits for the stream.  While a graph is captured they cannot be: None is returned, and a given sequence that is too short at a replay becomes NaN."""
+        device = self.values.device
+        if device.index != torch.cuda.current_device():  # whose stream the prefill takes
+            with torch.cuda.device(device):
+                return self.compress(cache, stream, sequences)
         L, H, G, D = self.shape
         rows = list(range(self.lens.shape[0])) if sequences is None else [int(b) for b in sequences]
         if any(not 0 <= b < self.lens.shape[0] for b in rows):
             raise ValueError(f"sequences {rows} of {self.lens.shape[0]}")
-        if cache.shape != (L, len(rows), H, G, D) or cache.dtype != self.dtype or cache.device != self.device:
-            raise ValueError(f"cache holds {cache.shape} {cache.dtype} on {cache.device}, these pages {(L, len(rows), H, G, D)} {self.dtype} on {self.device}")
+        if cache.shape != (L, len(rows), H, G, D) or cache.dtype != self.dtype or cache.state.device != device:
+            raise ValueError(f"cache holds {cache.shape} {cache.dtype} on {cache.state.device}, these pages {(L, len(rows), H, G, D)} {self.dtype} on {device}")
         d = cache.desc.c
         n = d.n_sink + d.M + d.n_recent
         with _on_stream(stream, self.device):

@@ -828,3 +828,16 @@ def test_compressing_in_a_captured_graph():
         torch.cuda.synchronize()
         for b in (0, 1):
             assert torch.equal(out[:, b], ref[:, b]) if ok[b] else torch.isnan(out[:, b].float()).all(), lens
+
+
+@pytest.mark.parametrize("names", [("cuda", "cuda:0"), ("cuda:0", "cuda"), ("cuda", "cuda")])
+def test_one_device_under_two_names(names):
+    """A cache made on "cuda" is on the same GPU as one made on "cuda:0"."""
+    c = B.PagedCache(2, 20, 2, 4, 128, torch.bfloat16, 1, 400, 32, names[0])
+    starts, slots = c.resize(dev(np.array([265], np.int32)), 265)
+    k, v = (torch.randn((2, 265, 2, 128), device=DEV).to(torch.bfloat16) for _ in range(2))
+    c.write(k, v, slots)
+    cache = frequency_cache(1, device=names[1])
+    assert c.compress(cache) == [0]
+    assert torch.isfinite(cache.attend(torch.randn((2, 1, 4, 128), device=DEV).to(torch.bfloat16)).float()).all()
+    cache.close()
