@@ -194,7 +194,7 @@ __global__ __launch_bounds__(256) void resize_wave_kernel(ResizeArgs a) {
   resize_fill(a, Fill{keep[0], keep[1], keep[2], keep[3], keep[4], state}, threadIdx.x, 256);
 }
 
-// Every slot looks its sequence up, in LDS where the sequences fit (256 sequences, 280000 slots: 5.9 us with eight dependent loads from memory, 5.2 with the starts in LDS,
+// Every slot looks its sequence up, in LDS where the sequences fit (256 sequences, 387346 slots: 5.9 us with eight dependent loads from memory, 5.2 with the starts in LDS,
 // 4.8 with what is looked up there beside them).
 __global__ __launch_bounds__(256) void resize_fill_kernel(ResizeArgs a) {
   __shared__ int32_t keep[3][kResizeOneBatch];
@@ -286,7 +286,7 @@ struct Octet {
 
 // A run -- new tokens that follow each other in one page -- is one wave's work for each head and tensor: its largest value, the page's exponent, the
 // values, and no two waves meet.  Up to kHeld octets stay in registers, all on their way at a time; a longer run (pages of 128) is read twice, the
-// second time from the caches.  Bound by memory: 46000 tokens of 8 heads, bf16 (189 MB):
+// second time from the caches.  Bound by memory: 30675 tokens of 8 heads, bf16 (126 MB read, 63 written):
 // 78 us with every run read twice, 256 bytes at a time, 50 held in registers, 43 with integer maxima.
 // old: the page's exponent, used from its second token on; returns the new one.  Old values are only touched where it grows; of an octet of V that
 // holds other tokens too the bytes of those stay.

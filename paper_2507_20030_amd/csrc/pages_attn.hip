@@ -55,9 +55,11 @@ __device__ __forceinline__ float sum_of_powers(const float* x, float top, float 
 
 // ------------------------------------------------------------------------------------------------ sharing out the work
 // A block is `rows` consecutive (new token, query head of the KV head) pairs of a sequence; its tokens are cut into parts, one workgroup each, such that
-// all parts of a call hold about the same number of tiles and there are no more than `parts` of them, as many as the chip holds at a time (one more would run
-// alone in the end: 16 contexts of 4096 to 16384 tokens 90 us, with the blocks' last, shorter parts counted in 78, 71 with what is below).  Lengths live on the
-// device, so every wave works out the shares by itself, 64 sequences at a time: the launch only has to be large enough.
+// all parts of a call hold about the same number of tiles and, up to parts / 2 blocks, there are about `parts` of them: two workgroups on each CU (more would run
+// alone in the end: 16 contexts of 4096 to 16384 tokens 90 us, with the blocks' last, shorter parts counted in 78, 72 with what is below).  More blocks make more parts, and
+// the two kinds of rows count for themselves.  Lengths live on the device, so every wave works out the shares by itself, 64 sequences at a time: the launch only has to be large enough.
+// The kernels that leave a SIMD one wave (64 rows in bf16, 32 rows and prompts in fp32) run 256 workgroups at a time, so 512 parts are two rounds there; us with 512 / 256:
+// one sequence of 65536 tokens and 48 rows 71 / 59, in fp32 20 rows 57 / 50; four of up to 16384 and 48 rows 31 / 34, 800 rows over 32768 in fp32 300 / 318, 4096 tokens' prompt 357 / 356.
 // Short parts cost more in the join than the second workgroup on a CU gains: one token over 8192 tokens of 8 heads 15.0 us with parts of 4 tiles, 12.0 with 8,
 // over 16000 17.3 with 8 and 15.6 with 16.
 constexpr int kLeastTiles = 4, kCus = 256;
@@ -193,7 +195,7 @@ __device__ __forceinline__ half8 operand(uint32_t lo, uint32_t hi) {
 __device__ __forceinline__ uint32_t nan_bytes(uint32_t w) {  // 1 in every byte that is NaN (0x7f, 0xff)
   return (((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) >> 7;
 }
-template <int N, int PARTS>
+template <int PARTS>
 __device__ __forceinline__ void to_halves(const float* x, half8* parts) {  // x[8] as PARTS fp16 numbers that add up to it
 #pragma unroll
   for (int c = 0; c < 8; ++c) {
@@ -418,7 +420,7 @@ __device__ __forceinline__ void few_rows(const PagesAttn& a, uint32_t x0, uint32
         for (int c = 0; c < 8; ++c) z.q8[0][c] = hi[c], z.q8[1][c] = lo[c];
       } else {
 #pragma unroll
-        for (int c = 0; c < 4; ++c) to_halves<8, PARTS>(f[c / 2] + 8 * (c % 2), z.q[c]);
+        for (int c = 0; c < 4; ++c) to_halves<PARTS>(f[c / 2] + 8 * (c % 2), z.q[c]);
       }
     }
 
@@ -501,7 +503,7 @@ __device__ __forceinline__ void few_rows(const PagesAttn& a, uint32_t x0, uint32
 #pragma unroll
         for (int j = 0; j < 8; ++j) y[j] = __builtin_amdgcn_exp2f(sc[j] - ref), sum += y[j];
         z.l += ldexpf(sum, shift);
-        to_halves<8, PARTS>(y, pw[r]);
+        to_halves<PARTS>(y, pw[r]);
       }
 #pragma unroll
       for (int p = 0; p < 4; ++p) {
@@ -654,7 +656,7 @@ __device__ __forceinline__ uint32_t many_rows(const PagesAttn& a, uint32_t x0, u
         }
       } else {
 #pragma unroll
-        for (int c = 0; c < 8; ++c) to_halves<8, PARTS>(f[c / 2] + 8 * (c % 2), q[c]);
+        for (int c = 0; c < 8; ++c) to_halves<PARTS>(f[c / 2] + 8 * (c % 2), q[c]);
       }
     }
     const float q_scale = ldexpf(1.f, eq);
@@ -803,7 +805,7 @@ __device__ __forceinline__ uint32_t many_rows(const PagesAttn& a, uint32_t x0, u
           float y[8], sum = 0.f;
 #pragma unroll
           for (int j = 0; j < 8; ++j) y[j] = __builtin_amdgcn_exp2f(sc[8 * t + j]);
-          to_halves<8, PARTS>(y, pw[t]);
+          to_halves<PARTS>(y, pw[t]);
 #pragma unroll
           for (int j = 0; j < 8; ++j) sum += y[j];  // not of the rounded weights: where V's pages are far apart, those of a small page may all be 0 in fp16
           l += sum * inv[t];
@@ -936,7 +938,7 @@ __device__ __forceinline__ void join_rows(const PagesAttn& a, const PagesRows& w
 
 // ------------------------------------------------------------------------------------------------ launches
 // R: row tiles of few_rows (0: none), MANY: many_rows too.  A call that may have both kinds of sequences is one launch, the blocks of many rows first: the
-// others fill what these leave free in the end.  (Two 1000-token prompts beside six single tokens, windows: four launches 206 us, one and a join 181; 150 with what is below.)
+// others fill what these leave free in the end.  (Prompts of 791 and 630 tokens beside five single ones, windows: four launches 206 us, one and a join 181; 152 with what is below.)
 template <bool BF16, int R, bool MANY>
 __global__ __launch_bounds__(kWaves* kWave, BF16 ? (R <= 2 ? 2 : 1) : (R == 1 && !MANY ? 2 : 1)) void pages_attn_kernel(PagesAttn a) {
   uint32_t x = blockIdx.x;
@@ -981,7 +983,9 @@ bool may_cut(const Pages& S) { return ((int64_t)S.max_pages << S.logP) > (int64_
 Launches launches_of(const Pages& S, int batch, int n_tokens, bool bf16) {
   Launches n;
   const int64_t rows = (int64_t)n_tokens * S.G, average = S.G * (((int64_t)n_tokens + batch - 1) / batch);
-  n.many = rows > kFewRows && n_tokens >= 2 * (int64_t)batch;  // about one token for each sequence: few_rows alone, whoever brings more
+  // About one token for each row of the table, idle ones among them: few_rows alone, whoever brings more.  (500 tokens of one sequence of 8192, 4 query heads, and
+  // 250 idle rows 191 us, with 248 idle ones, where many_rows takes them, 144, with none 118; 250 tokens beside 255 single ones 312, these alone 220.)
+  n.many = rows > kFewRows && n_tokens >= 2 * (int64_t)batch;
   if (!n.many || batch > 1) n.few = few_tiles(average > kFewRows ? S.G : average, bf16, n.many);  // beside prompts: single tokens
   n.cut = may_cut(S);
   if (n.cut) {
