@@ -374,8 +374,8 @@ int iwdft_pages_write(const iwdft_pages_desc* desc, int32_t layer, int32_t n_lay
  * p = lens[b] - (starts[b + 1] - starts[b]) + i and sees the tokens j <= p, with n_recent > 0 those with j < n_sink or j > p - n_recent only (the windows of
  * Sec. 4.2.1).  d_q, d_out: [n_layers][n_tokens][n_q_heads][head_dim], kv_dtype, not overlapping.  scale <= 0 selects 1/sqrt(head_dim).  A row without
  * a token to see, or whose scores are all -infinity, is 0; rows from starts[batch] on stay as they are.  What a token holds that a row does not see, NaN too, does not reach the row.
- * Prompts, drafts of a few tokens and single ones may be mixed.  Stored values enter the products exactly; bf16 queries down to 2^-14 of
- * their row's largest value, smaller ones err by 2^-22 of that; fp32 queries and their weights have 22 bits, the weights of bf16 calls 11; weights times the scale of V's page err by 2^-31
+ * Prompts, drafts of a few tokens and single ones may be mixed.  Stored values enter the products exactly; bf16 queries down to 2^-31 of
+ * their row's largest value, smaller ones err by 2^-39 of that; fp32 queries and their weights have 22 bits, the weights of bf16 calls 11; weights times the scale of V's page err by 2^-31
  * (bf16; fp32 2^-40) of the largest such product whatever their size; sums, the weights' among them, are fp32.  Scores, and the largest |q| of a row times the scale
  * of a page of K, have to stay in fp32's range: a row where they pass it may be NaN. */
 int iwdft_pages_attn(const iwdft_pages_desc* desc, int32_t layer, int32_t n_layers, const void* d_q, const int32_t* d_starts, int32_t n_tokens,

@@ -3,11 +3,10 @@
 //   o_t = sum_j p_j v_j,  p = softmax_j (scale q_t k_j),  over the tokens j that t sees.
 //
 // All products run on the matrix cores.  What keeps them exact:
-//  * q k in bf16 calls: K goes in as the bytes it is stored as.  A bf16 number has 8 significant bits and is the sum of two e4m3 numbers of 4: the
-//    nearest one and the rest, 32 times as large, which the instruction scales back.  A row of q is multiplied by the power of two that
-//    brings its largest value to [2^7, 2^8); down to 2^-14 of that value the sum is exact, smaller ones err by 2^-22 of it.  Two products of
-//    bytes take as long as one of fp16, and nothing has to be converted.
-//  * q k in fp32 calls: fp16, which holds e4m3 exactly; q, its largest value in [2^14, 2^15), as the sum of two fp16 parts (22 bits).
+//  * q k: fp16, which holds e4m3 exactly.  A row of q is multiplied by the power of two that brings its largest value to [2^14, 2^15); a bf16 number is exact in
+//    fp16 down to 2^-31 of that value, a smaller one errs by 2^-39 of it; fp32 queries are the sum of two fp16 parts (22 bits).  (The block-scaled products of e4m3 bytes
+//    need no conversions and make prompts 8 % faster, but one of them loses what is 2^14 times smaller than the largest product of its group: a score's sum errs by up to
+//    2^-12 of sum |q k|, 2^-15 in the mean, with fp16 products by 2^-22 and 2^-25.)
 //  * p v: fp16.
 //  * the pages' exponents: that of K enters the score's factor; that of V joins the exponent of the weight.  With s_j the score times log2 e and
 //    eV_j the exponent of j's page, the weights in the sum are P_j = 2^(s_j + eV_j - m), m a running bound of s_j + eV_j, and the
@@ -34,10 +33,10 @@ constexpr int kWaves = 4;
 template <bool BF16>
 struct Weights {
   static constexpr float lift = BF16 ? 6.f : 15.f, slack = BF16 ? 8.f : 0.f;
-  static constexpr int q_top = BF16 ? 7 : 14;  // rows of q: largest value in [2^q_top, 2^(q_top + 1))
   static constexpr int down = (int)lift + 4;   // what the sums are larger than 2^4 times the denominator by
   static constexpr float unit = 1.f / (float)(1 << down);
 };
+constexpr int kQTop = 14;  // rows of q: largest value in [2^kQTop, 2^(kQTop + 1))
 constexpr int kNear = 32;
 // x * 2^d.  In two factors: 2^d may be out of range where the product is not.
 __device__ __forceinline__ float times_power(float x, float d) {
@@ -208,23 +207,6 @@ __device__ __forceinline__ void to_halves(const float* x, half8* parts) {  // x[
     }
   }
 }
-// 16 values as bytes hi + 2^-5 lo; what is not finite becomes NaN.
-typedef int intx8 __attribute__((ext_vector_type(8)));
-constexpr int kOne = 0x7f7f7f7f, kThirtySecond = 0x7a7a7a7a;  // scales of the matrix instructions: 2^0, 2^-5
-__device__ __forceinline__ void to_bytes(const float* x, int* hi, int* lo) {
-#pragma unroll
-  for (int c = 0; c < 16; c += 4) {
-    float y[4], back[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) y[j] = fabsf(x[c + j]) <= (float)kE4m3Max ? x[c + j] : __builtin_nanf("");
-    hi[c / 4] = (int)floats_e4m3(y);
-    e4m3_floats((uint32_t)hi[c / 4], back);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) y[j] = 32.f * (y[j] - back[j]);
-    lo[c / 4] = (int)floats_e4m3(y);
-  }
-}
-__device__ __forceinline__ intx8 operand8(uint4 a, uint4 b) { return intx8{(int)a.x, (int)a.y, (int)a.z, (int)a.w, (int)b.x, (int)b.y, (int)b.z, (int)b.w}; }
 __device__ __forceinline__ float max_over_16s(float x) {  // over lanes that differ in their upper two bits
   x = fmaxf(x, __shfl_xor(x, 16));
   return fmaxf(x, __shfl_xor(x, 32));
@@ -301,8 +283,7 @@ __device__ __forceinline__ Span span_of(const PagesAttn& a, int p_lo, int p_hi) 
 // One row tile of 16 query rows: lane l holds row l % 16.
 template <int PARTS>
 struct Rows {
-  half8 q[PARTS == 1 ? 1 : 4][PARTS];  // fp32: [chunk of 16 channels oct + 4 (c / 2)][8 of them: c % 2]
-  intx8 q8[2];                         // bf16: both chunks, hi and lo
+  half8 q[4][PARTS];  // [chunk of 16 channels oct + 4 (c / 2)][8 of them: c % 2]
   floatx4 o[8];   // [16-byte load of V][channel of the pair]: row l % 16, channels 32 (i / 2) + 8 (l / 16) + 2 c + i % 2
   float m, l;
   int pos, from, eq;
@@ -317,7 +298,7 @@ struct Rows {
 template <bool BF16, int R, int W>
 __device__ __forceinline__ void few_rows(const PagesAttn& a, uint32_t x0, uint32_t step) {
   using Geo = Few<R>;
-  constexpr int PARTS = BF16 ? 1 : 2, BR = Geo::rows, kTile = Geo::tile, kQTop = Weights<BF16>::q_top;
+  constexpr int PARTS = BF16 ? 1 : 2, BR = Geo::rows, kTile = Geo::tile;
   const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int row = lane & 15, oct = lane >> 4;
   __shared__ __attribute__((aligned(16))) float join[W][16][kHeadDim + 4];
@@ -413,15 +394,8 @@ __device__ __forceinline__ void few_rows(const PagesAttn& a, uint32_t x0, uint32
       for (int p = 0; p < 2; ++p)
 #pragma unroll
         for (int c = 0; c < 16; ++c) f[p][c] = ldexpf(f[p][c], kQTop - z.eq);
-      if constexpr (BF16) {
-        int hi[8], lo[8];
-        to_bytes(f[0], hi, lo), to_bytes(f[1], hi + 4, lo + 4);
 #pragma unroll
-        for (int c = 0; c < 8; ++c) z.q8[0][c] = hi[c], z.q8[1][c] = lo[c];
-      } else {
-#pragma unroll
-        for (int c = 0; c < 4; ++c) to_halves<PARTS>(f[c / 2] + 8 * (c % 2), z.q[c]);
-      }
+      for (int c = 0; c < 4; ++c) to_halves<PARTS>(f[c / 2] + 8 * (c % 2), z.q[c]);
     }
 
     int near = kNear;  // -1 from the first far page on
@@ -446,12 +420,11 @@ __device__ __forceinline__ void few_rows(const PagesAttn& a, uint32_t x0, uint32
         poison = __any(nans != 0);
       }
 
-      half8 kf[2][BF16 ? 1 : 4];
-      if constexpr (!BF16)
+      half8 kf[2][4];
 #pragma unroll
-        for (int u = 0; u < 2; ++u)
+      for (int u = 0; u < 2; ++u)
 #pragma unroll
-          for (int p = 0; p < 2; ++p) kf[u][2 * p] = operand(d.k[u][p].x, d.k[u][p].y), kf[u][2 * p + 1] = operand(d.k[u][p].z, d.k[u][p].w);
+        for (int p = 0; p < 2; ++p) kf[u][2 * p] = operand(d.k[u][p].x, d.k[u][p].y), kf[u][2 * p + 1] = operand(d.k[u][p].z, d.k[u][p].w);
       const float ev = (float)d.e.y;
       const bool far = __builtin_expect(__any(abs(d.e.y) > near), 0);
       near = far ? -1 : near;
@@ -466,16 +439,10 @@ __device__ __forceinline__ void few_rows(const PagesAttn& a, uint32_t x0, uint32
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
           floatx4 acc{0.f, 0.f, 0.f, 0.f};
-          if constexpr (BF16) {
-            const intx8 k8 = operand8(d.k[u][0], d.k[u][1]);
-            acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k8, z.q8[1], acc, 0, 0, 0, kOne, 0, kThirtySecond);
-            acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k8, z.q8[0], acc, 0, 0, 0, kOne, 0, kOne);
-          } else {
 #pragma unroll
-            for (int c = 0; c < 4; ++c)
+          for (int c = 0; c < 4; ++c)
 #pragma unroll
-              for (int p = PARTS - 1; p >= 0; --p) acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[u][c], z.q[c][p], acc, 0, 0, 0);
-          }
+            for (int p = PARTS - 1; p >= 0; --p) acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[u][c], z.q[c][p], acc, 0, 0, 0);
 #pragma unroll
           for (int j = 0; j < 4; ++j) sc[4 * u + j] = acc[j];
         }
@@ -589,13 +556,13 @@ __device__ __forceinline__ void few_rows(const PagesAttn& a, uint32_t x0, uint32
 
 // ------------------------------------------------------------------------------------------------ many rows
 // Prompts: four waves of 32 rows share tiles of 64 tokens that go through LDS as bytes, the next tile's loads in flight while this one is multiplied; a wave
-// turns the bytes into operands itself (32 conversions per 8 products of 32 cycles; fp16 in LDS would need the LDS's whole bandwidth).
+// turns the bytes into operands itself (128 conversions per 32 products of 32 cycles; K as fp16 in LDS: a prompt of 8000 tokens 1 % faster, a mixed call 40 % slower, whose CUs then hold one workgroup).
 // S^T = K Q^T leaves lane l with row l % 32 and tokens 16 t + 8 (l / 32) + j, the operand of O^T = V^T P^T.  K's 16-byte chunks are
 // swizzled by their token so that the eight lanes of a bank group read eight different ones.
 template <bool BF16>
 __device__ __forceinline__ uint32_t many_rows(const PagesAttn& a, uint32_t x0, uint32_t step) {  // returns the workgroups' number
   using Geo = Many;
-  constexpr int PARTS = BF16 ? 1 : 2, BR = Geo::rows, kTile = Geo::tile, kHalf = 32, kQTop = Weights<BF16>::q_top;
+  constexpr int PARTS = BF16 ? 1 : 2, BR = Geo::rows, kTile = Geo::tile, kHalf = 32;
   constexpr float kLift = Weights<BF16>::lift;
   static_assert(BR == 32 * kWaves && kTile == 2 * kHalf, "");
   const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
@@ -626,8 +593,7 @@ __device__ __forceinline__ uint32_t many_rows(const PagesAttn& a, uint32_t x0, u
     const int sink = a.n_recent ? a.n_sink : 0, from = window_from(a, pos), w_from = window_from(a, max(w_lo, -1));
     const int64_t out_at = (((int64_t)layer * a.n_tokens + s.first + token) * (a.S.H * G) + h * G + (int)(mine - (uint32_t)token * (uint32_t)G)) * kHeadDim;
 
-    half8 q[BF16 ? 1 : 8][PARTS];  // fp32: [chunk of 16 channels 2 (c / 2) + grp][8 of them: c % 2]
-    intx8 q8[2][2];                // bf16: [two chunks][hi, lo]
+    half8 q[8][PARTS];  // [chunk of 16 channels 2 (c / 2) + grp][8 of them: c % 2]
     int eq;
     {
       float f[4][16], top = 0.f;
@@ -646,18 +612,8 @@ __device__ __forceinline__ uint32_t many_rows(const PagesAttn& a, uint32_t x0, u
       for (int c = 0; c < 4; ++c)
 #pragma unroll
         for (int j = 0; j < 16; ++j) f[c][j] = ldexpf(f[c][j], kQTop - eq);
-      if constexpr (BF16) {
 #pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          int hi[8], lo[8];
-          to_bytes(f[2 * c], hi, lo), to_bytes(f[2 * c + 1], hi + 4, lo + 4);
-#pragma unroll
-          for (int j = 0; j < 8; ++j) q8[c][0][j] = hi[j], q8[c][1][j] = lo[j];
-        }
-      } else {
-#pragma unroll
-        for (int c = 0; c < 8; ++c) to_halves<PARTS>(f[c / 2] + 8 * (c % 2), q[c]);
-      }
+      for (int c = 0; c < 8; ++c) to_halves<PARTS>(f[c / 2] + 8 * (c % 2), q[c]);
     }
     const float q_scale = ldexpf(1.f, eq);
     floatx16 o[4];  // rows 8 (i / 4) + 4 grp + i % 4 =: u of channel tile c: channel 64 (c / 2) + 2 u + c % 2
@@ -728,28 +684,16 @@ __device__ __forceinline__ uint32_t many_rows(const PagesAttn& a, uint32_t x0, u
 #pragma unroll
           for (int j = 0; j < 16; ++j) acc[u][j] = 0.f;
         const auto chunk = [&](int u, int c) { return ((const uint4*)kbuf[b])[(kHalf * u + k_tok) * 8 + ((2 * c + grp) ^ k_swz)]; };
-        if constexpr (BF16) {
 #pragma unroll
-          for (int c = 0; c < 2; ++c)
+        for (int c = 0; c < 4; ++c) {
+          const uint4 kw[2] = {chunk(0, c), chunk(1, c)};
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-              const intx8 k8 = operand8(chunk(u, 2 * c), chunk(u, 2 * c + 1));
-              acc[u] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(k8, q8[c][1], acc[u], 0, 0, 0, kOne, 0, kThirtySecond);
-              acc[u] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(k8, q8[c][0], acc[u], 0, 0, 0, kOne, 0, kOne);
-            }
-        } else {
+          for (int i = 0; i < 2; ++i)
 #pragma unroll
-          for (int c = 0; c < 4; ++c)
+            for (int p = PARTS - 1; p >= 0; --p)
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-              const uint4 kw = chunk(u, c);
-              const half8 k0 = operand(kw.x, kw.y), k1 = operand(kw.z, kw.w);
-#pragma unroll
-              for (int p = PARTS - 1; p >= 0; --p) {
-                acc[u] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k0, q[2 * c][p], acc[u], 0, 0, 0);
-                acc[u] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k1, q[2 * c + 1][p], acc[u], 0, 0, 0);
-              }
-            }
+              for (int u = 0; u < 2; ++u)
+                acc[u] = __builtin_amdgcn_mfma_f32_32x32x16_f16(i ? operand(kw[u].z, kw[u].w) : operand(kw[u].x, kw[u].y), q[2 * c + i][p], acc[u], 0, 0, 0);
         }
         const int base = t0 + 8 * grp;  // tokens of the lane: base + 16 t + j
         float inv[4], far = -__builtin_inff();

@@ -841,3 +841,31 @@ def test_one_device_under_two_names(names):
     assert c.compress(cache) == [0]
     assert torch.isfinite(cache.attend(torch.randn((2, 1, 4, 128), device=DEV).to(torch.bfloat16)).float()).all()
     cache.close()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("lens,news,G", [([6, 20, 40], [1, 1, 3], 4), ([30, 8], [2, 8], 17), ([300], [1], 3), ([40, 12], [40, 12], 8), ([90], [70], 1)])
+@pytest.mark.parametrize("channels", [(0, 1), (3, 40), (17, 127)])
+def test_attention_of_products_that_cancel(channels, lens, news, G, dtype):
+    """Two channels whose products are hundreds of times as large as the others' and cancel: a score is a sum in fp32, so the small ones keep their bits.  `near`
+    allows for 140 * 2^-24 of the sum of all |products|."""
+    rng = np.random.default_rng(channels[0] + len(lens) + G)
+    for size in (50.0, 400.0):
+        pool = Pool(rng, lens, 16, heads=2, scale=1.0)
+        raw = pool.store.raw
+        raw[:, :, :, 0, :, :] = po.to_e4m3(rng.normal(size=raw.shape[:3] + raw.shape[4:]))
+        raw[:, :, :, 0, :, channels[0]] = po.to_e4m3(size * rng.uniform(0.5, 1.0, size=raw.shape[:3] + raw.shape[4:5]))
+        raw[:, :, :, 0, :, channels[1]] = raw[:, :, :, 0, :, channels[0]] ^ 128
+        pool.store.exponents[..., 0] = 0
+        pool.upload()
+        q = dev(rng.normal(size=(1, sum(news), 2 * G, 128))).to(DT[dtype])
+        q[..., channels[0]] = q[..., channels[1]] = 8.0 * (1.0 + torch.rand(q.shape[:3], device=DEV)).to(DT[dtype])
+        attend(pool, rng, news, G, dtype, q=q)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("lens,news,G", [([32], [17], 17), ([27], [6], 12), ([0, 27, 20], [0, 25, 20], 8), ([2, 3, 1], [1, 1, 1], 33), ([324, 158], [12, 12], 8)])
+def test_attention_of_large_scores(lens, news, G, dtype):
+    rng = np.random.default_rng(G + sum(lens))
+    for P in (16, 128):
+        attend(Pool(rng, lens, P, heads=2), rng, news, G, dtype, q_scale=20.0)
