@@ -55,12 +55,12 @@ __device__ __forceinline__ float sum_of_powers(const float* x, float top, float 
 // ------------------------------------------------------------------------------------------------ sharing out the work
 // A block is `rows` consecutive (new token, query head of the KV head) pairs of a sequence; its tokens are cut into parts, one workgroup each, such that
 // all parts of a call hold about the same number of tiles and, up to parts / 2 blocks, there are about `parts` of them: two workgroups on each CU (more would run
-// alone in the end: 16 contexts of 4096 to 16384 tokens 90 us, with the blocks' last, shorter parts counted in 78, 72 with what is below).  More blocks make more parts, and
+// alone in the end: 16 contexts of 4096 to 16384 tokens 90 us, with the blocks' last, shorter parts counted in 78, 71 with what is below).  More blocks make more parts, and
 // the two kinds of rows count for themselves.  Lengths live on the device, so every wave works out the shares by itself, 64 sequences at a time: the launch only has to be large enough.
 // The kernels that leave a SIMD one wave (64 rows in bf16, 32 rows and prompts in fp32) run 256 workgroups at a time, so 512 parts are two rounds there; us with 512 / 256:
-// one sequence of 65536 tokens and 48 rows 71 / 59, in fp32 20 rows 57 / 50; four of up to 16384 and 48 rows 31 / 34, 800 rows over 32768 in fp32 300 / 318, 4096 tokens' prompt 357 / 356.
-// Short parts cost more in the join than the second workgroup on a CU gains: one token over 8192 tokens of 8 heads 15.0 us with parts of 4 tiles, 12.0 with 8,
-// over 16000 17.3 with 8 and 15.6 with 16.
+// one sequence of 65536 tokens and 48 rows 70 / 58, in fp32 20 rows 57 / 49; four of up to 16384 and 48 rows 28 / 33, 800 rows over 32768 in fp32 297 / 314, 4096 tokens' prompt 355 / 355.
+// Short parts cost more in the join than the second workgroup on a CU gains: one token over 8192 tokens of 8 heads 14.3 us with parts of 4 tiles, 11.6 with 8,
+// over 16000 17.3 with 8 and 15.1 with 16.
 constexpr int kLeastTiles = 4, kCus = 256;
 constexpr float kMostBlocks = 1100000000.f;  // 2^30 rows have fewer: starts that overlap, whose counts would not fit; such a call does nothing
 constexpr int kFewRows = 64;  // sequences of up to so many rows go to few_rows, where a call may have both
@@ -882,7 +882,7 @@ __device__ __forceinline__ void join_rows(const PagesAttn& a, const PagesRows& w
 
 // ------------------------------------------------------------------------------------------------ launches
 // R: row tiles of few_rows (0: none), MANY: many_rows too.  A call that may have both kinds of sequences is one launch, the blocks of many rows first: the
-// others fill what these leave free in the end.  (Prompts of 791 and 630 tokens beside five single ones, windows: four launches 206 us, one and a join 181; 152 with what is below.)
+// others fill what these leave free in the end.  (Prompts of 791 and 630 tokens beside five single ones, windows: four launches 206 us, one and a join 181; 150 with what is below, 163 since scores are fp16 products.)
 template <bool BF16, int R, bool MANY>
 __global__ __launch_bounds__(kWaves* kWave, BF16 ? (R <= 2 ? 2 : 1) : (R == 1 && !MANY ? 2 : 1)) void pages_attn_kernel(PagesAttn a) {
   uint32_t x = blockIdx.x;
@@ -894,8 +894,8 @@ __global__ __launch_bounds__(kWaves* kWave, BF16 ? (R <= 2 ? 2 : 1) : (R == 1 &&
   if constexpr (R > 0) few_rows<BF16, R, kWaves>(a, x, gridDim.x);
 }
 // Tables of up to kShortTiles tiles: blocks are not cut, so nothing is to be joined; twice the waves share their tiles.  One sequence, 8 heads, us with parts
-// and a join / so: fp32, 100 tokens 7.9 / 6.2, 500 9.1 / 9.0, 1000 9.2 / 11.9; bf16, 4 query heads, 500 10.1 / 9.6, 1000 10.4 / 11.9 (a workgroup cannot
-// draw more than 50 KB a microsecond); 8 sequences of 1000 13.7 / 12.9, 64 29.2 / 30.3.
+// and a join / so: fp32, 100 tokens 7.9 / 6.3, 500 9.1 / 9.2, 1000 9.4 / 12.2; bf16, 4 query heads, 500 9.3 / 8.7, 1000 9.6 / 11.0 (a workgroup cannot
+// draw more than 50 KB a microsecond); 8 sequences of 1000 11.2 / 12.0, 64 29.0 / 30.3.
 constexpr int kShortTiles = 17, kShortWaves = 8;
 template <bool BF16, int R>
 __global__ __launch_bounds__(kShortWaves* kWave, 2) void pages_short_kernel(PagesAttn a) {
