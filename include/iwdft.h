@@ -389,6 +389,42 @@ int iwdft_pages_attn_bytes(const iwdft_pages_desc* desc, int32_t n_layers, int32
 int iwdft_pages_read(const iwdft_pages_desc* desc, int32_t layer, int32_t n_layers, const int32_t* d_table, const int32_t* d_lens, int32_t batch, int32_t n_tokens,
                      const void* d_values, const int32_t* d_exponents, void* d_K, void* d_V, void* hip_stream);
 
+/* ---- Pages that sequences share ----
+ *
+ * Samples of one prompt, beams, requests with one beginning hold the same pages at the beginning of their rows of the table.
+ *   refs       int32 [n_pages]: how many sequences hold a page; at first 0.  All of them hold it at the same place, and all pages before it.
+ *   copies     int32 [n][2], 8-byte aligned: (from, to) pages; -1: none.
+ * iwdft_pages_write, _attn and _read serve such tables as they are; what changes tables has to be one of these calls, which keep refs (iwdft_pages_resize frees a page whose other
+ * holders live on).  This build: up to 1024 sequences; batch * max_pages < 2^31. */
+
+/* Sequence b becomes the first d_keep[b] tokens (NULL, negative or more: all) of what sequence d_parent[b] (outside [0, batch): b itself) was before the call; all
+ * at once, so that rows may change places.  Nothing is copied: the pages are shared.  Pages that no sequence holds any more go back on the stack, as if those who
+ * leave them gave them back one by one, from the last page of the last sequence on.  Needs no page and cannot fail. */
+int iwdft_pages_fork(int32_t page_tokens, int32_t n_pages, int32_t max_pages, const int32_t* d_parent, const int32_t* d_keep, int32_t batch, int32_t* d_table,
+                     int32_t* d_lens, int32_t* d_free, int32_t* d_refs, void* d_workspace, size_t workspace_bytes, void* hip_stream);
+/* Its workspace: 0 for tables of up to 8192 entries. */
+int iwdft_pages_fork_bytes(int32_t batch, int32_t max_pages, size_t* workspace_bytes);
+
+/* iwdft_pages_resize where pages are shared.  A page is free once its last holder has given it back.  A sequence that grows into a page that others hold leaves it to
+ * them: it takes a page more, and d_copies[b] (int32 [batch][2], out) says from which page to which iwdft_pages_copy has to bring, before
+ * anything is written; of several that share it, and all grow, the last one stays, held to the pages that are left as those are.  No page of d_copies' second column is in its first.  Without
+ * shared pages the result is that of iwdft_pages_resize; entries of the stack above its count are not defined. */
+int iwdft_pages_resize_shared(int32_t page_tokens, int32_t n_pages, int32_t max_pages, const int32_t* d_want, int32_t batch, int32_t* d_table, int32_t* d_lens,
+                              int32_t* d_free, int32_t* d_refs, int32_t* d_starts, int32_t* d_slots, int32_t n_slots, int32_t* d_copies, void* hip_stream);
+
+/* Page d_copies[i][1] of the pool d_to_values, d_to_exponents (to_pages pages; may be the same pool) becomes page d_copies[i][0] of the other one, byte for byte, in layers layer .. layer +
+ * n_layers - 1 of both; pairs with a page outside of its pool are left out.  No page may be copied to twice, nor from and to in one pool. */
+int iwdft_pages_copy(const iwdft_pages_desc* desc, int32_t layer, int32_t n_layers, const int32_t* d_copies, int32_t n_copies, const void* d_values,
+                     const int32_t* d_exponents, int32_t to_pages, void* d_to_values, int32_t* d_to_exponents, void* hip_stream);
+
+/* Held pages together at the pool's beginning: the highest one to the lowest free place, the next highest to the next, while that brings them down, n_moves of
+ * them at most.  Brings up to date d_table, d_refs and d_free, whose top becomes the lowest free page; d_moves (int32 [n_moves][2], out: from, to; -1 behind the last) is
+ * what iwdft_pages_copy has to do.  n_pages / 2 moves are always enough: the held pages are then 0 .. n_pages - d_free[0] - 1. */
+int iwdft_pages_compact(int32_t page_tokens, int32_t n_pages, int32_t max_pages, int32_t batch, int32_t* d_table, int32_t* d_lens, int32_t* d_free,
+                        int32_t* d_refs, int32_t* d_moves, int32_t n_moves, void* d_workspace, size_t workspace_bytes, void* hip_stream);
+/* Its workspace (8-byte aligned). */
+int iwdft_pages_compact_bytes(int32_t n_pages, size_t* workspace_bytes);
+
 const char* iwdft_last_error(void); /* thread-local, static storage, never NULL */
 
 #ifdef __cplusplus

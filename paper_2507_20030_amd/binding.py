@@ -33,6 +33,7 @@ EXPORTED = [
     "iwdft_num_tokens", "iwdft_set_num_tokens", "iwdft_last_error", "iwdft_phase_timing", "iwdft_phase_times", "iwdft_prefill_kind", "iwdft_attn_kind", "iwdft_attn_pipelined",
     "iwdft_select_bins", "iwdft_ablate_chunk", "iwdft_flush", "compressed_decode_attn_static", "iwdft_query_attn",
     "iwdft_pages_query_bytes", "iwdft_pages_resize", "iwdft_pages_resize_bytes", "iwdft_pages_write", "iwdft_pages_attn", "iwdft_pages_attn_bytes", "iwdft_pages_read",
+    "iwdft_pages_fork", "iwdft_pages_fork_bytes", "iwdft_pages_resize_shared", "iwdft_pages_copy", "iwdft_pages_compact", "iwdft_pages_compact_bytes",
 ]
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libiwdft.so")
@@ -106,6 +107,12 @@ def load_library() -> ctypes.CDLL:
     lib.iwdft_pages_attn.argtypes = [pp, i32, i32, vp, vp, i32, vp, vp, i32, vp, vp, vp, i32, i32, f32, vp, ctypes.c_size_t, vp]
     lib.iwdft_pages_attn_bytes.argtypes = [pp, i32, i32, i32, szp]
     lib.iwdft_pages_read.argtypes = [pp, i32, i32, vp, vp, i32, i32, vp, vp, vp, vp, vp]
+    lib.iwdft_pages_fork.argtypes = [i32, i32, i32, vp, vp, i32, vp, vp, vp, vp, vp, ctypes.c_size_t, vp]
+    lib.iwdft_pages_fork_bytes.argtypes = [i32, i32, szp]
+    lib.iwdft_pages_resize_shared.argtypes = [i32, i32, i32, vp, i32, vp, vp, vp, vp, vp, vp, i32, vp, vp]
+    lib.iwdft_pages_copy.argtypes = [pp, i32, i32, vp, i32, vp, vp, i32, vp, vp, vp]
+    lib.iwdft_pages_compact.argtypes = [i32, i32, i32, i32, vp, vp, vp, vp, vp, i32, vp, ctypes.c_size_t, vp]
+    lib.iwdft_pages_compact_bytes.argtypes = [i32, szp]
     lib.iwdft_num_tokens.argtypes = [vp]
     lib.iwdft_num_tokens.restype = i64
     lib.iwdft_set_num_tokens.argtypes = [vp, i64]
@@ -581,6 +588,98 @@ def iwdft_pages_read(values, exponents, table, lens, K, V, layer: int = 0, strea
     rc = load_library().iwdft_pages_read(_pages_ref(n_layers, n_pages, heads, heads, 128, P, size[1], dtype), layer, shape[0], table.data_ptr(), lens.data_ptr(),
                                          size[0], shape[3], values.data_ptr(), exponents.data_ptr(), K.data_ptr() if K is not None else None,
                                          V.data_ptr() if V is not None else None, _stream_of(stream, index))
+    if rc:
+        _check(rc)
+
+
+# Pages that sequences share: refs int32 [pages], copies int32 [n, 2].
+@functools.lru_cache(maxsize=1024)
+def iwdft_pages_fork_bytes(batch: int, max_pages: int) -> int:
+    return _bytes_of(load_library().iwdft_pages_fork_bytes, batch, max_pages)
+
+
+@functools.lru_cache(maxsize=1024)
+def iwdft_pages_compact_bytes(n_pages: int) -> int:
+    return _bytes_of(load_library().iwdft_pages_compact_bytes, n_pages)
+
+
+def _table_sizes(table: torch.Tensor, refs: torch.Tensor, **others):
+    """(index of the GPU, batch, max_pages, pages); others: (tensor, shape, None where any size will do; the batch as -1, one more as -2, one more than the pages as -3)."""
+    index, shape, i32 = table.get_device(), table.shape, torch.int32
+    if len(shape) != 2 or index < 0:
+        raise ValueError(f"table must be a device tensor [batch, max_pages], not {tuple(shape)} on {table.device}")
+    n_pages = refs.numel()
+    sizes = {None: None, 2: 2, -1: shape[0], -2: shape[0] + 1, -3: n_pages + 1}
+    if not (table.dtype is refs.dtype is i32 and refs.dim() == 1 and refs.get_device() == index and table.is_contiguous() and refs.is_contiguous()):
+        _expect("table", table, i32, shape, table.device)
+        _expect("refs", refs, i32, (n_pages,), table.device)
+    for name, (t, size) in others.items():
+        s = t.shape
+        if not (t.dtype is i32 and t.get_device() == index and len(s) == len(size) and t.is_contiguous() and all(n is None or sizes[n] == m for n, m in zip(size, s))):
+            _expect(name, t, i32, tuple(sizes[n] for n in size), table.device)
+    return index, shape[0], shape[1], n_pages
+
+
+def iwdft_pages_fork(parent, keep, table, lens, free, refs, page_tokens: int, stream=None, workspace=None) -> None:
+    """Sequence b becomes the first keep[b] tokens (keep None, or negative: all) of what sequence parent[b] was: table, lens, free and refs are brought up to date."""
+    more = {} if keep is None else dict(keep=(keep, (-1,)))
+    index, batch, max_pages, n_pages = _table_sizes(table, refs, parent=(parent, (-1,)), lens=(lens, (-1,)), free=(free, (-3,)), **more)
+    if index != torch._C._cuda_getDevice():
+        with torch.cuda.device(index):
+            return iwdft_pages_fork(parent, keep, table, lens, free, refs, page_tokens, stream, workspace)
+    need = iwdft_pages_fork_bytes(batch, max_pages)
+    ws = _scratch(need, table.device, stream, workspace) if need or workspace is not None else None
+    rc = load_library().iwdft_pages_fork(page_tokens, n_pages, max_pages, parent.data_ptr(), None if keep is None else keep.data_ptr(), batch, table.data_ptr(),
+                                         lens.data_ptr(), free.data_ptr(), refs.data_ptr(), ws.data_ptr() if ws is not None else None,
+                                         ws.nbytes if ws is not None else 0, _stream_of(stream, index))
+    if rc:
+        _check(rc)
+
+
+def iwdft_pages_resize_shared(want, table, lens, free, refs, starts, slots, copies, page_tokens: int, stream=None) -> None:
+    """iwdft_pages_resize where pages are shared; copies [batch, 2] says what iwdft_pages_copy has to do before anything is written."""
+    index, batch, max_pages, n_pages = _table_sizes(table, refs, want=(want, (-1,)), lens=(lens, (-1,)), free=(free, (-3,)), starts=(starts, (-2,)), slots=(slots, (None,)),
+                                                    copies=(copies, (-1, 2)))
+    if index != torch._C._cuda_getDevice():
+        with torch.cuda.device(index):
+            return iwdft_pages_resize_shared(want, table, lens, free, refs, starts, slots, copies, page_tokens, stream)
+    rc = load_library().iwdft_pages_resize_shared(page_tokens, n_pages, max_pages, want.data_ptr(), batch, table.data_ptr(), lens.data_ptr(), free.data_ptr(),
+                                                  refs.data_ptr(), starts.data_ptr(), slots.data_ptr(), slots.numel(), copies.data_ptr(), _stream_of(stream, index))
+    if rc:
+        _check(rc)
+
+
+def iwdft_pages_compact(table, lens, free, refs, moves, page_tokens: int, stream=None, workspace=None) -> None:
+    """Held pages together at the pool's beginning, moves.shape[0] of them at most: moves [n, 2] says what iwdft_pages_copy has to do."""
+    index, batch, max_pages, n_pages = _table_sizes(table, refs, lens=(lens, (-1,)), free=(free, (-3,)), moves=(moves, (None, 2)))
+    if index != torch._C._cuda_getDevice():
+        with torch.cuda.device(index):
+            return iwdft_pages_compact(table, lens, free, refs, moves, page_tokens, stream, workspace)
+    ws = _scratch(iwdft_pages_compact_bytes(n_pages), table.device, stream, workspace)
+    rc = load_library().iwdft_pages_compact(page_tokens, n_pages, max_pages, batch, table.data_ptr(), lens.data_ptr(), free.data_ptr(), refs.data_ptr(),
+                                            moves.data_ptr(), moves.shape[0], ws.data_ptr(), ws.nbytes, _stream_of(stream, index))
+    if rc:
+        _check(rc)
+
+
+def iwdft_pages_copy(copies, values, exponents, to_values=None, to_exponents=None, layer: int = 0, n_layers: Optional[int] = None, stream=None) -> None:
+    """Pages copies[:, 0] of values, exponents to copies[:, 1] of the other pool, or (None) of the same one, in n_layers layers from `layer` on (None: all that follow)."""
+    index, all_layers, n_pages, heads, P = _pool_sizes(values, exponents)
+    if (to_values is None) != (to_exponents is None):
+        raise ValueError("to_values and to_exponents belong together")
+    if to_values is None:
+        to_values, to_exponents = values, exponents
+    to_index, to_layers, to_pages, to_heads, to_P = _pool_sizes(to_values, to_exponents)
+    if (to_index, to_layers, to_heads, to_P) != (index, all_layers, heads, P):
+        raise ValueError(f"the pools differ: {tuple(values.shape)} on {values.device} and {tuple(to_values.shape)} on {to_values.device}")
+    if not (copies.dtype is torch.int32 and copies.dim() == 2 and copies.shape[1] == 2 and copies.get_device() == index and copies.is_contiguous()):
+        _expect("copies", copies, torch.int32, (None, 2), values.device)
+    if index != torch._C._cuda_getDevice():
+        with torch.cuda.device(index):
+            return iwdft_pages_copy(copies, values, exponents, to_values, to_exponents, layer, n_layers, stream)
+    n = all_layers - layer if n_layers is None else n_layers
+    rc = load_library().iwdft_pages_copy(_pages_ref(all_layers, n_pages, heads, heads, 128, P, 1, torch.float32), layer, n, copies.data_ptr(), copies.shape[0],
+                                         values.data_ptr(), exponents.data_ptr(), to_pages, to_values.data_ptr(), to_exponents.data_ptr(), _stream_of(stream, index))
     if rc:
         _check(rc)
 

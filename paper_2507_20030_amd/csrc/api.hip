@@ -662,6 +662,14 @@ int check_pages(const iwdft_pages_desc* d, int32_t layer, int32_t n_layers) {
     return fail(IWDFT_ERR_ARG, "%d layers of %d pages of %d heads: too many bytes", d->n_layers, d->n_pages, d->n_kv_heads);
   return rc;
 }
+int check_shared(int32_t page_tokens, int32_t n_pages, int32_t max_pages, int32_t batch) {
+  const int rc = check_page_size(page_tokens, n_pages, max_pages);
+  if (rc != IWDFT_OK) return rc;
+  if (batch < 0) return fail(IWDFT_ERR_ARG, "batch = %d: negative", batch);
+  if (batch > kSharedBatch) return fail(IWDFT_ERR_UNSUPPORTED, "batch = %d: this build shares pages among up to %d sequences", batch, kSharedBatch);
+  if ((int64_t)batch * max_pages > 0x7fffffff) return fail(IWDFT_ERR_ARG, "%d sequences of %d pages: too many entries", batch, max_pages);
+  return IWDFT_OK;
+}
 int check_attn(const iwdft_pages_desc* d, int32_t layer, int32_t n_layers, int32_t batch, int32_t n_tokens) {
   const int rc = check_pages(d, layer, n_layers);
   if (rc == IWDFT_OK && (batch < 0 || batch > kMostCount || n_tokens < 0 || (double)n_tokens * d->n_q_heads * n_layers > kMostRows))
@@ -1257,6 +1265,78 @@ int iwdft_pages_read(const iwdft_pages_desc* desc, int32_t layer, int32_t n_laye
   if (unaligned(16, d_K, d_V, d_values) || unaligned(4, d_table, d_lens) || unaligned(8, d_exponents)) return fail(IWDFT_ERR_ARG, "%s", kPageAlignMsg);
   return launched(launch_pages_read(pages, layer, n_layers, desc->kv_dtype == IWDFT_BF16, d_table, d_lens, batch, n_tokens, d_K, d_V, (hipStream_t)hip_stream),
                   "page read launch");
+}
+
+// ---------------------------------------------------------------------------------------------- pages that sequences share
+
+int iwdft_pages_fork_bytes(int32_t batch, int32_t max_pages, size_t* workspace_bytes) {
+  if (!workspace_bytes) return fail(IWDFT_ERR_ARG, "output pointer is NULL");
+  const int rc = check_shared(16, 1, max_pages, batch);
+  if (rc != IWDFT_OK) return rc;
+  *workspace_bytes = pages_fork_bytes(batch, max_pages);
+  return IWDFT_OK;
+}
+
+int iwdft_pages_fork(int32_t page_tokens, int32_t n_pages, int32_t max_pages, const int32_t* d_parent, const int32_t* d_keep, int32_t batch, int32_t* d_table,
+                     int32_t* d_lens, int32_t* d_free, int32_t* d_refs, void* d_workspace, size_t workspace_bytes, void* hip_stream) {
+  const int rc = check_shared(page_tokens, n_pages, max_pages, batch);
+  if (rc != IWDFT_OK) return rc;
+  const size_t need = pages_fork_bytes(batch, max_pages);
+  if (batch == 0) return IWDFT_OK;
+  if (!d_parent || !d_table || !d_lens || !d_free || !d_refs) return fail(IWDFT_ERR_ARG, "a device pointer is NULL");
+  if (unaligned(4, d_parent, d_keep, d_table, d_lens, d_free, d_refs, d_workspace)) return fail(IWDFT_ERR_ARG, "an int32 array is not 4-byte aligned");
+  if (need && (!d_workspace || workspace_bytes < need)) return fail(IWDFT_ERR_SIZE, "workspace has %zu bytes, %zu needed", d_workspace ? workspace_bytes : 0, need);
+  const ForkArgs a{{batch, log2_of(page_tokens), max_pages, n_pages, d_table, d_lens, d_free, d_refs}, d_parent, d_keep, need ? (int32_t*)d_workspace : nullptr};
+  return launched(launch_pages_fork(a, (hipStream_t)hip_stream), "page fork launch");
+}
+
+int iwdft_pages_resize_shared(int32_t page_tokens, int32_t n_pages, int32_t max_pages, const int32_t* d_want, int32_t batch, int32_t* d_table, int32_t* d_lens,
+                              int32_t* d_free, int32_t* d_refs, int32_t* d_starts, int32_t* d_slots, int32_t n_slots, int32_t* d_copies, void* hip_stream) {
+  const int rc = check_shared(page_tokens, n_pages, max_pages, batch);
+  if (rc != IWDFT_OK) return rc;
+  if (n_slots < 0 || n_slots > kMostCount) return fail(IWDFT_ERR_ARG, "n_slots = %d out of range", n_slots);
+  if (!d_free || !d_refs || !d_starts || (batch && (!d_want || !d_table || !d_lens || !d_copies)) || (n_slots && !d_slots)) return fail(IWDFT_ERR_ARG, "a device pointer is NULL");
+  if (unaligned(4, d_want, d_table, d_lens, d_free, d_refs, d_starts, d_slots) || unaligned(8, d_copies))
+    return fail(IWDFT_ERR_ARG, "an int32 array is not 4-byte aligned, or copies not 8-byte");
+  const GrowArgs a{{batch, log2_of(page_tokens), max_pages, n_pages, d_table, d_lens, d_free, d_refs}, d_want, n_slots, d_starts, d_slots, d_copies};
+  return launched(launch_pages_grow(a, (hipStream_t)hip_stream), "shared page table launch");
+}
+
+int iwdft_pages_copy(const iwdft_pages_desc* desc, int32_t layer, int32_t n_layers, const int32_t* d_copies, int32_t n_copies, const void* d_values,
+                     const int32_t* d_exponents, int32_t to_pages, void* d_to_values, int32_t* d_to_exponents, void* hip_stream) {
+  int rc = check_pages(desc, layer, n_layers);
+  if (rc != IWDFT_OK) return rc;
+  iwdft_pages_desc to = *desc;
+  to.n_pages = to_pages;
+  rc = check_pages(&to, layer, n_layers);
+  if (rc != IWDFT_OK) return rc;
+  const Pages source = pages_of(*desc, (void*)d_values, (int32_t*)d_exponents), target = pages_of(to, d_to_values, d_to_exponents);
+  if (n_copies < 0 || (double)pages_copy_units(source, 1, 1) * n_copies * n_layers * 4 > (double)kMostUnits) return fail(IWDFT_ERR_ARG, "n_copies = %d out of range", n_copies);
+  if (n_copies == 0) return IWDFT_OK;
+  if (!d_copies || !d_values || !d_exponents || !d_to_values || !d_to_exponents) return fail(IWDFT_ERR_ARG, "a device pointer is NULL");
+  if (unaligned(16, d_values, d_to_values) || unaligned(8, d_copies, d_exponents, d_to_exponents)) return fail(IWDFT_ERR_ARG, "values must be 16-byte aligned, exponents and copies 8-byte");
+  return launched(launch_pages_copy(source, target, layer, n_layers, d_copies, n_copies, (hipStream_t)hip_stream), "page copy launch");
+}
+
+int iwdft_pages_compact_bytes(int32_t n_pages, size_t* workspace_bytes) {
+  if (!workspace_bytes) return fail(IWDFT_ERR_ARG, "output pointer is NULL");
+  const int rc = check_page_size(16, n_pages, 1);
+  if (rc != IWDFT_OK) return rc;
+  *workspace_bytes = pages_compact_bytes(n_pages);
+  return IWDFT_OK;
+}
+
+int iwdft_pages_compact(int32_t page_tokens, int32_t n_pages, int32_t max_pages, int32_t batch, int32_t* d_table, int32_t* d_lens, int32_t* d_free,
+                        int32_t* d_refs, int32_t* d_moves, int32_t n_moves, void* d_workspace, size_t workspace_bytes, void* hip_stream) {
+  const int rc = check_shared(page_tokens, n_pages, max_pages, batch);
+  if (rc != IWDFT_OK) return rc;
+  if (n_moves < 0) return fail(IWDFT_ERR_ARG, "n_moves = %d: negative", n_moves);
+  const size_t need = pages_compact_bytes(n_pages);
+  if (!d_free || !d_refs || (batch && (!d_table || !d_lens)) || (n_moves && !d_moves)) return fail(IWDFT_ERR_ARG, "a device pointer is NULL");
+  if (unaligned(4, d_table, d_lens, d_free, d_refs) || unaligned(8, d_moves, d_workspace)) return fail(IWDFT_ERR_ARG, "an int32 array is not 4-byte aligned, or moves or workspace not 8-byte");
+  if (!d_workspace || workspace_bytes < need) return fail(IWDFT_ERR_SIZE, "workspace has %zu bytes, %zu needed", d_workspace ? workspace_bytes : 0, need);
+  const CompactArgs a{{batch, log2_of(page_tokens), max_pages, n_pages, d_table, d_lens, d_free, d_refs}, d_moves, n_moves, (int32_t*)d_workspace};
+  return launched(launch_pages_compact(a, (hipStream_t)hip_stream), "page compaction launch");
 }
 
 }  // extern "C"

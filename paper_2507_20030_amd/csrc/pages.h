@@ -68,6 +68,34 @@ __device__ __forceinline__ int scan(int x) {
 }
 __device__ __forceinline__ int last_lane(int x) { return __builtin_amdgcn_readlane(x, 63); }
 
+constexpr int kLanes = 64;
+// Sums of N numbers >= 0 over the threads before this one and over all threads of the workgroup; every thread calls it.  In two halves of 16 bits, whose sums over
+// a wave fit 32.
+template <int THREADS, int N>
+__device__ __forceinline__ void sums_before(const int (&x)[N], long long (&before)[N], long long (&all)[N], long long (*lds)[N]) {
+  const int lane = threadIdx.x % kLanes, wave = threadIdx.x / kLanes;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const int lo = scan(x[i] & 0xffff), hi = scan((int)((uint32_t)x[i] >> 16));
+    before[i] = ((long long)hi << 16) + lo;
+  }
+  __syncthreads();  // the last call's sums have been read
+  if (lane == kLanes - 1)
+#pragma unroll
+    for (int i = 0; i < N; ++i) lds[wave][i] = before[i];
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    long long sum = 0, mine = 0;
+#pragma unroll 4
+    for (int w = 0; w < THREADS / kLanes; ++w) {
+      mine = w == wave ? sum : mine;
+      sum += lds[w][i];
+    }
+    before[i] += mine - x[i], all[i] = sum;
+  }
+}
+
 struct ResizeArgs {
   const int32_t* want;
   int32_t batch, logP, max_pages, n_pages, n_slots;
@@ -78,6 +106,36 @@ constexpr int kResizeThreads = 1024, kResizeSmallThreads = 256;  // up to so man
 // One launch, without scratch, up to so many sequences and slots; one wave's scans up to kResizeWaveBatch sequences.
 constexpr int kResizeOneBatch = 1024, kResizeOneSlots = 2048, kResizeWaveBatch = 64;
 hipError_t launch_pages_resize(const ResizeArgs& a, hipStream_t st);
+
+// Pages that sequences share (pages_tables.hip).
+constexpr int kSharedBatch = 1024;  // sequences: a thread for each
+struct SharedTables {
+  int32_t batch, logP, max_pages, n_pages;
+  int32_t *table, *lens, *free, *refs;
+};
+struct GrowArgs {
+  SharedTables t;
+  const int32_t* want;
+  int32_t n_slots;
+  int32_t *starts, *slots, *copies;
+};
+struct ForkArgs {
+  SharedTables t;
+  const int32_t *parent, *keep;
+  int32_t* scratch;  // null: one launch
+};
+struct CompactArgs {
+  SharedTables t;
+  int32_t *moves, n_moves;
+  int32_t* scratch;
+};
+size_t pages_fork_bytes(int batch, int max_pages);
+size_t pages_compact_bytes(int n_pages);
+hipError_t launch_pages_grow(const GrowArgs& a, hipStream_t st);
+hipError_t launch_pages_fork(const ForkArgs& a, hipStream_t st);
+hipError_t launch_pages_compact(const CompactArgs& a, hipStream_t st);
+int64_t pages_copy_units(const Pages& S, int n_layers, int n);
+hipError_t launch_pages_copy(const Pages& from, const Pages& to, int layer, int n_layers, const int32_t* copies, int n, hipStream_t st);
 
 constexpr int64_t kMostUnits = ((int64_t)1 << 26) - 4;  // waves of a launch: 2^32 threads are too many
 int64_t pages_write_units(const Pages& S, int n_layers, int n_tokens);

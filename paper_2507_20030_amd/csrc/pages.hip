@@ -18,33 +18,6 @@ struct ResizeState {
   int count, released, taken, total;  // total: new tokens
 };
 
-// Sums of N numbers >= 0 over the threads before this one and over all threads of the workgroup; every thread calls it.  In two halves of 16 bits, whose sums over
-// a wave fit 32.
-template <int THREADS, int N>
-__device__ __forceinline__ void sums_before(const int (&x)[N], long long (&before)[N], long long (&all)[N], long long (*lds)[N]) {
-  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    const int lo = scan(x[i] & 0xffff), hi = scan((int)((uint32_t)x[i] >> 16));
-    before[i] = ((long long)hi << 16) + lo;
-  }
-  __syncthreads();  // the last call's sums have been read
-  if (lane == kWave - 1)
-#pragma unroll
-    for (int i = 0; i < N; ++i) lds[wave][i] = before[i];
-  __syncthreads();
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    long long sum = 0, mine = 0;
-#pragma unroll 4
-    for (int w = 0; w < THREADS / kWave; ++w) {
-      mine = w == wave ? sum : mine;
-      sum += lds[w][i];
-    }
-    before[i] += mine - x[i], all[i] = sum;
-  }
-}
-
 struct Change {
   int have, want;  // want: have where the sequence stays or cannot be so long
 };
