@@ -425,6 +425,20 @@ int iwdft_pages_compact(int32_t page_tokens, int32_t n_pages, int32_t max_pages,
 /* Its workspace (8-byte aligned). */
 int iwdft_pages_compact_bytes(int32_t n_pages, size_t* workspace_bytes);
 
+/* Attention as iwdft_pages_attn computes it, that reads the pages at the beginning of several rows of the table once for all of them: samples, beams and requests with one
+ * beginning.  A plan says who shares what; it is made once a step from what the step's calls are given, on the GPU, and serves every layer:
+ * calls on it take the same descriptor, n_layers (of a call), n_tokens, batch, windows and d_table (unchanged since).  A plan for other sizes or windows leaves
+ * d_out as it is, as starts that overlap do.  Any table is served; what is shared at any place of a row is found, but sequences whose pages have
+ * no order in common (more than 3 * batch changes of who shares) are read one by one.  Rows, windows, refusals and accuracy as there; up to 2^28 rows (token, head, layer) a call.
+ * Nothing in the workspace outlives a call; calls that may overlap in time need one each, and may share a plan. */
+int iwdft_pages_plan(const iwdft_pages_desc* desc, int32_t n_layers, const int32_t* d_starts, int32_t n_tokens, const int32_t* d_table, const int32_t* d_lens,
+                     int32_t batch, int32_t n_sink, int32_t n_recent, void* d_plan, size_t plan_bytes, void* hip_stream);
+int iwdft_pages_plan_bytes(const iwdft_pages_desc* desc, int32_t n_layers, int32_t batch, int32_t n_tokens, size_t* plan_bytes);
+int iwdft_pages_attn_shared(const iwdft_pages_desc* desc, int32_t layer, int32_t n_layers, const void* d_q, int32_t n_tokens, const void* d_plan, size_t plan_bytes,
+                            const int32_t* d_table, int32_t batch, const void* d_values, const int32_t* d_exponents, void* d_out, int32_t n_sink,
+                            int32_t n_recent, float scale, void* d_workspace, size_t workspace_bytes, void* hip_stream);
+int iwdft_pages_attn_shared_bytes(const iwdft_pages_desc* desc, int32_t n_layers, int32_t batch, int32_t n_tokens, size_t* workspace_bytes);
+
 const char* iwdft_last_error(void); /* thread-local, static storage, never NULL */
 
 #ifdef __cplusplus

@@ -34,6 +34,7 @@ EXPORTED = [
     "iwdft_select_bins", "iwdft_ablate_chunk", "iwdft_flush", "compressed_decode_attn_static", "iwdft_query_attn",
     "iwdft_pages_query_bytes", "iwdft_pages_resize", "iwdft_pages_resize_bytes", "iwdft_pages_write", "iwdft_pages_attn", "iwdft_pages_attn_bytes", "iwdft_pages_read",
     "iwdft_pages_fork", "iwdft_pages_fork_bytes", "iwdft_pages_resize_shared", "iwdft_pages_copy", "iwdft_pages_compact", "iwdft_pages_compact_bytes",
+    "iwdft_pages_plan", "iwdft_pages_plan_bytes", "iwdft_pages_attn_shared", "iwdft_pages_attn_shared_bytes",
 ]
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libiwdft.so")
@@ -113,6 +114,10 @@ def load_library() -> ctypes.CDLL:
     lib.iwdft_pages_copy.argtypes = [pp, i32, i32, vp, i32, vp, vp, i32, vp, vp, vp]
     lib.iwdft_pages_compact.argtypes = [i32, i32, i32, i32, vp, vp, vp, vp, vp, i32, vp, ctypes.c_size_t, vp]
     lib.iwdft_pages_compact_bytes.argtypes = [i32, szp]
+    lib.iwdft_pages_plan.argtypes = [pp, i32, vp, i32, vp, vp, i32, i32, i32, vp, ctypes.c_size_t, vp]
+    lib.iwdft_pages_plan_bytes.argtypes = [pp, i32, i32, i32, szp]
+    lib.iwdft_pages_attn_shared.argtypes = [pp, i32, i32, vp, i32, vp, ctypes.c_size_t, vp, i32, vp, vp, vp, i32, i32, f32, vp, ctypes.c_size_t, vp]
+    lib.iwdft_pages_attn_shared_bytes.argtypes = [pp, i32, i32, i32, szp]
     lib.iwdft_num_tokens.argtypes = [vp]
     lib.iwdft_num_tokens.restype = i64
     lib.iwdft_set_num_tokens.argtypes = [vp, i64]
@@ -680,6 +685,88 @@ def iwdft_pages_copy(copies, values, exponents, to_values=None, to_exponents=Non
     n = all_layers - layer if n_layers is None else n_layers
     rc = load_library().iwdft_pages_copy(_pages_ref(all_layers, n_pages, heads, heads, 128, P, 1, torch.float32), layer, n, copies.data_ptr(), copies.shape[0],
                                          values.data_ptr(), exponents.data_ptr(), to_pages, to_values.data_ptr(), to_exponents.data_ptr(), _stream_of(stream, index))
+    if rc:
+        _check(rc)
+
+
+@functools.lru_cache(maxsize=1024)
+def _shared_sizes(n_layers, batch, n_tokens, *desc):
+    """The descriptor, as the calls take it, the plan's bytes and the workspace's."""
+    ref, lib = _pages_ref(*desc), load_library()
+    return ref, _bytes_of(lib.iwdft_pages_plan_bytes, ref, n_layers, batch, n_tokens), _bytes_of(lib.iwdft_pages_attn_shared_bytes, ref, n_layers, batch, n_tokens)
+
+
+def iwdft_pages_plan_bytes(desc: iwdft_pages_desc, n_layers: int, batch: int, n_tokens: int) -> int:
+    return _bytes_of(load_library().iwdft_pages_plan_bytes, ctypes.byref(desc), n_layers, batch, n_tokens)
+
+
+def iwdft_pages_attn_shared_bytes(desc: iwdft_pages_desc, n_layers: int, batch: int, n_tokens: int) -> int:
+    return _bytes_of(load_library().iwdft_pages_attn_shared_bytes, ctypes.byref(desc), n_layers, batch, n_tokens)
+
+
+class PagesPlan:
+    """Who shares what in a step: iwdft_pages_plan's buffer and what it was made for."""
+
+    __slots__ = ("buffer", "n_layers", "n_tokens", "batch", "max_pages", "n_pages", "n_kv_heads", "n_q_heads", "page_tokens", "dtype", "n_sink", "n_recent")
+
+
+def iwdft_pages_plan(starts, table, lens, n_tokens: int, n_pages: int, n_kv_heads: int, n_q_heads: int, page_tokens: int, dtype: torch.dtype, n_layers: int = 1,
+                     n_sink: int = 0, n_recent: int = 0, stream=None, plan: Optional[PagesPlan] = None) -> PagesPlan:
+    """The plan of a step for iwdft_pages_attn_shared, whose calls have n_tokens rows and n_layers layers each; `plan`: an earlier one of these sizes and windows, made
+    anew in its buffer (as a captured graph needs it)."""
+    index, size = table.get_device(), table.shape
+    if len(size) != 2 or index < 0:
+        raise ValueError(f"table must be a device tensor [batch, max_pages], not {tuple(size)} on {table.device}")
+    if not (starts.dtype is table.dtype is lens.dtype is torch.int32 and lens.shape == size[:1] and starts.shape == (size[0] + 1,)
+            and index == starts.get_device() == lens.get_device() and starts.is_contiguous() and table.is_contiguous() and lens.is_contiguous()):
+        for name, t, shape in (("table", table, size), ("starts", starts, (size[0] + 1,)), ("lens", lens, size[:1])):
+            _expect(name, t, torch.int32, shape, table.device)
+    if dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError("dtype must be float32 or bfloat16")
+    if index != torch._C._cuda_getDevice():
+        with torch.cuda.device(index):
+            return iwdft_pages_plan(starts, table, lens, n_tokens, n_pages, n_kv_heads, n_q_heads, page_tokens, dtype, n_layers, n_sink, n_recent, stream, plan)
+    batch, max_pages = size
+    desc, need, _ = _shared_sizes(n_layers, batch, n_tokens, n_layers, n_pages, n_kv_heads, n_q_heads, 128, page_tokens, max_pages, dtype)
+    made_for = (n_layers, n_tokens, batch, max_pages, n_pages, n_kv_heads, n_q_heads, page_tokens, dtype, n_sink, n_recent)
+    if plan is None:
+        plan = PagesPlan()
+        plan.buffer = _scratch(need, table.device, stream, None)
+        for name, value in zip(PagesPlan.__slots__[1:], made_for):
+            setattr(plan, name, value)
+    elif made_for != tuple(getattr(plan, name) for name in PagesPlan.__slots__[1:]) or (need and plan.buffer.get_device() != index):
+        raise ValueError(f"the plan was made for {[(name, getattr(plan, name)) for name in PagesPlan.__slots__[1:]]}, not {made_for}")
+    buffer = plan.buffer
+    rc = load_library().iwdft_pages_plan(desc, n_layers, starts.data_ptr(), n_tokens, table.data_ptr(), lens.data_ptr(), batch, n_sink, n_recent,
+                                         buffer.data_ptr() if buffer is not None else None, buffer.nbytes if buffer is not None else 0, _stream_of(stream, index))
+    if rc:
+        _check(rc)
+    return plan
+
+
+def iwdft_pages_attn_shared(values, exponents, q, plan: PagesPlan, table, out, layer: int = 0, scale: float = 0.0, stream=None, workspace=None) -> None:
+    """iwdft_pages_attn with pages that sequences share read once: q, out [layers, tokens, query heads, 128], as many layers and tokens as the plan was made for."""
+    index, n_layers, n_pages, heads, P = _pool_sizes(values, exponents)
+    dtype, shape = _kv_dtype("q", q), q.shape
+    if not (shape == (plan.n_layers, plan.n_tokens, plan.n_q_heads, 128) and out.dtype is dtype is plan.dtype and shape == out.shape and table.dtype is torch.int32
+            and table.shape == (plan.batch, plan.max_pages) and (n_pages, heads, P) == (plan.n_pages, plan.n_kv_heads, plan.page_tokens)
+            and index == q.get_device() == out.get_device() == table.get_device() and (plan.buffer is None or plan.buffer.get_device() == index)
+            and q.is_contiguous() and out.is_contiguous() and table.is_contiguous()):
+        device = values.device
+        _expect("q", q, plan.dtype, (plan.n_layers, plan.n_tokens, plan.n_q_heads, 128), device)
+        _expect("out", out, dtype, shape, device)
+        _expect("table", table, torch.int32, (plan.batch, plan.max_pages), device)
+        raise ValueError(f"the plan was made for {plan.n_pages} pages of {plan.page_tokens} tokens and {plan.n_kv_heads} heads, not {tuple(values.shape)} on {device}")
+    if index != torch._C._cuda_getDevice():
+        with torch.cuda.device(index):
+            return iwdft_pages_attn_shared(values, exponents, q, plan, table, out, layer, scale, stream, workspace)
+    desc, _, need = _shared_sizes(plan.n_layers, plan.batch, plan.n_tokens, n_layers, n_pages, heads, plan.n_q_heads, 128, P, plan.max_pages, dtype)
+    ws = _scratch(need, values.device, stream, workspace) if need or workspace is not None else None
+    buffer = plan.buffer
+    rc = load_library().iwdft_pages_attn_shared(desc, layer, plan.n_layers, q.data_ptr(), plan.n_tokens, buffer.data_ptr() if buffer is not None else None,
+                                                buffer.nbytes if buffer is not None else 0, table.data_ptr(), plan.batch, values.data_ptr(), exponents.data_ptr(),
+                                                out.data_ptr(), plan.n_sink, plan.n_recent, scale, ws.data_ptr() if ws is not None else None,
+                                                ws.nbytes if ws is not None else 0, _stream_of(stream, index))
     if rc:
         _check(rc)
 

@@ -679,6 +679,24 @@ int check_attn(const iwdft_pages_desc* d, int32_t layer, int32_t n_layers, int32
 Pages pages_of(const iwdft_pages_desc& d, void* values, int32_t* exponents) {
   return Pages{d.n_pages, d.n_kv_heads, d.n_q_heads / d.n_kv_heads, log2_of(d.page_tokens), d.max_pages, (uint8_t*)values, exponents};
 }
+int check_windows(int32_t n_sink, int32_t n_recent) {
+  if (n_sink < 0 || n_recent < 0) return fail(IWDFT_ERR_ARG, "n_sink = %d, n_recent = %d: negative", n_sink, n_recent);
+  if (n_sink > 0 && n_recent == 0) return fail(IWDFT_ERR_ARG, "n_sink = %d without a window: n_recent = 0 lets every row see all tokens before it", n_sink);
+  return IWDFT_OK;
+}
+bool overlaps(const iwdft_pages_desc* d, int32_t n_layers, int32_t n_tokens, const void* q, const void* out) {
+  const size_t bytes = (size_t)n_layers * (size_t)n_tokens * (size_t)d->n_q_heads * kHeadDim * (d->kv_dtype == IWDFT_BF16 ? 2 : 4);
+  return (const char*)q < (const char*)out + bytes && (const char*)out < (const char*)q + bytes;
+}
+PagesAttn attn_of(const iwdft_pages_desc& d, int32_t layer, int32_t n_layers, int32_t batch, int32_t n_tokens, int32_t n_sink, int32_t n_recent, float scale,
+                  const void* q, void* out, const void* values, const int32_t* exponents) {
+  PagesAttn a{};
+  a.S = pages_of(d, (void*)values, (int32_t*)exponents);
+  a.layer = layer, a.n_layers = n_layers, a.batch = batch, a.n_tokens = n_tokens, a.n_sink = n_sink, a.n_recent = n_recent;
+  a.scale = (scale > 0.f ? scale : (float)(1.0 / std::sqrt((double)kHeadDim))) * 1.4426950408889634f;
+  a.q = q, a.out = out;
+  return a;
+}
 
 }  // namespace
 
@@ -1235,21 +1253,16 @@ int iwdft_pages_attn(const iwdft_pages_desc* desc, int32_t layer, int32_t n_laye
   const int rc = check_attn(desc, layer, n_layers, batch, n_tokens);
   if (rc != IWDFT_OK) return rc;
   const size_t need = pages_attn_bytes(pages_of(*desc, nullptr, nullptr), batch, n_tokens, desc->kv_dtype == IWDFT_BF16);
-  if (n_sink < 0 || n_recent < 0) return fail(IWDFT_ERR_ARG, "n_sink = %d, n_recent = %d: negative", n_sink, n_recent);
-  if (n_sink > 0 && n_recent == 0) return fail(IWDFT_ERR_ARG, "n_sink = %d without a window: n_recent = 0 lets every row see all tokens before it", n_sink);
+  if (const int bad = check_windows(n_sink, n_recent)) return bad;
   if (scale != scale) return fail(IWDFT_ERR_ARG, "scale is NaN");
   if (n_tokens == 0 || batch == 0) return IWDFT_OK;
   if (!d_q || !d_starts || !d_table || !d_lens || !d_values || !d_exponents || !d_out) return fail(IWDFT_ERR_ARG, "a device pointer is NULL");
   if (unaligned(16, d_q, d_out, d_values) || unaligned(4, d_starts, d_table, d_lens) || unaligned(8, d_exponents)) return fail(IWDFT_ERR_ARG, "%s", kPageAlignMsg);
-  const size_t bytes = (size_t)n_layers * (size_t)n_tokens * (size_t)desc->n_q_heads * kHeadDim * (desc->kv_dtype == IWDFT_BF16 ? 2 : 4);
-  if ((const char*)d_q < (const char*)d_out + bytes && (const char*)d_out < (const char*)d_q + bytes) return fail(IWDFT_ERR_ARG, "d_q and d_out overlap");
+  if (overlaps(desc, n_layers, n_tokens, d_q, d_out)) return fail(IWDFT_ERR_ARG, "d_q and d_out overlap");
   if (need && (!d_workspace || workspace_bytes < need)) return fail(IWDFT_ERR_SIZE, "workspace has %zu bytes, %zu needed", d_workspace ? workspace_bytes : 0, need);
   if (need && unaligned(256, d_workspace)) return fail(IWDFT_ERR_ARG, "d_workspace must be 256-byte aligned");
-  PagesAttn a{};
-  a.S = pages_of(*desc, (void*)d_values, (int32_t*)d_exponents);
-  a.layer = layer, a.n_layers = n_layers, a.batch = batch, a.n_tokens = n_tokens, a.n_sink = n_sink, a.n_recent = n_recent;
-  a.scale = (scale > 0.f ? scale : (float)(1.0 / std::sqrt((double)kHeadDim))) * 1.4426950408889634f;
-  a.q = d_q, a.out = d_out, a.starts = d_starts, a.table = d_table, a.lens = d_lens;
+  PagesAttn a = attn_of(*desc, layer, n_layers, batch, n_tokens, n_sink, n_recent, scale, d_q, d_out, d_values, d_exponents);
+  a.starts = d_starts, a.table = d_table, a.lens = d_lens;
   return launched(launch_pages_attn(a, desc->kv_dtype == IWDFT_BF16, need ? d_workspace : nullptr, (hipStream_t)hip_stream), "page attention launch");
 }
 
@@ -1337,6 +1350,69 @@ int iwdft_pages_compact(int32_t page_tokens, int32_t n_pages, int32_t max_pages,
   if (!d_workspace || workspace_bytes < need) return fail(IWDFT_ERR_SIZE, "workspace has %zu bytes, %zu needed", d_workspace ? workspace_bytes : 0, need);
   const CompactArgs a{{batch, log2_of(page_tokens), max_pages, n_pages, d_table, d_lens, d_free, d_refs}, d_moves, n_moves, (int32_t*)d_workspace};
   return launched(launch_pages_compact(a, (hipStream_t)hip_stream), "page compaction launch");
+}
+
+namespace {
+constexpr double kMostSharedRows = 1 << 28;  // rows of sums are counted in 32 bits
+int check_plan(const iwdft_pages_desc* d, int32_t layer, int32_t n_layers, int32_t batch, int32_t n_tokens, int32_t n_sink, int32_t n_recent) {
+  int rc = check_attn(d, layer, n_layers, batch, n_tokens);
+  if (rc == IWDFT_OK) rc = check_shared(d->page_tokens, d->n_pages, d->max_pages, batch);
+  if (rc != IWDFT_OK) return rc;
+  if ((double)n_tokens * d->n_q_heads * n_layers > kMostSharedRows) return fail(IWDFT_ERR_ARG, "n_tokens = %d out of range", n_tokens);
+  return check_windows(n_sink, n_recent);
+}
+}  // namespace
+
+int iwdft_pages_plan_bytes(const iwdft_pages_desc* desc, int32_t n_layers, int32_t batch, int32_t n_tokens, size_t* plan_bytes) {
+  if (!plan_bytes) return fail(IWDFT_ERR_ARG, "output pointer is NULL");
+  const int rc = check_plan(desc, 0, n_layers, batch, n_tokens, 0, 0);
+  if (rc != IWDFT_OK) return rc;
+  *plan_bytes = batch == 0 || n_tokens == 0 ? 0 : pages_plan_bytes(pages_of(*desc, nullptr, nullptr), n_layers, batch, n_tokens);
+  return IWDFT_OK;
+}
+
+int iwdft_pages_plan(const iwdft_pages_desc* desc, int32_t n_layers, const int32_t* d_starts, int32_t n_tokens, const int32_t* d_table, const int32_t* d_lens,
+                     int32_t batch, int32_t n_sink, int32_t n_recent, void* d_plan, size_t plan_bytes, void* hip_stream) {
+  const int rc = check_plan(desc, 0, n_layers, batch, n_tokens, n_sink, n_recent);
+  if (rc != IWDFT_OK) return rc;
+  if (n_tokens == 0 || batch == 0) return IWDFT_OK;
+  if (!d_starts || !d_table || !d_lens) return fail(IWDFT_ERR_ARG, "a device pointer is NULL");
+  if (unaligned(4, d_starts, d_table, d_lens)) return fail(IWDFT_ERR_ARG, "an int32 array is not 4-byte aligned");
+  PagesAttn a{};
+  a.S = pages_of(*desc, nullptr, nullptr);
+  a.n_layers = n_layers, a.batch = batch, a.n_tokens = n_tokens, a.n_sink = n_sink, a.n_recent = n_recent;
+  a.starts = d_starts, a.table = d_table, a.lens = d_lens;
+  const size_t need = pages_plan_bytes(a.S, n_layers, batch, n_tokens);
+  if (!d_plan || plan_bytes < need) return fail(IWDFT_ERR_SIZE, "plan has %zu bytes, %zu needed", d_plan ? plan_bytes : 0, need);
+  if (unaligned(256, d_plan)) return fail(IWDFT_ERR_ARG, "d_plan must be 256-byte aligned");
+  return launched(launch_pages_plan(a, desc->kv_dtype == IWDFT_BF16, d_plan, (hipStream_t)hip_stream), "page plan launch");
+}
+
+int iwdft_pages_attn_shared_bytes(const iwdft_pages_desc* desc, int32_t n_layers, int32_t batch, int32_t n_tokens, size_t* workspace_bytes) {
+  if (!workspace_bytes) return fail(IWDFT_ERR_ARG, "output pointer is NULL");
+  const int rc = check_plan(desc, 0, n_layers, batch, n_tokens, 0, 0);
+  if (rc != IWDFT_OK) return rc;
+  *workspace_bytes = pages_shared_bytes(pages_of(*desc, nullptr, nullptr), n_layers, batch, n_tokens);
+  return IWDFT_OK;
+}
+
+int iwdft_pages_attn_shared(const iwdft_pages_desc* desc, int32_t layer, int32_t n_layers, const void* d_q, int32_t n_tokens, const void* d_plan, size_t plan_bytes,
+                            const int32_t* d_table, int32_t batch, const void* d_values, const int32_t* d_exponents, void* d_out, int32_t n_sink,
+                            int32_t n_recent, float scale, void* d_workspace, size_t workspace_bytes, void* hip_stream) {
+  const int rc = check_plan(desc, layer, n_layers, batch, n_tokens, n_sink, n_recent);
+  if (rc != IWDFT_OK) return rc;
+  if (scale != scale) return fail(IWDFT_ERR_ARG, "scale is NaN");
+  if (n_tokens == 0 || batch == 0) return IWDFT_OK;
+  if (!d_q || !d_table || !d_values || !d_exponents || !d_out) return fail(IWDFT_ERR_ARG, "a device pointer is NULL");
+  if (unaligned(16, d_q, d_out, d_values) || unaligned(4, d_table) || unaligned(8, d_exponents)) return fail(IWDFT_ERR_ARG, "%s", kPageAlignMsg);
+  if (overlaps(desc, n_layers, n_tokens, d_q, d_out)) return fail(IWDFT_ERR_ARG, "d_q and d_out overlap");
+  PagesAttn a = attn_of(*desc, layer, n_layers, batch, n_tokens, n_sink, n_recent, scale, d_q, d_out, d_values, d_exponents);
+  a.table = d_table;
+  const size_t plan_need = pages_plan_bytes(a.S, n_layers, batch, n_tokens), need = pages_shared_bytes(a.S, n_layers, batch, n_tokens);
+  if (!d_plan || plan_bytes < plan_need) return fail(IWDFT_ERR_SIZE, "plan has %zu bytes, %zu needed", d_plan ? plan_bytes : 0, plan_need);
+  if (!d_workspace || workspace_bytes < need) return fail(IWDFT_ERR_SIZE, "workspace has %zu bytes, %zu needed", d_workspace ? workspace_bytes : 0, need);
+  if (unaligned(256, d_plan, d_workspace)) return fail(IWDFT_ERR_ARG, "d_plan and d_workspace must be 256-byte aligned");
+  return launched(launch_pages_shared(a, desc->kv_dtype == IWDFT_BF16, d_plan, d_workspace, (hipStream_t)hip_stream), "shared page attention launch");
 }
 
 }  // extern "C"

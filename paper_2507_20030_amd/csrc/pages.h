@@ -165,4 +165,10 @@ size_t pages_attn_bytes(const Pages& S, int batch, int n_tokens, bool bf16);    
 size_t pages_attn_most_bytes(const Pages& S, int batch, int n_tokens, bool bf16);  // of any call of up to these sizes
 hipError_t launch_pages_attn(PagesAttn a, bool bf16, void* ws, hipStream_t st);
 
+// Attention over pages that sequences share (pages_shared.hip); of the arguments the plan takes all but the pool, q and out.
+size_t pages_plan_bytes(const Pages& S, int n_layers, int batch, int n_tokens);
+size_t pages_shared_bytes(const Pages& S, int n_layers, int batch, int n_tokens);
+hipError_t launch_pages_plan(const PagesAttn& a, bool bf16, void* plan, hipStream_t st);
+hipError_t launch_pages_shared(const PagesAttn& a, bool bf16, const void* plan, void* ws, hipStream_t st);
+
 }  // namespace iwdft

@@ -1,0 +1,585 @@
+// Attention over pages that sequences share: every page is read once for all sequences that hold it.
+//
+// A run is a range of places in the table and the sequences that hold the same pages there, as many as there are and the same ones from its first place to
+// its last.  The rows of all of them -- (new token, query head of the KV head) -- go through the run's tokens together: blocks of rows and parts of
+// tokens, as pages_rows.h has them.  A row's runs follow each other along its sequence, so its softmax is joined from their parts:
+//   m = max m_i,  o = sum 2^(m_i - m) o_i / sum 2^(m_i - m) l_i.
+// Who shares what is read off the table, whatever brought it about: the plan.  It is made once a step, for all layers:
+//   1. for every place the sequences that hold the same page there, named by the first of them; where a set begins, ends or changes;
+//   2. the runs, cut into parts of about the same work, and where their rows, parts and sums lie;
+//   3. for every run its rows, for every sequence its runs, for every workgroup what it does.
+// Tables without an order in what they share -- pages at several places, sets that change at every place -- have more runs than the plan holds; then nothing is
+// shared, and the result is the same.
+#include "pages_rows.h"
+
+namespace iwdft {
+
+namespace {
+
+// ------------------------------------------------------------------------------------------------ the plan
+constexpr int kPlaces = 4;         // of a wave in the first launch
+constexpr int kShareThreads = 1024;
+constexpr int kMostEvents = 3 * kSharedBatch;  // where a set begins or ends; sequences that fork have fewer than 3 each
+constexpr int kSharedParts = 512;  // of a call: two workgroups on each CU
+constexpr int kSharedFew = 32;     // runs of up to so many rows go to few_rows
+constexpr int kPlanMark = 0x49574446;
+
+struct PlanHead {
+  int32_t mark, n_layers, H, G, logP, max_pages, batch, n_tokens, n_sink, n_recent, few_rows;
+  int32_t n_runs, many, few, slots, unshared;  // items of each kind; rows of sums of a (layer, head)
+};
+struct Run {
+  int32_t leader, from, to, tokens;  // whose row of the table, places, new tokens of all its sequences
+  int32_t mem, item, np, slot;       // first entry of the rows, first item, parts, first row of sums
+};
+struct Item {
+  int32_t leader, from, to, mem;
+  int32_t row0, rows, part, np;
+  int32_t slot, kind, pad0, pad1;
+};
+static_assert(sizeof(PlanHead) == 64 && sizeof(Run) == 32 && sizeof(Item) == 48, "");
+
+struct PlanSizes {
+  int places, chunks, events, chain;
+  int64_t mem, items, slots;
+};
+// n: of rows of sums of all (layer, head)
+int64_t most_slots(const Pages& S, int n_layers, int n_tokens) {
+  const int64_t rows = (int64_t)n_tokens * S.G;
+  return (2 * kSharedParts + 64) * std::min<int64_t>(128, (rows + 15) / 16 * 16) + 4 * rows * n_layers * S.H;
+}
+PlanSizes sizes_of(const Pages& S, int n_layers, int batch, int n_tokens) {
+  PlanSizes z;
+  z.places = (S.max_pages + kPlaces - 1) / kPlaces * kPlaces;
+  z.chunks = z.places / kPlaces;
+  z.events = 3 * batch;
+  z.chain = std::min(S.max_pages, z.events);
+  z.mem = n_tokens + std::min<int64_t>((int64_t)n_tokens * std::min(S.max_pages, batch), 1 << 20);
+  z.slots = most_slots(S, n_layers, n_tokens) / ((int64_t)n_layers * S.H);
+  z.items = std::min(z.mem * S.G / 16 + z.events + 2 * (2 * kSharedParts + 64), z.slots);  // each has a row of sums
+  return z;
+}
+struct Plan {
+  PlanHead* head;
+  Item* items;
+  Run* runs;
+  int4* chain;       // [sequence][chain]: first row of sums, parts, rows of a part
+  int2* mem;         // (row of q, position)
+  int2* events;      // [chunk][events]: sequence and place, new tokens of its set (-1: it is none's first)
+  uint16_t* names;   // [sequence][places]: the first sequence that holds the same page there
+  int32_t *counts, *chained;  // events of a chunk; runs of a sequence
+  int2* owner;                // of a row of q: its sequence (-1: none), which of its new tokens it is
+};
+template <class Take>
+void lay_out(const PlanSizes& z, int batch, int n_tokens, Plan* p, Take take) {
+  p->head = (PlanHead*)take(sizeof(PlanHead));
+  p->items = (Item*)take(z.items * sizeof(Item));
+  p->runs = (Run*)take(z.events * sizeof(Run));
+  p->chain = (int4*)take((size_t)batch * z.chain * sizeof(int4));
+  p->mem = (int2*)take(z.mem * sizeof(int2));
+  p->events = (int2*)take((size_t)z.chunks * z.events * sizeof(int2));
+  p->names = (uint16_t*)take((size_t)batch * z.places * sizeof(uint16_t));
+  p->counts = (int32_t*)take(z.chunks * sizeof(int32_t));
+  p->chained = (int32_t*)take(batch * sizeof(int32_t));
+  p->owner = (int2*)take(n_tokens * sizeof(int2));
+}
+
+struct PlanArgs {
+  Pages S;
+  int32_t n_layers, batch, n_tokens, n_sink, n_recent, few_rows;
+  const int32_t *starts, *table, *lens;
+  PlanSizes z;
+  Plan p;
+};
+struct News {
+  int len, first, n;  // tokens, first new one (row of q), new ones
+};
+__device__ __forceinline__ News news_of(const PlanArgs& a, int b) {
+  News s;
+  s.len = min(max(a.lens[b], 0), a.S.max_pages << a.S.logP);
+  s.first = min(max(a.starts[b], 0), a.n_tokens);
+  s.n = min(max(a.starts[b + 1], s.first), a.n_tokens) - s.first;
+  return s;
+}
+__device__ __forceinline__ int pages_of_news(const PlanArgs& a, const News& s) { return s.n ? page_count(s.len, a.S.logP) : 0; }  // who brings nothing is not asked
+__device__ __forceinline__ void in_wave() {  // LDS that the lanes of a wave exchange
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
+// A wave has kPlaces places, and looks at the one before them; its lanes have the sequences in turn.  Equal pages meet in a hash table in LDS.
+template <int EACH, int WAVES>
+__global__ __launch_bounds__(WAVES* kWave) void plan_sets_kernel(PlanArgs a) {
+  constexpr int kRows = EACH * kWave, kSlots = 2 * kRows;
+  __shared__ int32_t keys[WAVES][kSlots], firsts[WAVES][kSlots], tokens[WAVES][kRows], changes[WAVES][kRows];
+  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, chunk = blockIdx.x * WAVES + wave, c0 = chunk * kPlaces;
+  for (int64_t t = (int64_t)blockIdx.x * (WAVES * kWave) + threadIdx.x; t < a.n_tokens; t += (int64_t)gridDim.x * (WAVES * kWave)) a.p.owner[t] = make_int2(-1, 0);
+  if (chunk >= a.z.chunks) return;
+  int pages[EACH], news[EACH], most = 0;
+#pragma unroll
+  for (int i = 0; i < EACH; ++i) {
+    const int x = lane + kWave * i;
+    const News s = x < a.batch ? news_of(a, x) : News{0, 0, 0};
+    pages[i] = pages_of_news(a, s), news[i] = s.n, most = max(most, pages[i]);
+  }
+#pragma unroll
+  for (int d = 1; d < kWave; d <<= 1) most = max(most, __shfl_xor(most, d));
+  int n = 0;
+  if (c0 < most) {
+    int prev[EACH];
+    uint32_t name[EACH][kPlaces / 2];
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+      prev[i] = -2;
+#pragma unroll
+      for (int c = 0; c < kPlaces / 2; ++c) name[i][c] = 0xffffffffu;
+    }
+#pragma unroll
+    for (int cc = -1; cc < kPlaces; ++cc) {
+      const int c = c0 + cc;
+      if (c < 0 || c >= most) continue;
+      for (int i = lane; i < kSlots; i += kWave) keys[wave][i] = -1, firsts[wave][i] = kRows;
+      for (int i = lane; i < kRows; i += kWave) tokens[wave][i] = 0, changes[wave][i] = 0;
+      in_wave();
+      int cur[EACH], at[EACH];
+#pragma unroll
+      for (int i = 0; i < EACH; ++i) {
+        const int x = lane + kWave * i;
+        cur[i] = -1, at[i] = -1;
+        if (c < pages[i]) {
+          const int page = a.table[(int64_t)x * a.S.max_pages + c];
+          cur[i] = x;  // a page that is not there is shared with nobody
+          if ((uint32_t)page < (uint32_t)a.S.n_pages) {
+            uint32_t s = ((uint32_t)page * 2654435769u) >> 8;
+            for (;; ++s) {  // there are twice as many slots as sequences
+              s &= kSlots - 1;
+              const int was = atomicCAS(&keys[wave][s], -1, page);
+              if (was == -1 || was == page) break;
+            }
+            atomicMin(&firsts[wave][s], x);
+            at[i] = (int)s;
+          }
+        }
+      }
+      in_wave();
+#pragma unroll
+      for (int i = 0; i < EACH; ++i)
+        if (at[i] >= 0) cur[i] = firsts[wave][at[i]];
+      if (cc >= 0) {
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) {
+          if (cur[i] == prev[i]) continue;
+          if (cur[i] >= 0) changes[wave][cur[i]] = 1;
+          if (prev[i] >= 0) changes[wave][prev[i]] = 1;
+        }
+        in_wave();
+#pragma unroll
+        for (int i = 0; i < EACH; ++i)
+          if (cur[i] >= 0 && changes[wave][cur[i]]) atomicAdd(&tokens[wave][cur[i]], news[i]);
+        in_wave();
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) {
+          const int x = lane + kWave * i;
+          const bool leads = cur[i] == x, event = changes[wave][x] && (leads || (prev[i] == x && cur[i] >= 0));  // where its row ends is known
+          const unsigned long long m = __ballot(event);
+          const int to = n + __popcll(m & ((1ull << lane) - 1));
+          if (event && to < a.z.events) a.p.events[(int64_t)chunk * a.z.events + to] = make_int2(x | cc << 16, leads ? tokens[wave][x] : -1);
+          n += __popcll(m);
+          name[i][cc / 2] = cc % 2 ? (name[i][cc / 2] & 0xffffu) | (uint32_t)cur[i] << 16 : (name[i][cc / 2] & 0xffff0000u) | ((uint32_t)cur[i] & 0xffffu);
+        }
+        in_wave();
+      }
+#pragma unroll
+      for (int i = 0; i < EACH; ++i) prev[i] = cur[i];
+    }
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+      const int x = lane + kWave * i;
+      if (x < a.batch) *(uint2*)(a.p.names + (int64_t)x * a.z.places + c0) = make_uint2(name[i][0], name[i][1]);
+    }
+  }
+  if (lane == 0) a.p.counts[chunk] = n;
+}
+
+// Tokens of a run that rows at position p see, about: the work is shared out by it.
+__device__ __forceinline__ int tokens_seen(const PlanArgs& a, int t0, int t1, int p) {
+  if (!a.n_recent) return t1 - t0;
+  const int near = max(t1 - max(t0, p - min(a.n_recent, p)), 0), sinks = max(min(t1, a.n_sink) - t0, 0);
+  return min(near + sinks, t1 - t0);
+}
+
+// One workgroup: the runs from the events, which lie in the order of their places.
+__global__ __launch_bounds__(kShareThreads) void plan_share_kernel(PlanArgs a) {
+  __shared__ int32_t leader[kMostEvents], from[kMostEvents], news[kMostEvents], tiles[kMostEvents], base[kShareThreads];
+  __shared__ long long lds1[kShareThreads / kWave][1], lds3[kShareThreads / kWave][3];
+  __shared__ float lds_f[kShareThreads / kWave][4];
+  const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
+  const float slices = (float)(a.n_layers * a.S.H);
+  {  // starts that overlap: rows would belong to several sequences, nothing is done
+    const int x[1] = {tid < a.batch ? news_of(a, tid).n : 0};
+    long long before[1], all[1];
+    sums_before<kShareThreads>(x, before, all, lds1);
+    if (all[0] > a.n_tokens) {
+      if (tid == 0) *a.p.head = PlanHead{};
+      return;
+    }
+  }
+  int n = 0;
+  bool unshared = false;
+  for (int c0 = 0; c0 < a.z.chunks && !unshared; c0 += kShareThreads) {
+    const int c = c0 + tid, mine = c < a.z.chunks ? a.p.counts[c] : 0;
+    const int x[1] = {mine};
+    long long before[1], all[1];
+    sums_before<kShareThreads>(x, before, all, lds1);
+    unshared = __syncthreads_or(mine > a.z.events) || n + all[0] > a.z.events;
+    if (unshared) break;
+    base[tid] = (int)before[0];
+    __syncthreads();
+    for (int e = tid; e < (int)all[0]; e += kShareThreads) {
+      int lo = 0, hi = kShareThreads;  // largest with base <= e
+      while (hi - lo > 1) {
+        const int m = (lo + hi) >> 1;
+        if (base[m] <= e) lo = m;
+        else hi = m;
+      }
+      const int2 v = a.p.events[(int64_t)(c0 + lo) * a.z.events + e - base[lo]];
+      leader[n + e] = v.x & 0xffff, from[n + e] = (c0 + lo) * kPlaces + (v.x >> 16), news[n + e] = v.y;
+    }
+    n += (int)all[0];
+    __syncthreads();
+  }
+  for (;; unshared = true) {
+    if (unshared) {
+      __syncthreads();
+      n = a.batch;
+      for (int i = tid; i < n; i += kShareThreads) leader[i] = i, from[i] = 0, news[i] = news_of(a, i).n;
+      __syncthreads();
+    }
+    const auto end_of = [&](int i) {
+      for (int k = i + 1; k < n && !unshared; ++k)
+        if (leader[k] == leader[i]) return from[k];
+      return pages_of_news(a, news_of(a, leader[i]));
+    };
+    const auto rows_of = [&](int i) { return max(news[i], 0) * a.S.G; };
+    const auto is_many = [&](int rows) { return rows > kSharedFew; };
+    const auto blocks_of = [&](int rows) { return is_many(rows) ? (rows + Many::rows - 1) / Many::rows : (rows + a.few_rows - 1) / a.few_rows; };
+    float sums[4] = {0.f, 0.f, 0.f, 0.f};  // tiles times blocks and blocks, of the few and of the many
+    for (int i = tid; i < n; i += kShareThreads) {
+      const int to = end_of(i), rows = rows_of(i), tile = is_many(rows) ? Many::tile : Few<1>::tile;
+      const int seen = tokens_seen(a, from[i] << a.S.logP, to << a.S.logP, news_of(a, leader[i]).len - 1);
+      if (to <= from[i]) news[i] = 0;
+      tiles[i] = to > from[i] && rows ? max((seen + tile - 1) / tile, 1) : 0;
+      const float blocks = tiles[i] ? (float)blocks_of(rows) : 0.f;
+      const int k = is_many(rows) ? 2 : 0;
+      sums[k] += blocks * (float)tiles[i], sums[k + 1] += blocks;
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+#pragma unroll
+      for (int d = 1; d < kWave; d <<= 1) sums[k] += __shfl_xor(sums[k], d);
+      if (lane == 0) lds_f[wave][k] = sums[k];
+    }
+    __syncthreads();
+    float per[2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      float sum = 0.f, blocks = 0.f;
+      for (int w = 0; w < kShareThreads / kWave; ++w) sum += lds_f[w][2 * k], blocks += lds_f[w][2 * k + 1];
+      sum *= slices, blocks *= slices;
+      const float alone = fminf(ceilf(sum / (float)kCus), (float)(k ? Many::pair : Few<1>::pair));
+      per[k] = fminf(fmaxf(fmaxf((float)kLeastTiles, alone), ceilf(sum / fmaxf((float)kSharedParts - blocks, 0.5f * kSharedParts))), 1e9f);
+    }
+    __syncthreads();
+    // where everything lies; longer parts where the sums of all of them would not fit
+    const auto parts_of = [&](int i) { return i < n && tiles[i] ? max(1, (int)ceilf((float)tiles[i] / per[is_many(rows_of(i))])) : 0; };
+    long long mem, items, slots;
+    for (;;) {
+      mem = items = slots = 0;
+      for (int i0 = 0; i0 < n; i0 += kShareThreads) {
+        const int i = i0 + tid, np = parts_of(i), rows = np ? rows_of(i) : 0;
+        const int x[3] = {np ? news[i] : 0, min(blocks_of(rows), 1 << 20) * min(np, 1 << 10), (int)min((long long)rows * np, 0x7fffffffll)};
+        long long before[3], all[3];
+        sums_before<kShareThreads>(x, before, all, lds3);
+        mem += all[0], items += all[1], slots += all[2];
+      }
+      if ((slots <= a.z.slots && items <= a.z.items) || per[0] > 1e8f) break;
+      per[0] *= 2.f, per[1] *= 2.f;
+    }
+    if (!unshared && (slots > a.z.slots || items > a.z.items || mem > a.z.mem)) continue;
+
+    mem = items = slots = 0;
+    long long many = 0;
+    for (int pass = 0; pass < 2; ++pass) {  // items of the many first
+      for (int i0 = 0; i0 < n; i0 += kShareThreads) {
+        const int i = i0 + tid;
+        const bool here = i < n && is_many(rows_of(i)) == (pass == 0);
+        const int np = here ? parts_of(i) : 0, rows = np ? rows_of(i) : 0;
+        const int x[3] = {np ? news[i] : 0, blocks_of(rows) * np, rows * np};
+        long long before[3], all[3];
+        sums_before<kShareThreads>(x, before, all, lds3);
+        if (here)
+          a.p.runs[i] = Run{leader[i], from[i], np ? end_of(i) : from[i], np ? news[i] : 0, (int)(mem + before[0]), (int)(items + before[1]), np, (int)(slots + before[2])};
+        mem += all[0], items += all[1], slots += all[2];
+      }
+      if (pass == 0) many = items;
+    }
+    if (tid == 0)
+      *a.p.head = PlanHead{kPlanMark, a.n_layers, a.S.H, a.S.G, a.S.logP, a.S.max_pages, a.batch, a.n_tokens, a.n_sink, a.n_recent, a.few_rows,
+                           n, (int)many, (int)(items - many), (int)slots, unshared ? 1 : 0};
+    return;
+  }
+}
+
+// A wave for each sequence: its runs, in order, and its rows in them.  A wave for each run: its items.
+__global__ __launch_bounds__(256) void plan_rows_kernel(PlanArgs a) {
+  const int lane = threadIdx.x % kWave, unit = blockIdx.x * 4 + threadIdx.x / kWave;
+  const PlanHead& head = *a.p.head;
+  const int n = head.n_runs;
+  const bool unshared = head.unshared != 0;
+  const auto holds = [&](int x, const News& s, const Run& r) {
+    return s.n > 0 && r.from < page_count(s.len, a.S.logP) && (unshared ? r.leader == x : (int)a.p.names[(int64_t)x * a.z.places + r.from] == r.leader);
+  };
+  if (unit < a.batch) {
+    const int x = unit;
+    const News s = news_of(a, x);
+    int k = 0;
+    for (int i0 = 0; i0 < n && s.n; i0 += kWave) {
+      const int i = i0 + lane;
+      const Run mine = i < n ? a.p.runs[i] : Run{};
+      unsigned long long in = __ballot(mine.tokens > 0 && holds(x, s, mine));
+      for (; in; in &= in - 1, ++k) {
+        const Run r = a.p.runs[i0 + __builtin_ctzll(in)];
+        int before = 0;
+        if (!unshared)
+          for (int y0 = 0; y0 < x; y0 += kWave) {
+            const int y = y0 + lane;
+            if (y < x) {
+              const News o = news_of(a, y);
+              before += holds(y, o, r) ? o.n : 0;
+            }
+          }
+#pragma unroll
+        for (int d = 1; d < kWave; d <<= 1) before += __shfl_xor(before, d);
+        for (int t = lane; t < s.n; t += kWave)
+          if (r.mem + before + t < a.z.mem) a.p.mem[r.mem + before + t] = make_int2(s.first + t, s.len - s.n + t);
+        if (lane == 0 && k < a.z.chain) a.p.chain[(int64_t)x * a.z.chain + k] = make_int4(r.slot + before * a.S.G, r.np, r.tokens * a.S.G, 0);
+      }
+    }
+    for (int t = lane; t < s.n; t += kWave) a.p.owner[s.first + t] = make_int2(x, t);
+    if (lane == 0) a.p.chained[x] = min(k, a.z.chain);
+  } else {
+    const int waves = gridDim.x * 4 - a.batch;
+    for (int i = unit - a.batch; i < n; i += waves) {
+      const Run r = a.p.runs[i];
+      const int rows = r.tokens * a.S.G, size = rows > kSharedFew ? Many::rows : a.few_rows, blocks = (rows + size - 1) / size;
+      for (int k = lane; k < blocks * r.np; k += kWave) {
+        if (r.item + k >= a.z.items) break;
+        const int part = k / blocks, block = blocks - 1 - (k - part * blocks), row0 = block * size;  // blocks that read the same tokens side by side
+        a.p.items[r.item + k] = Item{r.leader, r.from, r.to, r.mem, row0, min(size, rows - row0), part, r.np, r.slot + part * rows + row0, 0, 0, 0};
+      }
+    }
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ attention
+struct SharedAttn {
+  PagesAttn a;
+  Plan p;
+  PlanSizes z;
+  int32_t few_rows;
+  float* part;
+  float2* stat;
+};
+__device__ __forceinline__ bool is_for(const PlanHead& h, const SharedAttn& s) {
+  const PagesAttn& a = s.a;
+  return h.mark == kPlanMark && h.n_layers == a.n_layers && h.H == a.S.H && h.G == a.S.G && h.logP == a.S.logP && h.max_pages == a.S.max_pages && h.batch == a.batch &&
+         h.n_tokens == a.n_tokens && h.n_sink == a.n_sink && h.n_recent == a.n_recent && h.few_rows == s.few_rows;
+}
+
+// The items of one kind: see pages_rows.h for what the kernels ask.
+class Items {
+ public:
+  float* part;
+  float2* stat;
+
+  __device__ __forceinline__ Items(const SharedAttn& s, bool many, int lane)
+      : part(s.part), stat(s.stat), s(s), lane(lane), first(many ? 0 : s.p.head->many), n(many ? s.p.head->many : s.p.head->few), slots(s.p.head->slots),
+        slices((uint32_t)(s.a.n_layers * s.a.S.H)) {}
+
+  struct Block {
+    const int32_t* table;
+    int layer, h, rows, p_lo, p_hi, from_lo, from_hi, part, np, last_page, base, last_token, mem, row0, lh, slot;
+    static constexpr bool whole = false;
+  };
+  __device__ __forceinline__ uint32_t count() const { return (uint32_t)n * slices; }
+  __device__ __forceinline__ Block block(uint32_t x) const {
+    const PagesAttn& a = s.a;
+    const int4* at = (const int4*)(s.p.items + first + x / slices);
+    const int4 u = at[0], v = at[1], w = at[2];
+    Block k;
+    k.lh = (int)(x % slices), k.layer = (int)((uint32_t)k.lh / (uint32_t)a.S.H), k.h = k.lh - k.layer * a.S.H;
+    const auto uni = [](int y) { return __builtin_amdgcn_readfirstlane(y); };
+    k.table = a.table + (int64_t)uni(u.x) * a.S.max_pages, k.base = uni(u.y) << a.S.logP, k.last_page = uni(u.z) - 1, k.last_token = (uni(u.z) << a.S.logP) - 1;
+    k.mem = uni(u.w), k.row0 = uni(v.x), k.rows = uni(v.y), k.part = uni(v.z), k.np = uni(v.w), k.slot = uni(w.x);
+    int lo = 0x7fffffff, hi = -1;
+    for (int r = lane; r < k.rows; r += kWave) {
+      const int p = max(s.p.mem[k.mem + (int)((uint32_t)(k.row0 + r) / (uint32_t)a.S.G)].y, -1);
+      lo = min(lo, p), hi = max(hi, p);
+    }
+#pragma unroll
+    for (int d = 1; d < kWave; d <<= 1) lo = min(lo, __shfl_xor(lo, d)), hi = max(hi, __shfl_xor(hi, d));
+    lo = uni(lo), hi = uni(hi);
+    k.from_lo = window_from(a, lo), k.from_hi = window_from(a, hi), k.p_lo = min(lo, k.last_token), k.p_hi = min(hi, k.last_token);
+    return k;
+  }
+  __device__ __forceinline__ RowAt row(const Block& k, int r) const {
+    const PagesAttn& a = s.a;
+    const uint32_t m = (uint32_t)(k.row0 + min(r, k.rows - 1)), G = (uint32_t)a.S.G;
+    const int token = (int)(m / G);
+    const int2 at = s.p.mem[k.mem + token];
+    const int pos = max(at.y, -1);
+    return RowAt{((int64_t)k.layer * a.n_tokens + at.x) * (a.S.H * a.S.G) + k.h * a.S.G + (int)(m - (uint32_t)token * G), min(pos, k.last_token), window_from(a, pos)};
+  }
+  __device__ __forceinline__ WaveRows wave_rows(const Block& k, int wave) const { return WaveRows{32 * wave < k.rows ? k.p_hi : -1, k.from_lo}; }
+  __device__ __forceinline__ int64_t slot(const Block& k) const { return (int64_t)k.lh * slots + k.slot; }
+
+ private:
+  const SharedAttn& s;
+  int lane, first, n, slots;
+  uint32_t slices;
+};
+
+template <bool BF16, int R, bool MANY>
+__global__ __launch_bounds__(kWaves* kWave, BF16 ? 2 : (R == 1 && !MANY ? 2 : 1)) void shared_attn_kernel(SharedAttn s) {
+  if (!is_for(*s.p.head, s)) return;
+  uint32_t x = blockIdx.x;
+  if constexpr (MANY) {
+    const uint32_t n = many_rows<BF16>(s.a, Items(s, true, threadIdx.x % kWave), x, gridDim.x);
+    if (x < n) x += (n - x + gridDim.x - 1) / gridDim.x * gridDim.x;  // its next turn
+    x -= n;
+  }
+  if constexpr (R > 0) few_rows<BF16, R, kWaves>(s.a, Items(s, false, threadIdx.x % kWave), x, gridDim.x);
+}
+
+// A row's parts, run by run.  Few rows: a workgroup for each, its waves take the parts in turn.  Many: a wave for each.
+constexpr int64_t kManyShared = 4096;
+template <bool BF16>
+__global__ __launch_bounds__(kWaves* kWave) void shared_join_kernel(SharedAttn s, int64_t all, int many) {
+  __shared__ float2 sums[kWaves][kWave], stats[kWaves];
+  const PagesAttn& a = s.a;
+  if (!is_for(*s.p.head, s)) return;
+  const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), slots = s.p.head->slots, G = a.S.G;
+  for (int64_t x = many ? (int64_t)blockIdx.x * kWaves + wave : blockIdx.x; x < all; x += (int64_t)gridDim.x * (many ? kWaves : 1)) {
+    const int lh = (int)(x / ((int64_t)a.n_tokens * G)), r = (int)(x - (int64_t)lh * a.n_tokens * G), token = (int)((uint32_t)r / (uint32_t)G);
+    const int2 owner = s.p.owner[token];
+    const int b = __builtin_amdgcn_readfirstlane(owner.x), mine = __builtin_amdgcn_readfirstlane(owner.y) * G + r - token * G;
+    if (b < 0) continue;  // behind the last sequence
+    const int n = s.p.chained[b], k0 = many ? 0 : wave, dk = many ? 1 : kWaves;
+    float m = -FLT_MAX, l = 0.f;
+    float2 o = make_float2(0.f, 0.f);
+    const auto add = [&](float2 st, float2 v) {  // (reference, sum of weights), sum
+      const float up = fmaxf(m, st.x), f = __builtin_amdgcn_exp2f(0.5f * (m - up)), g = __builtin_amdgcn_exp2f(0.5f * (st.x - up));
+      o.x = o.x * (f * f) + v.x * (g * g), o.y = o.y * (f * f) + v.y * (g * g), l = l * f * f + st.y * g * g, m = up;
+    };
+    for (int i = 0; i < n; ++i) {
+      const int4 run = s.p.chain[(int64_t)b * s.z.chain + i];
+      const int64_t slot = (int64_t)lh * slots + run.x + mine;
+#pragma unroll 8
+      for (int k = k0; k < run.y; k += dk) {
+        const int64_t at = slot + (int64_t)k * run.z;
+        add(s.stat[at], *(const float2*)(s.part + at * kHeadDim + 2 * lane));
+      }
+    }
+    if (!many) {
+      sums[wave][lane] = o;
+      if (lane == 0) stats[wave] = make_float2(m, l);
+      __syncthreads();
+      m = -FLT_MAX, l = 0.f, o = make_float2(0.f, 0.f);
+#pragma unroll
+      for (int i = 0; i < kWaves; ++i) add(stats[i], sums[i][lane]);
+      __syncthreads();
+      if (wave) continue;
+    }
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    const int layer = (int)((uint32_t)lh / (uint32_t)a.S.H), h = lh - layer * a.S.H;
+    const int64_t to = (((int64_t)layer * a.n_tokens + token) * (a.S.H * G) + h * G + r - token * G) * kHeadDim + 2 * lane;
+    if constexpr (BF16) *(uint32_t*)((uint16_t*)a.out + to) = (uint32_t)f32_to_bf16(result<true>(o.x, inv)) | (uint32_t)f32_to_bf16(result<true>(o.y, inv)) << 16;
+    else *(float2*)((float*)a.out + to) = make_float2(result<false>(o.x, inv), result<false>(o.y, inv));
+  }
+}
+
+int few_rows_of(const Pages& S, int n_tokens, bool bf16) { return bf16 && (int64_t)n_tokens * S.G > 16 ? 32 : 16; }
+
+Plan plan_at(const PlanSizes& z, int batch, int n_tokens, void* at) {
+  Plan p;
+  size_t done = 0;
+  lay_out(z, batch, n_tokens, &p, [&](size_t bytes) {
+    char* here = (char*)at + done;
+    done += (bytes + 255) / 256 * 256;
+    return here;
+  });
+  return p;
+}
+
+template <bool BF16, int R, bool MANY>
+hipError_t launch_shared(const SharedAttn& s, hipStream_t st) {
+  const int64_t lh = (int64_t)s.a.n_layers * s.a.S.H, rows = (int64_t)s.a.n_tokens * s.a.S.G;
+  const int64_t grid = (MANY ? 2 : 1) * kSharedParts + lh * (2 * s.a.batch + rows / 32);
+  shared_attn_kernel<BF16, R, MANY><<<(unsigned)std::min<int64_t>(grid, 1 << 20), kWaves * kWave, 0, st>>>(s);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+size_t pages_plan_bytes(const Pages& S, int n_layers, int batch, int n_tokens) {
+  Plan p;
+  size_t done = 0;
+  lay_out(sizes_of(S, n_layers, batch, n_tokens), batch, n_tokens, &p, [&](size_t bytes) {
+    done += (bytes + 255) / 256 * 256;
+    return (void*)nullptr;
+  });
+  return done;
+}
+size_t pages_shared_bytes(const Pages& S, int n_layers, int batch, int n_tokens) {
+  return batch == 0 || n_tokens == 0 ? 0 : (size_t)most_slots(S, n_layers, n_tokens) * (kHeadDim * sizeof(float) + sizeof(float2));
+}
+
+hipError_t launch_pages_plan(const PagesAttn& g, bool bf16, void* plan, hipStream_t st) {
+  PlanArgs a{g.S, g.n_layers, g.batch, g.n_tokens, g.n_sink, g.n_recent, few_rows_of(g.S, g.n_tokens, bf16), g.starts, g.table, g.lens, {}, {}};
+  a.z = sizes_of(g.S, g.n_layers, g.batch, g.n_tokens);
+  a.p = plan_at(a.z, g.batch, g.n_tokens, plan);
+  const auto grid = [&](int waves) { return (unsigned)((a.z.chunks + waves - 1) / waves); };
+  if (g.batch <= kWave) plan_sets_kernel<1, 4><<<grid(4), 4 * kWave, 0, st>>>(a);
+  else if (g.batch <= 4 * kWave) plan_sets_kernel<4, 4><<<grid(4), 4 * kWave, 0, st>>>(a);
+  else plan_sets_kernel<16, 2><<<grid(2), 2 * kWave, 0, st>>>(a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  plan_share_kernel<<<1, kShareThreads, 0, st>>>(a);
+  e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  plan_rows_kernel<<<(unsigned)((2 * g.batch + 64 + 3) / 4), 256, 0, st>>>(a);
+  return hipGetLastError();
+}
+
+hipError_t launch_pages_shared(const PagesAttn& g, bool bf16, const void* plan, void* ws, hipStream_t st) {
+  SharedAttn s{};
+  s.a = g, s.z = sizes_of(g.S, g.n_layers, g.batch, g.n_tokens), s.p = plan_at(s.z, g.batch, g.n_tokens, (void*)plan);
+  s.few_rows = few_rows_of(g.S, g.n_tokens, bf16);
+  s.part = (float*)ws, s.stat = (float2*)(s.part + most_slots(g.S, g.n_layers, g.n_tokens) * kHeadDim);
+  const int64_t rows = (int64_t)g.n_tokens * g.S.G;
+  hipError_t e;
+  if (bf16) e = rows <= 16 ? launch_shared<true, 1, false>(s, st) : rows <= kSharedFew ? launch_shared<true, 2, false>(s, st) : launch_shared<true, 2, true>(s, st);
+  else {
+    e = rows > kSharedFew ? launch_shared<false, 0, true>(s, st) : hipSuccess;
+    if (e == hipSuccess) e = launch_shared<false, 1, false>(s, st);
+  }
+  if (e != hipSuccess) return e;
+  const int64_t all = rows * g.n_layers * g.S.H;
+  const bool many = all > kManyShared;
+  const unsigned grid = (unsigned)std::min<int64_t>(many ? (all + kWaves - 1) / kWaves : all, 4096);
+  if (bf16) shared_join_kernel<true><<<grid, kWaves * kWave, 0, st>>>(s, all, many);
+  else shared_join_kernel<false><<<grid, kWaves * kWave, 0, st>>>(s, all, many);
+  return hipGetLastError();
+}
+
+}  // namespace iwdft

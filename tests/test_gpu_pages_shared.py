@@ -6,6 +6,7 @@ import torch
 from oracle import pages_oracle as po
 from oracle.pages_shared_oracle import Tables
 from paper_2507_20030_amd import binding as B
+from test_gpu_pages import near
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -182,3 +183,214 @@ def test_copy_far_into_a_long_pool():
     values[0, 159_999], exponents[0, 159_999] = 3, 4
     B.iwdft_pages_copy(ints([[159_999, 140_000], [159_999, 2]]), values, exponents)
     assert (values[0, [2, 140_000]] == 3).all() and (exponents[0, [2, 140_000]] == 4).all() and int((values.view(-1)[:: 1 << 13] != 0).sum()) == 3 * 4
+
+
+# ------------------------------------------------------------------------------------------------------------------ attention
+class Pool:
+    """Sequences (parent or -1, tokens shared with it, length) over a pool full of tokens; pages in random order."""
+
+    def __init__(self, rng, forest, P, heads=2, layers=1):
+        rows = []
+        n = 0
+        for parent, keep, length in forest:
+            row = rows[parent][:keep // P] if parent >= 0 else []
+            fresh = -(-length // P) - len(row)
+            rows.append(row + list(range(n, n + fresh)))
+            n += fresh
+        self.P, self.n_pages = P, n + 3
+        order = rng.permutation(self.n_pages)
+        self.lens = np.array([length for _, _, length in forest], np.int32)
+        self.table = np.full((len(forest), max(1, max(map(len, rows))) + 1), -1, np.int32)
+        for b, row in enumerate(rows):
+            self.table[b, :len(row)] = order[row]
+        self.store = po.Store(layers, self.n_pages, heads, P)
+        full = rng.normal(size=(layers, self.n_pages * P, heads, 128)) * 10.0 ** rng.uniform(-1, 1, size=128)
+        self.store.write(full, rng.normal(size=full.shape) * 10.0 ** rng.uniform(-2, 2, size=(1, full.shape[1], 1, 1)), np.arange(self.n_pages * P))
+        self.upload()
+
+    def upload(self):
+        self.values, self.exponents, self.d_table, self.d_lens = (dev(x) for x in (self.store.packed(), self.store.exponents, self.table, self.lens))
+
+
+def plan_of(pool, starts, n, G, dtype, layers=1, **kw):
+    return B.iwdft_pages_plan(ints(starts), pool.d_table, pool.d_lens, n, pool.n_pages, pool.store.raw.shape[2], pool.store.raw.shape[2] * G, pool.P, DT[dtype],
+                              n_layers=layers, **kw)
+
+
+def attend(pool, rng, news, G, dtype, layer=0, layers=1, pad=0, scale=None, q=None, **kw):
+    starts = np.concatenate([[0], np.cumsum(news)]).astype(np.int32)
+    n = int(starts[-1]) + pad
+    q = dev(rng.normal(size=(layers, n, pool.store.raw.shape[2] * G, 128))).to(DT[dtype]) if q is None else q
+    out = torch.full_like(q, 7.0)
+    plan = plan_of(pool, starts, n, G, dtype, layers, **kw)
+    B.iwdft_pages_attn_shared(pool.values, pool.exponents, q, plan, pool.d_table, out, layer, scale=scale or 0.0)
+    ref, *rest = pool.store.attend(f64(q), starts, pool.table, pool.lens, layer, scale=scale, **kw)
+    if pad:
+        assert (out[:, starts[-1]:] == 7.0).all()
+        ref, out = ref[:, :starts[-1]], out[:, :starts[-1]]
+        rest = [r[:, :starts[-1]] for r in rest]
+    near(out, ref, *rest, dtype)
+    return out
+
+
+def forest_of(rng, kind, batch, prompt, tail):
+    got = [(-1, 0, prompt + int(rng.integers(1, tail + 1)))]
+    for b in range(1, batch):
+        own = int(rng.integers(1, tail + 1))
+        if kind == "samples":
+            got.append((0, prompt, prompt + own))
+        elif kind == "nested":
+            parent = int(rng.integers(b))
+            keep = int(rng.integers(0, got[parent][2] + 1))
+            got.append((parent, keep, keep + own))
+        elif kind == "chain":  # each begins with all of the one before
+            got.append((b - 1, got[-1][2], got[-1][2] + own))
+        elif kind == "cut":  # nothing of their own: shorter and shorter beginnings
+            got.append((0, prompt * (batch - b) // batch, prompt * (batch - b) // batch))
+        else:
+            got.append((-1, 0, int(rng.integers(0, prompt + own))))
+    return got
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("P", [16, 32, 64, 128])
+@pytest.mark.parametrize("kind", ["samples", "nested", "chain", "cut", "alone"])
+def test_attention_of_who_shares_what(kind, P, dtype):
+    rng = np.random.default_rng(P + len(kind))
+    forest = forest_of(rng, kind, 7, 300, 90)
+    attend(Pool(rng, forest, P), rng, [1 if n else 0 for _, _, n in forest], 4, dtype, pad=2)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("batch,G,heads", [(1, 1, 1), (3, 5, 1), (4, 4, 1), (5, 7, 1), (8, 4, 2), (17, 8, 1), (9, 16, 1), (33, 8, 1), (70, 2, 2), (300, 1, 1)])
+def test_attention_rows(batch, G, heads, dtype):
+    """From one row to blocks of rows in each of the kernels, several sequences to a row of LDS."""
+    rng = np.random.default_rng(batch + G)
+    forest = forest_of(rng, "samples", batch, 120, 20 if batch > 40 else 200)
+    attend(Pool(rng, forest, 32, heads=heads), rng, [1] * batch, G, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("kind,news,G", [("samples", [1, 5, 1, 3], 4), ("nested", [9, 0, 1, 40, 2, 7], 2), ("chain", [0, 70, 1, 1], 3), ("cut", [1, 130, 0, 2], 8), ("samples", [400, 1, 1], 1)])
+def test_attention_drafts_and_prompts(kind, news, G, dtype):
+    """New tokens that see each other, more of them than the sequence is long, rows behind the last one."""
+    rng = np.random.default_rng(sum(news))
+    attend(Pool(rng, forest_of(rng, kind, len(news), 310, 50), 16), rng, news, G, dtype, pad=3, scale=0.1)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("sink,recent", [(0, 1), (0, 40), (10, 50), (33, 64), (1, 1), (64, 1000), (500, 3), (0, 2 ** 31 - 1), (2 ** 31 - 1, 5)])
+def test_attention_windows(sink, recent, dtype):
+    rng = np.random.default_rng(sink % 1000 + recent % 1000)
+    forest = forest_of(rng, "samples", 6, 400, 150) + [(-1, 0, 12), (2, 390, 391), (0, 64, 64), (0, 0, 0)]
+    attend(Pool(rng, forest, 16), rng, [1, 7, 12, 1, 1, 2, 12, 1, 1, 0], 2, dtype, n_sink=sink, n_recent=recent)
+    attend(Pool(rng, forest_of(rng, "nested", 40, 200, 60), 32, heads=1), rng, [1] * 40, 4, dtype, n_sink=sink, n_recent=recent)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_attention_layers(dtype):
+    rng = np.random.default_rng(3)
+    pool = Pool(rng, forest_of(rng, "samples", 12, 200, 40), 32, heads=3, layers=4)
+    attend(pool, rng, [1] * 12, 4, dtype, layer=1, layers=2)
+    attend(pool, rng, [1] * 12, 4, dtype, layer=3)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("batch,W,n_pages", [(5, 9, 4), (40, 30, 3), (70, 12, 50), (3, 200, 2)])
+def test_attention_any_table(batch, W, n_pages, dtype):
+    """Pages at several places, sets that change at every place and come together again, pages that are not there: more changes than a plan holds, too."""
+    rng = np.random.default_rng(batch)
+    pool = Pool(rng, [(-1, 0, 16 * n_pages)], 16)
+    pool.table = rng.integers(-1, n_pages + 4, size=(batch, W)).astype(np.int32)
+    pool.table[batch // 2:, : W // 2] = pool.table[0, : W // 2]
+    pool.lens = rng.integers(0, W * 16 + 1, size=batch).astype(np.int32)
+    pool.upload()
+    attend(pool, rng, rng.integers(0, 3, size=batch), 2, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_attention_does_not_see_what_is_masked(dtype):
+    """NaN and the largest values behind the sequences' ends, in pages of nobody, and in shared tokens that only some of the rows see."""
+    rng = np.random.default_rng(9)
+    for batch, G in ((3, 2), (20, 4)):
+        forest = [(-1, 0, 100)] + [(0, 100, 100 + 3 * b) for b in range(1, batch)]
+        pool = Pool(rng, forest, 32)
+        raw = pool.store.raw
+        held = set()
+        for b in range(batch):
+            n = int(pool.lens[b])
+            raw[0, pool.table[b, (n - 1) // 32], :, :, n % 32 or 32:] = 0x7f
+            held.update(pool.table[b, :-(-n // 32)].tolist())
+        for p in set(range(pool.n_pages)) - held:
+            raw[0, p] = 0xff
+        raw[0, pool.table[0, 1], 1, 1, 8, 40] = 0x7f      # V, token 40, channel 40: within the window of the first sequence only
+        pool.upload()
+        out = attend(pool, rng, [1] * batch, G, dtype, n_sink=2, n_recent=60)
+        nan = torch.isnan(out.float())
+        assert nan[0, 0, G:, 40].all() and int(nan.sum()) == G
+        out = attend(pool, rng, [1] * batch, G, dtype)
+        assert int(torch.isnan(out.float()).sum()) == G * batch
+
+
+def test_attention_one_sequence_for_each_row_of_a_large_table():
+    rng = np.random.default_rng(2)
+    forest = forest_of(rng, "nested", 1024, 40, 5)
+    attend(Pool(rng, forest, 16, heads=1), rng, [1 if n else 0 for _, _, n in forest], 1, "bf16")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_attention_long_and_as_page_attention(dtype):
+    """Thousands of tokens, many parts: against iwdft_pages_attn, which is within its roundings of the definition."""
+    for batch, prompt, G, H, window in ((16, 9000, 4, 8, {}), (2, 30000, 8, 2, {}), (64, 5000, 2, 4, dict(n_sink=5, n_recent=3000)), (3, 40, 1, 1, {})):
+        g = torch.Generator(device=DEV).manual_seed(batch)
+        P, rng = 64, np.random.default_rng(batch)
+        forest = forest_of(rng, "nested" if batch == 64 else "samples", batch, prompt, 700)
+        t = Both(batch, 200 if batch == 64 else 600, 9000, P, rng)
+        t.resize([forest[0][2]] + [0] * (batch - 1), 100_000)
+        for b, (parent, keep, length) in enumerate(forest[1:], 1):
+            ids, keeps = np.arange(batch), np.full(batch, -1)
+            ids[b], keeps[b] = parent, keep
+            t.o.fork(ids, keeps)
+            want = np.full(batch, -1)
+            want[b] = length
+            t.o.resize(want, 100_000)
+        table, lens = ints(t.o.table), ints(t.o.lens)
+        values = torch.randint(0, 127, (1, 9000, H, 2, P * 128), dtype=torch.uint8, device=DEV, generator=g) ^ (torch.randint(0, 2, (1, 9000, H, 2, P * 128), dtype=torch.uint8, device=DEV, generator=g) << 7)
+        exponents = torch.randint(-8, -4, (1, 9000, H, 2), dtype=torch.int32, device=DEV, generator=g)
+        q = torch.randn((1, batch, G * H, 128), device=DEV, generator=g).to(DT[dtype]) * 0.02
+        starts = ints(range(batch + 1))
+        ref, out = torch.zeros_like(q), torch.zeros_like(q)
+        B.iwdft_pages_attn(values, exponents, q, starts, table, lens, ref, **window)
+        plan = B.iwdft_pages_plan(starts, table, lens, batch, 9000, H, G * H, P, DT[dtype], **window)
+        B.iwdft_pages_attn_shared(values, exponents, q, plan, table, out)
+        err = float((out.double() - ref.double()).norm() / ref.double().norm())
+        assert err < (2.0 ** -7 if dtype == "bf16" else 2.0 ** -17), err  # two roundings of the result; both sums' 22 bits and what sums of tens of thousands of tokens lose
+        again = torch.zeros_like(q)
+        B.iwdft_pages_attn_shared(values, exponents, q, plan, table, again)
+        assert torch.equal(out, again)
+
+
+def test_plans_that_do_not_fit():
+    """Another plan's sizes, starts that overlap: out stays; the binding refuses what it can see."""
+    rng = np.random.default_rng(1)
+    pool = Pool(rng, forest_of(rng, "samples", 4, 100, 20), 16)
+    q = torch.randn((1, 4, 4, 128), device=DEV)
+    out = torch.full_like(q, 7.0)
+    starts = ints([0, 3, 1, 4, 4])
+    plan = B.iwdft_pages_plan(starts, pool.d_table, pool.d_lens, 4, pool.n_pages, 2, 4, 16, torch.float32)
+    B.iwdft_pages_attn_shared(pool.values, pool.exponents, q, plan, pool.d_table, out)
+    assert (out == 7.0).all()
+    good = B.iwdft_pages_plan(ints(range(5)), pool.d_table, pool.d_lens, 4, pool.n_pages, 2, 4, 16, torch.float32, plan=plan)
+    assert good is plan
+    plan.n_recent = 5                                           # not what the buffer holds
+    B.iwdft_pages_attn_shared(pool.values, pool.exponents, q, plan, pool.d_table, out)
+    assert (out == 7.0).all()
+    plan.n_recent = 0
+    B.iwdft_pages_attn_shared(pool.values, pool.exponents, q, plan, pool.d_table, out)
+    assert not (out == 7.0).all(dim=-1).any()
+    for bad in (dict(q=q[:, :3].contiguous()), dict(q=q.bfloat16()), dict(table=pool.d_table[:3]), dict(out=out[:, :, :2]), dict(values=pool.values[:, :-1].contiguous(), exponents=pool.exponents[:, :-1].contiguous())):
+        args = {**dict(values=pool.values, exponents=pool.exponents, q=q, plan=plan, table=pool.d_table, out=out), **bad}
+        with pytest.raises(ValueError):
+            B.iwdft_pages_attn_shared(**args)
+    with pytest.raises(ValueError):
+        B.iwdft_pages_plan(ints(range(5)), pool.d_table, pool.d_lens, 4, pool.n_pages, 2, 4, 16, torch.float32, n_recent=9, plan=plan)
