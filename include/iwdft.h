@@ -395,14 +395,14 @@ int iwdft_pages_read(const iwdft_pages_desc* desc, int32_t layer, int32_t n_laye
  *   refs       int32 [n_pages]: how many sequences hold a page; at first 0.  All of them hold it at the same place, and all pages before it.
  *   copies     int32 [n][2], 8-byte aligned: (from, to) pages; -1: none.
  * iwdft_pages_write, _attn and _read serve such tables as they are; what changes tables has to be one of these calls, which keep refs (iwdft_pages_resize frees a page whose other
- * holders live on).  This build: up to 1024 sequences; batch * max_pages < 2^31. */
+ * holders live on).  This build: up to 1024 sequences; batch * max_pages <= 2^30. */
 
 /* Sequence b becomes the first d_keep[b] tokens (NULL, negative or more: all) of what sequence d_parent[b] (outside [0, batch): b itself) was before the call; all
  * at once, so that rows may change places.  Nothing is copied: the pages are shared.  Pages that no sequence holds any more go back on the stack, as if those who
  * leave them gave them back one by one, from the last page of the last sequence on.  Needs no page and cannot fail. */
 int iwdft_pages_fork(int32_t page_tokens, int32_t n_pages, int32_t max_pages, const int32_t* d_parent, const int32_t* d_keep, int32_t batch, int32_t* d_table,
                      int32_t* d_lens, int32_t* d_free, int32_t* d_refs, void* d_workspace, size_t workspace_bytes, void* hip_stream);
-/* Its workspace: 0 for tables of up to 8192 entries. */
+/* Its workspace (8-byte aligned): 0 for tables of up to 8192 entries. */
 int iwdft_pages_fork_bytes(int32_t batch, int32_t max_pages, size_t* workspace_bytes);
 
 /* iwdft_pages_resize where pages are shared.  A page is free once its last holder has given it back.  A sequence that grows into a page that others hold leaves it to

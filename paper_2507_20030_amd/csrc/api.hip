@@ -667,7 +667,7 @@ int check_shared(int32_t page_tokens, int32_t n_pages, int32_t max_pages, int32_
   if (rc != IWDFT_OK) return rc;
   if (batch < 0) return fail(IWDFT_ERR_ARG, "batch = %d: negative", batch);
   if (batch > kSharedBatch) return fail(IWDFT_ERR_UNSUPPORTED, "batch = %d: this build shares pages among up to %d sequences", batch, kSharedBatch);
-  if ((int64_t)batch * max_pages > 0x7fffffff) return fail(IWDFT_ERR_ARG, "%d sequences of %d pages: too many entries", batch, max_pages);
+  if ((int64_t)batch * max_pages > (1 << 30)) return fail(IWDFT_ERR_ARG, "%d sequences of %d pages: too many entries", batch, max_pages);
   return IWDFT_OK;
 }
 int check_attn(const iwdft_pages_desc* d, int32_t layer, int32_t n_layers, int32_t batch, int32_t n_tokens) {
@@ -1297,7 +1297,8 @@ int iwdft_pages_fork(int32_t page_tokens, int32_t n_pages, int32_t max_pages, co
   const size_t need = pages_fork_bytes(batch, max_pages);
   if (batch == 0) return IWDFT_OK;
   if (!d_parent || !d_table || !d_lens || !d_free || !d_refs) return fail(IWDFT_ERR_ARG, "a device pointer is NULL");
-  if (unaligned(4, d_parent, d_keep, d_table, d_lens, d_free, d_refs, d_workspace)) return fail(IWDFT_ERR_ARG, "an int32 array is not 4-byte aligned");
+  if (unaligned(4, d_parent, d_keep, d_table, d_lens, d_free, d_refs) || unaligned(8, d_workspace))
+    return fail(IWDFT_ERR_ARG, "an int32 array is not 4-byte aligned, or the workspace not 8-byte");
   if (need && (!d_workspace || workspace_bytes < need)) return fail(IWDFT_ERR_SIZE, "workspace has %zu bytes, %zu needed", d_workspace ? workspace_bytes : 0, need);
   const ForkArgs a{{batch, log2_of(page_tokens), max_pages, n_pages, d_table, d_lens, d_free, d_refs}, d_parent, d_keep, need ? (int32_t*)d_workspace : nullptr};
   return launched(launch_pages_fork(a, (hipStream_t)hip_stream), "page fork launch");

@@ -14,11 +14,11 @@ namespace {
 
 constexpr int kWave = kLanes;
 
-// refs are changed by atomics, which the L2 carries out: read past the L1.
-__device__ __forceinline__ int32_t refs_now(const int32_t* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
-__device__ __forceinline__ void refs_add(int32_t* p, int x) { __hip_atomic_fetch_add(p, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
-__device__ __forceinline__ void refs_least(int32_t* p, int x) { __hip_atomic_fetch_min(p, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
-__device__ __forceinline__ void refs_set(int32_t* p, int x) { __hip_atomic_store(p, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+// refs are changed by atomics of one workgroup (a page is held at one place, which one workgroup looks after), in its L2: read past the L1.
+__device__ __forceinline__ int32_t refs_now(const int32_t* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP); }
+__device__ __forceinline__ void refs_add(int32_t* p, int x) { __hip_atomic_fetch_add(p, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP); }
+__device__ __forceinline__ void refs_least(int32_t* p, int x) { __hip_atomic_fetch_min(p, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP); }
+__device__ __forceinline__ void refs_set(int32_t* p, int x) { __hip_atomic_store(p, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP); }
 __device__ __forceinline__ void all_here() {  // what the workgroup has written, in memory too, is there for all of it; its atomics have arrived
   __threadfence_block();
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -49,6 +49,8 @@ __device__ __forceinline__ int sum_before(int x, int* all, long long (*lds)[1]) 
 // One workgroup, a thread for each sequence.  A sequence whose last page has room, and which others hold, leaves that page before it grows: it gets a new one and
 // an entry in copies.  Where all holders leave in this call, the last of them stays.  It is held to the pages that are left as those before it
 // are: had one of them been refused, the page would still be shared.
+constexpr int kForkEntries = 8192;  // of a small table: in LDS, one launch
+constexpr int kGiven = 8;  // entries of a thread that are on their way at a time
 template <int THREADS>
 __global__ __launch_bounds__(THREADS) void pages_grow_kernel(GrowArgs a) {
   __shared__ long long lds1[THREADS / kWave][1], lds2[THREADS / kWave][2];
@@ -72,26 +74,48 @@ __global__ __launch_bounds__(THREADS) void pages_grow_kernel(GrowArgs a) {
   if (gone > 0) {
     base[b] = gone_before, first[b] = get;
     __syncthreads();
-    const auto entry = [&](int o) {
-      const int s = last_not_above(base, THREADS, o), j = first[s] + o - base[s];
-      const int p = t.table[(int64_t)s * t.max_pages + min(j, t.max_pages - 1)];
-      return is_page(t, p) ? p : -1;
-    };
-    for (int o = b; o < gone; o += THREADS)
-      if (const int p = entry(o); p >= 0) refs_add(t.refs + p, -1);
-    all_here();
-    for (int o = b; o < gone; o += THREADS)
-      if (const int p = entry(o); p >= 0 && refs_now(t.refs + p) <= 0) refs_least(t.refs + p, o - gone);
-    all_here();
-    for (int e0 = 0; e0 < gone; e0 += THREADS) {
-      const int o = gone - 1 - e0 - b, p = o >= 0 ? entry(o) : -1;
-      const bool goes = p >= 0 && refs_now(t.refs + p) == o - gone;
-      int n;
-      const int at = released + sum_before<THREADS>(goes ? 1 : 0, &n, lds1);
-      if (goes) {
-        if (count + at < t.n_pages) t.free[1 + count + at] = p;
-        refs_set(t.refs + p, 0);
+    int page[kGiven];
+    const auto entries = [&](int e0) {  // of this thread, from the end
+#pragma unroll
+      for (int i = 0; i < kGiven; ++i) {
+        const int o = gone - 1 - e0 - kGiven * b - i, s = last_not_above(base, THREADS, max(o, 0));
+        const int p = o >= 0 ? t.table[(int64_t)s * t.max_pages + min(first[s] + o - base[s], t.max_pages - 1)] : -1;
+        page[i] = is_page(t, p) ? p : -1;
       }
+    };
+    const auto mark = [&](int e0, int i) { return -1 - e0 - kGiven * b - i; };  // the later an entry is given back the smaller
+    for (int e0 = 0; e0 < gone; e0 += kGiven * THREADS) {
+      entries(e0);
+#pragma unroll
+      for (int i = 0; i < kGiven; ++i)
+        if (page[i] >= 0) refs_add(t.refs + page[i], -1);
+    }
+    all_here();
+    for (int e0 = 0; e0 < gone; e0 += kGiven * THREADS) {
+      if (gone > kGiven * THREADS) entries(e0);
+      int left[kGiven];
+#pragma unroll
+      for (int i = 0; i < kGiven; ++i) left[i] = page[i] >= 0 ? refs_now(t.refs + page[i]) : 1;
+#pragma unroll
+      for (int i = 0; i < kGiven; ++i)
+        if (left[i] <= 0) refs_least(t.refs + page[i], mark(e0, i));
+    }
+    all_here();
+    for (int e0 = 0; e0 < gone; e0 += kGiven * THREADS) {
+      if (gone > kGiven * THREADS) entries(e0);
+      int left[kGiven], mine_goes = 0, n;
+#pragma unroll
+      for (int i = 0; i < kGiven; ++i) left[i] = page[i] >= 0 ? refs_now(t.refs + page[i]) : 0;
+#pragma unroll
+      for (int i = 0; i < kGiven; ++i) mine_goes += left[i] == mark(e0, i);
+      int at = count + released + sum_before<THREADS>(mine_goes, &n, lds1);
+#pragma unroll
+      for (int i = 0; i < kGiven; ++i)
+        if (left[i] == mark(e0, i)) {
+          if (at < t.n_pages) t.free[1 + at] = page[i];
+          ++at;
+          refs_set(t.refs + page[i], 0);
+        }
       released += n;
     }
     released = min(released, t.n_pages - count);
@@ -187,41 +211,36 @@ __global__ __launch_bounds__(256) void pages_slots_kernel(GrowArgs a) {
 }
 
 // ------------------------------------------------------------------------------------------------ forking
-// Every row takes its parent's entries, all at once: a workgroup has some places of all rows, reads them whole and then writes.  A page is held at one place, so
-// who gives it up meets in one workgroup.
-constexpr int kForkEntries = 8192;  // in LDS
-constexpr int kForkGroups = 64;     // workgroups: each leaves a count for every row
+// Every row takes its parent's entries, all at once: whoever has a place reads it of all rows and then writes.  A page is held at one place, so those who leave
+// and enter it meet there.
 
 struct ForkRows {
   int32_t parent[kSharedBatch], had[kSharedBatch], get[kSharedBatch], len[kSharedBatch];
 };
 template <int THREADS>
-__device__ __forceinline__ int fork_rows(const ForkArgs& a, ForkRows& r) {  // returns the most pages of a row, before or after
-  int most = 0;
+__device__ __forceinline__ void fork_rows(const ForkArgs& a, ForkRows& r) {
   for (int b = threadIdx.x; b < a.t.batch; b += THREADS) {
     int p = a.parent[b];
     p = (uint32_t)p < (uint32_t)a.t.batch ? p : b;
     const int keep = a.keep ? a.keep[b] : -1, len = length_of(a.t, p), n = keep < 0 ? len : min(keep, len);
     r.parent[b] = p, r.len[b] = n, r.had[b] = page_count(length_of(a.t, b), a.t.logP), r.get[b] = page_count(n, a.t.logP);
-    most = max(most, max(r.had[b], r.get[b]));
   }
-  return most;
 }
 
-// Places [j0, j0 + n) of all rows; drop(b, j, page) for every entry that a row had: page where it goes back on the stack, else -1.
-template <int THREADS, class Drop>
-__device__ __forceinline__ void fork_places(const ForkArgs& a, const ForkRows& r, int32_t* lds, int j0, int n, Drop drop) {
+// Small tables, all of them in LDS; left in place of an entry that is given up: the page where it goes back on the stack, else -1.
+template <int THREADS>
+__device__ __forceinline__ void fork_places(const ForkArgs& a, const ForkRows& r, int32_t* lds) {
   const SharedTables& t = a.t;
-  const int all = t.batch * n;
+  const int n = t.max_pages, all = t.batch * n;
   const auto each = [&](auto use) {  // neighbouring threads: neighbouring places
     for (int i = threadIdx.x; i < all; i += THREADS) {
-      const int b = (int)((uint32_t)i / (uint32_t)n), j = j0 + i - b * n;
-      use(i, b, j);
+      const int b = (int)((uint32_t)i / (uint32_t)n);
+      use(i, b, i - b * n);
     }
   };
   each([&](int i, int b, int j) { lds[i] = j < r.had[b] ? t.table[(int64_t)b * t.max_pages + j] : -1; });
   __syncthreads();
-  const auto now_of = [&](int b, int j) { return j < r.get[b] ? lds[r.parent[b] * n + j - j0] : -1; };
+  const auto now_of = [&](int b, int j) { return j < r.get[b] ? lds[r.parent[b] * n + j] : -1; };
   each([&](int i, int b, int j) {
     const int old = lds[i], now = now_of(b, j);
     if (j < r.get[b]) t.table[(int64_t)b * t.max_pages + j] = now;
@@ -238,13 +257,12 @@ __device__ __forceinline__ void fork_places(const ForkArgs& a, const ForkRows& r
   each([&](int i, int b, int j) {
     if (j >= r.had[b]) return;
     const int old = lds[i];
-    const bool goes = is_page(t, old) && refs_now(t.refs + old) == b - t.batch;  // it has left it; drop may write where lds[i] is
+    const bool goes = is_page(t, old) && refs_now(t.refs + old) == b - t.batch;  // it has left it: nobody else's entry is looked at
     if (goes) refs_set(t.refs + old, 0);
-    drop(b, j, goes ? old : -1);
+    lds[i] = goes ? old : -1;
   });
 }
 
-// Small tables: one launch.
 template <int THREADS>
 __global__ __launch_bounds__(THREADS) void pages_fork_one_kernel(ForkArgs a) {
   __shared__ ForkRows r;
@@ -254,7 +272,7 @@ __global__ __launch_bounds__(THREADS) void pages_fork_one_kernel(ForkArgs a) {
   fork_rows<THREADS>(a, r);
   __syncthreads();
   const int n = t.max_pages, all = t.batch * n;
-  fork_places<THREADS>(a, r, entries, 0, n, [&](int b, int j, int page) { entries[b * n + j] = page; });
+  fork_places<THREADS>(a, r, entries);
   const int count = min(max(t.free[0], 0), t.n_pages);
   __syncthreads();
   int released = 0;
@@ -270,107 +288,179 @@ __global__ __launch_bounds__(THREADS) void pages_fork_one_kernel(ForkArgs a) {
   if (threadIdx.x == 0) t.free[0] = min(count + released, t.n_pages);
 }
 
-// scratch: new lengths [batch], pages given back [kForkGroups][batch], of every entry the page that is given back [batch][max_pages], the stack's count
-__global__ __launch_bounds__(256) void pages_fork_kernel(ForkArgs a) {
-  __shared__ ForkRows r;
-  __shared__ int32_t entries[kForkEntries], gone[kSharedBatch], most;
+// Large tables: a wave for each place.  What leaves and what enters meets in a hash table in LDS, so that refs are read and written once, by the first of those who
+// leave a page or, where nobody does, of those who enter it.
+// scratch: the stack's count, the most pages of a row, new lengths [batch], bits of the rows whose entry is given back [places][words], those pages [batch][max_pages]
+struct ForkScratch {
+  int32_t *head, *lens;
+  unsigned long long* bits;
+  int32_t* drops;
+  int words;
+  __device__ __host__ ForkScratch(int32_t* p, int batch, int max_pages) {
+    words = (batch + kWave - 1) / kWave;
+    bits = (unsigned long long*)p, head = p + 2 * (int64_t)words * max_pages, lens = head + 2, drops = lens + batch;
+  }
+};
+template <int EACH, int WAVES>
+__global__ __launch_bounds__(WAVES* kWave) void pages_fork_kernel(ForkArgs a) {
+  constexpr int kRows = EACH * kWave, kSlots = 4 * kRows;  // up to two pages of a row
+  __shared__ int32_t column[WAVES][kRows], keys[WAVES][kSlots], sums[WAVES][kSlots], firsts[WAVES][kSlots];
   const SharedTables& t = a.t;
-  if (threadIdx.x == 0) most = 0;
-  __syncthreads();
-  atomicMax(&most, fork_rows<256>(a, r));
-  for (int b = threadIdx.x; b < t.batch; b += 256) gone[b] = 0;
-  __syncthreads();
-  int32_t *lens = a.scratch, *counts = lens + t.batch + (int64_t)blockIdx.x * t.batch, *drops = a.scratch + (int64_t)t.batch * (1 + kForkGroups);
-  const int n = min(64, kForkEntries / t.batch);
-  for (int64_t j0 = (int64_t)blockIdx.x * n; j0 < most; j0 += (int64_t)gridDim.x * n) {
-    fork_places<256>(a, r, entries, (int)j0, min(n, t.max_pages - (int)j0), [&](int b, int j, int page) {
-      drops[(int64_t)b * t.max_pages + j] = page;
-      if (page >= 0) atomicAdd(&gone[b], 1);
-    });
-    __syncthreads();
+  const ForkScratch w(a.scratch, t.batch, t.max_pages);
+  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, j = blockIdx.x * WAVES + wave;
+  if (j >= t.max_pages) return;
+  const auto in_wave = [] {  // LDS that the lanes of a wave exchange
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+  };
+  int parent[EACH], had[EACH], get[EACH], len[EACH], most = 0;
+#pragma unroll
+  for (int i = 0; i < EACH; ++i) {
+    const int x = lane + kWave * i;
+    parent[i] = x, had[i] = get[i] = len[i] = 0;
+    if (x < t.batch) {
+      const int p = a.parent[x], keep = a.keep ? a.keep[x] : -1;
+      parent[i] = (uint32_t)p < (uint32_t)t.batch ? p : x;
+      const int n = length_of(t, parent[i]);
+      len[i] = keep < 0 ? n : min(keep, n), had[i] = page_count(length_of(t, x), t.logP), get[i] = page_count(len[i], t.logP);
+      most = max(most, max(had[i], get[i]));
+    }
   }
-  for (int b = threadIdx.x; b < t.batch; b += 256) {
-    counts[b] = gone[b];
-    if (blockIdx.x == 0) lens[b] = r.len[b];
+#pragma unroll
+  for (int d = 1; d < kWave; d <<= 1) most = max(most, __shfl_xor(most, d));
+  if (j == 0) {
+    if (lane == 0) w.head[0] = t.free[0], w.head[1] = most;
+#pragma unroll
+    for (int i = 0; i < EACH; ++i)
+      if (lane + kWave * i < t.batch) w.lens[lane + kWave * i] = len[i];
   }
-  if (blockIdx.x == 0 && threadIdx.x == 0) drops[(int64_t)t.batch * t.max_pages] = t.free[0];
+  if (j >= most) return;
+#pragma unroll
+  for (int i = 0; i < EACH; ++i) column[wave][lane + kWave * i] = j < had[i] ? t.table[(int64_t)(lane + kWave * i) * t.max_pages + j] : -1;
+  for (int i = lane; i < kSlots; i += kWave) keys[wave][i] = -1, sums[wave][i] = 0, firsts[wave][i] = 2 * kRows;
+  in_wave();
+  int out[EACH], in[EACH], leaves[EACH], enters[EACH];  // pages; their slots, -1: none
+  const auto slot_of = [&](int page) {
+    uint32_t s = ((uint32_t)page * 2654435769u) >> 8;
+    for (;; ++s) {  // there are twice as many slots as pages
+      s &= kSlots - 1;
+      const int was = atomicCAS(&keys[wave][s], -1, page);
+      if (was == -1 || was == page) return (int)s;
+    }
+  };
+#pragma unroll
+  for (int i = 0; i < EACH; ++i) {
+    const int x = lane + kWave * i;
+    out[i] = column[wave][x], in[i] = j < get[i] ? column[wave][parent[i]] : -1, leaves[i] = enters[i] = -1;
+    if (out[i] == in[i]) continue;
+    if (is_page(t, out[i])) {
+      leaves[i] = slot_of(out[i]);
+      atomicAdd(&sums[wave][leaves[i]], -1), atomicMin(&firsts[wave][leaves[i]], x);
+    }
+    if (is_page(t, in[i])) {
+      enters[i] = slot_of(in[i]);
+      atomicAdd(&sums[wave][enters[i]], 1), atomicMin(&firsts[wave][enters[i]], kRows + x);
+    }
+  }
+  in_wave();
+#pragma unroll
+  for (int i = 0; i < EACH; ++i) {
+    const int x = lane + kWave * i;
+    bool goes = false;
+    if (leaves[i] >= 0 && firsts[wave][leaves[i]] == x) {
+      const int left = t.refs[out[i]] + sums[wave][leaves[i]];
+      goes = left <= 0;
+      t.refs[out[i]] = max(left, 0);
+    }
+    if (enters[i] >= 0 && firsts[wave][enters[i]] == kRows + x) t.refs[in[i]] = (int)min((long long)t.refs[in[i]] + sums[wave][enters[i]], 0x7fffffffll);
+    if (j < get[i] && (out[i] != in[i] || j >= had[i])) t.table[(int64_t)x * t.max_pages + j] = in[i];
+    if (goes) w.drops[(int64_t)x * t.max_pages + j] = out[i];
+    const unsigned long long m = __ballot(goes);
+    if (lane == 0 && i < w.words) w.bits[(int64_t)j * w.words + i] = m;
+  }
 }
 // A workgroup for each row: behind what the rows after it give back.
-__global__ __launch_bounds__(256) void pages_fork_free_kernel(ForkArgs a, int groups) {
-  __shared__ long long lds1[256 / kWave][1], lds2[256 / kWave][2];
+__global__ __launch_bounds__(256) void pages_fork_free_kernel(ForkArgs a) {
+  __shared__ long long lds1[256 / kWave][1];
   const SharedTables& t = a.t;
-  const int32_t *lens = a.scratch, *counts = lens + t.batch, *drops = a.scratch + (int64_t)t.batch * (1 + kForkGroups);
-  const int b = blockIdx.x, had = page_count(length_of(t, b), t.logP);
-  const int count = min(max(drops[(int64_t)t.batch * t.max_pages], 0), t.n_pages);
-  int x[2] = {0, 0};
-  for (int i = threadIdx.x; i < groups * t.batch; i += 256) {
-    const int c = i % t.batch;
-    x[0] += c > b ? counts[i] : 0, x[1] += c == b ? counts[i] : 0;
-  }
-  long long before[2], all[2];
-  sums_before<256>(x, before, all, lds2);
-  int released = (int)all[0];
-  const int own = (int)all[1];
-  for (int e0 = 0; own && e0 < had; e0 += 256) {
-    const int j = had - 1 - e0 - (int)threadIdx.x, p = j >= 0 ? drops[(int64_t)b * t.max_pages + j] : -1;
+  const ForkScratch w(a.scratch, t.batch, t.max_pages);
+  const int b = blockIdx.x, word = b / kWave, count = min(max(w.head[0], 0), t.n_pages), most = w.head[1];
+  const unsigned long long bit = 1ull << (b % kWave);
+  if (threadIdx.x == 0) t.lens[b] = w.lens[b];
+  bool any = false;
+  for (int j = threadIdx.x; j < most; j += 256) any |= (w.bits[(int64_t)j * w.words + word] & bit) != 0;
+  if (!__syncthreads_or(any) && b) return;
+  int before = 0, all, own = 0;
+  for (int j = threadIdx.x; j < most; j += 256)
+    for (int i = word; i < w.words; ++i) {
+      const unsigned long long m = w.bits[(int64_t)j * w.words + i];
+      before += __popcll(i == word ? m & ~(bit | (bit - 1)) : m);
+      if (i == word) own += (m & bit) != 0;
+    }
+  sum_before<256>(before, &all, lds1);
+  int released = all, n;
+  sum_before<256>(own, &n, lds1);
+  if (b == 0 && threadIdx.x == 0) t.free[0] = min(count + released + n, t.n_pages);
+  for (int e0 = 0; n && e0 < most; e0 += 256) {
+    const int j = most - 1 - e0 - (int)threadIdx.x;
+    const bool goes = j >= 0 && (w.bits[(int64_t)j * w.words + word] & bit);
     int m;
-    const int at = released + sum_before<256>(p >= 0 ? 1 : 0, &m, lds1);
-    if (p >= 0 && count + at < t.n_pages) t.free[1 + count + at] = p;
+    const int at = count + released + sum_before<256>(goes ? 1 : 0, &m, lds1);
+    if (goes && at < t.n_pages) t.free[1 + at] = w.drops[(int64_t)b * t.max_pages + j];
     released += m;
-  }
-  __syncthreads();  // the length has been read
-  if (threadIdx.x == 0) {
-    t.lens[b] = lens[b];
-    if (b == 0) t.free[0] = (int)min((long long)count + all[0] + own, (long long)t.n_pages);
   }
 }
 
 // ------------------------------------------------------------------------------------------------ compacting
 // The i-th highest held page goes to the i-th lowest free place, while that is below it.  Held pages as bits, 64 to a word; ranks are sums of their counts.
-// scratch: where each page that moves goes [n_pages], the lowest page that moves, how many, bits [2 * words]
-constexpr int kCompactThreads = 1024;
+// scratch: where each page that moves goes [n_pages], the lowest page that moves, how many, and, of a large pool, the bits
+constexpr int kCompactThreads = 1024, kCompactWords = 2048;  // words in LDS
+template <bool LDS>
 __global__ __launch_bounds__(kCompactThreads) void pages_compact_kernel(CompactArgs a) {
   __shared__ long long lds1[kCompactThreads / kWave][1];
+  __shared__ unsigned long long kept[LDS ? kCompactWords : 1];
+  __shared__ int32_t base[kCompactThreads];
   const SharedTables& t = a.t;
+  constexpr int kWaves = kCompactThreads / kWave;
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, words = (t.n_pages + kWave - 1) / kWave;
   int32_t *to = a.scratch, *head = to + t.n_pages;
-  unsigned long long* bits = (unsigned long long*)(((uintptr_t)(head + 2) + 7) & ~(uintptr_t)7);
-  const auto word_mask = [&](int w) { return w == words - 1 && (t.n_pages & 63) ? (1ull << (t.n_pages & 63)) - 1 : ~0ull; };
-  for (int w = wave; w < words; w += kCompactThreads / kWave) {
-    const int p = w * kWave + lane;
-    const unsigned long long m = __ballot(p < t.n_pages && t.refs[p] > 0);
-    if (lane == 0) bits[w] = m;
+  unsigned long long* bits = LDS ? kept : (unsigned long long*)(((uintptr_t)(head + 2) + 7) & ~(uintptr_t)7);
+  const auto load = [&](int w) { return LDS ? bits[w] : __hip_atomic_load(&bits[w], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP); };
+  // use(w, its bits, held pages before it) by a wave for each word
+  const auto each_word = [&](auto use) {
+    int before = 0;
+    for (int w0 = 0; w0 < words; w0 += kCompactThreads) {
+      const int mine = w0 + threadIdx.x < words ? __popcll(load(w0 + threadIdx.x)) : 0;
+      int n;
+      const int at = before + sum_before<kCompactThreads>(mine, &n, lds1);
+      __syncthreads();
+      base[threadIdx.x] = at;
+      __syncthreads();
+      before += n;
+      for (int w = w0 + wave; w < min(words, w0 + kCompactThreads); w += kWaves) use(w, load(w), base[w - w0]);
+    }
+  };
+  int held = 0;
+  {
+    int mine = 0;
+#pragma unroll 8
+    for (int w = wave; w < words; w += kWaves) {
+      const int p = w * kWave + lane;
+      const unsigned long long m = __ballot(p < t.n_pages && t.refs[p] > 0);
+      if (lane == 0) bits[w] = m, mine += __popcll(m);
+    }
+    sum_before<kCompactThreads>(mine, &held, lds1);
   }
   for (int i = threadIdx.x; i < a.n_moves; i += kCompactThreads) ((int2*)a.moves)[i] = make_int2(-1, -1);
   all_here();
-  int held = 0;
-  for (int w0 = 0; w0 < words; w0 += kCompactThreads) {
-    const int w = w0 + threadIdx.x;
-    int n;
-    sum_before<kCompactThreads>(w < words ? __popcll(bits[w]) : 0, &n, lds1);
-    held += n;
-  }
   // held pages from `held` on and free places below: as many of each
-  int below = 0;  // held pages before the word
-  for (int w0 = 0; w0 < words; w0 += kCompactThreads) {
-    const int w = w0 + threadIdx.x;
-    const unsigned long long m = w < words ? bits[w] : 0;
-    int n, before = below + sum_before<kCompactThreads>(__popcll(m), &n, lds1);
-    below += n;
-    if (w >= words) continue;
-    unsigned long long rest = m;
-    int rank = held - 1 - before;  // from the highest held page on
-    for (; rest; rest &= rest - 1, --rank) {
-      const int p = w * kWave + __builtin_ctzll(rest);
-      if (p >= held && rank < a.n_moves) a.moves[2 * rank] = p;
-    }
-    rest = ~m & word_mask(w);
-    int place = w * kWave - before;  // free places before the word
-    for (; rest; rest &= rest - 1, ++place) {
-      const int p = w * kWave + __builtin_ctzll(rest);
-      if (p < held && place < a.n_moves) a.moves[2 * place + 1] = p;
-    }
-  }
+  const unsigned long long below = (1ull << lane) - 1;
+  each_word([&](int w, unsigned long long m, int before) {
+    const int p = w * kWave + lane, mine = before + __popcll(m & below);  // held pages before p
+    if (p >= t.n_pages) return;
+    if ((m >> lane & 1) && p >= held && held - 1 - mine < a.n_moves) a.moves[2 * (held - 1 - mine)] = p;
+    if (!(m >> lane & 1) && p < held && p - mine < a.n_moves) a.moves[2 * (p - mine) + 1] = p;
+  });
   all_here();
   int lowest = t.n_pages, moved = 0;
   for (int i0 = 0; i0 < a.n_moves; i0 += kCompactThreads) {
@@ -379,25 +469,20 @@ __global__ __launch_bounds__(kCompactThreads) void pages_compact_kernel(CompactA
     if (m.x >= 0) {
       to[m.x] = m.y, lowest = m.x;
       t.refs[m.y] = t.refs[m.x], t.refs[m.x] = 0;
-      atomicAnd(&bits[m.x / kWave], ~(1ull << (m.x % kWave)));
-      atomicOr(&bits[m.y / kWave], 1ull << (m.y % kWave));
+      __hip_atomic_fetch_and(&bits[m.x / kWave], ~(1ull << (m.x % kWave)), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+      __hip_atomic_fetch_or(&bits[m.y / kWave], 1ull << (m.y % kWave), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
     }
-    int n;
-    sum_before<kCompactThreads>(m.x >= 0 ? 1 : 0, &n, lds1);
+    const int n = __syncthreads_count(m.x >= 0);
     moved += n;
+    if (n < kCompactThreads) break;  // the moves lie before what has none
   }
   all_here();
   if (threadIdx.x == 0) head[1] = moved, t.free[0] = t.n_pages - held;
   if (moved ? lowest == a.moves[2 * (moved - 1)] : threadIdx.x == 0) head[0] = lowest;
-  int free_before = 0;
-  for (int w0 = 0; w0 < words; w0 += kCompactThreads) {  // free pages, the lowest on top
-    const int w = w0 + threadIdx.x;
-    unsigned long long m = 0;
-    if (w < words) m = ~__hip_atomic_load(&bits[w], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) & word_mask(w);
-    int n, rank = free_before + sum_before<kCompactThreads>(__popcll(m), &n, lds1);
-    free_before += n;
-    for (; m; m &= m - 1, ++rank) t.free[t.n_pages - held - rank] = w * kWave + __builtin_ctzll(m);
-  }
+  each_word([&](int w, unsigned long long m, int before) {  // free pages, the lowest on top
+    const int p = w * kWave + lane, rank = p - before - __popcll(m & below);  // free pages before p
+    if (p < t.n_pages && !(m >> lane & 1)) t.free[t.n_pages - held - rank] = p;
+  });
 }
 // The pages that move are the highest ones held: an entry from the lowest of them on is one of them.
 __global__ __launch_bounds__(256) void pages_compact_table_kernel(CompactArgs a) {
@@ -444,12 +529,14 @@ bool fork_in_one(int batch, int max_pages) { return (int64_t)batch * max_pages <
 }  // namespace
 
 size_t pages_fork_bytes(int batch, int max_pages) {
-  return fork_in_one(batch, max_pages) ? 0 : sizeof(int32_t) * ((size_t)batch * (1 + kForkGroups + (size_t)max_pages) + 1);
+  if (fork_in_one(batch, max_pages)) return 0;
+  const ForkScratch w(nullptr, batch, max_pages);
+  return (size_t)((const char*)(w.drops + (int64_t)batch * max_pages) - (const char*)nullptr);
 }
 size_t pages_compact_bytes(int n_pages) { return sizeof(int32_t) * ((size_t)n_pages + 4) + sizeof(long long) * (((size_t)n_pages + 63) / 64 + 1); }
 
 hipError_t launch_pages_grow(const GrowArgs& a, hipStream_t st) {
-  if (a.t.batch <= 256) pages_grow_kernel<256><<<1, 256, 0, st>>>(a);
+  if (a.t.batch <= 256 && (int64_t)a.t.batch * a.t.max_pages <= kForkEntries) pages_grow_kernel<256><<<1, 256, 0, st>>>(a);
   else pages_grow_kernel<kSharedBatch><<<1, kSharedBatch, 0, st>>>(a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.n_slots <= kResizeOneSlots) return e;
@@ -462,16 +549,19 @@ hipError_t launch_pages_fork(const ForkArgs& a, hipStream_t st) {
     pages_fork_one_kernel<kSharedBatch><<<1, kSharedBatch, 0, st>>>(a);
     return hipGetLastError();
   }
-  const int n = std::min(64, kForkEntries / a.t.batch), groups = std::min(kForkGroups, (a.t.max_pages + n - 1) / n);
-  pages_fork_kernel<<<groups, 256, 0, st>>>(a);
+  const auto grid = [&](int waves) { return (unsigned)((a.t.max_pages + waves - 1) / waves); };
+  if (a.t.batch <= kWave) pages_fork_kernel<1, 4><<<grid(4), 4 * kWave, 0, st>>>(a);
+  else if (a.t.batch <= 4 * kWave) pages_fork_kernel<4, 4><<<grid(4), 4 * kWave, 0, st>>>(a);
+  else pages_fork_kernel<16, 1><<<grid(1), kWave, 0, st>>>(a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  pages_fork_free_kernel<<<a.t.batch, 256, 0, st>>>(a, groups);
+  pages_fork_free_kernel<<<a.t.batch, 256, 0, st>>>(a);
   return hipGetLastError();
 }
 
 hipError_t launch_pages_compact(const CompactArgs& a, hipStream_t st) {
-  pages_compact_kernel<<<1, kCompactThreads, 0, st>>>(a);
+  if (a.t.n_pages <= kCompactWords * kWave) pages_compact_kernel<true><<<1, kCompactThreads, 0, st>>>(a);
+  else pages_compact_kernel<false><<<1, kCompactThreads, 0, st>>>(a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.t.batch == 0) return e;
   pages_compact_table_kernel<<<dim3((unsigned)std::min(16, (a.t.max_pages + 255) / 256), (unsigned)a.t.batch), 256, 0, st>>>(a);
