@@ -608,27 +608,25 @@ def iwdft_pages_compact_bytes(n_pages: int) -> int:
     return _bytes_of(load_library().iwdft_pages_compact_bytes, n_pages)
 
 
-def _table_sizes(table: torch.Tensor, refs: torch.Tensor, **others):
-    """(index of the GPU, batch, max_pages, pages); others: (tensor, shape, None where any size will do; the batch as -1, one more as -2, one more than the pages as -3)."""
-    index, shape, i32 = table.get_device(), table.shape, torch.int32
-    if len(shape) != 2 or index < 0:
-        raise ValueError(f"table must be a device tensor [batch, max_pages], not {tuple(shape)} on {table.device}")
-    n_pages = refs.numel()
-    sizes = {None: None, 2: 2, -1: shape[0], -2: shape[0] + 1, -3: n_pages + 1}
-    if not (table.dtype is refs.dtype is i32 and refs.dim() == 1 and refs.get_device() == index and table.is_contiguous() and refs.is_contiguous()):
-        _expect("table", table, i32, shape, table.device)
-        _expect("refs", refs, i32, (n_pages,), table.device)
-    for name, (t, size) in others.items():
-        s = t.shape
-        if not (t.dtype is i32 and t.get_device() == index and len(s) == len(size) and t.is_contiguous() and all(n is None or sizes[n] == m for n, m in zip(size, s))):
-            _expect(name, t, i32, tuple(sizes[n] for n in size), table.device)
-    return index, shape[0], shape[1], n_pages
+def _check_tables(table, refs, batch, n_pages, others):
+    """Says which tensor does not fit; others: (name, tensor, shape)."""
+    if len(table.shape) != 2 or table.get_device() < 0:
+        raise ValueError(f"table must be a device tensor [batch, max_pages], not {tuple(table.shape)} on {table.device}")
+    for name, t, size in (("table", table, table.shape), ("refs", refs, (n_pages,)), *others):
+        _expect(name, t, torch.int32, size, table.device)
 
 
 def iwdft_pages_fork(parent, keep, table, lens, free, refs, page_tokens: int, stream=None, workspace=None) -> None:
     """Sequence b becomes the first keep[b] tokens (keep None, or negative: all) of what sequence parent[b] was: table, lens, free and refs are brought up to date."""
-    more = {} if keep is None else dict(keep=(keep, (-1,)))
-    index, batch, max_pages, n_pages = _table_sizes(table, refs, parent=(parent, (-1,)), lens=(lens, (-1,)), free=(free, (-3,)), **more)
+    index, shape, i32, n_pages = table.get_device(), table.shape, torch.int32, refs.numel()
+    batch, max_pages = shape if len(shape) == 2 else (0, 0)
+    if not (len(shape) == 2 and index >= 0 and parent.dtype is table.dtype is lens.dtype is free.dtype is refs.dtype is i32
+            and index == parent.get_device() == lens.get_device() == free.get_device() == refs.get_device()
+            and parent.shape == lens.shape == (batch,) and free.shape == (n_pages + 1,) and refs.dim() == 1
+            and (keep is None or (keep.dtype is i32 and keep.get_device() == index and keep.shape == (batch,) and keep.is_contiguous()))
+            and parent.is_contiguous() and table.is_contiguous() and lens.is_contiguous() and free.is_contiguous() and refs.is_contiguous()):
+        _check_tables(table, refs, batch, n_pages, [("parent", parent, (batch,)), ("lens", lens, (batch,)), ("free", free, (n_pages + 1,))]
+                      + ([] if keep is None else [("keep", keep, (batch,))]))
     if index != torch._C._cuda_getDevice():
         with torch.cuda.device(index):
             return iwdft_pages_fork(parent, keep, table, lens, free, refs, page_tokens, stream, workspace)
@@ -643,8 +641,15 @@ def iwdft_pages_fork(parent, keep, table, lens, free, refs, page_tokens: int, st
 
 def iwdft_pages_resize_shared(want, table, lens, free, refs, starts, slots, copies, page_tokens: int, stream=None) -> None:
     """iwdft_pages_resize where pages are shared; copies [batch, 2] says what iwdft_pages_copy has to do before anything is written."""
-    index, batch, max_pages, n_pages = _table_sizes(table, refs, want=(want, (-1,)), lens=(lens, (-1,)), free=(free, (-3,)), starts=(starts, (-2,)), slots=(slots, (None,)),
-                                                    copies=(copies, (-1, 2)))
+    index, shape, i32, n_pages = table.get_device(), table.shape, torch.int32, refs.numel()
+    batch, max_pages = shape if len(shape) == 2 else (0, 0)
+    if not (len(shape) == 2 and index >= 0 and want.dtype is table.dtype is lens.dtype is free.dtype is refs.dtype is starts.dtype is slots.dtype is copies.dtype is i32
+            and index == want.get_device() == lens.get_device() == free.get_device() == refs.get_device() == starts.get_device() == slots.get_device() == copies.get_device()
+            and want.shape == lens.shape == (batch,) and starts.shape == (batch + 1,) and copies.shape == (batch, 2) and free.shape == (n_pages + 1,)
+            and refs.dim() == slots.dim() == 1 and want.is_contiguous() and table.is_contiguous() and lens.is_contiguous() and free.is_contiguous()
+            and refs.is_contiguous() and starts.is_contiguous() and slots.is_contiguous() and copies.is_contiguous()):
+        _check_tables(table, refs, batch, n_pages, [("want", want, (batch,)), ("lens", lens, (batch,)), ("free", free, (n_pages + 1,)), ("starts", starts, (batch + 1,)),
+                                                    ("slots", slots, (None,)), ("copies", copies, (batch, 2))])
     if index != torch._C._cuda_getDevice():
         with torch.cuda.device(index):
             return iwdft_pages_resize_shared(want, table, lens, free, refs, starts, slots, copies, page_tokens, stream)
@@ -656,7 +661,13 @@ def iwdft_pages_resize_shared(want, table, lens, free, refs, starts, slots, copi
 
 def iwdft_pages_compact(table, lens, free, refs, moves, page_tokens: int, stream=None, workspace=None) -> None:
     """Held pages together at the pool's beginning, moves.shape[0] of them at most: moves [n, 2] says what iwdft_pages_copy has to do."""
-    index, batch, max_pages, n_pages = _table_sizes(table, refs, lens=(lens, (-1,)), free=(free, (-3,)), moves=(moves, (None, 2)))
+    index, shape, i32, n_pages = table.get_device(), table.shape, torch.int32, refs.numel()
+    batch, max_pages = shape if len(shape) == 2 else (0, 0)
+    if not (len(shape) == 2 and index >= 0 and table.dtype is lens.dtype is free.dtype is refs.dtype is moves.dtype is i32
+            and index == lens.get_device() == free.get_device() == refs.get_device() == moves.get_device()
+            and lens.shape == (batch,) and free.shape == (n_pages + 1,) and refs.dim() == 1 and moves.dim() == 2 and moves.shape[1] == 2
+            and table.is_contiguous() and lens.is_contiguous() and free.is_contiguous() and refs.is_contiguous() and moves.is_contiguous()):
+        _check_tables(table, refs, batch, n_pages, [("lens", lens, (batch,)), ("free", free, (n_pages + 1,)), ("moves", moves, (None, 2))])
     if index != torch._C._cuda_getDevice():
         with torch.cuda.device(index):
             return iwdft_pages_compact(table, lens, free, refs, moves, page_tokens, stream, workspace)

@@ -17,6 +17,7 @@ constexpr int kWave = kLanes;
 // refs are changed by atomics of one workgroup (a page is held at one place, which one workgroup looks after), in its L2: read past the L1.
 __device__ __forceinline__ int32_t refs_now(const int32_t* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP); }
 __device__ __forceinline__ void refs_add(int32_t* p, int x) { __hip_atomic_fetch_add(p, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP); }
+__device__ __forceinline__ int32_t refs_less(int32_t* p) { return __hip_atomic_fetch_add(p, -1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP); }  // what it was
 __device__ __forceinline__ void refs_least(int32_t* p, int x) { __hip_atomic_fetch_min(p, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP); }
 __device__ __forceinline__ void refs_set(int32_t* p, int x) { __hip_atomic_store(p, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP); }
 __device__ __forceinline__ void all_here() {  // what the workgroup has written, in memory too, is there for all of it; its atomics have arrived
@@ -49,12 +50,13 @@ __device__ __forceinline__ int sum_before(int x, int* all, long long (*lds)[1]) 
 // One workgroup, a thread for each sequence.  A sequence whose last page has room, and which others hold, leaves that page before it grows: it gets a new one and
 // an entry in copies.  Where all holders leave in this call, the last of them stays.  It is held to the pages that are left as those before it
 // are: had one of them been refused, the page would still be shared.
-constexpr int kForkEntries = 8192;  // of a small table: in LDS, one launch
-constexpr int kGiven = 8;  // entries of a thread that are on their way at a time
+constexpr int kSmallTable = 8192;  // of a small table: in LDS, one launch
+constexpr int kGiven = 16;  // entries of a thread that are on their way at a time
 template <int THREADS>
 __global__ __launch_bounds__(THREADS) void pages_grow_kernel(GrowArgs a) {
   __shared__ long long lds1[THREADS / kWave][1], lds2[THREADS / kWave][2];
-  __shared__ int32_t base[THREADS + 1], first[THREADS], open[THREADS], back[THREADS];
+  __shared__ int32_t base[THREADS], first[THREADS], back[THREADS];
+  __shared__ __attribute__((aligned(16))) int32_t open[THREADS];
   const SharedTables& t = a.t;
   const int b = threadIdx.x, P = 1 << t.logP, most = t.max_pages << t.logP;
   const bool mine = b < t.batch;
@@ -68,77 +70,90 @@ __global__ __launch_bounds__(THREADS) void pages_grow_kernel(GrowArgs a) {
   const int had = page_count(have, t.logP), get = page_count(want, t.logP);
   int32_t* const row = t.table + (int64_t)b * t.max_pages;
 
-  // pages that are given up, from the last one of the last sequence on
-  int gone = 0, released = 0;
-  const int gone_before = sum_before<THREADS>(max(had - get, 0), &gone, lds1);
-  if (gone > 0) {
-    base[b] = gone_before, first[b] = get;
-    __syncthreads();
-    int page[kGiven];
-    const auto entries = [&](int e0) {  // of this thread, from the end
-#pragma unroll
-      for (int i = 0; i < kGiven; ++i) {
-        const int o = gone - 1 - e0 - kGiven * b - i, s = last_not_above(base, THREADS, max(o, 0));
-        const int p = o >= 0 ? t.table[(int64_t)s * t.max_pages + min(first[s] + o - base[s], t.max_pages - 1)] : -1;
-        page[i] = is_page(t, p) ? p : -1;
-      }
-    };
-    const auto mark = [&](int e0, int i) { return -1 - e0 - kGiven * b - i; };  // the later an entry is given back the smaller
-    for (int e0 = 0; e0 < gone; e0 += kGiven * THREADS) {
-      entries(e0);
-#pragma unroll
-      for (int i = 0; i < kGiven; ++i)
-        if (page[i] >= 0) refs_add(t.refs + page[i], -1);
-    }
-    all_here();
-    for (int e0 = 0; e0 < gone; e0 += kGiven * THREADS) {
-      if (gone > kGiven * THREADS) entries(e0);
-      int left[kGiven];
-#pragma unroll
-      for (int i = 0; i < kGiven; ++i) left[i] = page[i] >= 0 ? refs_now(t.refs + page[i]) : 1;
-#pragma unroll
-      for (int i = 0; i < kGiven; ++i)
-        if (left[i] <= 0) refs_least(t.refs + page[i], mark(e0, i));
-    }
-    all_here();
-    for (int e0 = 0; e0 < gone; e0 += kGiven * THREADS) {
-      if (gone > kGiven * THREADS) entries(e0);
-      int left[kGiven], mine_goes = 0, n;
-#pragma unroll
-      for (int i = 0; i < kGiven; ++i) left[i] = page[i] >= 0 ? refs_now(t.refs + page[i]) : 0;
-#pragma unroll
-      for (int i = 0; i < kGiven; ++i) mine_goes += left[i] == mark(e0, i);
-      int at = count + released + sum_before<THREADS>(mine_goes, &n, lds1);
-#pragma unroll
-      for (int i = 0; i < kGiven; ++i)
-        if (left[i] == mark(e0, i)) {
-          if (at < t.n_pages) t.free[1 + at] = page[i];
-          ++at;
-          refs_set(t.refs + page[i], 0);
-        }
-      released += n;
-    }
-    released = min(released, t.n_pages - count);
-    all_here();
-  }
-
-  // who has to leave a shared page
   const bool up = mine && want > have;
   int last = -1;
   if (up && (have & (P - 1))) {
     last = row[had - 1];
     last = is_page(t, last) ? last : -1;
   }
+
+  // pages that are given up, from the last one of the last sequence on
+  int gone = 0, released = 0;
+  const int gone_before = sum_before<THREADS>(max(had - get, 0), &gone, lds1);
+  if (gone > 0) {
+    // those that give something up, side by side: base, the first place that goes, who it is
+    int givers;
+    const int at = sum_before<THREADS>(had > get ? 1 : 0, &givers, lds1);
+    if (had > get) base[at] = gone_before, first[at] = get, back[at] = b;
+    __syncthreads();
+    int page[kGiven], holders[kGiven];
+    const int per = min((gone + THREADS - 1) / THREADS, kGiven);  // of a thread, side by side
+    const auto mark = [&](int e0, int i) { return -1 - e0 - per * b - i; };  // the later an entry is given back the smaller
+    for (int e0 = 0; e0 < gone; e0 += per * THREADS) {  // batch by batch: a page that two batches give up goes with the second
+      int o = gone - 1 - e0 - per * b, s = o >= 0 ? last_not_above(base, givers, o) : 0;
+#pragma unroll
+      for (int i = 0; i < kGiven; ++i, --o) {
+        page[i] = -1;
+        if (i >= per || o < 0) continue;
+        if (o < base[s]) --s;
+        const int p = t.table[(int64_t)back[s] * t.max_pages + min(first[s] + o - base[s], t.max_pages - 1)];
+        page[i] = is_page(t, p) ? p : -1;
+      }
+#pragma unroll
+      for (int i = 0; i < kGiven; ++i) holders[i] = page[i] >= 0 ? refs_now(t.refs + page[i]) : -1;
+      all_here();
+      // who holds a page alone gives it back; of several, one sees the count come to nothing, then the last in this order does
+      bool open = false;
+#pragma unroll
+      for (int i = 0; i < kGiven; ++i)
+        if (holders[i] > 1) {
+          holders[i] = refs_less(t.refs + page[i]) > 1 ? 2 : 3;
+          open |= holders[i] == 3;
+        }
+      if (__syncthreads_or(open)) {
+#pragma unroll
+        for (int i = 0; i < kGiven; ++i)
+          if (holders[i] >= 2) holders[i] = refs_now(t.refs + page[i]) <= 0 ? 3 : 2;
+        all_here();
+#pragma unroll
+        for (int i = 0; i < kGiven; ++i)
+          if (holders[i] == 3) refs_least(t.refs + page[i], mark(e0, i));
+        all_here();
+#pragma unroll
+        for (int i = 0; i < kGiven; ++i)
+          if (holders[i] == 3) holders[i] = refs_now(t.refs + page[i]) == mark(e0, i);
+      }
+      int n, goes = 0;  // holders 1: it goes
+#pragma unroll
+      for (int i = 0; i < kGiven; ++i) goes += holders[i] == 1;
+      int to = count + released + sum_before<THREADS>(goes, &n, lds1);
+#pragma unroll
+      for (int i = 0; i < kGiven; ++i)
+        if (holders[i] == 1) {
+          if (to < t.n_pages) t.free[1 + to] = page[i];
+          ++to;
+          refs_set(t.refs + page[i], 0);
+        }
+      released += n;
+      all_here();
+    }
+    released = min(released, t.n_pages - count);
+  }
+
+  // who has to leave a shared page
   const int holders = last >= 0 ? refs_now(t.refs + last) : 0;
   const bool shared = holders > 1;
   bool leave = shared;
   open[b] = shared ? last : -1;
   if (__syncthreads_or(shared)) {
     if (shared) {
-      int n = 0, after = 0;
-      for (int c = 0; c < t.batch; ++c) {
-        n += open[c] == last;
-        after += c > b && open[c] == last;
+      int n = 0, after = 0;  // those who share the page and leave it; behind this one
+#pragma unroll 8
+      for (int c = 0; c < t.batch; c += 4) {
+        const int4 o = *(const int4*)(open + c);
+        const int is[4] = {o.x == last, o.y == last, o.z == last, o.w == last};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) n += is[k], after += c + k > b ? is[k] : 0;
       }
       leave = n < holders || after > 0;
     }
@@ -266,7 +281,7 @@ __device__ __forceinline__ void fork_places(const ForkArgs& a, const ForkRows& r
 template <int THREADS>
 __global__ __launch_bounds__(THREADS) void pages_fork_one_kernel(ForkArgs a) {
   __shared__ ForkRows r;
-  __shared__ int32_t entries[kForkEntries];
+  __shared__ int32_t entries[kSmallTable];
   __shared__ long long lds1[THREADS / kWave][1];
   const SharedTables& t = a.t;
   fork_rows<THREADS>(a, r);
@@ -413,33 +428,44 @@ __global__ __launch_bounds__(256) void pages_fork_free_kernel(ForkArgs a) {
 
 // ------------------------------------------------------------------------------------------------ compacting
 // The i-th highest held page goes to the i-th lowest free place, while that is below it.  Held pages as bits, 64 to a word; ranks are sums of their counts.
-// scratch: where each page that moves goes [n_pages], the lowest page that moves, how many, and, of a large pool, the bits
+// With h held pages and m moves, what becomes of a page follows from the held pages before it alone:
+//   held, h - 1 - (held before) =: i < m         moves to the i-th lowest free place
+//   free, (free before) < m                      is that place
+//   otherwise free, or moving                    lies on the stack: free pages below it when all is done = free before - m, plus held before - (h - m) where positive
+// scratch: which move a page is [n_pages], the lowest page that moves, how many move, and, of a large pool, the bits
 constexpr int kCompactThreads = 1024, kCompactWords = 2048;  // words in LDS
-template <bool LDS>
+__device__ __forceinline__ int32_t* compact_head(const CompactArgs& a) { return a.scratch + a.t.n_pages; }
+// Counts and entries after the moves, by thread `at` of `step`: a page from the lowest that moves on, if held, moves.
+__device__ __forceinline__ void compact_refs(const CompactArgs& a, int moved, int at, int step) {
+  for (int i = at; i < moved; i += step) {
+    const int2 m = ((const int2*)a.moves)[i];
+    a.t.refs[m.y] = a.t.refs[m.x], a.t.refs[m.x] = 0;
+  }
+}
+__device__ __forceinline__ void compact_row(const CompactArgs& a, int moved, int lowest, int b, int at, int step) {
+  const SharedTables& t = a.t;
+  const int n = page_count(length_of(t, b), t.logP);
+  for (int j = at; j < n; j += step) {
+    int32_t* entry = t.table + (int64_t)b * t.max_pages + j;
+    const int p = *entry;
+    if (p < lowest || p >= t.n_pages) continue;
+    const int i = a.scratch[p];
+    if ((uint32_t)i < (uint32_t)moved) *entry = a.moves[2 * i + 1];  // always, unless the page is counted as free
+  }
+}
+
+// ONE: the table, which is small, too.
+template <bool LDS, bool ONE>
 __global__ __launch_bounds__(kCompactThreads) void pages_compact_kernel(CompactArgs a) {
   __shared__ long long lds1[kCompactThreads / kWave][1];
   __shared__ unsigned long long kept[LDS ? kCompactWords : 1];
-  __shared__ int32_t base[kCompactThreads];
+  __shared__ int32_t base[kCompactThreads], found[2];
   const SharedTables& t = a.t;
   constexpr int kWaves = kCompactThreads / kWave;
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, words = (t.n_pages + kWave - 1) / kWave;
-  int32_t *to = a.scratch, *head = to + t.n_pages;
+  int32_t *move = a.scratch, *head = compact_head(a);
   unsigned long long* bits = LDS ? kept : (unsigned long long*)(((uintptr_t)(head + 2) + 7) & ~(uintptr_t)7);
-  const auto load = [&](int w) { return LDS ? bits[w] : __hip_atomic_load(&bits[w], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP); };
-  // use(w, its bits, held pages before it) by a wave for each word
-  const auto each_word = [&](auto use) {
-    int before = 0;
-    for (int w0 = 0; w0 < words; w0 += kCompactThreads) {
-      const int mine = w0 + threadIdx.x < words ? __popcll(load(w0 + threadIdx.x)) : 0;
-      int n;
-      const int at = before + sum_before<kCompactThreads>(mine, &n, lds1);
-      __syncthreads();
-      base[threadIdx.x] = at;
-      __syncthreads();
-      before += n;
-      for (int w = w0 + wave; w < min(words, w0 + kCompactThreads); w += kWaves) use(w, load(w), base[w - w0]);
-    }
-  };
+  const unsigned long long below = (1ull << lane) - 1;
   int held = 0;
   {
     int mine = 0;
@@ -451,50 +477,52 @@ __global__ __launch_bounds__(kCompactThreads) void pages_compact_kernel(CompactA
     }
     sum_before<kCompactThreads>(mine, &held, lds1);
   }
-  for (int i = threadIdx.x; i < a.n_moves; i += kCompactThreads) ((int2*)a.moves)[i] = make_int2(-1, -1);
   all_here();
-  // held pages from `held` on and free places below: as many of each
-  const unsigned long long below = (1ull << lane) - 1;
-  each_word([&](int w, unsigned long long m, int before) {
-    const int p = w * kWave + lane, mine = before + __popcll(m & below);  // held pages before p
-    if (p >= t.n_pages) return;
-    if ((m >> lane & 1) && p >= held && held - 1 - mine < a.n_moves) a.moves[2 * (held - 1 - mine)] = p;
-    if (!(m >> lane & 1) && p < held && p - mine < a.n_moves) a.moves[2 * (p - mine) + 1] = p;
-  });
-  all_here();
-  int lowest = t.n_pages, moved = 0;
-  for (int i0 = 0; i0 < a.n_moves; i0 += kCompactThreads) {
-    const int i = i0 + threadIdx.x;
-    const int2 m = i < a.n_moves ? ((const int2*)a.moves)[i] : make_int2(-1, -1);
-    if (m.x >= 0) {
-      to[m.x] = m.y, lowest = m.x;
-      t.refs[m.y] = t.refs[m.x], t.refs[m.x] = 0;
-      __hip_atomic_fetch_and(&bits[m.x / kWave], ~(1ull << (m.x % kWave)), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
-      __hip_atomic_fetch_or(&bits[m.y / kWave], 1ull << (m.y % kWave), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+  // held pages from `held` on, which is as many as free places below
+  int above = 0;
+  {
+    int mine = 0;
+    for (int w = held / kWave + threadIdx.x; w < words; w += kCompactThreads) mine += __popcll(w == held / kWave ? bits[w] & ~((1ull << (held % kWave)) - 1) : bits[w]);
+    sum_before<kCompactThreads>(mine, &above, lds1);
+  }
+  const int moved = min(above, a.n_moves);
+  if (threadIdx.x == 0) found[0] = t.n_pages;
+  int before = 0;
+  for (int w0 = 0; w0 < words; w0 += kCompactThreads) {
+    int n;
+    const int at = before + sum_before<kCompactThreads>(w0 + threadIdx.x < words ? __popcll(bits[w0 + threadIdx.x]) : 0, &n, lds1);
+    base[threadIdx.x] = at;
+    __syncthreads();
+    before += n;
+#pragma unroll 4
+    for (int w = w0 + wave; w < min(words, w0 + kCompactThreads); w += kWaves) {
+      const unsigned long long m = bits[w];
+      const int p = w * kWave + lane, held_before = base[w - w0] + __popcll(m & below), free_before = p - held_before;
+      if (p >= t.n_pages) continue;
+      const bool is_held = m >> lane & 1;
+      const int i = held - 1 - held_before;
+      if (is_held && i < moved) {
+        move[p] = i, a.moves[2 * i] = p;
+        if (i == moved - 1) found[0] = p;
+      }
+      if (!is_held && free_before < moved) a.moves[2 * free_before + 1] = p;
+      if (is_held ? i < moved : free_before >= moved) t.free[t.n_pages - held - (free_before - moved) - max(held_before - (held - moved), 0)] = p;
     }
-    const int n = __syncthreads_count(m.x >= 0);
-    moved += n;
-    if (n < kCompactThreads) break;  // the moves lie before what has none
+    __syncthreads();
   }
+  for (int64_t i = moved + threadIdx.x; i < a.n_moves; i += kCompactThreads) ((int2*)a.moves)[i] = make_int2(-1, -1);
+  const int lowest = found[0];
+  if (threadIdx.x == 0) head[0] = lowest, head[1] = moved, t.free[0] = t.n_pages - held;
+  if (!ONE || moved == 0) return;
   all_here();
-  if (threadIdx.x == 0) head[1] = moved, t.free[0] = t.n_pages - held;
-  if (moved ? lowest == a.moves[2 * (moved - 1)] : threadIdx.x == 0) head[0] = lowest;
-  each_word([&](int w, unsigned long long m, int before) {  // free pages, the lowest on top
-    const int p = w * kWave + lane, rank = p - before - __popcll(m & below);  // free pages before p
-    if (p < t.n_pages && !(m >> lane & 1)) t.free[t.n_pages - held - rank] = p;
-  });
+  compact_refs(a, moved, threadIdx.x, kCompactThreads);
+  for (int b = wave; b < t.batch; b += kWaves) compact_row(a, moved, lowest, b, lane, kWave);
 }
-// The pages that move are the highest ones held: an entry from the lowest of them on is one of them.
 __global__ __launch_bounds__(256) void pages_compact_table_kernel(CompactArgs a) {
-  const SharedTables& t = a.t;
-  const int32_t *to = a.scratch, *head = to + t.n_pages;
-  const int lowest = head[0], b = blockIdx.y, n = page_count(length_of(t, b), t.logP);
-  if (head[1] == 0) return;
-  for (int j = blockIdx.x * 256 + threadIdx.x; j < n; j += gridDim.x * 256) {
-    int32_t* at = t.table + (int64_t)b * t.max_pages + j;
-    const int p = *at;
-    if (p >= lowest && p < t.n_pages) *at = to[p];
-  }
+  const int lowest = compact_head(a)[0], moved = compact_head(a)[1], at = blockIdx.x * 256 + threadIdx.x, step = gridDim.x * 256;
+  if (moved == 0) return;
+  if ((int)blockIdx.y < a.t.batch) compact_row(a, moved, lowest, blockIdx.y, at, step);
+  else compact_refs(a, moved, at, step);
 }
 
 // ------------------------------------------------------------------------------------------------ copying
@@ -524,7 +552,7 @@ __global__ __launch_bounds__(256) void pages_copy_kernel(Pages from, Pages to, i
 }
 int64_t copy_pieces(const Pages& S) { return (((int64_t)S.H << (S.logP + 8)) + kCopyBytes - 1) / kCopyBytes; }
 
-bool fork_in_one(int batch, int max_pages) { return (int64_t)batch * max_pages <= kForkEntries; }
+bool fork_in_one(int batch, int max_pages) { return (int64_t)batch * max_pages <= kSmallTable; }
 
 }  // namespace
 
@@ -536,7 +564,7 @@ size_t pages_fork_bytes(int batch, int max_pages) {
 size_t pages_compact_bytes(int n_pages) { return sizeof(int32_t) * ((size_t)n_pages + 4) + sizeof(long long) * (((size_t)n_pages + 63) / 64 + 1); }
 
 hipError_t launch_pages_grow(const GrowArgs& a, hipStream_t st) {
-  if (a.t.batch <= 256 && (int64_t)a.t.batch * a.t.max_pages <= kForkEntries) pages_grow_kernel<256><<<1, 256, 0, st>>>(a);
+  if (a.t.batch <= 256 && (int64_t)a.t.batch * a.t.max_pages <= kSmallTable) pages_grow_kernel<256><<<1, 256, 0, st>>>(a);
   else pages_grow_kernel<kSharedBatch><<<1, kSharedBatch, 0, st>>>(a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.n_slots <= kResizeOneSlots) return e;
@@ -560,11 +588,13 @@ hipError_t launch_pages_fork(const ForkArgs& a, hipStream_t st) {
 }
 
 hipError_t launch_pages_compact(const CompactArgs& a, hipStream_t st) {
-  if (a.t.n_pages <= kCompactWords * kWave) pages_compact_kernel<true><<<1, kCompactThreads, 0, st>>>(a);
-  else pages_compact_kernel<false><<<1, kCompactThreads, 0, st>>>(a);
+  const bool lds = a.t.n_pages <= kCompactWords * kWave, one = lds && (int64_t)a.t.batch * a.t.max_pages <= kSmallTable;
+  if (one) pages_compact_kernel<true, true><<<1, kCompactThreads, 0, st>>>(a);
+  else if (lds) pages_compact_kernel<true, false><<<1, kCompactThreads, 0, st>>>(a);
+  else pages_compact_kernel<false, false><<<1, kCompactThreads, 0, st>>>(a);
   const hipError_t e = hipGetLastError();
-  if (e != hipSuccess || a.t.batch == 0) return e;
-  pages_compact_table_kernel<<<dim3((unsigned)std::min(16, (a.t.max_pages + 255) / 256), (unsigned)a.t.batch), 256, 0, st>>>(a);
+  if (e != hipSuccess || one) return e;
+  pages_compact_table_kernel<<<dim3((unsigned)std::min(16, (a.t.max_pages + 255) / 256), (unsigned)a.t.batch + 1), 256, 0, st>>>(a);
   return hipGetLastError();
 }
 
