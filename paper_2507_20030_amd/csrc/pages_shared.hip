@@ -21,7 +21,7 @@ constexpr int kPlaces = 4;         // of a wave in the first launch
 constexpr int kShareThreads = 1024;
 constexpr int kMostEvents = 3 * kSharedBatch;  // where a set begins or ends; sequences that fork have fewer than 3 each
 constexpr int kSharedParts = 512;  // of a call: two workgroups on each CU
-constexpr int kSharedFew = 32;     // runs of up to so many rows go to few_rows
+constexpr int kSharedFew = 64;      // runs of up to so many rows go to few_rows
 constexpr int kPlanMark = 0x49574446;
 
 struct PlanHead {
@@ -126,13 +126,16 @@ __global__ __launch_bounds__(WAVES* kWave) void plan_sets_kernel(PlanArgs a) {
   for (int d = 1; d < kWave; d <<= 1) most = max(most, __shfl_xor(most, d));
   int n = 0;
   if (c0 < most) {
-    int prev[EACH];
+    int prev[EACH], entry[EACH][kPlaces + 1];  // pages of the places, the one before them first
     uint32_t name[EACH][kPlaces / 2];
 #pragma unroll
     for (int i = 0; i < EACH; ++i) {
       prev[i] = -2;
 #pragma unroll
       for (int c = 0; c < kPlaces / 2; ++c) name[i][c] = 0xffffffffu;
+      const int32_t* at = a.table + (int64_t)(lane + kWave * i) * a.S.max_pages + c0;
+#pragma unroll
+      for (int c = 0; c <= kPlaces; ++c) entry[i][c] = c0 + c - 1 >= 0 && c0 + c - 1 < pages[i] ? at[c - 1] : -1;
     }
 #pragma unroll
     for (int cc = -1; cc < kPlaces; ++cc) {
@@ -147,7 +150,7 @@ __global__ __launch_bounds__(WAVES* kWave) void plan_sets_kernel(PlanArgs a) {
         const int x = lane + kWave * i;
         cur[i] = -1, at[i] = -1;
         if (c < pages[i]) {
-          const int page = a.table[(int64_t)x * a.S.max_pages + c];
+          const int page = entry[i][cc + 1];
           cur[i] = x;  // a page that is not there is shared with nobody
           if ((uint32_t)page < (uint32_t)a.S.n_pages) {
             uint32_t s = ((uint32_t)page * 2654435769u) >> 8;
@@ -208,35 +211,35 @@ __device__ __forceinline__ int tokens_seen(const PlanArgs& a, int t0, int t1, in
   return min(near + sinks, t1 - t0);
 }
 
-// One workgroup: the runs from the events, which lie in the order of their places.
-__global__ __launch_bounds__(kShareThreads) void plan_share_kernel(PlanArgs a) {
-  __shared__ int32_t leader[kMostEvents], from[kMostEvents], news[kMostEvents], tiles[kMostEvents], base[kShareThreads];
-  __shared__ long long lds1[kShareThreads / kWave][1], lds3[kShareThreads / kWave][3];
-  __shared__ float lds_f[kShareThreads / kWave][4];
+// One workgroup: the runs from the events, which lie in the order of their places.  THREADS: 256 for up to 64 sequences, whose events one thread each can have
+// as a rule: sums over 16 waves take longer.
+template <int THREADS>
+__global__ __launch_bounds__(THREADS) void plan_share_kernel(PlanArgs a) {
+  constexpr int kEvents = THREADS == kShareThreads ? kMostEvents : 3 * kWave;
+  __shared__ int32_t leader[kEvents], from[kEvents], news[kEvents], tiles[kEvents], base[THREADS];
+  __shared__ long long lds2[THREADS / kWave][2], lds4[THREADS / kWave][4];
+  __shared__ float lds_f[THREADS / kWave][4];
   const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
   const float slices = (float)(a.n_layers * a.S.H);
-  {  // starts that overlap: rows would belong to several sequences, nothing is done
-    const int x[1] = {tid < a.batch ? news_of(a, tid).n : 0};
-    long long before[1], all[1];
-    sums_before<kShareThreads>(x, before, all, lds1);
-    if (all[0] > a.n_tokens) {
+  int n = 0;
+  bool unshared = false;
+  for (int c0 = 0; c0 < a.z.chunks; c0 += THREADS) {
+    const int c = c0 + tid, mine = c < a.z.chunks ? a.p.counts[c] : 0;
+    int x[2] = {mine, 0};
+    if (c0 == 0)
+      for (int b = tid; b < a.batch; b += THREADS) x[1] += news_of(a, b).n;
+    long long before[2], all[2];
+    sums_before<THREADS>(x, before, all, lds2);
+    if (c0 == 0 && all[1] > a.n_tokens) {  // starts that overlap: rows would belong to several sequences, nothing is done
       if (tid == 0) *a.p.head = PlanHead{};
       return;
     }
-  }
-  int n = 0;
-  bool unshared = false;
-  for (int c0 = 0; c0 < a.z.chunks && !unshared; c0 += kShareThreads) {
-    const int c = c0 + tid, mine = c < a.z.chunks ? a.p.counts[c] : 0;
-    const int x[1] = {mine};
-    long long before[1], all[1];
-    sums_before<kShareThreads>(x, before, all, lds1);
     unshared = __syncthreads_or(mine > a.z.events) || n + all[0] > a.z.events;
     if (unshared) break;
     base[tid] = (int)before[0];
     __syncthreads();
-    for (int e = tid; e < (int)all[0]; e += kShareThreads) {
-      int lo = 0, hi = kShareThreads;  // largest with base <= e
+    for (int e = tid; e < (int)all[0]; e += THREADS) {
+      int lo = 0, hi = THREADS;  // largest with base <= e
       while (hi - lo > 1) {
         const int m = (lo + hi) >> 1;
         if (base[m] <= e) lo = m;
@@ -252,7 +255,7 @@ __global__ __launch_bounds__(kShareThreads) void plan_share_kernel(PlanArgs a) {
     if (unshared) {
       __syncthreads();
       n = a.batch;
-      for (int i = tid; i < n; i += kShareThreads) leader[i] = i, from[i] = 0, news[i] = news_of(a, i).n;
+      for (int i = tid; i < n; i += THREADS) leader[i] = i, from[i] = 0, news[i] = news_of(a, i).n;
       __syncthreads();
     }
     const auto end_of = [&](int i) {
@@ -264,14 +267,16 @@ __global__ __launch_bounds__(kShareThreads) void plan_share_kernel(PlanArgs a) {
     const auto is_many = [&](int rows) { return rows > kSharedFew; };
     const auto blocks_of = [&](int rows) { return is_many(rows) ? (rows + Many::rows - 1) / Many::rows : (rows + a.few_rows - 1) / a.few_rows; };
     float sums[4] = {0.f, 0.f, 0.f, 0.f};  // tiles times blocks and blocks, of the few and of the many
-    for (int i = tid; i < n; i += kShareThreads) {
-      const int to = end_of(i), rows = rows_of(i), tile = is_many(rows) ? Many::tile : Few<1>::tile;
+    int to = 0;
+    for (int i = tid; i < n; i += THREADS) {
+      const int rows = rows_of(i), tile = is_many(rows) ? Many::tile : Few<1>::tile;
+      to = end_of(i);
       const int seen = tokens_seen(a, from[i] << a.S.logP, to << a.S.logP, news_of(a, leader[i]).len - 1);
-      if (to <= from[i]) news[i] = 0;
       tiles[i] = to > from[i] && rows ? max((seen + tile - 1) / tile, 1) : 0;
       const float blocks = tiles[i] ? (float)blocks_of(rows) : 0.f;
-      const int k = is_many(rows) ? 2 : 0;
-      sums[k] += blocks * (float)tiles[i], sums[k + 1] += blocks;
+      const bool many = is_many(rows);
+      sums[0] += many ? 0.f : blocks * (float)tiles[i], sums[1] += many ? 0.f : blocks;
+      sums[2] += many ? blocks * (float)tiles[i] : 0.f, sums[3] += many ? blocks : 0.f;
     }
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
@@ -284,48 +289,52 @@ __global__ __launch_bounds__(kShareThreads) void plan_share_kernel(PlanArgs a) {
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
       float sum = 0.f, blocks = 0.f;
-      for (int w = 0; w < kShareThreads / kWave; ++w) sum += lds_f[w][2 * k], blocks += lds_f[w][2 * k + 1];
+#pragma unroll
+      for (int w = 0; w < THREADS / kWave; ++w) sum += lds_f[w][2 * k], blocks += lds_f[w][2 * k + 1];
       sum *= slices, blocks *= slices;
       const float alone = fminf(ceilf(sum / (float)kCus), (float)(k ? Many::pair : Few<1>::pair));
       per[k] = fminf(fmaxf(fmaxf((float)kLeastTiles, alone), ceilf(sum / fmaxf((float)kSharedParts - blocks, 0.5f * kSharedParts))), 1e9f);
     }
-    __syncthreads();
-    // where everything lies; longer parts where the sums of all of them would not fit
-    const auto parts_of = [&](int i) { return i < n && tiles[i] ? max(1, (int)ceilf((float)tiles[i] / per[is_many(rows_of(i))])) : 0; };
-    long long mem, items, slots;
+    // where everything lies, items of the many first; longer parts where the sums of all of them would not fit
+    struct Place {
+      int np;
+      long long mem, many, few, slot;
+    };
+    long long sum[4];  // rows, items of the many and of the few, rows of sums
+    const auto places = [&](int i, long long (&done)[4]) {  // of run i of this thread, behind `done`
+      const bool there = i < n && tiles[i];
+      const int rows = there ? rows_of(i) : 0;
+      const bool many = is_many(rows);
+      const int np = there ? max(1, (int)ceilf((float)tiles[i] / (many ? per[1] : per[0]))) : 0;
+      const int items = (int)min((long long)blocks_of(rows) * np, 0x3fffffffll);
+      const int x[4] = {there ? news[i] : 0, many ? items : 0, many ? 0 : items, (int)min((long long)rows * np, 0x7fffffffll)};
+      long long before[4], all[4];
+      sums_before<THREADS>(x, before, all, lds4);
+      const Place p{np, done[0] + before[0], done[1] + before[1], done[2] + before[2], done[3] + before[3]};
+#pragma unroll
+      for (int c = 0; c < 4; ++c) done[c] += all[c];
+      return p;
+    };
+    Place p{};
     for (;;) {
-      mem = items = slots = 0;
-      for (int i0 = 0; i0 < n; i0 += kShareThreads) {
-        const int i = i0 + tid, np = parts_of(i), rows = np ? rows_of(i) : 0;
-        const int x[3] = {np ? news[i] : 0, min(blocks_of(rows), 1 << 20) * min(np, 1 << 10), (int)min((long long)rows * np, 0x7fffffffll)};
-        long long before[3], all[3];
-        sums_before<kShareThreads>(x, before, all, lds3);
-        mem += all[0], items += all[1], slots += all[2];
-      }
-      if ((slots <= a.z.slots && items <= a.z.items) || per[0] > 1e8f) break;
+      sum[0] = sum[1] = sum[2] = sum[3] = 0;
+      for (int i0 = 0; i0 < n; i0 += THREADS) p = places(i0 + tid, sum);
+      if ((sum[3] <= a.z.slots && sum[1] + sum[2] <= a.z.items) || per[0] > 1e8f) break;
       per[0] *= 2.f, per[1] *= 2.f;
     }
-    if (!unshared && (slots > a.z.slots || items > a.z.items || mem > a.z.mem)) continue;
-
-    mem = items = slots = 0;
-    long long many = 0;
-    for (int pass = 0; pass < 2; ++pass) {  // items of the many first
-      for (int i0 = 0; i0 < n; i0 += kShareThreads) {
-        const int i = i0 + tid;
-        const bool here = i < n && is_many(rows_of(i)) == (pass == 0);
-        const int np = here ? parts_of(i) : 0, rows = np ? rows_of(i) : 0;
-        const int x[3] = {np ? news[i] : 0, blocks_of(rows) * np, rows * np};
-        long long before[3], all[3];
-        sums_before<kShareThreads>(x, before, all, lds3);
-        if (here)
-          a.p.runs[i] = Run{leader[i], from[i], np ? end_of(i) : from[i], np ? news[i] : 0, (int)(mem + before[0]), (int)(items + before[1]), np, (int)(slots + before[2])};
-        mem += all[0], items += all[1], slots += all[2];
+    if (!unshared && (sum[3] > a.z.slots || sum[1] + sum[2] > a.z.items || sum[0] > a.z.mem)) continue;
+    long long done[4] = {0, 0, 0, 0};
+    for (int i0 = 0; i0 < n; i0 += THREADS) {
+      const int i = i0 + tid;
+      if (n > THREADS) p = places(i, done), to = i < n ? end_of(i) : 0;
+      if (i < n) {
+        const bool many = is_many(rows_of(i));
+        a.p.runs[i] = Run{leader[i], from[i], p.np ? to : from[i], p.np ? news[i] : 0, (int)p.mem, (int)(many ? p.many : sum[1] + p.few), p.np, (int)p.slot};
       }
-      if (pass == 0) many = items;
     }
     if (tid == 0)
       *a.p.head = PlanHead{kPlanMark, a.n_layers, a.S.H, a.S.G, a.S.logP, a.S.max_pages, a.batch, a.n_tokens, a.n_sink, a.n_recent, a.few_rows,
-                           n, (int)many, (int)(items - many), (int)slots, unshared ? 1 : 0};
+                           n, (int)sum[1], (int)sum[2], (int)sum[3], unshared ? 1 : 0};
     return;
   }
 }
@@ -346,24 +355,43 @@ __global__ __launch_bounds__(256) void plan_rows_kernel(PlanArgs a) {
     for (int i0 = 0; i0 < n && s.n; i0 += kWave) {
       const int i = i0 + lane;
       const Run mine = i < n ? a.p.runs[i] : Run{};
-      unsigned long long in = __ballot(mine.tokens > 0 && holds(x, s, mine));
-      for (; in; in &= in - 1, ++k) {
-        const Run r = a.p.runs[i0 + __builtin_ctzll(in)];
-        int before = 0;
-        if (!unshared)
-          for (int y0 = 0; y0 < x; y0 += kWave) {
-            const int y = y0 + lane;
-            if (y < x) {
-              const News o = news_of(a, y);
-              before += holds(y, o, r) ? o.n : 0;
-            }
-          }
-#pragma unroll
-        for (int d = 1; d < kWave; d <<= 1) before += __shfl_xor(before, d);
-        for (int t = lane; t < s.n; t += kWave)
-          if (r.mem + before + t < a.z.mem) a.p.mem[r.mem + before + t] = make_int2(s.first + t, s.len - s.n + t);
-        if (lane == 0 && k < a.z.chain) a.p.chain[(int64_t)x * a.z.chain + k] = make_int4(r.slot + before * a.S.G, r.np, r.tokens * a.S.G, 0);
+      const bool member = mine.tokens > 0 && holds(x, s, mine);
+      const unsigned long long in = __ballot(member);
+      // its rows begin behind those of the sequences before it: a lane for each run, or for each sequence
+      int before = 0;
+      const bool each_run = !unshared && __popcll(in) * ((x + kWave - 1) / kWave) > x / 4;
+      if (each_run && member) {
+#pragma unroll 4
+        for (int y = 0; y < x; ++y) {
+          const News o = news_of(a, y);
+          before += holds(y, o, mine) ? o.n : 0;
+        }
       }
+      for (unsigned long long rest = in; rest && !each_run && !unshared; rest &= rest - 1) {
+        const int l = __builtin_ctzll(rest);
+        const Run r = a.p.runs[i0 + l];
+        int sum = 0;
+        for (int y = lane; y < x; y += kWave) {
+          const News o = news_of(a, y);
+          sum += holds(y, o, r) ? o.n : 0;
+        }
+#pragma unroll
+        for (int d = 1; d < kWave; d <<= 1) sum += __shfl_xor(sum, d);
+        before = lane == l ? sum : before;
+      }
+      const int at = k + __popcll(in & ((1ull << lane) - 1));
+      if (member && at < a.z.chain) a.p.chain[(int64_t)x * a.z.chain + at] = make_int4(mine.slot + before * a.S.G, mine.np, mine.tokens * a.S.G, 0);
+      if (s.n <= 4) {
+        for (int t = 0; t < s.n; ++t)
+          if (member && mine.mem + before + t < a.z.mem) a.p.mem[mine.mem + before + t] = make_int2(s.first + t, s.len - s.n + t);
+      } else {
+        for (unsigned long long rest = in; rest; rest &= rest - 1) {
+          const int l = __builtin_ctzll(rest), to = __builtin_amdgcn_readlane(mine.mem + before, l);
+          for (int t = lane; t < s.n; t += kWave)
+            if (to + t < a.z.mem) a.p.mem[to + t] = make_int2(s.first + t, s.len - s.n + t);
+        }
+      }
+      k += __popcll(in);
     }
     for (int t = lane; t < s.n; t += kWave) a.p.owner[s.first + t] = make_int2(x, t);
     if (lane == 0) a.p.chained[x] = min(k, a.z.chain);
@@ -461,7 +489,8 @@ __global__ __launch_bounds__(kWaves* kWave, BF16 ? 2 : (R == 1 && !MANY ? 2 : 1)
   if constexpr (R > 0) few_rows<BF16, R, kWaves>(s.a, Items(s, false, threadIdx.x % kWave), x, gridDim.x);
 }
 
-// A row's parts, run by run.  Few rows: a workgroup for each, its waves take the parts in turn.  Many: a wave for each.
+// A row's parts: its runs' first rows of sums and numbers of parts, a lane for each, become a list of all parts; a lane for each reads its reference, then all
+// sums are on their way at once.  Few rows: a workgroup for each, its waves share the parts.  Many: a wave for each.
 constexpr int64_t kManyShared = 4096;
 template <bool BF16>
 __global__ __launch_bounds__(kWaves* kWave) void shared_join_kernel(SharedAttn s, int64_t all, int many) {
@@ -469,25 +498,45 @@ __global__ __launch_bounds__(kWaves* kWave) void shared_join_kernel(SharedAttn s
   const PagesAttn& a = s.a;
   if (!is_for(*s.p.head, s)) return;
   const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), slots = s.p.head->slots, G = a.S.G;
-  for (int64_t x = many ? (int64_t)blockIdx.x * kWaves + wave : blockIdx.x; x < all; x += (int64_t)gridDim.x * (many ? kWaves : 1)) {
-    const int lh = (int)(x / ((int64_t)a.n_tokens * G)), r = (int)(x - (int64_t)lh * a.n_tokens * G), token = (int)((uint32_t)r / (uint32_t)G);
+  const uint32_t row_heads = (uint32_t)(a.n_tokens * G);
+  for (uint32_t x = many ? blockIdx.x * kWaves + wave : blockIdx.x; x < (uint32_t)all; x += gridDim.x * (many ? kWaves : 1)) {
+    const int lh = (int)(x / row_heads), r = (int)(x - (uint32_t)lh * row_heads), token = (int)((uint32_t)r / (uint32_t)G);
     const int2 owner = s.p.owner[token];
     const int b = __builtin_amdgcn_readfirstlane(owner.x), mine = __builtin_amdgcn_readfirstlane(owner.y) * G + r - token * G;
     if (b < 0) continue;  // behind the last sequence
-    const int n = s.p.chained[b], k0 = many ? 0 : wave, dk = many ? 1 : kWaves;
+    const int n = __builtin_amdgcn_readfirstlane(s.p.chained[b]);
+    const int64_t slot0 = (int64_t)lh * slots + mine;
     float m = -FLT_MAX, l = 0.f;
     float2 o = make_float2(0.f, 0.f);
-    const auto add = [&](float2 st, float2 v) {  // (reference, sum of weights), sum
-      const float up = fmaxf(m, st.x), f = __builtin_amdgcn_exp2f(0.5f * (m - up)), g = __builtin_amdgcn_exp2f(0.5f * (st.x - up));
-      o.x = o.x * (f * f) + v.x * (g * g), o.y = o.y * (f * f) + v.y * (g * g), l = l * f * f + st.y * g * g, m = up;
+    const auto add = [&](float top, float2 v, float sum, float half) {  // half: 2^(half of the reference's distance)
+      const float up = fmaxf(m, top), f = __builtin_amdgcn_exp2f(0.5f * (m - up));
+      o.x = o.x * (f * f) + v.x * (half * half), o.y = o.y * (f * f) + v.y * (half * half), l = l * f * f + sum * half * half, m = up;
     };
-    for (int i = 0; i < n; ++i) {
-      const int4 run = s.p.chain[(int64_t)b * s.z.chain + i];
-      const int64_t slot = (int64_t)lh * slots + run.x + mine;
+    for (int i0 = 0; i0 < n; i0 += kWave) {
+      const int4 run = i0 + lane < n ? s.p.chain[(int64_t)b * s.z.chain + i0 + lane] : make_int4(0, 0, 0, 0);
+      const int to = scan(run.y), parts = last_lane(to), size = many ? kWave : min(kWave, (parts + kWaves - 1) / kWaves);
+      for (int p0 = many ? 0 : wave * size; p0 < parts; p0 += size * (many ? 1 : kWaves)) {
+        const int part = p0 + lane, here = min(parts - p0, size);
+        int which = 0;  // the run of the lane's part: how many end before it
+        for (int c = 0; c < min(n - i0, kWave); ++c) which += __builtin_amdgcn_readlane(to, c) <= part;
+        which = min(which, kWave - 1);
+        const int64_t at = slot0 + __shfl(run.x, which) + (int64_t)(part - (__shfl(to, which) - __shfl(run.y, which))) * __shfl(run.z, which);
+        const float2 st = lane < here ? s.stat[at] : make_float2(-FLT_MAX, 0.f);
+        float top = st.x;
+#pragma unroll
+        for (int d = 1; d < kWave; d <<= 1) top = fmaxf(top, __shfl_xor(top, d));
+        const float up = fmaxf(m, top), g = __builtin_amdgcn_exp2f(0.5f * (st.x - up)), f = __builtin_amdgcn_exp2f(0.5f * (m - up));
+        float sum = st.y * g * g;  // a denominator's share may need both factors
+#pragma unroll
+        for (int d = 1; d < kWave; d <<= 1) sum += __shfl_xor(sum, d);
+        l = l * f * f + sum, o.x *= f * f, o.y *= f * f, m = up;
 #pragma unroll 8
-      for (int k = k0; k < run.y; k += dk) {
-        const int64_t at = slot + (int64_t)k * run.z;
-        add(s.stat[at], *(const float2*)(s.part + at * kHeadDim + 2 * lane));
+        for (int c = 0; c < here; ++c) {
+          const int64_t row = (int64_t)(uint32_t)__builtin_amdgcn_readlane((int)at, c) | (int64_t)__builtin_amdgcn_readlane((int)(at >> 32), c) << 32;
+          const float2 v = *(const float2*)(s.part + row * kHeadDim + 2 * lane);
+          const float w = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(g), c)), ww = w * w;
+          o.x += v.x * ww, o.y += v.y * ww;
+        }
       }
     }
     if (!many) {
@@ -496,7 +545,7 @@ __global__ __launch_bounds__(kWaves* kWave) void shared_join_kernel(SharedAttn s
       __syncthreads();
       m = -FLT_MAX, l = 0.f, o = make_float2(0.f, 0.f);
 #pragma unroll
-      for (int i = 0; i < kWaves; ++i) add(stats[i], sums[i][lane]);
+      for (int i = 0; i < kWaves; ++i) add(stats[i].x, sums[i][lane], stats[i].y, __builtin_amdgcn_exp2f(0.5f * (stats[i].x - fmaxf(m, stats[i].x))));
       __syncthreads();
       if (wave) continue;
     }
@@ -554,7 +603,8 @@ hipError_t launch_pages_plan(const PagesAttn& g, bool bf16, void* plan, hipStrea
   else plan_sets_kernel<16, 2><<<grid(2), 2 * kWave, 0, st>>>(a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  plan_share_kernel<<<1, kShareThreads, 0, st>>>(a);
+  if (g.batch <= kWave) plan_share_kernel<256><<<1, 256, 0, st>>>(a);
+  else plan_share_kernel<kShareThreads><<<1, kShareThreads, 0, st>>>(a);
   e = hipGetLastError();
   if (e != hipSuccess) return e;
   plan_rows_kernel<<<(unsigned)((2 * g.batch + 64 + 3) / 4), 256, 0, st>>>(a);
