@@ -491,7 +491,7 @@ __global__ __launch_bounds__(kWaves* kWave, BF16 ? 2 : (R == 1 && !MANY ? 2 : 1)
 
 // A row's parts: its runs' first rows of sums and numbers of parts, a lane for each, become a list of all parts; a lane for each reads its reference, then all
 // sums are on their way at once.  Few rows: a workgroup for each, its waves share the parts.  Many: a wave for each.
-constexpr int64_t kManyShared = 4096;
+constexpr int64_t kManyShared = 2048;
 template <bool BF16>
 __global__ __launch_bounds__(kWaves* kWave) void shared_join_kernel(SharedAttn s, int64_t all, int many) {
   __shared__ float2 sums[kWaves][kWave], stats[kWaves];
