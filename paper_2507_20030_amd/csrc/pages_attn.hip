@@ -120,23 +120,22 @@ class Schedule {
 template <class Geo>
 class Sequences {
  public:
-  float* part;
-  float2* stat;
-
-  __device__ __forceinline__ Sequences(const PagesAttn& a, const PagesRows& which, int lane)
-      : part(which.part), stat(which.stat), a(a), plan(a, which, lane), slices((uint32_t)(a.n_layers * a.S.H)) {}
+  __device__ __forceinline__ Sequences(const PagesAttn& a, const PagesRows& which, int lane) : a(a), which(which), plan(a, which, lane) {}
+  __device__ __forceinline__ float* part() const { return which.part; }
+  __device__ __forceinline__ float2* stat() const { return which.stat; }
 
   struct Block {
     static constexpr int base = 0;
     const int32_t* table;
-    int layer, h, rows, p_lo, p_hi, from_lo, from_hi, part, np, last_page, lh, slot, row0, first, before;
+    int layer, h, rows, p_lo, p_hi, from_lo, part, np, last_page, lh, slot, row0, first, before;
     bool whole;
+    __device__ __forceinline__ int from_hi(const PagesAttn& a) const { return window_from(a, max(p_hi, -1)); }
   };
-  __device__ __forceinline__ uint32_t count() const { return (uint32_t)plan.w.parts * slices; }
+  __device__ __forceinline__ uint32_t count() const { return (uint32_t)plan.w.parts * slices(); }
   __device__ __forceinline__ Block block(uint32_t x) const {
     Block k;
-    k.lh = (int)(x % slices);  // workgroups are dealt to the XCDs in turn: with 8 heads each reads one head's pages
-    const Place at = plan.find((int)(x / slices), [](const Seq& s, int np) { return np * Schedule<Geo>::blocks(s.rows); });
+    k.lh = (int)(x % slices());  // workgroups are dealt to the XCDs in turn: with 8 heads each reads one head's pages
+    const Place at = plan.find((int)(x / slices()), [](const Seq& s, int np) { return np * Schedule<Geo>::blocks(s.rows); });
     const Seq& s = at.s;
     const int turn = (int)((uint32_t)at.at / (uint32_t)at.np), block = plan.blocks(s.rows) - 1 - turn;  // the longest first
     k.part = at.at - turn * at.np, k.np = at.np, k.whole = at.np == 1;
@@ -145,7 +144,7 @@ class Sequences {
     k.row0 = block * Geo::rows, k.rows = min(s.rows - k.row0, Geo::rows);
     k.first = s.first, k.before = s.len - s.nq;  // position of the sequence's first new token
     k.p_lo = k.before + (int)((uint32_t)k.row0 / G), k.p_hi = k.before + (int)((uint32_t)(k.row0 + k.rows - 1) / G);
-    k.from_lo = window_from(a, max(k.p_lo, -1)), k.from_hi = window_from(a, max(k.p_hi, -1));
+    k.from_lo = window_from(a, max(k.p_lo, -1));
     k.table = a.table + (int64_t)at.b * a.S.max_pages, k.last_page = max(page_count(s.len, a.S.logP) - 1, 0);
     k.slot = at.before + at.at;
     return k;
@@ -163,8 +162,9 @@ class Sequences {
 
  private:
   const PagesAttn& a;
+  const PagesRows& which;
   const Schedule<Geo> plan;
-  uint32_t slices;
+  __device__ __forceinline__ uint32_t slices() const { return (uint32_t)(a.n_layers * a.S.H); }
 };
 
 // ------------------------------------------------------------------------------------------------ joining the parts

@@ -181,7 +181,7 @@ __device__ __forceinline__ Span span_of(const PagesAttn& a, int base, int from, 
 //                        largest left border of their windows; part of np; whole: its results go to out
 //   row(block, r)        where row r of the block is and what it sees; any r, but what r >= rows gives is not used
 //   wave_rows(block, w)  what rows 32 w .. 32 w + 31 see: p_hi: their largest position, -1 without rows; from: their least left border
-//   slot(block)          the first row of its sums in part, stat
+//   slot(block)          the first row of its sums in part(), stat()
 // A row sees no token behind its position, which may be set lower to end the tokens that are its block's.
 struct RowAt {
   int64_t at;     // of q and out, in heads
@@ -270,8 +270,9 @@ __device__ __forceinline__ void few_rows(const PagesAttn& a, const Work& work, u
     for (int r = 0; r < R; ++r) {
       Rows<PARTS>& z = rt[r];
       const bool have = 16 * r + row < rows;
-      const RowAt mine_at = work.row(at, 16 * r + row);
-      z.pos = have ? mine_at.pos : -1, z.from = have ? mine_at.from : -1;
+      RowAt mine_at{0, -1, -1};
+      if (have) mine_at = work.row(at, 16 * r + row);
+      z.pos = mine_at.pos, z.from = mine_at.from;
       z.m = -FLT_MAX, z.l = 0.f;
 #pragma unroll
       for (int i = 0; i < 8; ++i) z.o[i] = floatx4{0.f, 0.f, 0.f, 0.f};
@@ -310,7 +311,7 @@ __device__ __forceinline__ void few_rows(const PagesAttn& a, const Work& work, u
       }
       const int t0 = at.base + span.tile(i) * kTile, t1 = t0 + kTile - 1, j0 = t0 + 8 * oct;
       // whether every row sees the whole tile
-      const bool edge = t1 > p_lo || (t1 >= sink && t0 <= at.from_hi) || __any(d.bad);
+      const bool edge = t1 > p_lo || (t1 >= sink && t0 <= at.from_hi(a)) || __any(d.bad);
       bool poison = false;
       if (edge) {  // tokens that no row sees may hold anything
         const uint32_t any = d.bad ? 0u : seen_bits(j0, all_from, p_hi, sink), keep[2] = {bytes_of_bits(any) * 0xffu, bytes_of_bits(any >> 4) * 0xffu};
@@ -445,9 +446,9 @@ __device__ __forceinline__ void few_rows(const PagesAttn& a, const Work& work, u
         store8<BF16>(a.out, work.row(at, 16 * r + jr).at * kHeadDim + jc, y, l == 0.f ? 0.f : 1.f / l);
       } else {
         const int64_t slot = work.slot(at) + 16 * r + jr;
-        float* to = work.part + slot * kHeadDim + jc;
+        float* to = work.part() + slot * kHeadDim + jc;
         *(float4*)to = make_float4(y[0], y[1], y[2], y[3]), *(float4*)(to + 4) = make_float4(y[4], y[5], y[6], y[7]);
-        if (jc == 0) work.stat[slot] = make_float2(m, l);
+        if (jc == 0) work.stat()[slot] = make_float2(m, l);
       }
     }
     __syncthreads();
@@ -694,7 +695,7 @@ __device__ __forceinline__ uint32_t many_rows(const PagesAttn& a, const Work& wo
       __syncthreads();
     };
     // The tiles that every row sees whole lie side by side, between the sinks and the window's left border and the diagonal.
-    const int full_from = max(t_from, a.n_recent ? max(max(at.from_hi + kTile - at.base, 0) / kTile - span.skip, span.sinks) : 0);
+    const int full_from = max(t_from, a.n_recent ? max(max(at.from_hi(a) + kTile - at.base, 0) / kTile - span.skip, span.sinks) : 0);
     const int full_to = min(t_to, (p_lo + 1 - at.base) / kTile - span.skip);
     int i = t_from;
     for (const int to = min(full_from, t_to); i < to; ++i) step(i, std::true_type{});
@@ -706,7 +707,7 @@ __device__ __forceinline__ uint32_t many_rows(const PagesAttn& a, const Work& wo
       const bool whole = at.whole;
       const int64_t slot = work.slot(at) + 32 * wave + row;
       const float inv = l == 0.f ? 0.f : 1.f / l;
-      float* to = work.part + slot * kHeadDim;
+      float* to = work.part() + slot * kHeadDim;
 #pragma unroll
       for (int p = 0; p < 2; ++p)
 #pragma unroll
@@ -721,7 +722,7 @@ __device__ __forceinline__ uint32_t many_rows(const PagesAttn& a, const Work& wo
             *(float4*)(to + c0) = make_float4(y[0], y[1], y[2], y[3]), *(float4*)(to + c0 + 4) = make_float4(y[4], y[5], y[6], y[7]);
           }
         }
-      if (!whole && grp == 0) work.stat[slot] = make_float2(m, l);
+      if (!whole && grp == 0) work.stat()[slot] = make_float2(m, l);
     }
   }
   return all;

@@ -427,17 +427,18 @@ __device__ __forceinline__ bool is_for(const PlanHead& h, const SharedAttn& s) {
 // The items of one kind: see pages_rows.h for what the kernels ask.
 class Items {
  public:
-  float* part;
-  float2* stat;
+  __device__ __forceinline__ float* part() const { return s.part; }
+  __device__ __forceinline__ float2* stat() const { return s.stat; }
 
   __device__ __forceinline__ Items(const SharedAttn& s, bool many, int lane)
-      : part(s.part), stat(s.stat), s(s), lane(lane), first(many ? 0 : s.p.head->many), n(many ? s.p.head->many : s.p.head->few), slots(s.p.head->slots),
+      : s(s), lane(lane), first(many ? 0 : s.p.head->many), n(many ? s.p.head->many : s.p.head->few), slots(s.p.head->slots),
         slices((uint32_t)(s.a.n_layers * s.a.S.H)) {}
 
   struct Block {
     const int32_t* table;
-    int layer, h, rows, p_lo, p_hi, from_lo, from_hi, part, np, last_page, base, last_token, mem, row0, lh, slot;
+    int layer, h, rows, p_lo, p_hi, from_lo, hi, part, np, last_page, base, last_token, mem, row0, lh, slot;
     static constexpr bool whole = false;
+    __device__ __forceinline__ int from_hi(const PagesAttn& a) const { return window_from(a, hi); }
   };
   __device__ __forceinline__ uint32_t count() const { return (uint32_t)n * slices; }
   __device__ __forceinline__ Block block(uint32_t x) const {
@@ -457,7 +458,7 @@ class Items {
 #pragma unroll
     for (int d = 1; d < kWave; d <<= 1) lo = min(lo, __shfl_xor(lo, d)), hi = max(hi, __shfl_xor(hi, d));
     lo = uni(lo), hi = uni(hi);
-    k.from_lo = window_from(a, lo), k.from_hi = window_from(a, hi), k.p_lo = min(lo, k.last_token), k.p_hi = min(hi, k.last_token);
+    k.from_lo = window_from(a, lo), k.hi = hi, k.p_lo = min(lo, k.last_token), k.p_hi = min(hi, k.last_token);
     return k;
   }
   __device__ __forceinline__ RowAt row(const Block& k, int r) const {
