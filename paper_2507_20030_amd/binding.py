@@ -786,9 +786,13 @@ class PagedCache:
     """Owns the arrays of an 8-bit paged cache of up to max_batch sequences of max_tokens tokens; methods forward to the C calls.
 
     A step: ``starts, slots = resize(want, n)``, and for each layer ``write(k, v, slots, layer)`` and ``attend(q, starts, layer)``; a sequence
-    that is to have 0 tokens gives its pages back.  ``compress`` hands what it holds to a frequency-domain cache."""
+    that is to have 0 tokens gives its pages back.  ``compress`` hands what it holds to a frequency-domain cache.
 
-    def __init__(self, n_layers, n_pages, n_kv_heads, n_q_heads, head_dim, dtype: torch.dtype, max_batch, max_tokens, page_tokens=32, device="cuda:0"):
+    With ``shared`` sequences may hold the same pages: ``fork`` lets them begin as others do, ``resize`` copies a page that others hold before its sequence writes to it,
+    ``plan`` finds out who shares what in a step, and ``attend`` with that plan reads shared pages once; ``compact`` and ``repool`` give memory back.
+    Up to 1024 sequences then."""
+
+    def __init__(self, n_layers, n_pages, n_kv_heads, n_q_heads, head_dim, dtype: torch.dtype, max_batch, max_tokens, page_tokens=32, device="cuda:0", shared=False):
         if dtype not in (torch.float32, torch.bfloat16):
             raise ValueError("dtype must be float32 or bfloat16")
         self.dtype, self.device, self.page_tokens = dtype, torch.device(device), page_tokens
@@ -801,22 +805,83 @@ class PagedCache:
         self.table = torch.full((max_batch, max_pages), -1, **ints)
         self.lens = torch.zeros(max_batch, **ints)
         self.free = torch.cat([torch.tensor([n_pages], **ints), torch.arange(n_pages, **ints)])
+        if shared:
+            iwdft_pages_fork_bytes(max_batch, max_pages)  # checks the sizes
+        self.refs = torch.zeros(n_pages, **ints) if shared else None
+
+    def _shares(self) -> None:
+        if self.refs is None:
+            raise ValueError("this cache was made without shared=True: a page belongs to one sequence")
 
     def resize(self, want: torch.Tensor, n_slots: int, stream=None):
         """want: int32 [max_batch] on the device.  Returns starts, slots; lens tells which sequences could not grow."""
         with _on_stream(stream, self.device):
             starts, slots = (torch.empty(n, dtype=torch.int32, device=self.device) for n in (self.lens.shape[0] + 1, n_slots))
-        iwdft_pages_resize(want, self.table, self.lens, self.free, starts, slots, self.page_tokens, stream)
+            copies = None if self.refs is None else torch.empty((self.lens.shape[0], 2), dtype=torch.int32, device=self.device)
+        if self.refs is None:
+            iwdft_pages_resize(want, self.table, self.lens, self.free, starts, slots, self.page_tokens, stream)
+        else:
+            iwdft_pages_resize_shared(want, self.table, self.lens, self.free, self.refs, starts, slots, copies, self.page_tokens, stream)
+            iwdft_pages_copy(copies, self.values, self.exponents, stream=stream)
         return starts, slots
+
+    def fork(self, parent: torch.Tensor, keep: Optional[torch.Tensor] = None, stream=None) -> None:
+        """parent, keep: int32 [max_batch] on the device.  Sequence b becomes the first keep[b] tokens (None, negative: all) of what sequence parent[b] was; b itself
+        where parent[b] is b or negative.  Nothing is copied."""
+        self._shares()
+        iwdft_pages_fork(parent, keep, self.table, self.lens, self.free, self.refs, self.page_tokens, stream)
+
+    def plan(self, starts, n_tokens: int, n_layers: int = 1, n_sink: int = 0, n_recent: int = 0, stream=None, plan: Optional[PagesPlan] = None) -> PagesPlan:
+        """Who shares what, for the step's ``attend`` calls on n_layers layers and n_tokens rows each; valid until the tables change."""
+        L, H, G, _ = self.shape
+        return iwdft_pages_plan(starts, self.table, self.lens, n_tokens, self.values.shape[1], H, G, self.page_tokens, self.dtype, n_layers, n_sink, n_recent, stream, plan)
+
+    def compact(self, n_moves: Optional[int] = None, stream=None) -> torch.Tensor:
+        """Moves held pages together at the pool's beginning, n_moves of them at most (None: all that have to).  Returns the moves, int32 [n_moves, 2]."""
+        self._shares()
+        n = self.values.shape[1] // 2 if n_moves is None else n_moves
+        with _on_stream(stream, self.device):
+            moves = torch.empty((n, 2), dtype=torch.int32, device=self.device)
+        iwdft_pages_compact(self.table, self.lens, self.free, self.refs, moves, self.page_tokens, stream)
+        iwdft_pages_copy(moves, self.values, self.exponents, stream=stream)
+        return moves
+
+    def repool(self, n_pages: int, stream=None) -> None:
+        """The sequences in a pool of n_pages pages, larger or smaller; plans made before are void.  Needs both pools at a time, and waits for the stream to learn how many pages are held."""
+        self._shares()
+        L, H, G, D = self.shape
+        iwdft_pages_query_bytes(pages_desc(L, n_pages, H, G, D, self.page_tokens, self.table.shape[1], self.dtype))
+        with _on_stream(stream, self.device):
+            held = self.values.shape[1] - int(self.free[0])
+        if held > n_pages:
+            raise ValueError(f"{held} pages are held, more than {n_pages}")
+        self.compact(stream=stream)
+        with _on_stream(stream, self.device):
+            ints = dict(dtype=torch.int32, device=self.device)
+            values = torch.zeros((L, n_pages, *self.values.shape[2:]), dtype=torch.uint8, device=self.device)
+            exponents = torch.zeros((L, n_pages, H, 2), **ints)
+            copies = torch.arange(held, **ints)[:, None].repeat(1, 2)
+            refs, free = torch.zeros(n_pages, **ints), torch.zeros(1 + n_pages, **ints)
+            refs[:held] = self.refs[:held]
+            none = torch.empty((0, 2), **ints)
+        iwdft_pages_copy(copies, self.values, self.exponents, values, exponents, stream=stream)
+        iwdft_pages_compact(self.table, self.lens, free, refs, none, self.page_tokens, stream)  # nothing moves: the stack of the new pool
+        self.values, self.exponents, self.refs, self.free = values, exponents, refs, free
 
     def write(self, k, v, slots, layer=0, stream=None):
         iwdft_pages_write(self.values, self.exponents, k, v, slots, layer, stream)
 
-    def attend(self, q, starts, layer=0, out=None, n_sink=0, n_recent=0, scale=0.0, stream=None):
-        """Without `out` a new tensor, which costs one more launch: rows behind the last sequence, which the attention leaves as they are, are 0 in it."""
+    def attend(self, q, starts, layer=0, out=None, n_sink=0, n_recent=0, scale=0.0, stream=None, plan: Optional[PagesPlan] = None):
+        """Without `out` a new tensor, which costs one more launch: rows behind the last sequence, which the attention leaves as they are, are 0 in it.  With a plan
+        of this step shared pages are read once; windows are the plan's."""
         if out is None:
             with _on_stream(stream, self.device):
                 out = torch.zeros_like(q)  # rows behind the last sequence
+        if plan is not None:
+            if (n_sink, n_recent) not in ((0, 0), (plan.n_sink, plan.n_recent)):
+                raise ValueError(f"the plan was made for windows {(plan.n_sink, plan.n_recent)}, not {(n_sink, n_recent)}")
+            iwdft_pages_attn_shared(self.values, self.exponents, q, plan, self.table, out, layer, scale, stream)
+            return out
         iwdft_pages_attn(self.values, self.exponents, q, starts, self.table, self.lens, out, layer, n_sink, n_recent, scale, stream)
         return out
 

@@ -394,3 +394,211 @@ def test_plans_that_do_not_fit():
             B.iwdft_pages_attn_shared(**args)
     with pytest.raises(ValueError):
         B.iwdft_pages_plan(ints(range(5)), pool.d_table, pool.d_lens, 4, pool.n_pages, 2, 4, 16, torch.float32, n_recent=9, plan=plan)
+
+
+# ------------------------------------------------------------------------------------------------------------------ together
+class Served:
+    """A shared PagedCache and the oracles of its tables and of its pool, through the same steps."""
+
+    def __init__(self, rng, batch, W, n_pages, P, heads, G, layers, dtype):
+        self.c = B.PagedCache(layers, n_pages, heads, heads * G, 128, DT[dtype], batch, W * P, P, DEV, shared=True)
+        self.t, self.store, self.rng, self.dtype, self.G = Tables(batch, W, n_pages, P), po.Store(layers, n_pages, heads, P), rng, dtype, G
+
+    def tokens(self, n, heads):
+        L = self.store.raw.shape[0]
+        return dev(self.rng.normal(size=(L, n, heads, 128)) * 2.0 ** self.rng.integers(-2, 3, size=(1, n, 1, 1))).to(DT[self.dtype])
+
+    def fork(self, parent, keep=None):
+        self.t.fork(parent, keep)
+        self.c.fork(ints(parent), None if keep is None else ints(keep))
+
+    def step(self, want, shared=True, **windows):
+        layers, _, heads = self.store.raw.shape[:3]
+        n = int(sum(max(0, w - h) for w, h in zip(want, self.t.lens))) + 2
+        starts, slots, copies = self.t.resize(want, n)
+        for a, b in copies[copies[:, 0] >= 0]:
+            self.store.raw[:, b], self.store.exponents[:, b] = self.store.raw[:, a], self.store.exponents[:, a]
+        k, v, q = self.tokens(n, heads), self.tokens(n, heads), self.tokens(n, heads * self.G)
+        self.store.write(f64(k), f64(v), list(slots))
+        d_starts, d_slots = self.c.resize(ints(want), n)
+        assert np.array_equal(d_starts.cpu().numpy(), starts) and np.array_equal(d_slots.cpu().numpy(), slots)
+        plan = self.c.plan(d_starts, n, **windows) if shared else None
+        outs = []
+        for layer in range(layers):
+            self.c.write(k[layer:layer + 1], v[layer:layer + 1], d_slots, layer)
+            outs.append(self.c.attend(q[layer:layer + 1], d_starts, layer, plan=plan, **({} if shared else windows)))
+        out = torch.cat(outs)
+        ref, *rest = self.store.attend(f64(q), starts, self.t.table, self.t.lens, **windows)
+        m = int(starts[-1])
+        near(out[:, :m], ref[:, :m], *(r[:, :m] for r in rest), self.dtype)
+        assert not out[:, m:].any()
+
+    def same_pool(self):
+        held = np.flatnonzero(self.t.refs > 0)
+        assert np.array_equal(self.c.refs.cpu().numpy()[held], self.t.refs[held]) and np.array_equal(self.c.lens.cpu().numpy(), self.t.lens)
+        assert np.array_equal(self.c.values[:, held].cpu().numpy(), self.store.packed()[:, held])
+        assert np.array_equal(self.c.exponents[:, held].cpu().numpy(), self.store.exponents[:, held])
+
+
+@pytest.mark.parametrize("dtype,P,G,windows", [("bf16", 32, 4, {}), ("f32", 16, 2, {}), ("bf16", 16, 8, dict(n_sink=3, n_recent=60))])
+def test_beams_from_a_prompt_to_an_answer(dtype, P, G, windows):
+    """A prompt, its samples, steps of beam search that drop and double beams, a second prompt, drafts taken back, pages moved together, another pool."""
+    rng = np.random.default_rng(P + G)
+    s = Served(rng, 8, 12, 90, P, 2, G, 2, dtype)
+    s.step([5 * P + 3, 0, 0, 0, 0, 0, 0, 0], **windows)
+    s.fork([0] * 6 + [6, 7])
+    s.same_pool()
+    for r in range(6):
+        s.step([n + 1 if n and b != 3 else -1 for b, n in enumerate(s.t.lens)], shared=r != 2, **windows)
+        s.same_pool()
+        if r == 1:
+            s.step([-1] * 6 + [3 * P, 40], **windows)
+        s.fork(rng.choice(6, size=6).tolist() + [6, 7 if r < 4 else 6], None if r % 2 else [-1] * 7 + [2 * P + 5])
+    s.step([int(n) + 3 for n in s.t.lens], **windows)                      # drafts
+    s.step([max(0, int(n) - 2) for n in s.t.lens], **windows)              # two of three are taken back
+    for n_moves in (3, 45):
+        for a, b in s.t.compact(n_moves):
+            if a >= 0:
+                s.store.raw[:, b], s.store.exponents[:, b] = s.store.raw[:, a], s.store.exponents[:, a]
+        s.c.compact(n_moves)
+        s.same_pool()
+    held = int((s.t.refs > 0).sum())
+    before = s.c.read(40)
+    with pytest.raises(ValueError):
+        s.c.repool(held - 1)
+    for n_pages in (held + 40, held):
+        s.c.repool(n_pages)
+        assert s.c.values.shape[1] == n_pages and int(s.c.free[0]) == n_pages - held and all(torch.equal(x, y) for x, y in zip(before, s.c.read(40)))
+        assert s.c.free[1:1 + n_pages - held].tolist() == list(range(n_pages - 1, held - 1, -1))
+    s.c.fork(ints(range(8)), ints([0] * 8))
+    assert int(s.c.free[0]) == held and not s.c.refs.any() and not s.c.lens.any()
+
+
+def test_a_shared_beginning_is_compressed():
+    """Two requests with one beginning, handed to the frequency domain together: as from pages of their own."""
+    rng = np.random.default_rng(7)
+    c = B.PagedCache(1, 60, 2, 4, 128, torch.bfloat16, 3, 400, 16, DEV, shared=True)
+    x = dev(rng.normal(size=(2, 1, 300, 2, 128))).bfloat16()
+    _, slots = c.resize(ints([300, 0, 0]), 300)
+    c.write(x[0], x[1], slots)
+    c.fork(ints([0, 0, 2]), ints([-1, 272, -1]))
+    K, V = c.read(272)
+    assert torch.equal(K[:, 0], K[:, 1]) and torch.equal(V[:, 0], V[:, 1])
+    frozen = B.Cache(1, 2, 2, 4, 128, torch.bfloat16, 256, [np.arange(32, dtype=np.int32)], n_sink=4, n_recent=12, device=DEV)
+    assert c.compress(frozen, sequences=[1, 0]) == [0, 28]
+    a, b = frozen.export_coeffs(0)
+    assert torch.equal(a[0], a[1]) and torch.equal(b[0], b[1])
+    frozen.close()
+
+
+def test_a_captured_step_replayed():
+    """Fork, growth with copies on write, writing, the plan and attention of two layers in a graph: every replay as the same step issued call by call, with eager work in between."""
+    rng = np.random.default_rng(11)
+    P, batch, H, G, n = 16, 6, 2, 4, 12
+
+    def cache():
+        return B.PagedCache(2, 80, H, H * G, 128, torch.bfloat16, batch, 20 * P, P, DEV, shared=True)
+
+    first = torch.Generator(device=DEV).manual_seed(1)
+    x = torch.randn((2, 2, 100, H, 128), device=DEV, generator=first).bfloat16()
+    caches = [cache(), cache()]
+    for c in caches:
+        _, slots = c.resize(ints([100, 0, 0, 0, 0, 0]), 100)
+        c.write(x[0], x[1], slots)
+    parent, want = ints([0] * 6), ints([-1] * 6)
+    k, v = (torch.zeros((2, n, H, 128), device=DEV, dtype=torch.bfloat16) for _ in range(2))
+    q, out = (torch.zeros((2, n, H * G, 128), device=DEV, dtype=torch.bfloat16) for _ in range(2))
+
+    def step(c, out):
+        c.fork(parent)
+        starts, slots = c.resize(want, n)
+        plan = c.plan(starts, n)
+        for layer in range(2):
+            c.write(k[layer:layer + 1], v[layer:layer + 1], slots, layer)
+            c.attend(q[layer:layer + 1], starts, layer, out=out[layer:layer + 1], plan=plan)
+
+    stream = torch.cuda.Stream()
+    with torch.cuda.stream(stream):
+        step(cache(), torch.zeros_like(out))  # before the capture: everything loaded
+    stream.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(caches[0], out)
+    for r in range(6):
+        parent.copy_(ints(rng.integers(0, 6, size=6) if r else [0] * 6))
+        lens = caches[1].lens[parent.long()]
+        want.copy_(lens + ints(rng.integers(0, 3, size=6)))
+        for y in (k, v, q):
+            y.normal_()
+        graph.replay()
+        other = torch.zeros_like(out)
+        step(caches[1], other)
+        torch.cuda.synchronize()
+        m = int((caches[1].lens - lens).sum())
+        assert torch.equal(out[:, :m], other[:, :m]) and m > 0
+        assert torch.equal(caches[0].refs, caches[1].refs) and torch.equal(caches[0].lens, caches[1].lens)
+        held = caches[0].refs > 0
+        assert torch.equal(caches[0].values[:, held], caches[1].values[:, held])
+
+
+def test_two_graphs_and_another_stream():
+    """Two captured attentions on one plan, replayed at once on two streams, and calls on a stream of their own."""
+    rng = np.random.default_rng(12)
+    pool = Pool(rng, forest_of(rng, "samples", 24, 900, 300), 32, heads=4)
+    q = [torch.randn((1, 24, 16, 128), device=DEV).bfloat16() for _ in range(2)]
+    plan = plan_of(pool, range(25), 24, 4, "bf16")
+    ref = [torch.zeros_like(x) for x in q]
+    for x, o in zip(q, ref):
+        B.iwdft_pages_attn_shared(pool.values, pool.exponents, x, plan, pool.d_table, o)
+    out, graphs, streams = [torch.zeros_like(x) for x in q], [], [torch.cuda.Stream() for _ in q]
+    torch.cuda.synchronize()
+    for x, o in zip(q, out):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            for _ in range(4):
+                B.iwdft_pages_attn_shared(pool.values, pool.exponents, x, plan, pool.d_table, o)
+        graphs.append(g)
+    for _ in range(5):
+        for o in out:
+            o.zero_()
+        torch.cuda.synchronize()
+        for g, s in zip(graphs, streams):
+            with torch.cuda.stream(s):
+                g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(out, ref))
+    side = torch.cuda.Stream()
+    o = torch.zeros_like(ref[0])
+    side.wait_stream(torch.cuda.current_stream())
+    starts = ints(range(25))
+    torch.cuda.synchronize()
+    p = B.iwdft_pages_plan(starts, pool.d_table, pool.d_lens, 24, pool.n_pages, 4, 16, 32, torch.bfloat16, stream=side)
+    B.iwdft_pages_attn_shared(pool.values, pool.exponents, q[0], p, pool.d_table, o, stream=side.cuda_stream)
+    side.synchronize()
+    assert torch.equal(o, ref[0])
+
+
+def test_calls_without_rows_or_sequences():
+    """No new tokens, no sequences, sequences that bring nothing: nothing is written where nothing is to be."""
+    rng = np.random.default_rng(13)
+    pool = Pool(rng, forest_of(rng, "samples", 3, 60, 10), 16)
+    none = torch.empty((1, 0, 4, 128), device=DEV)
+    B.iwdft_pages_attn_shared(pool.values, pool.exponents, none, plan_of(pool, [0] * 4, 0, 2, "f32"), pool.d_table, torch.empty_like(none))
+    q = torch.randn((1, 5, 4, 128), device=DEV)
+    out = torch.full_like(q, 7.0)
+    B.iwdft_pages_attn_shared(pool.values, pool.exponents, q, plan_of(pool, [0] * 4, 5, 2, "f32"), pool.d_table, out)
+    assert (out == 7.0).all()
+    B.iwdft_pages_attn_shared(pool.values, pool.exponents, q, plan_of(pool, [2, 2, 4, 4], 5, 2, "f32"), pool.d_table, out)
+    assert (out[:, [0, 1, 4]] == 7.0).all() and not (out[:, 2:4] == 7.0).any()
+    table, lens = torch.empty((0, 4), dtype=torch.int32, device=DEV), torch.empty(0, dtype=torch.int32, device=DEV)
+    plan = B.iwdft_pages_plan(ints([0]), table, lens, 5, pool.n_pages, 2, 4, 16, torch.float32)
+    out.fill_(7.0)
+    B.iwdft_pages_attn_shared(pool.values, pool.exponents, q, plan, table, out)
+    assert (out == 7.0).all()
+    zero = Pool(rng, [(-1, 0, 40), (0, 0, 0), (0, 40, 40)], 16)
+    attend(zero, rng, [1, 2, 3], 2, "f32")                      # a sequence without tokens whose rows see nothing
+    B.iwdft_pages_copy(torch.empty((0, 2), dtype=torch.int32, device=DEV), pool.values, pool.exponents)
+    with pytest.raises(ValueError, match="shared"):
+        B.PagedCache(1, 4, 1, 1, 128, torch.float32, 2, 64, 16, DEV).fork(ints([0, 0]))
+    with pytest.raises(B.IwdftError):
+        B.PagedCache(1, 4, 1, 1, 128, torch.float32, 1025, 64, 16, DEV, shared=True)
