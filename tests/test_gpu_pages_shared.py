@@ -602,3 +602,20 @@ def test_calls_without_rows_or_sequences():
         B.PagedCache(1, 4, 1, 1, 128, torch.float32, 2, 64, 16, DEV).fork(ints([0, 0]))
     with pytest.raises(B.IwdftError):
         B.PagedCache(1, 4, 1, 1, 128, torch.float32, 1025, 64, 16, DEV, shared=True)
+
+
+def test_copy_of_more_than_the_caches_hold():
+    """Over 256 MB of pages go another way."""
+    g = torch.Generator(device=DEV).manual_seed(1)
+    values = torch.randint(0, 256, (2, 300, 9, 2, 128 * 128), dtype=torch.uint8, device=DEV, generator=g)
+    exponents = torch.randint(-100, 100, (2, 300, 9, 2), dtype=torch.int32, device=DEV, generator=g)
+    other = torch.zeros((2, 520, 9, 2, 128 * 128), dtype=torch.uint8, device=DEV), torch.zeros((2, 520, 9, 2), dtype=torch.int32, device=DEV)
+    to = torch.randperm(520, device=DEV, generator=g)[:500].to(torch.int32)
+    source = torch.randint(-1, 300, (500,), dtype=torch.int32, device=DEV, generator=g)
+    B.iwdft_pages_copy(torch.stack([source, to], 1).contiguous(), values, exponents, *other)
+    there = source >= 0
+    assert 1 < int(there.sum()) < 500 and torch.equal(other[0][:, to[there].long()], values[:, source[there].long()])
+    assert torch.equal(other[1][:, to[there].long()], exponents[:, source[there].long()])
+    rest = torch.ones(520, dtype=torch.bool, device=DEV)
+    rest[to[there].long()] = False
+    assert not other[0][:, rest].any() and not other[1][:, rest].any()
