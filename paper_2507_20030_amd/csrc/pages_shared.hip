@@ -216,7 +216,8 @@ __device__ __forceinline__ int tokens_seen(const PlanArgs& a, int t0, int t1, in
 template <int THREADS>
 __global__ __launch_bounds__(THREADS) void plan_share_kernel(PlanArgs a) {
   constexpr int kEvents = THREADS == kShareThreads ? kMostEvents : 3 * kWave;
-  __shared__ int32_t leader[kEvents], from[kEvents], news[kEvents], tiles[kEvents], base[THREADS];
+  __shared__ __attribute__((aligned(16))) int32_t leader[kEvents], from[kEvents];
+  __shared__ int32_t news[kEvents], tiles[kEvents], base[THREADS];
   __shared__ long long lds2[THREADS / kWave][2], lds4[THREADS / kWave][4];
   __shared__ float lds_f[THREADS / kWave][4];
   const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
@@ -258,10 +259,17 @@ __global__ __launch_bounds__(THREADS) void plan_share_kernel(PlanArgs a) {
       for (int i = tid; i < n; i += THREADS) leader[i] = i, from[i] = 0, news[i] = news_of(a, i).n;
       __syncthreads();
     }
-    const auto end_of = [&](int i) {
-      for (int k = i + 1; k < n && !unshared; ++k)
-        if (leader[k] == leader[i]) return from[k];
-      return pages_of_news(a, news_of(a, leader[i]));
+    const auto end_of = [&](int i) {  // where its leader's next event is, or its row ends
+      const int mine = leader[i];
+      int end = pages_of_news(a, news_of(a, mine));
+      if (unshared) return end;
+#pragma unroll 4
+      for (int k = i / 4 * 4; k < n; k += 4) {
+        const int4 l = *(const int4*)(leader + k), f = *(const int4*)(from + k);
+        const auto next = [&](int c, int lead, int at) { end = k + c > i && k + c < n && lead == mine ? min(end, at) : end; };
+        next(0, l.x, f.x), next(1, l.y, f.y), next(2, l.z, f.z), next(3, l.w, f.w);
+      }
+      return end;
     };
     const auto rows_of = [&](int i) { return max(news[i], 0) * a.S.G; };
     const auto is_many = [&](int rows) { return rows > kSharedFew; };
@@ -369,7 +377,8 @@ __global__ __launch_bounds__(256) void plan_rows_kernel(PlanArgs a) {
       }
       for (unsigned long long rest = in; rest && !each_run && !unshared; rest &= rest - 1) {
         const int l = __builtin_ctzll(rest);
-        const Run r = a.p.runs[i0 + l];
+        Run r{};
+        r.leader = __builtin_amdgcn_readlane(mine.leader, l), r.from = __builtin_amdgcn_readlane(mine.from, l);
         int sum = 0;
         for (int y = lane; y < x; y += kWave) {
           const News o = news_of(a, y);
