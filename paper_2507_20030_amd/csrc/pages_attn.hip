@@ -120,6 +120,7 @@ class Schedule {
 template <class Geo>
 class Sequences {
  public:
+  static constexpr bool looks_up = false;
   __device__ __forceinline__ Sequences(const PagesAttn& a, const PagesRows& which, int lane) : a(a), which(which), plan(a, which, lane) {}
   __device__ __forceinline__ float* part() const { return which.part; }
   __device__ __forceinline__ float2* stat() const { return which.stat; }

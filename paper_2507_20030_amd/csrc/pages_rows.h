@@ -179,6 +179,7 @@ __device__ __forceinline__ Span span_of(const PagesAttn& a, int base, int from, 
 //   block(x)             the x-th of them, a struct with: layer (of the call), h; rows; table, last_page: the row of the table that its tokens are in and the last page
 //                        to be read there; base: the token at which its tiles begin; p_lo, p_hi: least and largest position of its rows; from_lo, from_hi: least and
 //                        largest left border of their windows; part of np; whole: its results go to out
+//   looks_up             whether row() reads memory
 //   row(block, r)        where row r of the block is and what it sees; any r, but what r >= rows gives is not used
 //   wave_rows(block, w)  what rows 32 w .. 32 w + 31 see: p_hi: their largest position, -1 without rows; from: their least left border
 //   slot(block)          the first row of its sums in part(), stat()
@@ -223,6 +224,17 @@ __device__ __forceinline__ void few_rows(const PagesAttn& a, const Work& work, u
     const Share mine = share_of(span.n, at.part, at.np);
     const int n_rt = (rows + 15) / 16;
     const int sink = a.n_recent ? a.n_sink : 0, all_from = at.from_lo;
+
+    // Where the rows are: looked up before the tokens, since loads come back in order.
+    RowAt places[R];
+    const auto look_up = [&](int r) {
+      places[r] = RowAt{0, -1, -1};
+      if (16 * r + row < rows) places[r] = work.row(at, 16 * r + row);
+    };
+    if constexpr (Work::looks_up) {
+#pragma unroll
+      for (int r = 0; r < R; ++r) look_up(r);
+    }
 
     // pages of a lane's octets: that of its K row and that of its tokens in V and in the scores
     const int32_t* table = at.table;
@@ -270,16 +282,15 @@ __device__ __forceinline__ void few_rows(const PagesAttn& a, const Work& work, u
     for (int r = 0; r < R; ++r) {
       Rows<PARTS>& z = rt[r];
       const bool have = 16 * r + row < rows;
-      RowAt mine_at{0, -1, -1};
-      if (have) mine_at = work.row(at, 16 * r + row);
-      z.pos = mine_at.pos, z.from = mine_at.from;
+      if constexpr (!Work::looks_up) look_up(r);
+      z.pos = places[r].pos, z.from = places[r].from;
       z.m = -FLT_MAX, z.l = 0.f;
 #pragma unroll
       for (int i = 0; i < 8; ++i) z.o[i] = floatx4{0.f, 0.f, 0.f, 0.f};
       float f[2][16];
       float top = 0.f;
       if (have) {
-        const int64_t base = mine_at.at * kHeadDim;
+        const int64_t base = places[r].at * kHeadDim;
 #pragma unroll
         for (int p = 0; p < 2; ++p) load_channels<BF16>(a.q, base + 64 * p + 16 * oct, f[p]);
       } else {

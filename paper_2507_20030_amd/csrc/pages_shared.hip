@@ -20,8 +20,12 @@ namespace {
 constexpr int kPlaces = 4;         // of a wave in the first launch
 constexpr int kShareThreads = 1024;
 constexpr int kMostEvents = 3 * kSharedBatch;  // where a set begins or ends; sequences that fork have fewer than 3 each
-constexpr int kSharedParts = 512;  // of a call: two workgroups on each CU
-constexpr int kSharedFew = 64;      // runs of up to so many rows go to few_rows
+// Parts of a call: two workgroups on each CU, as iwdft_pages_attn has them; a second one from parts of 8 tiles (few rows 16) on.  64 requests of 480 rows over 32768 tokens:
+// many_rows with 256 parts 145 us, 512 130, 1024 141.
+constexpr int kSharedParts = 512;
+// Runs of up to so many rows go to few_rows, in blocks of 32 (fp32 16), the others to many_rows.  us, plan included, with up to 64 / up to 128 there (bf16, 8 heads): 60 rows over 65536
+// tokens 71.5 / 72.6 (with up to 32 75.2; fp32 100 / 99, 132); 92 rows over 65536 78 / 97; 120 over 8192 48.6 / 45.1, over 32768 63.0 / 70.2, over 131072 128 / 184.
+constexpr int kSharedFew = 64;
 constexpr int kPlanMark = 0x49574446;
 
 struct PlanHead {
@@ -107,7 +111,8 @@ __device__ __forceinline__ void in_wave() {  // LDS that the lanes of a wave exc
   __builtin_amdgcn_wave_barrier();
 }
 
-// A wave has kPlaces places, and looks at the one before them; its lanes have the sequences in turn.  Equal pages meet in a hash table in LDS.
+// A wave has kPlaces places, and looks at the one before them; its lanes have the sequences in turn.  Equal pages meet in a hash table in LDS: one look-up for each
+// sequence, whoever shares with whom.  A chain of loads and five rounds through LDS: 16 sequences of 272 pages 4.6 us, 64 of 528 6.2, 256 of 144 13.
 template <int EACH, int WAVES>
 __global__ __launch_bounds__(WAVES* kWave) void plan_sets_kernel(PlanArgs a) {
   constexpr int kRows = EACH * kWave, kSlots = 2 * kRows;
@@ -212,7 +217,8 @@ __device__ __forceinline__ int tokens_seen(const PlanArgs& a, int t0, int t1, in
 }
 
 // One workgroup: the runs from the events, which lie in the order of their places.  THREADS: 256 for up to 64 sequences, whose events one thread each can have
-// as a rule: sums over 16 waves take longer.
+// as a rule: with 1024 the sums over 16 waves of 16 sequences' plan took 16.6 us, so 7; 64 sequences 8, 256 19.  (All three launches in one, for tables of 128 pages:
+// 29 us with the attention, 25 so; each launch's loads would wait for the one workgroup's own.)
 template <int THREADS>
 __global__ __launch_bounds__(THREADS) void plan_share_kernel(PlanArgs a) {
   constexpr int kEvents = THREADS == kShareThreads ? kMostEvents : 3 * kWave;
@@ -347,7 +353,7 @@ __global__ __launch_bounds__(THREADS) void plan_share_kernel(PlanArgs a) {
   }
 }
 
-// A wave for each sequence: its runs, in order, and its rows in them.  A wave for each run: its items.
+// A wave for each sequence: its runs, in order, and its rows in them.  A wave for each run: its items.  16 sequences 4.5 us, 12 with forty runs 7, 256 9.6.
 __global__ __launch_bounds__(256) void plan_rows_kernel(PlanArgs a) {
   const int lane = threadIdx.x % kWave, unit = blockIdx.x * 4 + threadIdx.x / kWave;
   const PlanHead& head = *a.p.head;
@@ -433,9 +439,12 @@ __device__ __forceinline__ bool is_for(const PlanHead& h, const SharedAttn& s) {
          h.n_tokens == a.n_tokens && h.n_sink == a.n_sink && h.n_recent == a.n_recent && h.few_rows == s.few_rows;
 }
 
-// The items of one kind: see pages_rows.h for what the kernels ask.
+// The items of one kind: see pages_rows.h for what the kernels ask.  A short part is a chain: plan, item, rows (0.5 us), table and first tokens (0.9), queries (2), four tiles for each
+// wave (5.5, vector work as much as waiting: a second tile ahead is slower), sums through LDS (1.5 to 2).  Long parts of many rows run at what the products and conversions of
+// many_rows reach: two workgroups of 128 rows on a CU 1.28 us a tile of 64 tokens each, 840 TFLOP/s.  (The kinds taking turns on the CUs, a workgroup of each, gains nothing: 130 us for 127.)
 class Items {
  public:
+  static constexpr bool looks_up = true;
   __device__ __forceinline__ float* part() const { return s.part; }
   __device__ __forceinline__ float2* stat() const { return s.stat; }
 
@@ -500,7 +509,9 @@ __global__ __launch_bounds__(kWaves* kWave, BF16 ? 2 : (R == 1 && !MANY ? 2 : 1)
 }
 
 // A row's parts: its runs' first rows of sums and numbers of parts, a lane for each, become a list of all parts; a lane for each reads its reference, then all
-// sums are on their way at once.  Few rows: a workgroup for each, its waves share the parts.  Many: a wave for each.
+// sums are on their way at once.  Bound by four loads that wait for each other (run by run and part by part, each rescaling the last: 15.5 us for beams with twenty runs, so 10.3).
+// Few rows: a workgroup for each, its waves share the parts.  Many: a wave for each (3840 rows of 17 parts, 34 MB: 14.9 and 11.4 us; 2048 rows 7.2 and 7.9; 736 rows of beams
+// 10.3 and 20).
 constexpr int64_t kManyShared = 2048;
 template <bool BF16>
 __global__ __launch_bounds__(kWaves* kWave) void shared_join_kernel(SharedAttn s, int64_t all, int many) {
@@ -514,6 +525,8 @@ __global__ __launch_bounds__(kWaves* kWave) void shared_join_kernel(SharedAttn s
     const int2 owner = s.p.owner[token];
     const int b = __builtin_amdgcn_readfirstlane(owner.x), mine = __builtin_amdgcn_readfirstlane(owner.y) * G + r - token * G;
     if (b < 0) continue;  // behind the last sequence
+    const int4* chain = s.p.chain + (int64_t)b * s.z.chain;
+    const int4 first = chain[min(lane, s.z.chain - 1)];  // with their number on its way
     const int n = __builtin_amdgcn_readfirstlane(s.p.chained[b]);
     const int64_t slot0 = (int64_t)lh * slots + mine;
     float m = -FLT_MAX, l = 0.f;
@@ -523,7 +536,9 @@ __global__ __launch_bounds__(kWaves* kWave) void shared_join_kernel(SharedAttn s
       o.x = o.x * (f * f) + v.x * (half * half), o.y = o.y * (f * f) + v.y * (half * half), l = l * f * f + sum * half * half, m = up;
     };
     for (int i0 = 0; i0 < n; i0 += kWave) {
-      const int4 run = i0 + lane < n ? s.p.chain[(int64_t)b * s.z.chain + i0 + lane] : make_int4(0, 0, 0, 0);
+      int4 run = first;
+      if (i0) run = chain[min(i0 + lane, n - 1)];
+      if (i0 + lane >= n) run = make_int4(0, 0, 0, 0);
       const int to = scan(run.y), parts = last_lane(to), size = many ? kWave : min(kWave, (parts + kWaves - 1) / kWaves);
       for (int p0 = many ? 0 : wave * size; p0 < parts; p0 += size * (many ? 1 : kWaves)) {
         const int part = p0 + lane, here = min(parts - p0, size);
