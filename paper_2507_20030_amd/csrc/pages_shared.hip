@@ -47,7 +47,7 @@ struct PlanSizes {
   int places, chunks, events, chain;
   int64_t mem, items, slots;
 };
-// n: of rows of sums of all (layer, head)
+// Rows of sums of all (layer, head) that a call has room for.
 int64_t most_slots(const Pages& S, int n_layers, int n_tokens) {
   const int64_t rows = (int64_t)n_tokens * S.G;
   return (2 * kSharedParts + 64) * std::min<int64_t>(128, (rows + 15) / 16 * 16) + 4 * rows * n_layers * S.H;
@@ -226,17 +226,32 @@ __global__ __launch_bounds__(THREADS) void plan_share_kernel(PlanArgs a) {
   __shared__ int32_t news[kEvents], tiles[kEvents], base[THREADS];
   __shared__ long long lds2[THREADS / kWave][2], lds4[THREADS / kWave][4];
   __shared__ float lds_f[THREADS / kWave][4];
+  __shared__ int32_t longest[THREADS / kWave];
   const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
   const float slices = (float)(a.n_layers * a.S.H);
-  int n = 0;
+  int n = 0, chunks = a.z.chunks;
   bool unshared = false;
-  for (int c0 = 0; c0 < a.z.chunks; c0 += THREADS) {
-    const int c = c0 + tid, mine = c < a.z.chunks ? a.p.counts[c] : 0;
+  for (int c0 = 0; c0 < chunks; c0 += THREADS) {
+    const int c = c0 + tid, mine = c < chunks ? a.p.counts[c] : 0;
     int x[2] = {mine, 0};
-    if (c0 == 0)
-      for (int b = tid; b < a.batch; b += THREADS) x[1] += news_of(a, b).n;
+    if (c0 == 0) {
+      int most = 0;
+      for (int b = tid; b < a.batch; b += THREADS) {
+        const News s = news_of(a, b);
+        x[1] += s.n, most = max(most, pages_of_news(a, s));
+      }
+#pragma unroll
+      for (int d = 1; d < kWave; d <<= 1) most = max(most, __shfl_xor(most, d));
+      if (lane == 0) longest[wave] = most;
+    }
     long long before[2], all[2];
     sums_before<THREADS>(x, before, all, lds2);
+    if (c0 == 0) {  // of a wide table only what sequences have
+      int most = 0;
+#pragma unroll
+      for (int w = 0; w < THREADS / kWave; ++w) most = max(most, longest[w]);
+      chunks = min(chunks, (most + kPlaces - 1) / kPlaces);
+    }
     if (c0 == 0 && all[1] > a.n_tokens) {  // starts that overlap: rows would belong to several sequences, nothing is done
       if (tid == 0) *a.p.head = PlanHead{};
       return;

@@ -92,6 +92,29 @@ def test_tables(batch, W, P, n_pages, n_slots, most):
     assert n_pages < 100 or moved > 0  # small pools are full
 
 
+def test_many_pages_at_once():
+    """More pages given up than one turn of the workgroup takes, by holders alone and together; more slots than fit the first launch; a wide table that is hardly used."""
+    rng = np.random.default_rng(8)
+    t = Both(5, 9000, 30000, 16, rng)
+    t.resize([140_000, 30, 0, 90_000, 0], 300_000)
+    t.fork([0, 1, 0, 3, 3], [-1, -1, 139_000, -1, 50_001])
+    t.resize([139_990, 31, 139_001, 90_001, 50_002], 100)
+    t.resize([100, 31, 0, 80_000, 20], 100)                      # 16 thousand entries at a time, most of them held twice
+    t.fork([0, 3, 2, 4, 4])
+    t.resize([0, 0, 0, 0, 0], 0)
+    assert t.o.free[0] == 30000
+
+
+def test_a_pool_of_more_pages_than_bits_in_lds():
+    rng = np.random.default_rng(9)
+    t = Both(3, 3000, 140_001, 16, rng)
+    t.resize([40_000, 100, 20_000], 70_000)
+    t.fork([0, 0, 2], [-1, 30_000, -1])
+    assert (t.compact(70)[:, 0] >= 0).all()                     # some of what would have to move
+    t.resize([41_000, -1, 0], 2_000)
+    t.compact(20)
+
+
 def test_all_samples_of_a_prompt_leave_its_last_page_but_one():
     t = Both(6, 8, 30, 16, np.random.default_rng(0))
     t.resize([40, 0, 0, 0, 0, 0], 40)
@@ -330,6 +353,44 @@ def test_attention_does_not_see_what_is_masked(dtype):
         assert nan[0, 0, G:, 40].all() and int(nan.sum()) == G
         out = attend(pool, rng, [1] * batch, G, dtype)
         assert int(torch.isnan(out.float()).sum()) == G * batch
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_attention_queries_that_are_not_finite_stay_in_their_row(dtype):
+    rng = np.random.default_rng(10)
+    for batch in (3, 20):
+        pool = Pool(rng, forest_of(rng, "samples", batch, 200, 30), 32)
+        q = torch.randn((1, batch, 8, 128), device=DEV).to(DT[dtype])
+        q[0, 1, 2, 5], q[0, 1, 3, 7] = float("nan"), float("inf")
+        starts = ints(range(batch + 1))
+        out, plain = torch.zeros_like(q), torch.zeros_like(q)
+        B.iwdft_pages_attn_shared(pool.values, pool.exponents, q, plan_of(pool, range(batch + 1), batch, 4, dtype), pool.d_table, out)
+        B.iwdft_pages_attn(pool.values, pool.exponents, q, starts, pool.d_table, pool.d_lens, plain)
+        bad = torch.isnan(out.float()).any(-1)
+        assert torch.equal(bad, torch.isnan(plain.float()).any(-1)) and not bad[0, 0].any() and not bad[0, 2:].any() and bad[0, 1, 2]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_attention_of_pages_far_apart(dtype):
+    """Pages of V whose scales are up to 2^120 apart, within runs and between them; K's scales apart as far as scores stay small."""
+    rng = np.random.default_rng(14)
+    for batch, G in ((3, 4), (24, 4)):
+        pool = Pool(rng, forest_of(rng, "nested", batch, 150, 60), 16)
+        e = pool.store.exponents
+        e[..., 0] -= rng.integers(2, 12, size=e.shape[:3]).astype(np.int32)
+        e[..., 1] += rng.integers(-60, 60, size=e.shape[:3]).astype(np.int32)
+        pool.upload()
+        attend(pool, rng, [1] * batch, G, dtype)
+
+
+def test_attention_of_short_sequences_in_a_wide_table():
+    rng = np.random.default_rng(15)
+    pool = Pool(rng, forest_of(rng, "samples", 5, 50, 20), 16)
+    wide = np.full((5, 70_000), -1, np.int32)
+    wide[:, :pool.table.shape[1]] = pool.table
+    pool.table = wide
+    pool.upload()
+    attend(pool, rng, [1] * 5, 2, "f32")
 
 
 def test_attention_one_sequence_for_each_row_of_a_large_table():
@@ -614,7 +675,7 @@ def test_copy_of_more_than_the_caches_hold():
     source = torch.randint(-1, 300, (500,), dtype=torch.int32, device=DEV, generator=g)
     B.iwdft_pages_copy(torch.stack([source, to], 1).contiguous(), values, exponents, *other)
     there = source >= 0
-    assert 1 < int(there.sum()) < 500 and torch.equal(other[0][:, to[there].long()], values[:, source[there].long()])
+    assert int(there.sum()) > 400 and torch.equal(other[0][:, to[there].long()], values[:, source[there].long()])
     assert torch.equal(other[1][:, to[there].long()], exponents[:, source[there].long()])
     rest = torch.ones(520, dtype=torch.bool, device=DEV)
     rest[to[there].long()] = False
