@@ -1,9 +1,9 @@
 // Pages that several sequences hold: sequences that take over others' beginnings, lengths of a step with copies on write, pages moved together, pages copied.
 //
 // refs[p] counts the sequences that hold page p, each at the same place of its row (what shares a page shares all pages before it).  A page goes back on the
-// stack when its last holder gives it up.  Several threads give up the same page at once, so the order on the stack is settled in three steps: all count down; of a page
-// that has come to 0 the givers leave the smallest of their places in refs, as a negative number; who finds its own there pushes the page.
-// Sums over the threads place the pushes: nothing depends on the order in which atomics arrive.
+// stack when its last holder gives it up.  Several give up the same page at once: they meet, in a hash table in LDS or, in small tables, in refs itself, and the
+// last of them in the order that the call defines takes all off the count.  Sums over the threads place what goes on the stack: nothing depends on the order
+// in which atomics arrive.
 #include <algorithm>
 
 #include "pages.h"
@@ -14,10 +14,9 @@ namespace {
 
 constexpr int kWave = kLanes;
 
-// refs are changed by atomics of one workgroup (a page is held at one place, which one workgroup looks after), in its L2: read past the L1.
+// Atomics on refs are those of one workgroup (a page is held at one place, which one workgroup looks after), in its L2: read past the L1.
 __device__ __forceinline__ int32_t refs_now(const int32_t* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP); }
 __device__ __forceinline__ void refs_add(int32_t* p, int x) { __hip_atomic_fetch_add(p, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP); }
-__device__ __forceinline__ int32_t refs_less(int32_t* p) { return __hip_atomic_fetch_add(p, -1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP); }  // what it was
 __device__ __forceinline__ void refs_least(int32_t* p, int x) { __hip_atomic_fetch_min(p, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP); }
 __device__ __forceinline__ void refs_set(int32_t* p, int x) { __hip_atomic_store(p, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP); }
 __device__ __forceinline__ void all_here() {  // what the workgroup has written, in memory too, is there for all of it; its atomics have arrived
@@ -47,15 +46,20 @@ __device__ __forceinline__ int sum_before(int x, int* all, long long (*lds)[1]) 
 }
 
 // ------------------------------------------------------------------------------------------------ lengths of a step
-// One workgroup, a thread for each sequence: a chain of loads, sums and stores, 5.2 us for 16 samples that leave their shared page.  Pages that are given up cost that workgroup's random
-// accesses: 7840 of 256 sequences, most of them shared, 24 of 44 us (table 4, counts 3, atomics that return 13, whose last holder goes 4).  A sequence whose last page has room, and which others hold, leaves that page before it grows: it gets a new one and
+// One workgroup, a thread for each sequence: a chain of loads, sums and stores, 5.0 us for 16 samples that leave their shared page.  7840 pages given up by 256 sequences,
+// most of them shared, and 806 taken: 31 us, with atomics on refs in place of the hash table 44, in three passes over the entries 106.
+// A sequence whose last page has room, and which others hold, leaves that page before it grows: it gets a new one and
 // an entry in copies.  Where all holders leave in this call, the last of them stays.  It is held to the pages that are left as those before it
 // are: had one of them been refused, the page would still be shared.
 constexpr int kSmallTable = 8192;  // of a small table: in LDS, one launch
-constexpr int kGiven = 16;  // entries of a thread that are on their way at a time
+constexpr int kGiven = 4;  // entries of a thread that are given up at a time
 template <int THREADS>
 __global__ __launch_bounds__(THREADS) void pages_grow_kernel(GrowArgs a) {
+  constexpr int kGivenSlots = 2 * kGiven * THREADS;
   __shared__ long long lds1[THREADS / kWave][1], lds2[THREADS / kWave][2];
+  __shared__ struct {
+    int32_t page[kGivenSlots], last[kGivenSlots], count[kGivenSlots];
+  } given;
   __shared__ int32_t base[THREADS], first[THREADS], back[THREADS];
   __shared__ __attribute__((aligned(16))) int32_t open[THREADS];
   const SharedTables& t = a.t;
@@ -87,53 +91,50 @@ __global__ __launch_bounds__(THREADS) void pages_grow_kernel(GrowArgs a) {
     const int at = sum_before<THREADS>(had > get ? 1 : 0, &givers, lds1);
     if (had > get) base[at] = gone_before, first[at] = get, back[at] = b;
     __syncthreads();
-    int page[kGiven], holders[kGiven];
-    const int per = min((gone + THREADS - 1) / THREADS, kGiven);  // of a thread, side by side
-    const auto mark = [&](int e0, int i) { return -1 - e0 - per * b - i; };  // the later an entry is given back the smaller
-    for (int e0 = 0; e0 < gone; e0 += per * THREADS) {  // batch by batch: a page that two batches give up goes with the second
-      int o = gone - 1 - e0 - per * b, s = o >= 0 ? last_not_above(base, givers, o) : 0;
+    // Batch by batch: a page that two batches give up goes with the second.  Givers of a page meet in a hash table; the last of them in this order counts all off.
+    for (int e0 = 0; e0 < gone; e0 += kGiven * THREADS) {
+      for (int i = b; i < kGivenSlots; i += THREADS) given.page[i] = -1, given.last[i] = -1, given.count[i] = 0;
+      __syncthreads();
+      int page[kGiven], slot[kGiven], left[kGiven];
+      int o = gone - 1 - e0 - kGiven * b, s = o >= 0 ? last_not_above(base, givers, o) : 0;
 #pragma unroll
       for (int i = 0; i < kGiven; ++i, --o) {
-        page[i] = -1;
-        if (i >= per || o < 0) continue;
-        if (o < base[s]) --s;
-        const int p = t.table[(int64_t)back[s] * t.max_pages + min(first[s] + o - base[s], t.max_pages - 1)];
+        if (o >= 0 && o < base[s]) --s;
+        const int p = o >= 0 ? t.table[(int64_t)back[s] * t.max_pages + min(first[s] + o - base[s], t.max_pages - 1)] : -1;
         page[i] = is_page(t, p) ? p : -1;
       }
 #pragma unroll
-      for (int i = 0; i < kGiven; ++i) holders[i] = page[i] >= 0 ? refs_now(t.refs + page[i]) : -1;
-      all_here();
-      // who holds a page alone gives it back; of several, one sees the count come to nothing, then the last in this order does
-      bool open = false;
-#pragma unroll
-      for (int i = 0; i < kGiven; ++i)
-        if (holders[i] > 1) {
-          holders[i] = refs_less(t.refs + page[i]) > 1 ? 2 : 3;
-          open |= holders[i] == 3;
+      for (int i = 0; i < kGiven; ++i) {
+        slot[i] = -1;
+        if (page[i] < 0) continue;
+        uint32_t at = ((uint32_t)page[i] * 2654435769u) >> 8;
+        for (;; ++at) {  // there are twice as many slots as entries
+          at &= kGivenSlots - 1;
+          const int was = atomicCAS(&given.page[at], -1, page[i]);
+          if (was == -1 || was == page[i]) break;
         }
-      if (__syncthreads_or(open)) {
-#pragma unroll
-        for (int i = 0; i < kGiven; ++i)
-          if (holders[i] >= 2) holders[i] = refs_now(t.refs + page[i]) <= 0 ? 3 : 2;
-        all_here();
-#pragma unroll
-        for (int i = 0; i < kGiven; ++i)
-          if (holders[i] == 3) refs_least(t.refs + page[i], mark(e0, i));
-        all_here();
-#pragma unroll
-        for (int i = 0; i < kGiven; ++i)
-          if (holders[i] == 3) holders[i] = refs_now(t.refs + page[i]) == mark(e0, i);
+        slot[i] = (int)at;
+        atomicMax(&given.last[at], kGiven * b + i), atomicAdd(&given.count[at], 1);
       }
-      int n, goes = 0;  // holders 1: it goes
+      __syncthreads();
+      int n, goes = 0;
 #pragma unroll
-      for (int i = 0; i < kGiven; ++i) goes += holders[i] == 1;
+      for (int i = 0; i < kGiven; ++i) {
+        left[i] = 1;
+        if (slot[i] >= 0 && given.last[slot[i]] == kGiven * b + i) left[i] = t.refs[page[i]] - given.count[slot[i]];
+        else slot[i] = -1;
+      }
+#pragma unroll
+      for (int i = 0; i < kGiven; ++i) {
+        if (slot[i] >= 0) t.refs[page[i]] = max(left[i], 0);
+        goes += left[i] <= 0;
+      }
       int to = count + released + sum_before<THREADS>(goes, &n, lds1);
 #pragma unroll
       for (int i = 0; i < kGiven; ++i)
-        if (holders[i] == 1) {
+        if (left[i] <= 0) {
           if (to < t.n_pages) t.free[1 + to] = page[i];
           ++to;
-          refs_set(t.refs + page[i], 0);
         }
       released += n;
       all_here();
@@ -142,7 +143,7 @@ __global__ __launch_bounds__(THREADS) void pages_grow_kernel(GrowArgs a) {
   }
 
   // who has to leave a shared page
-  const int holders = last >= 0 ? refs_now(t.refs + last) : 0;
+  const int holders = last >= 0 ? t.refs[last] : 0;
   const bool shared = holders > 1;
   bool leave = shared;
   open[b] = shared ? last : -1;
