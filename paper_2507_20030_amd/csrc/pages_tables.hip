@@ -46,25 +46,34 @@ __device__ __forceinline__ int sum_before(int x, int* all, long long (*lds)[1]) 
 }
 
 // ------------------------------------------------------------------------------------------------ lengths of a step
-// One workgroup, a thread for each sequence: a chain of loads, sums and stores, 5.0 us for 16 samples that leave their shared page.  7840 pages given up by 256 sequences,
-// most of them shared, and 806 taken: 31 us, with atomics on refs in place of the hash table 44, in three passes over the entries 106.
+constexpr int kSmallTable = 8192;  // entries of a small table
+constexpr int kGiven = 4;          // entries of a thread that are given up at a time
+// One workgroup, a thread for each sequence: a chain of loads, sums and stores, 5.0 us for 16 samples that leave their shared page.  What large tables give up takes more threads
+// than they have sequences, which only wait while the others sum: 256 sequences that bring a token each 12.9 us with 256 threads, 18.4 with 1024 that all sum, 14.9 so (with the
+// slots' launch); 7840 pages given up, most of them shared, and 806 taken 51.7, 37.0, 32.0.  With atomics on refs in place of the hash table 49, in three passes over the entries 111.
 // A sequence whose last page has room, and which others hold, leaves that page before it grows: it gets a new one and
 // an entry in copies.  Where all holders leave in this call, the last of them stays.  It is held to the pages that are left as those before it
 // are: had one of them been refused, the page would still be shared.
-constexpr int kSmallTable = 8192;  // of a small table: in LDS, one launch
-constexpr int kGiven = 4;  // entries of a thread that are given up at a time
-template <int THREADS>
+template <int THREADS, int ROWS>
 __global__ __launch_bounds__(THREADS) void pages_grow_kernel(GrowArgs a) {
   constexpr int kGivenSlots = 2 * kGiven * THREADS;
-  __shared__ long long lds1[THREADS / kWave][1], lds2[THREADS / kWave][2];
+  __shared__ long long lds1[THREADS / kWave][1], lds2[ROWS / kWave][2], totals[2];
   __shared__ struct {
     int32_t page[kGivenSlots], last[kGivenSlots], count[kGivenSlots];
   } given;
-  __shared__ int32_t base[THREADS], first[THREADS], back[THREADS];
-  __shared__ __attribute__((aligned(16))) int32_t open[THREADS];
+  __shared__ int32_t base[ROWS], first[ROWS], back[ROWS];
+  __shared__ __attribute__((aligned(16))) int32_t open[ROWS];
   const SharedTables& t = a.t;
   const int b = threadIdx.x, P = 1 << t.logP, most = t.max_pages << t.logP;
   const bool mine = b < t.batch;
+  const auto sums_of_rows = [&](const int(&x)[2], long long(&before)[2], long long(&all)[2]) {  // other waves wait
+    if (b < ROWS) {
+      sums_before<ROWS>(x, before, all, lds2);
+    } else {
+      __syncthreads();
+      __syncthreads();
+    }
+  };
   const int count = min(max(t.free[0], 0), t.n_pages);
   int have = 0, want = 0;
   if (mine) {
@@ -82,14 +91,17 @@ __global__ __launch_bounds__(THREADS) void pages_grow_kernel(GrowArgs a) {
     last = is_page(t, last) ? last : -1;
   }
 
-  // pages that are given up, from the last one of the last sequence on
-  int gone = 0, released = 0;
-  const int gone_before = sum_before<THREADS>(max(had - get, 0), &gone, lds1);
+  // pages that are given up, from the last one of the last sequence on; by how many
+  const int given_up[2] = {max(had - get, 0), had > get ? 1 : 0};
+  long long gone_before[2], gone_all[2];
+  sums_of_rows(given_up, gone_before, gone_all);
+  if (b == 0) totals[0] = gone_all[0], totals[1] = gone_all[1];
+  __syncthreads();
+  const int gone = (int)totals[0], givers = (int)totals[1];
+  int released = 0;
   if (gone > 0) {
     // those that give something up, side by side: base, the first place that goes, who it is
-    int givers;
-    const int at = sum_before<THREADS>(had > get ? 1 : 0, &givers, lds1);
-    if (had > get) base[at] = gone_before, first[at] = get, back[at] = b;
+    if (had > get) base[gone_before[1]] = (int)gone_before[0], first[gone_before[1]] = get, back[gone_before[1]] = b;
     __syncthreads();
     // Batch by batch: a page that two batches give up goes with the second.  Givers of a page meet in a hash table; the last of them in this order counts all off.
     for (int e0 = 0; e0 < gone; e0 += kGiven * THREADS) {
@@ -146,7 +158,7 @@ __global__ __launch_bounds__(THREADS) void pages_grow_kernel(GrowArgs a) {
   const int holders = last >= 0 ? t.refs[last] : 0;
   const bool shared = holders > 1;
   bool leave = shared;
-  open[b] = shared ? last : -1;
+  if (b < ROWS) open[b] = shared ? last : -1;
   if (__syncthreads_or(shared)) {
     if (shared) {
       int n = 0, after = 0;  // those who share the page and leave it; behind this one
@@ -161,19 +173,19 @@ __global__ __launch_bounds__(THREADS) void pages_grow_kernel(GrowArgs a) {
     }
   }
   const int x[2] = {up ? get - had + (leave ? 1 : 0) : 0, up ? want - have : 0};
-  long long before[2], all[2];
-  sums_before<THREADS>(x, before, all, lds2);
+  long long before[2] = {0, 0}, all[2];
+  sums_of_rows(x, before, all);
   const bool ok = up && before[1] + x[1] <= a.n_slots && ((x[0] == 0 && !shared) || before[0] + x[0] <= (long long)count + released);
   leave = leave && ok;
   const int in[2] = {ok ? x[0] : 0, ok ? x[1] : 0};
   long long in_before[2], in_all[2];
-  sums_before<THREADS>(in, in_before, in_all, lds2);
-  const int taken = (int)in_all[0], total = (int)in_all[1], top = count + released - 1;
-
-  base[b] = (int)in_before[0], first[b] = leave ? had - 1 : had, back[b] = leave ? last : -1;
+  sums_of_rows(in, in_before, in_all);
+  if (b < ROWS) base[b] = (int)in_before[0], first[b] = leave ? had - 1 : had, back[b] = leave ? last : -1;
+  if (b == 0) totals[0] = in_all[0], totals[1] = in_all[1];
   __syncthreads();
+  const int taken = (int)totals[0], total = (int)totals[1], top = count + released - 1;
   for (int o = b; o < taken; o += THREADS) {  // pages from the top of the stack
-    const int s = last_not_above(base, THREADS, o), i = o - base[s], was = back[s];
+    const int s = last_not_above(base, ROWS, o), i = o - base[s], was = back[s];
     const int p = t.free[1 + max(top - o, 0)];
     t.table[(int64_t)s * t.max_pages + first[s] + i] = p;
     if (is_page(t, p)) refs_set(t.refs + p, 1);
@@ -193,12 +205,12 @@ __global__ __launch_bounds__(THREADS) void pages_grow_kernel(GrowArgs a) {
   }
   if (a.n_slots > kResizeOneSlots) return;  // pages_slots_kernel
   __syncthreads();  // base has been read
-  base[b] = (int)in_before[1], first[b] = have;
+  if (b < ROWS) base[b] = (int)in_before[1], first[b] = have;
   all_here();
   for (int i = b; i < a.n_slots; i += THREADS) {
     int slot = -1;
     if (i < total) {
-      const int s = last_not_above(base, min(THREADS, t.batch), i), pos = first[s] + i - base[s];
+      const int s = last_not_above(base, min(ROWS, t.batch), i), pos = first[s] + i - base[s];
       const int p = t.table[(int64_t)s * t.max_pages + (pos >> t.logP)];
       if (is_page(t, p)) slot = (p << t.logP) + (pos & (P - 1));
     }
@@ -571,8 +583,9 @@ size_t pages_fork_bytes(int batch, int max_pages) {
 size_t pages_compact_bytes(int n_pages) { return sizeof(int32_t) * ((size_t)n_pages + 4) + sizeof(long long) * (((size_t)n_pages + 63) / 64 + 1); }
 
 hipError_t launch_pages_grow(const GrowArgs& a, hipStream_t st) {
-  if (a.t.batch <= 256 && (int64_t)a.t.batch * a.t.max_pages <= kSmallTable) pages_grow_kernel<256><<<1, 256, 0, st>>>(a);
-  else pages_grow_kernel<kSharedBatch><<<1, kSharedBatch, 0, st>>>(a);
+  if (a.t.batch <= 256 && (int64_t)a.t.batch * a.t.max_pages <= kSmallTable) pages_grow_kernel<256, 256><<<1, 256, 0, st>>>(a);
+  else if (a.t.batch <= 256) pages_grow_kernel<kSharedBatch, 256><<<1, kSharedBatch, 0, st>>>(a);
+  else pages_grow_kernel<kSharedBatch, kSharedBatch><<<1, kSharedBatch, 0, st>>>(a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.n_slots <= kResizeOneSlots) return e;
   pages_slots_kernel<<<(unsigned)std::min(1024, (a.n_slots + 255) / 256), 256, 0, st>>>(a);
