@@ -18,8 +18,6 @@ namespace {
 
 // ------------------------------------------------------------------------------------------------ the plan
 constexpr int kPlaces = 4;         // of a wave in the first launch
-constexpr int kShareThreads = 1024;
-constexpr int kMostEvents = 3 * kSharedBatch;  // where a set begins or ends; sequences that fork have fewer than 3 each
 // Parts of a call: two workgroups on each CU, as iwdft_pages_attn has them; a second one from parts of 8 tiles (few rows 16) on.  64 requests of 480 rows over 32768 tokens:
 // many_rows with 256 parts 145 us, 512 130, 1024 141.
 constexpr int kSharedParts = 512;
@@ -216,12 +214,12 @@ __device__ __forceinline__ int tokens_seen(const PlanArgs& a, int t0, int t1, in
   return min(near + sinks, t1 - t0);
 }
 
-// One workgroup: the runs from the events, which lie in the order of their places.  THREADS: 256 for up to 64 sequences, whose events one thread each can have
-// as a rule: with 1024 the sums over 16 waves of 16 sequences' plan took 16.6 us, so 7; 64 sequences 8, 256 19.  (All three launches in one, for tables of 128 pages:
-// 29 us with the attention, 25 so; each launch's loads would wait for the one workgroup's own.)
-template <int THREADS>
+// One workgroup: the runs from the events, which lie in the order of their places.  Sums over 16 waves cost more than a few turns of 4: up to 256 sequences 256 threads (us with the
+// attention, 256 / 1024: 256 sequences with 16 beginnings 87 / 95, 100 nested ones 49 / 55; 1000 sequences with 40 beginnings 209 / 134).  16 sequences 7 us, 64 8.  (All three launches
+// in one, for tables of 128 pages: 29 us with the attention, 25 so; every load would wait for the one workgroup's own.)
+template <int THREADS, int BATCH>
 __global__ __launch_bounds__(THREADS) void plan_share_kernel(PlanArgs a) {
-  constexpr int kEvents = THREADS == kShareThreads ? kMostEvents : 3 * kWave;
+  constexpr int kEvents = 3 * BATCH;  // where a set begins or ends; sequences that fork have fewer than 3 each
   __shared__ __attribute__((aligned(16))) int32_t leader[kEvents], from[kEvents];
   __shared__ int32_t news[kEvents], tiles[kEvents], base[THREADS];
   __shared__ long long lds2[THREADS / kWave][2], lds4[THREADS / kWave][4];
@@ -643,8 +641,9 @@ hipError_t launch_pages_plan(const PagesAttn& g, bool bf16, void* plan, hipStrea
   else plan_sets_kernel<16, 2><<<grid(2), 2 * kWave, 0, st>>>(a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  if (g.batch <= kWave) plan_share_kernel<256><<<1, 256, 0, st>>>(a);
-  else plan_share_kernel<kShareThreads><<<1, kShareThreads, 0, st>>>(a);
+  if (g.batch <= kWave) plan_share_kernel<256, kWave><<<1, 256, 0, st>>>(a);
+  else if (g.batch <= 4 * kWave) plan_share_kernel<256, 4 * kWave><<<1, 256, 0, st>>>(a);
+  else plan_share_kernel<1024, kSharedBatch><<<1, 1024, 0, st>>>(a);
   e = hipGetLastError();
   if (e != hipSuccess) return e;
   plan_rows_kernel<<<(unsigned)((2 * g.batch + 64 + 3) / 4), 256, 0, st>>>(a);
