@@ -67,7 +67,7 @@ struct Plan {
   Run* runs;
   int4* chain;       // [sequence][chain]: first row of sums, parts, rows of a part
   int2* mem;         // (row of q, position)
-  int2* events;      // [chunk][events]: sequence and place, new tokens of its set (-1: it is none's first)
+  int4* events;      // [chunk][events]: sequence and place; of the set that begins with it there, new tokens (-1: none does) and the least position of one
   uint16_t* names;   // [sequence][places]: the first sequence that holds the same page there
   int32_t *counts, *chained;  // events of a chunk; runs of a sequence
   int2* owner;                // of a row of q: its sequence (-1: none), which of its new tokens it is
@@ -79,7 +79,7 @@ void lay_out(const PlanSizes& z, int batch, int n_tokens, Plan* p, Take take) {
   p->runs = (Run*)take(z.events * sizeof(Run));
   p->chain = (int4*)take((size_t)batch * z.chain * sizeof(int4));
   p->mem = (int2*)take(z.mem * sizeof(int2));
-  p->events = (int2*)take((size_t)z.chunks * z.events * sizeof(int2));
+  p->events = (int4*)take((size_t)z.chunks * z.events * sizeof(int4));
   p->names = (uint16_t*)take((size_t)batch * z.places * sizeof(uint16_t));
   p->counts = (int32_t*)take(z.chunks * sizeof(int32_t));
   p->chained = (int32_t*)take(batch * sizeof(int32_t));
@@ -114,16 +114,16 @@ __device__ __forceinline__ void in_wave() {  // LDS that the lanes of a wave exc
 template <int EACH, int WAVES>
 __global__ __launch_bounds__(WAVES* kWave) void plan_sets_kernel(PlanArgs a) {
   constexpr int kRows = EACH * kWave, kSlots = 2 * kRows;
-  __shared__ int32_t keys[WAVES][kSlots], firsts[WAVES][kSlots], tokens[WAVES][kRows], changes[WAVES][kRows];
+  __shared__ int32_t keys[WAVES][kSlots], firsts[WAVES][kSlots], tokens[WAVES][kRows], least[WAVES][kRows], changes[WAVES][kRows];
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, chunk = blockIdx.x * WAVES + wave, c0 = chunk * kPlaces;
   for (int64_t t = (int64_t)blockIdx.x * (WAVES * kWave) + threadIdx.x; t < a.n_tokens; t += (int64_t)gridDim.x * (WAVES * kWave)) a.p.owner[t] = make_int2(-1, 0);
   if (chunk >= a.z.chunks) return;
-  int pages[EACH], news[EACH], most = 0;
+  int pages[EACH], news[EACH], begin[EACH], most = 0;
 #pragma unroll
   for (int i = 0; i < EACH; ++i) {
     const int x = lane + kWave * i;
     const News s = x < a.batch ? news_of(a, x) : News{0, 0, 0};
-    pages[i] = pages_of_news(a, s), news[i] = s.n, most = max(most, pages[i]);
+    pages[i] = pages_of_news(a, s), news[i] = s.n, begin[i] = s.len - s.n, most = max(most, pages[i]);
   }
 #pragma unroll
   for (int d = 1; d < kWave; d <<= 1) most = max(most, __shfl_xor(most, d));
@@ -145,7 +145,7 @@ __global__ __launch_bounds__(WAVES* kWave) void plan_sets_kernel(PlanArgs a) {
       const int c = c0 + cc;
       if (c < 0 || c >= most) continue;
       for (int i = lane; i < kSlots; i += kWave) keys[wave][i] = -1, firsts[wave][i] = kRows;
-      for (int i = lane; i < kRows; i += kWave) tokens[wave][i] = 0, changes[wave][i] = 0;
+      for (int i = lane; i < kRows; i += kWave) tokens[wave][i] = 0, least[wave][i] = 0x7fffffff, changes[wave][i] = 0;
       in_wave();
       int cur[EACH], at[EACH];
 #pragma unroll
@@ -181,7 +181,7 @@ __global__ __launch_bounds__(WAVES* kWave) void plan_sets_kernel(PlanArgs a) {
         in_wave();
 #pragma unroll
         for (int i = 0; i < EACH; ++i)
-          if (cur[i] >= 0 && changes[wave][cur[i]]) atomicAdd(&tokens[wave][cur[i]], news[i]);
+          if (cur[i] >= 0 && changes[wave][cur[i]]) atomicAdd(&tokens[wave][cur[i]], news[i]), atomicMin(&least[wave][cur[i]], begin[i]);
         in_wave();
 #pragma unroll
         for (int i = 0; i < EACH; ++i) {
@@ -189,7 +189,7 @@ __global__ __launch_bounds__(WAVES* kWave) void plan_sets_kernel(PlanArgs a) {
           const bool leads = cur[i] == x, event = changes[wave][x] && (leads || (prev[i] == x && cur[i] >= 0));  // where its row ends is known
           const unsigned long long m = __ballot(event);
           const int to = n + __popcll(m & ((1ull << lane) - 1));
-          if (event && to < a.z.events) a.p.events[(int64_t)chunk * a.z.events + to] = make_int2(x | cc << 16, leads ? tokens[wave][x] : -1);
+          if (event && to < a.z.events) a.p.events[(int64_t)chunk * a.z.events + to] = make_int4(x | cc << 16, leads ? tokens[wave][x] : -1, least[wave][x], 0);
           n += __popcll(m);
           name[i][cc / 2] = cc % 2 ? (name[i][cc / 2] & 0xffffu) | (uint32_t)cur[i] << 16 : (name[i][cc / 2] & 0xffff0000u) | ((uint32_t)cur[i] & 0xffffu);
         }
@@ -207,10 +207,10 @@ __global__ __launch_bounds__(WAVES* kWave) void plan_sets_kernel(PlanArgs a) {
   if (lane == 0) a.p.counts[chunk] = n;
 }
 
-// Tokens of a run that rows at position p see, about: the work is shared out by it.
+// Tokens of a run that rows from position p on see: the work is shared out by it.
 __device__ __forceinline__ int tokens_seen(const PlanArgs& a, int t0, int t1, int p) {
   if (!a.n_recent) return t1 - t0;
-  const int near = max(t1 - max(t0, p - min(a.n_recent, p)), 0), sinks = max(min(t1, a.n_sink) - t0, 0);
+  const int near = max(t1 - max(t0, max(p, 0) - min(a.n_recent, max(p, 0))), 0), sinks = max(min(t1, a.n_sink) - t0, 0);
   return min(near + sinks, t1 - t0);
 }
 
@@ -221,7 +221,7 @@ template <int THREADS, int BATCH>
 __global__ __launch_bounds__(THREADS) void plan_share_kernel(PlanArgs a) {
   constexpr int kEvents = 3 * BATCH;  // where a set begins or ends; sequences that fork have fewer than 3 each
   __shared__ __attribute__((aligned(16))) int32_t leader[kEvents], from[kEvents];
-  __shared__ int32_t news[kEvents], tiles[kEvents], base[THREADS];
+  __shared__ int32_t news[kEvents], tiles[kEvents], least[kEvents], base[THREADS];
   __shared__ long long lds2[THREADS / kWave][2], lds4[THREADS / kWave][4];
   __shared__ float lds_f[THREADS / kWave][4];
   __shared__ int32_t longest[THREADS / kWave];
@@ -265,8 +265,8 @@ __global__ __launch_bounds__(THREADS) void plan_share_kernel(PlanArgs a) {
         if (base[m] <= e) lo = m;
         else hi = m;
       }
-      const int2 v = a.p.events[(int64_t)(c0 + lo) * a.z.events + e - base[lo]];
-      leader[n + e] = v.x & 0xffff, from[n + e] = (c0 + lo) * kPlaces + (v.x >> 16), news[n + e] = v.y;
+      const int4 v = a.p.events[(int64_t)(c0 + lo) * a.z.events + e - base[lo]];
+      leader[n + e] = v.x & 0xffff, from[n + e] = (c0 + lo) * kPlaces + (v.x >> 16), news[n + e] = v.y, least[n + e] = v.z;
     }
     n += (int)all[0];
     __syncthreads();
@@ -275,7 +275,7 @@ __global__ __launch_bounds__(THREADS) void plan_share_kernel(PlanArgs a) {
     if (unshared) {
       __syncthreads();
       n = a.batch;
-      for (int i = tid; i < n; i += THREADS) leader[i] = i, from[i] = 0, news[i] = news_of(a, i).n;
+      for (int i = tid; i < n; i += THREADS) leader[i] = i, from[i] = 0, news[i] = news_of(a, i).n, least[i] = news_of(a, i).len - news[i];
       __syncthreads();
     }
     const auto end_of = [&](int i) {  // where its leader's next event is, or its row ends
@@ -298,7 +298,7 @@ __global__ __launch_bounds__(THREADS) void plan_share_kernel(PlanArgs a) {
     for (int i = tid; i < n; i += THREADS) {
       const int rows = rows_of(i), tile = is_many(rows) ? Many::tile : Few<1>::tile;
       to = end_of(i);
-      const int seen = tokens_seen(a, from[i] << a.S.logP, to << a.S.logP, news_of(a, leader[i]).len - 1);
+      const int seen = tokens_seen(a, from[i] << a.S.logP, to << a.S.logP, least[i]);
       tiles[i] = to > from[i] && rows ? max((seen + tile - 1) / tile, 1) : 0;
       const float blocks = tiles[i] ? (float)blocks_of(rows) : 0.f;
       const bool many = is_many(rows);
