@@ -1,4 +1,4 @@
-// The 8-bit paged cache: layout and conversions shared by its kernels (pages.hip, pages_attn.hip).
+// The 8-bit paged cache: layout and conversions shared by its kernels (pages.hip, pages_attn.hip, pages_tables.hip, pages_shared.hip).
 //
 // Exact tokens of requests that are not (yet) in the frequency domain, P to a page, as OCP e4m3 with one power-of-two scale for each page,
 // KV head and tensor.  A power of two loses nothing: x 2^-e is exact, so a stored value is off by one rounding to four significant bits
