@@ -74,7 +74,7 @@ class Schedule {
   __device__ __forceinline__ Place find(int y, Count count) const {
     int done = 0, cut = 0;
     for (int b0 = 0;; b0 += kWave) {
-      const Seq s = b0 == 0 ? head : load(b0 + lane);
+      const Seq s = b0 == 0 && kHold ? head : load(b0 + lane);
       const int np = parts(s), n = count(s, np), c = np > 1 ? np * blocks(s.rows) : 0, in = scan(n), cin = scan(c);
       const unsigned long long m = __ballot(y < done + in);
       if (m || b0 + kWave >= a.batch) {  // always found: y is below the sum of all counts
@@ -90,7 +90,9 @@ class Schedule {
   const PagesAttn& a;
   const PagesRows& which;
   int lane;
-  Seq head;  // the lane's sequence of the first 64
+  // The lane's sequence of the first 64; read again by the kernel of 64 rows, which has no registers left (12 tokens over 65536: 71.1 us with it held, 68.6 so).
+  static constexpr bool kHold = Geo::rows != 64;
+  Seq head;
 
   template <class Do>
   __device__ __forceinline__ void each(Do use) const {
