@@ -37,7 +37,7 @@ struct Run {
 struct Item {
   int32_t leader, from, to, mem;
   int32_t row0, rows, part, np;
-  int32_t slot, kind, pad0, pad1;
+  int32_t slot, unused[3];
 };
 static_assert(sizeof(PlanHead) == 64 && sizeof(Run) == 32 && sizeof(Item) == 48, "");
 
@@ -431,7 +431,7 @@ __global__ __launch_bounds__(256) void plan_rows_kernel(PlanArgs a) {
       for (int k = lane; k < blocks * r.np; k += kWave) {
         if (r.item + k >= a.z.items) break;
         const int part = k / blocks, block = blocks - 1 - (k - part * blocks), row0 = block * size;  // blocks that read the same tokens side by side
-        a.p.items[r.item + k] = Item{r.leader, r.from, r.to, r.mem, row0, min(size, rows - row0), part, r.np, r.slot + part * rows + row0, 0, 0, 0};
+        a.p.items[r.item + k] = Item{r.leader, r.from, r.to, r.mem, row0, min(size, rows - row0), part, r.np, r.slot + part * rows + row0, {0, 0, 0}};
       }
     }
   }

@@ -242,7 +242,6 @@ __global__ __launch_bounds__(256) void pages_slots_kernel(GrowArgs a) {
 // ------------------------------------------------------------------------------------------------ forking
 // Every row takes its parent's entries, all at once: whoever has a place reads it of all rows and then writes.  A page is held at one place, so those who leave
 // and enter it meet there.
-
 struct ForkRows {
   int32_t parent[kSharedBatch], had[kSharedBatch], get[kSharedBatch], len[kSharedBatch];
 };
@@ -317,8 +316,8 @@ __global__ __launch_bounds__(THREADS) void pages_fork_one_kernel(ForkArgs a) {
   if (threadIdx.x == 0) t.free[0] = min(count + released, t.n_pages);
 }
 
-// Large tables: a wave for each place (256 rows of 550 places: 78 us with atomics on refs by workgroups of 8192 entries each, 10.2 so, and 5.6 for the stack).  What leaves and what enters meets in a hash table in LDS, so that refs are read and written once, by the first of those who
-// leave a page or, where nobody does, of those who enter it.
+// Large tables: a wave for each place.  What leaves and what enters meets in a hash table in LDS, so that refs are read and written once, by the first of those who
+// leave a page or, where nobody does, of those who enter it.  256 rows of 550 places: 10.2 us, and 5.6 for the stack; with atomics on refs, by workgroups of 8192 entries each, 78.
 // scratch: the stack's count, the most pages of a row, new lengths [batch], bits of the rows whose entry is given back [places][words], those pages [batch][max_pages]
 struct ForkScratch {
   int32_t *head, *lens;
