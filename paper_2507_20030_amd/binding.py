@@ -720,6 +720,15 @@ class PagesPlan:
 
     __slots__ = ("buffer", "n_layers", "n_tokens", "batch", "max_pages", "n_pages", "n_kv_heads", "n_q_heads", "page_tokens", "dtype", "n_sink", "n_recent")
 
+    def __init__(self, buffer, made_for):
+        self.buffer = buffer
+        (self.n_layers, self.n_tokens, self.batch, self.max_pages, self.n_pages, self.n_kv_heads, self.n_q_heads, self.page_tokens, self.dtype, self.n_sink,
+         self.n_recent) = made_for
+
+    def made_for(self):
+        return (self.n_layers, self.n_tokens, self.batch, self.max_pages, self.n_pages, self.n_kv_heads, self.n_q_heads, self.page_tokens, self.dtype, self.n_sink,
+                self.n_recent)
+
 
 def iwdft_pages_plan(starts, table, lens, n_tokens: int, n_pages: int, n_kv_heads: int, n_q_heads: int, page_tokens: int, dtype: torch.dtype, n_layers: int = 1,
                      n_sink: int = 0, n_recent: int = 0, stream=None, plan: Optional[PagesPlan] = None) -> PagesPlan:
@@ -741,12 +750,9 @@ def iwdft_pages_plan(starts, table, lens, n_tokens: int, n_pages: int, n_kv_head
     desc, need, _ = _shared_sizes(n_layers, batch, n_tokens, n_layers, n_pages, n_kv_heads, n_q_heads, 128, page_tokens, max_pages, dtype)
     made_for = (n_layers, n_tokens, batch, max_pages, n_pages, n_kv_heads, n_q_heads, page_tokens, dtype, n_sink, n_recent)
     if plan is None:
-        plan = PagesPlan()
-        plan.buffer = _scratch(need, table.device, stream, None)
-        for name, value in zip(PagesPlan.__slots__[1:], made_for):
-            setattr(plan, name, value)
-    elif made_for != tuple(getattr(plan, name) for name in PagesPlan.__slots__[1:]) or (need and plan.buffer.get_device() != index):
-        raise ValueError(f"the plan was made for {[(name, getattr(plan, name)) for name in PagesPlan.__slots__[1:]]}, not {made_for}")
+        plan = PagesPlan(_scratch(need, table.device, stream, None), made_for)
+    elif made_for != plan.made_for() or (need and plan.buffer.get_device() != index):
+        raise ValueError(f"the plan was made for {dict(zip(PagesPlan.__slots__[1:], plan.made_for()))}, not {made_for}")
     buffer = plan.buffer
     rc = load_library().iwdft_pages_plan(desc, n_layers, starts.data_ptr(), n_tokens, table.data_ptr(), lens.data_ptr(), batch, n_sink, n_recent,
                                          buffer.data_ptr() if buffer is not None else None, buffer.nbytes if buffer is not None else 0, _stream_of(stream, index))

@@ -383,6 +383,30 @@ def test_attention_of_pages_far_apart(dtype):
         attend(pool, rng, [1] * batch, G, dtype)
 
 
+def test_attention_far_into_a_long_pool_and_over_long_sequences():
+    """Offsets beyond 32 bits; half a million tokens shared by two sequences: against iwdft_pages_attn."""
+    g = torch.Generator(device=DEV).manual_seed(3)
+    n_pages, P = 160_000, 128
+    values, exponents = torch.zeros((1, n_pages, 1, 2, P * 128), dtype=torch.uint8, device=DEV), torch.full((1, n_pages, 1, 2), -7, dtype=torch.int32, device=DEV)
+    assert values.numel() > 1 << 32
+    values[:, 155_000:] = torch.randint(0, 120, (1, 5000, 1, 2, P * 128), dtype=torch.uint8, device=DEV, generator=g)
+    shared = torch.arange(n_pages - 1, n_pages - 1 - 4000, -1, dtype=torch.int32, device=DEV)
+    table = torch.full((3, 4100), -1, dtype=torch.int32, device=DEV)
+    table[:2, :4000] = shared
+    table[2, :1500] = shared[:1500]
+    table[1, 4000:4003], table[0, 4000], table[2, 1500] = torch.arange(155_500, 155_503, device=DEV), 155_400, 155_401
+    lens, starts = ints([4000 * P + 77, 4002 * P + 1, 1500 * P + 128]), ints([0, 1, 2, 4])
+    for dtype in ("f32", "bf16"):
+        q = (torch.randn((1, 4, 2, 128), device=DEV, generator=g) * 0.05).to(DT[dtype])
+        out, ref = torch.zeros_like(q), torch.zeros_like(q)
+        B.iwdft_pages_attn(values, exponents, q, starts, table, lens, ref)
+        plan = B.iwdft_pages_plan(starts, table, lens, 4, n_pages, 1, 2, P, DT[dtype])
+        B.iwdft_pages_attn_shared(values, exponents, q, plan, table, out)
+        err = float((out.double() - ref.double()).norm() / ref.double().norm())
+        # two roundings of the result; fp32: sums of 16000 tiles, 2^-24 each, of both calls (at random 2^-16, all one way 2^-9), far from each other's
+        assert err < (2.0 ** -7 if dtype == "bf16" else 2.0 ** -9), err
+
+
 def test_attention_of_short_sequences_in_a_wide_table():
     rng = np.random.default_rng(15)
     pool = Pool(rng, forest_of(rng, "samples", 5, 50, 20), 16)
@@ -425,7 +449,7 @@ def test_attention_long_and_as_page_attention(dtype):
         plan = B.iwdft_pages_plan(starts, table, lens, batch, 9000, H, G * H, P, DT[dtype], **window)
         B.iwdft_pages_attn_shared(values, exponents, q, plan, table, out)
         err = float((out.double() - ref.double()).norm() / ref.double().norm())
-        assert err < (2.0 ** -7 if dtype == "bf16" else 2.0 ** -17), err  # two roundings of the result; both sums' 22 bits and what sums of tens of thousands of tokens lose
+        assert err < (2.0 ** -7 if dtype == "bf16" else 2.0 ** -17), err  # two roundings of the result; fp32: 22 bits of both calls, sums of 1000 tiles at random: 2 sqrt(1000) 2^-24 = 2^-18
         again = torch.zeros_like(q)
         B.iwdft_pages_attn_shared(values, exponents, q, plan, table, again)
         assert torch.equal(out, again)
