@@ -25,6 +25,7 @@ constexpr int kSharedParts = 512;
 // tokens 71.5 / 72.6 (with up to 32 75.2; fp32 100 / 99, 132); 92 rows over 65536 78 / 97; 120 over 8192 48.6 / 45.1, over 32768 63.0 / 70.2, over 131072 128 / 184.
 constexpr int kSharedFew = 64;
 constexpr int kPlanMark = 0x49574446;
+constexpr int kFlat = kWave;  // parts of a row that are listed for it
 
 struct PlanHead {
   int32_t mark, n_layers, H, G, logP, max_pages, batch, n_tokens, n_sink, n_recent, few_rows;
@@ -70,7 +71,8 @@ struct Plan {
   int4* events;      // [chunk][events]: sequence and place; of the set that begins with it there, new tokens (-1: none does) and the least position of one
   uint16_t* names;   // [sequence][places]: the first sequence that holds the same page there
   int32_t *counts, *chained;  // events of a chunk; runs of a sequence
-  int2* owner;                // of a row of q: its sequence (-1: none), which of its new tokens it is
+  int4* owner;                // of a row of q: its sequence (-1: none), which of its new tokens it is, its parts
+  int32_t* flat;              // [row of q][kFlat]: the first row of sums of each of its parts, where they are no more
 };
 template <class Take>
 void lay_out(const PlanSizes& z, int batch, int n_tokens, Plan* p, Take take) {
@@ -83,7 +85,8 @@ void lay_out(const PlanSizes& z, int batch, int n_tokens, Plan* p, Take take) {
   p->names = (uint16_t*)take((size_t)batch * z.places * sizeof(uint16_t));
   p->counts = (int32_t*)take(z.chunks * sizeof(int32_t));
   p->chained = (int32_t*)take(batch * sizeof(int32_t));
-  p->owner = (int2*)take(n_tokens * sizeof(int2));
+  p->owner = (int4*)take(n_tokens * sizeof(int4));
+  p->flat = (int32_t*)take((size_t)n_tokens * kFlat * sizeof(int32_t));
 }
 
 struct PlanArgs {
@@ -116,7 +119,7 @@ __global__ __launch_bounds__(WAVES* kWave) void plan_sets_kernel(PlanArgs a) {
   constexpr int kRows = EACH * kWave, kSlots = 2 * kRows;
   __shared__ int32_t keys[WAVES][kSlots], firsts[WAVES][kSlots], tokens[WAVES][kRows], least[WAVES][kRows], changes[WAVES][kRows];
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, chunk = blockIdx.x * WAVES + wave, c0 = chunk * kPlaces;
-  for (int64_t t = (int64_t)blockIdx.x * (WAVES * kWave) + threadIdx.x; t < a.n_tokens; t += (int64_t)gridDim.x * (WAVES * kWave)) a.p.owner[t] = make_int2(-1, 0);
+  for (int64_t t = (int64_t)blockIdx.x * (WAVES * kWave) + threadIdx.x; t < a.n_tokens; t += (int64_t)gridDim.x * (WAVES * kWave)) a.p.owner[t] = make_int4(-1, 0, 0, 0);
   if (chunk >= a.z.chunks) return;
   int pages[EACH], news[EACH], begin[EACH], most = 0;
 #pragma unroll
@@ -366,6 +369,14 @@ __global__ __launch_bounds__(THREADS) void plan_share_kernel(PlanArgs a) {
   }
 }
 
+// The first row of sums of part `part` of a row's runs, a lane for each run: x of the run that it is in -- which is how many end before it --, y parts of z rows; to: their sums.
+__device__ __forceinline__ int part_slot(int4 run, int to, int runs, int part) {
+  int which = 0;
+  for (int c = 0; c < runs; ++c) which += __builtin_amdgcn_readlane(to, c) <= part;
+  which = min(which, kWave - 1);
+  return __shfl(run.x, which) + (part - (__shfl(to, which) - __shfl(run.y, which))) * __shfl(run.z, which);
+}
+
 // A wave for each sequence: its runs, in order, and its rows in them.  A wave for each run: its items.  16 sequences 4.5 us, 12 with forty runs 7, 256 9.6.
 __global__ __launch_bounds__(256) void plan_rows_kernel(PlanArgs a) {
   const int lane = threadIdx.x % kWave, unit = blockIdx.x * 4 + threadIdx.x / kWave;
@@ -421,7 +432,13 @@ __global__ __launch_bounds__(256) void plan_rows_kernel(PlanArgs a) {
       }
       k += __popcll(in);
     }
-    for (int t = lane; t < s.n; t += kWave) a.p.owner[s.first + t] = make_int2(x, t);
+    // all parts of its rows, run by run: a lane for each
+    const int4 run = lane < min(k, a.z.chain) ? a.p.chain[(int64_t)x * a.z.chain + lane] : make_int4(0, 0, 0, 0);
+    const int to = scan(run.y), parts = k > kFlat ? kFlat + 1 : last_lane(to);
+    const int first = part_slot(run, to, min(k, kFlat), lane);
+    for (int t = 0; t < s.n && parts <= kFlat; ++t)
+      if (lane < parts) a.p.flat[(int64_t)(s.first + t) * kFlat + lane] = first + t * a.S.G;
+    for (int t = lane; t < s.n; t += kWave) a.p.owner[s.first + t] = make_int4(x, t, parts, 0);
     if (lane == 0) a.p.chained[x] = min(k, a.z.chain);
   } else {
     const int waves = gridDim.x * 4 - a.batch;
@@ -521,8 +538,9 @@ __global__ __launch_bounds__(kWaves* kWave, BF16 ? 2 : (R == 1 && !MANY ? 2 : 1)
   if constexpr (R > 0) few_rows<BF16, R, kWaves>(s.a, Items(s, false, threadIdx.x % kWave), x, gridDim.x);
 }
 
-// A row's parts: its runs' first rows of sums and numbers of parts, a lane for each, become a list of all parts; a lane for each reads its reference, then all
-// sums are on their way at once.  Bound by four loads that wait for each other (run by run and part by part, each rescaling the last: 15.5 us for beams with twenty runs, so 10.3).
+// A row's parts: the plan lists where the sums of up to 64 of them are; of more they are found from its runs, a lane for each.  A lane for each part reads its reference, then all
+// sums are on their way at once.  Bound by loads that wait for each other: 480 rows of 17 parts 5.8 us (6.7 with the runs looked up for every row); beams of twenty runs, 17 MB, 9.8
+// (run by run and part by part, each rescaling the last, 15.5).
 // Few rows: a workgroup for each, its waves share the parts.  Many: a wave for each (3840 rows of 17 parts, 34 MB: 14.9 and 11.4 us; 2048 rows 7.2 and 7.9; 736 rows of beams
 // 10.3 and 20).
 constexpr int64_t kManyShared = 2048;
@@ -530,51 +548,51 @@ template <bool BF16>
 __global__ __launch_bounds__(kWaves* kWave) void shared_join_kernel(SharedAttn s, int64_t all, int many) {
   __shared__ float2 sums[kWaves][kWave], stats[kWaves];
   const PagesAttn& a = s.a;
-  if (!is_for(*s.p.head, s)) return;
+  const bool fits = is_for(*s.p.head, s);  // looked at together with the row, whose loads do not wait for it
   const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), slots = s.p.head->slots, G = a.S.G;
   const uint32_t row_heads = (uint32_t)(a.n_tokens * G);
   for (uint32_t x = many ? blockIdx.x * kWaves + wave : blockIdx.x; x < (uint32_t)all; x += gridDim.x * (many ? kWaves : 1)) {
     const int lh = (int)(x / row_heads), r = (int)(x - (uint32_t)lh * row_heads), token = (int)((uint32_t)r / (uint32_t)G);
-    const int2 owner = s.p.owner[token];
-    const int b = __builtin_amdgcn_readfirstlane(owner.x), mine = __builtin_amdgcn_readfirstlane(owner.y) * G + r - token * G;
-    if (b < 0) continue;  // behind the last sequence
-    const int4* chain = s.p.chain + (int64_t)b * s.z.chain;
-    const int4 first = chain[min(lane, s.z.chain - 1)];  // with their number on its way
-    const int n = __builtin_amdgcn_readfirstlane(s.p.chained[b]);
-    const int64_t slot0 = (int64_t)lh * slots + mine;
+    const int4 owner = s.p.owner[token];
+    const int listed = s.p.flat[(int64_t)token * kFlat + lane];
+    const int b = __builtin_amdgcn_readfirstlane(owner.x), listed_parts = __builtin_amdgcn_readfirstlane(owner.z);
+    if (!fits || b < 0) continue;  // behind the last sequence
     float m = -FLT_MAX, l = 0.f;
     float2 o = make_float2(0.f, 0.f);
     const auto add = [&](float top, float2 v, float sum, float half) {  // half: 2^(half of the reference's distance)
       const float up = fmaxf(m, top), f = __builtin_amdgcn_exp2f(0.5f * (m - up));
       o.x = o.x * (f * f) + v.x * (half * half), o.y = o.y * (f * f) + v.y * (half * half), l = l * f * f + sum * half * half, m = up;
     };
-    for (int i0 = 0; i0 < n; i0 += kWave) {
-      int4 run = first;
-      if (i0) run = chain[min(i0 + lane, n - 1)];
-      if (i0 + lane >= n) run = make_int4(0, 0, 0, 0);
-      const int to = scan(run.y), parts = last_lane(to), size = many ? kWave : min(kWave, (parts + kWaves - 1) / kWaves);
-      for (int p0 = many ? 0 : wave * size; p0 < parts; p0 += size * (many ? 1 : kWaves)) {
-        const int part = p0 + lane, here = min(parts - p0, size);
-        int which = 0;  // the run of the lane's part: how many end before it
-        for (int c = 0; c < min(n - i0, kWave); ++c) which += __builtin_amdgcn_readlane(to, c) <= part;
-        which = min(which, kWave - 1);
-        const int64_t at = slot0 + __shfl(run.x, which) + (int64_t)(part - (__shfl(to, which) - __shfl(run.y, which))) * __shfl(run.z, which);
-        const float2 st = lane < here ? s.stat[at] : make_float2(-FLT_MAX, 0.f);
-        float top = st.x;
+    const auto add_parts = [&](int64_t at, int here) {  // a lane for each
+      const float2 st = lane < here ? s.stat[at] : make_float2(-FLT_MAX, 0.f);
+      float top = st.x;
 #pragma unroll
-        for (int d = 1; d < kWave; d <<= 1) top = fmaxf(top, __shfl_xor(top, d));
-        const float up = fmaxf(m, top), g = __builtin_amdgcn_exp2f(0.5f * (st.x - up)), f = __builtin_amdgcn_exp2f(0.5f * (m - up));
-        float sum = st.y * g * g;  // a denominator's share may need both factors
+      for (int d = 1; d < kWave; d <<= 1) top = fmaxf(top, __shfl_xor(top, d));
+      const float up = fmaxf(m, top), g = __builtin_amdgcn_exp2f(0.5f * (st.x - up)), f = __builtin_amdgcn_exp2f(0.5f * (m - up));
+      float sum = st.y * g * g;  // a denominator's share may need both factors
 #pragma unroll
-        for (int d = 1; d < kWave; d <<= 1) sum += __shfl_xor(sum, d);
-        l = l * f * f + sum, o.x *= f * f, o.y *= f * f, m = up;
+      for (int d = 1; d < kWave; d <<= 1) sum += __shfl_xor(sum, d);
+      l = l * f * f + sum, o.x *= f * f, o.y *= f * f, m = up;
 #pragma unroll 8
-        for (int c = 0; c < here; ++c) {
-          const int64_t row = (int64_t)(uint32_t)__builtin_amdgcn_readlane((int)at, c) | (int64_t)__builtin_amdgcn_readlane((int)(at >> 32), c) << 32;
-          const float2 v = *(const float2*)(s.part + row * kHeadDim + 2 * lane);
-          const float w = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(g), c)), ww = w * w;
-          o.x += v.x * ww, o.y += v.y * ww;
-        }
+      for (int c = 0; c < here; ++c) {
+        const int64_t row = (int64_t)(uint32_t)__builtin_amdgcn_readlane((int)at, c) | (int64_t)__builtin_amdgcn_readlane((int)(at >> 32), c) << 32;
+        const float2 v = *(const float2*)(s.part + row * kHeadDim + 2 * lane);
+        const float w = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(g), c)), ww = w * w;
+        o.x += v.x * ww, o.y += v.y * ww;
+      }
+    };
+    const auto share = [&](int parts, auto slot_of) {  // those of this wave
+      const int size = many ? kWave : min(kWave, (parts + kWaves - 1) / kWaves);
+      for (int p0 = many ? 0 : wave * size; p0 < parts; p0 += size * (many ? 1 : kWaves)) add_parts((int64_t)lh * slots + (r - token * G) + slot_of(p0 + lane), min(parts - p0, size));
+    };
+    if (listed_parts <= kFlat) {
+      share(listed_parts, [&](int part) { return __shfl(listed, min(part, kWave - 1)); });
+    } else {
+      const int n = s.p.chained[b];
+      for (int i0 = 0; i0 < n; i0 += kWave) {
+        const int4 run = i0 + lane < n ? s.p.chain[(int64_t)b * s.z.chain + i0 + lane] : make_int4(0, 0, 0, 0);
+        const int to = scan(run.y);
+        share(last_lane(to), [&](int part) { return part_slot(run, to, min(n - i0, kWave), part) + owner.y * G; });
       }
     }
     if (!many) {
