@@ -377,7 +377,7 @@ __device__ __forceinline__ int part_slot(int4 run, int to, int runs, int part) {
   return __shfl(run.x, which) + (part - (__shfl(to, which) - __shfl(run.y, which))) * __shfl(run.z, which);
 }
 
-// A wave for each sequence: its runs, in order, and its rows in them.  A wave for each run: its items.  16 sequences 4.5 us, 12 with forty runs 7, 256 9.6.
+// A wave for each sequence: its runs, in order, its rows in them and their parts.  A wave for each run: its items.  16 sequences 5 us, 12 with forty runs 9, 256 10.
 __global__ __launch_bounds__(256) void plan_rows_kernel(PlanArgs a) {
   const int lane = threadIdx.x % kWave, unit = blockIdx.x * 4 + threadIdx.x / kWave;
   const PlanHead& head = *a.p.head;
