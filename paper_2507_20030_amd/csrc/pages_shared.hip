@@ -432,7 +432,8 @@ __global__ __launch_bounds__(256) void plan_rows_kernel(PlanArgs a) {
       }
       k += __popcll(in);
     }
-    // all parts of its rows, run by run: a lane for each
+    // all parts of its rows, run by run: a lane for each.  The lanes read what others of their wave have just stored.
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     const int4 run = lane < min(k, a.z.chain) ? a.p.chain[(int64_t)x * a.z.chain + lane] : make_int4(0, 0, 0, 0);
     const int to = scan(run.y), parts = k > kFlat ? kFlat + 1 : last_lane(to);
     const int first = part_slot(run, to, min(k, kFlat), lane);
