@@ -853,7 +853,8 @@ class PagedCache:
         return moves
 
     def repool(self, n_pages: int, stream=None) -> None:
-        """The sequences in a pool of n_pages pages, larger or smaller; plans made before are void.  Needs both pools at a time, and waits for the stream to learn how many pages are held."""
+        """The sequences in a pool of n_pages pages, larger or smaller; plans made before are void.  Needs both pools at a time, and waits for the stream: to learn how
+        many pages are held, and before the old pool's memory is given back."""
         self._shares()
         L, H, G, D = self.shape
         iwdft_pages_query_bytes(pages_desc(L, n_pages, H, G, D, self.page_tokens, self.table.shape[1], self.dtype))
@@ -872,6 +873,8 @@ class PagedCache:
             none = torch.empty((0, 2), **ints)
         iwdft_pages_copy(copies, self.values, self.exponents, values, exponents, stream=stream)
         iwdft_pages_compact(self.table, self.lens, free, refs, none, self.page_tokens, stream)  # nothing moves: the stack of the new pool
+        with _on_stream(stream, self.device):
+            torch.cuda.current_stream(self.device).synchronize()
         self.values, self.exponents, self.refs, self.free = values, exponents, refs, free
 
     def write(self, k, v, slots, layer=0, stream=None):

@@ -559,6 +559,22 @@ def test_beams_from_a_prompt_to_an_answer(dtype, P, G, windows):
     assert int(s.c.free[0]) == held and not s.c.refs.any() and not s.c.lens.any()
 
 
+def test_a_pool_is_given_back_when_its_last_read_is_done():
+    """repool on a stream of its own: once it returns, nobody reads the old pool, whose memory the next allocation may get."""
+    rng = np.random.default_rng(21)
+    c = B.PagedCache(2, 400, 2, 4, 128, torch.bfloat16, 2, 4000, 16, DEV, shared=True)
+    x = dev(rng.normal(size=(2, 2, 3000, 2, 128))).bfloat16()
+    _, slots = c.resize(ints([3000, 0]), 3000)
+    c.write(x[0], x[1], slots)
+    c.fork(ints([0, 0]))
+    before, side = c.read(3000), torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    for given, n_pages in ((side, 300), (side.cuda_stream, 200)):
+        c.repool(n_pages, stream=given)
+        assert side.query() and c.values.shape[1] == n_pages
+    assert all(torch.equal(a, b) for a, b in zip(before, c.read(3000)))
+
+
 def test_a_shared_beginning_is_compressed():
     """Two requests with one beginning, handed to the frequency domain together: as from pages of their own."""
     rng = np.random.default_rng(7)
