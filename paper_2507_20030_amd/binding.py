@@ -715,13 +715,25 @@ def iwdft_pages_attn_shared_bytes(desc: iwdft_pages_desc, n_layers: int, batch: 
     return _bytes_of(load_library().iwdft_pages_attn_shared_bytes, ctypes.byref(desc), n_layers, batch, n_tokens)
 
 
+def _raw(stream, index: int) -> int:
+    """The call's stream, as a number that can be compared."""
+    return torch._C._cuda_getCurrentRawStream(index) if stream is None else _stream(stream).value or 0
+
+
+def _used_on(buffer, stream: int) -> None:
+    """The memory of `buffer`, which its owner may drop at any time, is not given to anyone else before the work of that stream is done."""
+    if not torch.cuda.is_current_stream_capturing():  # who replays a graph keeps what it reads
+        buffer.record_stream(torch.cuda.ExternalStream(stream, buffer.device) if stream else torch.cuda.default_stream(buffer.device))
+
+
 class PagesPlan:
-    """Who shares what in a step: iwdft_pages_plan's buffer and what it was made for."""
+    """Who shares what in a step: iwdft_pages_plan's buffer and what it was made for.  It may be dropped as soon as the last call that reads it has been made, on whatever
+    stream that lives as long as it does; one that a captured graph reads is kept as long as the graph."""
 
-    __slots__ = ("buffer", "n_layers", "n_tokens", "batch", "max_pages", "n_pages", "n_kv_heads", "n_q_heads", "page_tokens", "dtype", "n_sink", "n_recent")
+    __slots__ = ("buffer", "n_layers", "n_tokens", "batch", "max_pages", "n_pages", "n_kv_heads", "n_q_heads", "page_tokens", "dtype", "n_sink", "n_recent", "stream")
 
-    def __init__(self, buffer, made_for):
-        self.buffer = buffer
+    def __init__(self, buffer, made_for, stream):
+        self.buffer, self.stream = buffer, stream  # whose order the buffer was allocated in
         (self.n_layers, self.n_tokens, self.batch, self.max_pages, self.n_pages, self.n_kv_heads, self.n_q_heads, self.page_tokens, self.dtype, self.n_sink,
          self.n_recent) = made_for
 
@@ -750,12 +762,14 @@ def iwdft_pages_plan(starts, table, lens, n_tokens: int, n_pages: int, n_kv_head
     desc, need, _ = _shared_sizes(n_layers, batch, n_tokens, n_layers, n_pages, n_kv_heads, n_q_heads, 128, page_tokens, max_pages, dtype)
     made_for = (n_layers, n_tokens, batch, max_pages, n_pages, n_kv_heads, n_q_heads, page_tokens, dtype, n_sink, n_recent)
     if plan is None:
-        plan = PagesPlan(_scratch(need, table.device, stream, None), made_for)
+        plan = PagesPlan(_scratch(need, table.device, stream, None), made_for, _raw(stream, index))
     elif made_for != plan.made_for() or (need and plan.buffer.get_device() != index):
-        raise ValueError(f"the plan was made for {dict(zip(PagesPlan.__slots__[1:], plan.made_for()))}, not {made_for}")
-    buffer = plan.buffer
+        raise ValueError(f"the plan was made for {dict(zip(PagesPlan.__slots__[1:-1], plan.made_for()))}, not {made_for}")
+    buffer, on = plan.buffer, _raw(stream, index)
+    if on != plan.stream and buffer is not None:
+        _used_on(buffer, on)
     rc = load_library().iwdft_pages_plan(desc, n_layers, starts.data_ptr(), n_tokens, table.data_ptr(), lens.data_ptr(), batch, n_sink, n_recent,
-                                         buffer.data_ptr() if buffer is not None else None, buffer.nbytes if buffer is not None else 0, _stream_of(stream, index))
+                                         buffer.data_ptr() if buffer is not None else None, buffer.nbytes if buffer is not None else 0, on)
     if rc:
         _check(rc)
     return plan
@@ -779,11 +793,13 @@ def iwdft_pages_attn_shared(values, exponents, q, plan: PagesPlan, table, out, l
             return iwdft_pages_attn_shared(values, exponents, q, plan, table, out, layer, scale, stream, workspace)
     desc, _, need = _shared_sizes(plan.n_layers, plan.batch, plan.n_tokens, n_layers, n_pages, heads, plan.n_q_heads, 128, P, plan.max_pages, dtype)
     ws = _scratch(need, values.device, stream, workspace) if need or workspace is not None else None
-    buffer = plan.buffer
+    buffer, on = plan.buffer, _raw(stream, index)
+    if on != plan.stream and buffer is not None:
+        _used_on(buffer, on)
     rc = load_library().iwdft_pages_attn_shared(desc, layer, plan.n_layers, q.data_ptr(), plan.n_tokens, buffer.data_ptr() if buffer is not None else None,
                                                 buffer.nbytes if buffer is not None else 0, table.data_ptr(), plan.batch, values.data_ptr(), exponents.data_ptr(),
                                                 out.data_ptr(), plan.n_sink, plan.n_recent, scale, ws.data_ptr() if ws is not None else None,
-                                                ws.nbytes if ws is not None else 0, _stream_of(stream, index))
+                                                ws.nbytes if ws is not None else 0, on)
     if rc:
         _check(rc)
 

@@ -679,6 +679,32 @@ def test_two_graphs_and_another_stream():
     assert torch.equal(o, ref[0])
 
 
+def test_a_plan_is_dropped_while_another_stream_reads_it():
+    """Made on one stream, read on another that is still at work when the plan goes: its memory is not handed out before."""
+    rng = np.random.default_rng(22)
+    pool = Pool(rng, forest_of(rng, "samples", 24, 900, 300), 32, heads=4)
+    starts, q = ints(range(25)), torch.randn((1, 24, 16, 128), device=DEV).bfloat16()
+    ref, out = torch.zeros_like(q), torch.zeros_like(q)
+    B.iwdft_pages_attn_shared(pool.values, pool.exponents, q, plan_of(pool, range(25), 24, 4, "bf16"), pool.d_table, ref)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for drop_on, read_on in ((side, torch.cuda.current_stream()), (torch.cuda.current_stream(), side)):
+        with torch.cuda.stream(drop_on):
+            plan = B.iwdft_pages_plan(starts, pool.d_table, pool.d_lens, 24, pool.n_pages, 4, 16, 32, torch.bfloat16)
+            drop_on.synchronize()
+            size, at = plan.buffer.nbytes, plan.buffer.data_ptr()
+        with torch.cuda.stream(read_on):
+            out.zero_()
+            torch.cuda._sleep(20_000_000)
+            B.iwdft_pages_attn_shared(pool.values, pool.exponents, q, plan, pool.d_table, out)
+        del plan
+        with torch.cuda.stream(drop_on):
+            others = [torch.empty(size, dtype=torch.uint8, device=DEV) for _ in range(4)]
+            assert all(t.data_ptr() != at for t in others) or read_on.query()
+        torch.cuda.synchronize()
+        assert torch.equal(out, ref)
+
+
 def test_calls_without_rows_or_sequences():
     """No new tokens, no sequences, sequences that bring nothing: nothing is written where nothing is to be."""
     rng = np.random.default_rng(13)
