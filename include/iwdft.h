@@ -413,7 +413,7 @@ int iwdft_pages_resize_shared(int32_t page_tokens, int32_t n_pages, int32_t max_
                               int32_t* d_free, int32_t* d_refs, int32_t* d_starts, int32_t* d_slots, int32_t n_slots, int32_t* d_copies, void* hip_stream);
 
 /* Page d_copies[i][1] of the pool d_to_values, d_to_exponents (to_pages pages; may be the same pool) becomes page d_copies[i][0] of the other one, byte for byte, in layers layer .. layer +
- * n_layers - 1 of both; pairs with a page outside of its pool are left out.  No page may be copied to twice, nor from and to in one pool. */
+ * n_layers - 1 of both; pairs with a page outside of its pool are left out.  No page may be copied to twice, nor from and to in one pool.  n_copies: up to 2^27, which is more than any pool has pages. */
 int iwdft_pages_copy(const iwdft_pages_desc* desc, int32_t layer, int32_t n_layers, const int32_t* d_copies, int32_t n_copies, const void* d_values,
                      const int32_t* d_exponents, int32_t to_pages, void* d_to_values, int32_t* d_to_exponents, void* hip_stream);
 

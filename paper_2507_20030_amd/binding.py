@@ -861,11 +861,11 @@ class PagedCache:
     def compact(self, n_moves: Optional[int] = None, stream=None) -> torch.Tensor:
         """Moves held pages together at the pool's beginning, n_moves of them at most (None: all that have to).  Returns the moves, int32 [n_moves, 2]."""
         self._shares()
-        n = self.values.shape[1] // 2 if n_moves is None else n_moves
+        most = self.values.shape[1] // 2
         with _on_stream(stream, self.device):
-            moves = torch.empty((n, 2), dtype=torch.int32, device=self.device)
+            moves = torch.empty((most if n_moves is None else n_moves, 2), dtype=torch.int32, device=self.device)
         iwdft_pages_compact(self.table, self.lens, self.free, self.refs, moves, self.page_tokens, stream)
-        iwdft_pages_copy(moves, self.values, self.exponents, stream=stream)
+        iwdft_pages_copy(moves[:most], self.values, self.exponents, stream=stream)  # the others are none
         return moves
 
     def repool(self, n_pages: int, stream=None) -> None:

@@ -632,6 +632,7 @@ int flush_pending(iwdft_ctx* c, hipStream_t st) {
 constexpr double kMostRows = 1 << 30;   // (token, head, layer) rows of a call: 32-bit counts
 constexpr int kMostCount = 1 << 30;     // sequences, slots
 constexpr double kMostBytes = 1e15;     // of the values
+constexpr int kMostPages = 1 << 27;     // a pool has fewer (2^31 tokens, 16 to a page), and no page is copied to twice
 const char kPageAlignMsg[] = "values and token tensors must be 16-byte aligned, exponents 8-byte, int32 arrays 4-byte";
 template <class... T>
 bool unaligned(uintptr_t n, T... p) {
@@ -1325,7 +1326,7 @@ int iwdft_pages_copy(const iwdft_pages_desc* desc, int32_t layer, int32_t n_laye
   rc = check_pages(&to, layer, n_layers);
   if (rc != IWDFT_OK) return rc;
   const Pages source = pages_of(*desc, (void*)d_values, (int32_t*)d_exponents), target = pages_of(to, d_to_values, d_to_exponents);
-  if (n_copies < 0 || 4.0 * pages_copy_units(source, n_layers, n_copies) > (double)kMostUnits) return fail(IWDFT_ERR_ARG, "n_copies = %d out of range", n_copies);
+  if (n_copies < 0 || n_copies > kMostPages) return fail(IWDFT_ERR_ARG, "n_copies = %d out of range", n_copies);
   if (n_copies == 0) return IWDFT_OK;
   if (!d_copies || !d_values || !d_exponents || !d_to_values || !d_to_exponents) return fail(IWDFT_ERR_ARG, "a device pointer is NULL");
   if (unaligned(16, d_values, d_to_values) || unaligned(8, d_copies, d_exponents, d_to_exponents)) return fail(IWDFT_ERR_ARG, "values must be 16-byte aligned, exponents and copies 8-byte");

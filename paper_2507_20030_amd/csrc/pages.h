@@ -134,7 +134,6 @@ size_t pages_compact_bytes(int n_pages);
 hipError_t launch_pages_grow(const GrowArgs& a, hipStream_t st);
 hipError_t launch_pages_fork(const ForkArgs& a, hipStream_t st);
 hipError_t launch_pages_compact(const CompactArgs& a, hipStream_t st);
-double pages_copy_units(const Pages& S, int n_layers, int n);
 hipError_t launch_pages_copy(const Pages& from, const Pages& to, int layer, int n_layers, const int32_t* copies, int n, hipStream_t st);
 
 constexpr int64_t kMostUnits = ((int64_t)1 << 26) - 4;  // waves of a launch: 2^32 threads are too many

@@ -547,9 +547,10 @@ __global__ __launch_bounds__(256) void pages_compact_table_kernel(CompactArgs a)
 typedef uint32_t uint4v __attribute__((ext_vector_type(4)));
 constexpr int64_t kCachedCopies = 256 << 20;
 template <int EACH, bool PAST>
-__global__ __launch_bounds__(256) void pages_copy_kernel(Pages from, Pages to, int layer0, int n, const int32_t* copies, int pieces) {
+__global__ __launch_bounds__(256) void pages_copy_kernel(Pages from, Pages to, int layer0, int n, const int32_t* copies, int pieces, int64_t piece0) {
   constexpr int64_t kBytes = EACH * 256 * 16;
-  const int piece = (int)(blockIdx.x % (uint32_t)pieces), rest = (int)(blockIdx.x / (uint32_t)pieces), layer = layer0 + rest / n;
+  const int64_t piece = piece0 + (int)(blockIdx.x % (uint32_t)pieces);
+  const int rest = (int)(blockIdx.x / (uint32_t)pieces), layer = layer0 + rest / n;
   const int2 c = ((const int2*)copies)[rest % n];
   if ((uint32_t)c.x >= (uint32_t)from.n_pages || (uint32_t)c.y >= (uint32_t)to.n_pages) return;
   const int64_t source = page_head(from, layer, c.x, 0), target = page_head(to, layer, c.y, 0), bytes = (int64_t)from.H << (from.logP + 8);
@@ -568,7 +569,6 @@ __global__ __launch_bounds__(256) void pages_copy_kernel(Pages from, Pages to, i
 }
 int64_t page_bytes(const Pages& S) { return (int64_t)S.H << (S.logP + 8); }
 bool copies_past(const Pages& S, int n_layers, int n) { return (double)page_bytes(S) * n_layers * n > (double)kCachedCopies; }
-int64_t copy_pieces(const Pages& S, bool past) { return (page_bytes(S) + (past ? 4095 : 8191)) / (past ? 4096 : 8192); }
 
 bool fork_in_one(int batch, int max_pages) { return (int64_t)batch * max_pages <= kSmallTable; }
 
@@ -617,14 +617,24 @@ hipError_t launch_pages_compact(const CompactArgs& a, hipStream_t st) {
   return hipGetLastError();
 }
 
-double pages_copy_units(const Pages& S, int n_layers, int n) { return (double)copy_pieces(S, copies_past(S, n_layers, n)) * n_layers * n; }
 hipError_t launch_pages_copy(const Pages& from, const Pages& to, int layer, int n_layers, const int32_t* copies, int n, hipStream_t st) {
   const bool past = copies_past(from, n_layers, n);
-  const int pieces = (int)copy_pieces(from, past);
-  const unsigned grid = (unsigned)((int64_t)pieces * n_layers * n);
-  if (past) pages_copy_kernel<1, true><<<grid, 256, 0, st>>>(from, to, layer, n, copies, pieces);
-  else pages_copy_kernel<2, false><<<grid, 256, 0, st>>>(from, to, layer, n, copies, pieces);
-  return hipGetLastError();
+  const int64_t size = past ? 4096 : 8192, pieces = (page_bytes(from) + size - 1) / size;
+  // One launch, unless that were too many threads: of 64 GB of a list's pages (cached: 128) each then.  A list is as long as it may have to be, and is never too long: tables
+  // have changed by the time it is here.
+  constexpr int64_t kMost = kMostUnits / 4;  // workgroups
+  const int64_t each_pieces = std::min(pieces, kMost), each_copies = std::min<int64_t>(n, kMost / each_pieces), each_layers = std::min<int64_t>(n_layers, kMost / (each_pieces * each_copies));
+  for (int64_t l = 0; l < n_layers; l += each_layers)
+    for (int64_t c = 0; c < n; c += each_copies)
+      for (int64_t p = 0; p < pieces; p += each_pieces) {
+        const int here = (int)std::min(pieces - p, each_pieces), some = (int)std::min<int64_t>(n - c, each_copies), layers = (int)std::min<int64_t>(n_layers - l, each_layers);
+        const unsigned grid = (unsigned)((int64_t)here * some * layers);
+        if (past) pages_copy_kernel<1, true><<<grid, 256, 0, st>>>(from, to, layer + (int)l, some, copies + 2 * c, here, p);
+        else pages_copy_kernel<2, false><<<grid, 256, 0, st>>>(from, to, layer + (int)l, some, copies + 2 * c, here, p);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+      }
+  return hipSuccess;
 }
 
 }  // namespace iwdft

@@ -746,3 +746,52 @@ def test_copy_of_more_than_the_caches_hold():
     rest = torch.ones(520, dtype=torch.bool, device=DEV)
     rest[to[there].long()] = False
     assert not other[0][:, rest].any() and not other[1][:, rest].any()
+
+
+def test_copy_of_a_list_longer_than_a_launch():
+    """More than 2^24 workgroups, most of them of pairs that are not there: pages at both ends of the list and at the borders between launches, each layer a launch of its own."""
+    values = torch.randint(0, 256, (2, 40, 8, 2, 128 * 128), dtype=torch.uint8, device=DEV)
+    exponents = torch.randint(-100, 100, (2, 40, 8, 2), dtype=torch.int32, device=DEV)
+    n = 300_000
+    pairs, ref = torch.full((n, 2), -1, dtype=torch.int32), (values.clone(), exponents.clone())
+    for i, at in enumerate((0, 1, 262_142, 262_143, 262_144, n - 1)):
+        pairs[at] = torch.tensor([i, 39 - i])
+        ref[0][:, 39 - i], ref[1][:, 39 - i] = values[:, i], exponents[:, i]
+    B.iwdft_pages_copy(pairs.to(DEV), values, exponents)
+    assert torch.equal(values, ref[0]) and torch.equal(exponents, ref[1])
+
+
+def test_a_pool_of_most_of_the_memory():
+    """130 GiB: a resize, pages moved together, 66 GiB of them into another pool."""
+    L, H, P, n_pages, held = 32, 8, 32, 66_560, 33_900
+    torch.cuda.empty_cache()
+    if torch.cuda.mem_get_info()[0] < 220 << 30:
+        pytest.skip("less than 220 GiB are free")
+    c = B.PagedCache(L, n_pages, H, H, 128, torch.bfloat16, 3, held * P, P, DEV, shared=True)
+    c.resize(ints([100 * P, (held - 2) * P, 0]), (held + 100) * P)
+    c.fork(ints([0, 1, 1]))
+    c.resize(ints([0, -1, (held - 2) * P + 1]), 1)
+    for b in (1, 2):
+        for place in (0, 77, held - 3, held - 2)[:2 + b]:
+            page = int(c.table[b, place])
+            c.values[:, page] = 16 * b + place % 16 + 1
+            c.exponents[:, page] = b + place
+    before = [[(c.values[:, p].clone(), c.exponents[:, p].clone()) for p in c.table[b, [0, 77, held - 3]].tolist()] for b in (1, 2)]
+    last = int(c.table[2, held - 2])
+    last = c.values[:, last].clone(), c.exponents[:, last].clone()
+
+    def same():
+        for b in (1, 2):
+            for p, (v, e) in zip(c.table[b, [0, 77, held - 3]].tolist(), before[b - 1]):
+                assert torch.equal(c.values[:, p], v) and torch.equal(c.exponents[:, p], e)
+        p = int(c.table[2, held - 2])
+        assert torch.equal(c.values[:, p], last[0]) and torch.equal(c.exponents[:, p], last[1]) and bool((last[0] > 32).all())
+
+    n = n_pages - int(c.free[0])
+    assert n == held - 1
+    assert int((c.compact()[:, 0] >= 0).sum()) > 0 and int(c.table[1:].max()) == n - 1
+    same()
+    c.repool(n + 3)
+    same()
+    del c
+    torch.cuda.empty_cache()

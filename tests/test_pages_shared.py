@@ -166,3 +166,22 @@ def test_a_large_calls_plan_and_workspace_serve_no_other_by_size():
             d = c_desc(n_layers=8, n_kv_heads=4, n_q_heads=32, max_pages=300, dtype=dtype)
             for a, b in (((1, 1, 1), (1, 1, 2)), ((1, 4, 9), (1, 5, 9)), ((1, 64, 64), (4, 64, 64)), ((2, 1024, 1024), (2, 1024, 5000))):
                 assert 0 < f(d, *a) <= f(d, *b)
+
+
+@pytest.mark.parametrize("layers,heads,P,pages", [(32, 8, 32, 66_560), (80, 8, 32, 27_000), (64, 32, 128, 2_100), (32, 8, 32, 143_000), (1, 1, 16, (1 << 27) - 1)])
+def test_no_list_of_a_caches_own_is_too_long_to_copy(layers, heads, P, pages):
+    """Lists that come with tables that have changed already: of a resize (1024 sequences), of a compaction, of all pages; pools of 130 GB and more.  Only the pointers are refused."""
+    lib, d = B.load_library(), ctypes.byref(c_desc(n_layers=layers, n_pages=pages, n_kv_heads=heads, n_q_heads=heads, page_tokens=P))
+    for n in (1024, pages // 2, pages):
+        assert lib.iwdft_pages_copy(d, 0, layers, None, n, None, None, pages, None, None, None) == B.IWDFT_ERR_ARG
+        assert "NULL" in B.iwdft_last_error(), (n, B.iwdft_last_error())
+
+
+def test_compact_copies_no_more_than_can_move(monkeypatch):
+    """A list longer than half of the pool, of which the rest is never anything."""
+    lengths = []
+    monkeypatch.setattr(B, "iwdft_pages_compact", lambda table, lens, free, refs, moves, *a: lengths.append(len(moves)))
+    monkeypatch.setattr(B, "iwdft_pages_copy", lambda moves, *a, **kw: lengths.append(len(moves)))
+    cache = type("cache", (), dict(refs=torch.zeros(9), table=None, lens=None, free=None, page_tokens=16, device=torch.device("cpu"), values=torch.zeros(1, 9), exponents=None,
+                                   _shares=lambda self: None))()
+    assert [len(B.PagedCache.compact(cache, n)) for n in (None, 3, 50)] == [4, 3, 50] and lengths == [4, 4, 3, 3, 50, 4]
