@@ -220,8 +220,10 @@ __device__ __forceinline__ int tokens_seen(const PlanArgs& a, int t0, int t1, in
 // One workgroup: the runs from the events, which lie in the order of their places.  Sums over 16 waves cost more than a few turns of 4: up to 256 sequences 256 threads (us with the
 // attention, 256 / 1024: 256 sequences with 16 beginnings 87 / 95, 100 nested ones 49 / 55; 1000 sequences with 40 beginnings 209 / 134).  16 sequences 7 us, 64 8.  (All three launches
 // in one, for tables of 128 pages: 29 us with the attention, 25 so; every load would wait for the one workgroup's own.)
+constexpr int kGoesBack = 1 << 30;  // more than rows; starts that ascend have no more new tokens than there are rows
 template <int THREADS, int BATCH>
 __global__ __launch_bounds__(THREADS) void plan_share_kernel(PlanArgs a) {
+  static_assert(BATCH <= THREADS, "");
   constexpr int kEvents = 3 * BATCH;  // where a set begins or ends; sequences that fork have fewer than 3 each
   __shared__ __attribute__((aligned(16))) int32_t leader[kEvents], from[kEvents];
   __shared__ int32_t news[kEvents], tiles[kEvents], least[kEvents], base[THREADS];
@@ -239,7 +241,7 @@ __global__ __launch_bounds__(THREADS) void plan_share_kernel(PlanArgs a) {
       int most = 0;
       for (int b = tid; b < a.batch; b += THREADS) {
         const News s = news_of(a, b);
-        x[1] += s.n, most = max(most, pages_of_news(a, s));
+        x[1] += a.starts[b + 1] < a.starts[b] ? kGoesBack : s.n, most = max(most, pages_of_news(a, s));  // one sequence a thread
       }
 #pragma unroll
       for (int d = 1; d < kWave; d <<= 1) most = max(most, __shfl_xor(most, d));
@@ -253,9 +255,19 @@ __global__ __launch_bounds__(THREADS) void plan_share_kernel(PlanArgs a) {
       for (int w = 0; w < THREADS / kWave; ++w) most = max(most, longest[w]);
       chunks = min(chunks, (most + kPlaces - 1) / kPlaces);
     }
-    if (c0 == 0 && all[1] > a.n_tokens) {  // starts that overlap: rows would belong to several sequences, nothing is done
-      if (tid == 0) *a.p.head = PlanHead{};
-      return;
+    if (c0 == 0 && all[1] > a.n_tokens) {  // starts that go back: where rows would belong to several sequences nothing is done
+      bool twice = false;
+      for (int b = tid; b < a.batch; b += THREADS) {
+        const News s = news_of(a, b);
+        for (int y = 0; y < b && s.n; ++y) {
+          const News o = news_of(a, y);
+          twice |= s.first < o.first + o.n && o.first < s.first + s.n && o.n;
+        }
+      }
+      if (__syncthreads_or(twice)) {
+        if (tid == 0) *a.p.head = PlanHead{};
+        return;
+      }
     }
     unshared = __syncthreads_or(mine > a.z.events) || n + all[0] > a.z.events;
     if (unshared) break;
@@ -381,6 +393,7 @@ __device__ __forceinline__ int part_slot(int4 run, int to, int runs, int part) {
 __global__ __launch_bounds__(256) void plan_rows_kernel(PlanArgs a) {
   const int lane = threadIdx.x % kWave, unit = blockIdx.x * 4 + threadIdx.x / kWave;
   const PlanHead& head = *a.p.head;
+  if (head.mark != kPlanMark) return;  // whose rows they are is not defined
   const int n = head.n_runs;
   const bool unshared = head.unshared != 0;
   const auto holds = [&](int x, const News& s, const Run& r) {

@@ -795,3 +795,34 @@ def test_a_pool_of_most_of_the_memory():
     same()
     del c
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("batch,starts", [
+    (3, [0, 4, 2, 6]), (3, [0, 2, 0, 1]), (4, [5, 8, 0, 6, 6]), (3, [4, 6, -3, 5]), (4, [0, 20, 3, 3, 5]), (70, [0] + [3, 2] * 35), (300, list(range(0, 299)) + [297, 299]),
+])
+def test_starts_that_overlap_are_found_whatever_they_add_up_to(batch, starts):
+    """Fewer new tokens than there are rows, and a row of two sequences all the same: out stays."""
+    rng = np.random.default_rng(batch)
+    pool = Pool(rng, [(-1, 0, 50)] + [(0, 48, 50 + b % 7) for b in range(1, batch)], 16, heads=1)
+    n = 400
+    q = torch.randn((1, n, 2, 128), device=DEV)
+    out = torch.full_like(q, 7.0)
+    B.iwdft_pages_attn_shared(pool.values, pool.exponents, q, plan_of(pool, starts, n, 2, "f32"), pool.d_table, out)
+    assert (out == 7.0).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("batch", [5, 69, 299])
+def test_starts_that_go_back_and_do_not_overlap(batch, dtype):
+    """Sequences whose rows lie in the other order, one without new tokens between every two of them."""
+    rng = np.random.default_rng(batch)
+    pool = Pool(rng, [(-1, 0, 50)] + [(0, 48, 50 + b % 7) for b in range(1, batch)], 16, heads=1)
+    n = 2 * batch + 3
+    starts = np.array([n - 2 * b + x for b in range(1, batch // 2 + 2) for x in (0, 2)], np.int32)[:batch + 1]
+    q = dev(rng.normal(size=(1, n, 2, 128))).to(DT[dtype])
+    out = torch.full_like(q, 7.0)
+    B.iwdft_pages_attn_shared(pool.values, pool.exponents, q, plan_of(pool, starts, n, 2, dtype), pool.d_table, out)
+    ref, *rest = pool.store.attend(f64(q), starts, pool.table, pool.lens)
+    rows = ~np.isnan(ref).all(axis=(0, 2, 3))
+    assert rows.sum() == 2 * ((batch + 1) // 2) and (out[:, ~rows] == 7.0).all()
+    near(out[:, rows], ref[:, rows], *(r[:, rows] for r in rest), dtype)
