@@ -826,3 +826,71 @@ def test_starts_that_go_back_and_do_not_overlap(batch, dtype):
     rows = ~np.isnan(ref).all(axis=(0, 2, 3))
     assert rows.sum() == 2 * ((batch + 1) // 2) and (out[:, ~rows] == 7.0).all()
     near(out[:, rows], ref[:, rows], *(r[:, rows] for r in rest), dtype)
+
+
+def events_of(table, lens, news, n_pages, P):
+    """What a plan counts: places where the set that a sequence names -- the first of those that hold the same page there -- begins, ends or changes; ends of rows do not count."""
+    pages = [-(-int(n) // P) if m else 0 for n, m in zip(lens, news)]
+    count, prev = 0, [-2] * len(lens)
+    for c in range(max(pages, default=0)):
+        first, cur = {}, []
+        for b, row in enumerate(table):
+            there = c < pages[b]
+            cur.append(first.setdefault(int(row[c]), b) if there and 0 <= row[c] < n_pages else b if there else -1)
+        changed = {x for pair in zip(cur, prev) if pair[0] != pair[1] for x in pair if x >= 0}
+        count += sum(1 for b in changed if cur[b] == b or prev[b] == b and cur[b] >= 0)
+        prev = cur
+    return count
+
+
+def head_of(plan):
+    """Runs; whether the plan gave up on sharing."""
+    head = plan.buffer[:64].view(torch.int32).tolist()
+    return head[11], head[15]
+
+
+@pytest.mark.parametrize("windows", [{}, dict(n_sink=5, n_recent=90)])
+@pytest.mark.parametrize("kind,batch", [("samples", 7), ("samples", 70), ("samples", 300), ("nested", 7), ("nested", 100), ("chain", 7), ("chain", 30), ("cut", 7), ("alone", 12)])
+def test_a_plan_shares_what_there_is(kind, batch, windows):
+    """As many runs as sets and no more: not sequence by sequence, which gives the same results."""
+    rng = np.random.default_rng(batch)
+    for P in (16, 64):
+        pool = Pool(rng, forest_of(rng, kind, batch, 320, 90), P, heads=1)
+        for news in ([1 if n else 0 for n in pool.lens], [min(int(n), b % 4) for b, n in enumerate(pool.lens)]):
+            starts = np.concatenate([[0], np.cumsum(news)])
+            runs, unshared = head_of(plan_of(pool, starts, int(starts[-1]), 2, "bf16", **windows))
+            count = events_of(pool.table, pool.lens, news, pool.n_pages, P)
+            assert not unshared and runs == count <= 3 * batch
+            if kind == "samples" and all(news):
+                assert runs == 1 + batch                       # the prompt, and what each has of its own
+            if kind == "alone" and all(news):
+                assert runs == batch
+
+
+@pytest.mark.parametrize("batch,W,n_pages", [(5, 9, 4), (40, 30, 3), (70, 12, 50), (3, 200, 2)])
+def test_a_plan_gives_up_where_there_is_no_order(batch, W, n_pages):
+    """More changes than a plan holds, and as many as it does."""
+    rng = np.random.default_rng(batch)
+    pool = Pool(rng, [(-1, 0, 16 * n_pages)], 16)
+    pool.table = rng.integers(-1, n_pages + 4, size=(batch, W)).astype(np.int32)
+    pool.lens = np.full(batch, W * 16, np.int32)
+    given_up = 0
+    for ordered in range(W, -1, -1):                            # so many places that all share
+        pool.table[:, :ordered] = pool.table[0, :ordered] = 0
+        pool.upload()
+        runs, unshared = head_of(plan_of(pool, range(batch + 1), batch, 2, "f32"))
+        count = events_of(pool.table, pool.lens, [1] * batch, pool.n_pages, 16)
+        assert unshared == (count > 3 * batch) and runs == (batch if unshared else count)
+        given_up += unshared
+        pool.table = rng.integers(-1, n_pages + 4, size=(batch, W)).astype(np.int32)
+    assert 0 < given_up <= W
+
+
+def test_all_who_share_a_page_grow_and_the_last_of_them_stays():
+    """With a page for whoever needs one; and with one too few, where a place before them takes it."""
+    for spare, lens in ((2, [17, 21, 21]), (3, [17, 21, 21]), (1, [17, 20, 20])):
+        t = Both(3, 4, 3 + spare, 16, np.random.default_rng(1))
+        t.resize([16, 20, 0], 40)
+        t.fork([0, 1, 1])
+        copies = t.resize([17, 21, 21], 40)[2]
+        assert list(t.o.lens) == lens and (copies[[0, 2]] == -1).all() and (copies[1, 0] >= 0) == (spare > 1)
