@@ -430,7 +430,9 @@ int iwdft_pages_compact_bytes(int32_t n_pages, size_t* workspace_bytes);
  * calls on it take the same descriptor, n_layers (of a call), n_tokens, batch, windows and d_table (unchanged since).  A plan for other sizes or windows leaves
  * d_out as it is, as starts that overlap do.  Any table is served; what is shared at any place of a row is found, but sequences whose pages have
  * no order in common (more than 3 * batch changes of who shares) are read one by one.  Rows, windows, refusals and accuracy as there; up to 2^28 rows (token, head, layer) a call.
- * Nothing in the workspace outlives a call; calls that may overlap in time need one each, and may share a plan. */
+ * Nothing in the workspace outlives a call; calls that may overlap in time need one each, and may share a plan.
+ * A plan has 15 bytes for each of the table's batch * max_pages entries, whatever the sequences hold, and some 0.6 KB for each new token (4 query heads to a KV head); the workspace up to 73 MB and
+ * 2 KB for each row: 8192 tokens of 32 heads 0.6 GB, 65536 4.4 GB, where iwdft_pages_attn takes 0.11.  Where little is shared that is the call to make: prompts, a few thousand tokens of a few sequences. */
 int iwdft_pages_plan(const iwdft_pages_desc* desc, int32_t n_layers, const int32_t* d_starts, int32_t n_tokens, const int32_t* d_table, const int32_t* d_lens,
                      int32_t batch, int32_t n_sink, int32_t n_recent, void* d_plan, size_t plan_bytes, void* hip_stream);
 int iwdft_pages_plan_bytes(const iwdft_pages_desc* desc, int32_t n_layers, int32_t batch, int32_t n_tokens, size_t* plan_bytes);

@@ -854,7 +854,8 @@ class PagedCache:
         iwdft_pages_fork(parent, keep, self.table, self.lens, self.free, self.refs, self.page_tokens, stream)
 
     def plan(self, starts, n_tokens: int, n_layers: int = 1, n_sink: int = 0, n_recent: int = 0, stream=None, plan: Optional[PagesPlan] = None) -> PagesPlan:
-        """Who shares what, for the step's ``attend`` calls on n_layers layers and n_tokens rows each; valid until the tables change."""
+        """Who shares what, for the step's ``attend`` calls on n_layers layers and n_tokens rows each; valid until the tables change.  With `plan`, an earlier one of these sizes
+        and windows, in its buffer; else in a new one: 15 bytes for each entry of the table and some 0.6 KB for each row."""
         L, H, G, _ = self.shape
         return iwdft_pages_plan(starts, self.table, self.lens, n_tokens, self.values.shape[1], H, G, self.page_tokens, self.dtype, n_layers, n_sink, n_recent, stream, plan)
 

@@ -46,7 +46,7 @@ struct PlanSizes {
   int places, chunks, events, chain;
   int64_t mem, items, slots;
 };
-// Rows of sums of all (layer, head) that a call has room for.
+// Rows of sums of all (layer, head) that a call has room for, four for each row and what cutting adds to few: every row goes through them, one with a single part too.
 int64_t most_slots(const Pages& S, int n_layers, int n_tokens) {
   const int64_t rows = (int64_t)n_tokens * S.G;
   return (2 * kSharedParts + 64) * std::min<int64_t>(128, (rows + 15) / 16 * 16) + 4 * rows * n_layers * S.H;
@@ -556,7 +556,7 @@ __global__ __launch_bounds__(kWaves* kWave, BF16 ? 2 : (R == 1 && !MANY ? 2 : 1)
 // sums are on their way at once.  Bound by loads that wait for each other: 480 rows of 17 parts 5.8 us (6.7 with the runs looked up for every row); beams of twenty runs, 17 MB, 9.8
 // (run by run and part by part, each rescaling the last, 15.5).
 // Few rows: a workgroup for each, its waves share the parts.  Many: a wave for each (3840 rows of 17 parts, 34 MB: 14.9 and 11.4 us; 2048 rows 7.2 and 7.9; 736 rows of beams
-// 10.3 and 20).
+// 10.3 and 20); all of these have 17 to 20 parts a row.
 constexpr int64_t kManyShared = 2048;
 template <bool BF16>
 __global__ __launch_bounds__(kWaves* kWave) void shared_join_kernel(SharedAttn s, int64_t all, int many) {

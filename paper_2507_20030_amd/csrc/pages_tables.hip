@@ -49,8 +49,9 @@ __device__ __forceinline__ int sum_before(int x, int* all, long long (*lds)[1]) 
 constexpr int kSmallTable = 8192;  // entries of a small table
 constexpr int kGiven = 4;          // entries of a thread that are given up at a time
 // One workgroup, a thread for each sequence: a chain of loads, sums and stores, 5.0 us for 16 samples that leave their shared page.  What large tables give up takes more threads
-// than they have sequences, which only wait while the others sum: 256 sequences that bring a token each 12.9 us with 256 threads, 18.4 with 1024 that all sum, 14.9 so (with the
-// slots' launch); 7840 pages given up, most of them shared, and 806 taken 51.7, 37.0, 32.0.  With atomics on refs in place of the hash table 49, in three passes over the entries 111.
+// than they have sequences, which only wait while the others sum.  With the tables' copy that comes before it in the timed step (2.2 us): 256 sequences that bring a token each 12.9 us with
+// 256 threads, 18.4 with 1024 that all sum, 14.9 so (the launch alone 10.7 and, so, 12.4); 7840 pages given up, most of them shared, and 806 taken, with the slots' launch, 51.7, 37.0, 32.0.
+// What a table could hold decides, since lengths are on the device.  With atomics on refs in place of the hash table 49, in three passes over the entries 111.
 // A sequence whose last page has room, and which others hold, leaves that page before it grows: it gets a new one and
 // an entry in copies.  Where all holders leave in this call, the last of them stays.  It is held to the pages that are left as those before it
 // are: had one of them been refused, the page would still be shared.
@@ -544,6 +545,9 @@ __global__ __launch_bounds__(256) void pages_compact_table_kernel(CompactArgs a)
 // again soon: with stores that go through the caches 33 MB (16 pages from 4, 32 layers) take 21.1 us, so 7.4.  What is read may be, by copies of the same
 // page: past the caches 33 MB take 12.7 us, and 165 MB 54 for 48.  Beyond what the last cache holds that turns: 330 MB 105 us past it in pieces of 4 KB (in pieces of
 // 8 108), 116 through it; 1.25 GB 397 and 447, 6.3 TB/s.
+// How many of a list are to be copied is on the device; a workgroup whose pair is not there ends at once, and 1000 of those take 0.37 us: 256 rows of 32 layers of 64 KB, as a step of growth
+// has them, 49 us.  2048 workgroups that read the list and take turns (4.2 us then) copy 33 MB in 9.1 us for 7.4 and 1.25 GB in 485 to 552 for 399: loads wait for older stores, and what runs
+// at a time lies apart.  Larger pieces: 16 KB 8.2 and 434, 64 KB 9.4 and 473.
 typedef uint32_t uint4v __attribute__((ext_vector_type(4)));
 constexpr int64_t kCachedCopies = 256 << 20;
 template <int EACH, bool PAST>
