@@ -624,7 +624,7 @@ hipError_t launch_pages_compact(const CompactArgs& a, hipStream_t st) {
 hipError_t launch_pages_copy(const Pages& from, const Pages& to, int layer, int n_layers, const int32_t* copies, int n, hipStream_t st) {
   const bool past = copies_past(from, n_layers, n);
   const int64_t size = past ? 4096 : 8192, pieces = (page_bytes(from) + size - 1) / size;
-  // One launch, unless that were too many threads: of 64 GB of a list's pages (cached: 128) each then.  A list is as long as it may have to be, and is never too long: tables
+  // One launch, unless that were too many threads: of 64 GiB of a list's pages each then.  A list is as long as it may have to be, and is never too long: tables
   // have changed by the time it is here.
   constexpr int64_t kMost = kMostUnits / 4;  // workgroups
   const int64_t each_pieces = std::min(pieces, kMost), each_copies = std::min<int64_t>(n, kMost / each_pieces), each_layers = std::min<int64_t>(n_layers, kMost / (each_pieces * each_copies));
